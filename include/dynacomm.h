@@ -52,7 +52,8 @@ typedef enum dc_status {
     DC_ERR_WORKSPACE = 5,  /* workspace NULL or smaller than the query returned */
     DC_ERR_CUDA = 6,       /* the CUDA runtime reported an error for a launch */
     DC_ERR_BAD_CONFIG = 7, /* a profile-generator config field is out of range */
-    DC_ERR_INTERNAL = 8    /* per instance: solver self-check failed (a bug) */
+    DC_ERR_INTERNAL = 8,   /* per instance: solver self-check failed (a bug) */
+    DC_ERR_BAD_LAYER = 9   /* a layer operator's size, stride, type or option is out of range */
 } dc_status;
 
 #define DC_L_MAX 4096
@@ -293,6 +294,135 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
                                    const int64_t *xfer, const int64_t *dt, int64_t *makespan,
                                    uint32_t *bits, int32_t *nseg, int32_t *status,
                                    cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Layer operators -- the training block of a mixture of experts, forward and
+ * backward. The costs fc and bc of Sec. IV-A are a profiler's times of a model's
+ * layers; these are layers of large language models that run on this GPU, so that such
+ * a model's costs can be measured here and scheduled. No counterpart in the paper.
+ *
+ * Conventions: device pointers, asynchronous on `stream`, no allocation, errors as
+ * above. Elements are bfloat16, IEEE half or float (DC_BF16, DC_FP16, DC_FP32) and
+ * aligned to their size; rows are contiguous, and a stride (ld...) is the distance of
+ * two rows in elements. Sums, statistics and gradients of parameters are held in 32-bit
+ * floats, and each output is rounded once. Outputs must not overlap inputs unless a
+ * call says so. No sum's order depends on timing: equal calls give equal bits.
+ * ---------------------------------------------------------------------- */
+#define DC_BF16 0
+#define DC_FP16 1
+#define DC_FP32 2
+#define DC_EXPERTS_MAX 1024
+#define DC_LAYER_DIM_MAX 1048576 /* N, K and the columns of dropout and gated units */
+#define DC_NORM_DIM_MAX 16384    /* D of the block norms: a row stays in registers */
+
+/* ------------------------------------------------------------------------
+ * dc_expert_matmul, dc_expert_matmul_grad_input, dc_expert_matmul_grad_weight --
+ * matrix products grouped by expert. Row r of x [rows][K] belongs to expert e when
+ * offsets[e] <= r < offsets[e+1] (offsets: experts + 1 device int64, in order):
+ *   y[r]  = W_e x[r]                  (y [rows][N], W_e [N][K])
+ *   dx[r] = W_e^T dy[r]
+ *   dW_e  = sum over e's rows of dy[r] x[r]^T
+ * Rows of no expert (before offsets[0] or from offsets[experts] on) get zeros in y and
+ * dx and count in no dW; an expert of no rows gets dW_e = 0. An offset outside [0, rows],
+ * or below an earlier one, counts as the nearest valid value. w and dw have the strides
+ * w_expert, w_n, w_k (elements); one of w_n and w_k is 1.
+ * 16-bit operands whose rows start on 16-byte boundaries run on the tensor cores; 2 to
+ * a few rows in all by a pass that streams the weights over every SM; others on the
+ * CUDA cores. status (device, nullable): set to DC_ERR_INTERNAL if a kernel gave up a
+ * wait (its outputs are then incomplete), else left as it is.
+ * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; rows outside [0, 2^31 - 1]; experts
+ * outside [1, DC_EXPERTS_MAX]; N or K outside [1, DC_LAYER_DIM_MAX]; a stride shorter than its
+ * row, or above 2^40); DC_ERR_CUDA.
+ * ---------------------------------------------------------------------- */
+typedef struct dc_expert_shape {
+    int32_t dtype; /* of x, y, w and their gradients */
+    int32_t experts;
+    int64_t rows;
+    int32_t N, K;
+    int64_t ldx, ldy;           /* rows of x or dx, rows of y or dy */
+    int64_t w_expert, w_n, w_k; /* w[e][n][k] or dw[e][n][k] */
+} dc_expert_shape;
+
+dc_status dc_expert_matmul(const dc_expert_shape *shape, const void *x, const void *w,
+                           const int64_t *offsets, void *y, int32_t *status, cudaStream_t stream);
+dc_status dc_expert_matmul_grad_input(const dc_expert_shape *shape, const void *dy, const void *w,
+                                      const int64_t *offsets, void *dx, int32_t *status,
+                                      cudaStream_t stream);
+dc_status dc_expert_matmul_grad_weight(const dc_expert_shape *shape, const void *dy, const void *x,
+                                       const int64_t *offsets, void *dw, int32_t *status,
+                                       cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * dc_gated_unit, dc_gated_unit_grad -- a[r][c] = act(h[r][c]) * h[r][F + c] for
+ * h [rows][2F], and from da [rows][F] the gradient dh [rows][2F] (act is evaluated again,
+ * nothing is kept). act: DC_ACT_SILU x / (1 + e^-x) or DC_ACT_GELU x Phi(x).
+ * Errors: DC_ERR_NULL, DC_ERR_BAD_LAYER, DC_ERR_CUDA.
+ * ---------------------------------------------------------------------- */
+#define DC_ACT_SILU 0
+#define DC_ACT_GELU 1
+dc_status dc_gated_unit(int32_t dtype, int32_t act, int64_t rows, int32_t F, const void *h,
+                        int64_t ldh, void *a, int64_t lda, cudaStream_t stream);
+dc_status dc_gated_unit_grad(int32_t dtype, int32_t act, int64_t rows, int32_t F, const void *da,
+                             int64_t ldda, const void *h, int64_t ldh, void *dh, int64_t lddh,
+                             cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * dc_dropout -- y = keep ? x / (1 - q) : 0, plus residual if not NULL, with a mask that
+ * is never stored: it is a function of (seed, offset, row, column), so that the same call
+ * on a gradient (without residual) is the backward pass. Column c of row r is kept when
+ * 16-bit field c % 4 (the lowest first) of SplitMix64 output number
+ *   offset + r * ceil(cols / 4) + c / 4 + 1      (state seed, as dc_profile_gen's draws)
+ * is at least t = floor(65536 p + 0.5), and q = t / 65536 is the probability in effect, so the
+ * mean is exact. p = 1 drops everything; dropped elements give 0 (or the residual)
+ * whatever they held. A call uses rows * ceil(cols / 4) draws: add that to offset for the
+ * next one. y may be x or residual themselves. Errors: DC_ERR_NULL,
+ * DC_ERR_BAD_LAYER (p outside [0, 1] or NaN, offset < 0, a size or stride), DC_ERR_CUDA.
+ * ---------------------------------------------------------------------- */
+dc_status dc_dropout(int32_t dtype, int64_t rows, int32_t cols, const void *x, int64_t ldx,
+                     const void *residual, int64_t ldr, void *y, int64_t ldy, double p,
+                     uint64_t seed, int64_t offset, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * dc_block_norm, dc_block_norm_grad -- the end of one block and the start of the next in
+ * one pass over the rows:
+ *   y = residual_scale * x + gate * drop(w_post * n(f))
+ *   h = w_pre * n(y)                                 (of y before it is rounded)
+ * n(v) = v / sqrt(mean(v^2) + eps) (DC_NORM_RMS) or the same of v - mean(v)
+ * (DC_NORM_LAYER); f is the block's output, drop the dropout of dc_dropout over
+ * [rows][D]. gate [ceil(rows / rows_per_gate)][D]: row r takes gate row
+ * r / rows_per_gate (1: one a token; >= rows: one for all). Every array is contiguous.
+ * Forms: with f NULL the call is the first norm alone (h = w_pre * n(x); y, gate and
+ * w_post not used); with h NULL it ends at y. gate, w_post and w_pre may be NULL (ones).
+ * The gradient takes dy and dh (the gradients of y and h; dy NULL: zero; dh NULL: no h), the
+ * saved y (x itself where f is NULL) and f, and writes
+ *   t = dy + n'(y)^T (dh * w_pre),  dx = residual_scale * t (t where f is NULL),  df,
+ *   dgate (of gate's type), dw_post and dw_pre (float, [D]); statistics are computed again.
+ * dgate, dw_post, dw_pre may be NULL (not wanted). workspace:
+ * dc_block_norm_grad_workspace_bytes(cfg) bytes, used during the call's kernels only.
+ * Errors: DC_ERR_NULL, DC_ERR_BAD_LAYER (dtype, kind, rows < 0 or > 2^31 - 1, D outside
+ * [1, DC_NORM_DIM_MAX], rows_per_gate < 1, eps < 0, p, offset), DC_ERR_WORKSPACE, DC_ERR_CUDA.
+ * ---------------------------------------------------------------------- */
+#define DC_NORM_RMS 0
+#define DC_NORM_LAYER 1
+typedef struct dc_block_norm_cfg {
+    int32_t dtype, kind;
+    int64_t rows;
+    int32_t D;
+    int64_t rows_per_gate;
+    double residual_scale, eps, p;
+    uint64_t seed;
+    int64_t offset;
+} dc_block_norm_cfg;
+
+dc_status dc_block_norm(const dc_block_norm_cfg *cfg, const void *x, const void *f,
+                        const void *gate, const void *w_post, const void *w_pre, void *y, void *h,
+                        cudaStream_t stream);
+size_t dc_block_norm_grad_workspace_bytes(const dc_block_norm_cfg *cfg);
+dc_status dc_block_norm_grad(const dc_block_norm_cfg *cfg, const void *dy, const void *dh,
+                             const void *y, const void *f, const void *gate, const void *w_post,
+                             const void *w_pre, void *dx, void *df, void *dgate, float *dw_post,
+                             float *dw_pre, void *workspace, size_t workspace_bytes,
+                             cudaStream_t stream);
 
 /* Static description of a status code. Never NULL. */
 const char *dc_status_string(dc_status s);

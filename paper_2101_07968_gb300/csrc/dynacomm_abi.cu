@@ -266,6 +266,7 @@ const char *dc_status_string(dc_status s)
         case DC_ERR_CUDA: return "CUDA runtime error";
         case DC_ERR_BAD_CONFIG: return "profile generator config out of range";
         case DC_ERR_INTERNAL: return "solver self-check failed";
+        case DC_ERR_BAD_LAYER: return "layer operator size, stride, type or option out of range";
     }
     return "unknown status";
 }

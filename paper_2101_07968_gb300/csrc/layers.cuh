@@ -1,0 +1,131 @@
+// Shared device and host helpers of the layer operators (expert products, block
+// norms, dropout, gated units).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "gen_device.cuh"
+
+namespace dc {
+
+template <typename T>
+__device__ __forceinline__ float to_float(T v);
+template <>
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <>
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <>
+__device__ __forceinline__ float to_float(float v) { return v; }
+
+// the one rounding of an output
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ float from_float(float v) { return v; }
+
+// V consecutive elements, moved by one load or store of V * sizeof(T) bytes
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Vec {
+    T e[V];
+};
+
+template <typename T>
+constexpr int kVec = 16 / int(sizeof(T));  // elements of a 16-byte access
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool dtype_ok(int dtype) { return dtype >= DC_BF16 && dtype <= DC_FP32; }
+inline int dtype_bytes(int dtype) { return dtype == DC_FP32 ? 4 : 2; }
+
+// Dropout: elements whose 16-bit field is at least `threshold` are kept and multiplied by
+// `scale` = 65536 / (65536 - threshold). Sixteen bits an element let one SplitMix64 draw
+// serve four: two 64-bit multiplications are what the mask costs, and one per element
+// would bound the pass by integer issue instead of memory.
+struct DropRule {
+    uint64_t seed;
+    int64_t offset;
+    uint32_t threshold;  // 0: everything is kept, no draws
+    float scale;
+};
+
+inline DropRule drop_rule(double p, uint64_t seed, int64_t offset)
+{
+    DropRule d;
+    d.seed = seed;
+    d.offset = offset;
+    d.threshold = uint32_t(p * 65536.0 + 0.5);
+    d.scale = d.threshold < 65536u ? float(65536.0 / double(65536u - d.threshold)) : 0.0f;
+    return d;
+}
+
+__device__ __forceinline__ bool kept(const DropRule &d, uint64_t draw, int field)
+{
+    return (uint32_t(draw >> (16 * field)) & 0xffffu) >= d.threshold;
+}
+
+// Runs body with T bound to the element type of `dtype`.
+#define DC_DTYPE_SWITCH(dtype, T, ...)                \
+    switch (dtype) {                                  \
+        case DC_BF16: {                               \
+            using T = __nv_bfloat16;                  \
+            __VA_ARGS__                               \
+        }                                             \
+        case DC_FP16: {                               \
+            using T = __half;                         \
+            __VA_ARGS__                               \
+        }                                             \
+        default: {                                    \
+            using T = float;                          \
+            __VA_ARGS__                               \
+        }                                             \
+    }
+
+cudaError_t sm_count(int &n);  // of the current device (layers_abi.cu)
+
+// launchers of the layer operators
+struct NormArgs {
+    const void *x, *f, *gate, *w_post, *w_pre;  // forward; x is y in the gradient
+    void *y, *h;
+    const void *dy, *dh;
+    void *dx, *df, *dgate;
+    float *dw_post, *dw_pre;
+    int64_t rows, rows_per_gate;
+    int32_t D;
+    bool layer;
+    float alpha, eps;
+    DropRule drop;
+};
+cudaError_t launch_dropout(int dtype, int64_t rows, int cols, const void *x, int64_t ldx,
+                           const void *res, int64_t ldr, void *y, int64_t ldy, const DropRule &d,
+                           cudaStream_t stream);
+cudaError_t launch_gated(int dtype, int act, int64_t rows, int F, const void *h, int64_t ldh,
+                         void *a, int64_t lda, cudaStream_t stream);
+cudaError_t launch_gated_grad(int dtype, int act, int64_t rows, int F, const void *da,
+                              int64_t ldda, const void *h, int64_t ldh, void *dh, int64_t lddh,
+                              cudaStream_t stream);
+cudaError_t launch_norm(int dtype, const NormArgs &a, cudaStream_t stream);
+size_t norm_grad_workspace(int dtype, int64_t rows, int D);
+cudaError_t launch_norm_grad(int dtype, const NormArgs &a, float *partial, cudaStream_t stream);
+
+// One product grouped by expert: C[m][n] = sum_r A[m][r] B[n][r], as strided arrays.
+// Rows (y, dx): m is a row, n a feature, B the expert's weights. Weights (dW): m, n index
+// the expert's matrix and r runs over its rows.
+struct ExpertArgs {
+    const void *a, *b;
+    void *c;
+    int64_t a_m, a_r;       // strides of A
+    int64_t b_e, b_n, b_r;  // strides of B (b_e between experts; 0 for weights)
+    int64_t c_e, c_m, c_n;  // strides of C (c_e between experts; 0 for rows)
+    const int64_t *offsets;
+    int64_t rows;
+    int32_t experts, m, n, r;  // rows: m unused; weights: r unused
+    int32_t *status;
+};
+cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
+cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, cudaStream_t stream);
+
+}  // namespace dc

@@ -25,9 +25,14 @@ CHECKED_UNITS = ("dp_deep", "dp_mid", "dp_warp", "dp_small", "dp_group", "dp_fus
 
 DC_OK, DC_ERR_NULL, DC_ERR_BAD_SHAPE, DC_ERR_NEGATIVE, DC_ERR_RANGE = 0, 1, 2, 3, 4
 DC_ERR_WORKSPACE, DC_ERR_CUDA, DC_ERR_BAD_CONFIG, DC_ERR_INTERNAL = 5, 6, 7, 8
+DC_ERR_BAD_LAYER = 9
 DC_L_MAX = 4096
 DC_STATIC_MAX_BATCH = 1048576
 FWD, BWD = 0, 1
+DC_BF16, DC_FP16, DC_FP32 = 0, 1, 2
+DC_ACT_SILU, DC_ACT_GELU = 0, 1
+DC_NORM_RMS, DC_NORM_LAYER = 0, 1
+DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX = 1024, 1048576, 16384
 
 
 class DynaCommError(RuntimeError):
@@ -52,10 +57,26 @@ class dc_profile_cfg(ctypes.Structure):
     ]
 
 
+class dc_expert_shape(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("experts", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("ldx", ctypes.c_int64),
+                ("ldy", ctypes.c_int64), ("w_expert", ctypes.c_int64), ("w_n", ctypes.c_int64),
+                ("w_k", ctypes.c_int64)]
+
+
+class dc_block_norm_cfg(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("kind", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("D", ctypes.c_int32), ("rows_per_gate", ctypes.c_int64),
+                ("residual_scale", ctypes.c_double), ("eps", ctypes.c_double),
+                ("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_int64)]
+
+
 _lib = None
 
 # name -> (restype, argtypes); the exported C ABI
 _VP, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+_F64, _U64 = ctypes.c_double, ctypes.c_uint64
+_SHAPE, _NORM = ctypes.POINTER(dc_expert_shape), ctypes.POINTER(dc_block_norm_cfg)
 _SIGNATURES = {
     "dc_profile_gen": (_I32, [ctypes.POINTER(dc_profile_cfg), _VP, _VP, _VP, _VP, _VP, _VP]),
     "dc_schedule_workspace_bytes": (_SZ, [_I64, _I32]),
@@ -80,6 +101,16 @@ _SIGNATURES = {
     "dc_status_string": (ctypes.c_char_p, [_I32]),
     "dc_roof_int_probe": (_I32, [_I32, _I32, _I32, _I64, _VP, _VP]),
     "dc_time_next_pass": (_I32, [_VP, _VP]),
+    "dc_expert_matmul": (_I32, [_SHAPE, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "dc_expert_matmul_grad_input": (_I32, [_SHAPE, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "dc_expert_matmul_grad_weight": (_I32, [_SHAPE, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "dc_gated_unit": (_I32, [_I32, _I32, _I64, _I32, _VP, _I64, _VP, _I64, _VP]),
+    "dc_gated_unit_grad": (_I32, [_I32, _I32, _I64, _I32, _VP, _I64, _VP, _I64, _VP, _I64, _VP]),
+    "dc_dropout": (_I32, [_I32, _I64, _I32, _VP, _I64, _VP, _I64, _VP, _I64, _F64, _U64, _I64,
+                          _VP]),
+    "dc_block_norm": (_I32, [_NORM, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "dc_block_norm_grad_workspace_bytes": (_SZ, [_NORM]),
+    "dc_block_norm_grad": (_I32, [_NORM] + [_VP] * 13 + [_SZ, _VP]),
 }
 
 

@@ -1,0 +1,292 @@
+"""Layer operators on torch tensors: the training block of a mixture of experts.
+
+The cost rows of a schedule are a model's measured layer times; these are layers of large
+language models, forward and backward, whose times can be measured on this GPU
+(``expert_chain`` does that and schedules the result). Every function allocates its outputs
+with torch, checks its arguments (ValueError) and launches the library's kernels on torch's
+current CUDA stream or ``stream``; nothing synchronises. A caller that uses tensors on
+another stream than their own orders the streams and keeps the tensors alive, as with any
+kernel launch.
+
+* ``expert_matmul``, ``expert_matmul_grad_input``, ``expert_matmul_grad_weight``
+* ``gated_unit``, ``gated_unit_grad``
+* ``dropout`` (its gradient is the same call on the gradient)
+* ``block_norm``, ``block_norm_grad``
+
+The operations are defined in include/dynacomm.h.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import dynacomm as dc
+
+_DTYPES = {torch.bfloat16: dc.DC_BF16, torch.float16: dc.DC_FP16, torch.float32: dc.DC_FP32}
+_ACTS = {"silu": dc.DC_ACT_SILU, "gelu": dc.DC_ACT_GELU}
+_KINDS = {"rms": dc.DC_NORM_RMS, "layer": dc.DC_NORM_LAYER}
+
+
+def _dtype(t) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"bfloat16, float16 or float32 expected, not {t.dtype}")
+    return code
+
+
+def _like(name, t, ref, shape):
+    """t has ref's type and device and the given shape."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected (the library takes device pointers)")
+    if t.dtype != ref.dtype or t.device != ref.device or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {tuple(shape)} {ref.dtype} on {ref.device} expected, not "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _rows(name, t) -> int:
+    """The stride of a [rows, columns] tensor whose rows are contiguous and apart."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected (the library takes device pointers)")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: two dimensions expected")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: contiguous rows expected")
+    if rows <= 1:
+        return cols
+    if t.stride(0) < cols:
+        raise ValueError(f"{name}: rows that do not overlap expected")
+    return t.stride(0)
+
+
+def _run(name, t, stream, *args):
+    """One call of the library on t's device."""
+    with torch.cuda.device(t.device):
+        dc._check(int(getattr(dc.lib(), name)(*args, dc._stream(stream))), name)
+
+
+# ------------------------------------------------------------------- expert products
+_status = {}
+
+
+def _status_of(device):
+    t = _status.get(device)
+    if t is None:
+        t = _status[device] = torch.zeros(1, dtype=torch.int32, device=device)
+    return t
+
+
+def check_status() -> None:
+    """Synchronises and raises DynaCommError if a kernel of this module has given up a wait
+    (a bug of the library or a fault of the machine; the call's outputs are incomplete)."""
+    for device, t in _status.items():
+        s = int(t.item())
+        if s:
+            t.zero_()
+            raise dc.DynaCommError(s, f"layer operators on {device}")
+
+
+def _weights(name, w):
+    if not w.is_cuda:
+        raise ValueError("device tensor expected (the library takes device pointers)")
+    if w.dim() != 3:
+        raise ValueError(f"{name}: [experts, N, K] expected")
+    E, N, K = w.shape
+    se, sn, sk = w.stride()
+    # a dimension of one element has no stride of its own
+    if K == 1:
+        sk = 1 if sn != 1 or N == 1 else N
+    if N == 1:
+        sn = K if sk == 1 else 1
+    if not (sk == 1 and sn >= K) and not (sn == 1 and sk >= N):
+        raise ValueError(f"{name}: N or K contiguous expected")
+    return E, N, K, (se if E > 1 else 0), sn, sk
+
+
+def _offsets(offsets, experts, ref):
+    if not offsets.is_cuda or offsets.device != ref.device or offsets.dtype != torch.int64 \
+            or offsets.dim() != 1 or offsets.numel() != experts + 1 \
+            or not offsets.is_contiguous():
+        raise ValueError(f"offsets: {experts + 1} contiguous int64 on {ref.device} expected")
+
+
+def _shape(code, E, rows, N, K, ldx, ldy, se, sn, sk):
+    return ctypes.byref(dc.dc_expert_shape(code, E, rows, N, K, ldx, ldy, se, sn, sk))
+
+
+def expert_matmul(x, w, offsets, stream=None):
+    """y [rows, N]: y[r] = w[e] @ x[r] for the expert e whose rows hold r (offsets[e] <= r <
+    offsets[e + 1], int64 [experts + 1]); zeros for rows of no expert. x [rows, K] with any row
+    stride, w [experts, N, K] with N or K contiguous."""
+    ldx = _rows("x", x)
+    E, N, K, se, sn, sk = _weights("w", w)
+    R = x.shape[0]
+    _like("x", x, w, (R, K))
+    _offsets(offsets, E, x)
+    y = torch.empty((R, N), dtype=x.dtype, device=x.device)
+    _run("dc_expert_matmul", x, stream, _shape(_dtype(x), E, R, N, K, ldx, N, se, sn, sk),
+         x.data_ptr(), w.data_ptr(), offsets.data_ptr(), y.data_ptr(),
+         _status_of(x.device).data_ptr())
+    return y
+
+
+def expert_matmul_grad_input(dy, w, offsets, stream=None):
+    """dx [rows, K] of expert_matmul from dy [rows, N]."""
+    ldy = _rows("dy", dy)
+    E, N, K, se, sn, sk = _weights("w", w)
+    R = dy.shape[0]
+    _like("dy", dy, w, (R, N))
+    _offsets(offsets, E, dy)
+    dx = torch.empty((R, K), dtype=dy.dtype, device=dy.device)
+    _run("dc_expert_matmul_grad_input", dy, stream,
+         _shape(_dtype(dy), E, R, N, K, K, ldy, se, sn, sk),
+         dy.data_ptr(), w.data_ptr(), offsets.data_ptr(), dx.data_ptr(),
+         _status_of(dy.device).data_ptr())
+    return dx
+
+
+def expert_matmul_grad_weight(dy, x, offsets, stream=None):
+    """dw [experts, N, K] of expert_matmul from dy [rows, N] and x [rows, K]; the number of
+    experts is that of offsets."""
+    ldy, ldx = _rows("dy", dy), _rows("x", x)
+    R, N = dy.shape
+    K = x.shape[1]
+    _like("x", x, dy, (R, K))
+    E = offsets.numel() - 1
+    _offsets(offsets, E, dy)
+    dw = torch.empty((E, N, K), dtype=dy.dtype, device=dy.device)
+    _run("dc_expert_matmul_grad_weight", dy, stream,
+         _shape(_dtype(dy), E, R, N, K, ldx, ldy, N * K, K, 1),
+         dy.data_ptr(), x.data_ptr(), offsets.data_ptr(), dw.data_ptr(),
+         _status_of(dy.device).data_ptr())
+    return dw
+
+
+# ------------------------------------------------------------------------ gated unit
+def _act(act) -> int:
+    if act not in _ACTS:
+        raise ValueError(f"act: one of {sorted(_ACTS)} expected")
+    return _ACTS[act]
+
+
+def gated_unit(h, act="silu", stream=None):
+    """[rows, F]: act(h[:, :F]) * h[:, F:] for h [rows, 2F]."""
+    ldh = _rows("h", h)
+    R, F2 = h.shape
+    if F2 % 2:
+        raise ValueError("h: an even number of columns expected")
+    a = torch.empty((R, F2 // 2), dtype=h.dtype, device=h.device)
+    _run("dc_gated_unit", h, stream, _dtype(h), _act(act), R, F2 // 2, h.data_ptr(), ldh,
+         a.data_ptr(), F2 // 2)
+    return a
+
+
+def gated_unit_grad(da, h, act="silu", stream=None):
+    """dh [rows, 2F] of gated_unit from da [rows, F] and h."""
+    ldh, ldda = _rows("h", h), _rows("da", da)
+    R, F2 = h.shape
+    if F2 % 2:
+        raise ValueError("h: an even number of columns expected")
+    _like("da", da, h, (R, F2 // 2))
+    dh = torch.empty((R, F2), dtype=h.dtype, device=h.device)
+    _run("dc_gated_unit_grad", h, stream, _dtype(h), _act(act), R, F2 // 2, da.data_ptr(), ldda,
+         h.data_ptr(), ldh, dh.data_ptr(), F2)
+    return dh
+
+
+# --------------------------------------------------------------------------- dropout
+def dropout_draws(rows, cols) -> int:
+    """How far one call on [rows, cols] moves the generator: add it to the next offset."""
+    return rows * ((cols + 3) // 4)
+
+
+def dropout(x, p, seed, offset=0, residual=None, stream=None):
+    """x / (1 - p) where kept, else 0, plus residual if given; the mask is a function of
+    (seed, offset, row, column) and is never stored. The gradient is the same call on dy."""
+    ldx = _rows("x", x)
+    R, C = x.shape
+    ldr, res = 0, None
+    if residual is not None:
+        ldr, res = _rows("residual", residual), residual.data_ptr()
+        _like("residual", residual, x, (R, C))
+    y = torch.empty((R, C), dtype=x.dtype, device=x.device)
+    _run("dc_dropout", x, stream, _dtype(x), R, C, x.data_ptr(), ldx, res, ldr, y.data_ptr(), C,
+         float(p), int(seed), int(offset))
+    return y
+
+
+# ----------------------------------------------------------------------- block norms
+def _norm_cfg(x, kind, rows_per_gate, residual_scale, eps, p, seed, offset):
+    if kind not in _KINDS:
+        raise ValueError(f"kind: one of {sorted(_KINDS)} expected")
+    R, D = x.shape
+    return dc.dc_block_norm_cfg(_dtype(x), _KINDS[kind], R, D, int(rows_per_gate) if rows_per_gate
+                                else max(R, 1), float(residual_scale), float(eps), float(p),
+                                int(seed), int(offset))
+
+
+def _norm_operands(x, f, gate, w_post, w_pre, rows_per_gate):
+    """Checks; the pointers of f, gate, w_post, w_pre."""
+    R, D = x.shape
+    if rows_per_gate is not None and rows_per_gate < 1:
+        raise ValueError("rows_per_gate: at least one expected")
+    gates = -(-R // rows_per_gate) if rows_per_gate else (1 if R else 0)
+    out = []
+    for name, t, shape in (("f", f, (R, D)), ("gate", gate, (gates, D)), ("w_post", w_post, (D,)),
+                           ("w_pre", w_pre, (D,))):
+        if t is not None:
+            _like(name, t, x, shape)
+        out.append(dc._ptr(t))
+    return out
+
+
+def block_norm(x, f=None, gate=None, w_post=None, w_pre=None, residual_scale=1.0, kind="rms",
+               eps=1e-6, p=0.0, seed=0, offset=0, rows_per_gate=None, want_h=True, stream=None):
+    """(y, h): y = residual_scale * x + gate * drop(w_post * n(f)) and h = w_pre * n(y), in one
+    pass. x, f [rows, D] contiguous; gate [ceil(rows / rows_per_gate), D] (rows_per_gate None:
+    one gate for all rows); w_post, w_pre [D]; any of the three None for ones. f None: the
+    first norm alone, y is x. want_h False: the last residual alone, h is None."""
+    if x.dim() != 2:
+        raise ValueError("x: two dimensions expected")
+    xp = dc._ptr(x)
+    fp, gp, pp, ep = _norm_operands(x, f, gate, w_post, w_pre, rows_per_gate)
+    if f is None and not want_h:
+        raise ValueError("f or want_h expected: there is nothing to compute")
+    cfg = _norm_cfg(x, kind, rows_per_gate, residual_scale, eps, p, seed, offset)
+    y = torch.empty_like(x) if f is not None else None
+    h = torch.empty_like(x) if want_h else None
+    _run("dc_block_norm", x, stream, ctypes.byref(cfg), xp, fp, gp, pp, ep, dc._ptr(y), dc._ptr(h))
+    return (x if y is None else y), h
+
+
+def block_norm_grad(dy, dh, y, f=None, gate=None, w_post=None, w_pre=None, residual_scale=1.0,
+                    kind="rms", eps=1e-6, p=0.0, seed=0, offset=0, rows_per_gate=None,
+                    stream=None):
+    """Gradients of block_norm as a dict: dx, df, dgate (gate's shape and type), dw_post and
+    dw_pre (float32 [D]); None for what the call did not have. dy, dh: the gradients of y and h
+    (either may be None: dy zero, dh for a call without h); y: the call's output (x where f was
+    None)."""
+    if y.dim() != 2:
+        raise ValueError("y: two dimensions expected")
+    yp = dc._ptr(y)
+    for name, t in (("dy", dy), ("dh", dh)):
+        if t is not None:
+            _like(name, t, y, y.shape)
+    if dh is None and (dy is None or f is None):
+        raise ValueError("dh expected, or dy and f")
+    fp, gp, pp, ep = _norm_operands(y, f, gate, w_post, w_pre, rows_per_gate)
+    cfg = _norm_cfg(y, kind, rows_per_gate, residual_scale, eps, p, seed, offset)
+    D, dev = y.shape[1], y.device
+    out = {"dx": torch.empty_like(y), "df": torch.empty_like(y) if f is not None else None,
+           "dgate": torch.empty_like(gate) if f is not None and gate is not None else None,
+           "dw_post": torch.empty(D, dtype=torch.float32, device=dev)
+           if f is not None and w_post is not None else None,
+           "dw_pre": torch.empty(D, dtype=torch.float32, device=dev)
+           if dh is not None and w_pre is not None else None}
+    need = int(dc.lib().dc_block_norm_grad_workspace_bytes(ctypes.byref(cfg)))
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    _run("dc_block_norm_grad", y, stream, ctypes.byref(cfg), dc._ptr(dy), dc._ptr(dh), yp, fp, gp,
+         pp, ep, dc._ptr(out["dx"]), dc._ptr(out["df"]), dc._ptr(out["dgate"]),
+         dc._ptr(out["dw_post"]), dc._ptr(out["dw_pre"]), ws.data_ptr(), need)
+    return out
