@@ -1,0 +1,452 @@
+// Expert products on the tensor cores (tcgen05), 16-bit operands.
+//
+// The feature axis is the M of a product and the rows of the batch its N, so that ragged
+// experts cost little: a tile's N is its rows rounded up to 16 (32 for a pair), where a tile
+// whose M is the rows would do 128 at a time. D[feature][row] = sum_r A[feature][r] B[row][r]:
+//   y   A = W_e (r = k contiguous)            B = x
+//   dx  A = W_e^T (features contiguous)       B = dy
+//   dW  A = dy^T, B = x^T (both with the summed axis, an expert's rows, outermost)
+// The hardware reads either order of an operand, so nothing is transposed.
+//
+// A persistent CTA (or pair of CTAs, one tile of 256 features between them) takes every
+// grid-th tile. Warp 4 copies operand blocks of 64 along the summed axis into a ring of
+// stages by TMA; a thread of warp 5 issues the products; warps 0-3 store the finished tile
+// from one half of the tensor memory while the next accumulates in the other. Rows of other
+// experts that a copy brings along end in columns that are not stored; for dW, where they
+// would be summed, warp 6 overwrites those of an expert's last block with zeros between the
+// copy's arrival and the product.
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "blackwell.cuh"
+#include "expert_rows.cuh"
+
+namespace dc {
+namespace {
+
+constexpr int kBK = 64;                  // summed axis per stage: a 128-byte line
+constexpr int kBM = 128;                 // features per CTA
+constexpr int kThreads = 7 * 32;
+constexpr uint32_t kABytes = kBM * kBK * 2;
+constexpr uint32_t kBoxBytes = 64 * kBK * 2;  // B comes in boxes of 64 rows
+constexpr int kMaxStages = 12;
+
+enum { kRowsK, kRowsMN, kWeights };  // rows with A K-major or MN-major; weights
+
+struct MmaArgs {
+    void *c;
+    int64_t c_e, c_m;   // weights: expert and row strides of dW; rows: c_m is a row's stride
+    const int64_t *offsets;
+    int64_t rows;
+    int32_t experts;
+    int32_t m, n, r;    // M extent; weights: N extent; rows: summed extent
+    int32_t *status;
+    bool wide;          // weights: 16-byte stores; rows: 4-byte stores
+};
+
+struct Tile {
+    int32_t e;      // expert
+    int32_t m0;     // first feature of the pair's or CTA's tile
+    int32_t n0;     // first row (rows) or column (weights)
+    int32_t cols;   // of them
+    int32_t r0, r;  // summed axis: start (weights) and extent
+};
+
+template <int MODE, int CG, int BN>
+__device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, int t)
+{
+    Tile q;
+    if (MODE == kWeights) {
+        const int nm = (a.m + kBM * CG - 1) / (kBM * CG), nn = (a.n + BN - 1) / BN;
+        q.e = t / (nm * nn);
+        const int i = t - q.e * (nm * nn);
+        q.m0 = (i % nm) * (kBM * CG);
+        q.n0 = (i / nm) * BN;
+        q.cols = min(BN, a.n - q.n0);
+        q.r0 = seg.start[q.e + 1];
+        q.r = seg.start[q.e + 2] - q.r0;
+    } else {
+        const int nm = (a.m + kBM * CG - 1) / (kBM * CG);
+        const int s = find_segment(seg, t);
+        const int i = t - seg.tile[s];
+        const bool none = s == 0 || s == seg.count - 1;
+        q.e = none ? 0 : s - 1;
+        q.m0 = (i % nm) * (kBM * CG);
+        q.n0 = seg.start[s] + (i / nm) * BN;
+        q.cols = min(BN, seg.start[s + 1] - q.n0);
+        q.r0 = 0;
+        q.r = none ? 0 : a.r;
+    }
+    return q;
+}
+
+template <int MODE, int CG, int BN>
+__device__ __forceinline__ int tile_count(const MmaArgs &a, const Segments &seg)
+{
+    if (MODE == kWeights)
+        return a.experts * ((a.m + kBM * CG - 1) / (kBM * CG)) * ((a.n + BN - 1) / BN);
+    return seg.tile[seg.count];
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// 32 finished columns of a lane's feature.
+template <typename T, int MODE>
+__device__ __forceinline__ void store_columns(const MmaArgs &a, const Tile &q, int feature, int c0,
+                                              const float (&v)[32])
+{
+    const int lane = threadIdx.x & 31;
+    if (MODE == kWeights) {  // the lane's row of dW, 32 columns of it
+        if (feature >= a.m) return;
+        T *p = static_cast<T *>(a.c) + q.e * a.c_e + feature * a.c_m + q.n0 + c0;
+        const int n = q.cols - c0;
+        if (a.wide && n >= 32) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+                *reinterpret_cast<uint4 *>(p + j) =
+                    make_uint4(pack2(v[j], v[j + 1], T()), pack2(v[j + 2], v[j + 3], T()),
+                               pack2(v[j + 4], v[j + 5], T()), pack2(v[j + 6], v[j + 7], T()));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < n) p[j] = from_float<T>(v[j]);
+        }
+        return;
+    }
+    const int n = q.cols - c0;
+    T *p = static_cast<T *>(a.c) + (int64_t(q.n0) + c0) * a.c_m + feature;
+    if (a.wide) {
+        // Lanes in pairs exchange a value, so that each stores two features of one row: the
+        // even lane those of row j, the odd one those of row j + 1.
+        const bool odd = lane & 1;
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float other = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+            const uint32_t w = odd ? pack2(other, v[j + 1], T()) : pack2(v[j], other, T());
+            const int row = j + odd;
+            if (row < n && feature < a.m)
+                *reinterpret_cast<uint32_t *>(p + row * a.c_m - odd) = w;
+        }
+    } else if (feature < a.m) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < n) p[j * a.c_m] = from_float<T>(v[j]);
+    }
+}
+
+template <typename T, int MODE, int CG, int BN, int STAGES>
+__global__ void __launch_bounds__(kThreads, 1)
+expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                  const MmaArgs a)
+{
+    constexpr uint32_t kBBytes = BN / CG * kBK * 2;
+    constexpr uint32_t kStage = kABytes + kBBytes;
+    constexpr uint32_t kColumns = BN * 2 < 32 ? 32 : BN * 2;
+    extern __shared__ unsigned char dyn[];
+    __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
+    __shared__ uint32_t tmem_at, gave_up;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? bw::cluster_rank() : 0;
+    const uint32_t ring = (bw::smem_addr(dyn) + 1023u) & ~1023u;
+    const Segments seg = segments_at(dyn + (ring - bw::smem_addr(dyn)) + STAGES * kStage, a.experts);
+    auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
+    auto lead = [&](uint64_t *b) { return CG == 2 ? bw::map_to(bw::smem_addr(b), 0) : bw::smem_addr(b); };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            bw::bar_init(bar(&full[i]), CG);
+            bw::bar_init(bar(&empty[i]), 1);
+            bw::bar_init(bar(&tail[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bw::bar_init(bar(&done[i]), 1);
+            bw::bar_init(bar(&free_[i]), 4 * CG);
+        }
+        gave_up = 0;
+        bw::bar_init_fence();
+    }
+    if (warp == 5) bw::tmem_alloc<CG>(bw::smem_addr(&tmem_at), kColumns);
+    if (warp == 4 && lane == 0) {
+        bw::prefetch_map(&map_a);
+        bw::prefetch_map(&map_b);
+    }
+    if (warp == 0)
+        build_segments(seg, a.offsets, a.rows, a.experts, BN, (a.m + kBM * CG - 1) / (kBM * CG));
+    bw::fence_before();
+    __syncthreads();
+    if (CG == 2) bw::cluster_sync();
+    bw::fence_after();
+    const uint32_t tmem = tmem_at;
+    const int tiles = tile_count<MODE, CG, BN>(a, seg);
+    const int step = int(gridDim.x) / CG, first = int(blockIdx.x) / CG;
+
+    if (warp == 4) {
+        if (lane == 0) {  // copies
+            int it = 0;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step) {
+                const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;  // of this CTA
+                const int boxes = (cols + 63) / 64;
+                const int m = q.m0 + int(rank) * kBM, n = q.n0 + int(rank) * cols;
+                const int blocks = (q.r + kBK - 1) / kBK;
+                for (int kb = 0; kb < blocks; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (it >= STAGES && !bw::bar_wait(bar(&empty[s]), (it / STAGES - 1) & 1, &gave_up)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
+                    const bool zeros = MODE == kWeights && kb == blocks - 1 && (q.r & 15);
+                    const uint32_t b = zeros ? bar(&tail[s]) : lead(&full[s]);
+                    bw::bar_arrive_bytes(b, kABytes + boxes * kBoxBytes);
+                    const int r = q.r0 + kb * kBK;
+                    if (MODE == kRowsK) {
+                        bw::copy_3d<CG == 2>(sa, &map_a, r, m, q.e, b);
+                    } else if (MODE == kRowsMN) {
+                        bw::copy_3d<CG == 2>(sa, &map_a, m, r, q.e, b);
+                        bw::copy_3d<CG == 2>(sa + kBoxBytes, &map_a, m + 64, r, q.e, b);
+                    } else {
+                        bw::copy_2d<CG == 2>(sa, &map_a, m, r, b);
+                        bw::copy_2d<CG == 2>(sa + kBoxBytes, &map_a, m + 64, r, b);
+                    }
+                    for (int i = 0; i < boxes; ++i)
+                        if (MODE == kWeights)
+                            bw::copy_2d<CG == 2>(sb + i * kBoxBytes, &map_b, n + 64 * i, r, b);
+                        else
+                            bw::copy_2d<CG == 2>(sb + i * kBoxBytes, &map_b, r, n + 64 * i, b);
+                }
+            }
+            // the products' arrivals land in this CTA's memory: it may not end before them
+            for (int i = it > STAGES ? it - STAGES : 0; i < it && ok; ++i)
+                ok = bw::bar_wait(bar(&empty[i % STAGES]), (i / STAGES) & 1, &gave_up);
+        }
+    } else if (warp == 5) {
+        if (lane == 0 && rank == 0) {  // products
+            int it = 0, tile = 0;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step, ++tile) {
+                const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                const uint32_t n = (q.cols + 16 * CG - 1) / (16 * CG) * (16 * CG);
+                const uint32_t shape = bw::f16_shape(std::is_same<T, __nv_bfloat16>::value, MODE != kRowsK, MODE == kWeights, kBM * CG, n);
+                const int half = tile & 1;
+                if (tile >= 2 && !bw::bar_wait(bar(&free_[half]), (tile / 2 - 1) & 1, &gave_up)) break;
+                bw::fence_after();
+                const uint32_t d = tmem + half * BN;
+                const int blocks = (q.r + kBK - 1) / kBK;
+                for (int kb = 0; kb < blocks; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (!bw::bar_wait(bar(&full[s]), (it / STAGES) & 1, &gave_up)) {
+                        ok = false;
+                        break;
+                    }
+                    bw::fence_after();
+                    const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
+                    const uint64_t da = bw::operand(sa, MODE == kRowsK ? 16 : kBoxBytes);
+                    const uint64_t db = bw::operand(sb, MODE == kWeights ? kBoxBytes : 16);
+                    const int left = q.r - kb * kBK;
+                    const int ks = left >= kBK ? kBK / 16 : (left + 15) / 16;
+#pragma unroll 4
+                    for (int i = 0; i < ks; ++i)
+                        bw::mma<CG>(d, da + i * (MODE == kRowsK ? 2 : 128), db + i * (MODE == kWeights ? 128 : 2),
+                                    shape, kb > 0 || i > 0);
+                    bw::commit<CG>(bar(&empty[s]));
+                }
+                if (ok) bw::commit<CG>(bar(&done[half]));
+            }
+        }
+    } else if (warp == 6) {
+        if (MODE == kWeights) {  // zeros after an expert's last row
+            int it = 0;
+            uint32_t uses = 0;  // parity of each stage's tail barrier
+            for (int t = first; t < tiles; t += step) {
+                const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                const int blocks = (q.r + kBK - 1) / kBK;
+                it += blocks;
+                if ((q.r & 15) == 0) continue;
+                const int s = (it - 1) % STAGES;
+                bool ok = bw::bar_wait(bar(&tail[s]), (uses >> s) & 1, &gave_up);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                uses ^= 1u << s;
+                const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;
+                const int boxes = 2 + (cols + 63) / 64;  // A's two come first
+                const int r = (q.r - 1) % kBK + 1, lines = (r + 15) / 16 * 16 - r;
+                unsigned char *at = dyn + (ring - bw::smem_addr(dyn)) + s * kStage + r * 128;
+                for (int i = lane; i < boxes * lines * 8; i += 32) {
+                    const int box = i / (lines * 8), j = i - box * (lines * 8);
+                    *reinterpret_cast<uint4 *>(at + box * kBoxBytes + j * 16) = make_uint4(0, 0, 0, 0);
+                }
+                bw::fence_async();
+                __syncwarp();
+                if (lane == 0) bw::bar_arrive(lead(&full[s]));
+            }
+        }
+    } else {  // finished tiles
+        int tile = 0;
+        for (int t = first; t < tiles; t += step, ++tile) {
+            const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+            const int half = tile & 1;
+            const bool ok = bw::bar_wait(bar(&done[half]), (tile / 2) & 1, &gave_up);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            bw::fence_after();
+            const int feature = q.m0 + int(rank) * kBM + warp * 32 + lane;
+            const uint32_t at = tmem + half * BN + (uint32_t(warp * 32) << 16);
+            float v[32];
+            for (int c0 = 0; c0 < q.cols; c0 += 32) {
+                __syncwarp();
+                if (q.r > 0) {
+                    bw::tmem_load(at + c0, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                }
+                if (c0 + 32 >= q.cols) {  // all read: the half may be overwritten
+                    bw::fence_before();
+                    __syncwarp();
+                    if (lane == 0) bw::bar_arrive(lead(&free_[half]));
+                }
+                store_columns<T, MODE>(a, q, feature, c0, v);
+            }
+        }
+    }
+    __syncwarp();
+    if (*const_cast<volatile uint32_t *>(&gave_up)) {
+        // copies and products in flight still write this CTA's memory: let them end
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (threadIdx.x == 0 && a.status) *a.status = DC_ERR_INTERNAL;
+    }
+    bw::fence_before();
+    __syncthreads();
+    if (CG == 2) bw::cluster_sync();
+    if (warp == 5) bw::tmem_free<CG>(tmem, kColumns);
+}
+
+// ------------------------------------------------------------------------------ host
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                                 const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) !=
+                cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return EncodeTiled(nullptr);
+        return EncodeTiled(p);
+    }();
+    return fn;
+}
+
+// A map of 16-bit elements [z][y][x], x contiguous, copied in boxes of 64 x `box_y`.
+bool make_map(CUtensorMap &map, bool bf16, const void *base, int64_t x, int64_t y, int64_t z,
+              int64_t stride_y, int64_t stride_z, int box_y)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)};
+    const cuuint64_t strides[2] = {cuuint64_t(stride_y) * 2, cuuint64_t(stride_z) * 2};
+    const cuuint32_t box[3] = {64, cuuint32_t(box_y), 1}, one[3] = {1, 1, 1};
+    return encode(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                  stride_z ? 3 : 2, const_cast<void *>(base), dims, strides, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int MODE, int CG, int BN, int STAGES>
+cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const MmaArgs &a,
+                         int64_t most_tiles, cudaStream_t stream)
+{
+    static_assert(STAGES <= kMaxStages, "");
+    auto kernel = expert_mma_kernel<T, MODE, CG, BN, STAGES>;
+    constexpr size_t ring = size_t(STAGES) * (kABytes + BN / CG * kBK * 2) + 1024;
+    const size_t smem = ring + segments_bytes(a.experts);
+    static DeviceCache cache;
+    int ready = 0, sms = 0;
+    cudaError_t e = cache.get(ready, [&](int &v) {
+        v = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    int(ring + segments_bytes(DC_EXPERTS_MAX)));
+    });
+    if (e == cudaSuccess) e = sm_count(sms);
+    if (e != cudaSuccess) return e;
+    int64_t units = sms / CG;
+    if (most_tiles < units) units = most_tiles;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(unsigned(units * CG));
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, kernel, ma, mb, a);
+}
+
+bool copies_ok(const void *p, int64_t stride) { return aligned16(p) && stride % 8 == 0; }
+
+}  // namespace
+
+bool expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream, cudaError_t &e)
+{
+    const bool k_major = g.b_r == 1;
+    const int64_t stride = k_major ? g.b_n : g.b_r;
+    if (dtype == DC_FP32 || !copies_ok(g.a, g.a_m) || !copies_ok(g.b, stride)) return false;
+    const int64_t inner = k_major ? g.r : g.n, outer = k_major ? g.n : g.r;
+    int64_t expert = g.b_e;
+    if (g.experts == 1) expert = stride * outer;  // not used, but it has to be valid
+    if (expert % 8) return false;
+    CUtensorMap ma, mb;
+    const bool bf16 = dtype == DC_BF16;
+    if (!make_map(ma, bf16, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
+        !make_map(mb, bf16, g.a, g.r, g.rows, 1, g.a_m, 0, 64))
+        return false;
+    MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false};
+    a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;
+    constexpr int BN = 256;
+    const int64_t tiles = (g.rows / BN + g.experts + 2) * ((g.n + 255) / 256);
+    if (bf16)
+        e = k_major ? launch_typed<__nv_bfloat16, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
+                    : launch_typed<__nv_bfloat16, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
+    else
+        e = k_major ? launch_typed<__half, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
+                    : launch_typed<__half, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
+    return true;
+}
+
+bool expert_mma_weights(int dtype, const ExpertArgs &g, cudaStream_t stream, cudaError_t &e)
+{
+    if (dtype == DC_FP32 || g.rows == 0 || !copies_ok(g.a, g.a_r) || !copies_ok(g.b, g.b_r)) return false;
+    CUtensorMap ma, mb;
+    const bool bf16 = dtype == DC_BF16;
+    if (!make_map(ma, bf16, g.a, g.m, g.rows, 1, g.a_r, 0, 64) ||
+        !make_map(mb, bf16, g.b, g.n, g.rows, 1, g.b_r, 0, 64))
+        return false;
+    MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false};
+    a.wide = g.c_m % 8 == 0 && g.c_e % 8 == 0 && aligned16(g.c);
+    constexpr int BN = 256;
+    const int64_t tiles = int64_t(g.experts) * ((g.m + 255) / 256) * ((g.n + BN - 1) / BN);
+    if (tiles > (int64_t(1) << 30)) return false;
+    e = bf16 ? launch_typed<__nv_bfloat16, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream)
+             : launch_typed<__half, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream);
+    return true;
+}
+
+}  // namespace dc

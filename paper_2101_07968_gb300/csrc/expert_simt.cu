@@ -88,6 +88,8 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g)
 
 cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, cudaStream_t stream)
 {
+    cudaError_t e = cudaSuccess;
+    if (expert_mma_rows(dtype, a, stream, e)) return e;
     // at most one short tile per segment
     const int64_t tiles = a.rows / kTile + a.experts + 2;
     const unsigned ty = unsigned(tiles < 32768 ? tiles : 32768);
@@ -100,6 +102,8 @@ cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, cudaStream_t stre
 
 cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, cudaStream_t stream)
 {
+    cudaError_t e = cudaSuccess;
+    if (expert_mma_weights(dtype, a, stream, e)) return e;
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), unsigned((a.m + kTile - 1) / kTile),
                     unsigned(a.experts));
     DC_DTYPE_SWITCH(dtype, T, {

@@ -127,5 +127,9 @@ struct ExpertArgs {
 };
 cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
 cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, cudaStream_t stream);
+// on the tensor cores (expert_mma.cu): false, and nothing launched, for operands they do
+// not take
+bool expert_mma_rows(int dtype, const ExpertArgs &a, cudaStream_t stream, cudaError_t &e);
+bool expert_mma_weights(int dtype, const ExpertArgs &a, cudaStream_t stream, cudaError_t &e);
 
 }  // namespace dc
