@@ -210,7 +210,13 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
                     const bool zeros = MODE == kWeights && kb == blocks - 1 && (q.r & 15);
                     const uint32_t b = zeros ? bar(&tail[s]) : lead(&full[s]);
-                    bw::bar_arrive_bytes(b, kABytes + boxes * kBoxBytes);
+                    const uint32_t bytes = kABytes + boxes * kBoxBytes;
+                    if (zeros) {
+                        bw::bar_arrive_bytes(b, bytes);
+                    } else if (rank == 0) {  // for both CTAs: the other's bytes count here too
+                        bw::bar_arrive_bytes(b, bytes * CG);
+                        if (CG == 2) bw::bar_arrive(b);
+                    }
                     const int r = q.r0 + kb * kBK;
                     if (MODE == kRowsK) {
                         bw::copy_3d<CG == 2>(sa, &map_a, r, m, q.e, b);
@@ -251,6 +257,8 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         ok = false;
                         break;
                     }
+                    if (CG == 2 && MODE == kWeights && kb == blocks - 1 && (q.r & 15))
+                        bw::fence_cluster();  // the other CTA's zeros
                     bw::fence_after();
                     const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
                     const uint64_t da = bw::operand(sa, MODE == kRowsK ? 16 : kBoxBytes);
@@ -289,7 +297,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
                 bw::fence_async();
                 __syncwarp();
-                if (lane == 0) bw::bar_arrive(lead(&full[s]));
+                if (lane == 0) bw::bar_arrive_cluster_release(lead(&full[s]));
             }
         }
     } else {  // finished tiles
@@ -314,7 +322,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 if (c0 + 32 >= q.cols) {  // all read: the half may be overwritten
                     bw::fence_before();
                     __syncwarp();
-                    if (lane == 0) bw::bar_arrive(lead(&free_[half]));
+                    if (lane == 0) bw::bar_arrive_cluster(lead(&free_[half]));
                 }
                 store_columns<T, MODE>(a, q, feature, c0, v);
             }
