@@ -121,6 +121,14 @@ __device__ __forceinline__ void copy_3d(uint32_t dst, const void *map, int x, in
             "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
             : "memory");
 }
+// n bytes (a multiple of 16, both addresses on 16-byte boundaries)
+__device__ __forceinline__ void copy_bytes(uint32_t dst, const void *src, uint32_t n, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+        "l"(src), "r"(n), "r"(bar)
+        : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const void *map)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");

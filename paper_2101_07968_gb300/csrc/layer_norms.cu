@@ -1,13 +1,15 @@
 // The norm after a block, its gate, dropout and scaled residual, and the norm before the
 // next block, in one pass over the rows; and the gradient of all of it.
 //
-// A team of threads (a warp, or the whole block) takes a row and keeps it in registers, 16
-// elements a thread, so every row is read once and written once: two sums over the row
-// for the root mean square norm, four for the layer norm, whose mean is taken first (sums
-// of squares of centred values lose nothing to cancellation). The gradient computes the
-// statistics again from the same rows. A team of the gradient takes a contiguous run of rows
-// and adds up the gradients of the weights and gates in registers; what several runs share
-// is written out per run and added in a fixed order by a second kernel.
+// A block takes a contiguous run of rows, one at a time, 16 elements a thread. Every row is read
+// once and written once: bulk copies bring the next rows into a ring in shared memory while
+// one is worked on, so that the latency of memory and the two sums of a row (four for the
+// layer norm, whose mean is taken first: sums of squares of centred values lose nothing to
+// cancellation) overlap. Rows that copies cannot take (off 16-byte boundaries, or too long for
+// the ring) are loaded straight into registers. The gradient computes the statistics again
+// from the same rows and adds up the gradients of weights and gates in registers; what
+// several runs share is written out per run and added in a fixed order by a second kernel.
+#include "blackwell.cuh"
 #include "layers.cuh"
 
 namespace dc {
@@ -16,16 +18,16 @@ namespace {
 constexpr int kElems = 16;  // elements of a row per thread
 // Rows above this take blocks of up to 1,024 threads, whose 64 registers each do not hold
 // the gradient's sums: they spill, which narrower rows are spared.
-constexpr int kWideD = 256 * kElems;
+constexpr int kNarrow = 256, kWideD = kNarrow * kElems;
 
 struct Team {
-    int size;  // threads of a row
-    int lane;  // this thread among them
+    int size;  // threads
+    int lane;
     int warps;
-    float *buf;  // [2][4][32] shared, one block one team (size > 32)
+    float *buf;  // [2][4][32] shared
     int phase;
 
-    // Sums of n values over the team, to every thread.
+    // Sums of n values over the block, to every thread.
     template <int N>
     __device__ __forceinline__ void sum(float (&v)[N])
     {
@@ -43,47 +45,106 @@ struct Team {
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = l < warps ? b[i * 32 + l] : 0.0f;
+        for (int i = 0; i < N; ++i) v[i] = l < warps ? b[i * 32 + l] : 0.0f;
+        for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; o > 0; o >>= 1)
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        }
+            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        // lane 0 holds the sum of lanes 0 .. warps - 1 in any case; spread it
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
     }
 };
 
-template <typename T, int V>
+// Rows on their way: A arrays' rows r, r + 1, ... in `stages` slots of shared memory. Slot
+// r % stages is filled again once every thread is past row r, which a later barrier shows.
+template <typename T, int A>
+struct Ring {
+    const T *src[A];
+    unsigned char *mem;
+    uint64_t *bars;
+    int stages, D;
+    int64_t first, end;
+
+    __device__ __forceinline__ T *at(int slot, int a) const
+    {
+        return reinterpret_cast<T *>(mem) + (int64_t(slot) * A + a) * D;
+    }
+    __device__ __forceinline__ void fetch(int64_t r)  // one thread
+    {
+        if (r >= end) return;
+        const int slot = int((r - first) % stages);
+        const uint32_t bar = bw::smem_addr(bars + slot), bytes = uint32_t(D * sizeof(T));
+        int n = 0;
+#pragma unroll
+        for (int a = 0; a < A; ++a) n += src[a] != nullptr;
+        bw::bar_arrive_bytes(bar, bytes * n);
+#pragma unroll
+        for (int a = 0; a < A; ++a)
+            if (src[a]) bw::copy_bytes(bw::smem_addr(at(slot, a)), src[a] + r * D, bytes, bar);
+    }
+    __device__ __forceinline__ void start()
+    {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < stages; ++i) bw::bar_init(bw::smem_addr(bars + i), 1);
+            bw::bar_init_fence();
+            for (int i = 0; i < stages; ++i) fetch(first + i);
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool wait(int64_t r, uint32_t *gave_up)
+    {
+        const int64_t i = r - first;
+        return bw::bar_wait(bw::smem_addr(bars + i % stages), uint32_t(i / stages) & 1u, gave_up);
+    }
+};
+constexpr int kMaxStages = 4;
+
+// A thread's 16 elements of a row: V neighbours, then the same `size` groups on. Elements
+// past D read as zero. FULL: there are none.
+template <typename T, int V, bool FULL>
 struct Row {
     static constexpr int kItems = kElems / V;
     Vec<T, V> e[kItems];
 
+    static __device__ __forceinline__ int column(int k, int lane, int size)
+    {
+        return ((k / V) * size + lane) * V + k % V;
+    }
+    static __device__ __forceinline__ bool inside(int k, int D, int lane, int size)
+    {
+        return FULL || column(k, lane, size) < D;
+    }
+    __device__ __forceinline__ void fill(float v)
+    {
+#pragma unroll
+        for (int k = 0; k < kElems; ++k) set(k, v);
+    }
     __device__ __forceinline__ void load(const T *p, int D, int lane, int size)
     {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int c = (i * size + lane) * V;
-            if (c < D)
-                e[i] = *reinterpret_cast<const Vec<T, V> *>(p + c);
+            if (inside(i * V, D, lane, size))
+                e[i] = *reinterpret_cast<const Vec<T, V> *>(p + column(i * V, lane, size));
             else
 #pragma unroll
                 for (int j = 0; j < V; ++j) e[i].e[j] = from_float<T>(0.0f);
         }
     }
-    __device__ __forceinline__ void ones()
+    __device__ __forceinline__ void load_or_ones(const void *p, int D, int lane, int size)
     {
-#pragma unroll
-        for (int i = 0; i < kItems; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) e[i].e[j] = from_float<T>(1.0f);
+        if (p)
+            load(static_cast<const T *>(p), D, lane, size);
+        else
+            fill(1.0f);
     }
     __device__ __forceinline__ float get(int k) const { return to_float(e[k / V].e[k % V]); }
     __device__ __forceinline__ void set(int k, float v) { e[k / V].e[k % V] = from_float<T>(v); }
     __device__ __forceinline__ void store(T *p, int D, int lane, int size) const
     {
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int c = (i * size + lane) * V;
-            if (c < D) *reinterpret_cast<Vec<T, V> *>(p + c) = e[i];
-        }
+        for (int i = 0; i < kItems; ++i)
+            if (inside(i * V, D, lane, size))
+                *reinterpret_cast<Vec<T, V> *>(p + column(i * V, lane, size)) = e[i];
     }
 };
 
@@ -116,38 +177,62 @@ __device__ __forceinline__ uint32_t keep_bits(const DropRule &d, int64_t row, in
     return m;
 }
 
-// Columns past D of a thread's slice (their values must not enter centred sums).
-template <int V>
-__device__ __forceinline__ bool inside(int k, int D, int lane, int size)
+// Run b of P holds rows [rows b / P, rows (b+1) / P).
+__host__ __device__ inline int64_t run_start(int64_t rows, int64_t P, int64_t b)
 {
-    return ((k / V) * size + lane) * V + k % V < D;
+    return rows * b / P;
 }
 
-template <typename T, int V, bool HAS_F, bool HAS_H, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a)
+template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool RING, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(NormArgs a, int stages)
 {
+    using R = Row<T, V, FULL>;
+    extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float buf[2 * 4 * 32];
-    const int size = blockDim.x, D = a.D;
-    Team team{size, int(threadIdx.x), size / 32, buf, 0};
-    const int lane = team.lane;
+    __shared__ alignas(8) uint64_t bars[kMaxStages];
+    __shared__ uint32_t gave_up;
+    const int size = blockDim.x, D = a.D, lane = threadIdx.x;
+    Team team{size, lane, size / 32, buf, 0};
     const float inv = 1.0f / float(D);
-    const T *xp = static_cast<const T *>(a.x);
-    const T *fp = static_cast<const T *>(a.f);
-    const T *gp = static_cast<const T *>(a.gate);
-    Row<T, V> post, pre;
-    if (a.w_post) post.load(static_cast<const T *>(a.w_post), D, lane, size); else post.ones();
-    if (a.w_pre) pre.load(static_cast<const T *>(a.w_pre), D, lane, size); else pre.ones();
-    const int64_t first = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
-    const int64_t step = int64_t(gridDim.x) * blockDim.y;
-    for (int64_t r = first; r < a.rows; r += step) {
-        Row<T, V> x;
-        x.load(xp + r * D, D, lane, size);
+    const int64_t r0 = run_start(a.rows, gridDim.x, blockIdx.x);
+    const int64_t r1 = run_start(a.rows, gridDim.x, blockIdx.x + 1);
+    const T *xp = static_cast<const T *>(a.x), *fp = static_cast<const T *>(a.f);
+    Ring<T, 2> ring{{xp, fp}, dyn, bars, stages, D, r0, r1};
+    if (RING) {
+        if (lane == 0) gave_up = 0;
+        ring.start();
+    }
+    R post, pre, gate;
+    if (HAS_F) {
+        post.load_or_ones(a.w_post, D, lane, size);
+        gate.fill(1.0f);
+    }
+    if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
+    int64_t g_end = r0;  // where the gate row in hand ends
+    for (int64_t r = r0; r < r1; ++r) {
+        if (HAS_F && a.gate && r >= g_end) {
+            const int64_t g = r / a.rows_per_gate;
+            g_end = (g + 1) * a.rows_per_gate;
+            gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
+        }
+        uint32_t keep = 0xffffffffu;
+        if (HAS_F) keep = keep_bits<V>(a.drop, r, D, lane, size);
+        R x, f;
+        const bool here = RING && ring.wait(r, &gave_up);
+        const int slot = here ? int((r - r0) % stages) : 0;
+        x.load(here ? ring.at(slot, 0) : xp + r * D, D, lane, size);
+        if (HAS_F) f.load(here ? ring.at(slot, 1) : fp + r * D, D, lane, size);
+        bool refill = RING;
+        auto taken = [&] {  // past a barrier: every thread has this row in registers
+            if (refill && lane == 0 && !gave_up) ring.fetch(r + stages);
+            refill = false;
+        };
+        if (RING && team.warps == 1) {
+            __syncwarp();
+            taken();
+        }
         float y[kElems];
         if (HAS_F) {
-            Row<T, V> f, gate;
-            f.load(fp + r * D, D, lane, size);
-            if (gp) gate.load(gp + (r / a.rows_per_gate) * D, D, lane, size); else gate.ones();
-            const uint32_t keep = keep_bits<V>(a.drop, r, D, lane, size);
             float mean = 0.0f, s[1];
             if (a.layer) {
                 s[0] = 0.0f;
@@ -160,16 +245,17 @@ __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a)
 #pragma unroll
             for (int k = 0; k < kElems; ++k) {
                 const float v = f.get(k) - mean;
-                if (inside<V>(k, D, lane, size)) s[0] += v * v;
+                if (R::inside(k, D, lane, size)) s[0] += v * v;
             }
             team.sum(s);
-            const float rstd = rsqrtf(s[0] * inv + a.eps);
+            taken();
+            const float rstd = rsqrtf(s[0] * inv + a.eps) * a.drop.scale;
 #pragma unroll
             for (int k = 0; k < kElems; ++k) {
-                const float z = (f.get(k) - mean) * rstd * post.get(k) * a.drop.scale;
+                const float z = (f.get(k) - mean) * rstd * post.get(k);
                 y[k] = a.alpha * x.get(k) + gate.get(k) * (keep >> k & 1 ? z : 0.0f);
             }
-            Row<T, V> o;
+            R o;
 #pragma unroll
             for (int k = 0; k < kElems; ++k) o.set(k, y[k]);
             o.store(static_cast<T *>(a.y) + r * D, D, lane, size);
@@ -183,7 +269,7 @@ __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a)
                 s[0] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < kElems; ++k)
-                    if (inside<V>(k, D, lane, size)) s[0] += y[k];
+                    if (R::inside(k, D, lane, size)) s[0] += y[k];
                 team.sum(s);
                 mean = s[0] * inv;
             }
@@ -191,81 +277,84 @@ __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a)
 #pragma unroll
             for (int k = 0; k < kElems; ++k) {
                 const float v = y[k] - mean;
-                if (inside<V>(k, D, lane, size)) s[0] += v * v;
+                if (R::inside(k, D, lane, size)) s[0] += v * v;
             }
             team.sum(s);
+            taken();
             const float rstd = rsqrtf(s[0] * inv + a.eps);
-            Row<T, V> o;
+            R o;
 #pragma unroll
             for (int k = 0; k < kElems; ++k) o.set(k, (y[k] - mean) * rstd * pre.get(k));
             o.store(static_cast<T *>(a.h) + r * D, D, lane, size);
         }
     }
+    if (RING && gave_up)  // a copy is late: it still writes this block's memory
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
 // ------------------------------------------------------------------------ gradient
-// Run b of P holds rows [rows b / P, rows (b+1) / P).
-__host__ __device__ inline int64_t run_start(int64_t rows, int64_t P, int64_t b)
-{
-    return rows * b / P;
-}
-
 // Per run: sums for w_post, w_pre, the gate row shared with the run before, the gate row
 // shared with the run after.
 constexpr int kSlots = 4;
 
-template <typename T, int V, bool HAS_F, bool HAS_H, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_grad_kernel(NormArgs a, float *partial, int64_t P)
+template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool RING, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : 1)
+norm_grad_kernel(NormArgs a, float *partial, int stages)
 {
+    using R = Row<T, V, FULL>;
+    extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float buf[2 * 4 * 32];
-    const int size = blockDim.x, D = a.D;
-    Team team{size, int(threadIdx.x), size / 32, buf, 0};
-    const int lane = team.lane;
+    __shared__ alignas(8) uint64_t bars[kMaxStages];
+    __shared__ uint32_t gave_up;
+    const int size = blockDim.x, D = a.D, lane = threadIdx.x;
+    Team team{size, lane, size / 32, buf, 0};
     const float inv = 1.0f / float(D);
-    const int64_t b = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
-    if (b >= P) return;  // a whole team; teams smaller than the block use no barrier
+    const int64_t b = blockIdx.x, P = gridDim.x;
     const int64_t r0 = run_start(a.rows, P, b), r1 = run_start(a.rows, P, b + 1);
-    const T *gp = static_cast<const T *>(a.gate);
-    Row<T, V> post, pre, gate;
+    const T *src[4] = {HAS_H ? static_cast<const T *>(a.x) : nullptr, static_cast<const T *>(a.dh),
+                       static_cast<const T *>(a.dy), HAS_F ? static_cast<const T *>(a.f) : nullptr};
+    Ring<T, 4> ring{{src[0], src[1], src[2], src[3]}, dyn, bars, stages, D, r0, r1};
+    if (RING) {
+        if (lane == 0) gave_up = 0;
+        ring.start();
+    }
+    R post, pre, gate;
     if (HAS_F) {
-        if (a.w_post) post.load(static_cast<const T *>(a.w_post), D, lane, size); else post.ones();
-        gate.ones();
+        post.load_or_ones(a.w_post, D, lane, size);
+        gate.fill(1.0f);
     }
-    if (HAS_H) {
-        if (a.w_pre) pre.load(static_cast<const T *>(a.w_pre), D, lane, size); else pre.ones();
-    }
+    if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
     float gpost[kElems], gpre[kElems], ggate[kElems];
 #pragma unroll
     for (int k = 0; k < kElems; ++k) gpost[k] = gpre[k] = ggate[k] = 0.0f;
     auto put = [&](float *p, const float (&v)[kElems]) {
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) {
-            const int c = ((k / V) * size + lane) * V + k % V;
-            if (c < D) p[c] = v[k];
-        }
+        for (int k = 0; k < kElems; ++k)
+            if (R::inside(k, D, lane, size)) p[R::column(k, lane, size)] = v[k];
     };
-    float *slot = partial + b * int64_t(kSlots) * D;
-    int64_t g = -1, g_end = 0;
+    float *slots = partial + b * int64_t(kSlots) * D;
+    int64_t g = 0, g_end = r0;
     for (int64_t r = r0; r < r1; ++r) {
-        if (HAS_F && (g < 0 || r == g_end)) {
+        if (HAS_F && r >= g_end) {
             g = r / a.rows_per_gate;
             g_end = (g + 1) * a.rows_per_gate;
-            if (gp) gate.load(gp + g * D, D, lane, size);
+            if (a.gate) gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
         }
-        Row<T, V> y, f, dy, dh;
-        if (HAS_H) {
-            y.load(static_cast<const T *>(a.x) + r * D, D, lane, size);
-            dh.load(static_cast<const T *>(a.dh) + r * D, D, lane, size);
-        }
-        if (HAS_F) f.load(static_cast<const T *>(a.f) + r * D, D, lane, size);
-        const bool has_dy = a.dy != nullptr;
-        if (has_dy) dy.load(static_cast<const T *>(a.dy) + r * D, D, lane, size);
         uint32_t keep = 0xffffffffu;
         if (HAS_F) keep = keep_bits<V>(a.drop, r, D, lane, size);
+        const bool here = RING && ring.wait(r, &gave_up);
+        const int slot = here ? int((r - r0) % stages) : 0;
+        auto row = [&](int i) { return here ? static_cast<const T *>(ring.at(slot, i)) : src[i] + r * D; };
+        R y, f, dy, dh;
 
         // statistics of y and f, and the sums of dn = dh * w_pre that n'(y)^T needs
         float ym = 0.0f, fm = 0.0f, dm = 0.0f;
         float s[3];
+        if (HAS_H) {
+            y.load(row(0), D, lane, size);
+            dh.load(row(1), D, lane, size);
+        }
+        if (HAS_F) f.load(row(3), D, lane, size);
         if (a.layer) {
             s[0] = s[1] = s[2] = 0.0f;
 #pragma unroll
@@ -284,7 +373,7 @@ __global__ void __launch_bounds__(MAXT) norm_grad_kernel(NormArgs a, float *part
         s[0] = s[1] = s[2] = 0.0f;
 #pragma unroll
         for (int k = 0; k < kElems; ++k) {
-            if (!inside<V>(k, D, lane, size)) continue;
+            if (!R::inside(k, D, lane, size)) continue;
             if (HAS_H) {
                 const float v = y.get(k) - ym;
                 s[0] += v * v;
@@ -296,22 +385,34 @@ __global__ void __launch_bounds__(MAXT) norm_grad_kernel(NormArgs a, float *part
             }
         }
         team.sum(s);
+        // past a barrier of this row, so every thread is done with the row before
+        if (RING) {
+            __syncwarp();
+            if (lane == 0 && r > r0 && !gave_up) ring.fetch(r - 1 + stages);
+        }
         const float yr = HAS_H ? rsqrtf(s[0] * inv + a.eps) : 0.0f;
         const float fr = HAS_F ? rsqrtf(s[1] * inv + a.eps) : 0.0f;
         const float proj = s[2] * inv * yr;  // mean of dn * yhat
 
         float t[kElems];
+        if (a.dy) {
+            dy.load(row(2), D, lane, size);
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) {
-            t[k] = has_dy ? dy.get(k) : 0.0f;
-            if (HAS_H) {
+            for (int k = 0; k < kElems; ++k) t[k] = dy.get(k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kElems; ++k) t[k] = 0.0f;
+        }
+        if (HAS_H) {
+#pragma unroll
+            for (int k = 0; k < kElems; ++k) {
                 const float yhat = (y.get(k) - ym) * yr;
                 const float d = dh.get(k);
                 t[k] += yr * (d * pre.get(k) - dm - yhat * proj);
                 gpre[k] += d * yhat;
             }
         }
-        Row<T, V> o;
+        R o;
 #pragma unroll
         for (int k = 0; k < kElems; ++k) o.set(k, a.alpha * t[k]);
         o.store(static_cast<T *>(a.dx) + r * D, D, lane, size);
@@ -323,13 +424,13 @@ __global__ void __launch_bounds__(MAXT) norm_grad_kernel(NormArgs a, float *part
             const float fhat = (f.get(k) - fm) * fr;
             const float kt = keep >> k & 1 ? t[k] * a.drop.scale : 0.0f;
             const float u = kt * gate.get(k), p = post.get(k);
-            if (inside<V>(k, D, lane, size)) {
+            t[k] = u * p;
+            if (R::inside(k, D, lane, size)) {
                 ggate[k] += kt * p * fhat;
                 gpost[k] += u * fhat;
-                s2[0] += u * p * fhat;
-                s2[1] += u * p;
+                s2[0] += t[k] * fhat;
+                s2[1] += t[k];
             }
-            t[k] = u * p;
         }
         team.sum(s2);
         const float fproj = s2[0] * inv, fdm = a.layer ? s2[1] * inv : 0.0f;
@@ -347,25 +448,27 @@ __global__ void __launch_bounds__(MAXT) norm_grad_kernel(NormArgs a, float *part
                 for (int k = 0; k < kElems; ++k) o.set(k, ggate[k]);
                 o.store(static_cast<T *>(a.dgate) + g * D, D, lane, size);
             } else {
-                put(slot + (g_start < r0 ? 2 : 3) * int64_t(D), ggate);
+                put(slots + (g_start < r0 ? 2 : 3) * int64_t(D), ggate);
             }
 #pragma unroll
             for (int k = 0; k < kElems; ++k) ggate[k] = 0.0f;
         }
     }
-    if (HAS_F && a.dw_post) put(slot, gpost);
-    if (HAS_H && a.dw_pre) put(slot + D, gpre);
+    if (HAS_F && a.dw_post) put(slots, gpost);
+    if (HAS_H && a.dw_pre) put(slots + D, gpre);
+    if (RING && gave_up)  // a copy is late: it still writes this block's memory
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
 // Adds the runs' sums: block row 0 those of the weights, block row b > 0 those of the
-// gate row that runs b - 1 and b share, if b - 1 is where it starts. Four threads a
-// column, each a quarter of the runs in order.
-constexpr int kFinishCols = 64;
+// gate row that runs b - 1 and b share, if b - 1 is where it starts. Sixteen threads a
+// column, each every sixteenth run in order.
+constexpr int kFinishCols = 32, kFinishLanes = 16;
 template <typename T>
-__global__ void __launch_bounds__(4 * kFinishCols)
+__global__ void __launch_bounds__(kFinishCols *kFinishLanes)
 norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
 {
-    __shared__ float part[2][4][kFinishCols];
+    __shared__ float part[2][kFinishLanes][kFinishCols];
     const int tx = threadIdx.x, ty = threadIdx.y;
     const int64_t c = int64_t(blockIdx.x) * kFinishCols + tx, D = a.D;
     const int64_t stride = kSlots * D;
@@ -373,11 +476,14 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
     float s0 = 0.0f, s1 = 0.0f;
     const int64_t b = blockIdx.y;
     if (b == 0) {
-        if (in)
-            for (int64_t i = ty; i < P; i += 4) {
-                if (a.dw_post) s0 += partial[i * stride + c];
-                if (a.dw_pre) s1 += partial[i * stride + D + c];
-            }
+        if (in) {
+            if (a.dw_post)
+#pragma unroll 8
+                for (int64_t i = ty; i < P; i += kFinishLanes) s0 += partial[i * stride + c];
+            if (a.dw_pre)
+#pragma unroll 8
+                for (int64_t i = ty; i < P; i += kFinishLanes) s1 += partial[i * stride + D + c];
+        }
     } else {
         const int64_t rb = run_start(a.rows, P, b);
         const int64_t g = rb / a.rows_per_gate, gs = g * a.rows_per_gate;
@@ -385,80 +491,110 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
         const int64_t ge = gs + a.rows_per_gate < a.rows ? gs + a.rows_per_gate : a.rows;
         if (in) {
             if (ty == 0) s0 = partial[(b - 1) * stride + 3 * D + c];
-            for (int64_t i = b + ty; i < P && run_start(a.rows, P, i) < ge; i += 4)
-                s0 += partial[i * stride + 2 * D + c];
+            int64_t last = b;  // runs b .. last - 1 start inside the group
+            if (ge == a.rows) {
+                last = P;
+            } else {
+                int64_t hi = P;
+                while (last < hi) {
+                    const int64_t mid = (last + hi) / 2;
+                    if (run_start(a.rows, P, mid) < ge) last = mid + 1; else hi = mid;
+                }
+            }
+#pragma unroll 8
+            for (int64_t i = b + ty; i < last; i += kFinishLanes) s0 += partial[i * stride + 2 * D + c];
         }
     }
     part[0][ty][tx] = s0;
     part[1][ty][tx] = s1;
     __syncthreads();
-    if (ty != 0 || !in) return;
-    s0 = (part[0][0][tx] + part[0][1][tx]) + (part[0][2][tx] + part[0][3][tx]);
-    s1 = (part[1][0][tx] + part[1][1][tx]) + (part[1][2][tx] + part[1][3][tx]);
+    if (ty > 1 || !in) return;
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kFinishLanes; ++i) v += part[ty][i][tx];
     if (b == 0) {
-        if (a.dw_post) a.dw_post[c] = s0;
-        if (a.dw_pre) a.dw_pre[c] = s1;
-    } else {
+        float *out = ty == 0 ? a.dw_post : a.dw_pre;
+        if (out) out[c] = v;
+    } else if (ty == 0) {
         const int64_t g = run_start(a.rows, P, b) / a.rows_per_gate;
-        static_cast<T *>(a.dgate)[g * D + c] = from_float<T>(s0);
+        static_cast<T *>(a.dgate)[g * D + c] = from_float<T>(v);
     }
 }
 
-// Threads of a row, and rows of a block: a warp per row up to 512 columns, four rows a
-// block; above, a block per row.
-dim3 team_block(int D)
+// ------------------------------------------------------------------------------ host
+int row_threads(int D) { return (D + kElems * 32 - 1) / (kElems * 32) * 32; }
+
+// Blocks an SM and slots of the ring: `threads` an SM as the registers allow, and the 224 KB
+// of shared memory shared between them; no ring (0 slots) where it would hold fewer than two rows.
+struct Plan {
+    int blocks, stages;
+    size_t smem;
+};
+Plan plan_for(int D, int arrays, int bytes, int threads)
 {
-    const int size = (D + kElems * 32 - 1) / (kElems * 32) * 32;
-    return dim3(unsigned(size), size == 32 ? 4u : 1u);
+    Plan p;
+    const int size = row_threads(D);
+    p.blocks = threads / size < 1 ? 1 : threads / size;
+    if (p.blocks > 16) p.blocks = 16;
+    const size_t row = size_t(arrays) * D * bytes, room = size_t(224) << 10;
+    while (p.blocks > 1 && room / p.blocks < 2 * row + 2048) --p.blocks;
+    p.stages = int((room / p.blocks - 2048) / row);
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    if (p.stages < 2) p.stages = 0;
+    p.smem = p.stages * row;
+    return p;
+}
+constexpr int kSms = 152;
+constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM
+
+int64_t grad_runs(int dtype, int64_t rows, int D)
+{
+    const int64_t most = int64_t(kSms) * plan_for(D, 4, dtype_bytes(dtype), kGradThreads).blocks;
+    return rows < most ? rows : most;
 }
 
-// Runs of the gradient: enough for every SM, and at least 16 rows each where there are
-// many rows (a run writes four rows of sums).
-int64_t grad_runs(int64_t rows, int D)
+template <typename T, int V, bool FULL, bool RING, int MAXT>
+cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
 {
-    const dim3 blk = team_block(D);
-    const int64_t teams = int64_t(152) * (blk.y > 1 ? 16 : D <= 4096 ? 2 : 1);
-    int64_t P = (rows + 15) / 16;
-    if (P < 152) P = rows < 152 ? rows : 152;
-    return P < teams ? P : teams;
-}
-
-template <typename T, int V, int MAXT>
-cudaError_t norm_typed(const NormArgs &a, cudaStream_t stream)
-{
-    const dim3 blk = team_block(a.D);
-    int sms = 0;
-    cudaError_t e = sm_count(sms);
-    if (e != cudaSuccess) return e;
-    int64_t grid = (a.rows + blk.y - 1) / blk.y;
-    const int64_t most = int64_t(sms) * (2048 / int(blk.x * blk.y) < 16 ? 2048 / int(blk.x * blk.y) : 16);
-    if (grid > most) grid = most;
-    if (a.f && a.h)
-        norm_kernel<T, V, true, true, MAXT><<<unsigned(grid), blk, 0, stream>>>(a);
-    else if (a.f)
-        norm_kernel<T, V, true, false, MAXT><<<unsigned(grid), blk, 0, stream>>>(a);
-    else
-        norm_kernel<T, V, false, true, MAXT><<<unsigned(grid), blk, 0, stream>>>(a);
+    auto kernel = a.f && a.h ? norm_kernel<T, V, FULL, true, true, RING, MAXT>
+                  : a.f      ? norm_kernel<T, V, FULL, true, false, RING, MAXT>
+                             : norm_kernel<T, V, FULL, false, true, RING, MAXT>;
+    static DeviceCache cache[3];
+    if (RING) {
+        int ready = 0;
+        const cudaError_t e = cache[a.f && a.h ? 0 : a.f ? 1 : 2].get(ready, [&](int &v) {
+            v = 1;
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 << 10);
+        });
+        if (e != cudaSuccess) return e;
+    }
+    const int64_t most = int64_t(kSms) * p.blocks;
+    kernel<<<unsigned(a.rows < most ? a.rows : most), unsigned(row_threads(a.D)), RING ? p.smem : 0, stream>>>(
+        a, p.stages);
     return cudaGetLastError();
 }
 
-template <typename T, int V, int MAXT>
-cudaError_t norm_grad_typed(const NormArgs &a, float *partial, cudaStream_t stream)
+template <typename T, int V, bool FULL, bool RING, int MAXT>
+cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const Plan &p,
+                             cudaStream_t stream)
 {
-    const dim3 blk = team_block(a.D);
-    const int64_t P = grad_runs(a.rows, a.D);
-    const unsigned grid = unsigned((P + blk.y - 1) / blk.y);
-    if (a.f && a.dh)
-        norm_grad_kernel<T, V, true, true, MAXT><<<grid, blk, 0, stream>>>(a, partial, P);
-    else if (a.f)
-        norm_grad_kernel<T, V, true, false, MAXT><<<grid, blk, 0, stream>>>(a, partial, P);
-    else
-        norm_grad_kernel<T, V, false, true, MAXT><<<grid, blk, 0, stream>>>(a, partial, P);
+    auto kernel = a.f && a.dh ? norm_grad_kernel<T, V, FULL, true, true, RING, MAXT>
+                  : a.f       ? norm_grad_kernel<T, V, FULL, true, false, RING, MAXT>
+                              : norm_grad_kernel<T, V, FULL, false, true, RING, MAXT>;
+    static DeviceCache cache[3];
+    if (RING) {
+        int ready = 0;
+        const cudaError_t e = cache[a.f && a.dh ? 0 : a.f ? 1 : 2].get(ready, [&](int &v) {
+            v = 1;
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 << 10);
+        });
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<unsigned(P), unsigned(row_threads(a.D)), RING ? p.smem : 0, stream>>>(a, partial, p.stages);
     const bool shared_gates = a.dgate && P > 1;
     if (a.dw_post || a.dw_pre || shared_gates) {
-        const dim3 g(unsigned((a.D + kFinishCols - 1) / kFinishCols),
-                     shared_gates ? unsigned(P) : 1u);
-        norm_finish_kernel<T><<<g, dim3(kFinishCols, 4), 0, stream>>>(a, partial, P);
+        const dim3 g(unsigned((a.D + kFinishCols - 1) / kFinishCols), shared_gates ? unsigned(P) : 1u);
+        norm_finish_kernel<T><<<g, dim3(kFinishCols, kFinishLanes), 0, stream>>>(a, partial, P);
     }
     return cudaGetLastError();
 }
@@ -476,28 +612,39 @@ bool vectors_ok(int dtype, const NormArgs &a)
 
 cudaError_t launch_norm(int dtype, const NormArgs &a, cudaStream_t stream)
 {
-    const bool vec = vectors_ok(dtype, a);
+    const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
+    const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads);
     DC_DTYPE_SWITCH(dtype, T, {
-        if (a.D <= kWideD)
-            return vec ? norm_typed<T, kVec<T>, 256>(a, stream) : norm_typed<T, 1, 256>(a, stream);
-        return vec ? norm_typed<T, kVec<T>, 1024>(a, stream) : norm_typed<T, 1, 1024>(a, stream);
+        constexpr int V = kVec<T>;
+        if (a.D > kWideD)
+            return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
+                       : norm_launch<T, 1, false, false, 1024>(a, p, stream);
+        if (!vec) return norm_launch<T, 1, false, false, kNarrow>(a, p, stream);
+        if (!p.stages) return norm_launch<T, V, false, false, kNarrow>(a, p, stream);
+        return full ? norm_launch<T, V, true, true, kNarrow>(a, p, stream)
+                    : norm_launch<T, V, false, true, kNarrow>(a, p, stream);
     })
 }
 
-size_t norm_grad_workspace(int, int64_t rows, int D)
+size_t norm_grad_workspace(int dtype, int64_t rows, int D)
 {
-    return size_t(grad_runs(rows, D)) * kSlots * size_t(D) * sizeof(float);
+    return size_t(grad_runs(dtype, rows, D)) * kSlots * size_t(D) * sizeof(float);
 }
 
 cudaError_t launch_norm_grad(int dtype, const NormArgs &a, float *partial, cudaStream_t stream)
 {
-    const bool vec = vectors_ok(dtype, a);
+    const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
+    const Plan p = plan_for(a.D, 4, dtype_bytes(dtype), kGradThreads);
+    const int64_t P = grad_runs(dtype, a.rows, a.D);
     DC_DTYPE_SWITCH(dtype, T, {
-        if (a.D <= kWideD)
-            return vec ? norm_grad_typed<T, kVec<T>, 256>(a, partial, stream)
-                       : norm_grad_typed<T, 1, 256>(a, partial, stream);
-        return vec ? norm_grad_typed<T, kVec<T>, 1024>(a, partial, stream)
-                   : norm_grad_typed<T, 1, 1024>(a, partial, stream);
+        constexpr int V = kVec<T>;
+        if (a.D > kWideD)
+            return vec ? norm_grad_launch<T, V, false, false, 1024>(a, partial, P, p, stream)
+                       : norm_grad_launch<T, 1, false, false, 1024>(a, partial, P, p, stream);
+        if (!vec) return norm_grad_launch<T, 1, false, false, kNarrow>(a, partial, P, p, stream);
+        if (!p.stages) return norm_grad_launch<T, V, false, false, kNarrow>(a, partial, P, p, stream);
+        return full ? norm_grad_launch<T, V, true, true, kNarrow>(a, partial, P, p, stream)
+                    : norm_grad_launch<T, V, false, true, kNarrow>(a, partial, P, p, stream);
     })
 }
 

@@ -77,8 +77,7 @@ dropout_rows_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr, T *y, in
     const int words = (cols + 3) / 4;
     const int w = blockIdx.y * blockDim.x + threadIdx.x;
     if (r >= rows || w >= words) return;
-    const uint64_t draw =
-        d.threshold ? splitmix(d.seed, uint64_t(d.offset + r * words + w)) : ~uint64_t(0);
+    const uint64_t draw = splitmix(d.seed, uint64_t(d.offset + r * words + w));
     T a[4], b[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

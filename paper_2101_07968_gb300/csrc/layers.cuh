@@ -62,9 +62,12 @@ inline DropRule drop_rule(double p, uint64_t seed, int64_t offset)
     return d;
 }
 
+// A field is at least `threshold` (1 .. 65536) when the word with that field on top is above
+// threshold 2^16 - 1 (the largest word for 65536, which drops all).
 __device__ __forceinline__ bool kept(const DropRule &d, uint64_t draw, int field)
 {
-    return (uint32_t(draw >> (16 * field)) & 0xffffu) >= d.threshold;
+    const uint32_t w = uint32_t(draw >> (field & 2 ? 32 : 0));
+    return d.threshold == 0 || (field & 1 ? w : w << 16) > (d.threshold << 16) - 1u;
 }
 
 // Runs body with T bound to the element type of `dtype`.
