@@ -16,6 +16,7 @@ namespace dc {
 namespace {
 
 constexpr int kElems = 16;  // elements of a row per thread
+constexpr int kPairs = kElems / 2;
 // Rows above this take blocks of up to 1,024 threads, whose 64 registers each do not hold
 // the gradient's sums: they spill, which narrower rows are spared.
 constexpr int kNarrow = 256, kWideD = kNarrow * kElems;
@@ -27,31 +28,60 @@ struct Team {
     float *buf;  // [2][4][32] shared
     int phase;
 
-    // Sums of n values over the block, to every thread.
+    // Sums of up to four values over the block, to every thread. Lanes halve the values
+    // they carry as they add: four values cost one shuffle more than one.
     template <int N>
     __device__ __forceinline__ void sum(float (&v)[N])
     {
+        static_assert(N >= 1 && N <= 4, "");
+        constexpr uint32_t kAll = 0xffffffffu;
+        const int l = lane & 31;
+        float x;
+        if (N > 2) {
+            const bool hi = l & 16;
+            const float send0 = hi ? v[0] : v[2], send1 = hi ? v[1] : (N > 3 ? v[3 % N] : 0.0f);
+            const float a0 = (hi ? v[2] : v[0]) + __shfl_xor_sync(kAll, send0, 16);
+            const float a1 = (hi ? (N > 3 ? v[3 % N] : 0.0f) : v[1]) + __shfl_xor_sync(kAll, send1, 16);
+            const bool odd = l & 8;
+            x = (odd ? a1 : a0) + __shfl_xor_sync(kAll, odd ? a0 : a1, 8);
+        } else if (N == 2) {
+            const bool hi = l & 16;
+            x = (hi ? v[1] : v[0]) + __shfl_xor_sync(kAll, hi ? v[0] : v[1], 16);
+            x += __shfl_xor_sync(kAll, x, 8);
+        } else {
+            x = v[0] + __shfl_xor_sync(kAll, v[0], 16);
+            x += __shfl_xor_sync(kAll, x, 8);
+        }
+        x += __shfl_xor_sync(kAll, x, 4);
+        x += __shfl_xor_sync(kAll, x, 2);
+        x += __shfl_xor_sync(kAll, x, 1);
+        // value i is in lanes 8 i .. 8 i + 7 (N > 2), 16 i .. (N == 2), or all
+        constexpr int kSpan = N > 2 ? 8 : N == 2 ? 16 : 32;
+        if (warps == 1) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        if (warps == 1) return;
+            for (int i = 0; i < N; ++i) v[i] = __shfl_sync(kAll, x, i * kSpan);
+            return;
+        }
         float *b = buf + phase * (4 * 32);
         phase ^= 1;
-        const int w = lane >> 5, l = lane & 31;
-        if (l == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) b[i * 32 + w] = v[i];
-        }
+        if (l % kSpan == 0 && l / kSpan < N) b[(lane >> 5) * N + l / kSpan] = x;
         __syncthreads();
+        // lane l adds the entries l, l + step, ..: step is a multiple of N, so they are all
+        // of value l % N
+        constexpr int kStep = N == 3 ? 24 : 32;
+        x = 0.0f;
+        if (l < kStep)
+            for (int i = l; i < warps * N; i += kStep) x += b[i];
+        if (N == 3) {
+            x += __shfl_down_sync(kAll, x, 12);
+            x += __shfl_down_sync(kAll, x, 6);
+            x += __shfl_down_sync(kAll, x, 3);
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = l < warps ? b[i * 32 + l] : 0.0f;
-        for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; o > 0; o >>= 1)
+            for (int o = 16; o >= N; o >>= 1) x += __shfl_down_sync(kAll, x, o);
+        }
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        // lane 0 holds the sum of lanes 0 .. warps - 1 in any case; spread it
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(kAll, x, i);
     }
 };
 
@@ -117,7 +147,7 @@ struct Row {
     __device__ __forceinline__ void fill(float v)
     {
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) set(k, v);
+        for (int i = 0; i < kPairs; ++i) set(i, twice(v));
     }
     __device__ __forceinline__ void load(const T *p, int D, int lane, int size)
     {
@@ -137,8 +167,28 @@ struct Row {
         else
             fill(1.0f);
     }
-    __device__ __forceinline__ float get(int k) const { return to_float(e[k / V].e[k % V]); }
-    __device__ __forceinline__ void set(int k, float v) { e[k / V].e[k % V] = from_float<T>(v); }
+    // pairs of elements 2 i, 2 i + 1
+    __device__ __forceinline__ float2 get(int i) const
+    {
+        if (V == 1) return make_float2(to_float(e[2 * i].e[0]), to_float(e[2 * i + 1].e[0]));
+        return pair_of(&e[2 * i / V].e[V == 1 ? 0 : 2 * i % V]);
+    }
+    __device__ __forceinline__ void set(int i, float2 v)
+    {
+        if (V == 1) {
+            e[2 * i].e[0] = from_float<T>(v.x);
+            e[2 * i + 1].e[0] = from_float<T>(v.y);
+        } else {
+            put_pair(&e[2 * i / V].e[V == 1 ? 0 : 2 * i % V], v);
+        }
+    }
+    // a pair with its elements past D at zero
+    static __device__ __forceinline__ float2 only_inside(float2 v, int i, int D, int lane, int size)
+    {
+        if (!inside(2 * i, D, lane, size)) v.x = 0.0f;
+        if (!inside(2 * i + 1, D, lane, size)) v.y = 0.0f;
+        return v;
+    }
     __device__ __forceinline__ void store(T *p, int D, int lane, int size) const
     {
 #pragma unroll
@@ -148,33 +198,34 @@ struct Row {
     }
 };
 
-// Bit k: this thread's element k is kept.
+// Zeros in place of this thread's dropped elements of row `row`.
 template <int V>
-__device__ __forceinline__ uint32_t keep_bits(const DropRule &d, int64_t row, int D, int lane,
-                                              int size)
+__device__ __forceinline__ void drop_row(const DropRule &d, float2 (&v)[kPairs], int64_t row, int D,
+                                         int lane, int size)
 {
-    if (d.threshold == 0) return 0xffffffffu;
-    const int64_t base = d.offset + row * ((D + 3) / 4);
-    uint32_t m = 0;
+    if (d.threshold == 0) return;
+    const uint32_t limit = (d.threshold << 16) - 1u;  // see kept()
+    const uint64_t z0 = d.seed + (uint64_t(d.offset + row * ((D + 3) / 4)) + 1u) * kGamma;
+    if (V >= 4) {
+        const uint64_t z1 = z0 + uint64_t(lane * (V / 4)) * kGamma;
+        const uint64_t step = uint64_t(size * (V / 4)) * kGamma;
 #pragma unroll
-    for (int i = 0; i < kElems / V; ++i) {
-        const int c = (i * size + lane) * V;
-        if (V >= 4) {
+        for (int k = 0; k < kElems; k += 4) {
+            const uint64_t w = splitmix_output(z1 + (k / V) * step + (k % V / 4) * kGamma);
+            const uint32_t lo = uint32_t(w), hi = uint32_t(w >> 32);
+            if (!(lo << 16 > limit)) v[k / 2].x = 0.0f;
+            if (!(lo > limit)) v[k / 2].y = 0.0f;
+            if (!(hi << 16 > limit)) v[k / 2 + 1].x = 0.0f;
+            if (!(hi > limit)) v[k / 2 + 1].y = 0.0f;
+        }
+    } else {
 #pragma unroll
-            for (int q = 0; q < (V >= 4 ? V / 4 : 1); ++q) {
-                const uint64_t draw = splitmix(d.seed, uint64_t(base + c / 4 + q));
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (kept(d, draw, j)) m |= 1u << (i * V + q * 4 + j);
-            }
-        } else {
-            const uint64_t draw = splitmix(d.seed, uint64_t(base + c / 4));
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (kept(d, draw, (c + j) & 3)) m |= 1u << (i * V + j);
+        for (int k = 0; k < kElems; ++k) {
+            const int c = Row<float, V, false>::column(k, lane, size);
+            const uint64_t w = splitmix_output(z0 + uint64_t(c / 4) * kGamma);
+            if (!kept(d, w, c & 3)) (k & 1 ? v[k / 2].y : v[k / 2].x) = 0.0f;
         }
     }
-    return m;
 }
 
 // Run b of P holds rows [rows b / P, rows (b+1) / P).
@@ -215,8 +266,6 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             g_end = (g + 1) * a.rows_per_gate;
             gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
         }
-        uint32_t keep = 0xffffffffu;
-        if (HAS_F) keep = keep_bits<V>(a.drop, r, D, lane, size);
         R x, f;
         const bool here = RING && ring.wait(r, &gave_up);
         const int slot = here ? int((r - r0) % stages) : 0;
@@ -231,60 +280,52 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             __syncwarp();
             taken();
         }
-        float y[kElems];
-        if (HAS_F) {
-            float mean = 0.0f, s[1];
+        float2 y[kPairs];
+        auto centre = [&] {  // y - mean, and the reciprocal root of its mean square
+            float s[1];
             if (a.layer) {
-                s[0] = 0.0f;
+                float2 q = twice(0.0f);
 #pragma unroll
-                for (int k = 0; k < kElems; ++k) s[0] += f.get(k);
+                for (int i = 0; i < kPairs; ++i) q = __fadd2_rn(q, y[i]);
+                s[0] = q.x + q.y;
                 team.sum(s);
-                mean = s[0] * inv;
-            }
-            s[0] = 0.0f;
+                taken();
+                const float2 mean = twice(-s[0] * inv);
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) {
-                const float v = f.get(k) - mean;
-                if (R::inside(k, D, lane, size)) s[0] += v * v;
+                for (int i = 0; i < kPairs; ++i)
+                    y[i] = R::only_inside(__fadd2_rn(y[i], mean), i, D, lane, size);
             }
+            float2 q = twice(0.0f);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) q = __ffma2_rn(y[i], y[i], q);
+            s[0] = q.x + q.y;
             team.sum(s);
             taken();
-            const float rstd = rsqrtf(s[0] * inv + a.eps) * a.drop.scale;
+            return rsqrtf(s[0] * inv + a.eps);
+        };
+        if (HAS_F) {
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) {
-                const float z = (f.get(k) - mean) * rstd * post.get(k);
-                y[k] = a.alpha * x.get(k) + gate.get(k) * (keep >> k & 1 ? z : 0.0f);
-            }
+            for (int i = 0; i < kPairs; ++i) y[i] = f.get(i);
+            const float2 rstd = twice(centre() * a.drop.scale), alpha = twice(a.alpha);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) y[i] = __fmul2_rn(__fmul2_rn(y[i], rstd), post.get(i));
+            drop_row<V>(a.drop, y, r, D, lane, size);
             R o;
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) o.set(k, y[k]);
+            for (int i = 0; i < kPairs; ++i) {
+                y[i] = __ffma2_rn(gate.get(i), y[i], __fmul2_rn(alpha, x.get(i)));
+                o.set(i, y[i]);
+            }
             o.store(static_cast<T *>(a.y) + r * D, D, lane, size);
         } else {
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) y[k] = x.get(k);
+            for (int i = 0; i < kPairs; ++i) y[i] = x.get(i);
         }
         if (HAS_H) {
-            float mean = 0.0f, s[1];
-            if (a.layer) {
-                s[0] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < kElems; ++k)
-                    if (R::inside(k, D, lane, size)) s[0] += y[k];
-                team.sum(s);
-                mean = s[0] * inv;
-            }
-            s[0] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kElems; ++k) {
-                const float v = y[k] - mean;
-                if (R::inside(k, D, lane, size)) s[0] += v * v;
-            }
-            team.sum(s);
-            taken();
-            const float rstd = rsqrtf(s[0] * inv + a.eps);
+            const float2 rstd = twice(centre());
             R o;
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) o.set(k, (y[k] - mean) * rstd * pre.get(k));
+            for (int i = 0; i < kPairs; ++i) o.set(i, __fmul2_rn(__fmul2_rn(y[i], rstd), pre.get(i)));
             o.store(static_cast<T *>(a.h) + r * D, D, lane, size);
         }
     }
@@ -324,13 +365,15 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         gate.fill(1.0f);
     }
     if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
-    float gpost[kElems], gpre[kElems], ggate[kElems];
+    float2 gpost[kPairs], gpre[kPairs], ggate[kPairs];
 #pragma unroll
-    for (int k = 0; k < kElems; ++k) gpost[k] = gpre[k] = ggate[k] = 0.0f;
-    auto put = [&](float *p, const float (&v)[kElems]) {
+    for (int i = 0; i < kPairs; ++i) gpost[i] = gpre[i] = ggate[i] = twice(0.0f);
+    auto put = [&](float *p, const float2 (&v)[kPairs]) {
 #pragma unroll
-        for (int k = 0; k < kElems; ++k)
-            if (R::inside(k, D, lane, size)) p[R::column(k, lane, size)] = v[k];
+        for (int i = 0; i < kPairs; ++i) {
+            if (R::inside(2 * i, D, lane, size)) p[R::column(2 * i, lane, size)] = v[i].x;
+            if (R::inside(2 * i + 1, D, lane, size)) p[R::column(2 * i + 1, lane, size)] = v[i].y;
+        }
     };
     float *slots = partial + b * int64_t(kSlots) * D;
     int64_t g = 0, g_end = r0;
@@ -340,103 +383,125 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             g_end = (g + 1) * a.rows_per_gate;
             if (a.gate) gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
         }
-        uint32_t keep = 0xffffffffu;
-        if (HAS_F) keep = keep_bits<V>(a.drop, r, D, lane, size);
         const bool here = RING && ring.wait(r, &gave_up);
         const int slot = here ? int((r - r0) % stages) : 0;
         auto row = [&](int i) { return here ? static_cast<const T *>(ring.at(slot, i)) : src[i] + r * D; };
-        R y, f, dy, dh;
+        R y, f, dh;
+
+        // Read again from the ring in each phase: the sums take most of the registers, and
+        // rows held over the barriers would spill.
+        auto reload = [&](bool with_y) {
+            if (!RING) return;
+            asm volatile("" ::: "memory");
+            if (HAS_H && with_y) {
+                y.load(row(0), D, lane, size);
+                dh.load(row(1), D, lane, size);
+            }
+            if (HAS_F) f.load(row(3), D, lane, size);
+        };
 
         // statistics of y and f, and the sums of dn = dh * w_pre that n'(y)^T needs
-        float ym = 0.0f, fm = 0.0f, dm = 0.0f;
+        float2 ym = twice(0.0f), fm = twice(0.0f), dm = twice(0.0f);  // minus the means
         float s[3];
         if (HAS_H) {
             y.load(row(0), D, lane, size);
             dh.load(row(1), D, lane, size);
         }
         if (HAS_F) f.load(row(3), D, lane, size);
-        if (a.layer) {
-            s[0] = s[1] = s[2] = 0.0f;
+        float2 q[3];
+        auto fold = [&] {
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) {
-                if (HAS_H) {
-                    s[0] += y.get(k);
-                    s[2] += dh.get(k) * pre.get(k);
-                }
-                if (HAS_F) s[1] += f.get(k);
-            }
+            for (int i = 0; i < 3; ++i) s[i] = q[i].x + q[i].y;
             team.sum(s);
-            ym = s[0] * inv;
-            fm = s[1] * inv;
-            dm = s[2] * inv;
-        }
-        s[0] = s[1] = s[2] = 0.0f;
+        };
+        if (a.layer) {
+            q[0] = q[1] = q[2] = twice(0.0f);
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) {
-            if (!R::inside(k, D, lane, size)) continue;
+            for (int i = 0; i < kPairs; ++i) {
+                if (HAS_H) {
+                    q[0] = __fadd2_rn(q[0], y.get(i));
+                    q[2] = __ffma2_rn(dh.get(i), pre.get(i), q[2]);
+                }
+                if (HAS_F) q[1] = __fadd2_rn(q[1], f.get(i));
+            }
+            fold();
+            ym = twice(-s[0] * inv);
+            fm = twice(-s[1] * inv);
+            dm = twice(-s[2] * inv);
+            reload(true);
+        }
+        q[0] = q[1] = q[2] = twice(0.0f);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
             if (HAS_H) {
-                const float v = y.get(k) - ym;
-                s[0] += v * v;
-                s[2] += dh.get(k) * pre.get(k) * v;
+                const float2 v = R::only_inside(__fadd2_rn(y.get(i), ym), i, D, lane, size);
+                q[0] = __ffma2_rn(v, v, q[0]);
+                q[2] = __ffma2_rn(__fmul2_rn(dh.get(i), pre.get(i)), v, q[2]);
             }
             if (HAS_F) {
-                const float v = f.get(k) - fm;
-                s[1] += v * v;
+                const float2 v = R::only_inside(__fadd2_rn(f.get(i), fm), i, D, lane, size);
+                q[1] = __ffma2_rn(v, v, q[1]);
             }
         }
-        team.sum(s);
-        // past a barrier of this row, so every thread is done with the row before
-        if (RING) {
+        fold();
+        if (RING) {  // past a barrier of this row, so every thread is done with the row before
             __syncwarp();
             if (lane == 0 && r > r0 && !gave_up) ring.fetch(r - 1 + stages);
         }
-        const float yr = HAS_H ? rsqrtf(s[0] * inv + a.eps) : 0.0f;
-        const float fr = HAS_F ? rsqrtf(s[1] * inv + a.eps) : 0.0f;
-        const float proj = s[2] * inv * yr;  // mean of dn * yhat
+        const float yr1 = HAS_H ? rsqrtf(s[0] * inv + a.eps) : 0.0f;
+        const float fr1 = HAS_F ? rsqrtf(s[1] * inv + a.eps) : 0.0f;
+        const float2 yr = twice(yr1), fr = twice(fr1);
+        const float2 proj = twice(-(s[2] * inv * yr1));  // minus the mean of dn * yhat
 
-        float t[kElems];
+        reload(true);
+        float2 t[kPairs];
         if (a.dy) {
+            R dy;
             dy.load(row(2), D, lane, size);
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) t[k] = dy.get(k);
+            for (int i = 0; i < kPairs; ++i) t[i] = dy.get(i);
         } else {
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) t[k] = 0.0f;
+            for (int i = 0; i < kPairs; ++i) t[i] = twice(0.0f);
         }
         if (HAS_H) {
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) {
-                const float yhat = (y.get(k) - ym) * yr;
-                const float d = dh.get(k);
-                t[k] += yr * (d * pre.get(k) - dm - yhat * proj);
-                gpre[k] += d * yhat;
+            for (int i = 0; i < kPairs; ++i) {
+                const float2 yhat = __fmul2_rn(__fadd2_rn(y.get(i), ym), yr), d = dh.get(i);
+                t[i] = __ffma2_rn(yr, __ffma2_rn(yhat, proj, __ffma2_rn(d, pre.get(i), dm)), t[i]);
+                gpre[i] = __ffma2_rn(d, yhat, gpre[i]);
             }
         }
         R o;
+        const float2 alpha = twice(a.alpha);
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) o.set(k, a.alpha * t[k]);
+        for (int i = 0; i < kPairs; ++i) o.set(i, __fmul2_rn(alpha, t[i]));
         o.store(static_cast<T *>(a.dx) + r * D, D, lane, size);
         if (!HAS_F) continue;
 
-        float s2[2] = {0.0f, 0.0f};
+        drop_row<V>(a.drop, t, r, D, lane, size);
+        const float2 scale = twice(a.drop.scale);
+        float2 s2[2] = {twice(0.0f), twice(0.0f)};
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) {
-            const float fhat = (f.get(k) - fm) * fr;
-            const float kt = keep >> k & 1 ? t[k] * a.drop.scale : 0.0f;
-            const float u = kt * gate.get(k), p = post.get(k);
-            t[k] = u * p;
-            if (R::inside(k, D, lane, size)) {
-                ggate[k] += kt * p * fhat;
-                gpost[k] += u * fhat;
-                s2[0] += t[k] * fhat;
-                s2[1] += t[k];
-            }
+        for (int i = 0; i < kPairs; ++i) {
+            const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
+            const float2 kt = R::only_inside(__fmul2_rn(t[i], scale), i, D, lane, size);
+            const float2 u = __fmul2_rn(kt, gate.get(i)), p = post.get(i);
+            t[i] = __fmul2_rn(u, p);
+            ggate[i] = __ffma2_rn(__fmul2_rn(kt, p), fhat, ggate[i]);
+            gpost[i] = __ffma2_rn(u, fhat, gpost[i]);
+            s2[0] = __ffma2_rn(t[i], fhat, s2[0]);
+            s2[1] = __fadd2_rn(s2[1], t[i]);
         }
-        team.sum(s2);
-        const float fproj = s2[0] * inv, fdm = a.layer ? s2[1] * inv : 0.0f;
+        float sums[2] = {s2[0].x + s2[0].y, s2[1].x + s2[1].y};
+        team.sum(sums);
+        reload(false);
+        const float2 fproj = twice(-(sums[0] * inv)), fdm = twice(a.layer ? -(sums[1] * inv) : 0.0f);
 #pragma unroll
-        for (int k = 0; k < kElems; ++k)
-            o.set(k, fr * (t[k] - fdm - (f.get(k) - fm) * fr * fproj));
+        for (int i = 0; i < kPairs; ++i) {
+            const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
+            o.set(i, __fmul2_rn(fr, __ffma2_rn(fhat, fproj, __fadd2_rn(t[i], fdm))));
+        }
         o.store(static_cast<T *>(a.df) + r * D, D, lane, size);
 
         // the gate row ends here, or this run does
@@ -445,13 +510,13 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             const int64_t g_start = g * a.rows_per_gate;
             if (ends && g_start >= r0) {
 #pragma unroll
-                for (int k = 0; k < kElems; ++k) o.set(k, ggate[k]);
+                for (int i = 0; i < kPairs; ++i) o.set(i, ggate[i]);
                 o.store(static_cast<T *>(a.dgate) + g * D, D, lane, size);
             } else {
                 put(slots + (g_start < r0 ? 2 : 3) * int64_t(D), ggate);
             }
 #pragma unroll
-            for (int k = 0; k < kElems; ++k) ggate[k] = 0.0f;
+            for (int i = 0; i < kPairs; ++i) ggate[i] = twice(0.0f);
         }
     }
     if (HAS_F && a.dw_post) put(slots, gpost);

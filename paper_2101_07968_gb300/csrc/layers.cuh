@@ -28,6 +28,15 @@ __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v
 template <>
 __device__ __forceinline__ float from_float(float v) { return v; }
 
+// Two neighbours at once: the sums and products of pairs are single instructions.
+__device__ __forceinline__ float2 pair_of(const __nv_bfloat16 *e) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(e)); }
+__device__ __forceinline__ float2 pair_of(const __half *e) { return __half22float2(*reinterpret_cast<const __half2 *>(e)); }
+__device__ __forceinline__ float2 pair_of(const float *e) { return *reinterpret_cast<const float2 *>(e); }
+__device__ __forceinline__ void put_pair(__nv_bfloat16 *e, float2 v) { *reinterpret_cast<__nv_bfloat162 *>(e) = __float22bfloat162_rn(v); }
+__device__ __forceinline__ void put_pair(__half *e, float2 v) { *reinterpret_cast<__half2 *>(e) = __float22half2_rn(v); }
+__device__ __forceinline__ void put_pair(float *e, float2 v) { *reinterpret_cast<float2 *>(e) = v; }
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
 // V consecutive elements, moved by one load or store of V * sizeof(T) bytes
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Vec {
