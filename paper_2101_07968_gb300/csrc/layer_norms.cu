@@ -86,45 +86,86 @@ struct Team {
 };
 
 // Rows on their way: A arrays' rows r, r + 1, ... in `stages` slots of shared memory. Slot
-// r % stages is filled again once every thread is past row r, which a later barrier shows.
-template <typename T, int A>
+// (r - first) % stages is filled again once every thread is past row r, which a later barrier
+// shows. Rows that start off 16-byte boundaries (SHIFTED) come with the bytes around them
+// up to the next boundaries; where those would lie outside the array, the row is not copied.
+template <typename T, int A, bool SHIFTED>
 struct Ring {
     const T *src[A];
     unsigned char *mem;
     uint64_t *bars;
     int stages, D;
-    int64_t first, end;
+    int64_t first, end, rows;
+    uint32_t *gave_up;
 
-    __device__ __forceinline__ T *at(int slot, int a) const
+    static __host__ __device__ size_t slot_bytes(int D)
     {
-        return reinterpret_cast<T *>(mem) + (int64_t(slot) * A + a) * D;
+        return (size_t(D) * sizeof(T) + 15) / 16 * 16 + (SHIFTED ? 16 : 0);
+    }
+    // by integers: arrays that a call does without are NULL, and arithmetic on such a pointer
+    // would let the compiler take it for a valid one
+    __device__ __forceinline__ uintptr_t address(int a, int64_t r) const
+    {
+        return reinterpret_cast<uintptr_t>(src[a]) + uintptr_t(r) * uintptr_t(D) * sizeof(T);
+    }
+    __device__ __forceinline__ bool copied(int64_t r) const
+    {
+        bool ok = true;
+        if (SHIFTED) {
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+                ok = ok && (!src[a] || ((address(a, r) & ~uintptr_t(15)) >= address(a, 0) &&
+                                        ((address(a, r + 1) + 15) & ~uintptr_t(15)) <= address(a, rows)));
+        }
+        return ok;
+    }
+    __device__ __forceinline__ unsigned char *slot(int64_t r, int a) const
+    {
+        return mem + (size_t((r - first) % stages) * A + a) * slot_bytes(D);
+    }
+    __device__ __forceinline__ const T *at(int64_t r, int a) const
+    {
+        return reinterpret_cast<const T *>(slot(r, a) + (SHIFTED ? address(a, r) & 15 : 0));
+    }
+    __device__ __forceinline__ uint32_t bar(int64_t r) const
+    {
+        return bw::smem_addr(bars + (r - first) % stages);
     }
     __device__ __forceinline__ void fetch(int64_t r)  // one thread
     {
-        if (r >= end) return;
-        const int slot = int((r - first) % stages);
-        const uint32_t bar = bw::smem_addr(bars + slot), bytes = uint32_t(D * sizeof(T));
-        int n = 0;
-#pragma unroll
-        for (int a = 0; a < A; ++a) n += src[a] != nullptr;
-        bw::bar_arrive_bytes(bar, bytes * n);
+        if (r >= end || *gave_up) return;
+        if (!copied(r)) {
+            bw::bar_arrive(bar(r));
+            return;
+        }
+        auto bytes = [&](int a) {
+            return uint32_t(((address(a, r + 1) + 15) & ~uintptr_t(15)) - (address(a, r) & ~uintptr_t(15)));
+        };
+        uint32_t all = 0;
 #pragma unroll
         for (int a = 0; a < A; ++a)
-            if (src[a]) bw::copy_bytes(bw::smem_addr(at(slot, a)), src[a] + r * D, bytes, bar);
+            if (src[a]) all += bytes(a);
+        bw::bar_arrive_bytes(bar(r), all);
+#pragma unroll
+        for (int a = 0; a < A; ++a)
+            if (src[a])
+                bw::copy_bytes(bw::smem_addr(slot(r, a)), reinterpret_cast<const void *>(address(a, r) & ~uintptr_t(15)),
+                               bytes(a), bar(r));
     }
     __device__ __forceinline__ void start()
     {
         if (threadIdx.x == 0) {
+            *gave_up = 0;
             for (int i = 0; i < stages; ++i) bw::bar_init(bw::smem_addr(bars + i), 1);
             bw::bar_init_fence();
             for (int i = 0; i < stages; ++i) fetch(first + i);
         }
         __syncthreads();
     }
-    __device__ __forceinline__ bool wait(int64_t r, uint32_t *gave_up)
+    // whether row r is in its slot; otherwise it is to be read from memory
+    __device__ __forceinline__ bool wait(int64_t r)
     {
-        const int64_t i = r - first;
-        return bw::bar_wait(bw::smem_addr(bars + i % stages), uint32_t(i / stages) & 1u, gave_up);
+        return bw::bar_wait(bar(r), uint32_t((r - first) / stages) & 1u, gave_up) && copied(r);
     }
 };
 constexpr int kMaxStages = 4;
@@ -248,11 +289,8 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
     const int64_t r0 = run_start(a.rows, gridDim.x, blockIdx.x);
     const int64_t r1 = run_start(a.rows, gridDim.x, blockIdx.x + 1);
     const T *xp = static_cast<const T *>(a.x), *fp = static_cast<const T *>(a.f);
-    Ring<T, 2> ring{{xp, fp}, dyn, bars, stages, D, r0, r1};
-    if (RING) {
-        if (lane == 0) gave_up = 0;
-        ring.start();
-    }
+    Ring<T, 2, V == 1> ring{{xp, fp}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up};
+    if (RING) ring.start();
     R post, pre, gate;
     if (HAS_F) {
         post.load_or_ones(a.w_post, D, lane, size);
@@ -267,13 +305,12 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
         }
         R x, f;
-        const bool here = RING && ring.wait(r, &gave_up);
-        const int slot = here ? int((r - r0) % stages) : 0;
-        x.load(here ? ring.at(slot, 0) : xp + r * D, D, lane, size);
-        if (HAS_F) f.load(here ? ring.at(slot, 1) : fp + r * D, D, lane, size);
+        const bool here = RING && ring.wait(r);
+        x.load(here ? ring.at(r, 0) : xp + r * D, D, lane, size);
+        if (HAS_F) f.load(here ? ring.at(r, 1) : fp + r * D, D, lane, size);
         bool refill = RING;
         auto taken = [&] {  // past a barrier: every thread has this row in registers
-            if (refill && lane == 0 && !gave_up) ring.fetch(r + stages);
+            if (refill && lane == 0) ring.fetch(r + stages);
             refill = false;
         };
         if (RING && team.warps == 1) {
@@ -337,8 +374,12 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
 // Per run: sums for w_post, w_pre, the gate row shared with the run before, the gate row
 // shared with the run after.
 constexpr int kSlots = 4;
+// Gate rows of at least this many rows: one sum A of t * fhat serves the gradients of the
+// gate and of w_post (w_post A and, gate by gate, gate A), which are added to the run's sums
+// when the gate row changes. For shorter ones that would cost more than the second sum.
+constexpr int kLongGate = 8;
 
-template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool RING, int MAXT>
+template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : 1)
 norm_grad_kernel(NormArgs a, float *partial, int stages)
 {
@@ -354,40 +395,52 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
     const int64_t r0 = run_start(a.rows, P, b), r1 = run_start(a.rows, P, b + 1);
     const T *src[4] = {HAS_H ? static_cast<const T *>(a.x) : nullptr, static_cast<const T *>(a.dh),
                        static_cast<const T *>(a.dy), HAS_F ? static_cast<const T *>(a.f) : nullptr};
-    Ring<T, 4> ring{{src[0], src[1], src[2], src[3]}, dyn, bars, stages, D, r0, r1};
-    if (RING) {
-        if (lane == 0) gave_up = 0;
-        ring.start();
-    }
-    R post, pre, gate;
+    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up};
+    if (RING) ring.start();
+    R pre, post, gate;
+    if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
     if (HAS_F) {
         post.load_or_ones(a.w_post, D, lane, size);
         gate.fill(1.0f);
     }
-    if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
-    float2 gpost[kPairs], gpre[kPairs], ggate[kPairs];
+    float2 gpre[kPairs], gpost[kPairs], ggate[kPairs];  // LONG: ggate holds A, gpost is in memory
+    float2 gp[kPairs];                                  // LONG: gate * w_post * scale
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) gpost[i] = gpre[i] = ggate[i] = twice(0.0f);
-    auto put = [&](float *p, const float2 (&v)[kPairs]) {
+    float *slots = partial + b * int64_t(kSlots) * D;
+    auto each = [&](auto &&op) {  // op(pair, half, column) of this thread's columns
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            if (R::inside(2 * i, D, lane, size)) p[R::column(2 * i, lane, size)] = v[i].x;
-            if (R::inside(2 * i + 1, D, lane, size)) p[R::column(2 * i + 1, lane, size)] = v[i].y;
+            if (R::inside(2 * i, D, lane, size)) op(i, 0, R::column(2 * i, lane, size));
+            if (R::inside(2 * i + 1, D, lane, size)) op(i, 1, R::column(2 * i + 1, lane, size));
         }
     };
-    float *slots = partial + b * int64_t(kSlots) * D;
+    auto half = [](float2 v, int h) { return h ? v.y : v.x; };
+    auto load_gate = [&](int64_t g) {
+        if (a.gate) gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
+        if (LONG) {
+            post.load_or_ones(a.w_post, D, lane, size);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i)
+                gp[i] = __fmul2_rn(__fmul2_rn(gate.get(i), post.get(i)), twice(a.drop.scale));
+        }
+    };
     int64_t g = 0, g_end = r0;
+    bool first_gate = true;
     for (int64_t r = r0; r < r1; ++r) {
         if (HAS_F && r >= g_end) {
             g = r / a.rows_per_gate;
             g_end = (g + 1) * a.rows_per_gate;
-            if (a.gate) gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
+            load_gate(g);
         }
-        const bool here = RING && ring.wait(r, &gave_up);
-        const int slot = here ? int((r - r0) % stages) : 0;
-        auto row = [&](int i) { return here ? static_cast<const T *>(ring.at(slot, i)) : src[i] + r * D; };
+        const bool here = RING && ring.wait(r);
+        auto row = [&](int i) { return here ? ring.at(r, i) : src[i] + r * D; };
         R y, f, dh;
-
+        if (HAS_H) {
+            y.load(row(0), D, lane, size);
+            dh.load(row(1), D, lane, size);
+        }
+        if (HAS_F) f.load(row(3), D, lane, size);
         // Read again from the ring in each phase: the sums take most of the registers, and
         // rows held over the barriers would spill.
         auto reload = [&](bool with_y) {
@@ -400,58 +453,83 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             if (HAS_F) f.load(row(3), D, lane, size);
         };
 
-        // statistics of y and f, and the sums of dn = dh * w_pre that n'(y)^T needs
-        float2 ym = twice(0.0f), fm = twice(0.0f), dm = twice(0.0f);  // minus the means
-        float s[3];
-        if (HAS_H) {
-            y.load(row(0), D, lane, size);
-            dh.load(row(1), D, lane, size);
-        }
-        if (HAS_F) f.load(row(3), D, lane, size);
-        float2 q[3];
-        auto fold = [&] {
+        // Statistics of y and f, and the sums of dn = dh * w_pre that n'(y)^T needs. The layer
+        // norm's mean square about the mean comes from sums about the row's first element, in
+        // the same pass; where that element lies more than two deviations from the mean, and
+        // the difference would lose digits, the sums are taken again about the mean.
+        float2 y0 = twice(0.0f), f0 = twice(0.0f);  // minus what the sums are about
+        float s[4], w[2];                           // sums: y, y^2, f, f^2; dn, dn y
+        float2 q[6];
+        auto sums = [&] {
 #pragma unroll
-            for (int i = 0; i < 3; ++i) s[i] = q[i].x + q[i].y;
-            team.sum(s);
-        };
-        if (a.layer) {
-            q[0] = q[1] = q[2] = twice(0.0f);
+            for (int i = 0; i < 6; ++i) q[i] = twice(0.0f);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
                 if (HAS_H) {
-                    q[0] = __fadd2_rn(q[0], y.get(i));
-                    q[2] = __ffma2_rn(dh.get(i), pre.get(i), q[2]);
+                    const float2 v = R::only_inside(__fadd2_rn(y.get(i), y0), i, D, lane, size);
+                    const float2 dn = __fmul2_rn(dh.get(i), pre.get(i));
+                    q[1] = __ffma2_rn(v, v, q[1]);
+                    q[5] = __ffma2_rn(dn, v, q[5]);
+                    if (a.layer) {
+                        q[0] = __fadd2_rn(q[0], v);
+                        q[4] = __fadd2_rn(q[4], dn);
+                    }
                 }
-                if (HAS_F) q[1] = __fadd2_rn(q[1], f.get(i));
+                if (HAS_F) {
+                    const float2 v = R::only_inside(__fadd2_rn(f.get(i), f0), i, D, lane, size);
+                    q[3] = __ffma2_rn(v, v, q[3]);
+                    if (a.layer) q[2] = __fadd2_rn(q[2], v);
+                }
             }
-            fold();
-            ym = twice(-s[0] * inv);
-            fm = twice(-s[1] * inv);
-            dm = twice(-s[2] * inv);
-            reload(true);
-        }
-        q[0] = q[1] = q[2] = twice(0.0f);
+            if (a.layer) {
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-            if (HAS_H) {
-                const float2 v = R::only_inside(__fadd2_rn(y.get(i), ym), i, D, lane, size);
-                q[0] = __ffma2_rn(v, v, q[0]);
-                q[2] = __ffma2_rn(__fmul2_rn(dh.get(i), pre.get(i)), v, q[2]);
+                for (int i = 0; i < 4; ++i) s[i] = q[i].x + q[i].y;
+                w[0] = q[4].x + q[4].y;
+                w[1] = q[5].x + q[5].y;
+                if (HAS_H && HAS_F) {
+                    team.sum(s);
+                    if (HAS_H) team.sum(w);
+                } else if (HAS_H) {
+                    float v[4] = {s[0], s[1], w[0], w[1]};
+                    team.sum(v);
+                    s[0] = v[0], s[1] = v[1], w[0] = v[2], w[1] = v[3];
+                } else {
+                    float v[2] = {s[2], s[3]};
+                    team.sum(v);
+                    s[2] = v[0], s[3] = v[1];
+                }
+            } else {
+                float v[3] = {q[1].x + q[1].y, q[3].x + q[3].y, q[5].x + q[5].y};
+                team.sum(v);
+                s[0] = s[2] = w[0] = 0.0f;
+                s[1] = v[0], s[3] = v[1], w[1] = v[2];
             }
-            if (HAS_F) {
-                const float2 v = R::only_inside(__fadd2_rn(f.get(i), fm), i, D, lane, size);
-                q[1] = __ffma2_rn(v, v, q[1]);
-            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] *= inv;
+            w[0] *= inv;
+            w[1] *= inv;
+        };
+        if (a.layer) {
+            if (HAS_H) y0 = twice(-to_float(*row(0)));
+            if (HAS_F) f0 = twice(-to_float(*row(3)));
         }
-        fold();
+        sums();
+        if (a.layer && (s[0] * s[0] > 0.8f * s[1] || s[2] * s[2] > 0.8f * s[3])) {
+            y0.x -= s[0], y0.y = y0.x;
+            f0.x -= s[2], f0.y = f0.x;
+            reload(true);
+            sums();
+        }
         if (RING) {  // past a barrier of this row, so every thread is done with the row before
             __syncwarp();
-            if (lane == 0 && r > r0 && !gave_up) ring.fetch(r - 1 + stages);
+            if (lane == 0 && r > r0) ring.fetch(r - 1 + stages);
         }
-        const float yr1 = HAS_H ? rsqrtf(s[0] * inv + a.eps) : 0.0f;
-        const float fr1 = HAS_F ? rsqrtf(s[1] * inv + a.eps) : 0.0f;
-        const float2 yr = twice(yr1), fr = twice(fr1);
-        const float2 proj = twice(-(s[2] * inv * yr1));  // minus the mean of dn * yhat
+        const float yr1 = HAS_H ? rsqrtf(fmaxf(s[1] - s[0] * s[0], 0.0f) + a.eps) : 0.0f;
+        const float fr1 = HAS_F ? rsqrtf(fmaxf(s[3] - s[2] * s[2], 0.0f) + a.eps) : 0.0f;
+        // yhat = (y + ym) yr; n'(y)^T dn = yr (dn + dm + yhat proj)
+        const float2 yr = twice(yr1), ym = twice(y0.x - s[0]), dm = twice(-w[0]);
+        const float2 proj = twice(-(w[1] - s[0] * w[0]) * yr1);
+        const float2 fr = twice(fr1), fm = twice(f0.x - s[2]);
 
         reload(true);
         float2 t[kPairs];
@@ -485,18 +563,24 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
             const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
-            const float2 kt = R::only_inside(__fmul2_rn(t[i], scale), i, D, lane, size);
-            const float2 u = __fmul2_rn(kt, gate.get(i)), p = post.get(i);
-            t[i] = __fmul2_rn(u, p);
-            ggate[i] = __ffma2_rn(__fmul2_rn(kt, p), fhat, ggate[i]);
-            gpost[i] = __ffma2_rn(u, fhat, gpost[i]);
+            float2 kt = R::only_inside(t[i], i, D, lane, size);
+            if (LONG) {
+                t[i] = __fmul2_rn(kt, gp[i]);
+                ggate[i] = __ffma2_rn(kt, fhat, ggate[i]);
+            } else {
+                kt = __fmul2_rn(kt, scale);
+                const float2 u = __fmul2_rn(kt, gate.get(i)), p = post.get(i);
+                t[i] = __fmul2_rn(u, p);
+                ggate[i] = __ffma2_rn(__fmul2_rn(kt, p), fhat, ggate[i]);
+                gpost[i] = __ffma2_rn(u, fhat, gpost[i]);
+            }
             s2[0] = __ffma2_rn(t[i], fhat, s2[0]);
             s2[1] = __fadd2_rn(s2[1], t[i]);
         }
-        float sums[2] = {s2[0].x + s2[0].y, s2[1].x + s2[1].y};
-        team.sum(sums);
+        float v[2] = {s2[0].x + s2[0].y, s2[1].x + s2[1].y};
+        team.sum(v);
         reload(false);
-        const float2 fproj = twice(-(sums[0] * inv)), fdm = twice(a.layer ? -(sums[1] * inv) : 0.0f);
+        const float2 fproj = twice(-(v[0] * inv)), fdm = twice(a.layer ? -(v[1] * inv) : 0.0f);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
             const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
@@ -506,28 +590,52 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
 
         // the gate row ends here, or this run does
         const bool ends = r + 1 == g_end || r + 1 == a.rows;
-        if (a.dgate && (ends || r + 1 == r1)) {
-            const int64_t g_start = g * a.rows_per_gate;
-            if (ends && g_start >= r0) {
+        if (ends || r + 1 == r1) {
+            if (LONG) {
+                post.load_or_ones(a.w_post, D, lane, size);
+                if (a.gate) gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
+                if (a.dw_post)
+                    each([&](int i, int h, int c) {
+                        const float v = half(gate.get(i), h) * half(ggate[i], h) * a.drop.scale;
+                        slots[c] = first_gate ? v : slots[c] + v;
+                    });
+                first_gate = false;
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) o.set(i, ggate[i]);
-                o.store(static_cast<T *>(a.dgate) + g * D, D, lane, size);
-            } else {
-                put(slots + (g_start < r0 ? 2 : 3) * int64_t(D), ggate);
+                for (int i = 0; i < kPairs; ++i)
+                    ggate[i] = __fmul2_rn(__fmul2_rn(post.get(i), scale), ggate[i]);
+            }
+            if (a.dgate) {
+                const int64_t g_start = g * a.rows_per_gate;
+                if (ends && g_start >= r0) {
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) o.set(i, ggate[i]);
+                    o.store(static_cast<T *>(a.dgate) + g * D, D, lane, size);
+                } else {
+                    float *p = slots + (g_start < r0 ? 2 : 3) * int64_t(D);
+                    each([&](int i, int h, int c) { p[c] = half(ggate[i], h); });
+                }
             }
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) ggate[i] = twice(0.0f);
         }
     }
-    if (HAS_F && a.dw_post) put(slots, gpost);
-    if (HAS_H && a.dw_pre) put(slots + D, gpre);
+    if (HAS_F && !LONG && a.dw_post) each([&](int i, int h, int c) { slots[c] = half(gpost[i], h); });
+    if (HAS_H && a.dw_pre) each([&](int i, int h, int c) { slots[D + c] = half(gpre[i], h); });
     if (RING && gave_up)  // a copy is late: it still writes this block's memory
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
-// Adds the runs' sums: block row 0 those of the weights, block row b > 0 those of the
-// gate row that runs b - 1 and b share, if b - 1 is where it starts. Sixteen threads a
-// column, each every sixteenth run in order.
+// The run that holds row r.
+__device__ __forceinline__ int64_t run_of(int64_t rows, int64_t P, int64_t r)
+{
+    int64_t b = r * P / rows;
+    while (b + 1 < P && run_start(rows, P, b + 1) <= r) ++b;
+    while (b > 0 && run_start(rows, P, b) > r) --b;
+    return b;
+}
+
+// Adds the runs' sums: block row 0 those of the weights, block row g + 1 those of gate row g if
+// it lies in several runs. Sixteen threads a column, each every sixteenth run in order.
 constexpr int kFinishCols = 32, kFinishLanes = 16;
 template <typename T>
 __global__ void __launch_bounds__(kFinishCols *kFinishLanes)
@@ -536,11 +644,10 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
     __shared__ float part[2][kFinishLanes][kFinishCols];
     const int tx = threadIdx.x, ty = threadIdx.y;
     const int64_t c = int64_t(blockIdx.x) * kFinishCols + tx, D = a.D;
-    const int64_t stride = kSlots * D;
+    const int64_t stride = kSlots * D, g = int64_t(blockIdx.y) - 1;
     const bool in = c < D;
     float s0 = 0.0f, s1 = 0.0f;
-    const int64_t b = blockIdx.y;
-    if (b == 0) {
+    if (g < 0) {
         if (in) {
             if (a.dw_post)
 #pragma unroll 8
@@ -550,25 +657,15 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
                 for (int64_t i = ty; i < P; i += kFinishLanes) s1 += partial[i * stride + D + c];
         }
     } else {
-        const int64_t rb = run_start(a.rows, P, b);
-        const int64_t g = rb / a.rows_per_gate, gs = g * a.rows_per_gate;
-        if (!a.dgate || gs == rb || gs < run_start(a.rows, P, b - 1)) return;  // the whole block
-        const int64_t ge = gs + a.rows_per_gate < a.rows ? gs + a.rows_per_gate : a.rows;
-        if (in) {
-            if (ty == 0) s0 = partial[(b - 1) * stride + 3 * D + c];
-            int64_t last = b;  // runs b .. last - 1 start inside the group
-            if (ge == a.rows) {
-                last = P;
-            } else {
-                int64_t hi = P;
-                while (last < hi) {
-                    const int64_t mid = (last + hi) / 2;
-                    if (run_start(a.rows, P, mid) < ge) last = mid + 1; else hi = mid;
-                }
-            }
+        const int64_t start = g * a.rows_per_gate;
+        const int64_t end = start + a.rows_per_gate < a.rows ? start + a.rows_per_gate : a.rows;
+        const int64_t b0 = run_of(a.rows, P, start), b1 = run_of(a.rows, P, end - 1);
+        if (b0 == b1) return;  // written by its run; the whole block
+        // run b0 holds the gate's first rows: shared with the run after
+        if (in)
 #pragma unroll 8
-            for (int64_t i = b + ty; i < last; i += kFinishLanes) s0 += partial[i * stride + 2 * D + c];
-        }
+            for (int64_t i = b0 + ty; i <= b1; i += kFinishLanes)
+                s0 += partial[i * stride + (i == b0 ? 3 : 2) * D + c];
     }
     part[0][ty][tx] = s0;
     part[1][ty][tx] = s1;
@@ -577,13 +674,25 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
     float v = 0.0f;
 #pragma unroll
     for (int i = 0; i < kFinishLanes; ++i) v += part[ty][i][tx];
-    if (b == 0) {
+    if (g < 0) {
         float *out = ty == 0 ? a.dw_post : a.dw_pre;
         if (out) out[c] = v;
     } else if (ty == 0) {
-        const int64_t g = run_start(a.rows, P, b) / a.rows_per_gate;
         static_cast<T *>(a.dgate)[g * D + c] = from_float<T>(v);
     }
+}
+
+// With more gate rows than runs, a gate row lies in at most two: one block per run adds the
+// row that it shares with the run before.
+template <typename T>
+__global__ void __launch_bounds__(128) norm_shared_gates_kernel(NormArgs a, const float *partial, int64_t P)
+{
+    const int64_t b = int64_t(blockIdx.x) + 1, rb = run_start(a.rows, P, b);
+    const int64_t g = rb / a.rows_per_gate, D = a.D;
+    if (g * a.rows_per_gate == rb) return;
+    const float *before = partial + ((b - 1) * kSlots + 3) * D, *after = partial + (b * kSlots + 2) * D;
+    for (int64_t c = threadIdx.x; c < D; c += blockDim.x)
+        static_cast<T *>(a.dgate)[g * D + c] = from_float<T>(before[c] + after[c]);
 }
 
 // ------------------------------------------------------------------------------ host
@@ -601,10 +710,10 @@ Plan plan_for(int D, int arrays, int bytes, int threads)
     const int size = row_threads(D);
     p.blocks = threads / size < 1 ? 1 : threads / size;
     if (p.blocks > 16) p.blocks = 16;
-    const size_t row = size_t(arrays) * D * bytes, room = size_t(224) << 10;
+    const size_t row = size_t(arrays) * ((size_t(D) * bytes + 15) / 16 * 16 + 16), room = size_t(224) << 10;
     while (p.blocks > 1 && room / p.blocks < 2 * row + 2048) --p.blocks;
-    p.stages = int((room / p.blocks - 2048) / row);
-    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    const size_t slots = room / p.blocks > 2048 ? (room / p.blocks - 2048) / row : 0;
+    p.stages = int(slots < kMaxStages ? slots : kMaxStages);
     if (p.stages < 2) p.stages = 0;
     p.smem = p.stages * row;
     return p;
@@ -643,24 +752,29 @@ template <typename T, int V, bool FULL, bool RING, int MAXT>
 cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const Plan &p,
                              cudaStream_t stream)
 {
-    auto kernel = a.f && a.dh ? norm_grad_kernel<T, V, FULL, true, true, RING, MAXT>
-                  : a.f       ? norm_grad_kernel<T, V, FULL, true, false, RING, MAXT>
-                              : norm_grad_kernel<T, V, FULL, false, true, RING, MAXT>;
-    static DeviceCache cache[3];
+    const bool lg = a.rows_per_gate >= kLongGate;
+    auto kernel = a.f && a.dh ? lg ? norm_grad_kernel<T, V, FULL, true, true, true, RING, MAXT>
+                                   : norm_grad_kernel<T, V, FULL, true, true, false, RING, MAXT>
+                  : a.f       ? norm_grad_kernel<T, V, FULL, true, false, false, RING, MAXT>
+                              : norm_grad_kernel<T, V, FULL, false, true, false, RING, MAXT>;
+    static DeviceCache cache[4];
     if (RING) {
         int ready = 0;
-        const cudaError_t e = cache[a.f && a.dh ? 0 : a.f ? 1 : 2].get(ready, [&](int &v) {
+        const cudaError_t e = cache[a.f && a.dh ? lg : a.f ? 2 : 3].get(ready, [&](int &v) {
             v = 1;
             return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 << 10);
         });
         if (e != cudaSuccess) return e;
     }
     kernel<<<unsigned(P), unsigned(row_threads(a.D)), RING ? p.smem : 0, stream>>>(a, partial, p.stages);
-    const bool shared_gates = a.dgate && P > 1;
-    if (a.dw_post || a.dw_pre || shared_gates) {
-        const dim3 g(unsigned((a.D + kFinishCols - 1) / kFinishCols), shared_gates ? unsigned(P) : 1u);
+    const int64_t gates = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate;
+    const bool few = gates < P;
+    if (a.dw_post || a.dw_pre || (a.dgate && few)) {
+        const dim3 g(unsigned((a.D + kFinishCols - 1) / kFinishCols), 1u + unsigned(a.dgate && few ? gates : 0));
         norm_finish_kernel<T><<<g, dim3(kFinishCols, kFinishLanes), 0, stream>>>(a, partial, P);
     }
+    if (a.dgate && !few && P > 1 && a.rows_per_gate > 1)
+        norm_shared_gates_kernel<T><<<unsigned(P - 1), 128, 0, stream>>>(a, partial, P);
     return cudaGetLastError();
 }
 
@@ -684,7 +798,9 @@ cudaError_t launch_norm(int dtype, const NormArgs &a, cudaStream_t stream)
         if (a.D > kWideD)
             return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
                        : norm_launch<T, 1, false, false, 1024>(a, p, stream);
-        if (!vec) return norm_launch<T, 1, false, false, kNarrow>(a, p, stream);
+        if (!vec)
+            return p.stages ? norm_launch<T, 1, false, true, kNarrow>(a, p, stream)
+                            : norm_launch<T, 1, false, false, kNarrow>(a, p, stream);
         if (!p.stages) return norm_launch<T, V, false, false, kNarrow>(a, p, stream);
         return full ? norm_launch<T, V, true, true, kNarrow>(a, p, stream)
                     : norm_launch<T, V, false, true, kNarrow>(a, p, stream);
@@ -706,7 +822,9 @@ cudaError_t launch_norm_grad(int dtype, const NormArgs &a, float *partial, cudaS
         if (a.D > kWideD)
             return vec ? norm_grad_launch<T, V, false, false, 1024>(a, partial, P, p, stream)
                        : norm_grad_launch<T, 1, false, false, 1024>(a, partial, P, p, stream);
-        if (!vec) return norm_grad_launch<T, 1, false, false, kNarrow>(a, partial, P, p, stream);
+        if (!vec)
+            return p.stages ? norm_grad_launch<T, 1, false, true, kNarrow>(a, partial, P, p, stream)
+                            : norm_grad_launch<T, 1, false, false, kNarrow>(a, partial, P, p, stream);
         if (!p.stages) return norm_grad_launch<T, V, false, false, kNarrow>(a, partial, P, p, stream);
         return full ? norm_grad_launch<T, V, true, true, kNarrow>(a, partial, P, p, stream)
                     : norm_grad_launch<T, V, false, true, kNarrow>(a, partial, P, p, stream);
