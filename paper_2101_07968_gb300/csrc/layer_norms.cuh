@@ -9,11 +9,13 @@
 // the ring) are loaded straight into registers. The gradient computes the statistics again
 // from the same rows and adds up the gradients of weights and gates in registers; what
 // several runs share is written out per run and added in a fixed order by a second kernel.
+#pragma once
+
 #include "blackwell.cuh"
 #include "layers.cuh"
 
 namespace dc {
-namespace {
+namespace norms {
 
 constexpr int kElems = 16;  // elements of a row per thread
 constexpr int kPairs = kElems / 2;
@@ -85,9 +87,9 @@ struct Team {
     }
 };
 
-// Rows on their way: A arrays' rows r, r + 1, ... in `stages` slots of shared memory. Slot
-// (r - first) % stages is filled again once every thread is past row r, which a later barrier
-// shows. Rows that start off 16-byte boundaries (SHIFTED) come with the bytes around them
+// Rows on their way: A arrays' rows r, r + 1, ... in `stages` slots of shared memory, taken in
+// turn. A row's slot is filled again (fetch_next) once every thread is past that row, which a
+// later barrier shows. Rows that start off 16-byte boundaries (SHIFTED) come with the bytes around them
 // up to the next boundaries; where those would lie outside the array, the row is not copied.
 template <typename T, int A, bool SHIFTED>
 struct Ring {
@@ -97,6 +99,9 @@ struct Ring {
     int stages, D;
     int64_t first, end, rows;
     uint32_t *gave_up;
+    int slot, phase;        // of the row in hand: advance() moves to the next
+    int fill;               // slot of the next row to fetch, and that row (one thread)
+    int64_t next;
 
     static __host__ __device__ size_t slot_bytes(int D)
     {
@@ -119,23 +124,23 @@ struct Ring {
         }
         return ok;
     }
-    __device__ __forceinline__ unsigned char *slot(int64_t r, int a) const
+    __device__ __forceinline__ unsigned char *place(int slot, int a) const
     {
-        return mem + (size_t((r - first) % stages) * A + a) * slot_bytes(D);
+        return mem + uint32_t(slot * A + a) * uint32_t(slot_bytes(D));
     }
-    __device__ __forceinline__ const T *at(int64_t r, int a) const
+    __device__ __forceinline__ const T *at(int64_t r, int a) const  // the row in hand
     {
-        return reinterpret_cast<const T *>(slot(r, a) + (SHIFTED ? address(a, r) & 15 : 0));
+        return reinterpret_cast<const T *>(place(slot, a) + (SHIFTED ? address(a, r) & 15 : 0));
     }
-    __device__ __forceinline__ uint32_t bar(int64_t r) const
+    __device__ __forceinline__ void fetch_next()  // one thread
     {
-        return bw::smem_addr(bars + (r - first) % stages);
-    }
-    __device__ __forceinline__ void fetch(int64_t r)  // one thread
-    {
+        const int64_t r = next++;
+        const uint32_t bar = bw::smem_addr(bars + fill);
+        const int to = fill;
+        if (++fill == stages) fill = 0;
         if (r >= end || *gave_up) return;
         if (!copied(r)) {
-            bw::bar_arrive(bar(r));
+            bw::bar_arrive(bar);
             return;
         }
         auto bytes = [&](int a) {
@@ -145,27 +150,36 @@ struct Ring {
 #pragma unroll
         for (int a = 0; a < A; ++a)
             if (src[a]) all += bytes(a);
-        bw::bar_arrive_bytes(bar(r), all);
+        bw::bar_arrive_bytes(bar, all);
 #pragma unroll
         for (int a = 0; a < A; ++a)
             if (src[a])
-                bw::copy_bytes(bw::smem_addr(slot(r, a)), reinterpret_cast<const void *>(address(a, r) & ~uintptr_t(15)),
-                               bytes(a), bar(r));
+                bw::copy_bytes(bw::smem_addr(place(to, a)), reinterpret_cast<const void *>(address(a, r) & ~uintptr_t(15)),
+                               bytes(a), bar);
     }
     __device__ __forceinline__ void start()
     {
+        slot = phase = fill = 0;
+        next = first;
         if (threadIdx.x == 0) {
             *gave_up = 0;
             for (int i = 0; i < stages; ++i) bw::bar_init(bw::smem_addr(bars + i), 1);
             bw::bar_init_fence();
-            for (int i = 0; i < stages; ++i) fetch(first + i);
+            for (int i = 0; i < stages; ++i) fetch_next();
         }
         __syncthreads();
     }
-    // whether row r is in its slot; otherwise it is to be read from memory
+    // whether row r, the one in hand, is in its slot; otherwise it is to be read from memory
     __device__ __forceinline__ bool wait(int64_t r)
     {
-        return bw::bar_wait(bar(r), uint32_t((r - first) / stages) & 1u, gave_up) && copied(r);
+        return bw::bar_wait(bw::smem_addr(bars + slot), uint32_t(phase), gave_up) && copied(r);
+    }
+    __device__ __forceinline__ void advance()
+    {
+        if (++slot == stages) {
+            slot = 0;
+            phase ^= 1;
+        }
     }
 };
 constexpr int kMaxStages = 4;
@@ -289,7 +303,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
     const int64_t r0 = run_start(a.rows, gridDim.x, blockIdx.x);
     const int64_t r1 = run_start(a.rows, gridDim.x, blockIdx.x + 1);
     const T *xp = static_cast<const T *>(a.x), *fp = static_cast<const T *>(a.f);
-    Ring<T, 2, V == 1> ring{{xp, fp}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up};
+    Ring<T, 2, V == 1> ring{{xp, fp}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
     if (RING) ring.start();
     R post, pre, gate;
     if (HAS_F) {
@@ -310,7 +324,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
         if (HAS_F) f.load(here ? ring.at(r, 1) : fp + r * D, D, lane, size);
         bool refill = RING;
         auto taken = [&] {  // past a barrier: every thread has this row in registers
-            if (refill && lane == 0) ring.fetch(r + stages);
+            if (refill && lane == 0) ring.fetch_next();
             refill = false;
         };
         if (RING && team.warps == 1) {
@@ -365,6 +379,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             for (int i = 0; i < kPairs; ++i) o.set(i, __fmul2_rn(__fmul2_rn(y[i], rstd), pre.get(i)));
             o.store(static_cast<T *>(a.h) + r * D, D, lane, size);
         }
+        if (RING) ring.advance();
     }
     if (RING && gave_up)  // a copy is late: it still writes this block's memory
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
@@ -395,7 +410,7 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
     const int64_t r0 = run_start(a.rows, P, b), r1 = run_start(a.rows, P, b + 1);
     const T *src[4] = {HAS_H ? static_cast<const T *>(a.x) : nullptr, static_cast<const T *>(a.dh),
                        static_cast<const T *>(a.dy), HAS_F ? static_cast<const T *>(a.f) : nullptr};
-    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up};
+    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
     if (RING) ring.start();
     R pre, post, gate;
     if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
@@ -434,7 +449,12 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             load_gate(g);
         }
         const bool here = RING && ring.wait(r);
-        auto row = [&](int i) { return here ? ring.at(r, i) : src[i] + r * D; };
+        const T *in[4] = {nullptr, nullptr, nullptr, nullptr};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (src[i]) in[i] = here ? ring.at(r, i) : src[i] + r * D;
+        if (RING) ring.advance();
+        auto row = [&](int i) { return in[i]; };
         R y, f, dh;
         if (HAS_H) {
             y.load(row(0), D, lane, size);
@@ -522,7 +542,7 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         }
         if (RING) {  // past a barrier of this row, so every thread is done with the row before
             __syncwarp();
-            if (lane == 0 && r > r0) ring.fetch(r - 1 + stages);
+            if (lane == 0 && r > r0) ring.fetch_next();
         }
         const float yr1 = HAS_H ? rsqrtf(fmaxf(s[1] - s[0] * s[0], 0.0f) + a.eps) : 0.0f;
         const float fr1 = HAS_F ? rsqrtf(fmaxf(s[3] - s[2] * s[2], 0.0f) + a.eps) : 0.0f;
@@ -696,7 +716,7 @@ __global__ void __launch_bounds__(128) norm_shared_gates_kernel(NormArgs a, cons
 }
 
 // ------------------------------------------------------------------------------ host
-int row_threads(int D) { return (D + kElems * 32 - 1) / (kElems * 32) * 32; }
+inline int row_threads(int D) { return (D + kElems * 32 - 1) / (kElems * 32) * 32; }
 
 // Blocks an SM and slots of the ring: `threads` an SM as the registers allow, and the 224 KB
 // of shared memory shared between them; no ring (0 slots) where it would hold fewer than two rows.
@@ -704,7 +724,7 @@ struct Plan {
     int blocks, stages;
     size_t smem;
 };
-Plan plan_for(int D, int arrays, int bytes, int threads)
+inline Plan plan_for(int D, int arrays, int bytes, int threads)
 {
     Plan p;
     const int size = row_threads(D);
@@ -721,7 +741,7 @@ Plan plan_for(int D, int arrays, int bytes, int threads)
 constexpr int kSms = 152;
 constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM
 
-int64_t grad_runs(int dtype, int64_t rows, int D)
+inline int64_t grad_runs(int dtype, int64_t rows, int D)
 {
     const int64_t most = int64_t(kSms) * plan_for(D, 4, dtype_bytes(dtype), kGradThreads).blocks;
     return rows < most ? rows : most;
@@ -778,7 +798,7 @@ cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const
     return cudaGetLastError();
 }
 
-bool vectors_ok(int dtype, const NormArgs &a)
+inline bool vectors_ok(int dtype, const NormArgs &a)
 {
     if (a.D % (16 / dtype_bytes(dtype))) return false;
     const void *p[] = {a.x, a.f, a.gate, a.w_post, a.w_pre, a.y, a.h, a.dy, a.dh, a.dx, a.df, a.dgate};
@@ -787,48 +807,40 @@ bool vectors_ok(int dtype, const NormArgs &a)
     return true;
 }
 
-}  // namespace
-
-cudaError_t launch_norm(int dtype, const NormArgs &a, cudaStream_t stream)
+template <typename T>
+cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
     const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads);
-    DC_DTYPE_SWITCH(dtype, T, {
-        constexpr int V = kVec<T>;
-        if (a.D > kWideD)
-            return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
-                       : norm_launch<T, 1, false, false, 1024>(a, p, stream);
-        if (!vec)
-            return p.stages ? norm_launch<T, 1, false, true, kNarrow>(a, p, stream)
-                            : norm_launch<T, 1, false, false, kNarrow>(a, p, stream);
-        if (!p.stages) return norm_launch<T, V, false, false, kNarrow>(a, p, stream);
-        return full ? norm_launch<T, V, true, true, kNarrow>(a, p, stream)
-                    : norm_launch<T, V, false, true, kNarrow>(a, p, stream);
-    })
+    constexpr int V = kVec<T>;
+    if (a.D > kWideD)
+        return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
+                   : norm_launch<T, 1, false, false, 1024>(a, p, stream);
+    if (!vec)
+        return p.stages ? norm_launch<T, 1, false, true, kNarrow>(a, p, stream)
+                        : norm_launch<T, 1, false, false, kNarrow>(a, p, stream);
+    if (!p.stages) return norm_launch<T, V, false, false, kNarrow>(a, p, stream);
+    return full ? norm_launch<T, V, true, true, kNarrow>(a, p, stream)
+                : norm_launch<T, V, false, true, kNarrow>(a, p, stream);
 }
 
-size_t norm_grad_workspace(int dtype, int64_t rows, int D)
-{
-    return size_t(grad_runs(dtype, rows, D)) * kSlots * size_t(D) * sizeof(float);
-}
-
-cudaError_t launch_norm_grad(int dtype, const NormArgs &a, float *partial, cudaStream_t stream)
+template <typename T>
+cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
     const Plan p = plan_for(a.D, 4, dtype_bytes(dtype), kGradThreads);
     const int64_t P = grad_runs(dtype, a.rows, a.D);
-    DC_DTYPE_SWITCH(dtype, T, {
-        constexpr int V = kVec<T>;
-        if (a.D > kWideD)
-            return vec ? norm_grad_launch<T, V, false, false, 1024>(a, partial, P, p, stream)
-                       : norm_grad_launch<T, 1, false, false, 1024>(a, partial, P, p, stream);
-        if (!vec)
-            return p.stages ? norm_grad_launch<T, 1, false, true, kNarrow>(a, partial, P, p, stream)
-                            : norm_grad_launch<T, 1, false, false, kNarrow>(a, partial, P, p, stream);
-        if (!p.stages) return norm_grad_launch<T, V, false, false, kNarrow>(a, partial, P, p, stream);
-        return full ? norm_grad_launch<T, V, true, true, kNarrow>(a, partial, P, p, stream)
-                    : norm_grad_launch<T, V, false, true, kNarrow>(a, partial, P, p, stream);
-    })
+    constexpr int V = kVec<T>;
+    if (a.D > kWideD)
+        return vec ? norm_grad_launch<T, V, false, false, 1024>(a, partial, P, p, stream)
+                   : norm_grad_launch<T, 1, false, false, 1024>(a, partial, P, p, stream);
+    if (!vec)
+        return p.stages ? norm_grad_launch<T, 1, false, true, kNarrow>(a, partial, P, p, stream)
+                        : norm_grad_launch<T, 1, false, false, kNarrow>(a, partial, P, p, stream);
+    if (!p.stages) return norm_grad_launch<T, V, false, false, kNarrow>(a, partial, P, p, stream);
+    return full ? norm_grad_launch<T, V, true, true, kNarrow>(a, partial, P, p, stream)
+                : norm_grad_launch<T, V, false, true, kNarrow>(a, partial, P, p, stream);
 }
 
+}  // namespace norms
 }  // namespace dc
