@@ -394,6 +394,24 @@ constexpr int kSlots = 4;
 // when the gate row changes. For shorter ones that would cost more than the second sum.
 constexpr int kLongGate = 8;
 
+// A thread's own floats in shared memory: pairs i and i + 1 (i even) in one access.
+struct Own {
+    float4 *at;
+    int size;
+
+    __device__ __forceinline__ void put(int i, float2 a, float2 b) const
+    {
+        at[i / 2 * size] = make_float4(a.x, a.y, b.x, b.y);
+    }
+    __device__ __forceinline__ void get(int i, float2 (&v)[2]) const
+    {
+        const float4 q = at[i / 2 * size];
+        v[0] = make_float2(q.x, q.y);
+        v[1] = make_float2(q.z, q.w);
+    }
+};
+constexpr int kOwn = 2;
+
 template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : 1)
 norm_grad_kernel(NormArgs a, float *partial, int stages)
@@ -410,16 +428,23 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
     const int64_t r0 = run_start(a.rows, P, b), r1 = run_start(a.rows, P, b + 1);
     const T *src[4] = {HAS_H ? static_cast<const T *>(a.x) : nullptr, static_cast<const T *>(a.dh),
                        static_cast<const T *>(a.dy), HAS_F ? static_cast<const T *>(a.f) : nullptr};
-    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
+    // This thread's w_pre and (LONG) gate * w_post * scale as floats, four to an access: in
+    // shared memory, where they cost no registers and no conversions.
+    const Own own_pre{reinterpret_cast<float4 *>(dyn) + lane, size};
+    const Own own_gp{own_pre.at + (kElems / 4) * size, size};
+    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn + kOwn * kElems * size * sizeof(float), bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
     if (RING) ring.start();
-    R pre, post, gate;
-    if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
+    R post, gate;
+    if (HAS_H) {
+        post.load_or_ones(a.w_pre, D, lane, size);
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) own_pre.put(i, post.get(i), post.get(i + 1));
+    }
     if (HAS_F) {
         post.load_or_ones(a.w_post, D, lane, size);
         gate.fill(1.0f);
     }
     float2 gpre[kPairs], gpost[kPairs], ggate[kPairs];  // LONG: ggate holds A, gpost is in memory
-    float2 gp[kPairs];                                  // LONG: gate * w_post * scale
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) gpost[i] = gpre[i] = ggate[i] = twice(0.0f);
     float *slots = partial + b * int64_t(kSlots) * D;
@@ -435,9 +460,9 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         if (a.gate) gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
         if (LONG) {
             post.load_or_ones(a.w_post, D, lane, size);
+            auto gp = [&](int i) { return __fmul2_rn(__fmul2_rn(gate.get(i), post.get(i)), twice(a.drop.scale)); };
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i)
-                gp[i] = __fmul2_rn(__fmul2_rn(gate.get(i), post.get(i)), twice(a.drop.scale));
+            for (int i = 0; i < kPairs; i += 2) own_gp.put(i, gp(i), gp(i + 1));
         }
     };
     int64_t g = 0, g_end = r0;
@@ -483,11 +508,13 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         auto sums = [&] {
 #pragma unroll
             for (int i = 0; i < 6; ++i) q[i] = twice(0.0f);
+            float2 pre[2];
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
                 if (HAS_H) {
+                    if (i % 2 == 0) own_pre.get(i, pre);
                     const float2 v = R::only_inside(__fadd2_rn(y.get(i), y0), i, D, lane, size);
-                    const float2 dn = __fmul2_rn(dh.get(i), pre.get(i));
+                    const float2 dn = __fmul2_rn(dh.get(i), pre[i % 2]);
                     q[1] = __ffma2_rn(v, v, q[1]);
                     q[5] = __ffma2_rn(dn, v, q[5]);
                     if (a.layer) {
@@ -562,11 +589,13 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) t[i] = twice(0.0f);
         }
+        float2 w2[2];
         if (HAS_H) {
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
+                if (i % 2 == 0) own_pre.get(i, w2);
                 const float2 yhat = __fmul2_rn(__fadd2_rn(y.get(i), ym), yr), d = dh.get(i);
-                t[i] = __ffma2_rn(yr, __ffma2_rn(yhat, proj, __ffma2_rn(d, pre.get(i), dm)), t[i]);
+                t[i] = __ffma2_rn(yr, __ffma2_rn(yhat, proj, __ffma2_rn(d, w2[i % 2], dm)), t[i]);
                 gpre[i] = __ffma2_rn(d, yhat, gpre[i]);
             }
         }
@@ -585,7 +614,8 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
             float2 kt = R::only_inside(t[i], i, D, lane, size);
             if (LONG) {
-                t[i] = __fmul2_rn(kt, gp[i]);
+                if (i % 2 == 0) own_gp.get(i, w2);
+                t[i] = __fmul2_rn(kt, w2[i % 2]);
                 ggate[i] = __ffma2_rn(kt, fhat, ggate[i]);
             } else {
                 kt = __fmul2_rn(kt, scale);
@@ -724,18 +754,19 @@ struct Plan {
     int blocks, stages;
     size_t smem;
 };
-inline Plan plan_for(int D, int arrays, int bytes, int threads)
+inline Plan plan_for(int D, int arrays, int bytes, int threads, int own)
 {
     Plan p;
     const int size = row_threads(D);
     p.blocks = threads / size < 1 ? 1 : threads / size;
     if (p.blocks > 16) p.blocks = 16;
+    const size_t fixed = 2048 + size_t(own) * size * kElems * sizeof(float);
     const size_t row = size_t(arrays) * ((size_t(D) * bytes + 15) / 16 * 16 + 16), room = size_t(224) << 10;
-    while (p.blocks > 1 && room / p.blocks < 2 * row + 2048) --p.blocks;
-    const size_t slots = room / p.blocks > 2048 ? (room / p.blocks - 2048) / row : 0;
+    while (p.blocks > 1 && room / p.blocks < 2 * row + fixed) --p.blocks;
+    const size_t slots = room / p.blocks > fixed ? (room / p.blocks - fixed) / row : 0;
     p.stages = int(slots < kMaxStages ? slots : kMaxStages);
     if (p.stages < 2) p.stages = 0;
-    p.smem = p.stages * row;
+    p.smem = p.stages * row + fixed - 2048;
     return p;
 }
 constexpr int kSms = 152;
@@ -743,7 +774,7 @@ constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM
 
 inline int64_t grad_runs(int dtype, int64_t rows, int D)
 {
-    const int64_t most = int64_t(kSms) * plan_for(D, 4, dtype_bytes(dtype), kGradThreads).blocks;
+    const int64_t most = int64_t(kSms) * plan_for(D, 4, dtype_bytes(dtype), kGradThreads, kOwn).blocks;
     return rows < most ? rows : most;
 }
 
@@ -778,7 +809,7 @@ cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const
                   : a.f       ? norm_grad_kernel<T, V, FULL, true, false, false, RING, MAXT>
                               : norm_grad_kernel<T, V, FULL, false, true, false, RING, MAXT>;
     static DeviceCache cache[4];
-    if (RING) {
+    {
         int ready = 0;
         const cudaError_t e = cache[a.f && a.dh ? lg : a.f ? 2 : 3].get(ready, [&](int &v) {
             v = 1;
@@ -786,7 +817,7 @@ cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const
         });
         if (e != cudaSuccess) return e;
     }
-    kernel<<<unsigned(P), unsigned(row_threads(a.D)), RING ? p.smem : 0, stream>>>(a, partial, p.stages);
+    kernel<<<unsigned(P), unsigned(row_threads(a.D)), p.smem, stream>>>(a, partial, p.stages);
     const int64_t gates = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate;
     const bool few = gates < P;
     if (a.dw_post || a.dw_pre || (a.dgate && few)) {
@@ -811,7 +842,7 @@ template <typename T>
 cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
-    const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads);
+    const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads, 0);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
         return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
@@ -828,7 +859,7 @@ template <typename T>
 cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
-    const Plan p = plan_for(a.D, 4, dtype_bytes(dtype), kGradThreads);
+    const Plan p = plan_for(a.D, 4, dtype_bytes(dtype), kGradThreads, kOwn);
     const int64_t P = grad_runs(dtype, a.rows, a.D);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
