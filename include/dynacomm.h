@@ -326,14 +326,20 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
  * dx and count in no dW; an expert of no rows gets dW_e = 0. An offset outside [0, rows],
  * or below an earlier one, counts as the nearest valid value. w and dw have the strides
  * w_expert, w_n, w_k (elements); one of w_n and w_k is 1.
- * 16-bit operands whose rows start on 16-byte boundaries run on the tensor cores; 2 to
- * a few rows in all by a pass that streams the weights over every SM; others on the
- * CUDA cores. status (device, nullable): set to DC_ERR_INTERNAL if a kernel gave up a
- * wait (its outputs are then incomplete), else left as it is.
+ * 16-bit operands run on the tensor cores; those whose rows start off 16-byte boundaries
+ * are first copied into the workspace, row by row, so that they start on them. Up to
+ * DC_FEW_ROWS rows in all take a pass that streams the weights over every SM; float
+ * operands run on the CUDA cores. workspace: dc_expert_workspace_bytes(shape, product, a,
+ * b) bytes, 256-byte aligned, used during the call's kernels only, where product is 0 for
+ * y, 1 for dx, 2 for dW and a, b are the call's two operands in its order (their addresses
+ * decide whether copies are needed); NULL where that is 0. status (device, nullable): set
+ * to DC_ERR_INTERNAL if a kernel gave up a wait (its outputs are then incomplete), else left
+ * as it is.
  * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; rows outside [0, 2^31 - 1]; experts
  * outside [1, DC_EXPERTS_MAX]; N or K outside [1, DC_LAYER_DIM_MAX]; a stride shorter than its
- * row, or above 2^40); DC_ERR_CUDA.
+ * row, or above 2^40); DC_ERR_WORKSPACE; DC_ERR_CUDA.
  * ---------------------------------------------------------------------- */
+#define DC_FEW_ROWS 16
 typedef struct dc_expert_shape {
     int32_t dtype; /* of x, y, w and their gradients */
     int32_t experts;
@@ -343,13 +349,18 @@ typedef struct dc_expert_shape {
     int64_t w_expert, w_n, w_k; /* w[e][n][k] or dw[e][n][k] */
 } dc_expert_shape;
 
+size_t dc_expert_workspace_bytes(const dc_expert_shape *shape, int32_t product, const void *a,
+                                 const void *b);
 dc_status dc_expert_matmul(const dc_expert_shape *shape, const void *x, const void *w,
-                           const int64_t *offsets, void *y, int32_t *status, cudaStream_t stream);
+                           const int64_t *offsets, void *y, int32_t *status, void *workspace,
+                           size_t workspace_bytes, cudaStream_t stream);
 dc_status dc_expert_matmul_grad_input(const dc_expert_shape *shape, const void *dy, const void *w,
                                       const int64_t *offsets, void *dx, int32_t *status,
+                                      void *workspace, size_t workspace_bytes,
                                       cudaStream_t stream);
 dc_status dc_expert_matmul_grad_weight(const dc_expert_shape *shape, const void *dy, const void *x,
                                        const int64_t *offsets, void *dw, int32_t *status,
+                                       void *workspace, size_t workspace_bytes,
                                        cudaStream_t stream);
 
 /* ------------------------------------------------------------------------

@@ -408,53 +408,44 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
     return cudaLaunchKernelEx(&lc, kernel, ma, mb, a);
 }
 
-bool copies_ok(const void *p, int64_t stride) { return aligned16(p) && stride % 8 == 0; }
-
 }  // namespace
 
-bool expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream, cudaError_t &e)
+// Operands on 16-byte boundaries, as expert_dispatch.cu has made sure.
+cudaError_t expert_mma_rows(bool bf16, const ExpertArgs &g, cudaStream_t stream)
 {
     const bool k_major = g.b_r == 1;
     const int64_t stride = k_major ? g.b_n : g.b_r;
-    if (dtype == DC_FP32 || !copies_ok(g.a, g.a_m) || !copies_ok(g.b, stride)) return false;
     const int64_t inner = k_major ? g.r : g.n, outer = k_major ? g.n : g.r;
-    int64_t expert = g.b_e;
-    if (g.experts == 1) expert = stride * outer;  // not used, but it has to be valid
-    if (expert % 8) return false;
+    // with one expert the stride between experts is not used, but it has to be valid
+    const int64_t expert = g.experts == 1 ? stride * outer : g.b_e;
     CUtensorMap ma, mb;
-    const bool bf16 = dtype == DC_BF16;
     if (!make_map(ma, bf16, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
         !make_map(mb, bf16, g.a, g.r, g.rows, 1, g.a_m, 0, 64))
-        return false;
+        return cudaErrorInvalidValue;
     MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false};
     a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;
     constexpr int BN = 256;
     const int64_t tiles = (g.rows / BN + g.experts + 2) * ((g.n + 255) / 256);
     if (bf16)
-        e = k_major ? launch_typed<__nv_bfloat16, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
-                    : launch_typed<__nv_bfloat16, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
-    else
-        e = k_major ? launch_typed<__half, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
-                    : launch_typed<__half, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
-    return true;
+        return k_major ? launch_typed<__nv_bfloat16, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
+                       : launch_typed<__nv_bfloat16, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
+    return k_major ? launch_typed<__half, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
+                   : launch_typed<__half, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
 }
 
-bool expert_mma_weights(int dtype, const ExpertArgs &g, cudaStream_t stream, cudaError_t &e)
+cudaError_t expert_mma_weights(bool bf16, const ExpertArgs &g, cudaStream_t stream)
 {
-    if (dtype == DC_FP32 || g.rows == 0 || !copies_ok(g.a, g.a_r) || !copies_ok(g.b, g.b_r)) return false;
     CUtensorMap ma, mb;
-    const bool bf16 = dtype == DC_BF16;
     if (!make_map(ma, bf16, g.a, g.m, g.rows, 1, g.a_r, 0, 64) ||
         !make_map(mb, bf16, g.b, g.n, g.rows, 1, g.b_r, 0, 64))
-        return false;
+        return cudaErrorInvalidValue;
     MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false};
     a.wide = g.c_m % 8 == 0 && g.c_e % 8 == 0 && aligned16(g.c);
     constexpr int BN = 256;
     const int64_t tiles = int64_t(g.experts) * ((g.m + 255) / 256) * ((g.n + BN - 1) / BN);
-    if (tiles > (int64_t(1) << 30)) return false;
-    e = bf16 ? launch_typed<__nv_bfloat16, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream)
-             : launch_typed<__half, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream);
-    return true;
+    if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;
+    return bf16 ? launch_typed<__nv_bfloat16, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream)
+                : launch_typed<__half, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream);
 }
 
 }  // namespace dc

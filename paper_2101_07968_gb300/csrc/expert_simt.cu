@@ -86,30 +86,22 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g)
 
 }  // namespace
 
-cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, cudaStream_t stream)
+cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream)
 {
-    cudaError_t e = cudaSuccess;
-    if (expert_mma_rows(dtype, a, stream, e)) return e;
     // at most one short tile per segment
     const int64_t tiles = a.rows / kTile + a.experts + 2;
     const unsigned ty = unsigned(tiles < 32768 ? tiles : 32768);
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), ty, unsigned((tiles + ty - 1) / ty));
-    DC_DTYPE_SWITCH(dtype, T, {
-        expert_simt_kernel<T, false><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a);
-        return cudaGetLastError();
-    })
+    expert_simt_kernel<float, false><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a);
+    return cudaGetLastError();
 }
 
-cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, cudaStream_t stream)
+cudaError_t expert_simt_weights(const ExpertArgs &a, cudaStream_t stream)
 {
-    cudaError_t e = cudaSuccess;
-    if (expert_mma_weights(dtype, a, stream, e)) return e;
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), unsigned((a.m + kTile - 1) / kTile),
                     unsigned(a.experts));
-    DC_DTYPE_SWITCH(dtype, T, {
-        expert_simt_kernel<T, true><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a);
-        return cudaGetLastError();
-    })
+    expert_simt_kernel<float, true><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace dc

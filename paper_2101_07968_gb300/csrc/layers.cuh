@@ -137,11 +137,16 @@ struct ExpertArgs {
     int32_t experts, m, n, r;  // rows: m unused; weights: r unused
     int32_t *status;
 };
-cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
-cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, cudaStream_t stream);
-// on the tensor cores (expert_mma.cu): false, and nothing launched, for operands they do
-// not take
-bool expert_mma_rows(int dtype, const ExpertArgs &a, cudaStream_t stream, cudaError_t &e);
-bool expert_mma_weights(int dtype, const ExpertArgs &a, cudaStream_t stream, cudaError_t &e);
+size_t expert_workspace(int dtype, const ExpertArgs &a, bool weights);
+cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, void *workspace, cudaStream_t stream);
+cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, void *workspace,
+                                  cudaStream_t stream);
+// the kernels behind them: 16-bit operands on 16-byte boundaries on the tensor cores
+// (expert_mma.cu), few rows of any type (expert_few.cu), floats (expert_simt.cu)
+cudaError_t expert_mma_rows(bool bf16, const ExpertArgs &a, cudaStream_t stream);
+cudaError_t expert_mma_weights(bool bf16, const ExpertArgs &a, cudaStream_t stream);
+cudaError_t expert_few_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
+cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream);
+cudaError_t expert_simt_weights(const ExpertArgs &a, cudaStream_t stream);
 
 }  // namespace dc

@@ -41,6 +41,57 @@ dc_status check_experts(const dc_expert_shape *s)
     return DC_OK;
 }
 
+// y, dx or dW (product 0, 1, 2) of operands a and b as one strided product
+ExpertArgs expert_args(const dc_expert_shape *s, int product, const void *a, const void *b,
+                       const int64_t *offsets, void *c, int32_t *status)
+{
+    ExpertArgs g = {};
+    g.c = c;
+    g.offsets = offsets;
+    g.rows = s->rows;
+    g.experts = s->experts;
+    g.status = status;
+    if (product < 2) {
+        g.a = a;
+        g.b = b;
+        g.a_r = g.c_n = 1;
+        g.b_e = s->w_expert;
+        g.a_m = product ? s->ldy : s->ldx;
+        g.c_m = product ? s->ldx : s->ldy;
+        g.b_n = product ? s->w_k : s->w_n;
+        g.b_r = product ? s->w_n : s->w_k;
+        g.n = product ? s->K : s->N;
+        g.r = product ? s->N : s->K;
+    } else {  // dw[e][n][k], or its transpose: the kernels take C with contiguous columns
+        const bool nk = s->w_k == 1;
+        g.a = nk ? a : b;
+        g.b = nk ? b : a;
+        g.a_m = g.b_n = g.c_n = 1;
+        g.a_r = nk ? s->ldy : s->ldx;
+        g.b_r = nk ? s->ldx : s->ldy;
+        g.c_e = s->w_expert;
+        g.c_m = nk ? s->w_n : s->w_k;
+        g.m = nk ? s->N : s->K;
+        g.n = nk ? s->K : s->N;
+    }
+    return g;
+}
+
+dc_status expert_product(const dc_expert_shape *s, int product, const void *a, const void *b,
+                         const int64_t *offsets, void *c, int32_t *status, void *workspace,
+                         size_t workspace_bytes, cudaStream_t stream)
+{
+    const dc_status st = check_experts(s);
+    if (st != DC_OK) return st;
+    if (s->rows == 0 && product < 2) return DC_OK;
+    if (!offsets || !c || (s->rows > 0 && (!a || !b))) return DC_ERR_NULL;
+    const ExpertArgs g = expert_args(s, product, a, b, offsets, c, status);
+    const size_t need = s->rows ? expert_workspace(s->dtype, g, product == 2) : 0;
+    if (need && (!workspace || workspace_bytes < need)) return DC_ERR_WORKSPACE;
+    return result(product < 2 ? launch_expert_rows(s->dtype, g, workspace, stream)
+                              : launch_expert_weights(s->dtype, g, workspace, stream));
+}
+
 dc_status check_drop(double p, int64_t offset)
 {
     return p >= 0.0 && p <= 1.0 && offset >= 0 ? DC_OK : DC_ERR_BAD_LAYER;
@@ -74,64 +125,37 @@ NormArgs norm_args(const dc_block_norm_cfg *c)
 
 extern "C" {
 
+size_t dc_expert_workspace_bytes(const dc_expert_shape *s, int32_t product, const void *a,
+                                 const void *b)
+{
+    if (dc::check_experts(s) != DC_OK || product < 0 || product > 2 || s->rows == 0) return 0;
+    return dc::expert_workspace(s->dtype, dc::expert_args(s, product, a, b, nullptr, nullptr, nullptr),
+                                product == 2);
+}
+
 dc_status dc_expert_matmul(const dc_expert_shape *s, const void *x, const void *w,
-                           const int64_t *offsets, void *y, int32_t *status, cudaStream_t stream)
+                           const int64_t *offsets, void *y, int32_t *status, void *workspace,
+                           size_t workspace_bytes, cudaStream_t stream)
 {
     const dc::NvtxRange nvtx("dc_expert_matmul");
-    const dc_status st = dc::check_experts(s);
-    if (st != DC_OK) return st;
-    if (s->rows == 0) return DC_OK;
-    if (!x || !w || !offsets || !y) return DC_ERR_NULL;
-    const dc::ExpertArgs a = {x,       w,         y,       s->ldx, 1,          s->w_expert, s->w_n,
-                              s->w_k,  0,         s->ldy,  1,      offsets,    s->rows,     s->experts,
-                              0,       s->N,      s->K,    status};
-    return dc::result(dc::launch_expert_rows(s->dtype, a, stream));
+    return dc::expert_product(s, 0, x, w, offsets, y, status, workspace, workspace_bytes, stream);
 }
 
 dc_status dc_expert_matmul_grad_input(const dc_expert_shape *s, const void *dy, const void *w,
                                       const int64_t *offsets, void *dx, int32_t *status,
-                                      cudaStream_t stream)
+                                      void *workspace, size_t workspace_bytes, cudaStream_t stream)
 {
     const dc::NvtxRange nvtx("dc_expert_matmul_grad_input");
-    const dc_status st = dc::check_experts(s);
-    if (st != DC_OK) return st;
-    if (s->rows == 0) return DC_OK;
-    if (!dy || !w || !offsets || !dx) return DC_ERR_NULL;
-    const dc::ExpertArgs a = {dy,      w,         dx,      s->ldy, 1,          s->w_expert, s->w_k,
-                              s->w_n,  0,         s->ldx,  1,      offsets,    s->rows,     s->experts,
-                              0,       s->K,      s->N,    status};
-    return dc::result(dc::launch_expert_rows(s->dtype, a, stream));
+    return dc::expert_product(s, 1, dy, w, offsets, dx, status, workspace, workspace_bytes, stream);
 }
 
 dc_status dc_expert_matmul_grad_weight(const dc_expert_shape *s, const void *dy, const void *x,
                                        const int64_t *offsets, void *dw, int32_t *status,
+                                       void *workspace, size_t workspace_bytes,
                                        cudaStream_t stream)
 {
     const dc::NvtxRange nvtx("dc_expert_matmul_grad_weight");
-    const dc_status st = dc::check_experts(s);
-    if (st != DC_OK) return st;
-    if (!offsets || !dw || (s->rows > 0 && (!dy || !x))) return DC_ERR_NULL;
-    // dw[e][n][k]: the kernels take C with its columns contiguous
-    const bool nk = s->w_k == 1;
-    const dc::ExpertArgs a = {nk ? dy : x,
-                              nk ? x : dy,
-                              dw,
-                              1,
-                              nk ? s->ldy : s->ldx,
-                              0,
-                              1,
-                              nk ? s->ldx : s->ldy,
-                              s->w_expert,
-                              nk ? s->w_n : s->w_k,
-                              1,
-                              offsets,
-                              s->rows,
-                              s->experts,
-                              nk ? s->N : s->K,
-                              nk ? s->K : s->N,
-                              0,
-                              status};
-    return dc::result(dc::launch_expert_weights(s->dtype, a, stream));
+    return dc::expert_product(s, 2, dy, x, offsets, dw, status, workspace, workspace_bytes, stream);
 }
 
 dc_status dc_gated_unit(int32_t dtype, int32_t act, int64_t rows, int32_t F, const void *h,

@@ -32,7 +32,7 @@ FWD, BWD = 0, 1
 DC_BF16, DC_FP16, DC_FP32 = 0, 1, 2
 DC_ACT_SILU, DC_ACT_GELU = 0, 1
 DC_NORM_RMS, DC_NORM_LAYER = 0, 1
-DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX = 1024, 1048576, 16384
+DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX, DC_FEW_ROWS = 1024, 1048576, 16384, 16
 
 
 class DynaCommError(RuntimeError):
@@ -101,9 +101,10 @@ _SIGNATURES = {
     "dc_status_string": (ctypes.c_char_p, [_I32]),
     "dc_roof_int_probe": (_I32, [_I32, _I32, _I32, _I64, _VP, _VP]),
     "dc_time_next_pass": (_I32, [_VP, _VP]),
-    "dc_expert_matmul": (_I32, [_SHAPE, _VP, _VP, _VP, _VP, _VP, _VP]),
-    "dc_expert_matmul_grad_input": (_I32, [_SHAPE, _VP, _VP, _VP, _VP, _VP, _VP]),
-    "dc_expert_matmul_grad_weight": (_I32, [_SHAPE, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "dc_expert_workspace_bytes": (_SZ, [_SHAPE, _I32, _VP, _VP]),
+    "dc_expert_matmul": (_I32, [_SHAPE] + [_VP] * 6 + [_SZ, _VP]),
+    "dc_expert_matmul_grad_input": (_I32, [_SHAPE] + [_VP] * 6 + [_SZ, _VP]),
+    "dc_expert_matmul_grad_weight": (_I32, [_SHAPE] + [_VP] * 6 + [_SZ, _VP]),
     "dc_gated_unit": (_I32, [_I32, _I32, _I64, _I32, _VP, _I64, _VP, _I64, _VP]),
     "dc_gated_unit_grad": (_I32, [_I32, _I32, _I64, _I32, _VP, _I64, _VP, _I64, _VP, _I64, _VP]),
     "dc_dropout": (_I32, [_I32, _I64, _I32, _VP, _I64, _VP, _I64, _VP, _I64, _F64, _U64, _I64,

@@ -36,10 +36,8 @@ def _dtype(t) -> int:
 
 
 def _like(name, t, ref, shape):
-    """t has ref's type and device and the given shape."""
-    if not t.is_cuda:
-        raise ValueError("device tensor expected (the library takes device pointers)")
-    if t.dtype != ref.dtype or t.device != ref.device or tuple(t.shape) != tuple(shape):
+    """t has ref's type and device and the given shape (ref is on a device)."""
+    if t.dtype != ref.dtype or t.shape != shape or t.device != ref.device:
         raise ValueError(f"{name}: {tuple(shape)} {ref.dtype} on {ref.device} expected, not "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
 
@@ -51,19 +49,35 @@ def _rows(name, t) -> int:
     if t.dim() != 2:
         raise ValueError(f"{name}: two dimensions expected")
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    ld, one = t.stride()
+    if cols > 1 and one != 1:
         raise ValueError(f"{name}: contiguous rows expected")
     if rows <= 1:
         return cols
-    if t.stride(0) < cols:
+    if ld < cols:
         raise ValueError(f"{name}: rows that do not overlap expected")
-    return t.stride(0)
+    return ld
 
 
 def _run(name, t, stream, *args):
     """One call of the library on t's device."""
-    with torch.cuda.device(t.device):
-        dc._check(int(getattr(dc.lib(), name)(*args, dc._stream(stream))), name)
+    fn = getattr(dc._lib or dc.lib(), name)
+    if t.get_device() == torch._C._cuda_getDevice():
+        st = fn(*args, dc._stream(stream))
+    else:
+        with torch.cuda.device(t.device):
+            st = fn(*args, dc._stream(stream))
+    if st:
+        raise dc.DynaCommError(st, name)
+
+
+def _used_on(ws, stream):
+    """A workspace goes back to the allocator when the call returns; tell it of a stream other
+    than the current one that still uses it."""
+    if ws is not None and stream is not None:
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=ws.device)
+        ws.record_stream(stream)
 
 
 # ------------------------------------------------------------------- expert products
@@ -71,16 +85,17 @@ _status = {}
 
 
 def _status_of(device):
-    t = _status.get(device)
-    if t is None:
-        t = _status[device] = torch.zeros(1, dtype=torch.int32, device=device)
-    return t
+    at = _status.get(device)
+    if at is None:
+        t = torch.zeros(1, dtype=torch.int32, device=device)
+        at = _status[device] = (t, t.data_ptr())
+    return at[1]
 
 
 def check_status() -> None:
     """Synchronises and raises DynaCommError if a kernel of this module has given up a wait
     (a bug of the library or a fault of the machine; the call's outputs are incomplete)."""
-    for device, t in _status.items():
+    for device, (t, _) in _status.items():
         s = int(t.item())
         if s:
             t.zero_()
@@ -105,14 +120,26 @@ def _weights(name, w):
 
 
 def _offsets(offsets, experts, ref):
-    if not offsets.is_cuda or offsets.device != ref.device or offsets.dtype != torch.int64 \
-            or offsets.dim() != 1 or offsets.numel() != experts + 1 \
-            or not offsets.is_contiguous():
+    if offsets.dtype != torch.int64 or offsets.shape != (experts + 1,) \
+            or offsets.device != ref.device or not offsets.is_contiguous():
         raise ValueError(f"offsets: {experts + 1} contiguous int64 on {ref.device} expected")
 
 
 def _shape(code, E, rows, N, K, ldx, ldy, se, sn, sk):
     return ctypes.byref(dc.dc_expert_shape(code, E, rows, N, K, ldx, ldy, se, sn, sk))
+
+
+_PRODUCTS = ("dc_expert_matmul", "dc_expert_matmul_grad_input", "dc_expert_matmul_grad_weight")
+
+
+def _product(which, shape, a, b, offsets, c, stream):
+    ap, bp = a.data_ptr(), b.data_ptr()
+    need = (dc._lib or dc.lib()).dc_expert_workspace_bytes(shape, which, ap, bp)
+    ws = a.new_empty(need, dtype=torch.uint8) if need else None
+    _run(_PRODUCTS[which], a, stream, shape, ap, bp, offsets.data_ptr(), c.data_ptr(),
+         _status_of(a.device), ws.data_ptr() if need else None, need)
+    _used_on(ws, stream)
+    return c
 
 
 def expert_matmul(x, w, offsets, stream=None):
@@ -124,11 +151,8 @@ def expert_matmul(x, w, offsets, stream=None):
     R = x.shape[0]
     _like("x", x, w, (R, K))
     _offsets(offsets, E, x)
-    y = torch.empty((R, N), dtype=x.dtype, device=x.device)
-    _run("dc_expert_matmul", x, stream, _shape(_dtype(x), E, R, N, K, ldx, N, se, sn, sk),
-         x.data_ptr(), w.data_ptr(), offsets.data_ptr(), y.data_ptr(),
-         _status_of(x.device).data_ptr())
-    return y
+    return _product(0, _shape(_dtype(x), E, R, N, K, ldx, N, se, sn, sk), x, w, offsets,
+                    x.new_empty((R, N)), stream)
 
 
 def expert_matmul_grad_input(dy, w, offsets, stream=None):
@@ -138,12 +162,8 @@ def expert_matmul_grad_input(dy, w, offsets, stream=None):
     R = dy.shape[0]
     _like("dy", dy, w, (R, N))
     _offsets(offsets, E, dy)
-    dx = torch.empty((R, K), dtype=dy.dtype, device=dy.device)
-    _run("dc_expert_matmul_grad_input", dy, stream,
-         _shape(_dtype(dy), E, R, N, K, K, ldy, se, sn, sk),
-         dy.data_ptr(), w.data_ptr(), offsets.data_ptr(), dx.data_ptr(),
-         _status_of(dy.device).data_ptr())
-    return dx
+    return _product(1, _shape(_dtype(dy), E, R, N, K, K, ldy, se, sn, sk), dy, w, offsets,
+                    dy.new_empty((R, K)), stream)
 
 
 def expert_matmul_grad_weight(dy, x, offsets, stream=None):
@@ -155,12 +175,8 @@ def expert_matmul_grad_weight(dy, x, offsets, stream=None):
     _like("x", x, dy, (R, K))
     E = offsets.numel() - 1
     _offsets(offsets, E, dy)
-    dw = torch.empty((E, N, K), dtype=dy.dtype, device=dy.device)
-    _run("dc_expert_matmul_grad_weight", dy, stream,
-         _shape(_dtype(dy), E, R, N, K, ldx, ldy, N * K, K, 1),
-         dy.data_ptr(), x.data_ptr(), offsets.data_ptr(), dw.data_ptr(),
-         _status_of(dy.device).data_ptr())
-    return dw
+    return _product(2, _shape(_dtype(dy), E, R, N, K, ldx, ldy, N * K, K, 1), dy, x, offsets,
+                    dy.new_empty((E, N, K)), stream)
 
 
 # ------------------------------------------------------------------------ gated unit
@@ -176,7 +192,7 @@ def gated_unit(h, act="silu", stream=None):
     R, F2 = h.shape
     if F2 % 2:
         raise ValueError("h: an even number of columns expected")
-    a = torch.empty((R, F2 // 2), dtype=h.dtype, device=h.device)
+    a = h.new_empty((R, F2 // 2))
     _run("dc_gated_unit", h, stream, _dtype(h), _act(act), R, F2 // 2, h.data_ptr(), ldh,
          a.data_ptr(), F2 // 2)
     return a
@@ -189,7 +205,7 @@ def gated_unit_grad(da, h, act="silu", stream=None):
     if F2 % 2:
         raise ValueError("h: an even number of columns expected")
     _like("da", da, h, (R, F2 // 2))
-    dh = torch.empty((R, F2), dtype=h.dtype, device=h.device)
+    dh = h.new_empty((R, F2))
     _run("dc_gated_unit_grad", h, stream, _dtype(h), _act(act), R, F2 // 2, da.data_ptr(), ldda,
          h.data_ptr(), ldh, dh.data_ptr(), F2)
     return dh
@@ -210,7 +226,7 @@ def dropout(x, p, seed, offset=0, residual=None, stream=None):
     if residual is not None:
         ldr, res = _rows("residual", residual), residual.data_ptr()
         _like("residual", residual, x, (R, C))
-    y = torch.empty((R, C), dtype=x.dtype, device=x.device)
+    y = x.new_empty((R, C))
     _run("dc_dropout", x, stream, _dtype(x), R, C, x.data_ptr(), ldx, res, ldr, y.data_ptr(), C,
          float(p), int(seed), int(offset))
     return y
@@ -226,19 +242,29 @@ def _norm_cfg(x, kind, rows_per_gate, residual_scale, eps, p, seed, offset):
                                 int(seed), int(offset))
 
 
+def _contiguous(name, t, ref, shape):
+    """t's address: contiguous, of ref's type and device and the given shape; None for None."""
+    if t is None:
+        return None
+    _like(name, t, ref, shape)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous tensor expected")
+    return t.data_ptr()
+
+
 def _norm_operands(x, f, gate, w_post, w_pre, rows_per_gate):
-    """Checks; the pointers of f, gate, w_post, w_pre."""
-    R, D = x.shape
+    """Checks; the pointers of x, f, gate, w_post, w_pre."""
+    if not x.is_cuda:
+        raise ValueError("device tensor expected (the library takes device pointers)")
+    if x.dim() != 2:
+        raise ValueError("x or y: two dimensions expected")
+    R, D = shape = x.shape
     if rows_per_gate is not None and rows_per_gate < 1:
         raise ValueError("rows_per_gate: at least one expected")
     gates = -(-R // rows_per_gate) if rows_per_gate else (1 if R else 0)
-    out = []
-    for name, t, shape in (("f", f, (R, D)), ("gate", gate, (gates, D)), ("w_post", w_post, (D,)),
-                           ("w_pre", w_pre, (D,))):
-        if t is not None:
-            _like(name, t, x, shape)
-        out.append(dc._ptr(t))
-    return out
+    return (_contiguous("x or y", x, x, shape), _contiguous("f", f, x, shape),
+            _contiguous("gate", gate, x, (gates, D)), _contiguous("w_post", w_post, x, (D,)),
+            _contiguous("w_pre", w_pre, x, (D,)))
 
 
 def block_norm(x, f=None, gate=None, w_post=None, w_pre=None, residual_scale=1.0, kind="rms",
@@ -247,16 +273,14 @@ def block_norm(x, f=None, gate=None, w_post=None, w_pre=None, residual_scale=1.0
     pass. x, f [rows, D] contiguous; gate [ceil(rows / rows_per_gate), D] (rows_per_gate None:
     one gate for all rows); w_post, w_pre [D]; any of the three None for ones. f None: the
     first norm alone, y is x. want_h False: the last residual alone, h is None."""
-    if x.dim() != 2:
-        raise ValueError("x: two dimensions expected")
-    xp = dc._ptr(x)
-    fp, gp, pp, ep = _norm_operands(x, f, gate, w_post, w_pre, rows_per_gate)
+    xp, fp, gp, pp, ep = _norm_operands(x, f, gate, w_post, w_pre, rows_per_gate)
     if f is None and not want_h:
         raise ValueError("f or want_h expected: there is nothing to compute")
     cfg = _norm_cfg(x, kind, rows_per_gate, residual_scale, eps, p, seed, offset)
     y = torch.empty_like(x) if f is not None else None
     h = torch.empty_like(x) if want_h else None
-    _run("dc_block_norm", x, stream, ctypes.byref(cfg), xp, fp, gp, pp, ep, dc._ptr(y), dc._ptr(h))
+    _run("dc_block_norm", x, stream, ctypes.byref(cfg), xp, fp, gp, pp, ep,
+         None if y is None else y.data_ptr(), None if h is None else h.data_ptr())
     return (x if y is None else y), h
 
 
@@ -267,26 +291,24 @@ def block_norm_grad(dy, dh, y, f=None, gate=None, w_post=None, w_pre=None, resid
     dw_pre (float32 [D]); None for what the call did not have. dy, dh: the gradients of y and h
     (either may be None: dy zero, dh for a call without h); y: the call's output (x where f was
     None)."""
-    if y.dim() != 2:
-        raise ValueError("y: two dimensions expected")
-    yp = dc._ptr(y)
-    for name, t in (("dy", dy), ("dh", dh)):
-        if t is not None:
-            _like(name, t, y, y.shape)
+    yp, fp, gp, pp, ep = _norm_operands(y, f, gate, w_post, w_pre, rows_per_gate)
+    dyp, dhp = _contiguous("dy", dy, y, y.shape), _contiguous("dh", dh, y, y.shape)
     if dh is None and (dy is None or f is None):
         raise ValueError("dh expected, or dy and f")
-    fp, gp, pp, ep = _norm_operands(y, f, gate, w_post, w_pre, rows_per_gate)
     cfg = _norm_cfg(y, kind, rows_per_gate, residual_scale, eps, p, seed, offset)
-    D, dev = y.shape[1], y.device
-    out = {"dx": torch.empty_like(y), "df": torch.empty_like(y) if f is not None else None,
-           "dgate": torch.empty_like(gate) if f is not None and gate is not None else None,
-           "dw_post": torch.empty(D, dtype=torch.float32, device=dev)
-           if f is not None and w_post is not None else None,
-           "dw_pre": torch.empty(D, dtype=torch.float32, device=dev)
-           if dh is not None and w_pre is not None else None}
-    need = int(dc.lib().dc_block_norm_grad_workspace_bytes(ctypes.byref(cfg)))
-    ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-    _run("dc_block_norm_grad", y, stream, ctypes.byref(cfg), dc._ptr(dy), dc._ptr(dh), yp, fp, gp,
-         pp, ep, dc._ptr(out["dx"]), dc._ptr(out["df"]), dc._ptr(out["dgate"]),
-         dc._ptr(out["dw_post"]), dc._ptr(out["dw_pre"]), ws.data_ptr(), need)
+    D = y.shape[1]
+    out = {"dx": torch.empty_like(y), "df": None, "dgate": None, "dw_post": None, "dw_pre": None}
+    if f is not None:
+        out["df"] = torch.empty_like(f)
+        if gate is not None:
+            out["dgate"] = torch.empty_like(gate)
+        if w_post is not None:
+            out["dw_post"] = y.new_empty(D, dtype=torch.float32)
+    if dh is not None and w_pre is not None:
+        out["dw_pre"] = y.new_empty(D, dtype=torch.float32)
+    need = (dc._lib or dc.lib()).dc_block_norm_grad_workspace_bytes(ctypes.byref(cfg))
+    ws = y.new_empty(max(need, 1), dtype=torch.uint8)
+    _run("dc_block_norm_grad", y, stream, ctypes.byref(cfg), dyp, dhp, yp, fp, gp, pp, ep,
+         *[None if t is None else t.data_ptr() for t in out.values()], ws.data_ptr(), need)
+    _used_on(ws, stream)
     return out
