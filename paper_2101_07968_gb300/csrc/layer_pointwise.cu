@@ -126,18 +126,63 @@ cudaError_t dropout_typed(int64_t rows, int cols, const T *x, int64_t ldx, const
 }
 
 // ---------------------------------------------------------------------- gated unit
-template <typename T, int ACT>
-__device__ __forceinline__ void act_and_slope(float g, float &a, float &slope)
+// The normal distribution at -|g|, as e^(-g^2/2) s P(s) with s = 1 / (|g| / sqrt 2 + 2): e^(z^2)
+// erfc(z) is smooth in 1 / (z + k) over all z >= 0 (the variable of Shepherd and Laframboise,
+// Math. Comp. 36, 1981, for the same function). P, of degree 8 in 4 s - 1, was fitted to the
+// least largest relative error, 4.4e-8; in 32 bits it stays within 3 2^-23, so that the tail
+// keeps its digits where 1/2 (1 + erf) loses them, at two special-function operations an
+// element. normcdff took 358 us where this takes the gradient of 65,536 x 2,048 to the
+// figure at gated_grad_kernel.
+__device__ __forceinline__ float2 normal_tail(float2 g, float2 &e)
+{
+    const float2 h = __fmul2_rn(__fmul2_rn(g, g), twice(-0.72134752044448170f));  // -log2(e) / 2
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(h.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(h.y));
+    const float2 s = make_float2(__fdividef(1.0f, fabsf(g.x) * 0.70710678f + 2.0f),
+                                 __fdividef(1.0f, fabsf(g.y) * 0.70710678f + 2.0f));
+    const float2 t = __ffma2_rn(s, twice(4.0f), twice(-1.0f));
+    float2 q = twice(-0.000231977624935098f);
+    q = __ffma2_rn(q, t, twice(0.0003795158118009567f));
+    q = __ffma2_rn(q, t, twice(0.0014894097112119198f));
+    q = __ffma2_rn(q, t, twice(-0.0032200065907090902f));
+    q = __ffma2_rn(q, t, twice(-0.01074141450226307f));
+    q = __ffma2_rn(q, t, twice(0.018217826262116432f));
+    q = __ffma2_rn(q, t, twice(0.13973475992679596f));
+    q = __ffma2_rn(q, t, twice(0.3435804843902588f));
+    q = __ffma2_rn(q, t, twice(0.5107913613319397f));
+    return __fmul2_rn(__fmul2_rn(q, s), e);
+}
+
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float2 g, float2 &a, float2 &slope)
 {
     if (ACT == DC_ACT_SILU) {
-        const float s = __fdividef(1.0f, 1.0f + __expf(-g));
-        a = g * s;
-        slope = s * (1.0f + g * (1.0f - s));
+        const float2 s = make_float2(__fdividef(1.0f, 1.0f + __expf(-g.x)), __fdividef(1.0f, 1.0f + __expf(-g.y)));
+        a = __fmul2_rn(g, s);
+        slope = __fmul2_rn(s, __ffma2_rn(g, make_float2(1.0f - s.x, 1.0f - s.y), twice(1.0f)));
     } else {
-        const float cdf = normcdff(g);
-        a = g * cdf;
-        slope = cdf + g * 0.3989422804014327f * __expf(-0.5f * g * g);
+        float2 e;
+        const float2 q = normal_tail(g, e);
+        const float2 cdf = make_float2(g.x > 0.0f ? 1.0f - q.x : q.x, g.y > 0.0f ? 1.0f - q.y : q.y);
+        a = __fmul2_rn(g, cdf);
+        slope = __ffma2_rn(__fmul2_rn(g, e), twice(0.3989422804014327f), cdf);
     }
+}
+
+// pairs of a thread's V elements; V = 1 works on one
+template <typename T, int V>
+__device__ __forceinline__ float2 pair_in(const Vec<T, V> &v, int j)
+{
+    if (V == 1) return make_float2(to_float(v.e[0]), 0.0f);
+    return pair_of(&v.e[V == 1 ? 0 : j]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void pair_out(Vec<T, V> &v, int j, float2 x)
+{
+    if (V == 1)
+        v.e[0] = from_float<T>(x.x);
+    else
+        put_pair(&v.e[V == 1 ? 0 : j], x);
 }
 
 template <typename T, int ACT, int V, int U>
@@ -161,10 +206,10 @@ gated_kernel(const T *h, int64_t ldh, T *out, int64_t lda, int64_t rows, int F)
         const int64_t r = r0 + u * blockDim.y;
         if (r >= rows) break;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float a, slope;
-            act_and_slope<T, ACT>(to_float(g[u].e[j]), a, slope);
-            g[u].e[j] = from_float<T>(a * to_float(m[u].e[j]));
+        for (int j = 0; j < V; j += 2) {
+            float2 a, slope;
+            act_and_slope<ACT>(pair_in(g[u], j), a, slope);
+            pair_out(g[u], j, __fmul2_rn(a, pair_in(m[u], j)));
         }
         *reinterpret_cast<Vec<T, V> *>(out + r * lda + c) = g[u];
     }
@@ -193,12 +238,12 @@ gated_grad_kernel(const T *da, int64_t ldda, const T *h, int64_t ldh, T *dh, int
         const int64_t r = r0 + u * blockDim.y;
         if (r >= rows) break;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float a, slope;
-            act_and_slope<T, ACT>(to_float(g[u].e[j]), a, slope);
-            const float dj = to_float(d[u].e[j]);
-            g[u].e[j] = from_float<T>(dj * to_float(m[u].e[j]) * slope);
-            m[u].e[j] = from_float<T>(dj * a);
+        for (int j = 0; j < V; j += 2) {
+            float2 a, slope;
+            act_and_slope<ACT>(pair_in(g[u], j), a, slope);
+            const float2 dj = pair_in(d[u], j);
+            pair_out(g[u], j, __fmul2_rn(__fmul2_rn(dj, pair_in(m[u], j)), slope));
+            pair_out(m[u], j, __fmul2_rn(dj, a));
         }
         *reinterpret_cast<Vec<T, V> *>(dh + r * lddh + c) = g[u];
         *reinterpret_cast<Vec<T, V> *>(dh + r * lddh + F + c) = m[u];

@@ -24,6 +24,7 @@ import torch
 from . import dynacomm as dc
 
 _DTYPES = {torch.bfloat16: dc.DC_BF16, torch.float16: dc.DC_FP16, torch.float32: dc.DC_FP32}
+_empty = torch.empty
 _ACTS = {"silu": dc.DC_ACT_SILU, "gelu": dc.DC_ACT_GELU}
 _KINDS = {"rms": dc.DC_NORM_RMS, "layer": dc.DC_NORM_LAYER}
 
@@ -135,7 +136,7 @@ _PRODUCTS = ("dc_expert_matmul", "dc_expert_matmul_grad_input", "dc_expert_matmu
 def _product(which, shape, a, b, offsets, c, stream):
     ap, bp = a.data_ptr(), b.data_ptr()
     need = (dc._lib or dc.lib()).dc_expert_workspace_bytes(shape, which, ap, bp)
-    ws = a.new_empty(need, dtype=torch.uint8) if need else None
+    ws = _empty(need, dtype=torch.uint8, device=a.device) if need else None
     _run(_PRODUCTS[which], a, stream, shape, ap, bp, offsets.data_ptr(), c.data_ptr(),
          _status_of(a.device), ws.data_ptr() if need else None, need)
     _used_on(ws, stream)
@@ -152,7 +153,7 @@ def expert_matmul(x, w, offsets, stream=None):
     _like("x", x, w, (R, K))
     _offsets(offsets, E, x)
     return _product(0, _shape(_dtype(x), E, R, N, K, ldx, N, se, sn, sk), x, w, offsets,
-                    x.new_empty((R, N)), stream)
+                    _empty((R, N), dtype=x.dtype, device=x.device), stream)
 
 
 def expert_matmul_grad_input(dy, w, offsets, stream=None):
@@ -163,7 +164,7 @@ def expert_matmul_grad_input(dy, w, offsets, stream=None):
     _like("dy", dy, w, (R, N))
     _offsets(offsets, E, dy)
     return _product(1, _shape(_dtype(dy), E, R, N, K, K, ldy, se, sn, sk), dy, w, offsets,
-                    dy.new_empty((R, K)), stream)
+                    _empty((R, K), dtype=dy.dtype, device=dy.device), stream)
 
 
 def expert_matmul_grad_weight(dy, x, offsets, stream=None):
@@ -176,7 +177,7 @@ def expert_matmul_grad_weight(dy, x, offsets, stream=None):
     E = offsets.numel() - 1
     _offsets(offsets, E, dy)
     return _product(2, _shape(_dtype(dy), E, R, N, K, ldx, ldy, N * K, K, 1), dy, x, offsets,
-                    dy.new_empty((E, N, K)), stream)
+                    _empty((E, N, K), dtype=dy.dtype, device=dy.device), stream)
 
 
 # ------------------------------------------------------------------------ gated unit
@@ -192,7 +193,7 @@ def gated_unit(h, act="silu", stream=None):
     R, F2 = h.shape
     if F2 % 2:
         raise ValueError("h: an even number of columns expected")
-    a = h.new_empty((R, F2 // 2))
+    a = _empty((R, F2 // 2), dtype=h.dtype, device=h.device)
     _run("dc_gated_unit", h, stream, _dtype(h), _act(act), R, F2 // 2, h.data_ptr(), ldh,
          a.data_ptr(), F2 // 2)
     return a
@@ -205,7 +206,7 @@ def gated_unit_grad(da, h, act="silu", stream=None):
     if F2 % 2:
         raise ValueError("h: an even number of columns expected")
     _like("da", da, h, (R, F2 // 2))
-    dh = h.new_empty((R, F2))
+    dh = _empty((R, F2), dtype=h.dtype, device=h.device)
     _run("dc_gated_unit_grad", h, stream, _dtype(h), _act(act), R, F2 // 2, da.data_ptr(), ldda,
          h.data_ptr(), ldh, dh.data_ptr(), F2)
     return dh
@@ -226,7 +227,7 @@ def dropout(x, p, seed, offset=0, residual=None, stream=None):
     if residual is not None:
         ldr, res = _rows("residual", residual), residual.data_ptr()
         _like("residual", residual, x, (R, C))
-    y = x.new_empty((R, C))
+    y = _empty((R, C), dtype=x.dtype, device=x.device)
     _run("dc_dropout", x, stream, _dtype(x), R, C, x.data_ptr(), ldx, res, ldr, y.data_ptr(), C,
          float(p), int(seed), int(offset))
     return y
@@ -303,11 +304,11 @@ def block_norm_grad(dy, dh, y, f=None, gate=None, w_post=None, w_pre=None, resid
         if gate is not None:
             out["dgate"] = torch.empty_like(gate)
         if w_post is not None:
-            out["dw_post"] = y.new_empty(D, dtype=torch.float32)
+            out["dw_post"] = _empty(D, dtype=torch.float32, device=y.device)
     if dh is not None and w_pre is not None:
-        out["dw_pre"] = y.new_empty(D, dtype=torch.float32)
+        out["dw_pre"] = _empty(D, dtype=torch.float32, device=y.device)
     need = (dc._lib or dc.lib()).dc_block_norm_grad_workspace_bytes(ctypes.byref(cfg))
-    ws = y.new_empty(max(need, 1), dtype=torch.uint8)
+    ws = _empty(max(need, 1), dtype=torch.uint8, device=y.device)
     _run("dc_block_norm_grad", y, stream, ctypes.byref(cfg), dyp, dhp, yp, fp, gp, pp, ep,
          *[None if t is None else t.data_ptr() for t in out.values()], ws.data_ptr(), need)
     _used_on(ws, stream)
