@@ -17,6 +17,17 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+// One thread of a converged warp. The compiler knows that a branch on this is taken by one
+// thread, and so feeds copies and products from uniform registers directly: under a branch
+// on the lane number each such instruction took some 200 cycles.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(p));
+    return p != 0;
+}
 // the address of this CTA's shared variable in CTA `rank` of the cluster
 __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank)
 {

@@ -192,7 +192,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const int step = int(gridDim.x) / CG, first = int(blockIdx.x) / CG;
 
     if (warp == 4) {
-        if (lane == 0) {  // copies
+        if (bw::elect_one()) {  // copies
             int it = 0;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
@@ -239,7 +239,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 ok = bw::bar_wait(bar(&empty[i % STAGES]), (i / STAGES) & 1, &gave_up);
         }
     } else if (warp == 5) {
-        if (lane == 0 && rank == 0) {  // products
+        if (rank == 0 && bw::elect_one()) {  // products
             int it = 0, tile = 0;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step, ++tile) {
