@@ -100,29 +100,12 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// 32 finished columns of a lane's feature.
-template <typename T, int MODE>
-__device__ __forceinline__ void store_columns(const MmaArgs &a, const Tile &q, int feature, int c0,
-                                              const float (&v)[32])
+// 32 finished columns (rows of the batch) of a lane's feature.
+template <typename T>
+__device__ __forceinline__ void store_rows(const MmaArgs &a, const Tile &q, int feature, int c0,
+                                           const float (&v)[32])
 {
     const int lane = threadIdx.x & 31;
-    if (MODE == kWeights) {  // the lane's row of dW, 32 columns of it
-        if (feature >= a.m) return;
-        T *p = static_cast<T *>(a.c) + q.e * a.c_e + feature * a.c_m + q.n0 + c0;
-        const int n = q.cols - c0;
-        if (a.wide && n >= 32) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 8)
-                *reinterpret_cast<uint4 *>(p + j) =
-                    make_uint4(pack2(v[j], v[j + 1], T()), pack2(v[j + 2], v[j + 3], T()),
-                               pack2(v[j + 4], v[j + 5], T()), pack2(v[j + 6], v[j + 7], T()));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < n) p[j] = from_float<T>(v[j]);
-        }
-        return;
-    }
     const int n = q.cols - c0;
     T *p = static_cast<T *>(a.c) + (int64_t(q.n0) + c0) * a.c_m + feature;
     if (a.wide) {
@@ -144,6 +127,46 @@ __device__ __forceinline__ void store_columns(const MmaArgs &a, const Tile &q, i
     }
 }
 
+// Rows of dW: a lane holds a row's neighbours, so 128 bytes a row go through shared memory
+// (16-byte units, swizzled by the row) and leave as whole lines. Straight from the lanes, an
+// instruction wrote 16 bytes to each of 32 rows: 2.8 TB/s where the output is the bound.
+struct Lines {
+    uint4 u[32][8];
+};
+template <typename T>
+__device__ __forceinline__ void stage_columns(Lines &s, int unit, const float (&v)[32])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < 32; j += 8, ++unit)
+        s.u[lane][unit ^ (lane & 7)] = make_uint4(pack2(v[j], v[j + 1], T()), pack2(v[j + 2], v[j + 3], T()),
+                                                  pack2(v[j + 4], v[j + 5], T()), pack2(v[j + 6], v[j + 7], T()));
+}
+template <typename T>
+__device__ __forceinline__ void store_lines(const Lines &s, const MmaArgs &a, const Tile &q, int row0,
+                                            int c0)
+{
+    constexpr int V = 16 / sizeof(T), kCols = 8 * V;
+    const int lane = threadIdx.x & 31;
+    const int n = min(kCols, q.cols - c0);
+    T *p = static_cast<T *>(a.c) + q.e * a.c_e + row0 * a.c_m + q.n0 + c0;
+    __syncwarp();
+    if (a.wide && n % V == 0) {
+        const int unit = lane & 7;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const int row = i + (lane >> 3);
+            if (row0 + row < a.m && unit * V < n)
+                *reinterpret_cast<uint4 *>(p + row * a.c_m + unit * V) = s.u[row][unit ^ (row & 7)];
+        }
+    } else {
+        for (int row = 0; row < 32 && row0 + row < a.m; ++row)
+            for (int c = lane; c < n; c += 32)
+                p[row * a.c_m + c] = reinterpret_cast<const T *>(&s.u[row][(c / V) ^ (row & 7)])[c % V];
+    }
+    __syncwarp();
+}
+
 template <typename T, int MODE, int CG, int BN, int STAGES>
 __global__ void __launch_bounds__(kThreads, 1)
 expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -155,6 +178,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     extern __shared__ unsigned char dyn[];
     __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
     __shared__ uint32_t tmem_at, gave_up;
+    __shared__ alignas(16) Lines lines[MODE == kWeights ? 4 : 1];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? bw::cluster_rank() : 0;
@@ -324,7 +348,13 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     __syncwarp();
                     if (lane == 0) bw::bar_arrive_cluster(lead(&free_[half]));
                 }
-                store_columns<T, MODE>(a, q, feature, c0, v);
+                if (MODE == kWeights) {
+                    stage_columns<T>(lines[warp], c0 / 8 % 8, v);
+                    if (c0 % 64 || c0 + 32 >= q.cols)
+                        store_lines<T>(lines[warp], a, q, feature - lane, c0 & ~63);
+                } else {
+                    store_rows<T>(a, q, feature, c0, v);
+                }
             }
         }
     }
