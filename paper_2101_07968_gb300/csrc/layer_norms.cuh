@@ -289,7 +289,31 @@ __host__ __device__ inline int64_t run_start(int64_t rows, int64_t P, int64_t b)
     return rows * b / P;
 }
 
-template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool RING, int MAXT>
+// A thread's own floats in shared memory: pairs i and i + 1 (i even) in one access.
+struct Own {
+    float4 *at;
+    int size;
+
+    __device__ __forceinline__ void put(int i, float2 a, float2 b) const
+    {
+        at[i / 2 * size] = make_float4(a.x, a.y, b.x, b.y);
+    }
+    __device__ __forceinline__ void get(int i, float2 (&v)[2]) const
+    {
+        const float4 q = at[i / 2 * size];
+        v[0] = make_float2(q.x, q.y);
+        v[1] = make_float2(q.z, q.w);
+    }
+};
+constexpr int kOwn = 2;
+
+// Gate rows of at least this many rows (LONG) are worked out once: gate * w_post * scale waits in
+// shared memory. For the gradient one sum A of t * fhat then serves both the gate's
+// gradient (w_post A) and, gate by gate, w_post's (gate A), which is added to the run's sums when
+// the gate row changes. For shorter ones that costs more than it saves.
+constexpr int kLongGate = 8;
+
+template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(NormArgs a, int stages)
 {
     using R = Row<T, V, FULL>;
@@ -303,20 +327,36 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
     const int64_t r0 = run_start(a.rows, gridDim.x, blockIdx.x);
     const int64_t r1 = run_start(a.rows, gridDim.x, blockIdx.x + 1);
     const T *xp = static_cast<const T *>(a.x), *fp = static_cast<const T *>(a.f);
-    Ring<T, 2, V == 1> ring{{xp, fp}, dyn, bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
+    const Own own_pre{reinterpret_cast<float4 *>(dyn) + lane, size};
+    const Own own_post{own_pre.at + (kElems / 4) * size, size};  // w_post * scale, LONG: times gate
+    Ring<T, 2, V == 1> ring{{xp, fp}, dyn + kOwn * kElems * size * sizeof(float), bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
     if (RING) ring.start();
-    R post, pre, gate;
-    if (HAS_F) {
-        post.load_or_ones(a.w_post, D, lane, size);
-        gate.fill(1.0f);
+    R gate, post;
+    if (HAS_H) {
+        post.load_or_ones(a.w_pre, D, lane, size);
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) own_pre.put(i, post.get(i), post.get(i + 1));
     }
-    if (HAS_H) pre.load_or_ones(a.w_pre, D, lane, size);
+    auto keep_post = [&] {
+        post.load_or_ones(a.w_post, D, lane, size);
+        auto v = [&](int i) {
+            const float2 p = __fmul2_rn(post.get(i), twice(a.drop.scale));
+            return LONG ? __fmul2_rn(p, gate.get(i)) : p;
+        };
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) own_post.put(i, v(i), v(i + 1));
+    };
+    if (HAS_F) {
+        gate.fill(1.0f);
+        keep_post();
+    }
     int64_t g_end = r0;  // where the gate row in hand ends
     for (int64_t r = r0; r < r1; ++r) {
         if (HAS_F && a.gate && r >= g_end) {
             const int64_t g = r / a.rows_per_gate;
             g_end = (g + 1) * a.rows_per_gate;
             gate.load(static_cast<const T *>(a.gate) + g * D, D, lane, size);
+            if (LONG) keep_post();
         }
         R x, f;
         const bool here = RING && ring.wait(r);
@@ -331,7 +371,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             __syncwarp();
             taken();
         }
-        float2 y[kPairs];
+        float2 y[kPairs], w[2];
         auto centre = [&] {  // y - mean, and the reciprocal root of its mean square
             float s[1];
             if (a.layer) {
@@ -357,14 +397,18 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
         if (HAS_F) {
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) y[i] = f.get(i);
-            const float2 rstd = twice(centre() * a.drop.scale), alpha = twice(a.alpha);
+            const float2 rstd = twice(centre()), alpha = twice(a.alpha);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) y[i] = __fmul2_rn(__fmul2_rn(y[i], rstd), post.get(i));
+            for (int i = 0; i < kPairs; ++i) {
+                if (i % 2 == 0) own_post.get(i, w);
+                y[i] = __fmul2_rn(__fmul2_rn(y[i], rstd), w[i % 2]);
+                if (!LONG) y[i] = __fmul2_rn(y[i], gate.get(i));
+            }
             drop_row<V>(a.drop, y, r, D, lane, size);
             R o;
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
-                y[i] = __ffma2_rn(gate.get(i), y[i], __fmul2_rn(alpha, x.get(i)));
+                y[i] = __ffma2_rn(alpha, x.get(i), y[i]);
                 o.set(i, y[i]);
             }
             o.store(static_cast<T *>(a.y) + r * D, D, lane, size);
@@ -376,7 +420,10 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             const float2 rstd = twice(centre());
             R o;
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) o.set(i, __fmul2_rn(__fmul2_rn(y[i], rstd), pre.get(i)));
+            for (int i = 0; i < kPairs; ++i) {
+                if (i % 2 == 0) own_pre.get(i, w);
+                o.set(i, __fmul2_rn(__fmul2_rn(y[i], rstd), w[i % 2]));
+            }
             o.store(static_cast<T *>(a.h) + r * D, D, lane, size);
         }
         if (RING) ring.advance();
@@ -389,28 +436,6 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
 // Per run: sums for w_post, w_pre, the gate row shared with the run before, the gate row
 // shared with the run after.
 constexpr int kSlots = 4;
-// Gate rows of at least this many rows: one sum A of t * fhat serves the gradients of the
-// gate and of w_post (w_post A and, gate by gate, gate A), which are added to the run's sums
-// when the gate row changes. For shorter ones that would cost more than the second sum.
-constexpr int kLongGate = 8;
-
-// A thread's own floats in shared memory: pairs i and i + 1 (i even) in one access.
-struct Own {
-    float4 *at;
-    int size;
-
-    __device__ __forceinline__ void put(int i, float2 a, float2 b) const
-    {
-        at[i / 2 * size] = make_float4(a.x, a.y, b.x, b.y);
-    }
-    __device__ __forceinline__ void get(int i, float2 (&v)[2]) const
-    {
-        const float4 q = at[i / 2 * size];
-        v[0] = make_float2(q.x, q.y);
-        v[1] = make_float2(q.z, q.w);
-    }
-};
-constexpr int kOwn = 2;
 
 template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : 1)
@@ -781,20 +806,20 @@ inline int64_t grad_runs(int dtype, int64_t rows, int D)
 template <typename T, int V, bool FULL, bool RING, int MAXT>
 cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
 {
-    auto kernel = a.f && a.h ? norm_kernel<T, V, FULL, true, true, RING, MAXT>
-                  : a.f      ? norm_kernel<T, V, FULL, true, false, RING, MAXT>
-                             : norm_kernel<T, V, FULL, false, true, RING, MAXT>;
-    static DeviceCache cache[3];
-    if (RING) {
-        int ready = 0;
-        const cudaError_t e = cache[a.f && a.h ? 0 : a.f ? 1 : 2].get(ready, [&](int &v) {
-            v = 1;
-            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 << 10);
-        });
-        if (e != cudaSuccess) return e;
-    }
+    const bool lg = a.rows_per_gate >= kLongGate;
+    auto kernel = a.f && a.h ? lg ? norm_kernel<T, V, FULL, true, true, true, RING, MAXT>
+                                  : norm_kernel<T, V, FULL, true, true, false, RING, MAXT>
+                  : a.f      ? norm_kernel<T, V, FULL, true, false, false, RING, MAXT>
+                             : norm_kernel<T, V, FULL, false, true, false, RING, MAXT>;
+    static DeviceCache cache[4];
+    int ready = 0;
+    const cudaError_t e = cache[a.f && a.h ? lg : a.f ? 2 : 3].get(ready, [&](int &v) {
+        v = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 << 10);
+    });
+    if (e != cudaSuccess) return e;
     const int64_t most = int64_t(kSms) * p.blocks;
-    kernel<<<unsigned(a.rows < most ? a.rows : most), unsigned(row_threads(a.D)), RING ? p.smem : 0, stream>>>(
+    kernel<<<unsigned(a.rows < most ? a.rows : most), unsigned(row_threads(a.D)), p.smem, stream>>>(
         a, p.stages);
     return cudaGetLastError();
 }
@@ -842,7 +867,7 @@ template <typename T>
 cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
-    const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads, 0);
+    const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
         return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
