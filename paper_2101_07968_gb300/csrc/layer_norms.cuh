@@ -17,8 +17,11 @@
 namespace dc {
 namespace norms {
 
-constexpr int kElems = 16;  // elements of a row per thread
-constexpr int kPairs = kElems / 2;
+// Elements of a row per thread (EL): 16, which spreads a row's sums over few shuffles, and
+// for rows of up to 128 and 256 columns, that one warp takes, 4 and 8, so that its lanes
+// have work.
+constexpr int kElems = 16;
+constexpr int elems_for(int D) { return D <= 128 ? 4 : D <= 256 ? 8 : kElems; }
 // Rows above this take blocks of up to 1,024 threads, whose 64 registers each do not hold
 // the gradient's sums: they spill, which narrower rows are spared.
 constexpr int kNarrow = 256, kWideD = kNarrow * kElems;
@@ -186,9 +189,9 @@ constexpr int kMaxStages = 4;
 
 // A thread's 16 elements of a row: V neighbours, then the same `size` groups on. Elements
 // past D read as zero. FULL: there are none.
-template <typename T, int V, bool FULL>
+template <typename T, int V, bool FULL, int EL>
 struct Row {
-    static constexpr int kItems = kElems / V;
+    static constexpr int kItems = EL / V;
     Vec<T, V> e[kItems];
 
     static __device__ __forceinline__ int column(int k, int lane, int size)
@@ -202,7 +205,7 @@ struct Row {
     __device__ __forceinline__ void fill(float v)
     {
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) set(i, twice(v));
+        for (int i = 0; i < (EL / 2); ++i) set(i, twice(v));
     }
     __device__ __forceinline__ void load(const T *p, int D, int lane, int size)
     {
@@ -254,8 +257,8 @@ struct Row {
 };
 
 // Zeros in place of this thread's dropped elements of row `row`.
-template <int V>
-__device__ __forceinline__ void drop_row(const DropRule &d, float2 (&v)[kPairs], int64_t row, int D,
+template <int V, int EL>
+__device__ __forceinline__ void drop_row(const DropRule &d, float2 (&v)[(EL / 2)], int64_t row, int D,
                                          int lane, int size)
 {
     if (d.threshold == 0) return;
@@ -265,7 +268,7 @@ __device__ __forceinline__ void drop_row(const DropRule &d, float2 (&v)[kPairs],
         const uint64_t z1 = z0 + uint64_t(lane * (V / 4)) * kGamma;
         const uint64_t step = uint64_t(size * (V / 4)) * kGamma;
 #pragma unroll
-        for (int k = 0; k < kElems; k += 4) {
+        for (int k = 0; k < EL; k += 4) {
             const uint64_t w = splitmix_output(z1 + (k / V) * step + (k % V / 4) * kGamma);
             const uint32_t lo = uint32_t(w), hi = uint32_t(w >> 32);
             if (!(lo << 16 > limit)) v[k / 2].x = 0.0f;
@@ -275,8 +278,8 @@ __device__ __forceinline__ void drop_row(const DropRule &d, float2 (&v)[kPairs],
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < kElems; ++k) {
-            const int c = Row<float, V, false>::column(k, lane, size);
+        for (int k = 0; k < EL; ++k) {
+            const int c = Row<float, V, false, EL>::column(k, lane, size);
             const uint64_t w = splitmix_output(z0 + uint64_t(c / 4) * kGamma);
             if (!kept(d, w, c & 3)) (k & 1 ? v[k / 2].y : v[k / 2].x) = 0.0f;
         }
@@ -313,10 +316,10 @@ constexpr int kOwn = 2;
 // the gate row changes. For shorter ones that costs more than it saves.
 constexpr int kLongGate = 8;
 
-template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(NormArgs a, int stages)
+template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
+__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 32 ? 32 : 1) norm_kernel(NormArgs a, int stages)
 {
-    using R = Row<T, V, FULL>;
+    using R = Row<T, V, FULL, EL>;
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float buf[2 * 4 * 32];
     __shared__ alignas(8) uint64_t bars[kMaxStages];
@@ -328,14 +331,14 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
     const int64_t r1 = run_start(a.rows, gridDim.x, blockIdx.x + 1);
     const T *xp = static_cast<const T *>(a.x), *fp = static_cast<const T *>(a.f);
     const Own own_pre{reinterpret_cast<float4 *>(dyn) + lane, size};
-    const Own own_post{own_pre.at + (kElems / 4) * size, size};  // w_post * scale, LONG: times gate
-    Ring<T, 2, V == 1> ring{{xp, fp}, dyn + kOwn * kElems * size * sizeof(float), bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
+    const Own own_post{own_pre.at + (EL / 4) * size, size};  // w_post * scale, LONG: times gate
+    Ring<T, 2, V == 1> ring{{xp, fp}, dyn + kOwn * EL * size * sizeof(float), bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
     if (RING) ring.start();
     R gate, post;
     if (HAS_H) {
         post.load_or_ones(a.w_pre, D, lane, size);
 #pragma unroll
-        for (int i = 0; i < kPairs; i += 2) own_pre.put(i, post.get(i), post.get(i + 1));
+        for (int i = 0; i < (EL / 2); i += 2) own_pre.put(i, post.get(i), post.get(i + 1));
     }
     auto keep_post = [&] {
         post.load_or_ones(a.w_post, D, lane, size);
@@ -344,7 +347,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             return LONG ? __fmul2_rn(p, gate.get(i)) : p;
         };
 #pragma unroll
-        for (int i = 0; i < kPairs; i += 2) own_post.put(i, v(i), v(i + 1));
+        for (int i = 0; i < (EL / 2); i += 2) own_post.put(i, v(i), v(i + 1));
     };
     if (HAS_F) {
         gate.fill(1.0f);
@@ -371,24 +374,24 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
             __syncwarp();
             taken();
         }
-        float2 y[kPairs], w[2];
+        float2 y[(EL / 2)], w[2];
         auto centre = [&] {  // y - mean, and the reciprocal root of its mean square
             float s[1];
             if (a.layer) {
                 float2 q = twice(0.0f);
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) q = __fadd2_rn(q, y[i]);
+                for (int i = 0; i < (EL / 2); ++i) q = __fadd2_rn(q, y[i]);
                 s[0] = q.x + q.y;
                 team.sum(s);
                 taken();
                 const float2 mean = twice(-s[0] * inv);
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i)
+                for (int i = 0; i < (EL / 2); ++i)
                     y[i] = R::only_inside(__fadd2_rn(y[i], mean), i, D, lane, size);
             }
             float2 q = twice(0.0f);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) q = __ffma2_rn(y[i], y[i], q);
+            for (int i = 0; i < (EL / 2); ++i) q = __ffma2_rn(y[i], y[i], q);
             s[0] = q.x + q.y;
             team.sum(s);
             taken();
@@ -396,31 +399,31 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
         };
         if (HAS_F) {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) y[i] = f.get(i);
+            for (int i = 0; i < (EL / 2); ++i) y[i] = f.get(i);
             const float2 rstd = twice(centre()), alpha = twice(a.alpha);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
+            for (int i = 0; i < (EL / 2); ++i) {
                 if (i % 2 == 0) own_post.get(i, w);
                 y[i] = __fmul2_rn(__fmul2_rn(y[i], rstd), w[i % 2]);
                 if (!LONG) y[i] = __fmul2_rn(y[i], gate.get(i));
             }
-            drop_row<V>(a.drop, y, r, D, lane, size);
+            drop_row<V, EL>(a.drop, y, r, D, lane, size);
             R o;
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
+            for (int i = 0; i < (EL / 2); ++i) {
                 y[i] = __ffma2_rn(alpha, x.get(i), y[i]);
                 o.set(i, y[i]);
             }
             o.store(static_cast<T *>(a.y) + r * D, D, lane, size);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) y[i] = x.get(i);
+            for (int i = 0; i < (EL / 2); ++i) y[i] = x.get(i);
         }
         if (HAS_H) {
             const float2 rstd = twice(centre());
             R o;
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
+            for (int i = 0; i < (EL / 2); ++i) {
                 if (i % 2 == 0) own_pre.get(i, w);
                 o.set(i, __fmul2_rn(__fmul2_rn(y[i], rstd), w[i % 2]));
             }
@@ -437,11 +440,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : 1) norm_kernel(Nor
 // shared with the run after.
 constexpr int kSlots = 4;
 
-template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : 1)
+template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
+__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : MAXT == 32 ? 32 : 1)
 norm_grad_kernel(NormArgs a, float *partial, int stages)
 {
-    using R = Row<T, V, FULL>;
+    using R = Row<T, V, FULL, EL>;
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float buf[2 * 4 * 32];
     __shared__ alignas(8) uint64_t bars[kMaxStages];
@@ -456,26 +459,26 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
     // This thread's w_pre and (LONG) gate * w_post * scale as floats, four to an access: in
     // shared memory, where they cost no registers and no conversions.
     const Own own_pre{reinterpret_cast<float4 *>(dyn) + lane, size};
-    const Own own_gp{own_pre.at + (kElems / 4) * size, size};
-    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn + kOwn * kElems * size * sizeof(float), bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
+    const Own own_gp{own_pre.at + (EL / 4) * size, size};
+    Ring<T, 4, V == 1> ring{{src[0], src[1], src[2], src[3]}, dyn + kOwn * EL * size * sizeof(float), bars, stages, D, r0, r1, a.rows, &gave_up, 0, 0, 0, 0};
     if (RING) ring.start();
     R post, gate;
     if (HAS_H) {
         post.load_or_ones(a.w_pre, D, lane, size);
 #pragma unroll
-        for (int i = 0; i < kPairs; i += 2) own_pre.put(i, post.get(i), post.get(i + 1));
+        for (int i = 0; i < (EL / 2); i += 2) own_pre.put(i, post.get(i), post.get(i + 1));
     }
     if (HAS_F) {
         post.load_or_ones(a.w_post, D, lane, size);
         gate.fill(1.0f);
     }
-    float2 gpre[kPairs], gpost[kPairs], ggate[kPairs];  // LONG: ggate holds A, gpost is in memory
+    float2 gpre[(EL / 2)], gpost[(EL / 2)], ggate[(EL / 2)];  // LONG: ggate holds A, gpost is in memory
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) gpost[i] = gpre[i] = ggate[i] = twice(0.0f);
+    for (int i = 0; i < (EL / 2); ++i) gpost[i] = gpre[i] = ggate[i] = twice(0.0f);
     float *slots = partial + b * int64_t(kSlots) * D;
     auto each = [&](auto &&op) {  // op(pair, half, column) of this thread's columns
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
+        for (int i = 0; i < (EL / 2); ++i) {
             if (R::inside(2 * i, D, lane, size)) op(i, 0, R::column(2 * i, lane, size));
             if (R::inside(2 * i + 1, D, lane, size)) op(i, 1, R::column(2 * i + 1, lane, size));
         }
@@ -487,7 +490,7 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             post.load_or_ones(a.w_post, D, lane, size);
             auto gp = [&](int i) { return __fmul2_rn(__fmul2_rn(gate.get(i), post.get(i)), twice(a.drop.scale)); };
 #pragma unroll
-            for (int i = 0; i < kPairs; i += 2) own_gp.put(i, gp(i), gp(i + 1));
+            for (int i = 0; i < (EL / 2); i += 2) own_gp.put(i, gp(i), gp(i + 1));
         }
     };
     int64_t g = 0, g_end = r0;
@@ -535,7 +538,7 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
             for (int i = 0; i < 6; ++i) q[i] = twice(0.0f);
             float2 pre[2];
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
+            for (int i = 0; i < (EL / 2); ++i) {
                 if (HAS_H) {
                     if (i % 2 == 0) own_pre.get(i, pre);
                     const float2 v = R::only_inside(__fadd2_rn(y.get(i), y0), i, D, lane, size);
@@ -604,20 +607,20 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         const float2 fr = twice(fr1), fm = twice(f0.x - s[2]);
 
         reload(true);
-        float2 t[kPairs];
+        float2 t[(EL / 2)];
         if (a.dy) {
             R dy;
             dy.load(row(2), D, lane, size);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) t[i] = dy.get(i);
+            for (int i = 0; i < (EL / 2); ++i) t[i] = dy.get(i);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) t[i] = twice(0.0f);
+            for (int i = 0; i < (EL / 2); ++i) t[i] = twice(0.0f);
         }
         float2 w2[2];
         if (HAS_H) {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
+            for (int i = 0; i < (EL / 2); ++i) {
                 if (i % 2 == 0) own_pre.get(i, w2);
                 const float2 yhat = __fmul2_rn(__fadd2_rn(y.get(i), ym), yr), d = dh.get(i);
                 t[i] = __ffma2_rn(yr, __ffma2_rn(yhat, proj, __ffma2_rn(d, w2[i % 2], dm)), t[i]);
@@ -627,15 +630,15 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         R o;
         const float2 alpha = twice(a.alpha);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) o.set(i, __fmul2_rn(alpha, t[i]));
+        for (int i = 0; i < (EL / 2); ++i) o.set(i, __fmul2_rn(alpha, t[i]));
         o.store(static_cast<T *>(a.dx) + r * D, D, lane, size);
         if (!HAS_F) continue;
 
-        drop_row<V>(a.drop, t, r, D, lane, size);
+        drop_row<V, EL>(a.drop, t, r, D, lane, size);
         const float2 scale = twice(a.drop.scale);
         float2 s2[2] = {twice(0.0f), twice(0.0f)};
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
+        for (int i = 0; i < (EL / 2); ++i) {
             const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
             float2 kt = R::only_inside(t[i], i, D, lane, size);
             if (LONG) {
@@ -657,7 +660,7 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
         reload(false);
         const float2 fproj = twice(-(v[0] * inv)), fdm = twice(a.layer ? -(v[1] * inv) : 0.0f);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
+        for (int i = 0; i < (EL / 2); ++i) {
             const float2 fhat = __fmul2_rn(__fadd2_rn(f.get(i), fm), fr);
             o.set(i, __fmul2_rn(fr, __ffma2_rn(fhat, fproj, __fadd2_rn(t[i], fdm))));
         }
@@ -676,14 +679,14 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
                     });
                 first_gate = false;
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i)
+                for (int i = 0; i < (EL / 2); ++i)
                     ggate[i] = __fmul2_rn(__fmul2_rn(post.get(i), scale), ggate[i]);
             }
             if (a.dgate) {
                 const int64_t g_start = g * a.rows_per_gate;
                 if (ends && g_start >= r0) {
 #pragma unroll
-                    for (int i = 0; i < kPairs; ++i) o.set(i, ggate[i]);
+                    for (int i = 0; i < (EL / 2); ++i) o.set(i, ggate[i]);
                     o.store(static_cast<T *>(a.dgate) + g * D, D, lane, size);
                 } else {
                     float *p = slots + (g_start < r0 ? 2 : 3) * int64_t(D);
@@ -691,7 +694,7 @@ norm_grad_kernel(NormArgs a, float *partial, int stages)
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) ggate[i] = twice(0.0f);
+            for (int i = 0; i < (EL / 2); ++i) ggate[i] = twice(0.0f);
         }
     }
     if (HAS_F && !LONG && a.dw_post) each([&](int i, int h, int c) { slots[c] = half(gpost[i], h); });
@@ -710,8 +713,8 @@ __device__ __forceinline__ int64_t run_of(int64_t rows, int64_t P, int64_t r)
 }
 
 // Adds the runs' sums: block row 0 those of the weights, block row g + 1 those of gate row g if
-// it lies in several runs. Sixteen threads a column, each every sixteenth run in order.
-constexpr int kFinishCols = 32, kFinishLanes = 16;
+// it lies in several runs. Thirty-two threads a column, each every thirty-second run in order.
+constexpr int kFinishCols = 32, kFinishLanes = 32;
 template <typename T>
 __global__ void __launch_bounds__(kFinishCols *kFinishLanes)
 norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
@@ -725,10 +728,10 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
     if (g < 0) {
         if (in) {
             if (a.dw_post)
-#pragma unroll 8
+#pragma unroll 16
                 for (int64_t i = ty; i < P; i += kFinishLanes) s0 += partial[i * stride + c];
             if (a.dw_pre)
-#pragma unroll 8
+#pragma unroll 16
                 for (int64_t i = ty; i < P; i += kFinishLanes) s1 += partial[i * stride + D + c];
         }
     } else {
@@ -757,6 +760,22 @@ norm_finish_kernel(NormArgs a, const float *partial, int64_t P)
     }
 }
 
+// Gate rows of a few runs each: a thread per column adds a gate row's runs one after another.
+constexpr int kGateThreads = 256, kGateSpan = 24;
+template <typename T>
+__global__ void __launch_bounds__(kGateThreads) norm_gates_kernel(NormArgs a, const float *partial, int64_t P)
+{
+    const int64_t g = blockIdx.x, D = a.D, c = int64_t(blockIdx.y) * blockDim.x + threadIdx.x;
+    const int64_t start = g * a.rows_per_gate;
+    const int64_t end = start + a.rows_per_gate < a.rows ? start + a.rows_per_gate : a.rows;
+    const int64_t b0 = run_of(a.rows, P, start), b1 = run_of(a.rows, P, end - 1);
+    if (b0 == b1 || c >= D) return;
+    float v = partial[(b0 * kSlots + 3) * D + c];
+#pragma unroll 4
+    for (int64_t i = b0 + 1; i <= b1; ++i) v += partial[(i * kSlots + 2) * D + c];
+    static_cast<T *>(a.dgate)[g * D + c] = from_float<T>(v);
+}
+
 // With more gate rows than runs, a gate row lies in at most two: one block per run adds the
 // row that it shares with the run before.
 template <typename T>
@@ -771,7 +790,11 @@ __global__ void __launch_bounds__(128) norm_shared_gates_kernel(NormArgs a, cons
 }
 
 // ------------------------------------------------------------------------------ host
-inline int row_threads(int D) { return (D + kElems * 32 - 1) / (kElems * 32) * 32; }
+inline int row_threads(int D)
+{
+    const int el = elems_for(D);
+    return (D + el * 32 - 1) / (el * 32) * 32;
+}
 
 // Blocks an SM and slots of the ring: `threads` an SM as the registers allow, and the 224 KB
 // of shared memory shared between them; no ring (0 slots) where it would hold fewer than two rows.
@@ -783,9 +806,10 @@ inline Plan plan_for(int D, int arrays, int bytes, int threads, int own)
 {
     Plan p;
     const int size = row_threads(D);
-    p.blocks = threads / size < 1 ? 1 : threads / size;
-    if (p.blocks > 16) p.blocks = 16;
-    const size_t fixed = 2048 + size_t(own) * size * kElems * sizeof(float);
+    p.blocks = elems_for(D) < kElems ? 32 : threads / size < 1 ? 1 : threads / size;
+    if (p.blocks > 32) p.blocks = 32;
+    if (elems_for(D) == kElems && p.blocks > 16) p.blocks = 16;
+    const size_t fixed = 2048 + size_t(own) * size * elems_for(D) * sizeof(float);
     const size_t row = size_t(arrays) * ((size_t(D) * bytes + 15) / 16 * 16 + 16), room = size_t(224) << 10;
     while (p.blocks > 1 && room / p.blocks < 2 * row + fixed) --p.blocks;
     const size_t slots = room / p.blocks > fixed ? (room / p.blocks - fixed) / row : 0;
@@ -795,7 +819,7 @@ inline Plan plan_for(int D, int arrays, int bytes, int threads, int own)
     return p;
 }
 constexpr int kSms = 152;
-constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM
+constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM; up to 32 single warps
 
 inline int64_t grad_runs(int dtype, int64_t rows, int D)
 {
@@ -803,14 +827,14 @@ inline int64_t grad_runs(int dtype, int64_t rows, int D)
     return rows < most ? rows : most;
 }
 
-template <typename T, int V, bool FULL, bool RING, int MAXT>
+template <typename T, int V, bool FULL, bool RING, int MAXT, int EL>
 cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
 {
     const bool lg = a.rows_per_gate >= kLongGate;
-    auto kernel = a.f && a.h ? lg ? norm_kernel<T, V, FULL, true, true, true, RING, MAXT>
-                                  : norm_kernel<T, V, FULL, true, true, false, RING, MAXT>
-                  : a.f      ? norm_kernel<T, V, FULL, true, false, false, RING, MAXT>
-                             : norm_kernel<T, V, FULL, false, true, false, RING, MAXT>;
+    auto kernel = a.f && a.h ? lg ? norm_kernel<T, V, FULL, true, true, true, RING, MAXT, EL>
+                                  : norm_kernel<T, V, FULL, true, true, false, RING, MAXT, EL>
+                  : a.f      ? norm_kernel<T, V, FULL, true, false, false, RING, MAXT, EL>
+                             : norm_kernel<T, V, FULL, false, true, false, RING, MAXT, EL>;
     static DeviceCache cache[4];
     int ready = 0;
     const cudaError_t e = cache[a.f && a.h ? lg : a.f ? 2 : 3].get(ready, [&](int &v) {
@@ -824,15 +848,15 @@ cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-template <typename T, int V, bool FULL, bool RING, int MAXT>
+template <typename T, int V, bool FULL, bool RING, int MAXT, int EL>
 cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const Plan &p,
                              cudaStream_t stream)
 {
     const bool lg = a.rows_per_gate >= kLongGate;
-    auto kernel = a.f && a.dh ? lg ? norm_grad_kernel<T, V, FULL, true, true, true, RING, MAXT>
-                                   : norm_grad_kernel<T, V, FULL, true, true, false, RING, MAXT>
-                  : a.f       ? norm_grad_kernel<T, V, FULL, true, false, false, RING, MAXT>
-                              : norm_grad_kernel<T, V, FULL, false, true, false, RING, MAXT>;
+    auto kernel = a.f && a.dh ? lg ? norm_grad_kernel<T, V, FULL, true, true, true, RING, MAXT, EL>
+                                   : norm_grad_kernel<T, V, FULL, true, true, false, RING, MAXT, EL>
+                  : a.f       ? norm_grad_kernel<T, V, FULL, true, false, false, RING, MAXT, EL>
+                              : norm_grad_kernel<T, V, FULL, false, true, false, RING, MAXT, EL>;
     static DeviceCache cache[4];
     {
         int ready = 0;
@@ -844,13 +868,18 @@ cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const
     }
     kernel<<<unsigned(P), unsigned(row_threads(a.D)), p.smem, stream>>>(a, partial, p.stages);
     const int64_t gates = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate;
-    const bool few = gates < P;
-    if (a.dw_post || a.dw_pre || (a.dgate && few)) {
-        const dim3 g(unsigned((a.D + kFinishCols - 1) / kFinishCols), 1u + unsigned(a.dgate && few ? gates : 0));
+    // how the gate rows that lie in several runs are added up
+    const bool shared = a.dgate && P > 1 && a.rows_per_gate > 1, few = gates < P;
+    const bool wide = shared && few && a.rows_per_gate * P / a.rows > kGateSpan;
+    if (a.dw_post || a.dw_pre || wide) {
+        const dim3 g(unsigned((a.D + kFinishCols - 1) / kFinishCols), 1u + unsigned(wide ? gates : 0));
         norm_finish_kernel<T><<<g, dim3(kFinishCols, kFinishLanes), 0, stream>>>(a, partial, P);
     }
-    if (a.dgate && !few && P > 1 && a.rows_per_gate > 1)
-        norm_shared_gates_kernel<T><<<unsigned(P - 1), 128, 0, stream>>>(a, partial, P);
+    if (shared && few && !wide) {
+        const int n = a.D < kGateThreads ? (a.D + 31) / 32 * 32 : kGateThreads;
+        norm_gates_kernel<T><<<dim3(unsigned(gates), unsigned((a.D + n - 1) / n)), n, 0, stream>>>(a, partial, P);
+    }
+    if (shared && !few) norm_shared_gates_kernel<T><<<unsigned(P - 1), 128, 0, stream>>>(a, partial, P);
     return cudaGetLastError();
 }
 
@@ -863,6 +892,7 @@ inline bool vectors_ok(int dtype, const NormArgs &a)
     return true;
 }
 
+// Rows of up to kWideD columns always leave room for a ring of two rows.
 template <typename T>
 cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
 {
@@ -870,14 +900,15 @@ cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
     const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
-        return vec ? norm_launch<T, V, false, false, 1024>(a, p, stream)
-                   : norm_launch<T, 1, false, false, 1024>(a, p, stream);
-    if (!vec)
-        return p.stages ? norm_launch<T, 1, false, true, kNarrow>(a, p, stream)
-                        : norm_launch<T, 1, false, false, kNarrow>(a, p, stream);
-    if (!p.stages) return norm_launch<T, V, false, false, kNarrow>(a, p, stream);
-    return full ? norm_launch<T, V, true, true, kNarrow>(a, p, stream)
-                : norm_launch<T, V, false, true, kNarrow>(a, p, stream);
+        return vec ? norm_launch<T, V, false, false, 1024, kElems>(a, p, stream)
+                   : norm_launch<T, 1, false, false, 1024, kElems>(a, p, stream);
+    if (a.D <= 128)
+        return vec ? norm_launch<T, 4, false, true, 32, 4>(a, p, stream) : norm_launch<T, 1, false, true, 32, 4>(a, p, stream);
+    if (a.D <= 256)
+        return vec ? norm_launch<T, V, false, true, 32, 8>(a, p, stream) : norm_launch<T, 1, false, true, 32, 8>(a, p, stream);
+    if (!vec) return norm_launch<T, 1, false, true, kNarrow, kElems>(a, p, stream);
+    return full ? norm_launch<T, V, true, true, kNarrow, kElems>(a, p, stream)
+                : norm_launch<T, V, false, true, kNarrow, kElems>(a, p, stream);
 }
 
 template <typename T>
@@ -888,14 +919,15 @@ cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t 
     const int64_t P = grad_runs(dtype, a.rows, a.D);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
-        return vec ? norm_grad_launch<T, V, false, false, 1024>(a, partial, P, p, stream)
-                   : norm_grad_launch<T, 1, false, false, 1024>(a, partial, P, p, stream);
-    if (!vec)
-        return p.stages ? norm_grad_launch<T, 1, false, true, kNarrow>(a, partial, P, p, stream)
-                        : norm_grad_launch<T, 1, false, false, kNarrow>(a, partial, P, p, stream);
-    if (!p.stages) return norm_grad_launch<T, V, false, false, kNarrow>(a, partial, P, p, stream);
-    return full ? norm_grad_launch<T, V, true, true, kNarrow>(a, partial, P, p, stream)
-                : norm_grad_launch<T, V, false, true, kNarrow>(a, partial, P, p, stream);
+        return vec ? norm_grad_launch<T, V, false, false, 1024, kElems>(a, partial, P, p, stream)
+                   : norm_grad_launch<T, 1, false, false, 1024, kElems>(a, partial, P, p, stream);
+    if (a.D <= 128)
+        return vec ? norm_grad_launch<T, 4, false, true, 32, 4>(a, partial, P, p, stream) : norm_grad_launch<T, 1, false, true, 32, 4>(a, partial, P, p, stream);
+    if (a.D <= 256)
+        return vec ? norm_grad_launch<T, V, false, true, 32, 8>(a, partial, P, p, stream) : norm_grad_launch<T, 1, false, true, 32, 8>(a, partial, P, p, stream);
+    if (!vec) return norm_grad_launch<T, 1, false, true, kNarrow, kElems>(a, partial, P, p, stream);
+    return full ? norm_grad_launch<T, V, true, true, kNarrow, kElems>(a, partial, P, p, stream)
+                : norm_grad_launch<T, V, false, true, kNarrow, kElems>(a, partial, P, p, stream);
 }
 
 }  // namespace norms
