@@ -212,6 +212,21 @@ __device__ __forceinline__ uint32_t f16_shape(bool bf16, bool a_mn, bool b_mn, u
     return 1u << 4 | f << 7 | f << 10 | uint32_t(a_mn) << 15 | uint32_t(b_mn) << 16 | (n >> 3) << 17 |
            (m >> 4) << 24;
 }
+// kind::tf32: floats whose low 13 bits are not read, both operands K-major
+__device__ __forceinline__ uint32_t tf32_shape(uint32_t m, uint32_t n)
+{
+    return 1u << 4 | 2u << 7 | 2u << 10 | (n >> 3) << 17 | (m >> 4) << 24;
+}
+template <int CG>
+__device__ __forceinline__ void mma_tf32(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
+{
+    static_assert(CG == 2, "");
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::tf32 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(shape), "r"(uint32_t(add))
+        : "memory");
+}
 template <int CG>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {

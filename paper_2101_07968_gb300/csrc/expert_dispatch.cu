@@ -1,6 +1,15 @@
-// Which kernel takes an expert product, and the copies of operands that the tensor cores'
-// tile copies cannot read: those need rows that start on 16-byte boundaries.
-#include "layers.cuh"
+// Which kernel takes an expert product, and the copies of operands that the tensor cores
+// cannot take as they are: tile copies need rows that start on 16-byte boundaries, and floats
+// go in parts.
+//
+// Floats on the tensor cores: x = hi + lo with hi and lo of the 11 significant bits that tf32
+// holds, and x w = hi hi + hi lo + lo hi, one product over a summed axis three times as long.
+// What is left out (lo lo, and the bits of x past lo) is below 3 2^-22 |x w| a product, some
+// 2^-23 on average, less than a 32-bit sum of more than a few products loses; so the
+// CUDA cores take products of fewer than kPartDepth summed elements, and weight gradients of
+// experts of fewer than kPartLeast rows. 16,384 x 2,048 x 2,048 over 8 experts: see the
+// figure at use_parts.
+#include "expert_rows.cuh"
 
 namespace dc {
 namespace {
@@ -74,11 +83,175 @@ void operands(const ExpertArgs &g, bool weights, Matrix &a, Matrix &b)
 
 bool few(const ExpertArgs &g, bool weights) { return !weights && g.rows <= DC_FEW_ROWS; }
 
+// ----------------------------------------------------------------- floats in parts
+constexpr int kPartDepth = 64, kPartLeast = 8;
+
+__device__ __forceinline__ void parts_of(float x, float &hi, float &lo)
+{
+    uint32_t h;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(h) : "f"(x));
+    hi = __uint_as_float(h & 0xffffe000u);
+    // rounded past the largest float (or infinite): cut off instead, without a second part
+    if (isinf(hi)) hi = __uint_as_float(__float_as_uint(x) & 0xffffe000u);
+    lo = isinf(hi) ? 0.0f : x - hi;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(h) : "f"(lo));
+    lo = __uint_as_float(h & 0xffffe000u);
+}
+
+// The three thirds of a row: hi, hi, lo for one operand (FIRST) and hi, lo, hi for the other.
+template <bool FIRST>
+__device__ __forceinline__ void put_parts(float *row, int64_t third, int64_t at, float x)
+{
+    float hi, lo;
+    parts_of(x, hi, lo);
+    row[at] = hi;
+    row[third + at] = FIRST ? hi : lo;
+    row[2 * third + at] = FIRST ? lo : hi;
+}
+
+// Rows [z][y][x], x contiguous and summed.
+template <bool FIRST>
+__global__ void __launch_bounds__(kThreads)
+split_rows_kernel(const float *src, float *dst, int64_t rows, int32_t y, int32_t x, int32_t pad,
+                  int64_t stride_z, int64_t stride_y)
+{
+    const int c = blockIdx.y * blockDim.x + threadIdx.x;
+    const int64_t r = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
+    if (c >= pad || r >= rows) return;
+    const float v = c < x ? src[(r / y) * stride_z + (r % y) * stride_y + c] : 0.0f;
+    put_parts<FIRST>(dst + r * 3 * pad, pad, c, v);
+}
+
+// [z][x][y], y contiguous and x summed, to rows [z][y].
+template <bool FIRST>
+__global__ void __launch_bounds__(kThreads)
+split_columns_kernel(const float *src, float *dst, int32_t y, int32_t x, int32_t pad, int64_t stride_z,
+                     int64_t stride_x)
+{
+    __shared__ float tile[32][33];
+    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
+    const int x0 = blockIdx.x * 32, y0 = blockIdx.y * 32;
+    const float *p = src + blockIdx.z * stride_z;
+    for (int i = ty; i < 32; i += kThreads / 32)
+        tile[i][tx] = x0 + i < x && y0 + tx < y ? p[(x0 + i) * stride_x + y0 + tx] : 0.0f;
+    __syncthreads();
+    for (int i = ty; i < 32; i += kThreads / 32)
+        if (y0 + i < y)
+            put_parts<FIRST>(dst + (int64_t(blockIdx.z) * y + y0 + i) * 3 * pad, pad, x0 + tx, tile[tx][i]);
+}
+
+// The rows of the batch [rows][y], summed expert by expert, to rows [y]: each segment's rows are
+// rounded up to kPartRows with zeros, and its three thirds lie side by side.
+template <bool FIRST>
+__global__ void __launch_bounds__(kThreads)
+split_segments_kernel(const float *src, float *dst, const int64_t *offsets, int64_t rows, int32_t experts,
+                      int32_t y, int64_t stride, int64_t pitch)
+{
+    extern __shared__ int32_t dyn[];
+    __shared__ float tile[kPartRows][33];
+    const Segments seg = segments_at(dyn, experts);
+    if (threadIdx.x < 32) build_segments(seg, offsets, rows, experts, kPartRows, 1);
+    __syncthreads();
+    const int t = blockIdx.x;
+    if (t >= seg.tile[seg.count]) return;
+    const int s = find_segment(seg, t), first = seg.tile[s];
+    const int64_t r0 = seg.start[s] + int64_t(t - first) * kPartRows, end = seg.start[s + 1];
+    const int64_t third = int64_t(seg.tile[s + 1] - first) * kPartRows;
+    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, y0 = blockIdx.y * 32;
+    for (int i = ty; i < kPartRows; i += kThreads / 32)
+        tile[i][tx] = r0 + i < end && y0 + tx < y ? src[(r0 + i) * stride + y0 + tx] : 0.0f;
+    __syncthreads();
+    for (int i = ty; i < 32; i += kThreads / 32)
+        if (y0 + i < y)
+            put_parts<FIRST>(dst + (y0 + i) * pitch + int64_t(first) * 3 * kPartRows, third,
+                             int64_t(t - first) * kPartRows + tx, tile[tx][i]);
+}
+
+int64_t part_pad(int64_t r) { return (r + 31) / 32 * 32; }
+// the longest that the segments' rounded rows can be
+int64_t part_rows(const ExpertArgs &g) { return (g.rows / kPartRows + g.experts + 3) * kPartRows; }
+size_t part_bytes(int64_t rows, int64_t length) { return (size_t(rows) * 3 * length * 4 + 255) / 256 * 256; }
+
+// Both sides measured, 8 experts: 16,384 rows x 2,048 x 2,048 and 200 x 512 x 512 (the sums of
+// the latter are no longer than the copies before them).
+bool use_parts(const ExpertArgs &g, bool weights)
+{
+    if (3 * part_rows(g) >= int64_t(1) << 31) return false;
+    return weights ? g.rows >= 64 && g.rows >= 2 * kPartLeast * int64_t(g.experts)
+                   : g.r >= kPartDepth;
+}
+
+template <bool FIRST>
+cudaError_t split_rows(const Matrix &m, float *dst, cudaStream_t stream)
+{
+    const int64_t pad = part_pad(m.x), rows = m.z * m.y;
+    const int bx = 32, by = kThreads / bx;
+    const dim3 grid(unsigned((rows + by - 1) / by), unsigned((pad + bx - 1) / bx));
+    split_rows_kernel<FIRST><<<grid, dim3(bx, by), 0, stream>>>(static_cast<const float *>(m.p), dst, rows, int32_t(m.y),
+                                                               int32_t(m.x), int32_t(pad), m.stride_z, m.stride_y);
+    return cudaGetLastError();
+}
+
+cudaError_t float_rows(const ExpertArgs &g, void *workspace, cudaStream_t stream)
+{
+    const int64_t pad = part_pad(g.r);
+    float *a = static_cast<float *>(workspace);
+    float *b = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(g.rows, pad));
+    cudaError_t e = split_rows<true>({g.a, 1, g.rows, g.r, 0, g.a_m}, a, stream);
+    if (e != cudaSuccess) return e;
+    if (g.b_r == 1) {
+        e = split_rows<false>({g.b, g.experts, g.n, g.r, g.b_e, g.b_n}, b, stream);
+    } else {
+        const dim3 grid(unsigned(pad / 32), unsigned((g.n + 31) / 32), unsigned(g.experts));
+        split_columns_kernel<false><<<grid, kThreads, 0, stream>>>(static_cast<const float *>(g.b), b, g.n, g.r,
+                                                                   int32_t(pad), g.b_e, g.b_r);
+        e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return e;
+    ExpertArgs h = g;
+    h.a = a;
+    h.a_m = 3 * pad;
+    h.b = b;
+    h.b_r = 1;
+    h.b_n = 3 * pad;
+    h.b_e = 3 * pad * g.n;
+    h.r = int32_t(3 * pad);
+    return expert_mma_rows(DC_FP32, h, stream);
+}
+
+cudaError_t float_weights(const ExpertArgs &g, void *workspace, cudaStream_t stream)
+{
+    const int64_t length = part_rows(g);
+    float *a = static_cast<float *>(workspace);
+    float *b = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(g.m, length));
+    const unsigned tiles = unsigned(length / kPartRows);
+    split_segments_kernel<true><<<dim3(tiles, unsigned((g.m + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
+        static_cast<const float *>(g.a), a, g.offsets, g.rows, g.experts, g.m, g.a_r, 3 * length);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    split_segments_kernel<false><<<dim3(tiles, unsigned((g.n + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
+        static_cast<const float *>(g.b), b, g.offsets, g.rows, g.experts, g.n, g.b_r, 3 * length);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    ExpertArgs h = g;
+    h.a = a;
+    h.a_r = 3 * length;
+    h.b = b;
+    h.b_r = 3 * length;
+    e = expert_mma_weights(DC_FP32, h, kPartLeast, stream);
+    return e != cudaSuccess ? e : expert_simt_weights(g, kPartLeast - 1, stream);
+}
+
 }  // namespace
 
 size_t expert_workspace(int dtype, const ExpertArgs &g, bool weights)
 {
-    if (dtype == DC_FP32 || few(g, weights)) return 0;
+    if (few(g, weights)) return 0;
+    if (dtype == DC_FP32) {
+        if (!use_parts(g, weights)) return 0;
+        return weights ? part_bytes(g.m, part_rows(g)) + part_bytes(g.n, part_rows(g))
+                       : part_bytes(g.rows, part_pad(g.r)) + part_bytes(int64_t(g.experts) * g.n, part_pad(g.r));
+    }
     Matrix a, b;
     operands(g, weights, a, b);
     return copy_bytes(a) + copy_bytes(b);
@@ -87,7 +260,7 @@ size_t expert_workspace(int dtype, const ExpertArgs &g, bool weights)
 cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, cudaStream_t stream)
 {
     if (few(g, false)) return expert_few_rows(dtype, g, stream);
-    if (dtype == DC_FP32) return expert_simt_rows(g, stream);
+    if (dtype == DC_FP32) return use_parts(g, false) ? float_rows(g, workspace, stream) : expert_simt_rows(g, stream);
     Matrix a, b;
     operands(g, false, a, b);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
@@ -100,15 +273,16 @@ cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, 
     h.b = b.p;
     h.b_e = b.stride_z;
     (g.b_r == 1 ? h.b_n : h.b_r) = b.stride_y;
-    return expert_mma_rows(dtype == DC_BF16, h, stream);
+    return expert_mma_rows(dtype, h, stream);
 }
 
 cudaError_t launch_expert_weights(int dtype, const ExpertArgs &g, void *workspace,
                                   cudaStream_t stream)
 {
-    if (g.rows == 0 || dtype == DC_FP32) {
-        if (dtype == DC_FP32) return expert_simt_weights(g, stream);
-        // no rows: every dW is zero, and there is nothing to read
+    if (dtype == DC_FP32)
+        return g.rows > 0 && use_parts(g, true) ? float_weights(g, workspace, stream)
+                                                : expert_simt_weights(g, g.rows, stream);
+    if (g.rows == 0) {  // every dW is zero, and there is nothing to read
         for (int e = 0; e < g.experts; ++e) {
             char *p = static_cast<char *>(g.c) + e * g.c_e * 2;
             const cudaError_t r = cudaMemset2DAsync(p, size_t(g.c_m) * 2, 0, size_t(g.n) * 2, size_t(g.m), stream);
@@ -127,7 +301,7 @@ cudaError_t launch_expert_weights(int dtype, const ExpertArgs &g, void *workspac
     h.a_r = a.stride_y;
     h.b = b.p;
     h.b_r = b.stride_y;
-    return expert_mma_weights(dtype == DC_BF16, h, stream);
+    return expert_mma_weights(dtype, h, 0, stream);
 }
 
 }  // namespace dc

@@ -1,4 +1,4 @@
-// Expert products on the tensor cores (tcgen05), 16-bit operands.
+// Expert products on the tensor cores (tcgen05): 16-bit operands, and floats as tf32 parts.
 //
 // The feature axis is the M of a product and the rows of the batch its N, so that ragged
 // experts cost little: a tile's N is its rows rounded up to 16 (32 for a pair), where a tile
@@ -7,6 +7,8 @@
 //   dx  A = W_e^T (features contiguous)       B = dy
 //   dW  A = dy^T, B = x^T (both with the summed axis, an expert's rows, outermost)
 // The hardware reads either order of an operand, so nothing is transposed.
+// Floats come as parts that tf32 holds (expert_dispatch.cu), with the summed axis innermost,
+// padded and three times as long: hi hi + hi lo + lo hi.
 //
 // A persistent CTA (or pair of CTAs, one tile of 256 features between them) takes every
 // grid-th tile. Warp 4 copies operand blocks of 64 along the summed axis into a ring of
@@ -25,14 +27,14 @@
 namespace dc {
 namespace {
 
-constexpr int kBK = 64;                  // summed axis per stage: a 128-byte line
+constexpr int kBKBytes = 128;            // summed axis per stage: a line
 constexpr int kBM = 128;                 // features per CTA
 constexpr int kThreads = 7 * 32;
-constexpr uint32_t kABytes = kBM * kBK * 2;
-constexpr uint32_t kBoxBytes = 64 * kBK * 2;  // B comes in boxes of 64 rows
+constexpr uint32_t kABytes = kBM * kBKBytes;
+constexpr uint32_t kBoxBytes = 64 * kBKBytes;  // B comes in boxes of 64 rows
 constexpr int kMaxStages = 12;
 
-enum { kRowsK, kRowsMN, kWeights };  // rows with A K-major or MN-major; weights
+enum { kRowsK, kRowsMN, kWeights, kWeightsK };  // rows with A K-major or MN-major; weights MN- or K-major
 
 struct MmaArgs {
     void *c;
@@ -43,6 +45,7 @@ struct MmaArgs {
     int32_t m, n, r;    // M extent; weights: N extent; rows: summed extent
     int32_t *status;
     bool wide;          // weights: 16-byte stores; rows: 4-byte stores
+    int32_t least;      // weights: experts of fewer rows are left to another kernel
 };
 
 struct Tile {
@@ -57,7 +60,7 @@ template <int MODE, int CG, int BN>
 __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, int t)
 {
     Tile q;
-    if (MODE == kWeights) {
+    if (MODE == kWeights || MODE == kWeightsK) {
         const int nm = (a.m + kBM * CG - 1) / (kBM * CG), nn = (a.n + BN - 1) / BN;
         q.e = t / (nm * nn);
         const int i = t - q.e * (nm * nn);
@@ -66,6 +69,11 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
         q.cols = min(BN, a.n - q.n0);
         q.r0 = seg.start[q.e + 1];
         q.r = seg.start[q.e + 2] - q.r0;
+        if (MODE == kWeightsK) {  // three parts of the padded rows
+            if (q.r < a.least) q.cols = 0;
+            q.r0 = 3 * kPartRows * seg.tile[q.e + 1];
+            q.r = 3 * kPartRows * (seg.tile[q.e + 2] - seg.tile[q.e + 1]);
+        }
     } else {
         const int nm = (a.m + kBM * CG - 1) / (kBM * CG);
         const int s = find_segment(seg, t);
@@ -84,7 +92,7 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
 template <int MODE, int CG, int BN>
 __device__ __forceinline__ int tile_count(const MmaArgs &a, const Segments &seg)
 {
-    if (MODE == kWeights)
+    if (MODE == kWeights || MODE == kWeightsK)
         return a.experts * ((a.m + kBM * CG - 1) / (kBM * CG)) * ((a.n + BN - 1) / BN);
     return seg.tile[seg.count];
 }
@@ -108,7 +116,7 @@ __device__ __forceinline__ void store_rows(const MmaArgs &a, const Tile &q, int 
     const int lane = threadIdx.x & 31;
     const int n = q.cols - c0;
     T *p = static_cast<T *>(a.c) + (int64_t(q.n0) + c0) * a.c_m + feature;
-    if (a.wide) {
+    if constexpr (sizeof(T) == 2) if (a.wide) {
         // Lanes in pairs exchange a value, so that each stores two features of one row: the
         // even lane those of row j, the odd one those of row j + 1.
         const bool odd = lane & 1;
@@ -120,7 +128,9 @@ __device__ __forceinline__ void store_rows(const MmaArgs &a, const Tile &q, int 
             if (row < n && feature < a.m)
                 *reinterpret_cast<uint32_t *>(p + row * a.c_m - odd) = w;
         }
-    } else if (feature < a.m) {
+        return;
+    }
+    if (feature < a.m) {
 #pragma unroll
         for (int j = 0; j < 32; ++j)
             if (j < n) p[j * a.c_m] = from_float<T>(v[j]);
@@ -137,6 +147,12 @@ template <typename T>
 __device__ __forceinline__ void stage_columns(Lines &s, int unit, const float (&v)[32])
 {
     const int lane = threadIdx.x & 31;
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4, ++unit)
+            *reinterpret_cast<float4 *>(&s.u[lane][unit ^ (lane & 7)]) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        return;
+    } else
 #pragma unroll
     for (int j = 0; j < 32; j += 8, ++unit)
         s.u[lane][unit ^ (lane & 7)] = make_uint4(pack2(v[j], v[j + 1], T()), pack2(v[j + 2], v[j + 3], T()),
@@ -172,13 +188,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                   const MmaArgs a)
 {
-    constexpr uint32_t kBBytes = BN / CG * kBK * 2;
+    constexpr uint32_t kBBytes = BN / CG * kBKBytes;
+    constexpr int kBK = kBKBytes / sizeof(T), kStep = 32 / sizeof(T);  // per stage, per product
+    constexpr bool kTf32 = std::is_same<T, float>::value, kOut = MODE == kWeights || MODE == kWeightsK;
+    constexpr bool kAMn = MODE == kRowsMN || MODE == kWeights;
     constexpr uint32_t kStage = kABytes + kBBytes;
     constexpr uint32_t kColumns = BN * 2 < 32 ? 32 : BN * 2;
     extern __shared__ unsigned char dyn[];
     __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
     __shared__ uint32_t tmem_at, gave_up;
-    __shared__ alignas(16) Lines lines[MODE == kWeights ? 4 : 1];
+    __shared__ alignas(16) Lines lines[kOut ? 4 : 1];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? bw::cluster_rank() : 0;
@@ -206,7 +225,8 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         bw::prefetch_map(&map_b);
     }
     if (warp == 0)
-        build_segments(seg, a.offsets, a.rows, a.experts, BN, (a.m + kBM * CG - 1) / (kBM * CG));
+        build_segments(seg, a.offsets, a.rows, a.experts, MODE == kWeightsK ? kPartRows : BN,
+                       MODE == kWeightsK ? 1 : (a.m + kBM * CG - 1) / (kBM * CG));
     bw::fence_before();
     __syncthreads();
     if (CG == 2) bw::cluster_sync();
@@ -221,6 +241,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                if (MODE == kWeightsK && q.cols == 0) continue;
                 const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;  // of this CTA
                 const int boxes = (cols + 63) / 64;
                 const int m = q.m0 + int(rank) * kBM, n = q.n0 + int(rank) * cols;
@@ -242,7 +263,9 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         if (CG == 2) bw::bar_arrive(b);
                     }
                     const int r = q.r0 + kb * kBK;
-                    if (MODE == kRowsK) {
+                    if (MODE == kWeightsK) {
+                        bw::copy_2d<CG == 2>(sa, &map_a, r, m, b);
+                    } else if (MODE == kRowsK) {
                         bw::copy_3d<CG == 2>(sa, &map_a, r, m, q.e, b);
                     } else if (MODE == kRowsMN) {
                         bw::copy_3d<CG == 2>(sa, &map_a, m, r, q.e, b);
@@ -266,10 +289,13 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         if (rank == 0 && bw::elect_one()) {  // products
             int it = 0, tile = 0;
             bool ok = true;
-            for (int t = first; t < tiles && ok; t += step, ++tile) {
+            for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                if (MODE == kWeightsK && q.cols == 0) continue;
                 const uint32_t n = (q.cols + 16 * CG - 1) / (16 * CG) * (16 * CG);
-                const uint32_t shape = bw::f16_shape(std::is_same<T, __nv_bfloat16>::value, MODE != kRowsK, MODE == kWeights, kBM * CG, n);
+                const uint32_t shape =
+                    kTf32 ? bw::tf32_shape(kBM * CG, n)
+                          : bw::f16_shape(std::is_same<T, __nv_bfloat16>::value, kAMn, MODE == kWeights, kBM * CG, n);
                 const int half = tile & 1;
                 if (tile >= 2 && !bw::bar_wait(bar(&free_[half]), (tile / 2 - 1) & 1, &gave_up)) break;
                 bw::fence_after();
@@ -285,17 +311,21 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         bw::fence_cluster();  // the other CTA's zeros
                     bw::fence_after();
                     const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
-                    const uint64_t da = bw::operand(sa, MODE == kRowsK ? 16 : kBoxBytes);
+                    const uint64_t da = bw::operand(sa, kAMn ? kBoxBytes : 16);
                     const uint64_t db = bw::operand(sb, MODE == kWeights ? kBoxBytes : 16);
                     const int left = q.r - kb * kBK;
-                    const int ks = left >= kBK ? kBK / 16 : (left + 15) / 16;
+                    const int ks = left >= kBK ? kBK / kStep : (left + kStep - 1) / kStep;
 #pragma unroll 4
                     for (int i = 0; i < ks; ++i)
-                        bw::mma<CG>(d, da + i * (MODE == kRowsK ? 2 : 128), db + i * (MODE == kWeights ? 128 : 2),
-                                    shape, kb > 0 || i > 0);
+                        if constexpr (kTf32)
+                            bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, kb > 0 || i > 0);
+                        else
+                            bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape,
+                                        kb > 0 || i > 0);
                     bw::commit<CG>(bar(&empty[s]));
                 }
                 if (ok) bw::commit<CG>(bar(&done[half]));
+                ++tile;
             }
         }
     } else if (warp == 6) {
@@ -304,6 +334,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             uint32_t uses = 0;  // parity of each stage's tail barrier
             for (int t = first; t < tiles; t += step) {
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                if (MODE == kWeightsK && q.cols == 0) continue;
                 const int blocks = (q.r + kBK - 1) / kBK;
                 it += blocks;
                 if ((q.r & 15) == 0) continue;
@@ -326,10 +357,12 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         }
     } else {  // finished tiles
         int tile = 0;
-        for (int t = first; t < tiles; t += step, ++tile) {
+        for (int t = first; t < tiles; t += step) {
             const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+            if (MODE == kWeightsK && q.cols == 0) continue;
             const int half = tile & 1;
             const bool ok = bw::bar_wait(bar(&done[half]), (tile / 2) & 1, &gave_up);
+            ++tile;
             if (!__all_sync(0xffffffffu, ok)) break;
             bw::fence_after();
             const int feature = q.m0 + int(rank) * kBM + warp * 32 + lane;
@@ -348,10 +381,11 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     __syncwarp();
                     if (lane == 0) bw::bar_arrive_cluster(lead(&free_[half]));
                 }
-                if (MODE == kWeights) {
-                    stage_columns<T>(lines[warp], c0 / 8 % 8, v);
-                    if (c0 % 64 || c0 + 32 >= q.cols)
-                        store_lines<T>(lines[warp], a, q, feature - lane, c0 & ~63);
+                if (kOut) {
+                    constexpr int kCols = 128 / sizeof(T);  // of a staged line
+                    stage_columns<T>(lines[warp], c0 % kCols * int(sizeof(T)) / 16, v);
+                    if ((c0 + 32) % kCols == 0 || c0 + 32 >= q.cols)
+                        store_lines<T>(lines[warp], a, q, feature - lane, c0 & ~(kCols - 1));
                 } else {
                     store_rows<T>(a, q, feature, c0, v);
                 }
@@ -390,16 +424,20 @@ EncodeTiled encode_tiled()
     return fn;
 }
 
-// A map of 16-bit elements [z][y][x], x contiguous, copied in boxes of 64 x `box_y`.
-bool make_map(CUtensorMap &map, bool bf16, const void *base, int64_t x, int64_t y, int64_t z,
+// A map of elements [z][y][x], x contiguous, copied in boxes of 128 bytes x `box_y`.
+bool make_map(CUtensorMap &map, int dtype, const void *base, int64_t x, int64_t y, int64_t z,
               int64_t stride_y, int64_t stride_z, int box_y)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)};
-    const cuuint64_t strides[2] = {cuuint64_t(stride_y) * 2, cuuint64_t(stride_z) * 2};
-    const cuuint32_t box[3] = {64, cuuint32_t(box_y), 1}, one[3] = {1, 1, 1};
-    return encode(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+    const int bytes = dtype_bytes(dtype);
+    const cuuint64_t strides[2] = {cuuint64_t(stride_y) * bytes, cuuint64_t(stride_z) * bytes};
+    const cuuint32_t box[3] = {cuuint32_t(kBKBytes / bytes), cuuint32_t(box_y), 1}, one[3] = {1, 1, 1};
+    const CUtensorMapDataType type = dtype == DC_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                     : dtype == DC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return encode(&map, type,
                   stride_z ? 3 : 2, const_cast<void *>(base), dims, strides, box, one,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -411,7 +449,7 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
 {
     static_assert(STAGES <= kMaxStages, "");
     auto kernel = expert_mma_kernel<T, MODE, CG, BN, STAGES>;
-    constexpr size_t ring = size_t(STAGES) * (kABytes + BN / CG * kBK * 2) + 1024;
+    constexpr size_t ring = size_t(STAGES) * (kABytes + BN / CG * kBKBytes) + 1024;
     const size_t smem = ring + segments_bytes(a.experts);
     static DeviceCache cache;
     int ready = 0, sms = 0;
@@ -440,8 +478,8 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
 
 }  // namespace
 
-// Operands on 16-byte boundaries, as expert_dispatch.cu has made sure.
-cudaError_t expert_mma_rows(bool bf16, const ExpertArgs &g, cudaStream_t stream)
+// Operands on 16-byte boundaries, or tf32 parts, as expert_dispatch.cu makes them.
+cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
 {
     const bool k_major = g.b_r == 1;
     const int64_t stride = k_major ? g.b_n : g.b_r;
@@ -449,33 +487,41 @@ cudaError_t expert_mma_rows(bool bf16, const ExpertArgs &g, cudaStream_t stream)
     // with one expert the stride between experts is not used, but it has to be valid
     const int64_t expert = g.experts == 1 ? stride * outer : g.b_e;
     CUtensorMap ma, mb;
-    if (!make_map(ma, bf16, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
-        !make_map(mb, bf16, g.a, g.r, g.rows, 1, g.a_m, 0, 64))
+    if (!make_map(ma, dtype, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
+        !make_map(mb, dtype, g.a, g.r, g.rows, 1, g.a_m, 0, 64))
         return cudaErrorInvalidValue;
-    MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false};
+    MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false, 0};
     a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;
     constexpr int BN = 256;
     const int64_t tiles = (g.rows / BN + g.experts + 2) * ((g.n + 255) / 256);
-    if (bf16)
+    if (dtype == DC_FP32) return launch_typed<float, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream);
+    if (dtype == DC_BF16)
         return k_major ? launch_typed<__nv_bfloat16, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
                        : launch_typed<__nv_bfloat16, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
     return k_major ? launch_typed<__half, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
                    : launch_typed<__half, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
 }
 
-cudaError_t expert_mma_weights(bool bf16, const ExpertArgs &g, cudaStream_t stream)
+// Floats: a and b are parts [feature][summed], of stride a_r and b_r, for experts of at least
+// `least` rows.
+cudaError_t expert_mma_weights(int dtype, const ExpertArgs &g, int least, cudaStream_t stream)
 {
     CUtensorMap ma, mb;
-    if (!make_map(ma, bf16, g.a, g.m, g.rows, 1, g.a_r, 0, 64) ||
-        !make_map(mb, bf16, g.b, g.n, g.rows, 1, g.b_r, 0, 64))
+    const bool parts = dtype == DC_FP32;
+    if (parts ? !make_map(ma, dtype, g.a, g.a_r, g.m, 1, g.a_r, 0, 128) ||
+                    !make_map(mb, dtype, g.b, g.b_r, g.n, 1, g.b_r, 0, 64)
+              : !make_map(ma, dtype, g.a, g.m, g.rows, 1, g.a_r, 0, 64) ||
+                    !make_map(mb, dtype, g.b, g.n, g.rows, 1, g.b_r, 0, 64))
         return cudaErrorInvalidValue;
-    MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false};
-    a.wide = g.c_m % 8 == 0 && g.c_e % 8 == 0 && aligned16(g.c);
+    MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false, least};
+    const int v = 16 / dtype_bytes(dtype);
+    a.wide = g.c_m % v == 0 && g.c_e % v == 0 && aligned16(g.c);
     constexpr int BN = 256;
     const int64_t tiles = int64_t(g.experts) * ((g.m + 255) / 256) * ((g.n + BN - 1) / BN);
     if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;
-    return bf16 ? launch_typed<__nv_bfloat16, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream)
-                : launch_typed<__half, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream);
+    return parts                ? launch_typed<float, kWeightsK, 2, BN, 6>(ma, mb, a, tiles, stream)
+           : dtype == DC_BF16 ? launch_typed<__nv_bfloat16, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream)
+                                : launch_typed<__half, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream);
 }
 
 }  // namespace dc

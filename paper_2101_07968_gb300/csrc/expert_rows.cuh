@@ -15,6 +15,9 @@ struct Segments {
     int count;       // experts + 2
 };
 
+// Float operands of a weight gradient are stored with each segment's rows rounded up to this.
+constexpr int kPartRows = 32;
+
 __host__ __device__ inline size_t segments_bytes(int experts) { return size_t(experts + 3) * 8; }
 
 __device__ __forceinline__ Segments segments_at(void *smem, int experts)

@@ -1,4 +1,4 @@
-// Expert products on the CUDA cores: any element type, stride and alignment. Tiles of
+// Small products of floats on the CUDA cores: any stride and alignment. Tiles of
 // 64 x 64, staged in shared memory as floats, 4 x 4 sums per thread.
 #include "expert_rows.cuh"
 
@@ -22,7 +22,7 @@ __device__ __forceinline__ void stage(float (&s)[kDepth][kTile + 1], const T *p,
 // WEIGHTS false: the block's tile of rows times the expert's matrix. true: the expert's
 // rows are what is summed over.
 template <typename T, bool WEIGHTS>
-__global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g)
+__global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int64_t most)
 {
     extern __shared__ int32_t dyn[];
     __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g)
         e = blockIdx.z;
         const int64_t r0 = seg.start[e + 1];
         depth = seg.start[e + 2] - r0;
+        if (depth > most) return;
         const int m0 = blockIdx.y * kTile;
         rows = min(kTile, g.m - m0);
         a += m0 * g.a_m + r0 * g.a_r;
@@ -92,15 +93,15 @@ cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream)
     const int64_t tiles = a.rows / kTile + a.experts + 2;
     const unsigned ty = unsigned(tiles < 32768 ? tiles : 32768);
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), ty, unsigned((tiles + ty - 1) / ty));
-    expert_simt_kernel<float, false><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a);
+    expert_simt_kernel<float, false><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a, 0);
     return cudaGetLastError();
 }
 
-cudaError_t expert_simt_weights(const ExpertArgs &a, cudaStream_t stream)
+cudaError_t expert_simt_weights(const ExpertArgs &a, int64_t most, cudaStream_t stream)
 {
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), unsigned((a.m + kTile - 1) / kTile),
                     unsigned(a.experts));
-    expert_simt_kernel<float, true><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a);
+    expert_simt_kernel<float, true><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a, most);
     return cudaGetLastError();
 }
 

@@ -141,12 +141,13 @@ size_t expert_workspace(int dtype, const ExpertArgs &a, bool weights);
 cudaError_t launch_expert_rows(int dtype, const ExpertArgs &a, void *workspace, cudaStream_t stream);
 cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, void *workspace,
                                   cudaStream_t stream);
-// the kernels behind them: 16-bit operands on 16-byte boundaries on the tensor cores
-// (expert_mma.cu), few rows of any type (expert_few.cu), floats (expert_simt.cu)
-cudaError_t expert_mma_rows(bool bf16, const ExpertArgs &a, cudaStream_t stream);
-cudaError_t expert_mma_weights(bool bf16, const ExpertArgs &a, cudaStream_t stream);
+// The kernels behind them: the tensor cores (expert_mma.cu) for 16-bit operands on 16-byte
+// boundaries and floats in tf32 parts, few rows of any type (expert_few.cu), the CUDA cores
+// for small float products (expert_simt.cu; experts of `most` rows or fewer).
+cudaError_t expert_mma_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
+cudaError_t expert_mma_weights(int dtype, const ExpertArgs &a, int least, cudaStream_t stream);
 cudaError_t expert_few_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
 cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream);
-cudaError_t expert_simt_weights(const ExpertArgs &a, cudaStream_t stream);
+cudaError_t expert_simt_weights(const ExpertArgs &a, int64_t most, cudaStream_t stream);
 
 }  // namespace dc
