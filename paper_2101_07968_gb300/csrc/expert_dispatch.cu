@@ -81,7 +81,12 @@ void operands(const ExpertArgs &g, bool weights, Matrix &a, Matrix &b)
     }
 }
 
-bool few(const ExpertArgs &g, bool weights) { return !weights && g.rows <= DC_FEW_ROWS; }
+// Floats go that way up to 64 rows: their parts would cost three times the weights' bytes to
+// write (30 rows over 4 experts x 2,048 x 2,048: 140 us).
+bool few(int dtype, const ExpertArgs &g, bool weights)
+{
+    return !weights && g.rows <= (dtype == DC_FP32 ? 4 * DC_FEW_ROWS : DC_FEW_ROWS);
+}
 
 // ----------------------------------------------------------------- floats in parts
 constexpr int kPartDepth = 64, kPartLeast = 8;
@@ -246,7 +251,7 @@ cudaError_t float_weights(const ExpertArgs &g, void *workspace, cudaStream_t str
 
 size_t expert_workspace(int dtype, const ExpertArgs &g, bool weights)
 {
-    if (few(g, weights)) return 0;
+    if (few(dtype, g, weights)) return 0;
     if (dtype == DC_FP32) {
         if (!use_parts(g, weights)) return 0;
         return weights ? part_bytes(g.m, part_rows(g)) + part_bytes(g.n, part_rows(g))
@@ -259,7 +264,7 @@ size_t expert_workspace(int dtype, const ExpertArgs &g, bool weights)
 
 cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, cudaStream_t stream)
 {
-    if (few(g, false)) return expert_few_rows(dtype, g, stream);
+    if (few(dtype, g, false)) return expert_few_rows(dtype, g, stream);
     if (dtype == DC_FP32) return use_parts(g, false) ? float_rows(g, workspace, stream) : expert_simt_rows(g, stream);
     Matrix a, b;
     operands(g, false, a, b);

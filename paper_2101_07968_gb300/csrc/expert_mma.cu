@@ -31,8 +31,7 @@ constexpr int kBKBytes = 128;            // summed axis per stage: a line
 constexpr int kBM = 128;                 // features per CTA
 constexpr int kThreads = 7 * 32;
 constexpr uint32_t kABytes = kBM * kBKBytes;
-constexpr uint32_t kBoxBytes = 64 * kBKBytes;  // B comes in boxes of 64 rows
-constexpr int kMaxStages = 12;
+constexpr uint32_t kBoxBytes = 64 * kBKBytes;  // a box of 64 lines
 
 enum { kRowsK, kRowsMN, kWeights, kWeightsK };  // rows with A K-major or MN-major; weights MN- or K-major
 
@@ -89,6 +88,10 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
     return q;
 }
 
+// Rows (MN-major: columns, in whole lines) of B that a CTA's stage holds.
+template <int MODE, int CG, int BN>
+constexpr int kStageRows = MODE == kWeights && BN / CG < 64 ? 64 : BN / CG;
+
 template <int MODE, int CG, int BN>
 __device__ __forceinline__ int tile_count(const MmaArgs &a, const Segments &seg)
 {
@@ -130,11 +133,10 @@ __device__ __forceinline__ void store_rows(const MmaArgs &a, const Tile &q, int 
         }
         return;
     }
-    if (feature < a.m) {
+    if (feature >= a.m) return;
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) p[j * a.c_m] = from_float<T>(v[j]);
-    }
+    for (int j = 0; j < 32; ++j)
+        if (j < n) p[j * a.c_m] = from_float<T>(v[j]);
 }
 
 // Rows of dW: a lane holds a row's neighbours, so 128 bytes a row go through shared memory
@@ -178,7 +180,7 @@ __device__ __forceinline__ void store_lines(const Lines &s, const MmaArgs &a, co
     } else {
         for (int row = 0; row < 32 && row0 + row < a.m; ++row)
             for (int c = lane; c < n; c += 32)
-                p[row * a.c_m + c] = reinterpret_cast<const T *>(&s.u[row][(c / V) ^ (row & 7)])[c % V];
+            p[row * a.c_m + c] = reinterpret_cast<const T *>(&s.u[row][(c / V) ^ (row & 7)])[c % V];
     }
     __syncwarp();
 }
@@ -188,10 +190,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                   const MmaArgs a)
 {
-    constexpr uint32_t kBBytes = BN / CG * kBKBytes;
+    // B: boxes of up to 64 rows, or (MN-major) of 64 columns
+    constexpr int kBoxRows = MODE == kWeights || BN / CG > 64 ? 64 : BN / CG;
+    constexpr uint32_t kBBox = kBoxRows * kBKBytes;
+    constexpr uint32_t kBBytes = kStageRows<MODE, CG, BN> * kBKBytes;
     constexpr int kBK = kBKBytes / sizeof(T), kStep = 32 / sizeof(T);  // per stage, per product
     constexpr bool kTf32 = std::is_same<T, float>::value, kOut = MODE == kWeights || MODE == kWeightsK;
     constexpr bool kAMn = MODE == kRowsMN || MODE == kWeights;
+    // Blocks summed in the tensor cores at a time. They cut a sum off at every step where a
+    // float would round, toward zero, some 2e-8 of it: over 192 steps float products came
+    // out 4e-6 off, ten times what sums in floats lose. So those of floats are handed over every
+    // 16 steps and added up in registers, rounded.
+    constexpr int kRound = kTf32 ? 4 : 1 << 24;
     constexpr uint32_t kStage = kABytes + kBBytes;
     constexpr uint32_t kColumns = BN * 2 < 32 ? 32 : BN * 2;
     extern __shared__ unsigned char dyn[];
@@ -243,7 +253,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
                 if (MODE == kWeightsK && q.cols == 0) continue;
                 const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;  // of this CTA
-                const int boxes = (cols + 63) / 64;
+                const int boxes = (cols + kBoxRows - 1) / kBoxRows;
                 const int m = q.m0 + int(rank) * kBM, n = q.n0 + int(rank) * cols;
                 const int blocks = (q.r + kBK - 1) / kBK;
                 for (int kb = 0; kb < blocks; ++kb, ++it) {
@@ -255,7 +265,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
                     const bool zeros = MODE == kWeights && kb == blocks - 1 && (q.r & 15);
                     const uint32_t b = zeros ? bar(&tail[s]) : lead(&full[s]);
-                    const uint32_t bytes = kABytes + boxes * kBoxBytes;
+                    const uint32_t bytes = kABytes + boxes * kBBox;
                     if (zeros) {
                         bw::bar_arrive_bytes(b, bytes);
                     } else if (rank == 0) {  // for both CTAs: the other's bytes count here too
@@ -276,9 +286,9 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     }
                     for (int i = 0; i < boxes; ++i)
                         if (MODE == kWeights)
-                            bw::copy_2d<CG == 2>(sb + i * kBoxBytes, &map_b, n + 64 * i, r, b);
+                            bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, n + kBoxRows * i, r, b);
                         else
-                            bw::copy_2d<CG == 2>(sb + i * kBoxBytes, &map_b, r, n + 64 * i, b);
+                            bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, r, n + kBoxRows * i, b);
                 }
             }
             // the products' arrivals land in this CTA's memory: it may not end before them
@@ -296,36 +306,37 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 const uint32_t shape =
                     kTf32 ? bw::tf32_shape(kBM * CG, n)
                           : bw::f16_shape(std::is_same<T, __nv_bfloat16>::value, kAMn, MODE == kWeights, kBM * CG, n);
-                const int half = tile & 1;
-                if (tile >= 2 && !bw::bar_wait(bar(&free_[half]), (tile / 2 - 1) & 1, &gave_up)) break;
-                bw::fence_after();
-                const uint32_t d = tmem + half * BN;
                 const int blocks = (q.r + kBK - 1) / kBK;
-                for (int kb = 0; kb < blocks; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (!bw::bar_wait(bar(&full[s]), (it / STAGES) & 1, &gave_up)) {
-                        ok = false;
-                        break;
-                    }
-                    if (CG == 2 && MODE == kWeights && kb == blocks - 1 && (q.r & 15))
-                        bw::fence_cluster();  // the other CTA's zeros
+                for (int k0 = 0; (k0 == 0 || k0 < blocks) && ok; k0 += kRound, ++tile) {
+                    const int half = tile & 1;
+                    ok = tile < 2 || bw::bar_wait(bar(&free_[half]), (tile / 2 - 1) & 1, &gave_up);
+                    if (!ok) break;
                     bw::fence_after();
-                    const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
-                    const uint64_t da = bw::operand(sa, kAMn ? kBoxBytes : 16);
-                    const uint64_t db = bw::operand(sb, MODE == kWeights ? kBoxBytes : 16);
-                    const int left = q.r - kb * kBK;
-                    const int ks = left >= kBK ? kBK / kStep : (left + kStep - 1) / kStep;
+                    const uint32_t d = tmem + half * BN;
+                    const int k1 = min(blocks, k0 + kRound);
+                    for (int kb = k0; kb < k1; ++kb, ++it) {
+                        const int s = it % STAGES;
+                        ok = bw::bar_wait(bar(&full[s]), (it / STAGES) & 1, &gave_up);
+                        if (!ok) break;
+                        if (CG == 2 && MODE == kWeights && kb == blocks - 1 && (q.r & 15))
+                            bw::fence_cluster();  // the other CTA's zeros
+                        bw::fence_after();
+                        const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
+                        const uint64_t da = bw::operand(sa, kAMn ? kBoxBytes : 16);
+                        const uint64_t db = bw::operand(sb, MODE == kWeights ? kBoxBytes : 16);
+                        const int left = q.r - kb * kBK;
+                        const int ks = left >= kBK ? kBK / kStep : (left + kStep - 1) / kStep;
 #pragma unroll 4
-                    for (int i = 0; i < ks; ++i)
-                        if constexpr (kTf32)
-                            bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, kb > 0 || i > 0);
-                        else
-                            bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape,
-                                        kb > 0 || i > 0);
-                    bw::commit<CG>(bar(&empty[s]));
+                        for (int i = 0; i < ks; ++i)
+                            if constexpr (kTf32)
+                                bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, kb > k0 || i > 0);
+                            else
+                                bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2),
+                                            shape, kb > k0 || i > 0);
+                        bw::commit<CG>(bar(&empty[s]));
+                    }
+                    if (ok) bw::commit<CG>(bar(&done[half]));
                 }
-                if (ok) bw::commit<CG>(bar(&done[half]));
-                ++tile;
             }
         }
     } else if (warp == 6) {
@@ -357,30 +368,13 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         }
     } else {  // finished tiles
         int tile = 0;
-        for (int t = first; t < tiles; t += step) {
+        bool ok = true;
+        for (int t = first; t < tiles && ok; t += step) {
             const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
             if (MODE == kWeightsK && q.cols == 0) continue;
-            const int half = tile & 1;
-            const bool ok = bw::bar_wait(bar(&done[half]), (tile / 2) & 1, &gave_up);
-            ++tile;
-            if (!__all_sync(0xffffffffu, ok)) break;
-            bw::fence_after();
             const int feature = q.m0 + int(rank) * kBM + warp * 32 + lane;
-            const uint32_t at = tmem + half * BN + (uint32_t(warp * 32) << 16);
-            float v[32];
-            for (int c0 = 0; c0 < q.cols; c0 += 32) {
-                __syncwarp();
-                if (q.r > 0) {
-                    bw::tmem_load(at + c0, v);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-                }
-                if (c0 + 32 >= q.cols) {  // all read: the half may be overwritten
-                    bw::fence_before();
-                    __syncwarp();
-                    if (lane == 0) bw::bar_arrive_cluster(lead(&free_[half]));
-                }
+            const int blocks = (q.r + kBK - 1) / kBK;
+            auto out = [&](int c0, const float (&v)[32]) {
                 if (kOut) {
                     constexpr int kCols = 128 / sizeof(T);  // of a staged line
                     stage_columns<T>(lines[warp], c0 % kCols * int(sizeof(T)) / 16, v);
@@ -388,6 +382,60 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         store_lines<T>(lines[warp], a, q, feature - lane, c0 & ~(kCols - 1));
                 } else {
                     store_rows<T>(a, q, feature, c0, v);
+                }
+            };
+            constexpr int kChunks = BN / 32;
+            float sum[kTf32 ? kChunks : 1][32];  // floats: the rounds so far
+            if (kTf32) {
+#pragma unroll
+                for (int c = 0; c < (kTf32 ? kChunks : 1); ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
+            }
+            for (int k0 = 0; k0 == 0 || k0 < blocks; k0 += kRound, ++tile) {
+                const int half = tile & 1;
+                ok = bw::bar_wait(bar(&done[half]), (tile / 2) & 1, &gave_up);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                bw::fence_after();
+                const uint32_t at = tmem + half * BN + (uint32_t(warp * 32) << 16);
+                auto all_read = [&] {  // the half may be overwritten
+                    bw::fence_before();
+                    __syncwarp();
+                    if (lane == 0) bw::bar_arrive_cluster(lead(&free_[half]));
+                };
+                if constexpr (kTf32) {
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) {
+                        if (c * 32 < q.cols && blocks > 0) {
+                            float v[32];
+                            __syncwarp();
+                            bw::tmem_load(at + c * 32, v);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                        }
+                    }
+                    all_read();
+                } else {
+                    float v[32];
+                    for (int c0 = 0; c0 < q.cols; c0 += 32) {
+                        __syncwarp();
+                        if (blocks > 0) {
+                            bw::tmem_load(at + c0, v);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                        }
+                        if (c0 + 32 >= q.cols) all_read();
+                        out(c0, v);
+                    }
+                }
+            }
+            if constexpr (kTf32) {
+                if (ok) {
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+                        if (c * 32 < q.cols) out(c * 32, sum[c]);
                 }
             }
         }
@@ -447,9 +495,8 @@ template <typename T, int MODE, int CG, int BN, int STAGES>
 cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const MmaArgs &a,
                          int64_t most_tiles, cudaStream_t stream)
 {
-    static_assert(STAGES <= kMaxStages, "");
-    auto kernel = expert_mma_kernel<T, MODE, CG, BN, STAGES>;
-    constexpr size_t ring = size_t(STAGES) * (kABytes + BN / CG * kBKBytes) + 1024;
+        auto kernel = expert_mma_kernel<T, MODE, CG, BN, STAGES>;
+    constexpr size_t ring = size_t(STAGES) * (kABytes + kStageRows<MODE, CG, BN> * kBKBytes) + 1024;
     const size_t smem = ring + segments_bytes(a.experts);
     static DeviceCache cache;
     int ready = 0, sms = 0;
@@ -476,6 +523,22 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
     return cudaLaunchKernelEx(&lc, kernel, ma, mb, a);
 }
 
+// Tiles of 256 rows (columns of dW) read the least. Tiles of 64 are four times as many, and a
+// step of one takes some 320 cycles against 512, bound by what an SM can read; so they pay
+// where all of them still fit in one round (1,234 rows over 7 experts x 515 x 1,001, dx: 8.7 us
+// against 11.9), but not above (4,000 rows over 2 x 1,024 x 1,024 floats: 132 us against 76).
+int tile_rows(int dtype, int64_t tiles) { return 4 * tiles <= 76 ? 64 : dtype == DC_FP32 ? 128 : 256; }
+
+template <typename T, int MODE>
+cudaError_t launch_size(int bn, const CUtensorMap &ma, const CUtensorMap &mb, const MmaArgs &a, int64_t tiles,
+                        cudaStream_t stream)
+{
+    // floats: 128 sums a thread of the four warps that add up the rounds
+    constexpr int kWide = std::is_same<T, float>::value ? 128 : 256;
+    return bn == 64 ? launch_typed<T, MODE, 2, 64, 8>(ma, mb, a, tiles, stream)
+                    : launch_typed<T, MODE, 2, kWide, kWide == 128 ? 8 : 6>(ma, mb, a, tiles, stream);
+}
+
 }  // namespace
 
 // Operands on 16-byte boundaries, or tf32 parts, as expert_dispatch.cu makes them.
@@ -486,42 +549,45 @@ cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
     const int64_t inner = k_major ? g.r : g.n, outer = k_major ? g.n : g.r;
     // with one expert the stride between experts is not used, but it has to be valid
     const int64_t expert = g.experts == 1 ? stride * outer : g.b_e;
+    // tiles of an average expert
+    const int64_t nm = (g.n + 255) / 256, each = (g.rows + g.experts - 1) / g.experts;
+    const int bn = tile_rows(dtype, g.experts * nm * ((each + 255) / 256));
     CUtensorMap ma, mb;
     if (!make_map(ma, dtype, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
-        !make_map(mb, dtype, g.a, g.r, g.rows, 1, g.a_m, 0, 64))
+        !make_map(mb, dtype, g.a, g.r, g.rows, 1, g.a_m, 0, bn < 128 ? bn / 2 : 64))
         return cudaErrorInvalidValue;
     MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false, 0};
     a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;
-    constexpr int BN = 256;
-    const int64_t tiles = (g.rows / BN + g.experts + 2) * ((g.n + 255) / 256);
-    if (dtype == DC_FP32) return launch_typed<float, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream);
+    const int64_t tiles = (g.rows / bn + g.experts + 2) * nm;
+    if (dtype == DC_FP32) return launch_size<float, kRowsK>(bn, ma, mb, a, tiles, stream);
     if (dtype == DC_BF16)
-        return k_major ? launch_typed<__nv_bfloat16, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
-                       : launch_typed<__nv_bfloat16, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
-    return k_major ? launch_typed<__half, kRowsK, 2, BN, 6>(ma, mb, a, tiles, stream)
-                   : launch_typed<__half, kRowsMN, 2, BN, 6>(ma, mb, a, tiles, stream);
+        return k_major ? launch_size<__nv_bfloat16, kRowsK>(bn, ma, mb, a, tiles, stream)
+                       : launch_size<__nv_bfloat16, kRowsMN>(bn, ma, mb, a, tiles, stream);
+    return k_major ? launch_size<__half, kRowsK>(bn, ma, mb, a, tiles, stream)
+                   : launch_size<__half, kRowsMN>(bn, ma, mb, a, tiles, stream);
 }
 
 // Floats: a and b are parts [feature][summed], of stride a_r and b_r, for experts of at least
 // `least` rows.
 cudaError_t expert_mma_weights(int dtype, const ExpertArgs &g, int least, cudaStream_t stream)
 {
+    const int64_t nm = (g.m + 255) / 256;
+    const int bn = tile_rows(dtype, g.experts * nm * ((g.n + 255) / 256));
     CUtensorMap ma, mb;
     const bool parts = dtype == DC_FP32;
     if (parts ? !make_map(ma, dtype, g.a, g.a_r, g.m, 1, g.a_r, 0, 128) ||
-                    !make_map(mb, dtype, g.b, g.b_r, g.n, 1, g.b_r, 0, 64)
+                    !make_map(mb, dtype, g.b, g.b_r, g.n, 1, g.b_r, 0, bn < 128 ? bn / 2 : 64)
               : !make_map(ma, dtype, g.a, g.m, g.rows, 1, g.a_r, 0, 64) ||
                     !make_map(mb, dtype, g.b, g.n, g.rows, 1, g.b_r, 0, 64))
         return cudaErrorInvalidValue;
     MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false, least};
     const int v = 16 / dtype_bytes(dtype);
     a.wide = g.c_m % v == 0 && g.c_e % v == 0 && aligned16(g.c);
-    constexpr int BN = 256;
-    const int64_t tiles = int64_t(g.experts) * ((g.m + 255) / 256) * ((g.n + BN - 1) / BN);
+    const int64_t tiles = int64_t(g.experts) * nm * ((g.n + bn - 1) / bn);
     if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;
-    return parts                ? launch_typed<float, kWeightsK, 2, BN, 6>(ma, mb, a, tiles, stream)
-           : dtype == DC_BF16 ? launch_typed<__nv_bfloat16, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream)
-                                : launch_typed<__half, kWeights, 2, BN, 6>(ma, mb, a, tiles, stream);
+    return parts              ? launch_size<float, kWeightsK>(bn, ma, mb, a, tiles, stream)
+           : dtype == DC_BF16 ? launch_size<__nv_bfloat16, kWeights>(bn, ma, mb, a, tiles, stream)
+                              : launch_size<__half, kWeights>(bn, ma, mb, a, tiles, stream);
 }
 
 }  // namespace dc
