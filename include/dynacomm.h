@@ -327,9 +327,10 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
  * or below an earlier one, counts as the nearest valid value. w and dw have the strides
  * w_expert, w_n, w_k (elements); one of w_n and w_k is 1.
  * 16-bit operands run on the tensor cores; those whose rows start off 16-byte boundaries
- * are first copied into the workspace, row by row, so that they start on them. Up to
- * DC_FEW_ROWS rows in all take a pass that streams the weights over every SM; float
- * operands run on the CUDA cores. workspace: dc_expert_workspace_bytes(shape, product, a,
+ * are first copied into the workspace, row by row, so that they start on them. Floats go
+ * there in three parts of 11 significant bits, whose products are summed as floats (small
+ * products of floats run on the CUDA cores). Up to DC_FEW_ROWS rows in all (floats: 16 times
+ * as many) take a pass that streams the weights over every SM. workspace: dc_expert_workspace_bytes(shape, product, a,
  * b) bytes, 256-byte aligned, used during the call's kernels only, where product is 0 for
  * y, 1 for dx, 2 for dW and a, b are the call's two operands in its order (their addresses
  * decide whether copies are needed); NULL where that is 0. status (device, nullable): set
@@ -339,7 +340,7 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
  * outside [1, DC_EXPERTS_MAX]; N or K outside [1, DC_LAYER_DIM_MAX]; a stride shorter than its
  * row, or above 2^40); DC_ERR_WORKSPACE; DC_ERR_CUDA.
  * ---------------------------------------------------------------------- */
-#define DC_FEW_ROWS 16
+#define DC_FEW_ROWS 4
 typedef struct dc_expert_shape {
     int32_t dtype; /* of x, y, w and their gradients */
     int32_t experts;

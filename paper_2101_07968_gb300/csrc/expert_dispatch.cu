@@ -81,11 +81,13 @@ void operands(const ExpertArgs &g, bool weights, Matrix &a, Matrix &b)
     }
 }
 
-// Floats go that way up to 64 rows: their parts would cost three times the weights' bytes to
-// write (30 rows over 4 experts x 2,048 x 2,048: 140 us).
+// Two rows, two experts x 4,096 x 2,048: 8.3 us, by tiles 12.2; eight rows 12.5 against 12.1;
+// sixteen rows of as many experts x 2,048 x 2,048 36 against 26.8. Floats go that way up to 64 rows:
+// their parts would cost three times the weights' bytes to write (30 rows over 4 experts x
+// 2,048 x 2,048: 55 us, in parts 140).
 bool few(int dtype, const ExpertArgs &g, bool weights)
 {
-    return !weights && g.rows <= (dtype == DC_FP32 ? 4 * DC_FEW_ROWS : DC_FEW_ROWS);
+    return !weights && g.rows <= (dtype == DC_FP32 ? 16 * DC_FEW_ROWS : DC_FEW_ROWS);
 }
 
 // ----------------------------------------------------------------- floats in parts

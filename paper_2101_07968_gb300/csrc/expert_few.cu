@@ -3,7 +3,7 @@
 // weights of the experts that have rows.
 //
 // A block takes one group of up to kGroup rows of one expert and a slice of features.
-// Weights with the summed axis contiguous: a warp per feature, lanes along the axis,
+// Weights with the summed axis contiguous: a warp per two features, lanes along the axis,
 // eight 16-byte loads a lane in flight. Weights with the features contiguous: a lane holds
 // several features and the block's lanes split the summed axis. The sums are added in a
 // fixed order.
@@ -73,24 +73,33 @@ __device__ __forceinline__ Group group_at(const ExpertArgs &g, int64_t r)
     return q;
 }
 
-// Weights with the summed axis contiguous.
+// Weights with the summed axis contiguous: kFeatures features of a warp at once, so that two
+// tokens' 8,192 products of 2,048 elements are all in flight in one round of blocks.
+constexpr int kFeatures = 2;
 template <typename T, int V, int ROWS>
 __device__ __forceinline__ void dot_rows(const ExpertArgs &g, const Group &q, int n)
 {
-    constexpr int U = V > 1 ? 8 : 16;  // loads in flight
+    constexpr int U = V > 1 ? 4 : 8;  // loads of a feature in flight
     const int lane = threadIdx.x & 31;
-    const T *w = static_cast<const T *>(g.b) + q.expert * g.b_e + n * g.b_n;
+    const T *w[kFeatures];
+#pragma unroll
+    for (int f = 0; f < kFeatures; ++f)  // the last feature again past the end
+        w[f] = static_cast<const T *>(g.b) + q.expert * g.b_e + int64_t(min(n + f, g.n - 1)) * g.b_n;
     const T *x = static_cast<const T *>(g.a) + q.row * g.a_m;
-    float acc[ROWS];
+    float acc[kFeatures][ROWS];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) acc[i] = 0.0f;
+    for (int f = 0; f < kFeatures; ++f)
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) acc[f][i] = 0.0f;
     for (int64_t k0 = lane * V; k0 < g.r; k0 += 32 * V * U) {
-        Vec<T, V> b[U];
+        Vec<T, V> b[kFeatures][U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t k = k0 + u * 32 * V;
-            if (k < g.r) b[u] = *reinterpret_cast<const Vec<T, V> *>(w + k);
-        }
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int f = 0; f < kFeatures; ++f) {
+                const int64_t k = k0 + u * 32 * V;
+                if (k < g.r) b[f][u] = *reinterpret_cast<const Vec<T, V> *>(w[f] + k);
+            }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t k = k0 + u * 32 * V;
@@ -99,27 +108,33 @@ __device__ __forceinline__ void dot_rows(const ExpertArgs &g, const Group &q, in
             for (int i = 0; i < ROWS; ++i) {
                 const Vec<T, V> a = *reinterpret_cast<const Vec<T, V> *>(x + i * g.a_m + k);
 #pragma unroll
-                for (int j = 0; j < V; ++j) acc[i] += to_float(a.e[j]) * to_float(b[u].e[j]);
+                for (int f = 0; f < kFeatures; ++f)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[f][i] += to_float(a.e[j]) * to_float(b[f][u].e[j]);
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
+    for (int f = 0; f < kFeatures; ++f)
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
-        if (lane == 0) static_cast<T *>(g.c)[(q.row + i) * g.c_m + n] = from_float<T>(acc[i]);
-    }
+        for (int i = 0; i < ROWS; ++i) {
+            float v = acc[f][i];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane == 0 && n + f < g.n) static_cast<T *>(g.c)[(q.row + i) * g.c_m + n + f] = from_float<T>(v);
+        }
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) few_dot_kernel(ExpertArgs g)
+__global__ void __launch_bounds__(kThreads, 2) few_dot_kernel(ExpertArgs g)
 {
     const Group q = group_at(g, blockIdx.y);
-    const int n = blockIdx.x * kWarps + threadIdx.x / 32;
-    if (q.rows == 0 || n >= g.n) return;
+    if (q.rows == 0) return;
+    const int n = (blockIdx.x * kWarps + threadIdx.x / 32) * kFeatures;
+    if (n >= g.n) return;
     if (q.expert < 0) {
-        if ((threadIdx.x & 31) < q.rows)
-            static_cast<T *>(g.c)[(q.row + (threadIdx.x & 31)) * g.c_m + n] = from_float<T>(0.0f);
+        const int i = (threadIdx.x & 31) / kFeatures, f = threadIdx.x % kFeatures;
+        if (i < q.rows && n + f < g.n) static_cast<T *>(g.c)[(q.row + i) * g.c_m + n + f] = from_float<T>(0.0f);
     } else if (q.rows == 1) {
         dot_rows<T, V, 1>(g, q, n);
     } else if (q.rows == 2) {
@@ -218,7 +233,8 @@ cudaError_t expert_few_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
     bool wide = aligned16(g.b) && stride % v == 0 && (g.experts == 1 || g.b_e % v == 0);
     if (dot) wide = wide && aligned16(g.a) && g.r % v == 0 && (g.rows == 1 || g.a_m % v == 0);
     else wide = wide && g.n % v == 0;
-    const dim3 grid(unsigned(dot ? (g.n + kWarps - 1) / kWarps : (g.n + kCols - 1) / kCols), unsigned(g.rows));
+    const dim3 grid(unsigned(dot ? (g.n + kWarps * kFeatures - 1) / (kWarps * kFeatures) : (g.n + kCols - 1) / kCols),
+                    unsigned(g.rows));
     DC_DTYPE_SWITCH(dtype, T, {
         constexpr int V = kVec<T>;
         if (dot) {

@@ -178,9 +178,32 @@ __device__ __forceinline__ void store_lines(const Lines &s, const MmaArgs &a, co
                 *reinterpret_cast<uint4 *>(p + row * a.c_m + unit * V) = s.u[row][unit ^ (row & 7)];
         }
     } else {
-        for (int row = 0; row < 32 && row0 + row < a.m; ++row)
-            for (int c = lane; c < n; c += 32)
-            p[row * a.c_m + c] = reinterpret_cast<const T *>(&s.u[row][(c / V) ^ (row & 7)])[c % V];
+        auto value = [&](int row, int c) {
+            return reinterpret_cast<const T *>(&s.u[row][(c / V) ^ (row & 7)])[c % V];
+        };
+        const int rows = min(32, a.m - row0);
+        if constexpr (sizeof(T) == 2) {
+            // rows that start on 2-byte boundaries: pairs from the next 4-byte boundary on, and
+            // what is left at both ends
+#pragma unroll 4
+            for (int row = 0; row < rows; ++row) {
+                T *r = p + row * a.c_m;
+                const int c = 2 * lane + int(reinterpret_cast<uintptr_t>(r) >> 1 & 1);
+                if (c + 1 < n) {
+                    Vec<T, 2> v;
+                    v.e[0] = value(row, c);
+                    v.e[1] = value(row, c + 1);
+                    *reinterpret_cast<Vec<T, 2> *>(r + c) = v;
+                } else if (c < n) {
+                    r[c] = value(row, c);
+                }
+                if (lane == 0 && c == 1) r[0] = value(row, 0);
+            }
+        } else {
+#pragma unroll 4
+            for (int row = 0; row < rows; ++row)
+                if (lane < n) p[row * a.c_m + lane] = value(row, lane);
+        }
     }
     __syncwarp();
 }

@@ -32,7 +32,7 @@ FWD, BWD = 0, 1
 DC_BF16, DC_FP16, DC_FP32 = 0, 1, 2
 DC_ACT_SILU, DC_ACT_GELU = 0, 1
 DC_NORM_RMS, DC_NORM_LAYER = 0, 1
-DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX, DC_FEW_ROWS = 1024, 1048576, 16384, 16
+DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX, DC_FEW_ROWS = 1024, 1048576, 16384, 4
 
 
 class DynaCommError(RuntimeError):

@@ -132,9 +132,9 @@ def measure(chain, x, assigned, dy, steps=5, warmup=2):
     return tuple([max(1, -int(-t * 1000 // steps)) for t in total[w]] for w in ("forward", "backward"))
 
 
-def profiles(fc, bc, parameters, links, bits=16, seed=0, bw=(1_000_000, 100_000_000), dt=(50, 5000)):
-    """Cost rows of one measured chain over `links` links: bandwidths (kbit/s) and latencies (us)
-    log-uniform in their ranges; pt = gt = ceil(bits * 1000 * parameters / bandwidth)."""
+def profiles(fc, bc, parameters, links, bits=16, seed=0, bw=(100_000_000, 10_000_000_000), dt=(5, 500)):
+    """Cost rows of one measured chain over `links` links, by default those of a machine room:
+    bandwidths (kbit/s) and latencies (us) log-uniform in their ranges; pt = gt = ceil(bits * 1000 * parameters / bandwidth)."""
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
 

@@ -54,7 +54,7 @@ def test_expert_workspace(lib):
     for which in range(3):
         assert q(shape(), which, FAKE, FAKE) == 0
         assert q(shape(), which, FAKE + 2, FAKE) > 0      # rows start off the boundary
-    assert q(shape(rows=16, K=33, ldx=33, w_n=33, w_expert=64 * 33), 0, FAKE, FAKE) == 0  # few rows
+    assert q(shape(rows=dc.DC_FEW_ROWS, K=33, ldx=33, w_n=33, w_expert=64 * 33), 0, FAKE, FAKE) == 0  # few rows
     assert q(shape(dtype=3), 0, FAKE, FAKE) == 0 and q(shape(), 3, FAKE, FAKE) == 0
     assert q(shape(rows=0), 0, FAKE, FAKE) == 0 and q(None, 0, FAKE, FAKE) == 0
     # floats: three parts of both operands
