@@ -223,10 +223,11 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     // Blocks summed in the tensor cores at a time. They cut a sum off at every step where a
     // float would round, toward zero, some 2e-8 of it: over 192 steps float products came
     // out 4e-6 off, ten times what sums in floats lose. So those of floats are handed over every
-    // 16 steps and added up in registers, rounded.
-    constexpr int kRound = kTf32 ? 4 : 1 << 24;
+    // 32 steps, which two sets of sums take in turn, and added up in registers, rounded: 3.5e-7 off.
+    constexpr int kRound = kTf32 ? 8 : 1 << 24;
     constexpr uint32_t kStage = kABytes + kBBytes;
-    constexpr uint32_t kColumns = BN * 2 < 32 ? 32 : BN * 2;
+    constexpr int kSets = kTf32 ? 2 : 1;
+    constexpr uint32_t kColumns = 2 * kSets * BN;
     extern __shared__ unsigned char dyn[];
     __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
     __shared__ uint32_t tmem_at, gave_up;
@@ -270,32 +271,32 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 
     if (warp == 4) {
         if (bw::elect_one()) {  // copies
-            int it = 0;
+            int s = 0, filled = 0;  // the next stage; stages filled so far, up to all
+            uint32_t phase = 1;     // of the stage's release: the first round waits for none
             bool ok = true;
+            const uint32_t full0 = lead(&full[0]);
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
                 if (MODE == kWeightsK && q.cols == 0) continue;
                 const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;  // of this CTA
                 const int boxes = (cols + kBoxRows - 1) / kBoxRows;
                 const int m = q.m0 + int(rank) * kBM, n = q.n0 + int(rank) * cols;
-                const int blocks = (q.r + kBK - 1) / kBK;
-                for (int kb = 0; kb < blocks; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (it >= STAGES && !bw::bar_wait(bar(&empty[s]), (it / STAGES - 1) & 1, &gave_up)) {
-                        ok = false;
+                const uint32_t bytes = kABytes + boxes * kBBox;
+                const int end = q.r0 + q.r;
+                for (int r = q.r0; r < end; r += kBK) {
+                    if (filled < STAGES)
+                        ++filled;
+                    else if (!(ok = bw::bar_wait(bar(&empty[s]), phase, &gave_up)))
                         break;
-                    }
                     const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
-                    const bool zeros = MODE == kWeights && kb == blocks - 1 && (q.r & 15);
-                    const uint32_t b = zeros ? bar(&tail[s]) : lead(&full[s]);
-                    const uint32_t bytes = kABytes + boxes * kBBox;
+                    const bool zeros = MODE == kWeights && end - r <= kBK && ((end - r) & 15);
+                    const uint32_t b = zeros ? bar(&tail[s]) : full0 + s * uint32_t(sizeof(uint64_t));
                     if (zeros) {
                         bw::bar_arrive_bytes(b, bytes);
                     } else if (rank == 0) {  // for both CTAs: the other's bytes count here too
-                        bw::bar_arrive_bytes(b, bytes * CG);
-                        if (CG == 2) bw::bar_arrive(b);
+                        bw::bar_arrive_bytes(bar(&full[s]), bytes * CG);
+                        if (CG == 2) bw::bar_arrive(bar(&full[s]));
                     }
-                    const int r = q.r0 + kb * kBK;
                     if (MODE == kWeightsK) {
                         bw::copy_2d<CG == 2>(sa, &map_a, r, m, b);
                     } else if (MODE == kRowsK) {
@@ -312,15 +313,24 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, n + kBoxRows * i, r, b);
                         else
                             bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, r, n + kBoxRows * i, b);
+                    if (++s == STAGES) {
+                        s = 0;
+                        phase ^= 1;
+                    }
                 }
             }
-            // the products' arrivals land in this CTA's memory: it may not end before them
-            for (int i = it > STAGES ? it - STAGES : 0; i < it && ok; ++i)
-                ok = bw::bar_wait(bar(&empty[i % STAGES]), (i / STAGES) & 1, &gave_up);
+            // The products' arrivals land in this CTA's memory: it may not end before them. The
+            // oldest stage in use comes next in turn.
+            for (int i = 0; i < filled && ok; ++i) {
+                const int at = filled == STAGES ? (s + i) % STAGES : i;
+                const uint32_t ph = filled == STAGES ? (s + i < STAGES ? phase : phase ^ 1) : 0;
+                ok = bw::bar_wait(bar(&empty[at]), ph, &gave_up);
+            }
         }
     } else if (warp == 5) {
         if (rank == 0 && bw::elect_one()) {  // products
-            int it = 0, tile = 0;
+            int s = 0, tile = 0;
+            uint32_t phase = 0;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
@@ -335,28 +345,36 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     ok = tile < 2 || bw::bar_wait(bar(&free_[half]), (tile / 2 - 1) & 1, &gave_up);
                     if (!ok) break;
                     bw::fence_after();
-                    const uint32_t d = tmem + half * BN;
+                    const uint32_t d = tmem + half * (kSets * BN);
                     const int k1 = min(blocks, k0 + kRound);
-                    for (int kb = k0; kb < k1; ++kb, ++it) {
-                        const int s = it % STAGES;
-                        ok = bw::bar_wait(bar(&full[s]), (it / STAGES) & 1, &gave_up);
+                    for (int kb = k0; kb < k1; ++kb) {
+                        ok = bw::bar_wait(bar(&full[s]), phase, &gave_up);
                         if (!ok) break;
-                        if (CG == 2 && MODE == kWeights && kb == blocks - 1 && (q.r & 15))
+                        const int left = q.r - kb * kBK;
+                        if (CG == 2 && MODE == kWeights && left <= kBK && (left & 15))
                             bw::fence_cluster();  // the other CTA's zeros
                         bw::fence_after();
-                        const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
+                        const uint32_t sa = ring + s * kStage;
                         const uint64_t da = bw::operand(sa, kAMn ? kBoxBytes : 16);
-                        const uint64_t db = bw::operand(sb, MODE == kWeights ? kBoxBytes : 16);
-                        const int left = q.r - kb * kBK;
-                        const int ks = left >= kBK ? kBK / kStep : (left + kStep - 1) / kStep;
-#pragma unroll 4
-                        for (int i = 0; i < ks; ++i)
+                        const uint64_t db = bw::operand(sa + kABytes, MODE == kWeights ? kBoxBytes : 16);
+                        auto step_of = [&](int i, bool add) {
+                            const uint32_t to = d + i % kSets * BN;
                             if constexpr (kTf32)
-                                bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, kb > k0 || i > 0);
+                                bw::mma_tf32<CG>(to, da + i * 2, db + i * 2, shape, add);
                             else
-                                bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2),
-                                            shape, kb > k0 || i > 0);
+                                bw::mma<CG>(to, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape, add);
+                        };
+                        if (left >= kBK) {  // straight on: a loop's branches would hold the products up
+#pragma unroll
+                            for (int i = 0; i < kBK / kStep; ++i) step_of(i, i >= kSets || kb > k0);
+                        } else {
+                            for (int i = 0; i * kStep < left; ++i) step_of(i, i >= kSets || kb > k0);
+                        }
                         bw::commit<CG>(bar(&empty[s]));
+                        if (++s == STAGES) {
+                            s = 0;
+                            phase ^= 1;
+                        }
                     }
                     if (ok) bw::commit<CG>(bar(&done[half]));
                 }
@@ -421,7 +439,8 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 bw::fence_after();
-                const uint32_t at = tmem + half * BN + (uint32_t(warp * 32) << 16);
+                const uint32_t at = tmem + half * (kSets * BN) + (uint32_t(warp * 32) << 16);
+                const bool second = kSets == 2 && q.r - k0 * kBK > kStep;  // set in use
                 auto all_read = [&] {  // the half may be overwritten
                     bw::fence_before();
                     __syncwarp();
@@ -436,6 +455,11 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             bw::tmem_load(at + c * 32, v);
 #pragma unroll
                             for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                            if (second) {
+                                bw::tmem_load(at + BN + c * 32, v);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                            }
                         }
                     }
                     all_read();
@@ -445,6 +469,12 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         __syncwarp();
                         if (blocks > 0) {
                             bw::tmem_load(at + c0, v);
+                            if (second) {
+                                float w[32];
+                                bw::tmem_load(at + BN + c0, w);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) v[j] += w[j];
+                            }
                         } else {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0.0f;
