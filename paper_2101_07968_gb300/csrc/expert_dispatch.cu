@@ -157,11 +157,11 @@ split_segments_kernel(const float *src, float *dst, const int64_t *offsets, int6
     extern __shared__ int32_t dyn[];
     __shared__ float tile[kPartRows][33];
     const Segments seg = segments_at(dyn, experts);
-    if (threadIdx.x < 32) build_segments(seg, offsets, rows, experts, kPartRows, 1);
+    if (threadIdx.x < 32) build_segments<false>(seg, offsets, rows, experts, kPartRows, 1);
     __syncthreads();
     const int t = blockIdx.x;
     if (t >= seg.tile[seg.count]) return;
-    const int s = find_segment(seg, t), first = seg.tile[s];
+    const int s = find_segment(seg.tile, seg.count, t), first = seg.tile[s];
     const int64_t r0 = seg.start[s] + int64_t(t - first) * kPartRows, end = seg.start[s + 1];
     const int64_t third = int64_t(seg.tile[s + 1] - first) * kPartRows;
     const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, y0 = blockIdx.y * 32;

@@ -75,8 +75,11 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
         }
     } else {
         const int nm = (a.m + kBM * CG - 1) / (kBM * CG);
-        const int s = find_segment(seg, t);
-        const int i = t - seg.tile[s];
+        const int whole = seg.tile[seg.count];
+        const int s = find_segment(t < whole ? seg.tile : seg.part, seg.count, t);
+        const int size = seg.start[s + 1] - seg.start[s];
+        // the last rows' tiles follow the whole ones
+        const int i = t < whole ? t - seg.tile[s] : t - seg.part[s] + size / BN * nm;
         const bool none = s == 0 || s == seg.count - 1;
         q.e = none ? 0 : s - 1;
         q.m0 = (i % nm) * (kBM * CG);
@@ -97,7 +100,7 @@ __device__ __forceinline__ int tile_count(const MmaArgs &a, const Segments &seg)
 {
     if (MODE == kWeights || MODE == kWeightsK)
         return a.experts * ((a.m + kBM * CG - 1) / (kBM * CG)) * ((a.n + BN - 1) / BN);
-    return seg.tile[seg.count];
+    return seg.part[seg.count];
 }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
@@ -259,7 +262,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         bw::prefetch_map(&map_b);
     }
     if (warp == 0)
-        build_segments(seg, a.offsets, a.rows, a.experts, MODE == kWeightsK ? kPartRows : BN,
+        build_segments<MODE != kWeightsK>(seg, a.offsets, a.rows, a.experts, MODE == kWeightsK ? kPartRows : BN,
                        MODE == kWeightsK ? 1 : (a.m + kBM * CG - 1) / (kBM * CG));
     bw::fence_before();
     __syncthreads();

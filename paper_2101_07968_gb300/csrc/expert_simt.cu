@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int
     extern __shared__ int32_t dyn[];
     __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
     const Segments seg = segments_at(dyn, g.experts);
-    if (threadIdx.x < 32) build_segments(seg, g.offsets, g.rows, g.experts, kTile, 1);
+    if (threadIdx.x < 32) build_segments<false>(seg, g.offsets, g.rows, g.experts, kTile, 1);
     __syncthreads();
     int e, rows;
     int64_t depth;
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int
     } else {
         const int64_t t = blockIdx.y + int64_t(blockIdx.z) * gridDim.y;
         if (t >= seg.tile[seg.count]) return;
-        const int s = find_segment(seg, int(t));
+        const int s = find_segment(seg.tile, seg.count, int(t));
         const int64_t r0 = seg.start[s] + int64_t(t - seg.tile[s]) * kTile;
         rows = int(min(int64_t(kTile), seg.start[s + 1] - r0));
         const bool none = s == 0 || s == seg.count - 1;
