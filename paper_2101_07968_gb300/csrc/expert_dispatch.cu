@@ -7,8 +7,9 @@
 // What is left out (lo lo, and the bits of x past lo) is below 3 2^-22 |x w| a product, some
 // 2^-23 on average, less than a 32-bit sum of more than a few products loses; so the
 // CUDA cores take products of fewer than kPartDepth summed elements, and weight gradients of
-// experts of fewer than kPartLeast rows. 16,384 x 2,048 x 2,048 over 8 experts: see the
-// figure at use_parts.
+// experts of fewer than kPartLeast rows. 16,384 rows over 8 experts x 2,048 x 2,048: 0.94-0.97 ms,
+// 145 TFLOP/s, of which the copies take some 0.16 ms (a library product of floats 2.3 ms), and
+// 3.5e-7 off in the root mean square, as sums in floats are.
 #include "expert_rows.cuh"
 
 namespace dc {
@@ -179,8 +180,9 @@ int64_t part_pad(int64_t r) { return (r + 31) / 32 * 32; }
 int64_t part_rows(const ExpertArgs &g) { return (g.rows / kPartRows + g.experts + 3) * kPartRows; }
 size_t part_bytes(int64_t rows, int64_t length) { return (size_t(rows) * 3 * length * 4 + 255) / 256 * 256; }
 
-// Both sides measured, 8 experts: 16,384 rows x 2,048 x 2,048 and 200 x 512 x 512 (the sums of
-// the latter are no longer than the copies before them).
+// Shorter sums and smaller batches stay on the CUDA cores, where the bounds above hold and the
+// copies would take longer than the products (200 rows over 8 experts x 512 x 512 take 33-36 us
+// in parts, of which 25 are copies and launches).
 bool use_parts(const ExpertArgs &g, bool weights)
 {
     if (3 * part_rows(g) >= int64_t(1) << 31) return false;

@@ -10,13 +10,21 @@
 // Floats come as parts that tf32 holds (expert_dispatch.cu), with the summed axis innermost,
 // padded and three times as long: hi hi + hi lo + lo hi.
 //
-// A persistent CTA (or pair of CTAs, one tile of 256 features between them) takes every
-// grid-th tile. Warp 4 copies operand blocks of 64 along the summed axis into a ring of
-// stages by TMA; a thread of warp 5 issues the products; warps 0-3 store the finished tile
-// from one half of the tensor memory while the next accumulates in the other. Rows of other
-// experts that a copy brings along end in columns that are not stored; for dW, where they
-// would be summed, warp 6 overwrites those of an expert's last block with zeros between the
-// copy's arrival and the product.
+// A persistent pair of CTAs, one tile of 256 features between them, takes every grid-th tile.
+// Warp 4 copies operand blocks of 128 bytes along the summed axis into a ring of stages by TMA;
+// a thread of warp 5 issues the products; warps 0-3 store the finished tile from one half of
+// the tensor memory while the next accumulates in the other. Rows of other experts that a copy
+// brings along end in columns that are not stored; for dW, where they would be summed, warp 6
+// overwrites those of an expert's last block with zeros between the copy's arrival and the
+// product. Every wait ends after a number of tries, and the kernel then reports it in status.
+//
+// Measured (bfloat16, one GB300): 16,384 rows over 16 experts x 4,096 x 2,048, y and dx 157 us,
+// dW 160 us (1,750 and 1,710 TFLOP/s); 65,536 rows over 32 experts x 2,048 x 4,096, 567-580 us
+// (1,900-1,940 TFLOP/s against a library product's 1,902). The tensor cores are busy 86 % of
+// the time; a block's products take 512 cycles and its copies, read by every pair through the
+// L2, some 630 (15 TB/s). A product takes some 100 cycles to issue whatever its columns, so
+// tiles narrower than 256 do not run at the tensor cores' rate. With one or a few experts' rows
+// the weights' bytes bound it: 128 rows over 24 of 32 experts x 2,048 x 2,048 38 us (5.3 TB/s).
 #include <cuda.h>
 
 #include <type_traits>

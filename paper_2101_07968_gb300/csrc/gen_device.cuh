@@ -32,16 +32,12 @@ struct GenParams {
 };
 static_assert(sizeof(GenParams) < 32000, "kernel parameter block limit");
 
-constexpr uint64_t kGamma = 0x9e3779b97f4a7c15ull;  // state step of SplitMix64
-__device__ __forceinline__ uint64_t splitmix_output(uint64_t z)
+__device__ __forceinline__ uint64_t splitmix(uint64_t seed, uint64_t ctr)
 {
+    uint64_t z = seed + (ctr + 1) * 0x9e3779b97f4a7c15ull;
     z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
     z = (z ^ (z >> 27)) * 0x94d049bb133111ebull;
     return z ^ (z >> 31);
-}
-__device__ __forceinline__ uint64_t splitmix(uint64_t seed, uint64_t ctr)
-{
-    return splitmix_output(seed + (ctr + 1) * kGamma);
 }
 
 __device__ __forceinline__ uint64_t counter(int64_t gi, int field, int layer)

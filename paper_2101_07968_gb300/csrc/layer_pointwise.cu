@@ -2,7 +2,10 @@
 //
 // All three move each byte once and are bound by memory: 16-byte accesses, several in
 // flight per thread. A thread takes one group of columns and U rows, so that no index is
-// divided; narrow rows share a block.
+// divided; narrow rows share a block. Measured (bfloat16, one GB300): dropout of 32,768 x 4,096
+// 79 us, 6.8 TB/s; the gated unit 16,384 x 2,048 32 us, 6.2 TB/s, and its gradient 65,536 x 2,048
+// 190 us, 7.1 TB/s. Rows whose columns do not fill 16-byte accesses go element by element:
+// 30,000 x 1,001 3.8 TB/s (gradient 4.3), dropout of 30,000 x 2,002 2.4.
 #include "layers.cuh"
 
 namespace dc {
@@ -131,8 +134,7 @@ cudaError_t dropout_typed(int64_t rows, int cols, const T *x, int64_t ldx, const
 // Math. Comp. 36, 1981, for the same function). P, of degree 8 in 4 s - 1, was fitted to the
 // least largest relative error, 4.4e-8; in 32 bits it stays within 3 2^-23, so that the tail
 // keeps its digits where 1/2 (1 + erf) loses them, at two special-function operations an
-// element. normcdff took 358 us where this takes the gradient of 65,536 x 2,048 to the
-// figure at gated_grad_kernel.
+// element. The gradient of 65,536 x 2,048 took 358 us with normcdff and takes 190 with this.
 __device__ __forceinline__ float2 normal_tail(float2 g, float2 &e)
 {
     const float2 h = __fmul2_rn(__fmul2_rn(g, g), twice(-0.72134752044448170f));  // -log2(e) / 2

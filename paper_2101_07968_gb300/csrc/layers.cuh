@@ -61,6 +61,16 @@ struct DropRule {
     float scale;
 };
 
+// SplitMix64 in two parts, for kernels that step the state themselves: splitmix(seed, n) is
+// splitmix_output(seed + (n + 1) kGamma).
+constexpr uint64_t kGamma = 0x9e3779b97f4a7c15ull;
+__device__ __forceinline__ uint64_t splitmix_output(uint64_t z)
+{
+    z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
+    z = (z ^ (z >> 27)) * 0x94d049bb133111ebull;
+    return z ^ (z >> 31);
+}
+
 inline DropRule drop_rule(double p, uint64_t seed, int64_t offset)
 {
     DropRule d;

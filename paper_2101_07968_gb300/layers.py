@@ -38,7 +38,7 @@ def _dtype(t) -> int:
 
 def _like(name, t, ref, shape):
     """t has ref's type and device and the given shape (ref is on a device)."""
-    if t.dtype != ref.dtype or t.shape != shape or t.device != ref.device:
+    if t.dtype is not ref.dtype or t.shape != shape or t.get_device() != ref.get_device():
         raise ValueError(f"{name}: {tuple(shape)} {ref.dtype} on {ref.device} expected, not "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
 
@@ -60,10 +60,28 @@ def _rows(name, t) -> int:
     return ld
 
 
+_current_device = torch._C._cuda_getDevice
+_library = None  # the one that _functions come from
+_functions = {}
+
+
+def _function(name):
+    """The library's function, looked up once: a call costs the host some ten microseconds."""
+    global _library
+    lib = dc._lib or dc.lib()
+    if lib is not _library:
+        _library = lib
+        _functions.clear()
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(lib, name)
+    return fn
+
+
 def _run(name, t, stream, *args):
     """One call of the library on t's device."""
-    fn = getattr(dc._lib or dc.lib(), name)
-    if t.get_device() == torch._C._cuda_getDevice():
+    fn = _function(name)
+    if t.get_device() == _current_device():
         st = fn(*args, dc._stream(stream))
     else:
         with torch.cuda.device(t.device):
@@ -88,7 +106,7 @@ _status = {}
 def _status_of(device):
     at = _status.get(device)
     if at is None:
-        t = torch.zeros(1, dtype=torch.int32, device=device)
+        t = torch.zeros(1, dtype=torch.int32, device=f"cuda:{device}")
         at = _status[device] = (t, t.data_ptr())
     return at[1]
 
@@ -100,7 +118,7 @@ def check_status() -> None:
         s = int(t.item())
         if s:
             t.zero_()
-            raise dc.DynaCommError(s, f"layer operators on {device}")
+            raise dc.DynaCommError(s, f"layer operators on cuda:{device}")
 
 
 def _weights(name, w):
@@ -121,8 +139,8 @@ def _weights(name, w):
 
 
 def _offsets(offsets, experts, ref):
-    if offsets.dtype != torch.int64 or offsets.shape != (experts + 1,) \
-            or offsets.device != ref.device or not offsets.is_contiguous():
+    if offsets.dtype is not torch.int64 or offsets.shape != (experts + 1,) \
+            or offsets.get_device() != ref.get_device() or not offsets.is_contiguous():
         raise ValueError(f"offsets: {experts + 1} contiguous int64 on {ref.device} expected")
 
 
@@ -135,10 +153,10 @@ _PRODUCTS = ("dc_expert_matmul", "dc_expert_matmul_grad_input", "dc_expert_matmu
 
 def _product(which, shape, a, b, offsets, c, stream):
     ap, bp = a.data_ptr(), b.data_ptr()
-    need = (dc._lib or dc.lib()).dc_expert_workspace_bytes(shape, which, ap, bp)
+    need = _function("dc_expert_workspace_bytes")(shape, which, ap, bp)
     ws = _empty(need, dtype=torch.uint8, device=a.device) if need else None
     _run(_PRODUCTS[which], a, stream, shape, ap, bp, offsets.data_ptr(), c.data_ptr(),
-         _status_of(a.device), ws.data_ptr() if need else None, need)
+         _status_of(a.get_device()), ws.data_ptr() if need else None, need)
     _used_on(ws, stream)
     return c
 
@@ -229,7 +247,7 @@ def dropout(x, p, seed, offset=0, residual=None, stream=None):
         _like("residual", residual, x, (R, C))
     y = _empty((R, C), dtype=x.dtype, device=x.device)
     _run("dc_dropout", x, stream, _dtype(x), R, C, x.data_ptr(), ldx, res, ldr, y.data_ptr(), C,
-         float(p), int(seed), int(offset))
+         p, int(seed), int(offset))
     return y
 
 
@@ -238,9 +256,8 @@ def _norm_cfg(x, kind, rows_per_gate, residual_scale, eps, p, seed, offset):
     if kind not in _KINDS:
         raise ValueError(f"kind: one of {sorted(_KINDS)} expected")
     R, D = x.shape
-    return dc.dc_block_norm_cfg(_dtype(x), _KINDS[kind], R, D, int(rows_per_gate) if rows_per_gate
-                                else max(R, 1), float(residual_scale), float(eps), float(p),
-                                int(seed), int(offset))
+    return dc.dc_block_norm_cfg(_dtype(x), _KINDS[kind], R, D, rows_per_gate or max(R, 1),
+                                residual_scale, eps, p, int(seed), int(offset))
 
 
 def _contiguous(name, t, ref, shape):
@@ -307,7 +324,7 @@ def block_norm_grad(dy, dh, y, f=None, gate=None, w_post=None, w_pre=None, resid
             out["dw_post"] = _empty(D, dtype=torch.float32, device=y.device)
     if dh is not None and w_pre is not None:
         out["dw_pre"] = _empty(D, dtype=torch.float32, device=y.device)
-    need = (dc._lib or dc.lib()).dc_block_norm_grad_workspace_bytes(ctypes.byref(cfg))
+    need = _function("dc_block_norm_grad_workspace_bytes")(ctypes.byref(cfg))
     ws = _empty(max(need, 1), dtype=torch.uint8, device=y.device)
     _run("dc_block_norm_grad", y, stream, ctypes.byref(cfg), dyp, dhp, yp, fp, gp, pp, ep,
          *[None if t is None else t.data_ptr() for t in out.values()], ws.data_ptr(), need)
