@@ -195,20 +195,34 @@ __device__ __forceinline__ void store_lines(const Lines &s, const MmaArgs &a, co
         const int rows = min(32, a.m - row0);
         if constexpr (sizeof(T) == 2) {
             // rows that start on 2-byte boundaries: pairs from the next 4-byte boundary on, and
-            // what is left at both ends
-#pragma unroll 4
-            for (int row = 0; row < rows; ++row) {
-                T *r = p + row * a.c_m;
-                const int c = 2 * lane + int(reinterpret_cast<uintptr_t>(r) >> 1 & 1);
-                if (c + 1 < n) {
-                    Vec<T, 2> v;
-                    v.e[0] = value(row, c);
-                    v.e[1] = value(row, c + 1);
-                    *reinterpret_cast<Vec<T, 2> *>(r + c) = v;
-                } else if (c < n) {
-                    r[c] = value(row, c);
+            // what is left at both ends; eight rows' values before their stores
+            constexpr int kAhead = 8;
+            for (int r0 = 0; r0 < rows; r0 += kAhead) {
+                Vec<T, 2> v[kAhead];
+                int first[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int row = r0 + i;
+                    first[i] = int(reinterpret_cast<uintptr_t>(p + row * a.c_m) >> 1 & 1);
+                    const int c = 2 * lane + first[i];
+                    v[i].e[0] = value(row, c);
+                    v[i].e[1] = value(row, (c + 1) & (kCols - 1));
                 }
-                if (lane == 0 && c == 1) r[0] = value(row, 0);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    T *r = p + (r0 + i) * a.c_m;
+                    const int c = 2 * lane + first[i];
+                    if (r0 + i >= rows) continue;
+                    if (c + 1 < n)
+                        *reinterpret_cast<Vec<T, 2> *>(r + c) = v[i];
+                    else if (c < n)
+                        r[c] = v[i].e[0];
+                }
+                // the first element of rows whose pairs start at the second: a lane per row
+                if (lane < kAhead && r0 + lane < rows) {
+                    T *r = p + (r0 + lane) * a.c_m;
+                    if (reinterpret_cast<uintptr_t>(r) >> 1 & 1) r[0] = value(r0 + lane, 0);
+                }
             }
         } else {
 #pragma unroll 4
