@@ -17,23 +17,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Rows [y][x] of z matrices, x contiguous, to rows padded with zeros to `pad` elements. A
-// thread writes eight elements; its eight loads hit the lines that its neighbours' do.
-__global__ void __launch_bounds__(kThreads)
-align_rows_kernel(const uint16_t *src, uint16_t *dst, int64_t rows, int32_t y, int32_t x, int32_t pad,
-                  int64_t stride_z, int64_t stride_y)
-{
-    const int groups = pad / 8;
-    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
-    const int64_t r = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
-    if (c >= groups * 8 || r >= rows) return;
-    const uint16_t *p = src + (r / y) * stride_z + (r % y) * stride_y;
-    Vec<uint16_t, 8> v;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v.e[j] = c + j < x ? p[c + j] : uint16_t(0);
-    *reinterpret_cast<Vec<uint16_t, 8> *>(dst + r * pad + c) = v;
-}
-
 struct Matrix {
     const void *p;
     int64_t z, y, x;  // extents, x contiguous
@@ -50,22 +33,63 @@ size_t copy_bytes(const Matrix &m)
     return aligned(m) ? 0 : (size_t(m.z) * m.y * padded(m.x) * 2 + 255) / 256 * 256;
 }
 
-cudaError_t align_rows(Matrix &m, unsigned char *&workspace, cudaStream_t stream)
+// One matrix of a copy: rows [z][y][x], x contiguous, to rows padded with zeros to `pad`
+// elements. A block takes (kThreads >> wide) rows by (1 << wide) groups of eight elements.
+struct Copy {
+    const uint16_t *src;
+    uint16_t *dst;
+    int64_t rows, stride_z, stride_y;
+    int32_t y, x, pad, wide;
+    int64_t blocks_x, blocks;
+};
+
+Copy copy_of(const Matrix &m, void *dst)
 {
-    const size_t bytes = copy_bytes(m);
-    if (!bytes) return cudaSuccess;
-    const int64_t pad = padded(m.x), rows = m.z * m.y;
-    int bx = 1;
-    while (bx < 64 && bx < pad / 8) bx *= 2;
-    const int by = kThreads / bx;
-    const dim3 grid(unsigned((rows + by - 1) / by), unsigned((pad / 8 + bx - 1) / bx));
-    align_rows_kernel<<<grid, dim3(unsigned(bx), unsigned(by)), 0, stream>>>(
-        static_cast<const uint16_t *>(m.p), reinterpret_cast<uint16_t *>(workspace), rows, int32_t(m.y),
-        int32_t(m.x), int32_t(pad), m.stride_z, m.stride_y);
-    m.p = workspace;
-    m.stride_y = pad;
-    m.stride_z = pad * m.y;
-    workspace += bytes;
+    Copy c = {static_cast<const uint16_t *>(m.p), static_cast<uint16_t *>(dst), m.z * m.y, m.stride_z, m.stride_y,
+              int32_t(m.y), int32_t(m.x), int32_t(padded(m.x)), 0, 0, 0};
+    while ((1 << c.wide) < 64 && (1 << c.wide) < c.pad / 8) ++c.wide;
+    const int by = kThreads >> c.wide, bx = 1 << c.wide;
+    c.blocks_x = (c.pad / 8 + bx - 1) / bx;
+    c.blocks = c.blocks_x * ((c.rows + by - 1) / by);
+    return c;
+}
+
+// Both operands' copies in one launch (a launch costs what a small copy does): the first
+// a.blocks blocks are a's, the others b's. A thread writes eight elements; its eight loads
+// hit the lines that its neighbours' do.
+__global__ void __launch_bounds__(kThreads) align_rows_kernel(Copy a, Copy b)
+{
+    const bool second = blockIdx.x >= a.blocks;
+    const Copy &m = second ? b : a;
+    const int64_t block = blockIdx.x - (second ? a.blocks : 0);
+    const int64_t r = block / m.blocks_x * (kThreads >> m.wide) + (threadIdx.x >> m.wide);
+    const int c = int(block % m.blocks_x << m.wide | (threadIdx.x & ((1 << m.wide) - 1))) * 8;
+    if (c >= m.pad || r >= m.rows) return;
+    const uint16_t *p = m.src + (r / m.y) * m.stride_z + (r % m.y) * m.stride_y;
+    Vec<uint16_t, 8> v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.e[j] = c + j < m.x ? p[c + j] : uint16_t(0);
+    *reinterpret_cast<Vec<uint16_t, 8> *>(m.dst + r * m.pad + c) = v;
+}
+
+// Copies of a and b that need them; a and b then are the copies.
+cudaError_t align_rows(Matrix &a, Matrix &b, void *workspace, cudaStream_t stream)
+{
+    Copy c[2] = {};
+    unsigned char *at = static_cast<unsigned char *>(workspace);
+    Matrix *m[2] = {&a, &b};
+    for (int i = 0; i < 2; ++i) {
+        const size_t bytes = copy_bytes(*m[i]);
+        if (!bytes) continue;
+        c[i] = copy_of(*m[i], at);
+        m[i]->p = at;
+        m[i]->stride_y = c[i].pad;
+        m[i]->stride_z = int64_t(c[i].pad) * m[i]->y;
+        at += bytes;
+    }
+    const int64_t blocks = c[0].blocks + c[1].blocks;
+    if (!blocks) return cudaSuccess;
+    align_rows_kernel<<<unsigned(blocks), kThreads, 0, stream>>>(c[0], c[1]);
     return cudaGetLastError();
 }
 
@@ -272,9 +296,7 @@ cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, 
     if (dtype == DC_FP32) return use_parts(g, false) ? float_rows(g, workspace, stream) : expert_simt_rows(g, stream);
     Matrix a, b;
     operands(g, false, a, b);
-    unsigned char *ws = static_cast<unsigned char *>(workspace);
-    cudaError_t e = align_rows(a, ws, stream);
-    if (e == cudaSuccess) e = align_rows(b, ws, stream);
+    const cudaError_t e = align_rows(a, b, workspace, stream);
     if (e != cudaSuccess) return e;
     ExpertArgs h = g;
     h.a = a.p;
@@ -301,9 +323,7 @@ cudaError_t launch_expert_weights(int dtype, const ExpertArgs &g, void *workspac
     }
     Matrix a, b;
     operands(g, true, a, b);
-    unsigned char *ws = static_cast<unsigned char *>(workspace);
-    cudaError_t e = align_rows(a, ws, stream);
-    if (e == cudaSuccess) e = align_rows(b, ws, stream);
+    const cudaError_t e = align_rows(a, b, workspace, stream);
     if (e != cudaSuccess) return e;
     ExpertArgs h = g;
     h.a = a.p;
