@@ -12,7 +12,7 @@
 //
 // Measured (one GB300): 32,768 x 2,048 bfloat16, rms, dropout, a gate per 2,048 rows: 94 us, 5.7 TB/s,
 // integer and floating issue 65 % busy (34 instructions an element; the generator's draws are
-// eight of them). Gradient, 32,765 x 4,096 half, layer norm, dropout, one gate: 403 us, 4.0 TB/s, at 54 % of
+// eight of them). Gradient, 32,765 x 4,096 half, layer norm, dropout, one gate: 369 us, 4.4 TB/s, at 54 % of
 // the issue slots with the 16 warps an SM that the sums in registers leave room for. One row
 // of 2,048: 3.2 us in a graph.
 #pragma once
@@ -322,15 +322,15 @@ constexpr int kOwn = 2;
 // the gate row changes. For shorter ones that costs more than it saves.
 constexpr int kLongGate = 8;
 
-template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
+template <typename T, int V, int FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 32 ? 32 : 1) norm_kernel(NormArgs a, int stages)
 {
-    using R = Row<T, V, FULL, EL>;
+    using R = Row<T, V, (FULL > 0), EL>;
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float buf[2 * 4 * 32];
     __shared__ alignas(8) uint64_t bars[kMaxStages];
     __shared__ uint32_t gave_up;
-    const int size = blockDim.x, D = a.D, lane = threadIdx.x;
+    const int size = FULL > 1 ? FULL : int(blockDim.x), D = FULL > 1 ? FULL * EL : a.D, lane = threadIdx.x;
     Team team{size, lane, size / 32, buf, 0};
     const float inv = 1.0f / float(D);
     const int64_t r0 = run_start(a.rows, gridDim.x, blockIdx.x);
@@ -446,16 +446,16 @@ __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 32 ? 32 : 
 // shared with the run after.
 constexpr int kSlots = 4;
 
-template <typename T, int V, bool FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
+template <typename T, int V, int FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 2 : MAXT == 32 ? 32 : 1)
 norm_grad_kernel(NormArgs a, float *partial, int stages)
 {
-    using R = Row<T, V, FULL, EL>;
+    using R = Row<T, V, (FULL > 0), EL>;
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float buf[2 * 4 * 32];
     __shared__ alignas(8) uint64_t bars[kMaxStages];
     __shared__ uint32_t gave_up;
-    const int size = blockDim.x, D = a.D, lane = threadIdx.x;
+    const int size = FULL > 1 ? FULL : int(blockDim.x), D = FULL > 1 ? FULL * EL : a.D, lane = threadIdx.x;
     Team team{size, lane, size / 32, buf, 0};
     const float inv = 1.0f / float(D);
     const int64_t b = blockIdx.x, P = gridDim.x;
@@ -833,7 +833,7 @@ inline int64_t grad_runs(int dtype, int64_t rows, int D)
     return rows < most ? rows : most;
 }
 
-template <typename T, int V, bool FULL, bool RING, int MAXT, int EL>
+template <typename T, int V, int FULL, bool RING, int MAXT, int EL>
 cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
 {
     const bool lg = a.rows_per_gate >= kLongGate;
@@ -854,7 +854,7 @@ cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-template <typename T, int V, bool FULL, bool RING, int MAXT, int EL>
+template <typename T, int V, int FULL, bool RING, int MAXT, int EL>
 cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const Plan &p,
                              cudaStream_t stream)
 {
@@ -906,15 +906,26 @@ cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
     const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
-        return vec ? norm_launch<T, V, false, false, 1024, kElems>(a, p, stream)
-                   : norm_launch<T, 1, false, false, 1024, kElems>(a, p, stream);
+        return vec ? norm_launch<T, V, 0, false, 1024, kElems>(a, p, stream)
+                   : norm_launch<T, 1, 0, false, 1024, kElems>(a, p, stream);
     if (a.D <= 128)
-        return vec ? norm_launch<T, 4, false, true, 32, 4>(a, p, stream) : norm_launch<T, 1, false, true, 32, 4>(a, p, stream);
+        return vec ? norm_launch<T, 4, 0, true, 32, 4>(a, p, stream) : norm_launch<T, 1, 0, true, 32, 4>(a, p, stream);
     if (a.D <= 256)
-        return vec ? norm_launch<T, V, false, true, 32, 8>(a, p, stream) : norm_launch<T, 1, false, true, 32, 8>(a, p, stream);
-    if (!vec) return norm_launch<T, 1, false, true, kNarrow, kElems>(a, p, stream);
-    return full ? norm_launch<T, V, true, true, kNarrow, kElems>(a, p, stream)
-                : norm_launch<T, V, false, true, kNarrow, kElems>(a, p, stream);
+        return vec ? norm_launch<T, V, 0, true, 32, 8>(a, p, stream) : norm_launch<T, 1, 0, true, 32, 8>(a, p, stream);
+    if (!vec) return norm_launch<T, 1, 0, true, kNarrow, kElems>(a, p, stream);
+    // Powers of two, whose strides are then constants: layer norm of 32,768 x 4,096 205 us against
+    // 229, 32,768 x 1,024 with short gates 51 against 57; but rms with long gates 102 against 95 (x 2,048)
+    // and 190 against 177 (x 4,096), where the sums are fewest.
+    const bool fixed = a.layer || a.rows_per_gate < kLongGate || a.D < 2048;
+    switch (fixed ? a.D : 0) {
+        case 512: return norm_launch<T, V, 32, true, kNarrow, kElems>(a, p, stream);
+        case 1024: return norm_launch<T, V, 64, true, kNarrow, kElems>(a, p, stream);
+        case 2048: return norm_launch<T, V, 128, true, kNarrow, kElems>(a, p, stream);
+        case 4096: return norm_launch<T, V, 256, true, kNarrow, kElems>(a, p, stream);
+        default: break;
+    }
+    return full ? norm_launch<T, V, 1, true, kNarrow, kElems>(a, p, stream)
+                : norm_launch<T, V, 0, true, kNarrow, kElems>(a, p, stream);
 }
 
 template <typename T>
@@ -925,15 +936,22 @@ cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t 
     const int64_t P = grad_runs(dtype, a.rows, a.D);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
-        return vec ? norm_grad_launch<T, V, false, false, 1024, kElems>(a, partial, P, p, stream)
-                   : norm_grad_launch<T, 1, false, false, 1024, kElems>(a, partial, P, p, stream);
+        return vec ? norm_grad_launch<T, V, 0, false, 1024, kElems>(a, partial, P, p, stream)
+                   : norm_grad_launch<T, 1, 0, false, 1024, kElems>(a, partial, P, p, stream);
     if (a.D <= 128)
-        return vec ? norm_grad_launch<T, 4, false, true, 32, 4>(a, partial, P, p, stream) : norm_grad_launch<T, 1, false, true, 32, 4>(a, partial, P, p, stream);
+        return vec ? norm_grad_launch<T, 4, 0, true, 32, 4>(a, partial, P, p, stream) : norm_grad_launch<T, 1, 0, true, 32, 4>(a, partial, P, p, stream);
     if (a.D <= 256)
-        return vec ? norm_grad_launch<T, V, false, true, 32, 8>(a, partial, P, p, stream) : norm_grad_launch<T, 1, false, true, 32, 8>(a, partial, P, p, stream);
-    if (!vec) return norm_grad_launch<T, 1, false, true, kNarrow, kElems>(a, partial, P, p, stream);
-    return full ? norm_grad_launch<T, V, true, true, kNarrow, kElems>(a, partial, P, p, stream)
-                : norm_grad_launch<T, V, false, true, kNarrow, kElems>(a, partial, P, p, stream);
+        return vec ? norm_grad_launch<T, V, 0, true, 32, 8>(a, partial, P, p, stream) : norm_grad_launch<T, 1, 0, true, 32, 8>(a, partial, P, p, stream);
+    if (!vec) return norm_grad_launch<T, 1, 0, true, kNarrow, kElems>(a, partial, P, p, stream);
+    switch (a.D) {  // as in forward: 32,765 x 4,096 layer norm 369 us against 405
+        case 512: return norm_grad_launch<T, V, 32, true, kNarrow, kElems>(a, partial, P, p, stream);
+        case 1024: return norm_grad_launch<T, V, 64, true, kNarrow, kElems>(a, partial, P, p, stream);
+        case 2048: return norm_grad_launch<T, V, 128, true, kNarrow, kElems>(a, partial, P, p, stream);
+        case 4096: return norm_grad_launch<T, V, 256, true, kNarrow, kElems>(a, partial, P, p, stream);
+        default: break;
+    }
+    return full ? norm_grad_launch<T, V, 1, true, kNarrow, kElems>(a, partial, P, p, stream)
+                : norm_grad_launch<T, V, 0, true, kNarrow, kElems>(a, partial, P, p, stream);
 }
 
 }  // namespace norms
