@@ -27,10 +27,14 @@ namespace norms {
 // for rows of up to 128 and 256 columns, that one warp takes, 4 and 8, so that its lanes
 // have work.
 constexpr int kElems = 16;
-constexpr int elems_for(int D) { return D <= 128 ? 4 : D <= 256 ? 8 : kElems; }
 // Rows above this take blocks of up to 1,024 threads, whose 64 registers each do not hold
 // the gradient's sums: they spill, which narrower rows are spared.
 constexpr int kNarrow = 256, kWideD = kNarrow * kElems;
+constexpr int elems_for(int D, bool vec)  // vec: rows on 16-byte boundaries
+{
+    // Without, an element takes a register of its own: 16 of three rows spill.
+    return D > kWideD ? kElems : D <= 128 ? 4 : D <= 256 || !vec ? 8 : kElems;
+}
 
 struct Team {
     int size;  // threads
@@ -284,10 +288,18 @@ __device__ __forceinline__ void drop_row(const DropRule &d, float2 (&v)[(EL / 2)
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < EL; ++k) {
-            const int c = Row<float, V, false, EL>::column(k, lane, size);
-            const uint64_t w = splitmix_output(z0 + uint64_t(c / 4) * kGamma);
-            if (!kept(d, w, c & 3)) (k & 1 ? v[k / 2].y : v[k / 2].x) = 0.0f;
+        for (int k = 0; k < EL; k += 4) {
+            // Four neighbouring lanes want the four fields of one draw, for each k: every lane
+            // draws for one of four k, and they pass them round.
+            const int c = ((k + (lane & 3)) * size + (lane & ~3)) / 4;
+            const uint64_t w = splitmix_output(z0 + uint64_t(c) * kGamma);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t lo = __shfl_sync(0xffffffffu, uint32_t(w), j, 4);
+                const uint32_t hi = __shfl_sync(0xffffffffu, uint32_t(w >> 32), j, 4);
+                const uint32_t x = lane & 2 ? hi : lo;
+                if (!((lane & 1 ? x : x << 16) > limit)) (j & 1 ? v[(k + j) / 2].y : v[(k + j) / 2].x) = 0.0f;
+            }
         }
     }
 }
@@ -796,26 +808,28 @@ __global__ void __launch_bounds__(128) norm_shared_gates_kernel(NormArgs a, cons
 }
 
 // ------------------------------------------------------------------------------ host
-inline int row_threads(int D)
+inline int row_threads(int D, bool vec)
 {
-    const int el = elems_for(D);
+    const int el = elems_for(D, vec);
     return (D + el * 32 - 1) / (el * 32) * 32;
 }
 
 // Blocks an SM and slots of the ring: `threads` an SM as the registers allow, and the 224 KB
 // of shared memory shared between them; no ring (0 slots) where it would hold fewer than two rows.
 struct Plan {
-    int blocks, stages;
+    int size, blocks, stages;
     size_t smem;
 };
-inline Plan plan_for(int D, int arrays, int bytes, int threads, int own)
+inline Plan plan_for(int D, bool vec, int arrays, int bytes, int threads, int own)
 {
     Plan p;
-    const int size = row_threads(D);
-    p.blocks = elems_for(D) < kElems ? 32 : threads / size < 1 ? 1 : threads / size;
+    const int size = row_threads(D, vec), el = elems_for(D, vec);
+    const bool one_warp = size == 32 && el < kElems;
+    p.size = size;
+    p.blocks = one_warp ? 32 : threads / size < 1 ? 1 : threads / size;
     if (p.blocks > 32) p.blocks = 32;
-    if (elems_for(D) == kElems && p.blocks > 16) p.blocks = 16;
-    const size_t fixed = 2048 + size_t(own) * size * elems_for(D) * sizeof(float);
+    if (!one_warp && p.blocks > 16) p.blocks = 16;
+    const size_t fixed = 2048 + size_t(own) * size * el * sizeof(float);
     const size_t row = size_t(arrays) * ((size_t(D) * bytes + 15) / 16 * 16 + 16), room = size_t(224) << 10;
     while (p.blocks > 1 && room / p.blocks < 2 * row + fixed) --p.blocks;
     const size_t slots = room / p.blocks > fixed ? (room / p.blocks - fixed) / row : 0;
@@ -827,9 +841,9 @@ inline Plan plan_for(int D, int arrays, int bytes, int threads, int own)
 constexpr int kSms = 152;
 constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM; up to 32 single warps
 
-inline int64_t grad_runs(int dtype, int64_t rows, int D)
+inline int64_t grad_runs(int dtype, int64_t rows, int D, bool vec)
 {
-    const int64_t most = int64_t(kSms) * plan_for(D, 4, dtype_bytes(dtype), kGradThreads, kOwn).blocks;
+    const int64_t most = int64_t(kSms) * plan_for(D, vec, 4, dtype_bytes(dtype), kGradThreads, kOwn).blocks;
     return rows < most ? rows : most;
 }
 
@@ -849,7 +863,7 @@ cudaError_t norm_launch(const NormArgs &a, const Plan &p, cudaStream_t stream)
     });
     if (e != cudaSuccess) return e;
     const int64_t most = int64_t(kSms) * p.blocks;
-    kernel<<<unsigned(a.rows < most ? a.rows : most), unsigned(row_threads(a.D)), p.smem, stream>>>(
+    kernel<<<unsigned(a.rows < most ? a.rows : most), unsigned(p.size), p.smem, stream>>>(
         a, p.stages);
     return cudaGetLastError();
 }
@@ -872,7 +886,7 @@ cudaError_t norm_grad_launch(const NormArgs &a, float *partial, int64_t P, const
         });
         if (e != cudaSuccess) return e;
     }
-    kernel<<<unsigned(P), unsigned(row_threads(a.D)), p.smem, stream>>>(a, partial, p.stages);
+    kernel<<<unsigned(P), unsigned(p.size), p.smem, stream>>>(a, partial, p.stages);
     const int64_t gates = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate;
     // how the gate rows that lie in several runs are added up
     const bool shared = a.dgate && P > 1 && a.rows_per_gate > 1, few = gates < P;
@@ -903,7 +917,7 @@ template <typename T>
 cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
-    const Plan p = plan_for(a.D, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
+    const Plan p = plan_for(a.D, vec, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
         return vec ? norm_launch<T, V, 0, false, 1024, kElems>(a, p, stream)
@@ -912,7 +926,8 @@ cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
         return vec ? norm_launch<T, 4, 0, true, 32, 4>(a, p, stream) : norm_launch<T, 1, 0, true, 32, 4>(a, p, stream);
     if (a.D <= 256)
         return vec ? norm_launch<T, V, 0, true, 32, 8>(a, p, stream) : norm_launch<T, 1, 0, true, 32, 8>(a, p, stream);
-    if (!vec) return norm_launch<T, 1, 0, true, kNarrow, kElems>(a, p, stream);
+    if (!vec)
+        return a.D <= 2048 ? norm_launch<T, 1, 0, true, kNarrow, 8>(a, p, stream) : norm_launch<T, 1, 0, true, 512, 8>(a, p, stream);
     // Powers of two, whose strides are then constants: layer norm of 32,768 x 4,096 205 us against
     // 229, 32,768 x 1,024 with short gates 51 against 57; but rms with long gates 102 against 95 (x 2,048)
     // and 190 against 177 (x 4,096), where the sums are fewest.
@@ -932,8 +947,8 @@ template <typename T>
 cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t stream)
 {
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
-    const Plan p = plan_for(a.D, 4, dtype_bytes(dtype), kGradThreads, kOwn);
-    const int64_t P = grad_runs(dtype, a.rows, a.D);
+    const Plan p = plan_for(a.D, vec, 4, dtype_bytes(dtype), kGradThreads, kOwn);
+    const int64_t P = grad_runs(dtype, a.rows, a.D, vec);
     constexpr int V = kVec<T>;
     if (a.D > kWideD)
         return vec ? norm_grad_launch<T, V, 0, false, 1024, kElems>(a, partial, P, p, stream)
@@ -942,7 +957,8 @@ cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t 
         return vec ? norm_grad_launch<T, 4, 0, true, 32, 4>(a, partial, P, p, stream) : norm_grad_launch<T, 1, 0, true, 32, 4>(a, partial, P, p, stream);
     if (a.D <= 256)
         return vec ? norm_grad_launch<T, V, 0, true, 32, 8>(a, partial, P, p, stream) : norm_grad_launch<T, 1, 0, true, 32, 8>(a, partial, P, p, stream);
-    if (!vec) return norm_grad_launch<T, 1, 0, true, kNarrow, kElems>(a, partial, P, p, stream);
+    if (!vec)
+        return a.D <= 2048 ? norm_grad_launch<T, 1, 0, true, kNarrow, 8>(a, partial, P, p, stream) : norm_grad_launch<T, 1, 0, true, 512, 8>(a, partial, P, p, stream);
     switch (a.D) {  // as in forward: 32,765 x 4,096 layer norm 369 us against 405
         case 512: return norm_grad_launch<T, V, 32, true, kNarrow, kElems>(a, partial, P, p, stream);
         case 1024: return norm_grad_launch<T, V, 64, true, kNarrow, kElems>(a, partial, P, p, stream);

@@ -6,7 +6,8 @@ namespace dc {
 
 size_t norm_grad_workspace(int dtype, int64_t rows, int D)
 {
-    return size_t(norms::grad_runs(dtype, rows, D)) * norms::kSlots * size_t(D) * sizeof(float);
+    const int64_t a = norms::grad_runs(dtype, rows, D, true), b = norms::grad_runs(dtype, rows, D, false);
+    return size_t(a > b ? a : b) * norms::kSlots * size_t(D) * sizeof(float);
 }
 
 cudaError_t norm_forward_fp16(const NormArgs &a, cudaStream_t stream);
