@@ -338,7 +338,7 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
  * as it is.
  * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; rows outside [0, 2^31 - 1]; experts
  * outside [1, DC_EXPERTS_MAX]; N or K outside [1, DC_LAYER_DIM_MAX]; a stride shorter than its
- * row, or above 2^40); DC_ERR_WORKSPACE; DC_ERR_CUDA.
+ * row, or above 2^37); DC_ERR_WORKSPACE; DC_ERR_CUDA.
  * ---------------------------------------------------------------------- */
 #define DC_FEW_ROWS 4
 typedef struct dc_expert_shape {

@@ -637,6 +637,7 @@ cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
     MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false, 0};
     a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;
     const int64_t tiles = (g.rows / bn + g.experts + 2) * nm;
+    if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;  // more than memory holds
     if (dtype == DC_FP32) return launch_size<float, kRowsK>(bn, ma, mb, a, tiles, stream);
     if (dtype == DC_BF16)
         return k_major ? launch_size<__nv_bfloat16, kRowsK>(bn, ma, mb, a, tiles, stream)

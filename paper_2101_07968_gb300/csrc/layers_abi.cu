@@ -18,7 +18,7 @@ cudaError_t sm_count(int &n)
 namespace {
 
 constexpr int64_t kRowsMax = (int64_t(1) << 31) - 1;
-constexpr int64_t kStrideMax = int64_t(1) << 40;
+constexpr int64_t kStrideMax = int64_t(1) << 37;  // tile copies take strides below 2^40 bytes
 
 bool rows_ok(int64_t rows) { return rows >= 0 && rows <= kRowsMax; }
 bool dim_ok(int64_t n) { return n >= 1 && n <= DC_LAYER_DIM_MAX; }
