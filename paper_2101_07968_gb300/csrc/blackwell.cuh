@@ -83,17 +83,32 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 }
 __device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
-// A wait that ends: after kWaitTries tries, or once another thread of the CTA has given
-// up, it gives up (false). A wait of this library's kernels lasts microseconds.
+// A wait that ends: after kWaitTries tries or kWaitNs nanoseconds (a try may sleep a while), or
+// once another thread of the CTA has given up, it gives up (false). A wait of this library's
+// kernels lasts microseconds.
 constexpr uint32_t kWaitTries = 1u << 23;
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+constexpr uint64_t kWaitNs = 2000000000ull;
+__device__ __forceinline__ uint64_t now_ns()
 {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    const uint64_t start = now_ns();
     for (uint32_t i = 0; i < kWaitTries; ++i) {
         if (bar_try(bar, parity)) return true;
-        if ((i & 1023u) == 1023u && *gave_up) return false;
+        if ((i & 63u) == 63u && (*gave_up || now_ns() - start > kWaitNs)) break;
     }
     *gave_up = 1u;
     return false;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    for (int i = 0; i < 16; ++i)
+        if (bar_try(bar, parity)) return true;
+    return bar_wait_long(bar, parity, gave_up);
 }
 
 // --------------------------------------------------------------------------- copies

@@ -153,7 +153,9 @@ _PRODUCTS = ("dc_expert_matmul", "dc_expert_matmul_grad_input", "dc_expert_matmu
 
 def _product(which, shape, a, b, offsets, c, stream):
     ap, bp = a.data_ptr(), b.data_ptr()
-    need = _function("dc_expert_workspace_bytes")(shape, which, ap, bp)
+    # few rows need none in any case
+    few = which < 2 and a.shape[0] <= dc.DC_FEW_ROWS
+    need = 0 if few else _function("dc_expert_workspace_bytes")(shape, which, ap, bp)
     ws = _empty(need, dtype=torch.uint8, device=a.device) if need else None
     _run(_PRODUCTS[which], a, stream, shape, ap, bp, offsets.data_ptr(), c.data_ptr(),
          _status_of(a.get_device()), ws.data_ptr() if need else None, need)
