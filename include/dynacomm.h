@@ -328,7 +328,7 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
  * w_expert, w_n, w_k (elements); one of w_n and w_k is 1.
  * 16-bit operands run on the tensor cores; those whose rows start off 16-byte boundaries
  * are first copied into the workspace, row by row, so that they start on them. Floats go
- * there in three parts of 11 significant bits, whose products are summed as floats (small
+ * there in two parts of 11 significant bits, whose products are summed as floats (small
  * products of floats run on the CUDA cores). Up to DC_FEW_ROWS rows in all (floats: 16 times
  * as many) take a pass that streams the weights over every SM. workspace: dc_expert_workspace_bytes(shape, product, a,
  * b) bytes, 256-byte aligned, used during the call's kernels only, where product is 0 for

@@ -3,12 +3,12 @@
 // go in parts.
 //
 // Floats on the tensor cores: x = hi + lo with hi and lo of the 11 significant bits that tf32
-// holds, and x w = hi hi + hi lo + lo hi, one product over a summed axis three times as long.
+// holds, and x w = hi hi + hi lo + lo hi: three products of operands that hold both parts.
 // What is left out (lo lo, and the bits of x past lo) is below 3 2^-22 |x w| a product, some
 // 2^-23 on average, less than a 32-bit sum of more than a few products loses; so the
 // CUDA cores take products of fewer than kPartDepth summed elements, and weight gradients of
-// experts of fewer than kPartLeast rows. 16,384 rows over 8 experts x 2,048 x 2,048: 0.94-0.97 ms,
-// 145 TFLOP/s, of which the copies take some 0.16 ms (a library product of floats 2.3 ms), and
+// experts of fewer than kPartLeast rows. 16,384 rows over 8 experts x 2,048 x 2,048: 0.66-0.69 ms,
+// 198-208 TFLOP/s, of which the copies take some 0.12 ms (a library product of floats 2.3 ms), and
 // 3.5e-7 off in the root mean square, as sums in floats are.
 #include "expert_rows.cuh"
 
@@ -108,8 +108,8 @@ void operands(const ExpertArgs &g, bool weights, Matrix &a, Matrix &b)
 
 // Two rows, two experts x 4,096 x 2,048: 8.3 us, by tiles 12.2; eight rows 12.5 against 12.1;
 // sixteen rows of as many experts x 2,048 x 2,048 36 against 26.8. Floats go that way up to 64 rows:
-// their parts would cost three times the weights' bytes to write (30 rows over 4 experts x
-// 2,048 x 2,048: 55 us, in parts 140).
+// their parts would cost twice the weights' bytes to write (30 rows over 4 experts x
+// 2,048 x 2,048: 43 us, in three parts 140).
 bool few(int dtype, const ExpertArgs &g, bool weights)
 {
     return !weights && g.rows <= (dtype == DC_FP32 ? 16 * DC_FEW_ROWS : DC_FEW_ROWS);
@@ -130,19 +130,16 @@ __device__ __forceinline__ void parts_of(float x, float &hi, float &lo)
     lo = __uint_as_float(h & 0xffffe000u);
 }
 
-// The three thirds of a row: hi, hi, lo for one operand (FIRST) and hi, lo, hi for the other.
-template <bool FIRST>
-__device__ __forceinline__ void put_parts(float *row, int64_t third, int64_t at, float x)
+// A row's high parts, then its low ones.
+__device__ __forceinline__ void put_parts(float *row, int64_t half, int64_t at, float x)
 {
     float hi, lo;
     parts_of(x, hi, lo);
     row[at] = hi;
-    row[third + at] = FIRST ? hi : lo;
-    row[2 * third + at] = FIRST ? lo : hi;
+    row[half + at] = lo;
 }
 
 // Rows [z][y][x], x contiguous and summed.
-template <bool FIRST>
 __global__ void __launch_bounds__(kThreads)
 split_rows_kernel(const float *src, float *dst, int64_t rows, int32_t y, int32_t x, int32_t pad,
                   int64_t stride_z, int64_t stride_y)
@@ -151,11 +148,10 @@ split_rows_kernel(const float *src, float *dst, int64_t rows, int32_t y, int32_t
     const int64_t r = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
     if (c >= pad || r >= rows) return;
     const float v = c < x ? src[(r / y) * stride_z + (r % y) * stride_y + c] : 0.0f;
-    put_parts<FIRST>(dst + r * 3 * pad, pad, c, v);
+    put_parts(dst + r * 2 * pad, pad, c, v);
 }
 
 // [z][x][y], y contiguous and x summed, to rows [z][y].
-template <bool FIRST>
 __global__ void __launch_bounds__(kThreads)
 split_columns_kernel(const float *src, float *dst, int32_t y, int32_t x, int32_t pad, int64_t stride_z,
                      int64_t stride_x)
@@ -169,12 +165,11 @@ split_columns_kernel(const float *src, float *dst, int32_t y, int32_t x, int32_t
     __syncthreads();
     for (int i = ty; i < 32; i += kThreads / 32)
         if (y0 + i < y)
-            put_parts<FIRST>(dst + (int64_t(blockIdx.z) * y + y0 + i) * 3 * pad, pad, x0 + tx, tile[tx][i]);
+            put_parts(dst + (int64_t(blockIdx.z) * y + y0 + i) * 2 * pad, pad, x0 + tx, tile[tx][i]);
 }
 
 // The rows of the batch [rows][y], summed expert by expert, to rows [y]: each segment's rows are
-// rounded up to kPartRows with zeros, and its three thirds lie side by side.
-template <bool FIRST>
+// rounded up to kPartRows with zeros, and its two parts lie side by side.
 __global__ void __launch_bounds__(kThreads)
 split_segments_kernel(const float *src, float *dst, const int64_t *offsets, int64_t rows, int32_t experts,
                       int32_t y, int64_t stride, int64_t pitch)
@@ -188,39 +183,38 @@ split_segments_kernel(const float *src, float *dst, const int64_t *offsets, int6
     if (t >= seg.tile[seg.count]) return;
     const int s = find_segment(seg.tile, seg.count, t), first = seg.tile[s];
     const int64_t r0 = seg.start[s] + int64_t(t - first) * kPartRows, end = seg.start[s + 1];
-    const int64_t third = int64_t(seg.tile[s + 1] - first) * kPartRows;
+    const int64_t half = int64_t(seg.tile[s + 1] - first) * kPartRows;
     const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, y0 = blockIdx.y * 32;
     for (int i = ty; i < kPartRows; i += kThreads / 32)
         tile[i][tx] = r0 + i < end && y0 + tx < y ? src[(r0 + i) * stride + y0 + tx] : 0.0f;
     __syncthreads();
     for (int i = ty; i < 32; i += kThreads / 32)
         if (y0 + i < y)
-            put_parts<FIRST>(dst + (y0 + i) * pitch + int64_t(first) * 3 * kPartRows, third,
+            put_parts(dst + (y0 + i) * pitch + int64_t(first) * 2 * kPartRows, half,
                              int64_t(t - first) * kPartRows + tx, tile[tx][i]);
 }
 
 int64_t part_pad(int64_t r) { return (r + 31) / 32 * 32; }
 // the longest that the segments' rounded rows can be
 int64_t part_rows(const ExpertArgs &g) { return (g.rows / kPartRows + g.experts + 3) * kPartRows; }
-size_t part_bytes(int64_t rows, int64_t length) { return (size_t(rows) * 3 * length * 4 + 255) / 256 * 256; }
+size_t part_bytes(int64_t rows, int64_t length) { return (size_t(rows) * 2 * length * 4 + 255) / 256 * 256; }
 
 // Shorter sums and smaller batches stay on the CUDA cores, where the bounds above hold and the
 // copies would take longer than the products (200 rows over 8 experts x 512 x 512 take 33-36 us
 // in parts, of which 25 are copies and launches).
 bool use_parts(const ExpertArgs &g, bool weights)
 {
-    if (3 * part_rows(g) >= int64_t(1) << 31) return false;
+    if (2 * part_rows(g) >= int64_t(1) << 31) return false;
     return weights ? g.rows >= 64 && g.rows >= 2 * kPartLeast * int64_t(g.experts)
                    : g.r >= kPartDepth;
 }
 
-template <bool FIRST>
 cudaError_t split_rows(const Matrix &m, float *dst, cudaStream_t stream)
 {
     const int64_t pad = part_pad(m.x), rows = m.z * m.y;
     const int bx = 32, by = kThreads / bx;
     const dim3 grid(unsigned((rows + by - 1) / by), unsigned((pad + bx - 1) / bx));
-    split_rows_kernel<FIRST><<<grid, dim3(bx, by), 0, stream>>>(static_cast<const float *>(m.p), dst, rows, int32_t(m.y),
+    split_rows_kernel<<<grid, dim3(bx, by), 0, stream>>>(static_cast<const float *>(m.p), dst, rows, int32_t(m.y),
                                                                int32_t(m.x), int32_t(pad), m.stride_z, m.stride_y);
     return cudaGetLastError();
 }
@@ -230,25 +224,25 @@ cudaError_t float_rows(const ExpertArgs &g, void *workspace, cudaStream_t stream
     const int64_t pad = part_pad(g.r);
     float *a = static_cast<float *>(workspace);
     float *b = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(g.rows, pad));
-    cudaError_t e = split_rows<true>({g.a, 1, g.rows, g.r, 0, g.a_m}, a, stream);
+    cudaError_t e = split_rows({g.a, 1, g.rows, g.r, 0, g.a_m}, a, stream);
     if (e != cudaSuccess) return e;
     if (g.b_r == 1) {
-        e = split_rows<false>({g.b, g.experts, g.n, g.r, g.b_e, g.b_n}, b, stream);
+        e = split_rows({g.b, g.experts, g.n, g.r, g.b_e, g.b_n}, b, stream);
     } else {
         const dim3 grid(unsigned(pad / 32), unsigned((g.n + 31) / 32), unsigned(g.experts));
-        split_columns_kernel<false><<<grid, kThreads, 0, stream>>>(static_cast<const float *>(g.b), b, g.n, g.r,
+        split_columns_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(g.b), b, g.n, g.r,
                                                                    int32_t(pad), g.b_e, g.b_r);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
     ExpertArgs h = g;
     h.a = a;
-    h.a_m = 3 * pad;
+    h.a_m = 2 * pad;
     h.b = b;
     h.b_r = 1;
-    h.b_n = 3 * pad;
-    h.b_e = 3 * pad * g.n;
-    h.r = int32_t(3 * pad);
+    h.b_n = 2 * pad;
+    h.b_e = 2 * pad * g.n;
+    h.r = int32_t(pad);
     return expert_mma_rows(DC_FP32, h, stream);
 }
 
@@ -258,19 +252,19 @@ cudaError_t float_weights(const ExpertArgs &g, void *workspace, cudaStream_t str
     float *a = static_cast<float *>(workspace);
     float *b = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(g.m, length));
     const unsigned tiles = unsigned(length / kPartRows);
-    split_segments_kernel<true><<<dim3(tiles, unsigned((g.m + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
-        static_cast<const float *>(g.a), a, g.offsets, g.rows, g.experts, g.m, g.a_r, 3 * length);
+    split_segments_kernel<<<dim3(tiles, unsigned((g.m + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
+        static_cast<const float *>(g.a), a, g.offsets, g.rows, g.experts, g.m, g.a_r, 2 * length);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    split_segments_kernel<false><<<dim3(tiles, unsigned((g.n + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
-        static_cast<const float *>(g.b), b, g.offsets, g.rows, g.experts, g.n, g.b_r, 3 * length);
+    split_segments_kernel<<<dim3(tiles, unsigned((g.n + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
+        static_cast<const float *>(g.b), b, g.offsets, g.rows, g.experts, g.n, g.b_r, 2 * length);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     ExpertArgs h = g;
     h.a = a;
-    h.a_r = 3 * length;
+    h.a_r = 2 * length;
     h.b = b;
-    h.b_r = 3 * length;
+    h.b_r = 2 * length;
     e = expert_mma_weights(DC_FP32, h, kPartLeast, stream);
     return e != cudaSuccess ? e : expert_simt_weights(g, kPartLeast - 1, stream);
 }

@@ -7,8 +7,9 @@
 //   dx  A = W_e^T (features contiguous)       B = dy
 //   dW  A = dy^T, B = x^T (both with the summed axis, an expert's rows, outermost)
 // The hardware reads either order of an operand, so nothing is transposed.
-// Floats come as parts that tf32 holds (expert_dispatch.cu), with the summed axis innermost,
-// padded and three times as long: hi hi + hi lo + lo hi.
+// Floats come as two parts that tf32 holds (expert_dispatch.cu), side by side along the summed
+// axis, which is innermost and padded. A stage takes both parts of both operands and feeds three
+// products: hi hi to one set of sums, hi lo and lo hi to another.
 //
 // A persistent pair of CTAs, one tile of 256 features between them, takes every grid-th tile.
 // Warp 4 copies operand blocks of 128 bytes along the summed axis into a ring of stages by TMA;
@@ -76,10 +77,10 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
         q.cols = min(BN, a.n - q.n0);
         q.r0 = seg.start[q.e + 1];
         q.r = seg.start[q.e + 2] - q.r0;
-        if (MODE == kWeightsK) {  // three parts of the padded rows
+        if (MODE == kWeightsK) {  // the padded rows' high parts, then their low ones
             if (q.r < a.least) q.cols = 0;
-            q.r0 = 3 * kPartRows * seg.tile[q.e + 1];
-            q.r = 3 * kPartRows * (seg.tile[q.e + 2] - seg.tile[q.e + 1]);
+            q.r0 = 2 * kPartRows * seg.tile[q.e + 1];
+            q.r = kPartRows * (seg.tile[q.e + 2] - seg.tile[q.e + 1]);
         }
     } else {
         const int nm = (a.m + kBM * CG - 1) / (kBM * CG);
@@ -247,11 +248,11 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     constexpr bool kAMn = MODE == kRowsMN || MODE == kWeights;
     // Blocks summed in the tensor cores at a time. They cut a sum off at every step where a
     // float would round, toward zero, some 2e-8 of it: over 192 steps float products came
-    // out 4e-6 off, ten times what sums in floats lose. So those of floats are handed over every
-    // 32 steps, which two sets of sums take in turn, and added up in registers, rounded: 3.5e-7 off.
-    constexpr int kRound = kTf32 ? 8 : 1 << 24;
-    constexpr uint32_t kStage = kABytes + kBBytes;
-    constexpr int kSets = kTf32 ? 2 : 1;
+    // out 4e-6 off, ten times what sums in floats lose. So the sums of floats are handed over every
+    // 16 steps of hi hi and added up in registers, rounded: 3.5e-7 off.
+    constexpr int kRound = kTf32 ? 4 : 1 << 24;
+    constexpr int kParts = kTf32 ? 2 : 1, kSets = kParts;
+    constexpr uint32_t kStage = kParts * (kABytes + kBBytes);
     constexpr uint32_t kColumns = 2 * kSets * BN;
     extern __shared__ unsigned char dyn[];
     __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
@@ -306,14 +307,14 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;  // of this CTA
                 const int boxes = (cols + kBoxRows - 1) / kBoxRows;
                 const int m = q.m0 + int(rank) * kBM, n = q.n0 + int(rank) * cols;
-                const uint32_t bytes = kABytes + boxes * kBBox;
+                const uint32_t bytes = kParts * (kABytes + boxes * kBBox);
                 const int end = q.r0 + q.r;
                 for (int r = q.r0; r < end; r += kBK) {
                     if (filled < STAGES)
                         ++filled;
                     else if (!(ok = bw::bar_wait(bar(&empty[s]), phase, &gave_up)))
                         break;
-                    const uint32_t sa = ring + s * kStage, sb = sa + kABytes;
+                    const uint32_t sa = ring + s * kStage, sb = sa + kParts * kABytes;
                     const bool zeros = MODE == kWeights && end - r <= kBK && ((end - r) & 15);
                     const uint32_t b = zeros ? bar(&tail[s]) : full0 + s * uint32_t(sizeof(uint64_t));
                     if (zeros) {
@@ -322,8 +323,17 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         bw::bar_arrive_bytes(bar(&full[s]), bytes * CG);
                         if (CG == 2) bw::bar_arrive(bar(&full[s]));
                     }
-                    if (MODE == kWeightsK) {
-                        bw::copy_2d<CG == 2>(sa, &map_a, r, m, b);
+                    if (kTf32) {  // both parts of both operands
+#pragma unroll
+                        for (int part = 0; part < kParts; ++part) {
+                            const int x = r + part * q.r;
+                            if (MODE == kWeightsK)
+                                bw::copy_2d<CG == 2>(sa + part * kABytes, &map_a, x, m, b);
+                            else
+                                bw::copy_3d<CG == 2>(sa + part * kABytes, &map_a, x, m, q.e, b);
+                            for (int i = 0; i < boxes; ++i)
+                                bw::copy_2d<CG == 2>(sb + part * kBBytes + i * kBBox, &map_b, x, n + kBoxRows * i, b);
+                        }
                     } else if (MODE == kRowsK) {
                         bw::copy_3d<CG == 2>(sa, &map_a, r, m, q.e, b);
                     } else if (MODE == kRowsMN) {
@@ -333,7 +343,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         bw::copy_2d<CG == 2>(sa, &map_a, m, r, b);
                         bw::copy_2d<CG == 2>(sa + kBoxBytes, &map_a, m + 64, r, b);
                     }
-                    for (int i = 0; i < boxes; ++i)
+                    for (int i = 0; i < boxes && !kTf32; ++i)
                         if (MODE == kWeights)
                             bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, n + kBoxRows * i, r, b);
                         else
@@ -381,19 +391,22 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         bw::fence_after();
                         const uint32_t sa = ring + s * kStage;
                         const uint64_t da = bw::operand(sa, kAMn ? kBoxBytes : 16);
-                        const uint64_t db = bw::operand(sa + kABytes, MODE == kWeights ? kBoxBytes : 16);
+                        const uint64_t db = bw::operand(sa + kParts * kABytes, MODE == kWeights ? kBoxBytes : 16);
                         auto step_of = [&](int i, bool add) {
-                            const uint32_t to = d + i % kSets * BN;
-                            if constexpr (kTf32)
-                                bw::mma_tf32<CG>(to, da + i * 2, db + i * 2, shape, add);
-                            else
-                                bw::mma<CG>(to, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape, add);
+                            if constexpr (kTf32) {
+                                constexpr uint64_t kLowA = kABytes >> 4, kLowB = kBBytes >> 4;
+                                bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, add);
+                                bw::mma_tf32<CG>(d + BN, da + i * 2, db + kLowB + i * 2, shape, add);
+                                bw::mma_tf32<CG>(d + BN, da + kLowA + i * 2, db + i * 2, shape, true);
+                            } else {
+                                bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape, add);
+                            }
                         };
                         if (left >= kBK) {  // straight on: a loop's branches would hold the products up
 #pragma unroll
-                            for (int i = 0; i < kBK / kStep; ++i) step_of(i, i >= kSets || kb > k0);
+                            for (int i = 0; i < kBK / kStep; ++i) step_of(i, i > 0 || kb > k0);
                         } else {
-                            for (int i = 0; i * kStep < left; ++i) step_of(i, i >= kSets || kb > k0);
+                            for (int i = 0; i * kStep < left; ++i) step_of(i, i > 0 || kb > k0);
                         }
                         bw::commit<CG>(bar(&empty[s]));
                         if (++s == STAGES) {
@@ -465,7 +478,6 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 if (!ok) break;
                 bw::fence_after();
                 const uint32_t at = tmem + half * (kSets * BN) + (uint32_t(warp * 32) << 16);
-                const bool second = kSets == 2 && q.r - k0 * kBK > kStep;  // set in use
                 auto all_read = [&] {  // the half may be overwritten
                     bw::fence_before();
                     __syncwarp();
@@ -480,11 +492,9 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             bw::tmem_load(at + c * 32, v);
 #pragma unroll
                             for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-                            if (second) {
-                                bw::tmem_load(at + BN + c * 32, v);
+                            bw::tmem_load(at + BN + c * 32, v);
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-                            }
+                            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
                         }
                     }
                     all_read();
@@ -494,12 +504,6 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         __syncwarp();
                         if (blocks > 0) {
                             bw::tmem_load(at + c0, v);
-                            if (second) {
-                                float w[32];
-                                bw::tmem_load(at + BN + c0, w);
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) v[j] += w[j];
-                            }
                         } else {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0.0f;
@@ -574,7 +578,7 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
                          int64_t most_tiles, cudaStream_t stream)
 {
         auto kernel = expert_mma_kernel<T, MODE, CG, BN, STAGES>;
-    constexpr size_t ring = size_t(STAGES) * (kABytes + kStageRows<MODE, CG, BN> * kBKBytes) + 1024;
+    constexpr size_t ring = size_t(STAGES) * (std::is_same<T, float>::value ? 2 : 1) * (kABytes + kStageRows<MODE, CG, BN> * kBKBytes) + 1024;
     const size_t smem = ring + segments_bytes(a.experts);
     static DeviceCache cache;
     int ready = 0, sms = 0;
@@ -611,10 +615,12 @@ template <typename T, int MODE>
 cudaError_t launch_size(int bn, const CUtensorMap &ma, const CUtensorMap &mb, const MmaArgs &a, int64_t tiles,
                         cudaStream_t stream)
 {
-    // floats: 128 sums a thread of the four warps that add up the rounds
-    constexpr int kWide = std::is_same<T, float>::value ? 128 : 256;
-    return bn == 64 ? launch_typed<T, MODE, 2, 64, 8>(ma, mb, a, tiles, stream)
-                    : launch_typed<T, MODE, 2, kWide, kWide == 128 ? 8 : 6>(ma, mb, a, tiles, stream);
+    if constexpr (std::is_same<T, float>::value)  // 128 sums a thread of the four warps that add up the rounds
+        return bn == 64 ? launch_typed<T, MODE, 2, 64, 4>(ma, mb, a, tiles, stream)
+                        : launch_typed<T, MODE, 2, 128, 4>(ma, mb, a, tiles, stream);
+    else
+        return bn == 64 ? launch_typed<T, MODE, 2, 64, 8>(ma, mb, a, tiles, stream)
+                        : launch_typed<T, MODE, 2, 256, 6>(ma, mb, a, tiles, stream);
 }
 
 }  // namespace
@@ -624,7 +630,8 @@ cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
 {
     const bool k_major = g.b_r == 1;
     const int64_t stride = k_major ? g.b_n : g.b_r;
-    const int64_t inner = k_major ? g.r : g.n, outer = k_major ? g.n : g.r;
+    const int parts = dtype == DC_FP32 ? 2 : 1;
+    const int64_t inner = k_major ? parts * int64_t(g.r) : g.n, outer = k_major ? g.n : g.r;
     // with one expert the stride between experts is not used, but it has to be valid
     const int64_t expert = g.experts == 1 ? stride * outer : g.b_e;
     // tiles of an average expert
@@ -632,7 +639,7 @@ cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
     const int bn = tile_rows(dtype, g.experts * nm * ((each + 255) / 256));
     CUtensorMap ma, mb;
     if (!make_map(ma, dtype, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
-        !make_map(mb, dtype, g.a, g.r, g.rows, 1, g.a_m, 0, bn < 128 ? bn / 2 : 64))
+        !make_map(mb, dtype, g.a, parts * int64_t(g.r), g.rows, 1, g.a_m, 0, bn < 128 ? bn / 2 : 64))
         return cudaErrorInvalidValue;
     MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false, 0};
     a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;

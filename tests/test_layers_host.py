@@ -57,10 +57,10 @@ def test_expert_workspace(lib):
     assert q(shape(rows=dc.DC_FEW_ROWS, K=33, ldx=33, w_n=33, w_expert=64 * 33), 0, FAKE, FAKE) == 0  # few rows
     assert q(shape(dtype=3), 0, FAKE, FAKE) == 0 and q(shape(), 3, FAKE, FAKE) == 0
     assert q(shape(rows=0), 0, FAKE, FAKE) == 0 and q(None, 0, FAKE, FAKE) == 0
-    # floats: three parts of both operands
+    # floats: two parts of both operands
     f = dict(dtype=dc.DC_FP32, rows=1000, K=256, ldx=256, w_n=256, w_expert=64 * 256)
-    assert q(shape(**f), 0, FAKE, FAKE) >= 3 * 4 * 256 * (1000 + 2 * 64)
-    assert q(shape(**f), 2, FAKE, FAKE) >= 3 * 4 * 1000 * (64 + 256)
+    assert q(shape(**f), 0, FAKE, FAKE) >= 2 * 4 * 256 * (1000 + 2 * 64)
+    assert q(shape(**f), 2, FAKE, FAKE) >= 2 * 4 * 1000 * (64 + 256)
 
 
 def test_gated_checks(lib):
