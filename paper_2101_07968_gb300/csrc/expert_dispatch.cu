@@ -109,7 +109,7 @@ void operands(const ExpertArgs &g, bool weights, Matrix &a, Matrix &b)
 // Two rows, two experts x 4,096 x 2,048: 8.3 us, by tiles 12.2; eight rows 12.5 against 12.1;
 // sixteen rows of as many experts x 2,048 x 2,048 36 against 26.8. Floats go that way up to 64 rows:
 // their parts would cost twice the weights' bytes to write (30 rows over 4 experts x
-// 2,048 x 2,048: 43 us, in three parts 140).
+// 2,048 x 2,048: 29 us in a graph, in parts 108).
 bool few(int dtype, const ExpertArgs &g, bool weights)
 {
     return !weights && g.rows <= (dtype == DC_FP32 ? 16 * DC_FEW_ROWS : DC_FEW_ROWS);
@@ -118,7 +118,7 @@ bool few(int dtype, const ExpertArgs &g, bool weights)
 // ----------------------------------------------------------------- floats in parts
 constexpr int kPartDepth = 64, kPartLeast = 8;
 
-__device__ __forceinline__ void parts_of(float x, float &hi, float &lo)
+__device__ __forceinline__ void parts_of(const float x, float &hi, float &lo)
 {
     uint32_t h;
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(h) : "f"(x));
@@ -139,16 +139,28 @@ __device__ __forceinline__ void put_parts(float *row, int64_t half, int64_t at, 
     row[half + at] = lo;
 }
 
-// Rows [z][y][x], x contiguous and summed.
+// Rows [z][y][x], x contiguous and summed; a thread takes four elements. wide: rows start on
+// 16-byte boundaries.
 __global__ void __launch_bounds__(kThreads)
 split_rows_kernel(const float *src, float *dst, int64_t rows, int32_t y, int32_t x, int32_t pad,
-                  int64_t stride_z, int64_t stride_y)
+                  int64_t stride_z, int64_t stride_y, bool wide)
 {
-    const int c = blockIdx.y * blockDim.x + threadIdx.x;
+    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4;
     const int64_t r = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
     if (c >= pad || r >= rows) return;
-    const float v = c < x ? src[(r / y) * stride_z + (r % y) * stride_y + c] : 0.0f;
-    put_parts(dst + r * 2 * pad, pad, c, v);
+    const float *p = src + (r / y) * stride_z + (r % y) * stride_y;
+    Vec<float, 4> v, lo;
+    if (wide && c + 4 <= x) {
+        v = *reinterpret_cast<const Vec<float, 4> *>(p + c);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v.e[j] = c + j < x ? p[c + j] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) parts_of(v.e[j], v.e[j], lo.e[j]);
+    float *q = dst + r * 2 * pad + c;
+    *reinterpret_cast<Vec<float, 4> *>(q) = v;
+    *reinterpret_cast<Vec<float, 4> *>(q + pad) = lo;
 }
 
 // [z][x][y], y contiguous and x summed, to rows [z][y].
@@ -212,10 +224,13 @@ bool use_parts(const ExpertArgs &g, bool weights)
 cudaError_t split_rows(const Matrix &m, float *dst, cudaStream_t stream)
 {
     const int64_t pad = part_pad(m.x), rows = m.z * m.y;
-    const int bx = 32, by = kThreads / bx;
-    const dim3 grid(unsigned((rows + by - 1) / by), unsigned((pad + bx - 1) / bx));
-    split_rows_kernel<<<grid, dim3(bx, by), 0, stream>>>(static_cast<const float *>(m.p), dst, rows, int32_t(m.y),
-                                                               int32_t(m.x), int32_t(pad), m.stride_z, m.stride_y);
+    int bx = 8;
+    while (bx < 64 && bx < pad / 4) bx *= 2;
+    const int by = kThreads / bx;
+    const dim3 grid(unsigned((rows + by - 1) / by), unsigned((pad / 4 + bx - 1) / bx));
+    const bool wide = aligned16(m.p) && m.stride_y % 4 == 0 && (m.z == 1 || m.stride_z % 4 == 0);
+    split_rows_kernel<<<grid, dim3(unsigned(bx), unsigned(by)), 0, stream>>>(
+        static_cast<const float *>(m.p), dst, rows, int32_t(m.y), int32_t(m.x), int32_t(pad), m.stride_z, m.stride_y, wide);
     return cudaGetLastError();
 }
 
