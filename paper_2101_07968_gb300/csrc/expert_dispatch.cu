@@ -7,9 +7,8 @@
 // What is left out (lo lo, and the bits of x past lo) is below 3 2^-22 |x w| a product, some
 // 2^-23 on average, less than a 32-bit sum of more than a few products loses; so the
 // CUDA cores take products of fewer than kPartDepth summed elements, and weight gradients of
-// experts of fewer than kPartLeast rows. 16,384 rows over 8 experts x 2,048 x 2,048: 0.66-0.69 ms,
-// 198-208 TFLOP/s, of which the copies take some 0.12 ms (a library product of floats 2.3 ms), and
-// 3.5e-7 off in the root mean square, as sums in floats are.
+// experts of fewer than kPartLeast rows. 16,384 rows over 8 experts x 2,048 x 2,048: 0.53-0.55 ms,
+// 250-257 TFLOP/s with the copies (a library product of floats 2.3 ms), and 3.5e-7 off in the root mean square, as sums in floats are.
 #include "expert_rows.cuh"
 
 namespace dc {
@@ -163,21 +162,38 @@ split_rows_kernel(const float *src, float *dst, int64_t rows, int32_t y, int32_t
     *reinterpret_cast<Vec<float, 4> *>(q + pad) = lo;
 }
 
+// The transposing copies: a block brings 32 summed lines of kAcross columns into shared memory
+// and writes them as parts, 32 neighbours of a column at a time.
+constexpr int kAcross = 128;
+struct Across {
+    float at[32][kAcross + 1];
+};
+__device__ __forceinline__ void load_across(Across &t, const float *p, int64_t stride, int64_t lines, int columns)
+{
+    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
+#pragma unroll
+    for (int i = 0; i < 32; i += kThreads / 32)
+#pragma unroll
+        for (int c = 0; c < kAcross; c += 32)
+            t.at[i + ty][c + tx] = i + ty < lines && c + tx < columns ? p[(i + ty) * stride + c + tx] : 0.0f;
+    __syncthreads();
+}
+__device__ __forceinline__ void put_across(const Across &t, float *rows, int64_t pitch, int64_t half, int columns)
+{
+    const int tx = threadIdx.x % 32;
+#pragma unroll 4
+    for (int c = threadIdx.x / 32; c < columns; c += kThreads / 32) put_parts(rows + c * pitch, half, tx, t.at[tx][c]);
+}
+
 // [z][x][y], y contiguous and x summed, to rows [z][y].
 __global__ void __launch_bounds__(kThreads)
 split_columns_kernel(const float *src, float *dst, int32_t y, int32_t x, int32_t pad, int64_t stride_z,
                      int64_t stride_x)
 {
-    __shared__ float tile[32][33];
-    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-    const int x0 = blockIdx.x * 32, y0 = blockIdx.y * 32;
-    const float *p = src + blockIdx.z * stride_z;
-    for (int i = ty; i < 32; i += kThreads / 32)
-        tile[i][tx] = x0 + i < x && y0 + tx < y ? p[(x0 + i) * stride_x + y0 + tx] : 0.0f;
-    __syncthreads();
-    for (int i = ty; i < 32; i += kThreads / 32)
-        if (y0 + i < y)
-            put_parts(dst + (int64_t(blockIdx.z) * y + y0 + i) * 2 * pad, pad, x0 + tx, tile[tx][i]);
+    __shared__ Across tile;
+    const int x0 = blockIdx.x * 32, y0 = blockIdx.y * kAcross, columns = min(kAcross, y - y0);
+    load_across(tile, src + blockIdx.z * stride_z + x0 * stride_x + y0, stride_x, x - x0, columns);
+    put_across(tile, dst + (int64_t(blockIdx.z) * y + y0) * 2 * pad + x0, 2 * int64_t(pad), pad, columns);
 }
 
 // The rows of the batch [rows][y], summed expert by expert, to rows [y]: each segment's rows are
@@ -187,23 +203,22 @@ split_segments_kernel(const float *src, float *dst, const int64_t *offsets, int6
                       int32_t y, int64_t stride, int64_t pitch)
 {
     extern __shared__ int32_t dyn[];
-    __shared__ float tile[kPartRows][33];
+    __shared__ Across tile;
     const Segments seg = segments_at(dyn, experts);
     if (threadIdx.x < 32) build_segments<false>(seg, offsets, rows, experts, kPartRows, 1);
     __syncthreads();
     const int t = blockIdx.x;
     if (t >= seg.tile[seg.count]) return;
     const int s = find_segment(seg.tile, seg.count, t), first = seg.tile[s];
-    const int64_t r0 = seg.start[s] + int64_t(t - first) * kPartRows, end = seg.start[s + 1];
+    const int64_t r0 = seg.start[s] + int64_t(t - first) * kPartRows;
     const int64_t half = int64_t(seg.tile[s + 1] - first) * kPartRows;
-    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, y0 = blockIdx.y * 32;
-    for (int i = ty; i < kPartRows; i += kThreads / 32)
-        tile[i][tx] = r0 + i < end && y0 + tx < y ? src[(r0 + i) * stride + y0 + tx] : 0.0f;
-    __syncthreads();
-    for (int i = ty; i < 32; i += kThreads / 32)
-        if (y0 + i < y)
-            put_parts(dst + (y0 + i) * pitch + int64_t(first) * 2 * kPartRows, half,
-                             int64_t(t - first) * kPartRows + tx, tile[tx][i]);
+    for (int y0 = blockIdx.y * kAcross; y0 < y; y0 += gridDim.y * kAcross) {
+        const int columns = min(kAcross, y - y0);
+        load_across(tile, src + r0 * stride + y0, stride, seg.start[s + 1] - r0, columns);
+        put_across(tile, dst + y0 * pitch + int64_t(first) * 2 * kPartRows + int64_t(t - first) * kPartRows, pitch, half,
+                   columns);
+        __syncthreads();
+    }
 }
 
 int64_t part_pad(int64_t r) { return (r + 31) / 32 * 32; }
@@ -212,8 +227,8 @@ int64_t part_rows(const ExpertArgs &g) { return (g.rows / kPartRows + g.experts 
 size_t part_bytes(int64_t rows, int64_t length) { return (size_t(rows) * 2 * length * 4 + 255) / 256 * 256; }
 
 // Shorter sums and smaller batches stay on the CUDA cores, where the bounds above hold and the
-// copies would take longer than the products (200 rows over 8 experts x 512 x 512 take 33-36 us
-// in parts, of which 25 are copies and launches).
+// copies would take longer than the products (200 rows over 8 experts x 512 x 512 take 27-32 us
+// in parts, most of it copies and launches).
 bool use_parts(const ExpertArgs &g, bool weights)
 {
     if (2 * part_rows(g) >= int64_t(1) << 31) return false;
@@ -244,7 +259,7 @@ cudaError_t float_rows(const ExpertArgs &g, void *workspace, cudaStream_t stream
     if (g.b_r == 1) {
         e = split_rows({g.b, g.experts, g.n, g.r, g.b_e, g.b_n}, b, stream);
     } else {
-        const dim3 grid(unsigned(pad / 32), unsigned((g.n + 31) / 32), unsigned(g.experts));
+        const dim3 grid(unsigned(pad / 32), unsigned((g.n + kAcross - 1) / kAcross), unsigned(g.experts));
         split_columns_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(g.b), b, g.n, g.r,
                                                                    int32_t(pad), g.b_e, g.b_r);
         e = cudaGetLastError();
@@ -267,11 +282,13 @@ cudaError_t float_weights(const ExpertArgs &g, void *workspace, cudaStream_t str
     float *a = static_cast<float *>(workspace);
     float *b = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(g.m, length));
     const unsigned tiles = unsigned(length / kPartRows);
-    split_segments_kernel<<<dim3(tiles, unsigned((g.m + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
+    // a block finds its segment once, for up to four slices of columns
+    auto slices = [](int n) { return unsigned((n + 4 * kAcross - 1) / (4 * kAcross)); };
+    split_segments_kernel<<<dim3(tiles, slices(g.m)), kThreads, segments_bytes(g.experts), stream>>>(
         static_cast<const float *>(g.a), a, g.offsets, g.rows, g.experts, g.m, g.a_r, 2 * length);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    split_segments_kernel<<<dim3(tiles, unsigned((g.n + 31) / 32)), kThreads, segments_bytes(g.experts), stream>>>(
+    split_segments_kernel<<<dim3(tiles, slices(g.n)), kThreads, segments_bytes(g.experts), stream>>>(
         static_cast<const float *>(g.b), b, g.offsets, g.rows, g.experts, g.n, g.b_r, 2 * length);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
