@@ -8,7 +8,8 @@
 // 2^-23 on average, less than a 32-bit sum of more than a few products loses; so the
 // CUDA cores take products of fewer than kPartDepth summed elements, and weight gradients of
 // experts of fewer than kPartLeast rows. 16,384 rows over 8 experts x 2,048 x 2,048: 0.53-0.55 ms,
-// 250-257 TFLOP/s with the copies (a library product of floats 2.3 ms), and 3.5e-7 off in the root mean square, as sums in floats are.
+// 250-257 TFLOP/s with the copies (a library product of floats 2.3 ms), and 3.5e-7 off in the
+// root mean square, as sums in floats are.
 #include "expert_rows.cuh"
 
 namespace dc {

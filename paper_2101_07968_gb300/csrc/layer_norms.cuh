@@ -12,7 +12,7 @@
 //
 // Measured (one GB300): 32,768 x 2,048 bfloat16, rms, dropout, a gate per 2,048 rows: 94 us, 5.7 TB/s,
 // integer and floating issue 65 % busy (34 instructions an element; the generator's draws are
-// eight of them). Gradient, 32,765 x 4,096 half, layer norm, dropout, one gate: 369 us, 4.4 TB/s, at 54 % of
+// eight of them). Gradient, 32,765 x 4,096 half, layer norm, dropout, one gate: 358 us, 4.5 TB/s, at 54 % of
 // the issue slots with the 16 warps an SM that the sums in registers leave room for. One row
 // of 2,048: 3.2 us in a graph.
 #pragma once
