@@ -21,7 +21,7 @@
 //
 // Measured (bfloat16, one GB300): 16,384 rows over 16 experts x 4,096 x 2,048, y and dx 157 us,
 // dW 160 us (1,750 and 1,710 TFLOP/s); 65,536 rows over 32 experts x 2,048 x 4,096, 567-580 us
-// (1,900-1,940 TFLOP/s against a library product's 1,902). The tensor cores are busy 86 % of
+// (1,900-1,940 TFLOP/s against a library product's 1,902). The tensor cores are busy 85 % of
 // the time; a block's products take 512 cycles and its copies, read by every pair through the
 // L2, some 630 (15 TB/s). A product takes some 100 cycles to issue whatever its columns, so
 // tiles narrower than 256 do not run at the tensor cores' rate. With one or a few experts' rows

@@ -27,8 +27,9 @@ namespace norms {
 // for rows of up to 128 and 256 columns, that one warp takes, 4 and 8, so that its lanes
 // have work.
 constexpr int kElems = 16;
-// Rows above this take blocks of up to 1,024 threads, whose 64 registers each do not hold
-// the gradient's sums: they spill, which narrower rows are spared.
+// Rows above this take blocks of 512 threads, with a ring of rows where there is room for two,
+// and above twice this of 1,024, whose 64 registers each do not hold the gradient's sums: they
+// spill, which narrower rows are spared.
 constexpr int kNarrow = 256, kWideD = kNarrow * kElems;
 constexpr int elems_for(int D, bool vec)  // vec: rows on 16-byte boundaries
 {
@@ -919,6 +920,8 @@ cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
     const Plan p = plan_for(a.D, vec, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
     constexpr int V = kVec<T>;
+    if (a.D > kWideD && p.size <= 512 && p.stages && vec)
+        return norm_launch<T, V, 0, true, 512, kElems>(a, p, stream);
     if (a.D > kWideD)
         return vec ? norm_launch<T, V, 0, false, 1024, kElems>(a, p, stream)
                    : norm_launch<T, 1, 0, false, 1024, kElems>(a, p, stream);
@@ -950,6 +953,8 @@ cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t 
     const Plan p = plan_for(a.D, vec, 4, dtype_bytes(dtype), kGradThreads, kOwn);
     const int64_t P = grad_runs(dtype, a.rows, a.D, vec);
     constexpr int V = kVec<T>;
+    if (a.D > kWideD && p.size <= 512 && p.stages && vec)
+        return norm_grad_launch<T, V, 0, true, 512, kElems>(a, partial, P, p, stream);
     if (a.D > kWideD)
         return vec ? norm_grad_launch<T, V, 0, false, 1024, kElems>(a, partial, P, p, stream)
                    : norm_grad_launch<T, 1, 0, false, 1024, kElems>(a, partial, P, p, stream);
