@@ -335,8 +335,10 @@ constexpr int kOwn = 2;
 // the gate row changes. For shorter ones that costs more than it saves.
 constexpr int kLongGate = 8;
 
+// Resident blocks: 24 warps an SM. Two of 512 threads serve 8,192 x 5,120 in 96 us and x 3,001 in 88,
+// one in 127 and 113 (x 8,192, whose blocks are full, 115 against 102).
 template <typename T, int V, int FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
-__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 32 ? 32 : 1) norm_kernel(NormArgs a, int stages)
+__global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 512 ? 2 : MAXT == 32 ? 32 : 1) norm_kernel(NormArgs a, int stages)
 {
     using R = Row<T, V, (FULL > 0), EL>;
     extern __shared__ __align__(16) unsigned char dyn[];

@@ -52,6 +52,13 @@ def test_block_norm_widths(ly, kind, dtype, rows, D, per_gate):
         lo.assert_within(r["d" + k], v[0], bd[0], "d" + k)
 
 
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,D,per_gate", [(7, 5120, 3), (400, 8192, None), (5, 8200, 2), (6, 4104, 1)])
+def test_block_norm_wide_rows(ly, kind, dtype, rows, D, per_gate):
+    test_block_norm_widths(ly, kind, dtype, rows, D, per_gate)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layer_norm_far_from_zero(ly, dtype):
     """Rows whose mean is many deviations from zero, and rows whose first element is far from
