@@ -274,7 +274,7 @@ cudaError_t float_rows(const ExpertArgs &g, void *workspace, cudaStream_t stream
     h.b_n = 2 * pad;
     h.b_e = 2 * pad * g.n;
     h.r = int32_t(pad);
-    return expert_mma_rows(DC_FP32, h, stream);
+    return expert_mma_rows(DC_FP32, h, nullptr, stream);
 }
 
 cudaError_t float_weights(const ExpertArgs &g, void *workspace, cudaStream_t stream)
@@ -298,7 +298,7 @@ cudaError_t float_weights(const ExpertArgs &g, void *workspace, cudaStream_t str
     h.a_r = 2 * length;
     h.b = b;
     h.b_r = 2 * length;
-    e = expert_mma_weights(DC_FP32, h, kPartLeast, stream);
+    e = expert_mma_weights(DC_FP32, h, kPartLeast, nullptr, stream);
     return e != cudaSuccess ? e : expert_simt_weights(g, kPartLeast - 1, stream);
 }
 
@@ -314,7 +314,14 @@ size_t expert_workspace(int dtype, const ExpertArgs &g, bool weights)
     }
     Matrix a, b;
     operands(g, weights, a, b);
-    return copy_bytes(a) + copy_bytes(b);
+    return copy_bytes(a) + copy_bytes(b) + expert_mma_sum_bytes(dtype, g, weights);
+}
+
+// After the copies: the sums of long products, NULL for others.
+static float *sums_at(int dtype, const ExpertArgs &g, bool weights, void *workspace, size_t copies)
+{
+    return expert_mma_sum_bytes(dtype, g, weights)
+               ? reinterpret_cast<float *>(static_cast<char *>(workspace) + copies) : nullptr;
 }
 
 cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, cudaStream_t stream)
@@ -323,6 +330,7 @@ cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, 
     if (dtype == DC_FP32) return use_parts(g, false) ? float_rows(g, workspace, stream) : expert_simt_rows(g, stream);
     Matrix a, b;
     operands(g, false, a, b);
+    float *sums = sums_at(dtype, g, false, workspace, copy_bytes(a) + copy_bytes(b));
     const cudaError_t e = align_rows(a, b, workspace, stream);
     if (e != cudaSuccess) return e;
     ExpertArgs h = g;
@@ -331,7 +339,7 @@ cudaError_t launch_expert_rows(int dtype, const ExpertArgs &g, void *workspace, 
     h.b = b.p;
     h.b_e = b.stride_z;
     (g.b_r == 1 ? h.b_n : h.b_r) = b.stride_y;
-    return expert_mma_rows(dtype, h, stream);
+    return expert_mma_rows(dtype, h, sums, stream);
 }
 
 cudaError_t launch_expert_weights(int dtype, const ExpertArgs &g, void *workspace,
@@ -350,6 +358,7 @@ cudaError_t launch_expert_weights(int dtype, const ExpertArgs &g, void *workspac
     }
     Matrix a, b;
     operands(g, true, a, b);
+    float *sums = sums_at(dtype, g, true, workspace, copy_bytes(a) + copy_bytes(b));
     const cudaError_t e = align_rows(a, b, workspace, stream);
     if (e != cudaSuccess) return e;
     ExpertArgs h = g;
@@ -357,7 +366,7 @@ cudaError_t launch_expert_weights(int dtype, const ExpertArgs &g, void *workspac
     h.a_r = a.stride_y;
     h.b = b.p;
     h.b_r = b.stride_y;
-    return expert_mma_weights(dtype, h, 0, stream);
+    return expert_mma_weights(dtype, h, 0, sums, stream);
 }
 
 }  // namespace dc

@@ -54,7 +54,19 @@ struct MmaArgs {
     int32_t *status;
     bool wide;          // weights: 16-byte stores; rows: 4-byte stores
     int32_t least;      // weights: experts of fewer rows are left to another kernel
+    float *sums;        // long sums: a CTA's tile of the rounds so far (sum_bytes)
 };
+
+// Blocks summed in the tensor cores at a time. They cut a sum off at every step where a float
+// would round, always toward zero: 1e-7 of it a step where the terms share a sign.
+// 16-bit operands: 512 steps lose 5e-5, a tenth of half's rounding, and a million rows in one
+// go 7e-3. So after 128 blocks (8,192 summed elements) a round's sums are added to those before it
+// in floats, rounded: in memory that stays in the L2, since no registers are left at 256 columns,
+// and while the next round is summed. One expert of 65,536 rows x 2,048 x 4,096, dW: 676 us against 671 in one go.
+// Shorter sums are one round. It bounds the wait for a finished round, too.
+constexpr int kRound16 = 128;
+constexpr int64_t kLongSum = int64_t(kRound16) * kBKBytes / 2;
+constexpr int kMostPairs = 80;  // of CTAs whose sums a workspace has room for
 
 struct Tile {
     int32_t e;      // expert
@@ -246,11 +258,10 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     constexpr int kBK = kBKBytes / sizeof(T), kStep = 32 / sizeof(T);  // per stage, per product
     constexpr bool kTf32 = std::is_same<T, float>::value, kOut = MODE == kWeights || MODE == kWeightsK;
     constexpr bool kAMn = MODE == kRowsMN || MODE == kWeights;
-    // Blocks summed in the tensor cores at a time. They cut a sum off at every step where a
-    // float would round, toward zero, some 2e-8 of it: over 192 steps float products came
-    // out 4e-6 off, ten times what sums in floats lose. So the sums of floats are handed over every
-    // 16 steps of hi hi and added up in registers, rounded: 3.5e-7 off.
-    constexpr int kRound = kTf32 ? 4 : 1 << 24;
+    // Floats, whose sums are to lose no more than this: over 192 steps they came out 4e-6 off, ten
+    // times what sums in floats lose. They are handed over every 16 steps of hi hi and added up in
+    // registers, rounded: 3.5e-7 off.
+    constexpr int kRound = kTf32 ? 4 : kRound16;
     constexpr int kParts = kTf32 ? 2 : 1, kSets = kParts;
     constexpr uint32_t kStage = kParts * (kABytes + kBBytes);
     constexpr uint32_t kColumns = 2 * kSets * BN;
@@ -500,16 +511,36 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     all_read();
                 } else {
                     float v[32];
-                    for (int c0 = 0; c0 < q.cols; c0 += 32) {
-                        __syncwarp();
-                        if (blocks > 0) {
-                            bw::tmem_load(at + c0, v);
-                        } else {
+                    if (blocks <= kRound) {
+                        for (int c0 = 0; c0 < q.cols; c0 += 32) {
+                            __syncwarp();
+                            if (blocks > 0) {
+                                bw::tmem_load(at + c0, v);
+                            } else {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                                for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                            }
+                            if (c0 + 32 >= q.cols) all_read();
+                            out(c0, v);
                         }
-                        if (c0 + 32 >= q.cols) all_read();
-                        out(c0, v);
+                    } else {
+                        for (int c0 = 0; c0 < q.cols; c0 += 32) {
+                            // a thread reads what it wrote itself
+                            float *so_far = a.sums + (int64_t(blockIdx.x) * BN + c0) * kBM + warp * 32 + lane;
+                            __syncwarp();
+                            bw::tmem_load(at + c0, v);
+                            if (c0 + 32 >= q.cols) all_read();
+                            if (k0 > 0) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) v[j] += so_far[j * kBM];
+                            }
+                            if (k0 + kRound < blocks) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) so_far[j * kBM] = v[j];
+                            } else {
+                                out(c0, v);
+                            }
+                        }
                     }
                 }
             }
@@ -591,6 +622,7 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
     if (e != cudaSuccess) return e;
     int64_t units = sms / CG;
     if (most_tiles < units) units = most_tiles;
+    if (a.sums && units > kMostPairs) units = kMostPairs;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(unsigned(units * CG));
     lc.blockDim = dim3(kThreads);
@@ -623,10 +655,37 @@ cudaError_t launch_size(int bn, const CUtensorMap &ma, const CUtensorMap &mb, co
                         : launch_typed<T, MODE, 2, 256, 6>(ma, mb, a, tiles, stream);
 }
 
+// Rows (columns of dW) of a tile, and the most tiles that there can be.
+struct Tiles {
+    int bn;
+    int64_t most;
+};
+Tiles tiles_for(int dtype, const ExpertArgs &g, bool weights)
+{
+    Tiles t;
+    if (weights) {
+        const int64_t nm = (g.m + 255) / 256;
+        t.bn = tile_rows(dtype, g.experts * nm * ((g.n + 255) / 256));
+        t.most = g.experts * nm * ((g.n + t.bn - 1) / t.bn);
+    } else {  // the choice by an average expert
+        const int64_t nm = (g.n + 255) / 256, each = (g.rows + g.experts - 1) / g.experts;
+        t.bn = tile_rows(dtype, g.experts * nm * ((each + 255) / 256));
+        t.most = (g.rows / t.bn + g.experts + 2) * nm;
+    }
+    return t;
+}
+
 }  // namespace
 
+size_t expert_mma_sum_bytes(int dtype, const ExpertArgs &g, bool weights)
+{
+    if (dtype == DC_FP32 || (weights ? g.rows : g.r) <= kLongSum) return 0;
+    const Tiles t = tiles_for(dtype, g, weights);
+    return size_t(t.most < kMostPairs ? t.most : kMostPairs) * 2 * kBM * t.bn * sizeof(float);
+}
+
 // Operands on 16-byte boundaries, or tf32 parts, as expert_dispatch.cu makes them.
-cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
+cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, float *sums, cudaStream_t stream)
 {
     const bool k_major = g.b_r == 1;
     const int64_t stride = k_major ? g.b_n : g.b_r;
@@ -634,16 +693,15 @@ cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
     const int64_t inner = k_major ? parts * int64_t(g.r) : g.n, outer = k_major ? g.n : g.r;
     // with one expert the stride between experts is not used, but it has to be valid
     const int64_t expert = g.experts == 1 ? stride * outer : g.b_e;
-    // tiles of an average expert
-    const int64_t nm = (g.n + 255) / 256, each = (g.rows + g.experts - 1) / g.experts;
-    const int bn = tile_rows(dtype, g.experts * nm * ((each + 255) / 256));
+    const Tiles t = tiles_for(dtype, g, false);
+    const int bn = t.bn;
     CUtensorMap ma, mb;
     if (!make_map(ma, dtype, g.b, inner, outer, g.experts, stride, expert, k_major ? 128 : 64) ||
         !make_map(mb, dtype, g.a, parts * int64_t(g.r), g.rows, 1, g.a_m, 0, bn < 128 ? bn / 2 : 64))
         return cudaErrorInvalidValue;
-    MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false, 0};
+    MmaArgs a = {g.c, 0, g.c_m, g.offsets, g.rows, g.experts, g.n, 0, g.r, g.status, false, 0, sums};
     a.wide = g.c_m % 2 == 0 && g.n % 2 == 0 && reinterpret_cast<uintptr_t>(g.c) % 4 == 0;
-    const int64_t tiles = (g.rows / bn + g.experts + 2) * nm;
+    const int64_t tiles = t.most;
     if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;  // more than memory holds
     if (dtype == DC_FP32) return launch_size<float, kRowsK>(bn, ma, mb, a, tiles, stream);
     if (dtype == DC_BF16)
@@ -655,10 +713,10 @@ cudaError_t expert_mma_rows(int dtype, const ExpertArgs &g, cudaStream_t stream)
 
 // Floats: a and b are parts [feature][summed], of stride a_r and b_r, for experts of at least
 // `least` rows.
-cudaError_t expert_mma_weights(int dtype, const ExpertArgs &g, int least, cudaStream_t stream)
+cudaError_t expert_mma_weights(int dtype, const ExpertArgs &g, int least, float *sums, cudaStream_t stream)
 {
-    const int64_t nm = (g.m + 255) / 256;
-    const int bn = tile_rows(dtype, g.experts * nm * ((g.n + 255) / 256));
+    const Tiles t = tiles_for(dtype, g, true);
+    const int bn = t.bn;
     CUtensorMap ma, mb;
     const bool parts = dtype == DC_FP32;
     if (parts ? !make_map(ma, dtype, g.a, g.a_r, g.m, 1, g.a_r, 0, 128) ||
@@ -666,10 +724,10 @@ cudaError_t expert_mma_weights(int dtype, const ExpertArgs &g, int least, cudaSt
               : !make_map(ma, dtype, g.a, g.m, g.rows, 1, g.a_r, 0, 64) ||
                     !make_map(mb, dtype, g.b, g.n, g.rows, 1, g.b_r, 0, 64))
         return cudaErrorInvalidValue;
-    MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false, least};
+    MmaArgs a = {g.c, g.c_e, g.c_m, g.offsets, g.rows, g.experts, g.m, g.n, 0, g.status, false, least, sums};
     const int v = 16 / dtype_bytes(dtype);
     a.wide = g.c_m % v == 0 && g.c_e % v == 0 && aligned16(g.c);
-    const int64_t tiles = int64_t(g.experts) * nm * ((g.n + bn - 1) / bn);
+    const int64_t tiles = t.most;
     if (tiles > (int64_t(1) << 30)) return cudaErrorInvalidValue;
     return parts              ? launch_size<float, kWeightsK>(bn, ma, mb, a, tiles, stream)
            : dtype == DC_BF16 ? launch_size<__nv_bfloat16, kWeights>(bn, ma, mb, a, tiles, stream)

@@ -154,8 +154,10 @@ cudaError_t launch_expert_weights(int dtype, const ExpertArgs &a, void *workspac
 // The kernels behind them: the tensor cores (expert_mma.cu) for 16-bit operands on 16-byte
 // boundaries and floats in tf32 parts, few rows of any type (expert_few.cu), the CUDA cores
 // for small float products (expert_simt.cu; experts of `most` rows or fewer).
-cudaError_t expert_mma_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
-cudaError_t expert_mma_weights(int dtype, const ExpertArgs &a, int least, cudaStream_t stream);
+// sums: expert_mma_sum_bytes for sums too long to stay in the tensor cores.
+size_t expert_mma_sum_bytes(int dtype, const ExpertArgs &a, bool weights);
+cudaError_t expert_mma_rows(int dtype, const ExpertArgs &a, float *sums, cudaStream_t stream);
+cudaError_t expert_mma_weights(int dtype, const ExpertArgs &a, int least, float *sums, cudaStream_t stream);
 cudaError_t expert_few_rows(int dtype, const ExpertArgs &a, cudaStream_t stream);
 cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream);
 cudaError_t expert_simt_weights(const ExpertArgs &a, int64_t most, cudaStream_t stream);

@@ -1,0 +1,93 @@
+"""Sums of the expert products: long ones, whose error must not grow with their length."""
+import math
+
+import pytest
+import torch
+
+import layer_oracle as lo
+from test_gpu_experts import check, normal, offs, operands
+
+pytestmark = pytest.mark.gpu
+HALVES = [torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def ly():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2101_07968_gb300 import build
+    build.build()
+    from paper_2101_07968_gb300 import layers
+    yield layers
+    layers.check_status()
+
+
+def positive(seed, lines, length, dtype, along):
+    """[lines, length] (along 1) or [length, lines] (along 0): terms of one sign, the lines' sums
+    spread over a factor of two, so that their roundings are spread, too."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = torch.rand(lines, length, generator=g, device="cuda") * 0.125
+    t = t * (1 + torch.rand(lines, 1, generator=g, device="cuda"))
+    return (t if along else t.t()).contiguous().to(dtype)
+
+
+# A round of 512 steps of the tensor cores loses at most two units of the last place of the sum so
+# far (its terms are cut off when they are aligned, and the sum is) a step, 2 x 2^-23, while that sum
+# grows evenly: 256 x 2^-22. Adding up 33 rounds, rounded, loses 33 x 2^-24 more.
+LOST = 2.0 ** -14 + 33 * 2.0 ** -24
+
+
+def assert_not_cut_off(got, exact):
+    """Elementwise within LOST and one rounding; on average within LOST and five deviations of the
+    mean of independent roundings, each of at most the type's unit."""
+    u = lo.UNIT[got.dtype]
+    off = (got.double() - exact) / exact
+    assert float(off.abs().max()) <= (1 + u) * (u + LOST)
+    assert abs(float(off.mean())) <= LOST + 5 * u / math.sqrt(3 * off.numel())
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_long_sums_of_one_sign(ly, dtype):
+    """2^18 summed elements: in one go the tensor cores would cut off some 1.7e-3."""
+    n, o = 1 << 18, offs(0, 30, 40)
+    x, w = positive(1, 40, n, dtype, 1), positive(2, 144, n, dtype, 1).view(2, 72, n)
+    y = ly.expert_matmul(x, w, o)
+    dx = ly.expert_matmul_grad_input(x, w.transpose(1, 2), o)  # the same sums, features contiguous or not
+    dx2 = ly.expert_matmul_grad_input(x, w.transpose(1, 2).contiguous(), o)
+    exact = torch.cat([x[:30].double() @ w[0].double().t(), x[30:].double() @ w[1].double().t()])
+    for t in (y, dx, dx2):
+        assert_not_cut_off(t, exact)
+    x, dy = positive(3, 72, n + 5000, dtype, 0), positive(4, 136, n + 5000, dtype, 0)
+    dw = ly.expert_matmul_grad_weight(dy, x, offs(0, 4999, n + 4999))
+    assert_not_cut_off(dw[1], dy[4999:-1].double().t() @ x[4999:-1].double())
+    assert_not_cut_off(dw[0], dy[:4999].double().t() @ x[:4999].double())
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("length", [8192, 8193, 16_384, 24_600])
+def test_sums_around_a_round(ly, dtype, length):
+    """One round, one element more, and several, of all three products."""
+    for rows, N, K, o in ((70, 136, length, (0, 3, 70)), (70, length, 72, (0, 3, 70)),
+                          (2 * length + 9, 136, 72, (5, length + 5, length + 6, 2 * length + 6))):
+        x, w, dy = operands(7, rows, len(o) - 1, N, K, dtype)
+        check(ly, x, w, dy, offs(*o))
+
+
+def test_long_sums_repeat_and_do_not_mix(ly):
+    """More tiles than pairs of SMs, each of several rounds: equal calls give equal bits, and each
+    tile's sums are its own."""
+    rows, N, K = 18_000, 2600, 2300
+    x, w, dy = operands(11, rows, 1, N, K, torch.bfloat16)
+    o = offs(0, rows)
+    dw = ly.expert_matmul_grad_weight(dy, x, o)
+    assert torch.equal(dw, ly.expert_matmul_grad_weight(dy, x, o))
+    exact = dy.double().t() @ x.double()
+    bound = (rows + 2) * lo.EPS * (dy.double().abs().t() @ x.double().abs())
+    lo.assert_within(dw[0], exact.cpu(), bound.cpu(), "dw")
+    x, w = normal(13, 3000, 18_000, dtype=torch.bfloat16), normal(14, 1, 3000, 18_000, dtype=torch.bfloat16)
+    o = offs(0, 3000)
+    y = ly.expert_matmul(x, w, o)
+    assert torch.equal(y, ly.expert_matmul(x, w, o))
+    exact = x.double() @ w[0].double().t()
+    bound = 18_002 * lo.EPS * (x.double().abs() @ w[0].double().abs().t())
+    lo.assert_within(y, exact.cpu(), bound.cpu(), "y")
