@@ -28,6 +28,7 @@
 // the weights' bytes bound it: 128 rows over 24 of 32 experts x 2,048 x 2,048 38 us (5.3 TB/s).
 #include <cuda.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include "blackwell.cuh"
@@ -504,8 +505,11 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
                             for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
                             bw::tmem_load(at + BN + c * 32, v);
+                            // hi hi alone knows an infinity's class: its factor's low part
+                            // may be zero or have the other sign
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                            for (int j = 0; j < 32; ++j)
+                                if (fabsf(sum[c][j]) < INFINITY) sum[c][j] += v[j];
                         }
                     }
                     all_read();

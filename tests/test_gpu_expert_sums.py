@@ -1,4 +1,5 @@
-"""Sums of the expert products: long ones, whose error must not grow with their length."""
+"""Sums of the expert products: long ones, whose error must not grow with their length, and sums
+with infinities among their terms."""
 import math
 
 import pytest
@@ -91,3 +92,43 @@ def test_long_sums_repeat_and_do_not_mix(ly):
     exact = x.double() @ w[0].double().t()
     bound = 18_002 * lo.EPS * (x.double().abs() @ w[0].double().abs().t())
     lo.assert_within(y, exact.cpu(), bound.cpu(), "y")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("rows", [4, 5, 64, 65, 300])
+@pytest.mark.parametrize("depth", [32, 63, 64, 256])
+def test_own_infinities(ly, dtype, rows, depth):
+    """Infinities and NaN among an expert's own operands give the infinities and NaN of the
+    definition, whichever kernel the sizes choose; the other outputs are as without them. Factors
+    of 1, whose low part is zero, and of 0 among them."""
+    x, w, dy = operands(17, rows, 2, depth, depth, dtype)
+    o, edge = offs(0, rows - 1, rows), float("inf")
+    for t in (x, w[0], dy):
+        t[0, :4] = torch.tensor([1.0, 0.0, -1.0, 0.5])
+        t[:, 2] = 1.0
+    plain = lo.expert_products(lo.d64(x), lo.d64(w), lo.d64(dy), o.tolist(), rows)
+    x[1, 3], x[2, 5], x[2, 7] = edge, -edge, float("nan")
+    dy[1, 4], dy[2, 6] = -edge, edge
+    w[0, 1, 2], w[0, 9, 11] = edge, -edge
+    exact = lo.expert_products(lo.d64(x), lo.d64(w), lo.d64(dy), o.tolist(), rows)
+    got = {"y": ly.expert_matmul(x, w, o), "dx": ly.expert_matmul_grad_input(dy, w, o),
+           "dw": ly.expert_matmul_grad_weight(dy, x, o)}
+    for k, t in got.items():
+        want = exact[k][0]
+        assert torch.equal(torch.isnan(lo.d64(t)), torch.isnan(want)), k
+        far = torch.isinf(want)
+        assert torch.equal(lo.d64(t)[far], want[far]), k
+        near = torch.isfinite(want)
+        lo.assert_within(t.cpu()[near], plain[k][0][near], plain[k][1][near], k)
+
+
+def test_floats_whose_products_pass_the_largest(ly):
+    """3e19 x 3e19 is past the largest float: an infinity of its sign, not a NaN."""
+    rows, depth = 300, 256
+    x, w, dy = operands(19, rows, 1, depth, depth, torch.float32)
+    big = 3.1415926e19
+    x[5, 3], w[0, 7, 3], dy[5, 7] = -big, big, big
+    o = offs(0, rows)
+    assert float(ly.expert_matmul(x, w, o)[5, 7]) == -float("inf")
+    assert float(ly.expert_matmul_grad_input(dy, w, o)[5, 3]) == float("inf")
+    assert float(ly.expert_matmul_grad_weight(dy, x, o)[0, 7, 3]) == -float("inf")
