@@ -329,8 +329,9 @@ dc_status dc_schedule_batch_static(int32_t dir, int64_t batch, int32_t L, const 
  * 16-bit operands run on the tensor cores; those whose rows start off 16-byte boundaries
  * are first copied into the workspace, row by row, so that they start on them. Floats go
  * there in two parts of 11 significant bits, whose products are summed as floats (small
- * products of floats run on the CUDA cores); digits below 2^-136 are not seen there, so that a
- * float below 2^-137 counts as zero. Infinities and NaN come out as the definition has them. 16-bit products summed over more than 8,192
+ * products of floats run on the CUDA cores): 1.35e-7 off in the root mean square for 64 summed
+ * elements and 2.4e-7 for 4,096, where a 32-bit sum of one product after another is 1.5e-7 and 11e-7 off.
+ * Digits below 2^-136 are not seen there, so that a float below 2^-137 counts as zero. Infinities and NaN come out as the definition has them. 16-bit products summed over more than 8,192
  * elements are added up from parts of that many, in floats in the workspace. Up to DC_FEW_ROWS rows in all (floats: 16 times
  * as many) take a pass that streams the weights over every SM. workspace: dc_expert_workspace_bytes(shape, product, a,
  * b) bytes, 256-byte aligned, used during the call's kernels only, where product is 0 for

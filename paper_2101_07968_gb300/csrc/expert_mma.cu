@@ -259,13 +259,17 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     constexpr int kBK = kBKBytes / sizeof(T), kStep = 32 / sizeof(T);  // per stage, per product
     constexpr bool kTf32 = std::is_same<T, float>::value, kOut = MODE == kWeights || MODE == kWeightsK;
     constexpr bool kAMn = MODE == kRowsMN || MODE == kWeights;
-    // Floats, whose sums are to lose no more than this: over 192 steps they came out 4e-6 off, ten
-    // times what sums in floats lose. They are handed over every 16 steps of hi hi and added up in
-    // registers, rounded: 3.5e-7 off.
-    constexpr int kRound = kTf32 ? 4 : kRound16;
-    constexpr int kParts = kTf32 ? 2 : 1, kSets = kParts;
+    // Floats, whose sums are to lose no more than sums in floats do: hi hi is handed over every
+    // block of 32 elements, four steps, and added up in registers, rounded; the sums of hi lo and
+    // lo hi, 2^-11 of it, stay until the tile's end. 1.35e-7 off in the root mean square for 64
+    // summed elements, 1.5e-7 for 512, 2.4e-7 for 4,096, where a 32-bit sum of one product after another
+    // is 1.5, 4.1 and 11.5e-7 off. Every 16 steps: 2.0, 3.5 and 3.7e-7, and 540 us against 576 for
+    // 16,384 rows over 8 experts x 2,048 x 2,048.
+    constexpr int kRound = kTf32 ? 1 : kRound16;
+    constexpr int kParts = kTf32 ? 2 : 1;
     constexpr uint32_t kStage = kParts * (kABytes + kBBytes);
-    constexpr uint32_t kColumns = 2 * kSets * BN;
+    // two rounds' sums, one read while the other grows; floats: after them two tiles' sums of hi lo
+    constexpr uint32_t kColumns = 2 * kParts * BN, kCross = 2 * BN;
     extern __shared__ unsigned char dyn[];
     __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
     __shared__ uint32_t tmem_at, gave_up;
@@ -377,7 +381,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     } else if (warp == 5) {
         if (rank == 0 && bw::elect_one()) {  // products
             int s = 0, tile = 0;
-            uint32_t phase = 0;
+            uint32_t phase = 0, cross = tmem + kCross;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
@@ -392,7 +396,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     ok = tile < 2 || bw::bar_wait(bar(&free_[half]), (tile / 2 - 1) & 1, &gave_up);
                     if (!ok) break;
                     bw::fence_after();
-                    const uint32_t d = tmem + half * (kSets * BN);
+                    const uint32_t d = tmem + half * BN;
                     const int k1 = min(blocks, k0 + kRound);
                     for (int kb = k0; kb < k1; ++kb) {
                         ok = bw::bar_wait(bar(&full[s]), phase, &gave_up);
@@ -404,21 +408,22 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         const uint32_t sa = ring + s * kStage;
                         const uint64_t da = bw::operand(sa, kAMn ? kBoxBytes : 16);
                         const uint64_t db = bw::operand(sa + kParts * kABytes, MODE == kWeights ? kBoxBytes : 16);
-                        auto step_of = [&](int i, bool add) {
+                        auto step_of = [&](int i) {
+                            const bool add = i > 0 || kb > k0;
                             if constexpr (kTf32) {
                                 constexpr uint64_t kLowA = kABytes >> 4, kLowB = kBBytes >> 4;
                                 bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, add);
-                                bw::mma_tf32<CG>(d + BN, da + i * 2, db + kLowB + i * 2, shape, add);
-                                bw::mma_tf32<CG>(d + BN, da + kLowA + i * 2, db + i * 2, shape, true);
+                                bw::mma_tf32<CG>(cross, da + i * 2, db + kLowB + i * 2, shape, i > 0 || kb > 0);
+                                bw::mma_tf32<CG>(cross, da + kLowA + i * 2, db + i * 2, shape, true);
                             } else {
                                 bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape, add);
                             }
                         };
                         if (left >= kBK) {  // straight on: a loop's branches would hold the products up
 #pragma unroll
-                            for (int i = 0; i < kBK / kStep; ++i) step_of(i, i > 0 || kb > k0);
+                            for (int i = 0; i < kBK / kStep; ++i) step_of(i);
                         } else {
-                            for (int i = 0; i * kStep < left; ++i) step_of(i, i > 0 || kb > k0);
+                            for (int i = 0; i * kStep < left; ++i) step_of(i);
                         }
                         bw::commit<CG>(bar(&empty[s]));
                         if (++s == STAGES) {
@@ -428,6 +433,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     }
                     if (ok) bw::commit<CG>(bar(&done[half]));
                 }
+                cross ^= (tmem + kCross) ^ (tmem + kCross + BN);
             }
         }
     } else if (warp == 6) {
@@ -459,6 +465,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         }
     } else {  // finished tiles
         int tile = 0;
+        uint32_t cross = kCross;
         bool ok = true;
         for (int t = first; t < tiles && ok; t += step) {
             const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
@@ -489,7 +496,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 bw::fence_after();
-                const uint32_t at = tmem + half * (kSets * BN) + (uint32_t(warp * 32) << 16);
+                const uint32_t lanes = tmem + (uint32_t(warp * 32) << 16), at = lanes + half * BN;
                 auto all_read = [&] {  // the half may be overwritten
                     bw::fence_before();
                     __syncwarp();
@@ -497,20 +504,30 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 };
                 if constexpr (kTf32) {
 #pragma unroll
-                    for (int c = 0; c < kChunks; ++c) {
+                    for (int c = 0; c < kChunks; c += 2) {
                         if (c * 32 < q.cols && blocks > 0) {
-                            float v[32];
+                            float v[64];
                             __syncwarp();
                             bw::tmem_load(at + c * 32, v);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-                            bw::tmem_load(at + BN + c * 32, v);
-                            // hi hi alone knows an infinity's class: its factor's low part
-                            // may be zero or have the other sign
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (fabsf(sum[c][j]) < INFINITY) sum[c][j] += v[j];
+                            for (int j = 0; j < 64; ++j) sum[c + j / 32][j % 32] += v[j];
                         }
+                    }
+                    if (k0 + kRound >= blocks) {
+                        // hi hi alone knows an infinity's class: its factor's low part may be
+                        // zero or have the other sign
+#pragma unroll
+                        for (int c = 0; c < kChunks; ++c) {
+                            if (c * 32 < q.cols && blocks > 0) {
+                                float v[32];
+                                __syncwarp();
+                                bw::tmem_load(lanes + cross + c * 32, v);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (fabsf(sum[c][j]) < INFINITY) sum[c][j] += v[j];
+                            }
+                        }
+                        cross ^= kCross ^ (kCross + BN);
                     }
                     all_read();
                 } else {

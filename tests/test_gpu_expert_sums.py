@@ -1,5 +1,5 @@
-"""Sums of the expert products: long ones, whose error must not grow with their length, and sums
-with infinities among their terms."""
+"""Sums of the expert products: long ones, whose error must not grow with their length, sums of
+floats against plain 32-bit ones, and sums with infinities among their terms."""
 import math
 
 import pytest
@@ -132,3 +132,21 @@ def test_floats_whose_products_pass_the_largest(ly):
     assert float(ly.expert_matmul(x, w, o)[5, 7]) == -float("inf")
     assert float(ly.expert_matmul_grad_input(dy, w, o)[5, 3]) == float("inf")
     assert float(ly.expert_matmul_grad_weight(dy, x, o)[0, 7, 3]) == -float("inf")
+
+
+@pytest.mark.parametrize("depth,sign", [(64, "both"), *[(d, s) for d in (96, 128, 200, 512, 2048) for s in ("both", "one")]])
+def test_floats_lose_no_more_than_a_sum_in_floats(ly, depth, sign):
+    """The root mean square error of float products in parts is below that of a 32-bit sum of one
+    product after another, on the same operands; of one sign, from 96 summed elements on."""
+    g = torch.Generator(device="cuda").manual_seed(depth)
+    draw = torch.randn if sign == "both" else torch.rand
+    a, b = (draw(512, depth, generator=g, device="cuda") for _ in range(2))
+    exact = a.double() @ b.double().t()
+    plain = torch.zeros(512, 512, device="cuda")
+    for k in range(depth):
+        plain = torch.addcmul(plain, a[:, k:k + 1], b[:, k][None])
+    off = lambda t: float((t.double() - exact).norm() / exact.norm())
+    o = offs(0, 512)
+    for got in (ly.expert_matmul(a, b[None], o), ly.expert_matmul_grad_input(a, b.t()[None].contiguous(), o),
+                ly.expert_matmul_grad_weight(a.t().contiguous(), b.t().contiguous(), offs(0, depth))[0]):
+        assert off(got) <= off(plain), (off(got), off(plain))
