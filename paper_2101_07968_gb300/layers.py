@@ -18,6 +18,7 @@ The operations are defined in include/dynacomm.h.
 from __future__ import annotations
 
 import ctypes
+import threading
 
 import torch
 
@@ -100,24 +101,39 @@ def _used_on(ws, stream):
 
 
 # ------------------------------------------------------------------- expert products
-_status = {}
+_status = {}  # per device: the word that kernels report to, and its address
+_status_lock = threading.Lock()
 
 
 def _status_of(device):
     at = _status.get(device)
     if at is None:
-        t = torch.zeros(1, dtype=torch.int32, device=f"cuda:{device}")
-        at = _status[device] = (t, t.data_ptr())
+        with _status_lock, torch.cuda.device(device):
+            at = _status.get(device)
+            if at is None:
+                # its fill must be done before a kernel of any stream, and be part of no graph,
+                # whose replays would clear what other calls reported
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("the first expert product on a device cannot be captured: "
+                                       "call one of them, or check_status(), before the capture")
+                t = torch.zeros(1, dtype=torch.int32, device=f"cuda:{device}")
+                torch.cuda.current_stream().synchronize()
+                at = _status[device] = (t, t.data_ptr())
     return at[1]
 
 
 def check_status() -> None:
-    """Synchronises and raises DynaCommError if a kernel of this module has given up a wait
-    (a bug of the library or a fault of the machine; the call's outputs are incomplete)."""
-    for device, (t, _) in _status.items():
+    """Waits for everything on the devices that expert products have run on (and the current
+    one) and raises DynaCommError if a kernel of this module has given up a wait (a bug of the
+    library or a fault of the machine; the call's outputs are incomplete)."""
+    if torch.cuda.is_available():
+        _status_of(torch.cuda.current_device())
+    for device, (t, _) in list(_status.items()):
+        torch.cuda.synchronize(device)
         s = int(t.item())
         if s:
             t.zero_()
+            torch.cuda.synchronize(device)
             raise dc.DynaCommError(s, f"layer operators on cuda:{device}")
 
 
