@@ -6,7 +6,8 @@ language models, forward and backward, whose times can be measured on this GPU
 with torch, checks its arguments (ValueError) and launches the library's kernels on torch's
 current CUDA stream or ``stream``; nothing synchronises. A caller that uses tensors on
 another stream than their own orders the streams and keeps the tensors alive, as with any
-kernel launch.
+kernel launch. No function builds an autograd graph: a tensor that requires a gradient is
+refused unless gradients are off (torch.no_grad()).
 
 * ``expert_matmul``, ``expert_matmul_grad_input``, ``expert_matmul_grad_weight``
 * ``gated_unit``, ``gated_unit_grad``
@@ -42,6 +43,16 @@ def _like(name, t, ref, shape):
     if t.dtype is not ref.dtype or t.shape != shape or t.get_device() != ref.get_device():
         raise ValueError(f"{name}: {tuple(shape)} {ref.dtype} on {ref.device} expected, not "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _no_graph(*tensors):
+    """Outputs carry no autograd graph, so a gradient that is asked for would be lost."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("a tensor requires a gradient, and the layer operators build no autograd graph: "
+                                 "call them under torch.no_grad() or on detached tensors, and their gradients "
+                                 "by the ..._grad functions")
 
 
 def _rows(name, t) -> int:
@@ -168,6 +179,7 @@ _PRODUCTS = ("dc_expert_matmul", "dc_expert_matmul_grad_input", "dc_expert_matmu
 
 
 def _product(which, shape, a, b, offsets, c, stream):
+    _no_graph(a, b)
     ap, bp = a.data_ptr(), b.data_ptr()
     # few rows need none in any case
     few = which < 2 and a.shape[0] <= dc.DC_FEW_ROWS
@@ -229,6 +241,7 @@ def gated_unit(h, act="silu", stream=None):
     R, F2 = h.shape
     if F2 % 2:
         raise ValueError("h: an even number of columns expected")
+    _no_graph(h)
     a = _empty((R, F2 // 2), dtype=h.dtype, device=h.device)
     _run("dc_gated_unit", h, stream, _dtype(h), _act(act), R, F2 // 2, h.data_ptr(), ldh,
          a.data_ptr(), F2 // 2)
@@ -242,6 +255,7 @@ def gated_unit_grad(da, h, act="silu", stream=None):
     if F2 % 2:
         raise ValueError("h: an even number of columns expected")
     _like("da", da, h, (R, F2 // 2))
+    _no_graph(da, h)
     dh = _empty((R, F2), dtype=h.dtype, device=h.device)
     _run("dc_gated_unit_grad", h, stream, _dtype(h), _act(act), R, F2 // 2, da.data_ptr(), ldda,
          h.data_ptr(), ldh, dh.data_ptr(), F2)
@@ -263,6 +277,7 @@ def dropout(x, p, seed, offset=0, residual=None, stream=None):
     if residual is not None:
         ldr, res = _rows("residual", residual), residual.data_ptr()
         _like("residual", residual, x, (R, C))
+    _no_graph(x, residual)
     y = _empty((R, C), dtype=x.dtype, device=x.device)
     _run("dc_dropout", x, stream, _dtype(x), R, C, x.data_ptr(), ldx, res, ldr, y.data_ptr(), C,
          p, int(seed), int(offset))
@@ -294,6 +309,7 @@ def _norm_operands(x, f, gate, w_post, w_pre, rows_per_gate):
         raise ValueError("device tensor expected (the library takes device pointers)")
     if x.dim() != 2:
         raise ValueError("x or y: two dimensions expected")
+    _no_graph(x, f, gate, w_post, w_pre)
     R, D = shape = x.shape
     if rows_per_gate is not None and rows_per_gate < 1:
         raise ValueError("rows_per_gate: at least one expected")
@@ -328,6 +344,7 @@ def block_norm_grad(dy, dh, y, f=None, gate=None, w_post=None, w_pre=None, resid
     (either may be None: dy zero, dh for a call without h); y: the call's output (x where f was
     None)."""
     yp, fp, gp, pp, ep = _norm_operands(y, f, gate, w_post, w_pre, rows_per_gate)
+    _no_graph(dy, dh)
     dyp, dhp = _contiguous("dy", dy, y, y.shape), _contiguous("dh", dh, y, y.shape)
     if dh is None and (dy is None or f is None):
         raise ValueError("dh expected, or dy and f")
