@@ -3,8 +3,8 @@
 The schedule of an iteration needs each layer's forward and backward compute time and the
 size of what is pulled and pushed for it (Sec. IV-A). Here the layers are the blocks of a
 language model's feed-forward chain, run by the layer operators: ``ExpertChain`` computes
-forward and backward, ``measure`` takes their times with CUDA events, and ``schedules`` solves
-the chain for many links at once.
+forward and backward, ``measure`` takes their times on the GPU with CUDA events, and
+``schedules`` solves the chain for many links at once.
 
     python -m paper_2101_07968_gb300.expert_chain [--layers 12] [--rows 8192] [--links 10000]
 
@@ -111,20 +111,24 @@ class ExpertChain:
 
 
 def measure(chain, x, assigned, dy, steps=5, warmup=2):
-    """Forward and backward time of every block in whole microseconds, rounded up: the mean of
-    `steps` iterations between CUDA events."""
+    """Forward and backward time of every block on the GPU in whole microseconds, rounded up: the
+    mean of `steps` iterations between CUDA events, after `warmup` (at least one). The iteration
+    and its events are captured once as a CUDA graph and replayed, so that the times are the
+    kernels' and not those of the host's calls, some 120 us for a block's forward."""
     L = len(chain.blocks)
+    for _ in range(max(warmup, 1)):
+        chain.step(x, assigned, dy)
+    torch.cuda.synchronize()
+    ev = {what: [torch.cuda.Event(enable_timing=True, external=True) for _ in range(L + 1)]
+          for what in ("forward", "backward")}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain.step(x, assigned, dy, lambda what, i: ev[what][i].record())
     total = {"forward": [0.0] * L, "backward": [0.0] * L}
-    for k in range(warmup + steps):
-        ev = {"forward": [None] * (L + 1), "backward": [None] * (L + 1)}
-
-        def mark(what, i):
-            ev[what][i] = torch.cuda.Event(enable_timing=True)
-            ev[what][i].record()
-        chain.step(x, assigned, dy, mark)
+    graph.replay()
+    for _ in range(steps):
+        graph.replay()
         torch.cuda.synchronize()
-        if k < warmup:
-            continue
         for i in range(L):
             total["forward"][i] += ev["forward"][i].elapsed_time(ev["forward"][i + 1])
             total["backward"][i] += ev["backward"][i + 1].elapsed_time(ev["backward"][i])
