@@ -113,39 +113,23 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 
 // --------------------------------------------------------------------------- copies
 // Boxes of a tensor map into this CTA's shared memory; the bytes are counted on `bar`, a
-// barrier of this CTA or (PAIR) of either CTA of a pair.
-template <bool PAIR>
+// barrier of either CTA of the pair.
 __device__ __forceinline__ void copy_2d(uint32_t dst, const void *map, int x, int y, uint32_t bar)
 {
-    if (PAIR)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
-            "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-            "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+        "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
 }
-template <bool PAIR>
 __device__ __forceinline__ void copy_3d(uint32_t dst, const void *map, int x, int y, int z,
                                         uint32_t bar)
 {
-    if (PAIR)
-        asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
-            "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-            "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-            : "memory");
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
 }
 // n bytes (a multiple of 16, both addresses on 16-byte boundaries)
 __device__ __forceinline__ void copy_bytes(uint32_t dst, const void *src, uint32_t n, uint32_t bar)
@@ -166,24 +150,15 @@ __device__ __forceinline__ void fence_async()
 }
 
 // -------------------------------------------------------------------- tensor memory
-template <int CG>
+// of both CTAs of a pair, by a warp of each
 __device__ __forceinline__ void tmem_alloc(uint32_t out, uint32_t columns)
 {
-    if (CG == 2) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(out), "r"(columns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(out), "r"(columns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(out), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
 }
-template <int CG>
 __device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns)
 {
-    if (CG == 2)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
-    else
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -257,45 +232,31 @@ __device__ __forceinline__ uint32_t tf32_shape(uint32_t m, uint32_t n)
 {
     return 1u << 4 | 2u << 7 | 2u << 10 | (n >> 3) << 17 | (m >> 4) << 24;
 }
-template <int CG>
+// Products of a pair of CTAs, by a thread of its first.
 __device__ __forceinline__ void mma_tf32(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {
-    static_assert(CG == 2, "");
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::2.kind::tf32 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(shape), "r"(uint32_t(add))
         : "memory");
 }
-template <int CG>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {
-    if (CG == 2)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-            "l"(a), "l"(b), "r"(shape), "r"(uint32_t(add))
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-            "l"(a), "l"(b), "r"(shape), "r"(uint32_t(add))
-            : "memory");
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(shape), "r"(uint32_t(add))
+        : "memory");
 }
-// An arrival on `bar` (of both CTAs of a pair) once this thread's products are done.
-template <int CG>
+// An arrival on `bar` of both CTAs once this thread's products are done.
 __device__ __forceinline__ void commit(uint32_t bar)
 {
-    if (CG == 2)
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-                bar),
-            "h"(uint16_t(3))
-            : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-                     : "memory");
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            bar),
+        "h"(uint16_t(3))
+        : "memory");
 }
 
 }  // namespace bw

@@ -38,6 +38,7 @@ namespace dc {
 namespace {
 
 constexpr int kBKBytes = 128;            // summed axis per stage: a line
+constexpr int kPair = 2;                 // CTAs that share a tile
 constexpr int kBM = 128;                 // features per CTA
 constexpr int kThreads = 7 * 32;
 constexpr uint32_t kABytes = kBM * kBKBytes;
@@ -77,15 +78,15 @@ struct Tile {
     int32_t r0, r;  // summed axis: start (weights) and extent
 };
 
-template <int MODE, int CG, int BN>
+template <int MODE, int BN>
 __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, int t)
 {
     Tile q;
     if (MODE == kWeights || MODE == kWeightsK) {
-        const int nm = (a.m + kBM * CG - 1) / (kBM * CG), nn = (a.n + BN - 1) / BN;
+        const int nm = (a.m + kBM * kPair - 1) / (kBM * kPair), nn = (a.n + BN - 1) / BN;
         q.e = t / (nm * nn);
         const int i = t - q.e * (nm * nn);
-        q.m0 = (i % nm) * (kBM * CG);
+        q.m0 = (i % nm) * (kBM * kPair);
         q.n0 = (i / nm) * BN;
         q.cols = min(BN, a.n - q.n0);
         q.r0 = seg.start[q.e + 1];
@@ -96,7 +97,7 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
             q.r = kPartRows * (seg.tile[q.e + 2] - seg.tile[q.e + 1]);
         }
     } else {
-        const int nm = (a.m + kBM * CG - 1) / (kBM * CG);
+        const int nm = (a.m + kBM * kPair - 1) / (kBM * kPair);
         const int whole = seg.tile[seg.count];
         const int s = find_segment(t < whole ? seg.tile : seg.part, seg.count, t);
         const int size = seg.start[s + 1] - seg.start[s];
@@ -104,7 +105,7 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
         const int i = t < whole ? t - seg.tile[s] : t - seg.part[s] + size / BN * nm;
         const bool none = s == 0 || s == seg.count - 1;
         q.e = none ? 0 : s - 1;
-        q.m0 = (i % nm) * (kBM * CG);
+        q.m0 = (i % nm) * (kBM * kPair);
         q.n0 = seg.start[s] + (i / nm) * BN;
         q.cols = min(BN, seg.start[s + 1] - q.n0);
         q.r0 = 0;
@@ -114,14 +115,14 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs &a, const Segments &seg, i
 }
 
 // Rows (MN-major: columns, in whole lines) of B that a CTA's stage holds.
-template <int MODE, int CG, int BN>
-constexpr int kStageRows = MODE == kWeights && BN / CG < 64 ? 64 : BN / CG;
+template <int MODE, int BN>
+constexpr int kStageRows = MODE == kWeights && BN / kPair < 64 ? 64 : BN / kPair;
 
-template <int MODE, int CG, int BN>
+template <int MODE, int BN>
 __device__ __forceinline__ int tile_count(const MmaArgs &a, const Segments &seg)
 {
     if (MODE == kWeights || MODE == kWeightsK)
-        return a.experts * ((a.m + kBM * CG - 1) / (kBM * CG)) * ((a.n + BN - 1) / BN);
+        return a.experts * ((a.m + kBM * kPair - 1) / (kBM * kPair)) * ((a.n + BN - 1) / BN);
     return seg.part[seg.count];
 }
 
@@ -247,15 +248,15 @@ __device__ __forceinline__ void store_lines(const Lines &s, const MmaArgs &a, co
     __syncwarp();
 }
 
-template <typename T, int MODE, int CG, int BN, int STAGES>
+template <typename T, int MODE, int BN, int STAGES>
 __global__ void __launch_bounds__(kThreads, 1)
 expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                   const MmaArgs a)
 {
     // B: boxes of up to 64 rows, or (MN-major) of 64 columns
-    constexpr int kBoxRows = MODE == kWeights || BN / CG > 64 ? 64 : BN / CG;
+    constexpr int kBoxRows = MODE == kWeights || BN / kPair > 64 ? 64 : BN / kPair;
     constexpr uint32_t kBBox = kBoxRows * kBKBytes;
-    constexpr uint32_t kBBytes = kStageRows<MODE, CG, BN> * kBKBytes;
+    constexpr uint32_t kBBytes = kStageRows<MODE, BN> * kBKBytes;
     constexpr int kBK = kBKBytes / sizeof(T), kStep = 32 / sizeof(T);  // per stage, per product
     constexpr bool kTf32 = std::is_same<T, float>::value, kOut = MODE == kWeights || MODE == kWeightsK;
     constexpr bool kAMn = MODE == kRowsMN || MODE == kWeights;
@@ -276,40 +277,40 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     __shared__ alignas(16) Lines lines[kOut ? 4 : 1];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? bw::cluster_rank() : 0;
+    const uint32_t rank = bw::cluster_rank();
     const uint32_t ring = (bw::smem_addr(dyn) + 1023u) & ~1023u;
     const Segments seg = segments_at(dyn + (ring - bw::smem_addr(dyn)) + STAGES * kStage, a.experts);
     auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
-    auto lead = [&](uint64_t *b) { return CG == 2 ? bw::map_to(bw::smem_addr(b), 0) : bw::smem_addr(b); };
+    auto lead = [&](uint64_t *b) { return bw::map_to(bw::smem_addr(b), 0); };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
-            bw::bar_init(bar(&full[i]), CG);
+            bw::bar_init(bar(&full[i]), kPair);
             bw::bar_init(bar(&empty[i]), 1);
             bw::bar_init(bar(&tail[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             bw::bar_init(bar(&done[i]), 1);
-            bw::bar_init(bar(&free_[i]), 4 * CG);
+            bw::bar_init(bar(&free_[i]), 4 * kPair);
         }
         gave_up = 0;
         bw::bar_init_fence();
     }
-    if (warp == 5) bw::tmem_alloc<CG>(bw::smem_addr(&tmem_at), kColumns);
+    if (warp == 5) bw::tmem_alloc(bw::smem_addr(&tmem_at), kColumns);
     if (warp == 4 && lane == 0) {
         bw::prefetch_map(&map_a);
         bw::prefetch_map(&map_b);
     }
     if (warp == 0)
         build_segments<MODE != kWeightsK>(seg, a.offsets, a.rows, a.experts, MODE == kWeightsK ? kPartRows : BN,
-                       MODE == kWeightsK ? 1 : (a.m + kBM * CG - 1) / (kBM * CG));
+                       MODE == kWeightsK ? 1 : (a.m + kBM * kPair - 1) / (kBM * kPair));
     bw::fence_before();
     __syncthreads();
-    if (CG == 2) bw::cluster_sync();
+    bw::cluster_sync();
     bw::fence_after();
     const uint32_t tmem = tmem_at;
-    const int tiles = tile_count<MODE, CG, BN>(a, seg);
-    const int step = int(gridDim.x) / CG, first = int(blockIdx.x) / CG;
+    const int tiles = tile_count<MODE, BN>(a, seg);
+    const int step = int(gridDim.x) / kPair, first = int(blockIdx.x) / kPair;
 
     if (warp == 4) {
         if (bw::elect_one()) {  // copies
@@ -318,9 +319,9 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             bool ok = true;
             const uint32_t full0 = lead(&full[0]);
             for (int t = first; t < tiles && ok; t += step) {
-                const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                const Tile q = tile_at<MODE, BN>(a, seg, t);
                 if (MODE == kWeightsK && q.cols == 0) continue;
-                const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;  // of this CTA
+                const int cols = (q.cols + 16 * kPair - 1) / (16 * kPair) * 16;  // of this CTA
                 const int boxes = (cols + kBoxRows - 1) / kBoxRows;
                 const int m = q.m0 + int(rank) * kBM, n = q.n0 + int(rank) * cols;
                 const uint32_t bytes = kParts * (kABytes + boxes * kBBox);
@@ -336,34 +337,34 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     if (zeros) {
                         bw::bar_arrive_bytes(b, bytes);
                     } else if (rank == 0) {  // for both CTAs: the other's bytes count here too
-                        bw::bar_arrive_bytes(bar(&full[s]), bytes * CG);
-                        if (CG == 2) bw::bar_arrive(bar(&full[s]));
+                        bw::bar_arrive_bytes(bar(&full[s]), bytes * kPair);
+                        bw::bar_arrive(bar(&full[s]));
                     }
                     if (kTf32) {  // both parts of both operands
 #pragma unroll
                         for (int part = 0; part < kParts; ++part) {
                             const int x = r + part * q.r;
                             if (MODE == kWeightsK)
-                                bw::copy_2d<CG == 2>(sa + part * kABytes, &map_a, x, m, b);
+                                bw::copy_2d(sa + part * kABytes, &map_a, x, m, b);
                             else
-                                bw::copy_3d<CG == 2>(sa + part * kABytes, &map_a, x, m, q.e, b);
+                                bw::copy_3d(sa + part * kABytes, &map_a, x, m, q.e, b);
                             for (int i = 0; i < boxes; ++i)
-                                bw::copy_2d<CG == 2>(sb + part * kBBytes + i * kBBox, &map_b, x, n + kBoxRows * i, b);
+                                bw::copy_2d(sb + part * kBBytes + i * kBBox, &map_b, x, n + kBoxRows * i, b);
                         }
                     } else if (MODE == kRowsK) {
-                        bw::copy_3d<CG == 2>(sa, &map_a, r, m, q.e, b);
+                        bw::copy_3d(sa, &map_a, r, m, q.e, b);
                     } else if (MODE == kRowsMN) {
-                        bw::copy_3d<CG == 2>(sa, &map_a, m, r, q.e, b);
-                        bw::copy_3d<CG == 2>(sa + kBoxBytes, &map_a, m + 64, r, q.e, b);
+                        bw::copy_3d(sa, &map_a, m, r, q.e, b);
+                        bw::copy_3d(sa + kBoxBytes, &map_a, m + 64, r, q.e, b);
                     } else {
-                        bw::copy_2d<CG == 2>(sa, &map_a, m, r, b);
-                        bw::copy_2d<CG == 2>(sa + kBoxBytes, &map_a, m + 64, r, b);
+                        bw::copy_2d(sa, &map_a, m, r, b);
+                        bw::copy_2d(sa + kBoxBytes, &map_a, m + 64, r, b);
                     }
                     for (int i = 0; i < boxes && !kTf32; ++i)
                         if (MODE == kWeights)
-                            bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, n + kBoxRows * i, r, b);
+                            bw::copy_2d(sb + i * kBBox, &map_b, n + kBoxRows * i, r, b);
                         else
-                            bw::copy_2d<CG == 2>(sb + i * kBBox, &map_b, r, n + kBoxRows * i, b);
+                            bw::copy_2d(sb + i * kBBox, &map_b, r, n + kBoxRows * i, b);
                     if (++s == STAGES) {
                         s = 0;
                         phase ^= 1;
@@ -384,12 +385,12 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             uint32_t phase = 0, cross = tmem + kCross;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
-                const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+                const Tile q = tile_at<MODE, BN>(a, seg, t);
                 if (MODE == kWeightsK && q.cols == 0) continue;
-                const uint32_t n = (q.cols + 16 * CG - 1) / (16 * CG) * (16 * CG);
+                const uint32_t n = (q.cols + 16 * kPair - 1) / (16 * kPair) * (16 * kPair);
                 const uint32_t shape =
-                    kTf32 ? bw::tf32_shape(kBM * CG, n)
-                          : bw::f16_shape(std::is_same<T, __nv_bfloat16>::value, kAMn, MODE == kWeights, kBM * CG, n);
+                    kTf32 ? bw::tf32_shape(kBM * kPair, n)
+                          : bw::f16_shape(std::is_same<T, __nv_bfloat16>::value, kAMn, MODE == kWeights, kBM * kPair, n);
                 const int blocks = (q.r + kBK - 1) / kBK;
                 for (int k0 = 0; (k0 == 0 || k0 < blocks) && ok; k0 += kRound, ++tile) {
                     const int half = tile & 1;
@@ -402,7 +403,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         ok = bw::bar_wait(bar(&full[s]), phase, &gave_up);
                         if (!ok) break;
                         const int left = q.r - kb * kBK;
-                        if (CG == 2 && MODE == kWeights && left <= kBK && (left & 15))
+                        if (MODE == kWeights && left <= kBK && (left & 15))
                             bw::fence_cluster();  // the other CTA's zeros
                         bw::fence_after();
                         const uint32_t sa = ring + s * kStage;
@@ -412,11 +413,11 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             const bool add = i > 0 || kb > k0;
                             if constexpr (kTf32) {
                                 constexpr uint64_t kLowA = kABytes >> 4, kLowB = kBBytes >> 4;
-                                bw::mma_tf32<CG>(d, da + i * 2, db + i * 2, shape, add);
-                                bw::mma_tf32<CG>(cross, da + i * 2, db + kLowB + i * 2, shape, i > 0 || kb > 0);
-                                bw::mma_tf32<CG>(cross, da + kLowA + i * 2, db + i * 2, shape, true);
+                                bw::mma_tf32(d, da + i * 2, db + i * 2, shape, add);
+                                bw::mma_tf32(cross, da + i * 2, db + kLowB + i * 2, shape, i > 0 || kb > 0);
+                                bw::mma_tf32(cross, da + kLowA + i * 2, db + i * 2, shape, true);
                             } else {
-                                bw::mma<CG>(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape, add);
+                                bw::mma(d, da + i * (kAMn ? 128 : 2), db + i * (MODE == kWeights ? 128 : 2), shape, add);
                             }
                         };
                         if (left >= kBK) {  // straight on: a loop's branches would hold the products up
@@ -425,13 +426,13 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         } else {
                             for (int i = 0; i * kStep < left; ++i) step_of(i);
                         }
-                        bw::commit<CG>(bar(&empty[s]));
+                        bw::commit(bar(&empty[s]));
                         if (++s == STAGES) {
                             s = 0;
                             phase ^= 1;
                         }
                     }
-                    if (ok) bw::commit<CG>(bar(&done[half]));
+                    if (ok) bw::commit(bar(&done[half]));
                 }
                 cross ^= (tmem + kCross) ^ (tmem + kCross + BN);
             }
@@ -441,8 +442,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             int it = 0;
             uint32_t uses = 0;  // parity of each stage's tail barrier
             for (int t = first; t < tiles; t += step) {
-                const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
-                if (MODE == kWeightsK && q.cols == 0) continue;
+                const Tile q = tile_at<MODE, BN>(a, seg, t);
                 const int blocks = (q.r + kBK - 1) / kBK;
                 it += blocks;
                 if ((q.r & 15) == 0) continue;
@@ -450,7 +450,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 bool ok = bw::bar_wait(bar(&tail[s]), (uses >> s) & 1, &gave_up);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 uses ^= 1u << s;
-                const int cols = (q.cols + 16 * CG - 1) / (16 * CG) * 16;
+                const int cols = (q.cols + 16 * kPair - 1) / (16 * kPair) * 16;
                 const int boxes = 2 + (cols + 63) / 64;  // A's two come first
                 const int r = (q.r - 1) % kBK + 1, lines = (r + 15) / 16 * 16 - r;
                 unsigned char *at = dyn + (ring - bw::smem_addr(dyn)) + s * kStage + r * 128;
@@ -468,7 +468,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         uint32_t cross = kCross;
         bool ok = true;
         for (int t = first; t < tiles && ok; t += step) {
-            const Tile q = tile_at<MODE, CG, BN>(a, seg, t);
+            const Tile q = tile_at<MODE, BN>(a, seg, t);
             if (MODE == kWeightsK && q.cols == 0) continue;
             const int feature = q.m0 + int(rank) * kBM + warp * 32 + lane;
             const int blocks = (q.r + kBK - 1) / kBK;
@@ -582,8 +582,8 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     }
     bw::fence_before();
     __syncthreads();
-    if (CG == 2) bw::cluster_sync();
-    if (warp == 5) bw::tmem_free<CG>(tmem, kColumns);
+    bw::cluster_sync();
+    if (warp == 5) bw::tmem_free(tmem, kColumns);
 }
 
 // ------------------------------------------------------------------------------ host
@@ -625,12 +625,12 @@ bool make_map(CUtensorMap &map, int dtype, const void *base, int64_t x, int64_t 
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int MODE, int CG, int BN, int STAGES>
+template <typename T, int MODE, int BN, int STAGES>
 cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const MmaArgs &a,
                          int64_t most_tiles, cudaStream_t stream)
 {
-        auto kernel = expert_mma_kernel<T, MODE, CG, BN, STAGES>;
-    constexpr size_t ring = size_t(STAGES) * (std::is_same<T, float>::value ? 2 : 1) * (kABytes + kStageRows<MODE, CG, BN> * kBKBytes) + 1024;
+    auto kernel = expert_mma_kernel<T, MODE, BN, STAGES>;
+    constexpr size_t ring = size_t(STAGES) * (std::is_same<T, float>::value ? 2 : 1) * (kABytes + kStageRows<MODE, BN> * kBKBytes) + 1024;
     const size_t smem = ring + segments_bytes(a.experts);
     static DeviceCache cache;
     int ready = 0, sms = 0;
@@ -641,17 +641,17 @@ cudaError_t launch_typed(const CUtensorMap &ma, const CUtensorMap &mb, const Mma
     });
     if (e == cudaSuccess) e = sm_count(sms);
     if (e != cudaSuccess) return e;
-    int64_t units = sms / CG;
+    int64_t units = sms / kPair;
     if (most_tiles < units) units = most_tiles;
     if (a.sums && units > kMostPairs) units = kMostPairs;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(unsigned(units * CG));
+    lc.gridDim = dim3(unsigned(units * kPair));
     lc.blockDim = dim3(kThreads);
     lc.dynamicSmemBytes = smem;
     lc.stream = stream;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.x = kPair;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     lc.attrs = at;
     lc.numAttrs = 1;
@@ -669,11 +669,11 @@ cudaError_t launch_size(int bn, const CUtensorMap &ma, const CUtensorMap &mb, co
                         cudaStream_t stream)
 {
     if constexpr (std::is_same<T, float>::value)  // 128 sums a thread of the four warps that add up the rounds
-        return bn == 64 ? launch_typed<T, MODE, 2, 64, 4>(ma, mb, a, tiles, stream)
-                        : launch_typed<T, MODE, 2, 128, 4>(ma, mb, a, tiles, stream);
+        return bn == 64 ? launch_typed<T, MODE, 64, 4>(ma, mb, a, tiles, stream)
+                        : launch_typed<T, MODE, 128, 4>(ma, mb, a, tiles, stream);
     else
-        return bn == 64 ? launch_typed<T, MODE, 2, 64, 8>(ma, mb, a, tiles, stream)
-                        : launch_typed<T, MODE, 2, 256, 6>(ma, mb, a, tiles, stream);
+        return bn == 64 ? launch_typed<T, MODE, 64, 8>(ma, mb, a, tiles, stream)
+                        : launch_typed<T, MODE, 256, 6>(ma, mb, a, tiles, stream);
 }
 
 // Rows (columns of dW) of a tile, and the most tiles that there can be.

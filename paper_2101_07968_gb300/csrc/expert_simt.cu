@@ -9,20 +9,19 @@ namespace {
 constexpr int kTile = 64, kDepth = 16, kThreads = 256;
 
 // Stages [kTile rows][kDepth] of a strided matrix, transposed: s[depth][row].
-template <typename T>
-__device__ __forceinline__ void stage(float (&s)[kDepth][kTile + 1], const T *p, int64_t s_row,
+__device__ __forceinline__ void stage(float (&s)[kDepth][kTile + 1], const float *p, int64_t s_row,
                                       int64_t s_dep, int rows, int depth, bool depth_first)
 {
     for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
         const int row = depth_first ? i / kDepth : i % kTile;
         const int dep = depth_first ? i % kDepth : i / kTile;
-        s[dep][row] = row < rows && dep < depth ? to_float(p[row * s_row + dep * s_dep]) : 0.0f;
+        s[dep][row] = row < rows && dep < depth ? p[row * s_row + dep * s_dep] : 0.0f;
     }
 }
 
 // WEIGHTS false: the block's tile of rows times the expert's matrix. true: the expert's
 // rows are what is summed over.
-template <typename T, bool WEIGHTS>
+template <bool WEIGHTS>
 __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int64_t most)
 {
     extern __shared__ int32_t dyn[];
@@ -32,8 +31,8 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int
     __syncthreads();
     int e, rows;
     int64_t depth;
-    const T *a = static_cast<const T *>(g.a), *b = static_cast<const T *>(g.b);
-    T *c = static_cast<T *>(g.c);
+    const float *a = static_cast<const float *>(g.a), *b = static_cast<const float *>(g.b);
+    float *c = static_cast<float *>(g.c);
     const int n0 = blockIdx.x * kTile;
     if (WEIGHTS) {
         e = blockIdx.z;
@@ -44,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int
         rows = min(kTile, g.m - m0);
         a += m0 * g.a_m + r0 * g.a_r;
         b += n0 * g.b_n + r0 * g.b_r;
-        c += e * g.c_e + m0 * g.c_m + n0 * g.c_n;
+        c += e * g.c_e + m0 * g.c_m + n0;
     } else {
         const int64_t t = blockIdx.y + int64_t(blockIdx.z) * gridDim.y;
         if (t >= seg.tile[seg.count]) return;
@@ -55,7 +54,7 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int
         depth = none ? 0 : g.r;
         a += r0 * g.a_m;
         b += (none ? 0 : s - 1) * g.b_e + n0 * g.b_n;
-        c += r0 * g.c_m + n0 * g.c_n;
+        c += r0 * g.c_m + n0;
     }
     const int cols = min(kTile, g.n - n0);
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
@@ -82,7 +81,7 @@ __global__ void __launch_bounds__(kThreads) expert_simt_kernel(ExpertArgs g, int
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int row = ty + 16 * i, col = tx + 16 * j;
-            if (row < rows && col < cols) c[row * g.c_m + col * g.c_n] = from_float<T>(acc[i][j]);
+            if (row < rows && col < cols) c[row * g.c_m + col] = acc[i][j];
         }
 }
 
@@ -94,7 +93,7 @@ cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream)
     const int64_t tiles = a.rows / kTile + a.experts + 2;
     const unsigned ty = unsigned(tiles < 32768 ? tiles : 32768);
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), ty, unsigned((tiles + ty - 1) / ty));
-    expert_simt_kernel<float, false><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a, 0);
+    expert_simt_kernel<false><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a, 0);
     return cudaGetLastError();
 }
 
@@ -102,7 +101,7 @@ cudaError_t expert_simt_weights(const ExpertArgs &a, int64_t most, cudaStream_t 
 {
     const dim3 grid(unsigned((a.n + kTile - 1) / kTile), unsigned((a.m + kTile - 1) / kTile),
                     unsigned(a.experts));
-    expert_simt_kernel<float, true><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a, most);
+    expert_simt_kernel<true><<<grid, kThreads, segments_bytes(a.experts), stream>>>(a, most);
     return cudaGetLastError();
 }
 

@@ -141,7 +141,7 @@ struct ExpertArgs {
     void *c;
     int64_t a_m, a_r;       // strides of A
     int64_t b_e, b_n, b_r;  // strides of B (b_e between experts; 0 for weights)
-    int64_t c_e, c_m, c_n;  // strides of C (c_e between experts; 0 for rows)
+    int64_t c_e, c_m;       // strides of C (c_e between experts; 0 for rows); c_n is 1
     const int64_t *offsets;
     int64_t rows;
     int32_t experts, m, n, r;  // rows: m unused; weights: r unused

@@ -54,7 +54,7 @@ ExpertArgs expert_args(const dc_expert_shape *s, int product, const void *a, con
     if (product < 2) {
         g.a = a;
         g.b = b;
-        g.a_r = g.c_n = 1;
+        g.a_r = 1;
         g.b_e = s->w_expert;
         g.a_m = product ? s->ldy : s->ldx;
         g.c_m = product ? s->ldx : s->ldy;
@@ -66,7 +66,7 @@ ExpertArgs expert_args(const dc_expert_shape *s, int product, const void *a, con
         const bool nk = s->w_k == 1;
         g.a = nk ? a : b;
         g.b = nk ? b : a;
-        g.a_m = g.b_n = g.c_n = 1;
+        g.a_m = g.b_n = 1;
         g.a_r = nk ? s->ldy : s->ldx;
         g.b_r = nk ? s->ldx : s->ldy;
         g.c_e = s->w_expert;
