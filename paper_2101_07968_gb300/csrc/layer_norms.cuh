@@ -1,12 +1,13 @@
 // The norm after a block, its gate, dropout and scaled residual, and the norm before the
 // next block, in one pass over the rows; and the gradient of all of it.
 //
-// A block takes a contiguous run of rows, one at a time, 16 elements a thread. Every row is read
+// A block takes a contiguous run of rows, one at a time, 4, 8 or 16 elements a thread. Every row is read
 // once and written once: bulk copies bring the next rows into a ring in shared memory while
 // one is worked on, so that the latency of memory and the two sums of a row (four for the
 // layer norm, whose mean is taken first: sums of squares of centred values lose nothing to
-// cancellation) overlap. Rows that copies cannot take (off 16-byte boundaries, or too long for
-// the ring) are loaded straight into registers. The gradient computes the statistics again
+// cancellation) overlap. Rows off 16-byte boundaries come with the bytes around them (the arrays'
+// first and last rows, where those would lie outside, are loaded by the threads). Above kWideD
+// columns such rows, and any that are too long for the ring, are loaded straight into registers. The gradient computes the statistics again
 // from the same rows and adds up the gradients of weights and gates in registers; what
 // several runs share is written out per run and added in a fixed order by a second kernel.
 //
@@ -28,8 +29,11 @@ namespace norms {
 // have work.
 constexpr int kElems = 16;
 // Rows above this take blocks of 512 threads, with a ring of rows where there is room for two,
-// and above twice this of 1,024, whose 64 registers each do not hold the gradient's sums: they
-// spill, which narrower rows are spared.
+// and above twice this of 1,024. The three sums of the gradient of both norms do not fit the registers
+// everywhere (bytes spilled a thread, bfloat16 and float): up to kWideD columns 0-32 and 12-220 with long gates,
+// 4-240 and 136-500 with short ones; single warps, 64 registers, 4-188 and 12-460, off 16-byte
+// boundaries 88-668; blocks of 512 with a ring 16-244 and 200-484; 1,024 threads, 64 registers,
+// 752-1,752.
 constexpr int kNarrow = 256, kWideD = kNarrow * kElems;
 constexpr int elems_for(int D, bool vec)  // vec: rows on 16-byte boundaries
 {
@@ -335,7 +339,7 @@ constexpr int kOwn = 2;
 // the gate row changes. For shorter ones that costs more than it saves.
 constexpr int kLongGate = 8;
 
-// Resident blocks: 24 warps an SM. Two of 512 threads serve 8,192 x 5,120 in 96 us and x 3,001 in 88,
+// Resident blocks: 24 warps an SM, 32 with blocks of 512 threads. Two of those serve 8,192 x 5,120 in 96 us and x 3,001 in 88,
 // one in 127 and 113 (x 8,192, whose blocks are full, 115 against 102).
 template <typename T, int V, int FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 512 ? 2 : MAXT == 32 ? 32 : 1) norm_kernel(NormArgs a, int stages)
@@ -837,7 +841,8 @@ inline Plan plan_for(int D, bool vec, int arrays, int bytes, int threads, int ow
     while (p.blocks > 1 && room / p.blocks < 2 * row + fixed) --p.blocks;
     const size_t slots = room / p.blocks > fixed ? (room / p.blocks - fixed) / row : 0;
     p.stages = int(slots < kMaxStages ? slots : kMaxStages);
-    if (p.stages < 2) p.stages = 0;
+    // wide rows take a ring on 16-byte boundaries and in blocks of up to 512 threads only
+    if (p.stages < 2 || (D > kWideD && (!vec || size > 512))) p.stages = 0;
     p.smem = p.stages * row + fixed - 2048;
     return p;
 }
@@ -922,7 +927,7 @@ cudaError_t forward(int dtype, const NormArgs &a, cudaStream_t stream)
     const bool vec = vectors_ok(dtype, a), full = a.D % (kElems * 32) == 0;
     const Plan p = plan_for(a.D, vec, 2, dtype_bytes(dtype), kForwardThreads, kOwn);
     constexpr int V = kVec<T>;
-    if (a.D > kWideD && p.size <= 512 && p.stages && vec)
+    if (a.D > kWideD && p.stages)
         return norm_launch<T, V, 0, true, 512, kElems>(a, p, stream);
     if (a.D > kWideD)
         return vec ? norm_launch<T, V, 0, false, 1024, kElems>(a, p, stream)
@@ -955,7 +960,7 @@ cudaError_t gradient(int dtype, const NormArgs &a, float *partial, cudaStream_t 
     const Plan p = plan_for(a.D, vec, 4, dtype_bytes(dtype), kGradThreads, kOwn);
     const int64_t P = grad_runs(dtype, a.rows, a.D, vec);
     constexpr int V = kVec<T>;
-    if (a.D > kWideD && p.size <= 512 && p.stages && vec)
+    if (a.D > kWideD && p.stages)
         return norm_grad_launch<T, V, 0, true, 512, kElems>(a, partial, P, p, stream);
     if (a.D > kWideD)
         return vec ? norm_grad_launch<T, V, 0, false, 1024, kElems>(a, partial, P, p, stream)
