@@ -470,6 +470,13 @@ dc_status dc_time_next_pass(cudaEvent_t start, cudaEvent_t stop);
 dc_status dc_roof_int_probe(int32_t variant, int32_t blocks, int32_t threads, int64_t iters,
                             uint32_t *sink, cudaStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * dc_wait_probe -- test support: one small block in which two threads wait, as the layer
+ * operators' kernels do, for copies that nothing has started. The waits run out within some
+ * two seconds, and the kernel ends and sets status (device) to DC_ERR_INTERNAL as theirs do.
+ * ---------------------------------------------------------------------- */
+dc_status dc_wait_probe(int32_t *status, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,5 +1,6 @@
 // C ABI of the layer operators (declared in include/dynacomm.h): host-side argument
 // checks, then kernel launches on the caller's stream. No allocation, no synchronisation.
+#include "blackwell.cuh"
 #include "layers.cuh"
 
 namespace dc {
@@ -118,6 +119,23 @@ NormArgs norm_args(const dc_block_norm_cfg *c)
     a.eps = float(c->eps);
     a.drop = drop_rule(c->p, c->seed, c->offset);
     return a;
+}
+
+// Both warps' waits end: the first to run out makes the other give up.
+__global__ void wait_probe_kernel(int32_t *status)
+{
+    __shared__ alignas(8) uint64_t bars[2];
+    __shared__ uint32_t gave_up;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) bw::bar_init(bw::smem_addr(&bars[i]), 1);
+        gave_up = 0;
+        bw::bar_init_fence();
+    }
+    __syncthreads();
+    bool arrived = false;
+    if (threadIdx.x % 32 == 0) arrived = bw::bar_wait(bw::smem_addr(&bars[threadIdx.x / 32]), 0, &gave_up);
+    const bool any = __syncthreads_or(arrived);
+    if (threadIdx.x == 0 && gave_up && !any) *status = DC_ERR_INTERNAL;
 }
 
 }  // namespace
@@ -264,6 +282,14 @@ dc_status dc_block_norm_grad(const dc_block_norm_cfg *cfg, const void *dy, const
     if (!f) a.alpha = 1.0f;
     return dc::result(
         dc::launch_norm_grad(cfg->dtype, a, static_cast<float *>(workspace), stream));
+}
+
+dc_status dc_wait_probe(int32_t *status, cudaStream_t stream)
+{
+    const dc::NvtxRange nvtx("dc_wait_probe");
+    if (!status) return DC_ERR_NULL;
+    dc::wait_probe_kernel<<<1, 64, 0, stream>>>(status);
+    return dc::result(cudaGetLastError());
 }
 
 }  // extern "C"

@@ -112,6 +112,7 @@ _SIGNATURES = {
     "dc_block_norm": (_I32, [_NORM, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
     "dc_block_norm_grad_workspace_bytes": (_SZ, [_NORM]),
     "dc_block_norm_grad": (_I32, [_NORM] + [_VP] * 13 + [_SZ, _VP]),
+    "dc_wait_probe": (_I32, [_VP, _VP]),
 }
 
 

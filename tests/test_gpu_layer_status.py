@@ -1,5 +1,5 @@
 """The word that the expert products' kernels report to: made once, outside of graphs, and read
-after every stream is done."""
+after every stream is done; and a wait that runs out."""
 import os
 import subprocess
 import sys
@@ -96,3 +96,24 @@ def test_one_word_for_threads_that_come_together(ly, monkeypatch):
     for t in threads:
         t.join()
     assert len(got) == 4 and len(set(got)) == 1 and got[0] == ly._status[device][0].data_ptr()
+
+
+def test_a_wait_that_runs_out_ends_and_reports(ly):
+    """Two threads wait for copies that nothing has started: the kernel ends within some two
+    seconds, reports, and the device goes on."""
+    from paper_2101_07968_gb300.dynacomm import DC_ERR_INTERNAL, DC_ERR_NULL, DynaCommError
+    x, w, _ = operands(1, 100, 2, 64, 64, torch.float16)
+    o = offs(0, 50, 100)
+    want = ly.expert_matmul(x, w, o)
+    ly.check_status()
+    start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    ly._run("dc_wait_probe", x, None, ly._status_of(x.get_device()))
+    stop.record()
+    with pytest.raises(DynaCommError) as e:
+        ly.check_status()
+    assert e.value.status == DC_ERR_INTERNAL
+    assert start.elapsed_time(stop) < 4000
+    assert ly._function("dc_wait_probe")(None, None) == DC_ERR_NULL
+    ly.check_status()
+    assert torch.equal(ly.expert_matmul(x, w, o), want)
