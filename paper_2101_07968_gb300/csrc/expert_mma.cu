@@ -19,9 +19,10 @@
 // overwrites those of an expert's last block with zeros between the copy's arrival and the
 // product. Every wait ends after a number of tries, and the kernel then reports it in status.
 //
-// Measured (bfloat16, one GB300): 16,384 rows over 16 experts x 4,096 x 2,048, y and dx 157 us,
-// dW 160 us (1,750 and 1,710 TFLOP/s); 65,536 rows over 32 experts x 2,048 x 4,096, 567-580 us
-// (1,900-1,940 TFLOP/s against a library product's 1,902). The tensor cores are busy 85 % of
+// Measured (bfloat16, one GB300, short runs): 16,384 rows over 16 even experts x 4,096 x 2,048, 154-160 us
+// each (1,720-1,780 TFLOP/s; ragged experts, whose last tiles are short, 173); 65,536 rows over 32 experts x
+// 2,048 x 4,096, 567-580 us (1,900-1,940 TFLOP/s against a library product's 1,902). Long runs lower the
+// clock to 1,450-1,500 of 2,070 MHz: 176 us, ragged 192, 726 a product of the larger. The tensor cores are busy 85 % of
 // the time; a block's products take 512 cycles and its copies, read by every pair through the
 // L2, some 630 (15 TB/s). A product takes some 100 cycles to issue whatever its columns, so
 // tiles narrower than 256 do not run at the tensor cores' rate. With one or a few experts' rows
@@ -56,7 +57,7 @@ struct MmaArgs {
     int32_t *status;
     bool wide;          // weights: 16-byte stores; rows: 4-byte stores
     int32_t least;      // weights: experts of fewer rows are left to another kernel
-    float *sums;        // long sums: a CTA's tile of the rounds so far (sum_bytes)
+    float *sums;        // long sums: a CTA's tile of the rounds so far (expert_mma_sum_bytes)
 };
 
 // Blocks summed in the tensor cores at a time. They cut a sum off at every step where a float

@@ -339,7 +339,7 @@ constexpr int kOwn = 2;
 // the gate row changes. For shorter ones that costs more than it saves.
 constexpr int kLongGate = 8;
 
-// Resident blocks: 24 warps an SM, 32 with blocks of 512 threads. Two of those serve 8,192 x 5,120 in 96 us and x 3,001 in 88,
+// Resident blocks: 24 warps an SM, 32 with blocks of 512 threads. Two of those serve 8,192 x 5,120 in 96 us (layer norm) and x 3,001 in 88,
 // one in 127 and 113 (x 8,192, whose blocks are full, 115 against 102).
 template <typename T, int V, int FULL, bool HAS_F, bool HAS_H, bool LONG, bool RING, int MAXT, int EL>
 __global__ void __launch_bounds__(MAXT, MAXT == kNarrow ? 3 : MAXT == 512 ? 2 : MAXT == 32 ? 32 : 1) norm_kernel(NormArgs a, int stages)
@@ -846,7 +846,7 @@ inline Plan plan_for(int D, bool vec, int arrays, int bytes, int threads, int ow
     p.smem = p.stages * row + fixed - 2048;
     return p;
 }
-constexpr int kSms = 152;
+constexpr int kSms = 152;  // a constant, so that a workspace query needs no device
 constexpr int kForwardThreads = 768, kGradThreads = 512;  // an SM; up to 32 single warps
 
 inline int64_t grad_runs(int dtype, int64_t rows, int D, bool vec)
