@@ -85,7 +85,8 @@ __device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cl
 
 // A wait that ends: after kWaitTries tries or kWaitNs nanoseconds (a try may sleep a while), or
 // once another thread of the CTA has given up, it gives up (false). A wait of this library's
-// kernels lasts microseconds.
+// kernels lasts microseconds; one that may outlast many copies passes a word that changes as the
+// CTA's work goes on, `progress`, and gives up once that has stood still for as long.
 constexpr uint32_t kWaitTries = 1u << 23;
 constexpr uint64_t kWaitNs = 2000000000ull;
 __device__ __forceinline__ uint64_t now_ns()
@@ -94,21 +95,30 @@ __device__ __forceinline__ uint64_t now_ns()
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up,
+                                                  volatile uint32_t *progress)
 {
-    const uint64_t start = now_ns();
+    uint64_t start = now_ns();
+    uint32_t seen = progress ? *progress : 0;
     for (uint32_t i = 0; i < kWaitTries; ++i) {
         if (bar_try(bar, parity)) return true;
-        if ((i & 63u) == 63u && (*gave_up || now_ns() - start > kWaitNs)) break;
+        if ((i & 63u) != 63u) continue;
+        if (progress && *progress != seen) {
+            seen = *progress;
+            start = now_ns();
+            i = 0;
+        }
+        if (*gave_up || now_ns() - start > kWaitNs) break;
     }
     *gave_up = 1u;
     return false;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up,
+                                         volatile uint32_t *progress = nullptr)
 {
     for (int i = 0; i < 16; ++i)
         if (bar_try(bar, parity)) return true;
-    return bar_wait_long(bar, parity, gave_up);
+    return bar_wait_long(bar, parity, gave_up, progress);
 }
 
 // --------------------------------------------------------------------------- copies

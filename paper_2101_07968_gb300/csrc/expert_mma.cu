@@ -275,6 +275,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     extern __shared__ unsigned char dyn[];
     __shared__ alignas(8) uint64_t full[STAGES], empty[STAGES], tail[STAGES], done[2], free_[2];
     __shared__ uint32_t tmem_at, gave_up;
+    __shared__ uint32_t rounds;  // weights: finished by this CTA (counted by the copying thread, its loop is a tenth slower)
     __shared__ alignas(16) Lines lines[kOut ? 4 : 1];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -294,7 +295,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             bw::bar_init(bar(&done[i]), 1);
             bw::bar_init(bar(&free_[i]), 4 * kPair);
         }
-        gave_up = 0;
+        gave_up = rounds = 0;
         bw::bar_init_fence();
     }
     if (warp == 5) bw::tmem_alloc(bw::smem_addr(&tmem_at), kColumns);
@@ -448,7 +449,8 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 it += blocks;
                 if ((q.r & 15) == 0) continue;
                 const int s = (it - 1) % STAGES;
-                bool ok = bw::bar_wait(bar(&tail[s]), (uses >> s) & 1, &gave_up);
+                // all blocks since the last such one come before this one: seconds for long experts
+                bool ok = bw::bar_wait(bar(&tail[s]), (uses >> s) & 1, &gave_up, &rounds);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 uses ^= 1u << s;
                 const int cols = (q.cols + 16 * kPair - 1) / (16 * kPair) * 16;
@@ -496,6 +498,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 ok = bw::bar_wait(bar(&done[half]), (tile / 2) & 1, &gave_up);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
+                if (MODE == kWeights && threadIdx.x == 0) *const_cast<volatile uint32_t *>(&rounds) = uint32_t(tile) + 1;
                 bw::fence_after();
                 const uint32_t lanes = tmem + (uint32_t(warp * 32) << 16), at = lanes + half * BN;
                 auto all_read = [&] {  // the half may be overwritten

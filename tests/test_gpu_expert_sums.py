@@ -150,3 +150,21 @@ def test_floats_lose_no_more_than_a_sum_in_floats(ly, depth, sign):
     for got in (ly.expert_matmul(a, b[None], o), ly.expert_matmul_grad_input(a, b.t()[None].contiguous(), o),
                 ly.expert_matmul_grad_weight(a.t().contiguous(), b.t().contiguous(), offs(0, depth))[0]):
         assert off(got) <= off(plain), (off(got), off(plain))
+
+
+def test_a_product_of_seconds(ly):
+    """One expert of 640 million rows, whose one tile takes longer than a wait may: the waits of
+    every warp go on as long as the tile's copies do. Terms of one sign: some 78,000 rounds are added
+    up, each within 2^-24."""
+    rows, n = 640_000_003, 8
+    x, dy = (torch.empty(rows, n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(23)
+    x.uniform_(0.25, 1, generator=g)
+    dy.uniform_(0.25, 1, generator=g)
+    dw = ly.expert_matmul_grad_weight(dy, x, offs(0, rows))
+    ly.check_status()
+    exact = torch.zeros(n, n, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 1 << 24):
+        exact += dy[i:i + (1 << 24)].double().t() @ x[i:i + (1 << 24)].double()
+    off = (dw[0].double() - exact) / exact
+    assert float(off.abs().max()) <= lo.UNIT[torch.bfloat16] + 2.0 ** -14 + 78_200 * 2.0 ** -24
