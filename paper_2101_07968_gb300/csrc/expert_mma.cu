@@ -65,7 +65,7 @@ struct MmaArgs {
 // 16-bit operands: 512 steps lose 5e-5, a tenth of half's rounding, and a million rows in one
 // go 7e-3. So after 128 blocks (8,192 summed elements) a round's sums are added to those before it
 // in floats, rounded: in memory that stays in the L2, since no registers are left at 256 columns,
-// and while the next round is summed. One expert of 65,536 rows x 2,048 x 4,096, dW: 676 us against 671 in one go.
+// and while the next round is summed. One expert of 65,536 rows x 2,048 x 4,096, dW: 676-698 us against 631-686 in one go.
 // Shorter sums are one round. It bounds the wait for a finished round, too.
 constexpr int kRound16 = 128;
 constexpr int64_t kLongSum = int64_t(kRound16) * kBKBytes / 2;

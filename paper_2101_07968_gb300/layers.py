@@ -194,7 +194,7 @@ def _product(which, shape, a, b, offsets, c, stream):
 def expert_matmul(x, w, offsets, stream=None):
     """y [rows, N]: y[r] = w[e] @ x[r] for the expert e whose rows hold r (offsets[e] <= r <
     offsets[e + 1], int64 [experts + 1]); zeros for rows of no expert. x [rows, K] with any row
-    stride, w [experts, N, K] with N or K contiguous."""
+    stride, w [experts, N, K] with N or K contiguous and each expert's matrix apart from the others'."""
     ldx = _rows("x", x)
     E, N, K, se, sn, sk = _weights("w", w)
     R = x.shape[0]
