@@ -439,6 +439,88 @@ dc_status dc_block_norm_grad(const dc_block_norm_cfg *cfg, const void *dy, const
                              float *dw_pre, void *workspace, size_t workspace_bytes,
                              cudaStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * dc_head_norm_rotary, dc_head_norm_rotary_grad -- the norms of queries and keys for each
+ * head and the rotation by position, in one pass over both. q [tokens][heads][D] and k
+ * [tokens][kv_heads][D] have contiguous heads and the strides q_token, q_head, k_token,
+ * k_head (elements); q_out and k_out are contiguous. For a head's elements x, with w its
+ * weight w_q or w_k [D] (NULL: ones):
+ *   z = w x / sqrt(mean(x^2) + eps)           (norm 0: z = w x)
+ * and pair i of the first `rotary` elements, (i, i + rotary / 2), or (2i, 2i + 1) where
+ * interleaved is not 0, turns by the angle a = positions[token] base^(-2i / rotary):
+ *   out1 = z1 cos a - z2 sin a,  out2 = z2 cos a + z1 sin a
+ * The other elements are z. Positions (device, int64) may have any value; the angle's whole
+ * turns are dropped in integers, so that far positions lose nothing.
+ * The gradient takes dq_out and dk_out (contiguous) and q and k again, and writes dq, dk
+ * (contiguous) and dw_q, dw_k (float [D]; NULL: not wanted). workspace:
+ * dc_head_norm_rotary_grad_workspace_bytes(cfg) bytes, used during the call's kernels only.
+ * Outputs may be their own inputs (q_out = q of contiguous q; dq = dq_out).
+ * Errors: DC_ERR_NULL, DC_ERR_BAD_LAYER (dtype; tokens outside [0, 2^31 - 1]; heads or kv_heads
+ * outside [1, DC_HEADS_MAX]; D outside [1, DC_HEAD_NORM_DIM_MAX]; rotary odd, negative or above D;
+ * base <= 0 or not finite; eps < 0; heads that overlap), DC_ERR_WORKSPACE, DC_ERR_CUDA.
+ * ---------------------------------------------------------------------- */
+#define DC_HEADS_MAX 1024
+#define DC_HEAD_NORM_DIM_MAX 256
+typedef struct dc_head_norm_cfg {
+    int32_t dtype, heads, kv_heads, D, rotary, interleaved, norm;
+    int64_t tokens;
+    int64_t q_token, q_head, k_token, k_head;
+    double base, eps;
+} dc_head_norm_cfg;
+
+dc_status dc_head_norm_rotary(const dc_head_norm_cfg *cfg, const void *q, const void *k,
+                              const int64_t *positions, const void *w_q, const void *w_k,
+                              void *q_out, void *k_out, cudaStream_t stream);
+size_t dc_head_norm_rotary_grad_workspace_bytes(const dc_head_norm_cfg *cfg);
+dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_out,
+                                   const void *dk_out, const void *q, const void *k,
+                                   const int64_t *positions, const void *w_q, const void *w_k,
+                                   void *dq, void *dk, float *dw_q, float *dw_k, void *workspace,
+                                   size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * dc_attention, dc_attention_grad -- causal attention of packed sequences. Row t of q
+ * [tokens][heads][D] belongs to sequence s when offsets[s] <= t < offsets[s+1] (offsets:
+ * sequences + 1 device int64, in order); head h reads key head h / (heads / kv_heads) of k
+ * and v [tokens][kv_heads][D]. Over the keys j of the same sequence with j <= i:
+ *   S_ij = scale q_i . k_j,  lse_i = log(sum_j e^S_ij),  y_i = sum_j e^(S_ij - lse_i) v_j
+ * with y [tokens][heads][D] and lse (float) [heads][tokens] contiguous. The gradient takes dy
+ * (of y; contiguous), the call's inputs, y and lse, and writes dq, dk, dv (contiguous):
+ *   P = e^(S - lse),  dS_ij = P_ij (dy_i . v_j - dy_i . y_i),
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dy_i
+ * with the sums of dk and dv over every head that reads the key head. What stands in rows of
+ * other sequences, or of keys after a row, has no effect on it, infinities and NaN included.
+ * Rows of no sequence (before offsets[0] or from offsets[sequences] on) get zeros in y, lse,
+ * dq, dk and dv. An offset outside [0, tokens], or below an earlier one, counts as the nearest
+ * valid value. q, k and v have contiguous heads and the strides given (elements).
+ * workspace: dc_attention_workspace_bytes(shape, grad, q, k, v, dy) bytes, 256-byte aligned, used
+ * during the call's kernels only (grad 0 or 1; the addresses decide whether copies are
+ * needed; dy of no account for grad 0). status (device, nullable): as for the expert products.
+ * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; tokens outside [0, 2^31 - 1]; sequences outside
+ * [0, DC_SEQUENCES_MAX]; heads or kv_heads outside [1, DC_HEADS_MAX]; heads not a multiple of
+ * kv_heads; D outside [1, DC_ATTENTION_DIM_MAX]; a scale that is not finite; heads that
+ * overlap, or strides above 2^37); DC_ERR_WORKSPACE; DC_ERR_CUDA.
+ * ---------------------------------------------------------------------- */
+#define DC_ATTENTION_DIM_MAX 128
+#define DC_SEQUENCES_MAX 1048576
+typedef struct dc_attention_shape {
+    int32_t dtype, heads, kv_heads, D, sequences;
+    int64_t tokens;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+    double scale;
+} dc_attention_shape;
+
+size_t dc_attention_workspace_bytes(const dc_attention_shape *shape, int32_t grad, const void *q,
+                                    const void *k, const void *v, const void *dy);
+dc_status dc_attention(const dc_attention_shape *shape, const void *q, const void *k,
+                       const void *v, const int64_t *offsets, void *y, float *lse,
+                       int32_t *status, void *workspace, size_t workspace_bytes,
+                       cudaStream_t stream);
+dc_status dc_attention_grad(const dc_attention_shape *shape, const void *dy, const void *q,
+                            const void *k, const void *v, const void *y, const float *lse,
+                            const int64_t *offsets, void *dq, void *dk, void *dv, int32_t *status,
+                            void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
 /* Static description of a status code. Never NULL. */
 const char *dc_status_string(dc_status s);
 

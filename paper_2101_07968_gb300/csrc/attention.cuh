@@ -1,0 +1,60 @@
+// Causal attention of packed sequences: what its kernels share. Rows are cut into tiles that never
+// cross a sequence's end; a list of them, those with the most work first, is made on the device
+// (attention_plan.cu), since the sequences' offsets are device data.
+#pragma once
+
+#include "layers.cuh"
+
+namespace dc {
+
+// `rows` rows from row0 on, tile `at` of `of` of a sequence that starts at row `first` and ends
+// before `end`. first < 0: rows of no sequence, whose outputs are zeros.
+struct AttentionTile {
+    int32_t row0, rows, first, end;
+};
+
+// The plan's head in the workspace, then its tiles.
+struct AttentionPlan {
+    int32_t tiles;
+    uint32_t top_v, top_do;  // largest finite magnitudes (float bits): the scale of halves' gradients
+    int32_t pad[13];
+};
+__host__ __device__ inline const AttentionTile *plan_tiles(const AttentionPlan *p)
+{
+    return reinterpret_cast<const AttentionTile *>(p + 1);
+}
+
+struct AttentionArgs {
+    const void *q, *k, *v, *dy;      // dy: the gradient of y, [tokens][heads][D]
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, dy_token, dy_head;  // strides
+    void *y, *dq, *dk, *dv;          // contiguous
+    float *lse;                      // [heads][tokens]
+    float *delta;                    // [heads][tokens]: sum of dy y
+    const AttentionPlan *plan;
+    int64_t tokens;
+    int32_t heads, kv_heads, group, D;
+    float scale;
+    int32_t *status;
+};
+
+// The most tiles of `rows` rows that a plan can have: a short one for each sequence, and the rows
+// before the first and after the last.
+inline int64_t attention_most_tiles(int64_t tokens, int32_t sequences, int rows)
+{
+    return tokens / rows + sequences + 2;
+}
+
+// Item `round` of a block, of items in order of falling work: every other round is dealt backwards,
+// so that the sums are even. -1: none left.
+__device__ __forceinline__ int64_t dealt(int64_t round, int64_t items)
+{
+    const int64_t at = round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x, i = round * gridDim.x + at;
+    return i < items ? i : -1;
+}
+
+// csrc/attention_simt.cu: floats, on the CUDA cores
+constexpr int kSimtRows = 64;
+cudaError_t launch_attention_simt(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
+cudaError_t launch_attention_grad_simt(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
+
+}  // namespace dc

@@ -1,0 +1,328 @@
+// Attention on the CUDA cores.
+//
+// Forward, a block per tile of 64 rows and head: keys 64 at a time; scores S = scale q k^T, the
+// running maximum m and sum l of each row, and y = sum e^(S - m) v / l, kept in registers.
+// Gradient, with P = e^(S - lse) and dS = P (dy v^T - delta):
+//   rows     a tile of 64 rows and a head, over the keys up to it: dq = scale dS k
+//   columns  a tile of 64 keys and a key head, over its group's heads and the rows from it on:
+//            dv = P^T dy, dk = scale dS^T q
+// Each sum has one owner and one order: no atomics. What a mask leaves out is skipped, not
+// multiplied by zero, so that whatever stands there is without effect.
+//
+// 256 threads, 4 x 4 scores a thread. Rows of operands lie in shared memory four floats apart from
+// whole banks' multiples, so that threads read four neighbouring elements of 16 rows without
+// conflicts: eight such reads feed 64 products.
+#include "attention.cuh"
+
+namespace dc {
+namespace {
+
+constexpr int kThreads = 256, kTile = kSimtRows;
+constexpr int kScorePitch = kTile + 4;
+
+template <int DP>
+constexpr int kPitch = DP + 4;
+
+// Rows row0 .. row0 + rows of x [token][D] to shared memory as floats; zeros beyond rows and D.
+template <typename T, int DP>
+__device__ __forceinline__ void bring(float *to, const T *x, int64_t stride, int rows, int D)
+{
+    for (int i = threadIdx.x; i < kTile * DP; i += kThreads) {
+        const int r = i / DP, d = i % DP;
+        to[r * kPitch<DP> + d] = r < rows && d < D ? to_float(x[r * stride + d]) : 0.0f;
+    }
+}
+
+// s[i][j] = sum over d of x[ty + 16 i][d] z[tx + 16 j][d]
+template <int DP>
+__device__ __forceinline__ void scores(const float *x, const float *z, float (&s)[4][4])
+{
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.0f;
+#pragma unroll 2
+    for (int d = 0; d < DP; d += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = *reinterpret_cast<const float4 *>(x + (ty + 16 * i) * kPitch<DP> + d);
+            b[i] = *reinterpret_cast<const float4 *>(z + (tx + 16 * i) * kPitch<DP> + d);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                s[i][j] += a[i].x * b[j].x + a[i].y * b[j].y + a[i].z * b[j].z + a[i].w * b[j].w;
+    }
+}
+
+// acc[i][4 m + e] += sum over the first n columns c of p[ty + 16 i][c] z[c][4 tx + 64 m + e], but
+// only columns that the row's mask lets through: from lo(i) up to hi(i).
+template <int DP, typename Lo, typename Hi>
+__device__ __forceinline__ void add_product(const float *p, const float *z, float (&acc)[4][DP / 16], Lo lo, Hi hi)
+{
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll 2
+    for (int c = 0; c < kTile; ++c) {
+        float4 b[DP / 64];
+#pragma unroll
+        for (int m = 0; m < DP / 64; ++m)
+            b[m] = *reinterpret_cast<const float4 *>(z + c * kPitch<DP> + 4 * tx + 64 * m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float w = p[(ty + 16 * i) * kScorePitch + c];
+            if (c < lo(i) || c >= hi(i)) continue;
+#pragma unroll
+            for (int m = 0; m < DP / 64; ++m) {
+                acc[i][4 * m] += w * b[m].x;
+                acc[i][4 * m + 1] += w * b[m].y;
+                acc[i][4 * m + 2] += w * b[m].z;
+                acc[i][4 * m + 3] += w * b[m].w;
+            }
+        }
+    }
+}
+
+// Rows of a tile to [token][heads][D]
+template <typename T, int DP>
+__device__ __forceinline__ void put(T *y, int64_t stride, int rows, int D, const float (&acc)[4][DP / 16],
+                                    const float (&by)[4])
+{
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = ty + 16 * i;
+        if (r >= rows) continue;
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) {
+            const int d = 4 * tx + 64 * (j / 4) + j % 4;
+            if (d < D) y[r * stride + d] = from_float<T>(acc[i][j] * by[i]);
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void put_zeros(T *y, int64_t stride, int rows, int D)
+{
+    for (int i = threadIdx.x; i < rows * D; i += kThreads) y[i / D * stride + i % D] = from_float<T>(0.0f);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_kernel(const AttentionArgs a)
+{
+    extern __shared__ float dyn[];
+    float *q = dyn, *kv = q + kTile * kPitch<DP>, *p = kv + kTile * kPitch<DP>;
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int64_t items = int64_t(a.plan->tiles) * a.heads;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const AttentionTile t = plan_tiles(a.plan)[item / a.heads];
+        const int h = int(item % a.heads), g = h / a.group;
+        const int64_t out = int64_t(a.heads) * a.D;
+        T *y = static_cast<T *>(a.y) + t.row0 * out + int64_t(h) * a.D;
+        if (t.first < 0) {
+            put_zeros(y, out, t.rows, a.D);
+            for (int r = threadIdx.x; r < t.rows; r += kThreads) a.lse[h * a.tokens + t.row0 + r] = 0.0f;
+            continue;
+        }
+        __syncthreads();
+        bring<T, DP>(q, static_cast<const T *>(a.q) + t.row0 * a.q_token + h * a.q_head, a.q_token, t.rows, a.D);
+        float m[4], l[4] = {}, acc[4][DP / 16] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
+        for (int c0 = t.first; c0 < t.row0 + t.rows; c0 += kTile) {
+            const int n = min(kTile, t.row0 + t.rows - c0);
+            __syncthreads();
+            bring<T, DP>(kv, static_cast<const T *>(a.k) + c0 * a.k_token + g * a.k_head, a.k_token, n, a.D);
+            __syncthreads();
+            float s[4][4];
+            scores<DP>(q, kv, s);
+            auto end = [&](int i) { return min(n, t.row0 + ty + 16 * i - c0 + 1); };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][j] = tx + 16 * j < end(i) ? s[i][j] * a.scale : -INFINITY;
+                    top = fmaxf(top, s[i][j]);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float next = fmaxf(m[i], top);
+                // nothing but -inf so far: any finite reference will do
+                const float from = next == -INFINITY ? 0.0f : next;
+                const float old = expf(m[i] - from);
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = tx + 16 * j < end(i) ? expf(s[i][j] - from) : 0.0f;
+                    sum += e;
+                    p[(ty + 16 * i) * kScorePitch + tx + 16 * j] = e;
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                l[i] = l[i] * old + sum;
+                m[i] = next;
+#pragma unroll
+                for (int j = 0; j < DP / 16; ++j) acc[i][j] *= old;
+            }
+            __syncthreads();
+            bring<T, DP>(kv, static_cast<const T *>(a.v) + c0 * a.v_token + g * a.v_head, a.v_token, n, a.D);
+            __syncthreads();
+            add_product<DP>(p, kv, acc, [](int) { return 0; }, end);
+        }
+        float by[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            by[i] = 1.0f / l[i];
+            if (tx == 0 && ty + 16 * i < t.rows) a.lse[h * a.tokens + t.row0 + ty + 16 * i] = m[i] + logf(l[i]);
+        }
+        put<T, DP>(y, out, t.rows, a.D, acc, by);
+    }
+}
+
+// One pair of tiles of the gradient: x0, x1 (64 stationary rows: q and dy, or k and v), z0, z1 (64
+// moving ones: k and v, or q and dy).
+template <typename T, int DP, bool COLUMNS>
+__global__ void __launch_bounds__(kThreads) attention_grad_simt_kernel(const AttentionArgs a)
+{
+    extern __shared__ float dyn[];
+    constexpr int kSize = kTile * kPitch<DP>;
+    float *x0 = dyn, *x1 = x0 + kSize, *z0 = x1 + kSize, *z1 = z0 + kSize, *p = z1 + kSize;
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int outer = COLUMNS ? a.kv_heads : a.heads;
+    const int64_t items = int64_t(a.plan->tiles) * outer;
+    const T *q = static_cast<const T *>(a.q), *k = static_cast<const T *>(a.k), *v = static_cast<const T *>(a.v);
+    const T *dy = static_cast<const T *>(a.dy);
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        AttentionTile t = plan_tiles(a.plan)[item / outer];
+        const int o = int(item % outer), g = COLUMNS ? o : o / a.group;
+        const int64_t out = int64_t(outer) * a.D;
+        if (COLUMNS && t.first >= 0) {  // tile i from the end has the work of tile i from the start
+            const int n = (t.end - t.first + kTile - 1) / kTile, i = n - 1 - (t.row0 - t.first) / kTile;
+            t.row0 = t.first + i * kTile;
+            t.rows = min(kTile, t.end - t.row0);
+        }
+        const int64_t at = t.row0 * out + int64_t(o) * a.D;
+        T *const d0 = static_cast<T *>(COLUMNS ? a.dk : a.dq) + at, *const d1 = COLUMNS ? static_cast<T *>(a.dv) + at : nullptr;
+        if (t.first < 0) {
+            put_zeros(d0, out, t.rows, a.D);
+            if (COLUMNS) put_zeros(d1, out, t.rows, a.D);
+            continue;
+        }
+        __syncthreads();
+        float acc0[4][DP / 16] = {}, acc1[4][COLUMNS ? DP / 16 : 1] = {};
+        if (COLUMNS) {
+            bring<T, DP>(x0, k + t.row0 * a.k_token + g * a.k_head, a.k_token, t.rows, a.D);
+            bring<T, DP>(x1, v + t.row0 * a.v_token + g * a.v_head, a.v_token, t.rows, a.D);
+        } else {
+            bring<T, DP>(x0, q + t.row0 * a.q_token + o * a.q_head, a.q_token, t.rows, a.D);
+            bring<T, DP>(x1, dy + t.row0 * a.dy_token + o * a.dy_head, a.dy_token, t.rows, a.D);
+        }
+        for (int h = COLUMNS ? g * a.group : o; h < (COLUMNS ? (g + 1) * a.group : o + 1); ++h) {
+            const int lo = COLUMNS ? t.row0 : t.first, hi = COLUMNS ? t.end : t.row0 + t.rows;
+            for (int c0 = lo; c0 < hi; c0 += kTile) {
+                const int n = min(kTile, hi - c0);
+                __syncthreads();
+                if (COLUMNS) {
+                    bring<T, DP>(z0, q + c0 * a.q_token + h * a.q_head, a.q_token, n, a.D);
+                    bring<T, DP>(z1, dy + c0 * a.dy_token + h * a.dy_head, a.dy_token, n, a.D);
+                } else {
+                    bring<T, DP>(z0, k + c0 * a.k_token + g * a.k_head, a.k_token, n, a.D);
+                    bring<T, DP>(z1, v + c0 * a.v_token + g * a.v_head, a.v_token, n, a.D);
+                }
+                __syncthreads();
+                float s[4][4], ds[4][4];
+                scores<DP>(x0, z0, s);
+                scores<DP>(x1, z1, ds);
+                // columns of row i that count: keys up to it, or rows from the key on
+                auto from = [&](int i) { return COLUMNS ? t.row0 + ty + 16 * i - c0 : 0; };
+                auto end = [&](int i) { return COLUMNS ? n : min(n, t.row0 + ty + 16 * i - c0 + 1); };
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int c = tx + 16 * j, r = ty + 16 * i;
+                        const int64_t row = h * a.tokens + (COLUMNS ? c0 + c : t.row0 + r);
+                        if (c >= from(i) && c < end(i) && r < t.rows) {
+                            s[i][j] = expf(s[i][j] * a.scale - a.lse[row]);
+                            ds[i][j] = s[i][j] * (ds[i][j] - a.delta[row]);
+                        } else {
+                            s[i][j] = ds[i][j] = 0.0f;
+                        }
+                        if (COLUMNS) p[r * kScorePitch + c] = s[i][j];
+                    }
+                if constexpr (COLUMNS) {
+                    __syncthreads();
+                    add_product<DP>(p, z1, acc1, from, end);
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[(ty + 16 * i) * kScorePitch + tx + 16 * j] = ds[i][j];
+                __syncthreads();
+                add_product<DP>(p, z0, acc0, from, end);
+            }
+        }
+        const float by0[4] = {a.scale, a.scale, a.scale, a.scale}, by1[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+        put<T, DP>(d0, out, t.rows, a.D, acc0, by0);
+        if constexpr (COLUMNS) put<T, DP>(d1, out, t.rows, a.D, acc1, by1);
+    }
+}
+
+template <typename T, int DP>
+cudaError_t forward(const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    constexpr size_t smem = sizeof(float) * (2 * kTile * kPitch<DP> + kTile * kScorePitch);
+    static DeviceCache cache;
+    int ready = 0;
+    auto kernel = attention_simt_kernel<T, DP>;
+    const cudaError_t e = cache.get(ready, [&](int &v) {
+        v = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    });
+    if (e != cudaSuccess) return e;
+    const int64_t items = most * a.heads, limit = int64_t(1) << 20;
+    kernel<<<unsigned(items < limit ? items : limit), kThreads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, int DP, bool COLUMNS>
+cudaError_t backward(const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    constexpr size_t smem = sizeof(float) * (4 * kTile * kPitch<DP> + kTile * kScorePitch);
+    static DeviceCache cache;
+    int ready = 0;
+    auto kernel = attention_grad_simt_kernel<T, DP, COLUMNS>;
+    const cudaError_t e = cache.get(ready, [&](int &v) {
+        v = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    });
+    if (e != cudaSuccess) return e;
+    const int64_t items = most * (COLUMNS ? a.kv_heads : a.heads), limit = int64_t(1) << 20;
+    kernel<<<unsigned(items < limit ? items : limit), kThreads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attention_simt(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    DC_DTYPE_SWITCH(dtype, T, {
+        return a.D <= 64 ? forward<T, 64>(a, most, stream) : forward<T, 128>(a, most, stream);
+    })
+}
+
+cudaError_t launch_attention_grad_simt(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    DC_DTYPE_SWITCH(dtype, T, {
+        cudaError_t e = a.D <= 64 ? backward<T, 64, true>(a, most, stream) : backward<T, 128, true>(a, most, stream);
+        if (e == cudaSuccess)
+            e = a.D <= 64 ? backward<T, 64, false>(a, most, stream) : backward<T, 128, false>(a, most, stream);
+        return e;
+    })
+}
+
+}  // namespace dc

@@ -162,4 +162,30 @@ cudaError_t expert_few_rows(int dtype, const ExpertArgs &a, cudaStream_t stream)
 cudaError_t expert_simt_rows(const ExpertArgs &a, cudaStream_t stream);
 cudaError_t expert_simt_weights(const ExpertArgs &a, int64_t most, cudaStream_t stream);
 
+// Norms and rotation of queries (0) and keys (1).
+struct HeadNormArgs {
+    const void *x[2], *dy[2], *w[2];  // dy: the gradient's, contiguous
+    void *y[2];                       // outputs (dx), contiguous
+    float *dw[2];
+    int64_t token[2], head[2];  // strides of x
+    int32_t heads[2];
+    const int64_t *positions;
+    int64_t tokens;
+    int32_t D, rotary;
+    bool interleaved, norm;
+    float eps;
+    float *partial;           // gradient of the weights: the blocks' sums (nullable)
+    int32_t parts, per_part;  // of a token's heads, and the heads of one (set by the launcher)
+    uint64_t turns[DC_HEAD_NORM_DIM_MAX / 2];  // of pair i per position, in 2^-64 of a turn
+};
+size_t head_norm_workspace(int D);
+cudaError_t launch_head_norm(int dtype, const HeadNormArgs &a, cudaStream_t stream);
+cudaError_t launch_head_norm_grad(int dtype, const HeadNormArgs &a, cudaStream_t stream);
+
+// attention_plan.cu
+struct AttentionArgs;
+size_t attention_workspace(int dtype, const AttentionArgs &a, int32_t sequences, bool grad);
+cudaError_t launch_attention(int dtype, AttentionArgs a, int32_t sequences, const int64_t *offsets, bool grad,
+                             void *workspace, cudaStream_t stream);
+
 }  // namespace dc

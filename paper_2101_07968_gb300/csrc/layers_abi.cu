@@ -1,7 +1,9 @@
 // C ABI of the layer operators (declared in include/dynacomm.h): host-side argument
 // checks, then kernel launches on the caller's stream. No allocation, no synchronisation.
+#include <cmath>
+
+#include "attention.cuh"
 #include "blackwell.cuh"
-#include "layers.cuh"
 
 namespace dc {
 
@@ -118,6 +120,86 @@ NormArgs norm_args(const dc_block_norm_cfg *c)
     a.alpha = float(c->residual_scale);
     a.eps = float(c->eps);
     a.drop = drop_rule(c->p, c->seed, c->offset);
+    return a;
+}
+
+// Heads [tokens][heads][D] with contiguous elements: no two share an element.
+bool heads_ok(int64_t token, int64_t head, int32_t heads, int32_t D, int64_t tokens)
+{
+    if (heads > 1 && !stride_ok(head, D)) return false;
+    if (tokens <= 1) return true;
+    // heads within a token, or tokens within a head
+    const int64_t across = (heads > 1 ? (heads - 1) * head : 0) + D;
+    return stride_ok(token, across) || (stride_ok(token, D) && heads > 1 && head >= (tokens - 1) * token + D);
+}
+bool count_ok(int32_t heads) { return heads >= 1 && heads <= DC_HEADS_MAX; }
+
+dc_status check_head_norm(const dc_head_norm_cfg *c)
+{
+    if (!c) return DC_ERR_NULL;
+    const bool ok = dtype_ok(c->dtype) && rows_ok(c->tokens) && count_ok(c->heads) && count_ok(c->kv_heads) &&
+                    c->D >= 1 && c->D <= DC_HEAD_NORM_DIM_MAX && c->rotary >= 0 && c->rotary <= c->D &&
+                    c->rotary % 2 == 0 && c->base > 0.0 && std::isfinite(c->base) && c->eps >= 0.0 &&
+                    heads_ok(c->q_token, c->q_head, c->heads, c->D, c->tokens) &&
+                    heads_ok(c->k_token, c->k_head, c->kv_heads, c->D, c->tokens);
+    return ok ? DC_OK : DC_ERR_BAD_LAYER;
+}
+
+HeadNormArgs head_norm_args(const dc_head_norm_cfg *c)
+{
+    HeadNormArgs a = {};
+    a.token[0] = c->q_token;
+    a.token[1] = c->k_token;
+    a.head[0] = c->q_head;
+    a.head[1] = c->k_head;
+    a.heads[0] = c->heads;
+    a.heads[1] = c->kv_heads;
+    a.tokens = c->tokens;
+    a.D = c->D;
+    a.rotary = c->rotary;
+    a.interleaved = c->interleaved != 0;
+    a.norm = c->norm != 0;
+    a.eps = float(c->eps);
+    for (int i = 0; i < c->rotary / 2; ++i) {
+        const double turns = std::pow(c->base, -2.0 * i / c->rotary) * 0.15915494309189533577;  // 1 / (2 pi)
+        a.turns[i] = uint64_t((turns - std::floor(turns)) * 18446744073709551616.0);
+    }
+    return a;
+}
+
+dc_status check_attention(const dc_attention_shape *s)
+{
+    if (!s) return DC_ERR_NULL;
+    const bool ok = dtype_ok(s->dtype) && rows_ok(s->tokens) && s->sequences >= 0 &&
+                    s->sequences <= DC_SEQUENCES_MAX && count_ok(s->heads) && count_ok(s->kv_heads) &&
+                    s->heads % s->kv_heads == 0 && s->D >= 1 && s->D <= DC_ATTENTION_DIM_MAX &&
+                    std::isfinite(s->scale) && heads_ok(s->q_token, s->q_head, s->heads, s->D, s->tokens) &&
+                    heads_ok(s->k_token, s->k_head, s->kv_heads, s->D, s->tokens) &&
+                    heads_ok(s->v_token, s->v_head, s->kv_heads, s->D, s->tokens);
+    return ok ? DC_OK : DC_ERR_BAD_LAYER;
+}
+
+AttentionArgs attention_args(const dc_attention_shape *s, const void *q, const void *k, const void *v, const void *dy)
+{
+    AttentionArgs a = {};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.dy = dy;
+    a.q_token = s->q_token;
+    a.q_head = s->q_head;
+    a.k_token = s->k_token;
+    a.k_head = s->k_head;
+    a.v_token = s->v_token;
+    a.v_head = s->v_head;
+    a.dy_token = int64_t(s->heads) * s->D;
+    a.dy_head = s->D;
+    a.tokens = s->tokens;
+    a.heads = s->heads;
+    a.kv_heads = s->kv_heads;
+    a.group = s->heads / s->kv_heads;
+    a.D = s->D;
+    a.scale = float(s->scale);
     return a;
 }
 
@@ -282,6 +364,113 @@ dc_status dc_block_norm_grad(const dc_block_norm_cfg *cfg, const void *dy, const
     if (!f) a.alpha = 1.0f;
     return dc::result(
         dc::launch_norm_grad(cfg->dtype, a, static_cast<float *>(workspace), stream));
+}
+
+dc_status dc_head_norm_rotary(const dc_head_norm_cfg *cfg, const void *q, const void *k,
+                              const int64_t *positions, const void *w_q, const void *w_k,
+                              void *q_out, void *k_out, cudaStream_t stream)
+{
+    const dc::NvtxRange nvtx("dc_head_norm_rotary");
+    const dc_status st = dc::check_head_norm(cfg);
+    if (st != DC_OK) return st;
+    if (cfg->tokens == 0) return DC_OK;
+    if (!q || !k || !positions || !q_out || !k_out) return DC_ERR_NULL;
+    dc::HeadNormArgs a = dc::head_norm_args(cfg);
+    a.x[0] = q;
+    a.x[1] = k;
+    a.w[0] = w_q;
+    a.w[1] = w_k;
+    a.y[0] = q_out;
+    a.y[1] = k_out;
+    a.positions = positions;
+    return dc::result(dc::launch_head_norm(cfg->dtype, a, stream));
+}
+
+size_t dc_head_norm_rotary_grad_workspace_bytes(const dc_head_norm_cfg *cfg)
+{
+    if (dc::check_head_norm(cfg) != DC_OK || cfg->tokens == 0) return 0;
+    return dc::head_norm_workspace(cfg->D);
+}
+
+dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_out,
+                                   const void *dk_out, const void *q, const void *k,
+                                   const int64_t *positions, const void *w_q, const void *w_k,
+                                   void *dq, void *dk, float *dw_q, float *dw_k, void *workspace,
+                                   size_t workspace_bytes, cudaStream_t stream)
+{
+    const dc::NvtxRange nvtx("dc_head_norm_rotary_grad");
+    const dc_status st = dc::check_head_norm(cfg);
+    if (st != DC_OK) return st;
+    if (cfg->tokens == 0) {  // sums over no tokens
+        cudaError_t e = cudaSuccess;
+        if (dw_q) e = cudaMemsetAsync(dw_q, 0, sizeof(float) * cfg->D, stream);
+        if (dw_k && e == cudaSuccess) e = cudaMemsetAsync(dw_k, 0, sizeof(float) * cfg->D, stream);
+        return dc::result(e);
+    }
+    if (!dq_out || !dk_out || !q || !k || !positions || !dq || !dk) return DC_ERR_NULL;
+    const bool sums = dw_q || dw_k;
+    if (sums && (!workspace || workspace_bytes < dc::head_norm_workspace(cfg->D))) return DC_ERR_WORKSPACE;
+    dc::HeadNormArgs a = dc::head_norm_args(cfg);
+    a.x[0] = q;
+    a.x[1] = k;
+    a.dy[0] = dq_out;
+    a.dy[1] = dk_out;
+    a.w[0] = w_q;
+    a.w[1] = w_k;
+    a.y[0] = dq;
+    a.y[1] = dk;
+    a.dw[0] = dw_q;
+    a.dw[1] = dw_k;
+    a.positions = positions;
+    a.partial = sums ? static_cast<float *>(workspace) : nullptr;
+    return dc::result(dc::launch_head_norm_grad(cfg->dtype, a, stream));
+}
+
+size_t dc_attention_workspace_bytes(const dc_attention_shape *s, int32_t grad, const void *q,
+                                    const void *k, const void *v, const void *dy)
+{
+    if (dc::check_attention(s) != DC_OK || s->tokens == 0 || grad < 0 || grad > 1) return 0;
+    return dc::attention_workspace(s->dtype, dc::attention_args(s, q, k, v, dy), s->sequences, grad == 1);
+}
+
+dc_status dc_attention(const dc_attention_shape *s, const void *q, const void *k, const void *v,
+                       const int64_t *offsets, void *y, float *lse, int32_t *status,
+                       void *workspace, size_t workspace_bytes, cudaStream_t stream)
+{
+    const dc::NvtxRange nvtx("dc_attention");
+    const dc_status st = dc::check_attention(s);
+    if (st != DC_OK) return st;
+    if (s->tokens == 0) return DC_OK;
+    if (!q || !k || !v || !offsets || !y || !lse) return DC_ERR_NULL;
+    dc::AttentionArgs a = dc::attention_args(s, q, k, v, nullptr);
+    if (!workspace || workspace_bytes < dc::attention_workspace(s->dtype, a, s->sequences, false))
+        return DC_ERR_WORKSPACE;
+    a.y = y;
+    a.lse = lse;
+    a.status = status;
+    return dc::result(dc::launch_attention(s->dtype, a, s->sequences, offsets, false, workspace, stream));
+}
+
+dc_status dc_attention_grad(const dc_attention_shape *s, const void *dy, const void *q,
+                            const void *k, const void *v, const void *y, const float *lse,
+                            const int64_t *offsets, void *dq, void *dk, void *dv, int32_t *status,
+                            void *workspace, size_t workspace_bytes, cudaStream_t stream)
+{
+    const dc::NvtxRange nvtx("dc_attention_grad");
+    const dc_status st = dc::check_attention(s);
+    if (st != DC_OK) return st;
+    if (s->tokens == 0) return DC_OK;
+    if (!dy || !q || !k || !v || !y || !lse || !offsets || !dq || !dk || !dv) return DC_ERR_NULL;
+    dc::AttentionArgs a = dc::attention_args(s, q, k, v, dy);
+    if (!workspace || workspace_bytes < dc::attention_workspace(s->dtype, a, s->sequences, true))
+        return DC_ERR_WORKSPACE;
+    a.y = const_cast<void *>(y);
+    a.lse = const_cast<float *>(lse);
+    a.dq = dq;
+    a.dk = dk;
+    a.dv = dv;
+    a.status = status;
+    return dc::result(dc::launch_attention(s->dtype, a, s->sequences, offsets, true, workspace, stream));
 }
 
 dc_status dc_wait_probe(int32_t *status, cudaStream_t stream)

@@ -32,6 +32,7 @@ FWD, BWD = 0, 1
 DC_BF16, DC_FP16, DC_FP32 = 0, 1, 2
 DC_ACT_SILU, DC_ACT_GELU = 0, 1
 DC_NORM_RMS, DC_NORM_LAYER = 0, 1
+DC_HEADS_MAX, DC_HEAD_NORM_DIM_MAX, DC_ATTENTION_DIM_MAX, DC_SEQUENCES_MAX = 1024, 256, 128, 1048576
 DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX, DC_FEW_ROWS = 1024, 1048576, 16384, 4
 
 
@@ -71,12 +72,25 @@ class dc_block_norm_cfg(ctypes.Structure):
                 ("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_int64)]
 
 
+class dc_head_norm_cfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "D", "rotary", "interleaved", "norm")] + [
+        (n, ctypes.c_int64) for n in ("tokens", "q_token", "q_head", "k_token", "k_head")] + [
+        ("base", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class dc_attention_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "D", "sequences")] + [
+        (n, ctypes.c_int64) for n in ("tokens", "q_token", "q_head", "k_token", "k_head", "v_token", "v_head")] + [
+        ("scale", ctypes.c_double)]
+
+
 _lib = None
 
 # name -> (restype, argtypes); the exported C ABI
 _VP, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _F64, _U64 = ctypes.c_double, ctypes.c_uint64
 _SHAPE, _NORM = ctypes.POINTER(dc_expert_shape), ctypes.POINTER(dc_block_norm_cfg)
+_HEADS, _ATTENTION = ctypes.POINTER(dc_head_norm_cfg), ctypes.POINTER(dc_attention_shape)
 _SIGNATURES = {
     "dc_profile_gen": (_I32, [ctypes.POINTER(dc_profile_cfg), _VP, _VP, _VP, _VP, _VP, _VP]),
     "dc_schedule_workspace_bytes": (_SZ, [_I64, _I32]),
@@ -112,6 +126,12 @@ _SIGNATURES = {
     "dc_block_norm": (_I32, [_NORM, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
     "dc_block_norm_grad_workspace_bytes": (_SZ, [_NORM]),
     "dc_block_norm_grad": (_I32, [_NORM] + [_VP] * 13 + [_SZ, _VP]),
+    "dc_head_norm_rotary": (_I32, [_HEADS] + [_VP] * 8),
+    "dc_head_norm_rotary_grad_workspace_bytes": (_SZ, [_HEADS]),
+    "dc_head_norm_rotary_grad": (_I32, [_HEADS] + [_VP] * 12 + [_SZ, _VP]),
+    "dc_attention_workspace_bytes": (_SZ, [_ATTENTION, _I32] + [_VP] * 4),
+    "dc_attention": (_I32, [_ATTENTION] + [_VP] * 8 + [_SZ, _VP]),
+    "dc_attention_grad": (_I32, [_ATTENTION] + [_VP] * 12 + [_SZ, _VP]),
     "dc_wait_probe": (_I32, [_VP, _VP]),
 }
 

@@ -1,4 +1,5 @@
-"""Layer operators on torch tensors: the training block of a mixture of experts.
+"""Layer operators on torch tensors: the training block of a mixture of experts, its attention
+included.
 
 The cost rows of a schedule are a model's measured layer times; these are layers of large
 language models, forward and backward, whose times can be measured on this GPU
@@ -13,6 +14,8 @@ refused unless gradients are off (torch.no_grad()).
 * ``gated_unit``, ``gated_unit_grad``
 * ``dropout`` (its gradient is the same call on the gradient)
 * ``block_norm``, ``block_norm_grad``
+* ``head_norm_rotary``, ``head_norm_rotary_grad``
+* ``attention``, ``attention_grad``
 
 The operations are defined in include/dynacomm.h.
 """
@@ -365,3 +368,134 @@ def block_norm_grad(dy, dh, y, f=None, gate=None, w_post=None, w_pre=None, resid
          *[None if t is None else t.data_ptr() for t in out.values()], ws.data_ptr(), need)
     _used_on(ws, stream)
     return out
+
+
+# ------------------------------------------------- norms and rotation of queries and keys
+def _heads(name, t, like=None):
+    """tokens, heads, D and the token and head strides of a [tokens, heads, D] tensor whose heads
+    are contiguous; like: a tensor whose type, device, tokens and D it has."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected (the library takes device pointers)")
+    if t.dim() != 3:
+        raise ValueError(f"{name}: [tokens, heads, D] expected")
+    T, H, D = t.shape
+    if like is not None:
+        _like(name, t, like, (like.shape[0], H, like.shape[2]))
+    token, head, one = t.stride()
+    if D > 1 and one != 1:
+        raise ValueError(f"{name}: contiguous heads expected")
+    if H == 1:  # a dimension of one element has no stride of its own
+        head = D
+    if T == 1:
+        token = H * head
+    return T, H, D, token, head
+
+
+def _positions(positions, ref):
+    if positions.dtype is not torch.int64 or positions.shape != (ref.shape[0],) \
+            or positions.get_device() != ref.get_device() or not positions.is_contiguous():
+        raise ValueError(f"positions: {ref.shape[0]} contiguous int64 on {ref.device} expected")
+    return positions.data_ptr()
+
+
+def _head_norm(q, k, positions, w_q, w_k, rotary, base, interleaved, norm, eps):
+    """Checks; the configuration and the pointers of q, k, positions, w_q, w_k."""
+    T, H, D, qt, qh = _heads("q", q)
+    _, G, _, kt, kh = _heads("k", k, q)
+    _no_graph(q, k, w_q, w_k)
+    cfg = dc.dc_head_norm_cfg(_dtype(q), H, G, D, D // 2 * 2 if rotary is None else rotary, bool(interleaved),
+                              bool(norm), T, qt, qh, kt, kh, base, eps)
+    return ctypes.byref(cfg), (q.data_ptr(), k.data_ptr(), _positions(positions, q),
+                               _contiguous("w_q", w_q, q, (D,)), _contiguous("w_k", w_k, q, (D,)))
+
+
+def head_norm_rotary(q, k, positions, w_q=None, w_k=None, rotary=None, base=10000.0, interleaved=False,
+                     norm=True, eps=1e-6, stream=None):
+    """(q', k'), contiguous: each head's elements over their root mean square, times w_q or w_k [D]
+    (None: ones), then the first `rotary` elements (None: all, an odd D's last apart) turned by
+    position: pair i, (i, i + rotary / 2) or (2i, 2i + 1) if interleaved, by the angle
+    positions[token] * base ** (-2i / rotary). norm False: no norm, the weights and the rotation
+    alone. q [tokens, heads, D], k [tokens, kv_heads, D] with contiguous heads, any strides besides
+    (slices of a projection's output); positions int64 [tokens]; D up to 256."""
+    cfg, args = _head_norm(q, k, positions, w_q, w_k, rotary, base, interleaved, norm, eps)
+    qo, ko = (_empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    _run("dc_head_norm_rotary", q, stream, cfg, *args, qo.data_ptr(), ko.data_ptr())
+    return qo, ko
+
+
+def head_norm_rotary_grad(dq, dk, q, k, positions, w_q=None, w_k=None, rotary=None, base=10000.0,
+                          interleaved=False, norm=True, eps=1e-6, stream=None):
+    """Gradients of head_norm_rotary as a dict: dq, dk (of its inputs, contiguous), dw_q, dw_k
+    (float32 [D]; None where there was no weight), from dq, dk, those of its outputs (contiguous),
+    and the call's inputs."""
+    cfg, args = _head_norm(q, k, positions, w_q, w_k, rotary, base, interleaved, norm, eps)
+    _no_graph(dq, dk)
+    dqp, dkp = _contiguous("dq", dq, q, q.shape), _contiguous("dk", dk, k, k.shape)
+    D = q.shape[2]
+    out = {"dq": torch.empty_like(dq), "dk": torch.empty_like(dk)}
+    for name, w in (("dw_q", w_q), ("dw_k", w_k)):
+        out[name] = None if w is None else _empty(D, dtype=torch.float32, device=q.device)
+    sums = w_q is not None or w_k is not None
+    need = _function("dc_head_norm_rotary_grad_workspace_bytes")(cfg) if sums else 0
+    ws = _empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _run("dc_head_norm_rotary_grad", q, stream, cfg, dqp, dkp, *args,
+         *[None if t is None else t.data_ptr() for t in out.values()], ws.data_ptr() if need else None, need)
+    _used_on(ws, stream)
+    return out
+
+
+# ------------------------------------------------------------------------- attention
+def _attention(q, k, v, offsets, scale):
+    """Checks; the shape."""
+    T, H, D, qt, qh = _heads("q", q)
+    _, G, _, kt, kh = _heads("k", k, q)
+    _, Gv, _, vt, vh = _heads("v", v, q)
+    if Gv != G or G < 1 or H % G:
+        raise ValueError(f"k, v: as many heads each, and a divisor of q's {H}, expected, not {G} and {Gv}")
+    _no_graph(q, k, v)
+    if offsets.dim() != 1 or offsets.numel() < 1:
+        raise ValueError("offsets: [sequences + 1] expected")
+    sequences = offsets.numel() - 1
+    _offsets(offsets, sequences, q)
+    return ctypes.byref(dc.dc_attention_shape(_dtype(q), H, G, D, sequences, T, qt, qh, kt, kh, vt, vh,
+                                              D ** -0.5 if scale is None and D else scale or 0.0))
+
+
+def attention(q, k, v, offsets, scale=None, stream=None):
+    """(y, lse): causal attention of packed sequences. Row t belongs to sequence s for offsets[s] <= t
+    < offsets[s + 1] (int64 [sequences + 1]) and sees the rows of s up to itself; head h of q
+    [tokens, heads, D] reads head h // (heads // kv_heads) of k and v [tokens, kv_heads, D]. Scores
+    are q . k * scale (None: D ** -0.5); y [tokens, heads, D], and lse float32 [heads, tokens] is the
+    logarithm of each row's sum of exponentials, which the gradient takes. Rows of no sequence get
+    zeros. Heads contiguous, any strides besides; D up to 128."""
+    shape = _attention(q, k, v, offsets, scale)
+    T, H, D = q.shape
+    y = _empty((T, H, D), dtype=q.dtype, device=q.device)
+    lse = _empty((H, T), dtype=torch.float32, device=q.device)
+    ptrs = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    need = _function("dc_attention_workspace_bytes")(shape, 0, *ptrs, None)
+    ws = _empty(need, dtype=torch.uint8, device=q.device)
+    _run("dc_attention", q, stream, shape, *ptrs, offsets.data_ptr(), y.data_ptr(), lse.data_ptr(),
+         _status_of(q.get_device()), ws.data_ptr(), need)
+    _used_on(ws, stream)
+    return y, lse
+
+
+def attention_grad(dy, q, k, v, y, lse, offsets, scale=None, stream=None):
+    """(dq, dk, dv), contiguous, of attention from dy, the gradient of y (contiguous), the call's
+    inputs and its outputs y and lse."""
+    shape = _attention(q, k, v, offsets, scale)
+    T, H, D = q.shape
+    _no_graph(dy, y, lse)
+    dyp, yp = _contiguous("dy", dy, q, (T, H, D)), _contiguous("y", y, q, (T, H, D))
+    if lse.dtype is not torch.float32 or lse.shape != (H, T) or lse.get_device() != q.get_device() \
+            or not lse.is_contiguous():
+        raise ValueError(f"lse: contiguous float32 [{H}, {T}] on {q.device} expected")
+    dq, dk, dv = (_empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    ptrs = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    need = _function("dc_attention_workspace_bytes")(shape, 1, *ptrs, dyp)
+    ws = _empty(need, dtype=torch.uint8, device=q.device)
+    _run("dc_attention_grad", q, stream, shape, dyp, *ptrs, yp, lse.data_ptr(), offsets.data_ptr(), dq.data_ptr(),
+         dk.data_ptr(), dv.data_ptr(), _status_of(q.get_device()), ws.data_ptr(), need)
+    _used_on(ws, stream)
+    return dq, dk, dv
