@@ -52,6 +52,13 @@ __device__ __forceinline__ int64_t dealt(int64_t round, int64_t items)
     return i < items ? i : -1;
 }
 
+// csrc/attention_mma.cu, csrc/attention_grad_mma.cu: 16-bit types on the tensor cores, operands on 16-byte boundaries
+// with strides of whole 16 bytes.
+constexpr int kMmaRows = 128;
+int attention_mma_rows(const AttentionArgs &a);  // of a tile of the forward pass
+cudaError_t launch_attention_mma(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
+cudaError_t launch_attention_grad_mma(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
+
 // csrc/attention_simt.cu: floats, on the CUDA cores
 constexpr int kSimtRows = 64;
 cudaError_t launch_attention_simt(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);

@@ -1,0 +1,433 @@
+// Causal attention of 16-bit types on the tensor cores, forward.
+//
+// A CTA holds two tiles of 128 rows at a time: two heads of one key head, or, where the group
+// is odd, neighbouring tiles of one head. Keys and values come in blocks of 128 through a ring.
+// For each tile and block: scores S = q k^T [row][key] into tensor memory; four warps, a thread
+// a row, take the row's maximum and write P = 2^(s - m) in 16 bits over the scores; y += P v,
+// with P read from tensor memory and y held there. While one tile's warps are at their
+// exponentials the tensor cores work on the other tile.
+//
+//   warps 0-3, 4-7  a tile each: softmax, and the finished rows
+//   warp 8          copies (TMA)
+//   warp 9          products, by one thread
+//
+// Rounding: P is rounded to the operands' type for the tensor cores, at most half a step of each
+// term, where y's own rounding is half a step of the sum; l adds the unrounded ones in floats.
+// The reference m is not raised with every larger maximum but once it is 2^8 too low: P up to 256
+// is as good in 16 bits with a floating point, and y in tensor memory is seldom rescaled.
+//
+// A mask cuts only the block on the diagonal, the tile's last. Values there that are not finite
+// would reach rows that must not see them through 0 * inf. So rows after the sequence's end are overwritten
+// with zeros there, and the block's own are looked through: where one is not finite, that block's
+// y += P v is done by its own threads (masked_product).
+#include <cmath>
+
+#include "attention_mma.cuh"
+
+namespace dc {
+namespace {
+
+using namespace am;
+
+constexpr int kThreads = 10 * 32;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.0f;  // how far, in powers of two, the reference may be below the maximum
+
+struct Item {
+    AttentionTile tile;
+    int32_t head[2], row0[2], rows[2], blocks[2], kv;
+};
+
+template <bool PAIR>
+__device__ __forceinline__ Item item_at(const AttentionArgs &a, int64_t i)
+{
+    const int per = PAIR ? a.heads / 2 : a.heads;
+    Item q;
+    const int64_t t = i / per;
+    q.tile = plan_tiles(a.plan)[t];
+    const int h = int(i - t * per);
+    const int before = (q.tile.row0 - max(q.tile.first, 0)) / kTile;
+    if (PAIR) {
+        q.head[0] = 2 * h;
+        q.head[1] = 2 * h + 1;
+        q.row0[0] = q.row0[1] = q.tile.row0;
+        q.rows[0] = q.rows[1] = q.tile.rows;
+        q.blocks[0] = q.blocks[1] = before + 1;
+    } else {
+        q.head[0] = q.head[1] = h;
+        q.row0[0] = q.tile.row0;
+        q.row0[1] = q.tile.row0 + kTile;
+        q.rows[0] = min(kTile, q.tile.rows);
+        q.rows[1] = q.tile.rows - q.rows[0];
+        q.blocks[0] = before + 1;
+        q.blocks[1] = q.rows[1] > 0 ? before + 2 : 0;
+    }
+    if (q.tile.first < 0) q.blocks[0] = q.blocks[1] = 0;
+    q.kv = q.head[0] / a.group;
+    return q;
+}
+
+template <typename T, int DP, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                     const __grid_constant__ CUtensorMap map_v, const AttentionArgs a)
+{
+    constexpr int kBoxes = DP / 64;
+    constexpr uint32_t kBytes = kBoxes * kBox;  // of a tile in shared memory
+    constexpr int kStages = DP == 64 ? 8 : 4;
+    extern __shared__ unsigned char dyn[];
+    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_full[2], y_full[2], last;
+    __shared__ uint32_t tmem_at, gave_up, by_hand[2];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
+    const uint32_t base = (bw::smem_addr(dyn) + 1023u) & ~1023u;
+    const uint32_t ring = base + 2 * kBytes;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            bw::bar_init(bar(&q_full[i]), 1);
+            bw::bar_init(bar(&q_free[i]), 1);
+            bw::bar_init(bar(&s_full[i]), 1);
+            bw::bar_init(bar(&p_full[i]), 4);
+            bw::bar_init(bar(&y_full[i]), 1);
+            by_hand[i] = 0;
+        }
+        for (int i = 0; i < kStages; ++i) {
+            bw::bar_init(bar(&full[i]), 1);
+            bw::bar_init(bar(&empty[i]), 1);
+        }
+        bw::bar_init(bar(&last), 1);
+        gave_up = 0;
+        bw::bar_init_fence();
+    }
+    if (warp == 9) bw::tmem_alloc1(bw::smem_addr(&tmem_at), 512);
+    if (warp == 8 && lane == 0) {
+        bw::prefetch_map(&map_q);
+        bw::prefetch_map(&map_k);
+        bw::prefetch_map(&map_v);
+    }
+    bw::fence_before();
+    __syncthreads();
+    bw::fence_after();
+    const uint32_t tmem = tmem_at;  // scores of both tiles, then y of both
+    const int64_t items = int64_t(a.plan->tiles) * (PAIR ? a.heads / 2 : a.heads);
+
+    if (warp == 8) {
+        if (bw::elect_one()) {  // copies
+            int s = 0, done[2] = {0, 0};
+            uint32_t phase = 1;
+            bool ok = true;
+            auto block = [&](const CUtensorMap &map, int head, int row) {
+                ok = ok && bw::bar_wait(bar(&empty[s]), phase, &gave_up);
+                if (!ok) return;
+                bw::bar_arrive_bytes(bar(&full[s]), kBytes);
+                for (int i = 0; i < kBoxes; ++i)
+                    bw::copy_3d1(ring + s * kBytes + i * kBox, &map, 64 * i, head, row, bar(&full[s]));
+                if (++s == kStages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            };
+            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+                const Item q = item_at<PAIR>(a, i);
+                for (int x = 0; x < 2; ++x) {
+                    if (q.blocks[x] == 0) continue;
+                    ok = ok && (done[x] == 0 || bw::bar_wait(bar(&q_free[x]), (done[x] - 1) & 1, &gave_up));
+                    if (!ok) break;
+                    ++done[x];
+                    bw::bar_arrive_bytes(bar(&q_full[x]), kBytes);
+                    for (int b = 0; b < kBoxes; ++b)
+                        bw::copy_3d1(base + x * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&q_full[x]));
+                    if (x == 0) block(map_k, q.kv, q.tile.first);
+                }
+                const int n = max(q.blocks[0], q.blocks[1]);
+                for (int j = 0; j < n && ok; ++j) {
+                    if (j > 0) block(map_k, q.kv, q.tile.first + j * kTile);
+                    block(map_v, q.kv, q.tile.first + j * kTile);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (bw::elect_one()) {  // products
+            constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
+            const uint32_t shape_s = bw::f16_shape(kBf, false, false, kTile, kTile);
+            const uint32_t shape_y = bw::f16_shape(kBf, false, true, kTile, DP);
+            uint32_t c = 0;  // blocks of the ring before this item
+            int done[2] = {0, 0};
+            uint32_t p_phase[2] = {0, 0};
+            bool ok = true;
+            auto have = [&](uint32_t n) {
+                ok = ok && bw::bar_wait(bar(&full[n % kStages]), (n / kStages) & 1, &gave_up);
+                return ok;
+            };
+            auto scores = [&](int x, uint32_t n) {
+                const uint64_t dq = bw::operand(base + x * kBytes, 16), dk = bw::operand(ring + n % kStages * kBytes, 16);
+                bw::fence_after();
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {
+                    const uint64_t at = (i / 4) * (kBox >> 4) + (i % 4) * 2;
+                    bw::mma1(tmem + x * kTile, dq + at, dk + at, shape_s, i > 0);
+                }
+            };
+            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+                const Item q = item_at<PAIR>(a, i);
+                const int n = max(q.blocks[0], q.blocks[1]);
+                if (n == 0) continue;
+                for (int x = 0; x < 2 && ok; ++x) {
+                    if (q.blocks[x] == 0) continue;
+                    ok = bw::bar_wait(bar(&q_full[x]), done[x] & 1, &gave_up);
+                    ++done[x];
+                    if (!have(c)) break;
+                    scores(x, c);
+                    bw::commit1(bar(&s_full[x]));
+                    if (q.blocks[x] == 1) bw::commit1(bar(&q_free[x]));
+                }
+                bw::commit1(bar(&empty[c % kStages]));
+                for (int j = 0; j < n && ok; ++j) {
+                    const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
+                    if (!have(v)) break;
+                    for (int x = 0; x < 2 && ok; ++x) {
+                        if (j >= q.blocks[x]) continue;
+                        ok = bw::bar_wait(bar(&p_full[x]), p_phase[x], &gave_up);
+                        if (!ok) break;
+                        p_phase[x] ^= 1;
+                        bw::fence_after();
+                        if (!*const_cast<volatile uint32_t *>(&by_hand[x])) {
+                            const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
+#pragma unroll
+                            for (int i = 0; i < kTile / 16; ++i)
+                                bw::mma1_tmem(tmem + 2 * kTile + x * DP, tmem + x * kTile + i * 8, dv + i * 128, shape_y,
+                                              j > 0 || i > 0);
+                        }
+                        if (j + 1 < q.blocks[x]) {
+                            if (!have(k)) break;
+                            scores(x, k);
+                            bw::commit1(bar(&s_full[x]));
+                            if (j + 2 == q.blocks[x]) bw::commit1(bar(&q_free[x]));
+                        } else {
+                            bw::commit1(bar(&y_full[x]));
+                        }
+                    }
+                    bw::commit1(bar(&empty[v % kStages]));
+                    if (j + 1 < n) bw::commit1(bar(&empty[k % kStages]));
+                }
+                c += 2 * n;
+            }
+            // arrivals land in this CTA's memory: it may not end before the last
+            bw::commit1(bar(&last));
+            bw::bar_wait(bar(&last), 0, &gave_up);
+        }
+    } else {  // softmax and the finished rows
+        const int x = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
+        const uint32_t at_s = lanes + x * kTile, at_y = lanes + 2 * kTile + x * DP;
+        const bool wide = a.D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
+        // scores are compared before they are scaled: by a positive factor, after the sign (or zero)
+        const float sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
+        const float scale = (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * kLog2e;
+        uint32_t s_phase = 0, y_phase = 0, c = 0;
+        bool ok = true;
+        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+            const Item q = item_at<PAIR>(a, i);
+            const int n = q.blocks[x];
+            T *y = static_cast<T *>(a.y) + (int64_t(q.row0[x]) + r) * a.heads * a.D + int64_t(q.head[x]) * a.D;
+            float *lse = a.lse + q.head[x] * a.tokens + q.row0[x] + r;
+            if (n == 0) {
+                if (r < q.rows[x]) {  // of no sequence
+                    put_zeros(y, a.D, wide);
+                    *lse = 0.0f;
+                }
+                c += 2 * max(q.blocks[0], q.blocks[1]);
+                continue;
+            }
+            float m = -INFINITY, l = 0.0f;
+            for (int j = 0; j < n; ++j) {
+                ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&s_full[x]), s_phase, &gave_up));
+                if (!ok) break;
+                s_phase ^= 1;
+                bw::fence_after();
+                float s[kTile];
+                {
+                    float(&lo)[64] = *reinterpret_cast<float(*)[64]>(s), (&hi)[64] = *reinterpret_cast<float(*)[64]>(s + 64);
+                    bw::tmem_load(at_s, lo);
+                    bw::tmem_load(at_s + 64, hi);
+                }
+                if (sign != 1.0f) {
+#pragma unroll
+                    for (int e = 0; e < kTile; ++e) s[e] *= sign;
+                }
+                const bool diagonal = j == n - 1;
+                if (diagonal) {
+#pragma unroll
+                    for (int e = 0; e < kTile; ++e) s[e] = e <= r ? s[e] : -INFINITY;
+                }
+                float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                for (int e = 4; e < kTile; ++e) top[e & 3] = fmaxf(top[e & 3], s[e]);
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                const float raised = fmaxf(m, most);
+                // (a row by its own scores alone: its bits do not depend on its neighbours)
+                const bool low = !((raised - m) * scale <= kSlack);
+                if (__any_sync(0xffffffffu, low)) {
+                    // y is not in use: the products before these scores are done
+                    float old = 1.0f;
+                    if (low) {
+                        old = m == -INFINITY ? 0.0f : exp2_fast((m - raised) * scale);
+                        m = raised;
+                        l *= old;
+                    }
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int d = 0; d < DP; d += 32) {
+                            float v[32];
+                            bw::tmem_load(at_y + d, v);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] *= old;
+                            bw::tmem_store(at_y + d, v);
+                        }
+                    }
+                }
+                // nothing but -inf so far: any finite reference will do
+                const float2 minus = twice(m == -INFINITY ? 0.0f : -m * scale), by = twice(scale);
+                float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+                for (int e0 = 0; e0 < kTile; e0 += 32) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 t = __ffma2_rn(make_float2(s[e0 + e], s[e0 + e + 1]), by, minus);
+                        t.x = exp2_fast(t.x);
+                        t.y = exp2_fast(t.y);
+                        sum[e / 2 & 1] = __fadd2_rn(sum[e / 2 & 1], t);
+                        p[e / 2] = pack2(t.x, t.y, T());
+                    }
+                    bw::tmem_store(at_s + e0 / 2, p);
+                }
+                sum[0] = __fadd2_rn(sum[0], sum[1]);
+                l += sum[0].x + sum[0].y;
+                bw::tmem_stored();
+                if (diagonal) {
+                    const uint32_t v = c + 2 * j + 1;
+                    unsigned char *tile = dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes;
+                    ok = bw::bar_wait(bar(&full[v % kStages]), (v / kStages) & 1, &gave_up);
+                    const bool some = any_of_group(ok && look_through<T, DP>(tile, r, q.rows[x]), 1 + x);
+                    if (some)
+                        masked_product<T, DP>(at_y, [&](int g) { return at_s + g * 16; }, 4, tile, 0, 0, r + 1, j > 0);
+                    if ((warp & 3) == 0 && lane == 0) *const_cast<volatile uint32_t *>(&by_hand[x]) = some;
+                }
+                bw::fence_before();
+                __syncwarp();
+                if (lane == 0) bw::bar_arrive(bar(&p_full[x]));
+            }
+            c += 2 * max(q.blocks[0], q.blocks[1]);
+            ok = ok && bw::bar_wait(bar(&y_full[x]), y_phase, &gave_up);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            y_phase ^= 1;
+            bw::fence_after();
+            if ((warp & 3) == 0 && lane == 0) *const_cast<volatile uint32_t *>(&by_hand[x]) = 0;
+            const float by = 1.0f / l;
+#pragma unroll 1
+            for (int d = 0; d < DP; d += 32) {
+                float v[32];
+                __syncwarp();
+                bw::tmem_load(at_y + d, v);
+                if (r < q.rows[x]) put_row(y + d, v, by, a.D - d, wide);
+            }
+            if (r < q.rows[x]) *lse = (m * scale + log2f(l)) * kLn2;
+        }
+    }
+    __syncwarp();
+    if (*const_cast<volatile uint32_t *>(&gave_up)) {
+        // copies and products in flight still write this CTA's memory: let them end
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (threadIdx.x == 0 && a.status) *a.status = DC_ERR_INTERNAL;
+    }
+    bw::fence_before();
+    __syncthreads();
+    if (warp == 9) bw::tmem_free1(tmem, 512);
+}
+
+// ------------------------------------------------------------------------------ host
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) !=
+                cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return EncodeTiled(nullptr);
+        return EncodeTiled(p);
+    }();
+    return fn;
+}
+
+template <typename T, int DP, bool PAIR>
+cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    CUtensorMap q, k, v;
+    if (!am::heads_map(q, dtype, a.q, a.D, a.heads, a.tokens, a.q_head, a.q_token) ||
+        !am::heads_map(k, dtype, a.k, a.D, a.kv_heads, a.tokens, a.k_head, a.k_token) ||
+        !am::heads_map(v, dtype, a.v, a.D, a.kv_heads, a.tokens, a.v_head, a.v_token))
+        return cudaErrorInvalidValue;
+    auto kernel = attention_mma_kernel<T, DP, PAIR>;
+    constexpr size_t smem = (2 + (DP == 64 ? 8 : 4)) * size_t(DP / 64) * kBox + 1024;
+    static DeviceCache cache;
+    int ready = 0, sms = 0;
+    cudaError_t e = cache.get(ready, [&](int &n) {
+        n = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    });
+    if (e == cudaSuccess) e = sm_count(sms);
+    if (e != cudaSuccess) return e;
+    const int64_t items = most * (PAIR ? a.heads / 2 : a.heads);
+    kernel<<<unsigned(items < sms ? items : sms), kThreads, smem, stream>>>(q, k, v, a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+namespace am {
+
+bool heads_map(CUtensorMap &map, int dtype, const void *base, int32_t D, int32_t heads, int64_t tokens, int64_t head,
+               int64_t token)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    // a dimension of one element has no stride of its own, but it has to be valid
+    const int64_t row = (D + 7) / 8 * 8;
+    if (heads == 1) head = row;
+    if (tokens == 1) token = heads * head;
+    const cuuint64_t dims[3] = {cuuint64_t(D), cuuint64_t(heads), cuuint64_t(tokens)};
+    const cuuint64_t strides[2] = {cuuint64_t(head) * 2, cuuint64_t(token) * 2};
+    const cuuint32_t box[3] = {64, 1, kTile}, one[3] = {1, 1, 1};
+    return encode(&map, dtype == DC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                  const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace am
+
+// Two heads of a group at a time; tiles of two blocks where the group is odd.
+int attention_mma_rows(const AttentionArgs &a) { return a.group % 2 == 0 ? kMmaRows : 2 * kMmaRows; }
+
+cudaError_t launch_attention_mma(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    const bool pair = a.group % 2 == 0;
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        if (a.D <= 64)
+            return pair ? launch<T, 64, true>(dtype, a, most, stream) : launch<T, 64, false>(dtype, a, most, stream);
+        return pair ? launch<T, 128, true>(dtype, a, most, stream) : launch<T, 128, false>(dtype, a, most, stream);
+    };
+    return dtype == DC_BF16 ? go(__nv_bfloat16()) : go(__half());
+}
+
+}  // namespace dc

@@ -128,49 +128,116 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArg
     if (lane == 0) a.delta[h * a.tokens + t] = s;
 }
 
+// The tensor cores' copies need heads that start on 16-byte boundaries: others are copied to rows of
+// whole 16 bytes first, eight elements a thread.
+struct Heads {
+    const void *p;
+    int64_t token, head;
+    int32_t heads;
+};
+int64_t padded(int32_t D) { return (int64_t(D) + 7) / 8 * 8; }
+bool aligned(const Heads &h, int64_t tokens)
+{
+    return aligned16(h.p) && (tokens == 1 || h.token % 8 == 0) && (h.heads == 1 || h.head % 8 == 0);
+}
+__global__ void __launch_bounds__(256)
+align_heads_kernel(const uint16_t *x, uint16_t *to, int64_t units, int32_t heads, int32_t D, int32_t per, int64_t token,
+                   int64_t head)
+{
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= units) return;
+    const int64_t row = i / per, t = row / heads;
+    const int d = int(i - row * per) * 8;
+    const uint16_t *p = x + t * token + (row - t * heads) * head + d;
+    Vec<uint16_t, 8> v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.e[j] = d + j < D ? p[j] : uint16_t(0);
+    *reinterpret_cast<Vec<uint16_t, 8> *>(to + i * 8) = v;
+}
+
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Parts of the workspace.
-struct Layout {
-    size_t first, start, delta, total;
-};
-Layout layout(const AttentionArgs &a, int32_t sequences, int rows, bool grad)
+Heads operand(const AttentionArgs &a, int i)
 {
-    Layout l;
+    switch (i) {
+        case 0: return {a.q, a.q_token, a.q_head, a.heads};
+        case 1: return {a.k, a.k_token, a.k_head, a.kv_heads};
+        case 2: return {a.v, a.v_token, a.v_head, a.kv_heads};
+        default: return {a.dy, a.dy_token, a.dy_head, a.heads};
+    }
+}
+
+// Parts of the workspace; copy[i]: of operand i, where it needs one.
+struct Layout {
+    int rows;  // of a tile
+    size_t first, start, delta, copy[4], total;
+    bool copied[4];
+};
+Layout layout(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
+{
+    Layout l = {};
+    l.rows = dtype == DC_FP32 || grad ? kSimtRows : attention_mma_rows(a);
     size_t at = round256(sizeof(AttentionPlan) +
-                         sizeof(AttentionTile) * size_t(attention_most_tiles(a.tokens, sequences, rows)));
+                         sizeof(AttentionTile) * size_t(attention_most_tiles(a.tokens, sequences, l.rows)));
     l.first = at;
     at += round256(sizeof(int32_t) * (size_t(sequences) + 3));
     l.start = at;
     at += round256(sizeof(int32_t) * (size_t(sequences) + 3));
     l.delta = at;
     if (grad) at += round256(sizeof(float) * size_t(a.heads) * size_t(a.tokens));
+    for (int i = 0; i < (grad ? 4 : 3) && dtype != DC_FP32; ++i) {
+        const Heads h = operand(a, i);
+        l.copied[i] = !aligned(h, a.tokens);
+        l.copy[i] = at;
+        if (l.copied[i]) at += round256(size_t(a.tokens) * h.heads * padded(a.D) * 2);
+    }
     l.total = at;
     return l;
 }
 
-int tile_rows(int dtype, const AttentionArgs &, bool) { return kSimtRows; }
+cudaError_t align_operands(AttentionArgs &a, const Layout &l, unsigned char *ws, cudaStream_t stream)
+{
+    for (int i = 0; i < 4; ++i) {
+        if (!l.copied[i]) continue;
+        const Heads h = operand(a, i);
+        const int64_t pad = padded(a.D), units = a.tokens * h.heads * (pad / 8), blocks = (units + 255) / 256;
+        if (blocks > (int64_t(1) << 31) - 1) return cudaErrorInvalidValue;
+        uint16_t *to = reinterpret_cast<uint16_t *>(ws + l.copy[i]);
+        align_heads_kernel<<<unsigned(blocks), 256, 0, stream>>>(static_cast<const uint16_t *>(h.p), to, units, h.heads, a.D,
+                                                                 int(pad / 8), h.token, h.head);
+        const void **p[4] = {&a.q, &a.k, &a.v, &a.dy};
+        int64_t *token[4] = {&a.q_token, &a.k_token, &a.v_token, &a.dy_token};
+        int64_t *head[4] = {&a.q_head, &a.k_head, &a.v_head, &a.dy_head};
+        *p[i] = to;
+        *token[i] = h.heads * pad;
+        *head[i] = pad;
+    }
+    return cudaSuccess;
+}
 
 }  // namespace
 
 size_t attention_workspace(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
 {
-    return layout(a, sequences, tile_rows(dtype, a, grad), grad).total;
+    return layout(dtype, a, sequences, grad).total;
 }
 
 cudaError_t launch_attention(int dtype, AttentionArgs a, int32_t sequences, const int64_t *offsets, bool grad,
                              void *workspace, cudaStream_t stream)
 {
-    const int rows = tile_rows(dtype, a, grad);
-    const Layout l = layout(a, sequences, rows, grad);
+    const Layout l = layout(dtype, a, sequences, grad);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     AttentionPlan *plan = reinterpret_cast<AttentionPlan *>(ws);
-    attention_plan_kernel<<<1, kPlanThreads, 0, stream>>>(offsets, sequences, a.tokens, rows, plan,
+    attention_plan_kernel<<<1, kPlanThreads, 0, stream>>>(offsets, sequences, a.tokens, l.rows, plan,
                                                           reinterpret_cast<int32_t *>(ws + l.first),
                                                           reinterpret_cast<int32_t *>(ws + l.start));
     a.plan = plan;
-    const int64_t most = attention_most_tiles(a.tokens, sequences, rows);
-    if (!grad) return launch_attention_simt(dtype, a, most, stream);
+    const int64_t most = attention_most_tiles(a.tokens, sequences, l.rows);
+    if (!grad) {
+        if (dtype == DC_FP32) return launch_attention_simt(dtype, a, most, stream);
+        const cudaError_t e = align_operands(a, l, ws, stream);
+        return e == cudaSuccess ? launch_attention_mma(dtype, a, most, stream) : e;
+    }
     a.delta = reinterpret_cast<float *>(ws + l.delta);
     const int64_t blocks = (a.tokens * a.heads + 7) / 8;
     if (blocks > (int64_t(1) << 31) - 1) return cudaErrorInvalidValue;
