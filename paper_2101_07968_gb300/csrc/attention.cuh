@@ -61,7 +61,7 @@ cudaError_t launch_attention_grad_mma(int dtype, const AttentionArgs &a, int64_t
 
 // csrc/attention_simt.cu: floats, on the CUDA cores
 constexpr int kSimtRows = 64;
-cudaError_t launch_attention_simt(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
-cudaError_t launch_attention_grad_simt(int dtype, const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
+cudaError_t launch_attention_simt(const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
+cudaError_t launch_attention_grad_simt(const AttentionArgs &a, int64_t most_tiles, cudaStream_t stream);
 
 }  // namespace dc

@@ -1,0 +1,499 @@
+// The gradient of causal attention of 16-bit types on the tensor cores.
+//
+//   P = 2^(scale' S - lse'), dS = P (dy v^T - delta), delta = dy . y
+//   columns: a tile of 128 keys and a key head, over its group's heads and the rows from it on:
+//            S^T = k q^T, dP^T = v dy^T, dv += P^T dy, dk += dS^T q
+//   rows:    a tile of 128 rows and a head, over the keys up to it: S = q k^T, dP = dy v^T, dq += dS k
+// Seven products a block instead of the five that one pass would need: dq of one pass would be summed
+// by many CTAs, in memory and in an order that depends on timing; so each sum has one owner.
+//
+// Both are one kernel: two stationary tiles, two rings of moving ones (X: q or k, Y: dy or v), scores
+// and dP in tensor memory [128][128], the sums [128][D] beside them, 512 columns in all.
+//   warps 0-7  a lane a row, four warps either half of the columns: P, then dS, in 16 bits over what
+//              they were made of (A operands may lie in tensor memory)
+//   warp 8     copies (TMA)       warp 9  products, by one thread
+//   warp 10    columns: lse and delta of each block's rows
+// The products of one kind run while the warps make the other: S of the next block and dv beside dS,
+// dP of the next block and dk beside P.
+//
+// Rounding: P and dS are rounded to the operands' type for the tensor cores, half a step of each
+// term. Halves have few exponents: P, at most 1, is held 2^8 times larger, and dS in a power of two
+// that no |dP - delta| <= 2 D max|dy| max|v| can overflow, known from a pass over dy and v; both are undone
+// in floats at the end. What a mask hides is zero by selection, and operands' rows behind it are
+// looked through as in the forward pass.
+#include <cmath>
+
+#include "attention_mma.cuh"
+
+namespace dc {
+namespace {
+
+using namespace am;
+
+constexpr int kThreads = 11 * 32;
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <int DP, bool COLUMNS>
+struct Shape {
+    static constexpr uint32_t kBytes = DP / 64 * kBox;
+    static constexpr int kX = DP == 64 ? 4 : 3, kY = DP == 64 ? 4 : 2, kL = 2;
+    static constexpr uint32_t kTiles = (2 + kX + kY) * kBytes;
+    static constexpr uint32_t kStats = COLUMNS ? kL * 2 * kTile * sizeof(float) : 0;
+    static constexpr uint32_t kBars = 512;
+    static constexpr uint32_t kSmem = kTiles + kStats + kBars;
+};
+
+// A block of columns: its first row (key), how many there are of it, the head, and whether the mask cuts it.
+struct Step {
+    int32_t head, c0, count;
+    bool diagonal;
+};
+template <bool COLUMNS>
+struct Item {
+    AttentionTile t;
+    int32_t outer, kv, per_head, steps;
+    __device__ __forceinline__ Step step(const AttentionArgs &a, int i) const
+    {
+        Step s;
+        if (COLUMNS) {
+            const int k = i / per_head, j = i - k * per_head;
+            s.head = outer * a.group + k;
+            s.c0 = t.row0 + j * kTile;
+            s.count = min(kTile, t.end - s.c0);
+            s.diagonal = j == 0;
+        } else {
+            s.head = outer;
+            s.c0 = t.first + i * kTile;
+            s.count = min(kTile, t.row0 + t.rows - s.c0);
+            s.diagonal = i == steps - 1;
+        }
+        return s;
+    }
+};
+template <bool COLUMNS>
+__device__ __forceinline__ Item<COLUMNS> item_at(const AttentionArgs &a, int64_t i)
+{
+    const int outer = COLUMNS ? a.kv_heads : a.heads;
+    Item<COLUMNS> q;
+    const int64_t at = i / outer;
+    q.t = plan_tiles(a.plan)[at];
+    q.outer = int(i - at * outer);
+    q.kv = COLUMNS ? q.outer : q.outer / a.group;
+    if (q.t.first < 0) {
+        q.per_head = q.steps = 0;
+        return q;
+    }
+    const int n = (q.t.end - q.t.first + kTile - 1) / kTile, before = (q.t.row0 - q.t.first) / kTile;
+    if (COLUMNS) {  // tile i from the end has the work of tile i from the start
+        q.t.row0 = q.t.first + (n - 1 - before) * kTile;
+        q.t.rows = min(kTile, q.t.end - q.t.row0);
+        q.per_head = before + 1;
+        q.steps = q.per_head * a.group;
+    } else {
+        q.per_head = q.steps = before + 1;
+    }
+    return q;
+}
+
+// The power of two that dS of halves is held in.
+template <typename T>
+__device__ __forceinline__ int half_power(const AttentionArgs &a)
+{
+    if constexpr (!std::is_same<T, __half>::value) return 0;
+    const float top = 2.0f * float(a.D) * __uint_as_float(a.plan->top_do) * __uint_as_float(a.plan->top_v);
+    return top > 0.0f ? min(max(15 - (ilogbf(top) + 1), -96), 96) : 0;
+}
+
+template <typename T, int DP, bool COLUMNS>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                          const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_dy,
+                          const AttentionArgs a)
+{
+    using G = Shape<DP, COLUMNS>;
+    constexpr int kBoxes = DP / 64;
+    constexpr uint32_t kBytes = G::kBytes;
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    constexpr int kPPower = kHalf && COLUMNS ? 8 : 0;  // P is held 2^kPPower times larger
+    extern __shared__ __align__(1024) unsigned char dyn[];
+    struct Bars {
+        uint64_t still_full, still_free, x_full[G::kX], x_free[G::kX], y_full[G::kY], y_free[G::kY], l_full[G::kL],
+            l_free[G::kL], s_full, p_full, dp_full, ds_full, sums_full, met, last;
+        uint32_t tmem_at, gave_up;
+        uint32_t by_hand[2];  // block n, counted from one, if its sums are done by hand: in turn
+    };
+    static_assert(sizeof(Bars) <= G::kBars, "barriers' room");
+    Bars &b = *reinterpret_cast<Bars *>(dyn + G::kTiles + G::kStats);
+    float *const stats = reinterpret_cast<float *>(dyn + G::kTiles);  // [kL][lse, delta][128]
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto bar = [](uint64_t *p) { return bw::smem_addr(p); };
+    const uint32_t base = bw::smem_addr(dyn), ring_x = base + 2 * kBytes, ring_y = ring_x + G::kX * kBytes;
+    uint32_t *const gave_up = &b.gave_up;
+
+    if (threadIdx.x == 0) {
+        bw::bar_init(bar(&b.still_full), 1);
+        bw::bar_init(bar(&b.still_free), 1);
+        for (int i = 0; i < G::kX; ++i) {
+            bw::bar_init(bar(&b.x_full[i]), 1);
+            bw::bar_init(bar(&b.x_free[i]), 1);
+        }
+        for (int i = 0; i < G::kY; ++i) {
+            bw::bar_init(bar(&b.y_full[i]), 1);
+            bw::bar_init(bar(&b.y_free[i]), 1);
+        }
+        for (int i = 0; i < G::kL; ++i) {
+            bw::bar_init(bar(&b.l_full[i]), 1);
+            bw::bar_init(bar(&b.l_free[i]), 8);
+        }
+        bw::bar_init(bar(&b.s_full), 1);
+        bw::bar_init(bar(&b.p_full), 8);
+        bw::bar_init(bar(&b.dp_full), 1);
+        bw::bar_init(bar(&b.ds_full), 8);
+        bw::bar_init(bar(&b.sums_full), 1);
+        bw::bar_init(bar(&b.met), 8);
+        bw::bar_init(bar(&b.last), 1);
+        b.gave_up = b.by_hand[0] = b.by_hand[1] = 0;
+        bw::bar_init_fence();
+    }
+    if (warp == 9) bw::tmem_alloc1(bw::smem_addr(&b.tmem_at), 512);
+    if (warp == 8 && lane == 0) {
+        bw::prefetch_map(&map_q);
+        bw::prefetch_map(&map_k);
+        bw::prefetch_map(&map_v);
+        bw::prefetch_map(&map_dy);
+    }
+    bw::fence_before();
+    __syncthreads();
+    bw::fence_after();
+    const uint32_t tmem = b.tmem_at;
+    constexpr uint32_t kDp = kTile, kSum1 = 2 * kTile, kSum0 = kSum1 + (COLUMNS ? DP : 0);  // columns
+    // A operand of step i of eight: pairs of 16 columns; the halves are 64 columns apart
+    auto packed_at = [](int i) { return uint32_t(i / 4 * 64 + i % 4 * 8); };
+    auto by_hand = [&](uint32_t n) { return *const_cast<volatile uint32_t *>(&b.by_hand[n & 1]) == n + 1; };
+    // the swizzled copies need tiles on 1,024-byte boundaries
+    const int64_t items = (base & 1023u) ? 0 : int64_t(a.plan->tiles) * (COLUMNS ? a.kv_heads : a.heads);
+    if ((base & 1023u) && threadIdx.x == 0) b.gave_up = 1;
+
+    if (warp == 8) {
+        if (bw::elect_one()) {  // copies
+            int done = 0;
+            uint32_t nx = 0, ny = 0;
+            bool ok = true;
+            auto tile = [&](uint32_t to, const CUtensorMap &map, int head, int row, uint32_t full) {
+                for (int i = 0; i < kBoxes; ++i) bw::copy_3d1(to + i * kBox, &map, 64 * i, head, row, full);
+            };
+            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+                const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
+                if (q.steps == 0) continue;
+                ok = done == 0 || bw::bar_wait(bar(&b.still_free), (done - 1) & 1, gave_up);
+                if (!ok) break;
+                ++done;
+                bw::bar_arrive_bytes(bar(&b.still_full), 2 * kBytes);
+                tile(base, COLUMNS ? map_k : map_q, COLUMNS ? q.kv : q.outer, q.t.row0, bar(&b.still_full));
+                tile(base + kBytes, COLUMNS ? map_v : map_dy, COLUMNS ? q.kv : q.outer, q.t.row0, bar(&b.still_full));
+                for (int j = 0; j < q.steps; ++j) {
+                    const Step s = q.step(a, j);
+                    const int head = COLUMNS ? s.head : q.kv;
+                    const uint32_t x = nx % G::kX, y = ny % G::kY;
+                    ok = nx < G::kX || bw::bar_wait(bar(&b.x_free[x]), (nx / G::kX - 1) & 1, gave_up);
+                    if (!ok) break;
+                    bw::bar_arrive_bytes(bar(&b.x_full[x]), kBytes);
+                    tile(ring_x + x * kBytes, COLUMNS ? map_q : map_k, head, s.c0, bar(&b.x_full[x]));
+                    ++nx;
+                    ok = ny < G::kY || bw::bar_wait(bar(&b.y_free[y]), (ny / G::kY - 1) & 1, gave_up);
+                    if (!ok) break;
+                    bw::bar_arrive_bytes(bar(&b.y_full[y]), kBytes);
+                    tile(ring_y + y * kBytes, COLUMNS ? map_dy : map_v, head, s.c0, bar(&b.y_full[y]));
+                    ++ny;
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (bw::elect_one()) {  // products
+            constexpr bool kBf = !kHalf;
+            const uint32_t shape_s = bw::f16_shape(kBf, false, false, kTile, kTile);
+            const uint32_t shape_d = bw::f16_shape(kBf, false, true, kTile, DP);
+            int done = 0;
+            uint32_t n = 0;  // blocks so far
+            bool ok = true;
+            auto x_there = [&](uint32_t m) { return ok = ok && bw::bar_wait(bar(&b.x_full[m % G::kX]), (m / G::kX) & 1, gave_up); };
+            auto y_there = [&](uint32_t m) { return ok = ok && bw::bar_wait(bar(&b.y_full[m % G::kY]), (m / G::kY) & 1, gave_up); };
+            auto scores = [&](uint32_t d, uint32_t still, uint32_t moving) {
+                const uint64_t da = bw::operand(still, 16), db = bw::operand(moving, 16);
+                bw::fence_after();
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {
+                    const uint64_t at = (i / 4) * (kBox >> 4) + (i % 4) * 2;
+                    bw::mma1(tmem + d, da + at, db + at, shape_s, i > 0);
+                }
+            };
+            auto sums = [&](uint32_t d, uint32_t packed, uint32_t moving, bool add) {
+                const uint64_t db = bw::operand(moving, kBox);
+#pragma unroll
+                for (int i = 0; i < kTile / 16; ++i)
+                    bw::mma1_tmem(tmem + d, tmem + packed + packed_at(i), db + i * 128, shape_d, add || i > 0);
+            };
+            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+                const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
+                if (q.steps == 0) continue;
+                ok = bw::bar_wait(bar(&b.still_full), done & 1, gave_up);
+                ++done;
+                auto first = [&](uint32_t m) {  // S of block m
+                    if (!x_there(m)) return;
+                    scores(0, base, ring_x + m % G::kX * kBytes);
+                    bw::commit1(bar(&b.s_full));
+                };
+                auto second = [&](uint32_t m, bool end) {  // dP
+                    if (!y_there(m)) return;
+                    scores(kDp, base + kBytes, ring_y + m % G::kY * kBytes);
+                    bw::commit1(bar(&b.dp_full));
+                    if (!COLUMNS) bw::commit1(bar(&b.y_free[m % G::kY]));
+                    if (end) bw::commit1(bar(&b.still_free));
+                };
+                first(n);
+                second(n, q.steps == 1);
+                for (int j = 0; j < q.steps && ok; ++j, ++n) {
+                    ok = bw::bar_wait(bar(&b.p_full), n & 1, gave_up);
+                    if (!ok) break;
+                    bw::fence_after();
+                    if (COLUMNS) {
+                        if (!by_hand(n)) sums(kSum1, 0, ring_y + n % G::kY * kBytes, j > 0);
+                        bw::commit1(bar(&b.y_free[n % G::kY]));
+                    }
+                    if (j + 1 < q.steps) first(n + 1);
+                    ok = ok && bw::bar_wait(bar(&b.ds_full), n & 1, gave_up);
+                    if (!ok) break;
+                    bw::fence_after();
+                    if (!by_hand(n)) sums(kSum0, kDp, ring_x + n % G::kX * kBytes, j > 0);
+                    bw::commit1(bar(&b.x_free[n % G::kX]));
+                    if (j + 1 < q.steps) second(n + 1, j + 2 == q.steps);
+                }
+                if (ok) bw::commit1(bar(&b.sums_full));
+            }
+            // arrivals land in this CTA's memory: it may not end before the last
+            bw::commit1(bar(&b.last));
+            bw::bar_wait(bar(&b.last), 0, gave_up);
+        }
+    } else if (warp == 10) {
+        if (COLUMNS) {  // lse and delta, as the warps use them
+            const float f = ldexpf(1.0f, half_power<T>(a) - kPPower);
+            uint32_t n = 0;
+            bool ok = true;
+            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+                const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
+                for (int j = 0; j < q.steps; ++j, ++n) {
+                    const Step s = q.step(a, j);
+                    const int64_t at = s.head * a.tokens + s.c0;
+                    float l[4], d[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = lane + 32 * k;
+                        l[k] = c < s.count ? a.lse[at + c] : 0.0f;
+                        d[k] = c < s.count ? a.delta[at + c] : 0.0f;
+                    }
+                    ok = n < G::kL || bw::bar_wait(bar(&b.l_free[n % G::kL]), (n / G::kL - 1) & 1, gave_up);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    float *to = stats + n % G::kL * 2 * kTile;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        to[lane + 32 * k] = -l[k] * kLog2e + float(kPPower);
+                        to[kTile + lane + 32 * k] = -d[k] * f;
+                    }
+                    __syncwarp();
+                    if (lane == 0) bw::bar_arrive(bar(&b.l_full[n % G::kL]));
+                }
+            }
+        }
+    } else {  // P, dS and the finished sums
+        const int side = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
+        const uint32_t at_s = lanes + side * 64, at_dp = at_s + kDp;
+        const int power = half_power<T>(a);
+        const float f = ldexpf(1.0f, power - kPPower), scale = a.scale * kLog2e;
+        const float by0 = a.scale * ldexpf(1.0f, -power), by1 = ldexpf(1.0f, -kPPower);
+        const bool wide = a.D % 8 == 0 && ((reinterpret_cast<uintptr_t>(COLUMNS ? a.dk : a.dq) |
+                                            reinterpret_cast<uintptr_t>(COLUMNS ? a.dv : a.dq)) & 15) == 0;
+        const float2 by = twice(scale), fs = twice(f);
+        uint32_t n = 0, finished = 0;
+        bool ok = true;
+        uint32_t meetings = 0;
+        auto meet = [&] {  // all eight warps
+            bw::fence_before();
+            __syncwarp();
+            if (lane == 0) bw::bar_arrive(bar(&b.met));
+            ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.met), meetings++ & 1, gave_up) && ok);
+            bw::fence_after();
+        };
+        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+            const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
+            const int64_t row = (int64_t(q.t.row0) + r) * (COLUMNS ? a.kv_heads : a.heads) * a.D + int64_t(q.outer) * a.D;
+            T *const out = static_cast<T *>(!COLUMNS ? a.dq : side ? a.dk : a.dv) + row;
+            if (q.steps == 0) {  // rows of no sequence
+                if (r < q.t.rows && (COLUMNS || side == 0)) put_zeros(out, a.D, wide);
+                continue;
+            }
+            float2 lse = {}, delta = {};
+            if (!COLUMNS) {
+                const int64_t at = q.outer * a.tokens + q.t.row0 + r;
+                const bool there = r < q.t.rows;
+                lse = twice(there ? -a.lse[at] * kLog2e : 0.0f);
+                delta = twice(there ? -a.delta[at] * f : 0.0f);
+            }
+            for (int j = 0; j < q.steps; ++j, ++n) {
+                const Step s = q.step(a, j);
+                const float *const l = stats + n % G::kL * 2 * kTile + side * 64;
+                ok = bw::bar_wait(bar(&b.s_full), n & 1, gave_up);
+                if (COLUMNS) ok = ok && bw::bar_wait(bar(&b.l_full[n % G::kL]), (n / G::kL) & 1, gave_up);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                bw::fence_after();
+                // columns of this side that count: rows from the key on, or keys up to the row
+                const bool cut = s.diagonal || (COLUMNS && s.count < kTile);
+                const int from = (COLUMNS && s.diagonal ? r : 0) - side * 64;
+                const int end = (!COLUMNS && s.diagonal ? r + 1 : s.count) - side * 64;
+                float p[64];
+                bw::tmem_load(at_s, p);
+#pragma unroll
+                for (int e0 = 0; e0 < 64; e0 += 32) {
+                    uint32_t out16[16];
+#pragma unroll
+                    for (int e = e0; e < e0 + 32; e += 2) {
+                        const float2 minus = COLUMNS ? *reinterpret_cast<const float2 *>(l + e) : lse;
+                        const float2 t = __ffma2_rn(make_float2(p[e], p[e + 1]), by, minus);
+                        p[e] = exp2_fast(t.x);
+                        p[e + 1] = exp2_fast(t.y);
+                        if (cut) {
+                            p[e] = e >= from && e < end ? p[e] : 0.0f;
+                            p[e + 1] = e + 1 >= from && e + 1 < end ? p[e + 1] : 0.0f;
+                        }
+                        if (COLUMNS) out16[(e - e0) / 2] = pack2(p[e], p[e + 1], T());
+                    }
+                    if (COLUMNS) bw::tmem_store(at_s + e0 / 2, out16);
+                }
+                if (COLUMNS) bw::tmem_stored();
+                bool some = false;
+                unsigned char *const tile_x = dyn + (2 + n % G::kX) * kBytes, *const tile_y = dyn + (2 + G::kX + n % G::kY) * kBytes;
+                if (cut) {
+                    // rows behind the mask: of X, and of Y where it is summed too
+                    const bool x = COLUMNS ? side == 1 : side == 0, y = COLUMNS && side == 0;
+                    if (x) ok = bw::bar_wait(bar(&b.x_full[n % G::kX]), (n / G::kX) & 1, gave_up);
+                    if (y) ok = bw::bar_wait(bar(&b.y_full[n % G::kY]), (n / G::kY) & 1, gave_up);
+                    const bool bad = ok && (x || y) && look_through<T, DP>(x ? tile_x : tile_y, r, s.count);
+                    if (s.diagonal) {
+                        if (bad) *const_cast<volatile uint32_t *>(&b.by_hand[n & 1]) = n + 1;
+                        meet();
+                        some = by_hand(n);
+                    }
+                }
+                if (COLUMNS && some && side == 0)
+                    masked_product<T, DP>(lanes + kSum1, [&](int g) { return lanes + packed_at(2 * g); }, 4, tile_y, 0,
+                                          r, s.count, j > 0);
+                bw::fence_before();
+                __syncwarp();
+                if (lane == 0) bw::bar_arrive(bar(&b.p_full));
+                ok = __all_sync(0xffffffffu, ok && bw::bar_wait(bar(&b.dp_full), n & 1, gave_up));
+                if (!ok) break;
+                bw::fence_after();
+#pragma unroll
+                for (int e0 = 0; e0 < 64; e0 += 32) {
+                    float d[32];
+                    bw::tmem_load(at_dp + e0, d);
+                    uint32_t out16[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 minus = COLUMNS ? *reinterpret_cast<const float2 *>(l + kTile + e0 + e) : delta;
+                        float2 t = __ffma2_rn(make_float2(d[e], d[e + 1]), fs, minus);
+                        t = __fmul2_rn(t, make_float2(p[e0 + e], p[e0 + e + 1]));
+                        if (cut) {
+                            t.x = e0 + e >= from && e0 + e < end ? t.x : 0.0f;
+                            t.y = e0 + e + 1 >= from && e0 + e + 1 < end ? t.y : 0.0f;
+                        }
+                        out16[e / 2] = pack2(t.x, t.y, T());
+                    }
+                    bw::tmem_store(at_dp + e0 / 2, out16);
+                }
+                bw::tmem_stored();
+                if (some) {
+                    meet();
+                    if (side == (COLUMNS ? 1 : 0))
+                        masked_product<T, DP>(lanes + kSum0, [&](int g) { return lanes + kDp + packed_at(2 * g); }, 4, tile_x,
+                                              0, COLUMNS ? r : 0, COLUMNS ? s.count : r + 1, j > 0);
+                }
+                bw::fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (COLUMNS) bw::bar_arrive(bar(&b.l_free[n % G::kL]));
+                    bw::bar_arrive(bar(&b.ds_full));
+                }
+            }
+            ok = ok && bw::bar_wait(bar(&b.sums_full), finished & 1, gave_up);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            ++finished;
+            bw::fence_after();
+            constexpr int kCols = COLUMNS ? DP : DP / 2;  // of a thread
+            const int d0 = COLUMNS ? 0 : side * kCols;
+            const uint32_t from = lanes + (COLUMNS && side == 0 ? kSum1 : kSum0) + d0;
+#pragma unroll 1
+            for (int d = 0; d < kCols; d += 32) {
+                float v[32];
+                __syncwarp();
+                bw::tmem_load(from + d, v);
+                if (r < q.t.rows) put_row(out + d0 + d, v, COLUMNS && side == 0 ? by1 : by0, a.D - d0 - d, wide);
+            }
+        }
+    }
+    __syncwarp();
+    if (*const_cast<volatile uint32_t *>(gave_up)) {
+        // copies and products in flight still write this CTA's memory: let them end
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (threadIdx.x == 0 && a.status) *a.status = DC_ERR_INTERNAL;
+    }
+    bw::fence_before();
+    __syncthreads();
+    if (warp == 9) bw::tmem_free1(tmem, 512);
+}
+
+// ------------------------------------------------------------------------------ host
+template <typename T, int DP, bool COLUMNS>
+cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    CUtensorMap q, k, v, dy;
+    if (!heads_map(q, dtype, a.q, a.D, a.heads, a.tokens, a.q_head, a.q_token) ||
+        !heads_map(k, dtype, a.k, a.D, a.kv_heads, a.tokens, a.k_head, a.k_token) ||
+        !heads_map(v, dtype, a.v, a.D, a.kv_heads, a.tokens, a.v_head, a.v_token) ||
+        !heads_map(dy, dtype, a.dy, a.D, a.heads, a.tokens, a.dy_head, a.dy_token))
+        return cudaErrorInvalidValue;
+    auto kernel = attention_grad_mma_kernel<T, DP, COLUMNS>;
+    constexpr int smem = int(Shape<DP, COLUMNS>::kSmem);
+    static_assert(smem <= 232448, "shared memory of a CTA");
+    static DeviceCache cache;
+    int ready = 0, sms = 0;
+    cudaError_t e = cache.get(ready, [&](int &n) {
+        n = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    });
+    if (e == cudaSuccess) e = sm_count(sms);
+    if (e != cudaSuccess) return e;
+    const int64_t items = most * (COLUMNS ? a.kv_heads : a.heads);
+    kernel<<<unsigned(items < sms ? items : sms), kThreads, smem, stream>>>(q, k, v, dy, a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attention_grad_mma(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        cudaError_t e = a.D <= 64 ? launch<T, 64, true>(dtype, a, most, stream) : launch<T, 128, true>(dtype, a, most, stream);
+        if (e == cudaSuccess)
+            e = a.D <= 64 ? launch<T, 64, false>(dtype, a, most, stream) : launch<T, 128, false>(dtype, a, most, stream);
+        return e;
+    };
+    return dtype == DC_BF16 ? go(__nv_bfloat16()) : go(__half());
+}
+
+}  // namespace dc

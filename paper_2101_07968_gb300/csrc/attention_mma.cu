@@ -76,8 +76,9 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     constexpr uint32_t kBytes = kBoxes * kBox;  // of a tile in shared memory
     constexpr int kStages = DP == 64 ? 8 : 4;
     extern __shared__ unsigned char dyn[];
-    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_full[2], y_full[2], last;
-    __shared__ uint32_t tmem_at, gave_up, by_hand[2];
+    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_full[2], y_full[2], met[2], last;
+    __shared__ uint32_t tmem_at, gave_up;
+    __shared__ uint32_t by_hand[2];  // a tile's block, counted from one, if its sums are done by hand
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
@@ -91,6 +92,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             bw::bar_init(bar(&s_full[i]), 1);
             bw::bar_init(bar(&p_full[i]), 4);
             bw::bar_init(bar(&y_full[i]), 1);
+            bw::bar_init(bar(&met[i]), 4);
             by_hand[i] = 0;
         }
         for (int i = 0; i < kStages; ++i) {
@@ -155,7 +157,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const uint32_t shape_y = bw::f16_shape(kBf, false, true, kTile, DP);
             uint32_t c = 0;  // blocks of the ring before this item
             int done[2] = {0, 0};
-            uint32_t p_phase[2] = {0, 0};
+            uint32_t blocks[2] = {0, 0};  // of either tile so far
             bool ok = true;
             auto have = [&](uint32_t n) {
                 ok = ok && bw::bar_wait(bar(&full[n % kStages]), (n / kStages) & 1, &gave_up);
@@ -189,11 +191,10 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (!have(v)) break;
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (j >= q.blocks[x]) continue;
-                        ok = bw::bar_wait(bar(&p_full[x]), p_phase[x], &gave_up);
+                        ok = bw::bar_wait(bar(&p_full[x]), blocks[x]++ & 1, &gave_up);
                         if (!ok) break;
-                        p_phase[x] ^= 1;
                         bw::fence_after();
-                        if (!*const_cast<volatile uint32_t *>(&by_hand[x])) {
+                        if (*const_cast<volatile uint32_t *>(&by_hand[x]) != blocks[x]) {
                             const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
 #pragma unroll
                             for (int i = 0; i < kTile / 16; ++i)
@@ -226,7 +227,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         // scores are compared before they are scaled: by a positive factor, after the sign (or zero)
         const float sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
         const float scale = (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * kLog2e;
-        uint32_t s_phase = 0, y_phase = 0, c = 0;
+        uint32_t blocks = 0, finished = 0, c = 0;  // blocks and rounds of this tile; blocks of the ring
         bool ok = true;
         for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
             const Item q = item_at<PAIR>(a, i);
@@ -243,9 +244,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < n; ++j) {
-                ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&s_full[x]), s_phase, &gave_up));
+                ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&s_full[x]), blocks++ & 1, &gave_up));
                 if (!ok) break;
-                s_phase ^= 1;
                 bw::fence_after();
                 float s[kTile];
                 {
@@ -311,22 +311,22 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     const uint32_t v = c + 2 * j + 1;
                     unsigned char *tile = dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes;
                     ok = bw::bar_wait(bar(&full[v % kStages]), (v / kStages) & 1, &gave_up);
-                    const bool some = any_of_group(ok && look_through<T, DP>(tile, r, q.rows[x]), 1 + x);
-                    if (some)
+                    if (ok && look_through<T, DP>(tile, r, q.rows[x])) *const_cast<volatile uint32_t *>(&by_hand[x]) = blocks;
+                    __syncwarp();
+                    if (lane == 0) bw::bar_arrive(bar(&met[x]));
+                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&met[x]), finished & 1, &gave_up) && ok);
+                    if (*const_cast<volatile uint32_t *>(&by_hand[x]) == blocks)
                         masked_product<T, DP>(at_y, [&](int g) { return at_s + g * 16; }, 4, tile, 0, 0, r + 1, j > 0);
-                    if ((warp & 3) == 0 && lane == 0) *const_cast<volatile uint32_t *>(&by_hand[x]) = some;
                 }
                 bw::fence_before();
                 __syncwarp();
                 if (lane == 0) bw::bar_arrive(bar(&p_full[x]));
             }
             c += 2 * max(q.blocks[0], q.blocks[1]);
-            ok = ok && bw::bar_wait(bar(&y_full[x]), y_phase, &gave_up);
+            ok = ok && bw::bar_wait(bar(&y_full[x]), finished++ & 1, &gave_up);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            y_phase ^= 1;
             bw::fence_after();
-            if ((warp & 3) == 0 && lane == 0) *const_cast<volatile uint32_t *>(&by_hand[x]) = 0;
             const float by = 1.0f / l;
 #pragma unroll 1
             for (int d = 0; d < DP; d += 32) {

@@ -73,19 +73,6 @@ __device__ __forceinline__ bool look_through(unsigned char *tile, int r, int row
     return bad;
 }
 
-// Whether any of the 128 threads that meet at this barrier says so.
-__device__ __forceinline__ bool any_of_group(bool mine, int barrier)
-{
-    uint32_t some;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(some)
-        : "r"(uint32_t(mine)), "r"(barrier)
-        : "memory");
-    return some != 0;
-}
-
 // acc[lane][..] (+)= the sum of w[lane][c] B[c][..] over columns c of the lane's own range [from, end), on the
 // CUDA cores: where B holds infinities or NaN that some lanes must not see, zero weights
 // would not hide them. w: packed pairs in tensor memory, 16 columns for 32 c, at(c / 32); DP columns of acc.

@@ -1,4 +1,6 @@
 // Attention: the list of tiles, the row sums of the gradient, and which kernels run.
+#include <type_traits>
+
 #include "attention.cuh"
 
 namespace dc {
@@ -108,24 +110,74 @@ attention_plan_kernel(const int64_t *offsets, int32_t sequences, int64_t tokens,
             __syncthreads();
         }
     }
-    if (threadIdx.x == 0) plan->tiles = tiles;
+    if (threadIdx.x == 0) {
+        plan->tiles = tiles;
+        plan->top_v = plan->top_do = 0;
+    }
 }
 
-// delta[h][t] = sum over d of dy y, a warp per row.
-template <typename T>
-__global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArgs a)
+// delta[h][t] = sum over d of dy y: sixteen lanes a row of a head, sixteen bytes a lane at a time. Halves: also the largest finite |dy| and |v| of the sequences' rows, from
+// which the power of two follows that dS is held in; a maximum does not depend on the order.
+__device__ __forceinline__ float largest(float top, float x)
 {
-    const int64_t i = int64_t(blockIdx.x) * 8 + threadIdx.x / 32;
-    if (i >= a.tokens * a.heads) return;
-    const int64_t t = i / a.heads;
-    const int h = int(i - t * a.heads), lane = threadIdx.x % 32;
-    const T *y = static_cast<const T *>(a.y) + i * a.D;
-    const T *dy = static_cast<const T *>(a.dy) + t * a.dy_token + h * a.dy_head;
-    float s = 0.0f;
-    for (int d = lane; d < a.D; d += 32) s += to_float(y[d]) * to_float(dy[d]);
+    x = fabsf(x);
+    return x < INFINITY ? fmaxf(top, x) : top;
+}
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArgs a, AttentionPlan *plan, const int32_t *start,
+                                                              int32_t sequences)
+{
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    constexpr int V = kVec<T>;
+    // the same elements to a lane whether they come in one access or not: the same bits
+    auto bring = [&](const T *p, int left) {
+        if (WIDE) return *reinterpret_cast<const Vec<T, V> *>(p);
+        Vec<T, V> v;
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) a.delta[h * a.tokens + t] = s;
+        for (int j = 0; j < V; ++j) v.e[j] = j < left ? p[j] : from_float<T>(0.0f);
+        return v;
+    };
+    const int64_t rows = a.tokens * a.heads, step = int64_t(gridDim.x) * 16;
+    const int l = threadIdx.x % 16;
+    const int lo = start[1], hi = start[sequences + 1];  // the sequences' rows
+    float top_dy = 0.0f, top_v = 0.0f;
+    for (int64_t i0 = int64_t(blockIdx.x) * 16; i0 < rows; i0 += step) {
+        const int64_t i = i0 + threadIdx.x / 16;
+        float s = 0.0f;
+        if (i < rows) {
+            const int64_t t = i / a.heads;
+            const T *y = static_cast<const T *>(a.y) + i * a.D;
+            const T *dy = static_cast<const T *>(a.dy) + t * a.dy_token + (i - t * a.heads) * a.dy_head;
+            const bool counts = t >= lo && t < hi;
+            for (int d = l * V; d < a.D; d += 16 * V) {
+                const Vec<T, V> p = bring(y + d, a.D - d), q = bring(dy + d, a.D - d);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float g = to_float(q.e[j]);
+                    s += to_float(p.e[j]) * g;
+                    if (kHalf && counts) top_dy = largest(top_dy, g);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (l == 0 && i < rows) a.delta[i % a.heads * a.tokens + i / a.heads] = s;
+    }
+    if constexpr (kHalf) {
+        const int64_t first = int64_t(lo) * a.kv_heads, end = int64_t(hi) * a.kv_heads;
+        for (int64_t i = first + int64_t(blockIdx.x) * 16 + threadIdx.x / 16; i < end; i += step) {
+            const int64_t t = i / a.kv_heads;
+            const T *v = static_cast<const T *>(a.v) + t * a.v_token + (i - t * a.kv_heads) * a.v_head;
+            for (int d = l * V; d < a.D; d += 16 * V) {
+                const Vec<T, V> p = bring(v + d, a.D - d);
+#pragma unroll
+                for (int j = 0; j < V; ++j) top_v = largest(top_v, to_float(p.e[j]));
+            }
+        }
+        // magnitudes' bits are in the order of their values
+        atomicMax(&plan->top_do, __reduce_max_sync(0xffffffffu, __float_as_uint(top_dy)));
+        atomicMax(&plan->top_v, __reduce_max_sync(0xffffffffu, __float_as_uint(top_v)));
+    }
 }
 
 // The tensor cores' copies need heads that start on 16-byte boundaries: others are copied to rows of
@@ -176,7 +228,7 @@ struct Layout {
 Layout layout(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
 {
     Layout l = {};
-    l.rows = dtype == DC_FP32 || grad ? kSimtRows : attention_mma_rows(a);
+    l.rows = dtype == DC_FP32 ? kSimtRows : grad ? kMmaRows : attention_mma_rows(a);
     size_t at = round256(sizeof(AttentionPlan) +
                          sizeof(AttentionTile) * size_t(attention_most_tiles(a.tokens, sequences, l.rows)));
     l.first = at;
@@ -215,6 +267,29 @@ cudaError_t align_operands(AttentionArgs &a, const Layout &l, unsigned char *ws,
     return cudaSuccess;
 }
 
+template <typename T>
+cudaError_t gradient(int dtype, const AttentionArgs &a, int32_t sequences, AttentionPlan *plan, const Layout &l, int64_t most,
+                     cudaStream_t stream)
+{
+    int sms = 0;
+    const cudaError_t e = sm_count(sms);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = (a.tokens * a.heads + 15) / 16, limit = int64_t(sms) * 16;
+    const unsigned grid = unsigned(blocks < limit ? blocks : limit);
+    const int32_t *start = reinterpret_cast<const int32_t *>(reinterpret_cast<unsigned char *>(plan) + l.start);
+    // operands of 16 bits are aligned by now; y is the caller's
+    const int unit = 16 / int(sizeof(T));
+    const bool wide = a.D % unit == 0 && aligned16(a.y) && aligned16(a.dy) && aligned16(a.v) && a.dy_token % unit == 0 &&
+                      a.dy_head % unit == 0 && (a.tokens == 1 || a.v_token % unit == 0) &&
+                      (a.kv_heads == 1 || a.v_head % unit == 0);
+    if (wide)
+        attention_delta_kernel<T, true><<<grid, 256, 0, stream>>>(a, plan, start, sequences);
+    else
+        attention_delta_kernel<T, false><<<grid, 256, 0, stream>>>(a, plan, start, sequences);
+    if (sizeof(T) == 2) return launch_attention_grad_mma(dtype, a, most, stream);
+    return launch_attention_grad_simt(a, most, stream);
+}
+
 }  // namespace
 
 size_t attention_workspace(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
@@ -234,19 +309,18 @@ cudaError_t launch_attention(int dtype, AttentionArgs a, int32_t sequences, cons
     a.plan = plan;
     const int64_t most = attention_most_tiles(a.tokens, sequences, l.rows);
     if (!grad) {
-        if (dtype == DC_FP32) return launch_attention_simt(dtype, a, most, stream);
+        if (dtype == DC_FP32) return launch_attention_simt(a, most, stream);
         const cudaError_t e = align_operands(a, l, ws, stream);
         return e == cudaSuccess ? launch_attention_mma(dtype, a, most, stream) : e;
     }
     a.delta = reinterpret_cast<float *>(ws + l.delta);
-    const int64_t blocks = (a.tokens * a.heads + 7) / 8;
-    if (blocks > (int64_t(1) << 31) - 1) return cudaErrorInvalidValue;
+    const cudaError_t e = align_operands(a, l, ws, stream);
+    if (e != cudaSuccess) return e;
     switch (dtype) {
-        case DC_BF16: attention_delta_kernel<__nv_bfloat16><<<unsigned(blocks), 256, 0, stream>>>(a); break;
-        case DC_FP16: attention_delta_kernel<__half><<<unsigned(blocks), 256, 0, stream>>>(a); break;
-        default: attention_delta_kernel<float><<<unsigned(blocks), 256, 0, stream>>>(a);
+        case DC_BF16: return gradient<__nv_bfloat16>(dtype, a, sequences, plan, l, most, stream);
+        case DC_FP16: return gradient<__half>(dtype, a, sequences, plan, l, most, stream);
+        default: return gradient<float>(dtype, a, sequences, plan, l, most, stream);
     }
-    return launch_attention_grad_simt(dtype, a, most, stream);
 }
 
 }  // namespace dc

@@ -1,4 +1,4 @@
-// Attention on the CUDA cores.
+// Attention of floats, on the CUDA cores.
 //
 // Forward, a block per tile of 64 rows and head: keys 64 at a time; scores S = scale q k^T, the
 // running maximum m and sum l of each row, and y = sum e^(S - m) v / l, kept in registers.
@@ -308,21 +308,17 @@ cudaError_t backward(const AttentionArgs &a, int64_t most, cudaStream_t stream)
 
 }  // namespace
 
-cudaError_t launch_attention_simt(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+cudaError_t launch_attention_simt(const AttentionArgs &a, int64_t most, cudaStream_t stream)
 {
-    DC_DTYPE_SWITCH(dtype, T, {
-        return a.D <= 64 ? forward<T, 64>(a, most, stream) : forward<T, 128>(a, most, stream);
-    })
+    return a.D <= 64 ? forward<float, 64>(a, most, stream) : forward<float, 128>(a, most, stream);
 }
 
-cudaError_t launch_attention_grad_simt(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+cudaError_t launch_attention_grad_simt(const AttentionArgs &a, int64_t most, cudaStream_t stream)
 {
-    DC_DTYPE_SWITCH(dtype, T, {
-        cudaError_t e = a.D <= 64 ? backward<T, 64, true>(a, most, stream) : backward<T, 128, true>(a, most, stream);
-        if (e == cudaSuccess)
-            e = a.D <= 64 ? backward<T, 64, false>(a, most, stream) : backward<T, 128, false>(a, most, stream);
-        return e;
-    })
+    cudaError_t e = a.D <= 64 ? backward<float, 64, true>(a, most, stream) : backward<float, 128, true>(a, most, stream);
+    if (e == cudaSuccess)
+        e = a.D <= 64 ? backward<float, 64, false>(a, most, stream) : backward<float, 128, false>(a, most, stream);
+    return e;
 }
 
 }  // namespace dc
