@@ -355,23 +355,34 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 const int end = (!COLUMNS && s.diagonal ? r + 1 : s.count) - side * 64;
                 float p[64];
                 bw::tmem_load(at_s, p);
+                auto make_p = [&](auto masked) {
 #pragma unroll
-                for (int e0 = 0; e0 < 64; e0 += 32) {
-                    uint32_t out16[16];
+                    for (int e0 = 0; e0 < 64; e0 += 32) {
+                        uint32_t out16[16];
 #pragma unroll
-                    for (int e = e0; e < e0 + 32; e += 2) {
-                        const float2 minus = COLUMNS ? *reinterpret_cast<const float2 *>(l + e) : lse;
-                        const float2 t = __ffma2_rn(make_float2(p[e], p[e + 1]), by, minus);
-                        p[e] = exp2_fast(t.x);
-                        p[e + 1] = exp2_fast(t.y);
-                        if (cut) {
-                            p[e] = e >= from && e < end ? p[e] : 0.0f;
-                            p[e + 1] = e + 1 >= from && e + 1 < end ? p[e + 1] : 0.0f;
+                        for (int e = e0; e < e0 + 32; e += 4) {
+                            const float4 minus = COLUMNS ? *reinterpret_cast<const float4 *>(l + e)
+                                                         : make_float4(lse.x, lse.x, lse.x, lse.x);
+                            const float2 t = __ffma2_rn(make_float2(p[e], p[e + 1]), by, make_float2(minus.x, minus.y));
+                            const float2 u = __ffma2_rn(make_float2(p[e + 2], p[e + 3]), by, make_float2(minus.z, minus.w));
+                            p[e] = exp2_fast(t.x);
+                            p[e + 1] = exp2_fast(t.y);
+                            p[e + 2] = exp2_fast(u.x);
+                            p[e + 3] = exp2_fast(u.y);
+                            if constexpr (decltype(masked)::value)
+#pragma unroll
+                                for (int k = e; k < e + 4; ++k) p[k] = k >= from && k < end ? p[k] : 0.0f;
+                            if (COLUMNS) {
+                                out16[(e - e0) / 2] = pack2(p[e], p[e + 1], T());
+                                out16[(e - e0) / 2 + 1] = pack2(p[e + 2], p[e + 3], T());
+                            }
                         }
-                        if (COLUMNS) out16[(e - e0) / 2] = pack2(p[e], p[e + 1], T());
+                        if (COLUMNS) bw::tmem_store(at_s + e0 / 2, out16);
                     }
-                    if (COLUMNS) bw::tmem_store(at_s + e0 / 2, out16);
-                }
+                };
+                // most blocks are whole: the mask's selections would double the work of a block
+                if (cut) make_p(std::true_type());
+                else make_p(std::false_type());
                 if (COLUMNS) bw::tmem_stored();
                 bool some = false;
                 unsigned char *const tile_x = dyn + (2 + n % G::kX) * kBytes, *const tile_y = dyn + (2 + G::kX + n % G::kY) * kBytes;
@@ -396,24 +407,35 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 ok = __all_sync(0xffffffffu, ok && bw::bar_wait(bar(&b.dp_full), n & 1, gave_up));
                 if (!ok) break;
                 bw::fence_after();
+                auto make_ds = [&](auto masked) {
 #pragma unroll
-                for (int e0 = 0; e0 < 64; e0 += 32) {
-                    float d[32];
-                    bw::tmem_load(at_dp + e0, d);
-                    uint32_t out16[16];
+                    for (int e0 = 0; e0 < 64; e0 += 32) {
+                        float d[32];
+                        bw::tmem_load(at_dp + e0, d);
+                        uint32_t out16[16];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float2 minus = COLUMNS ? *reinterpret_cast<const float2 *>(l + kTile + e0 + e) : delta;
-                        float2 t = __ffma2_rn(make_float2(d[e], d[e + 1]), fs, minus);
-                        t = __fmul2_rn(t, make_float2(p[e0 + e], p[e0 + e + 1]));
-                        if (cut) {
-                            t.x = e0 + e >= from && e0 + e < end ? t.x : 0.0f;
-                            t.y = e0 + e + 1 >= from && e0 + e + 1 < end ? t.y : 0.0f;
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 minus = COLUMNS ? *reinterpret_cast<const float4 *>(l + kTile + e0 + e)
+                                                         : make_float4(delta.x, delta.x, delta.x, delta.x);
+                            float2 t = __ffma2_rn(make_float2(d[e], d[e + 1]), fs, make_float2(minus.x, minus.y));
+                            float2 u = __ffma2_rn(make_float2(d[e + 2], d[e + 3]), fs, make_float2(minus.z, minus.w));
+                            t = __fmul2_rn(t, make_float2(p[e0 + e], p[e0 + e + 1]));
+                            u = __fmul2_rn(u, make_float2(p[e0 + e + 2], p[e0 + e + 3]));
+                            if constexpr (decltype(masked)::value) {
+                                const int k = e0 + e;
+                                t.x = k >= from && k < end ? t.x : 0.0f;
+                                t.y = k + 1 >= from && k + 1 < end ? t.y : 0.0f;
+                                u.x = k + 2 >= from && k + 2 < end ? u.x : 0.0f;
+                                u.y = k + 3 >= from && k + 3 < end ? u.y : 0.0f;
+                            }
+                            out16[e / 2] = pack2(t.x, t.y, T());
+                            out16[e / 2 + 1] = pack2(u.x, u.y, T());
                         }
-                        out16[e / 2] = pack2(t.x, t.y, T());
+                        bw::tmem_store(at_dp + e0 / 2, out16);
                     }
-                    bw::tmem_store(at_dp + e0 / 2, out16);
-                }
+                };
+                if (cut) make_ds(std::true_type());
+                else make_ds(std::false_type());
                 bw::tmem_stored();
                 if (some) {
                     meet();

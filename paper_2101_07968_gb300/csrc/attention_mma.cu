@@ -76,7 +76,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     constexpr uint32_t kBytes = kBoxes * kBox;  // of a tile in shared memory
     constexpr int kStages = DP == 64 ? 8 : 4;
     extern __shared__ unsigned char dyn[];
-    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_full[2], y_full[2], met[2], last;
+    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2], met[2], last;
     __shared__ uint32_t tmem_at, gave_up;
     __shared__ uint32_t by_hand[2];  // a tile's block, counted from one, if its sums are done by hand
 
@@ -90,6 +90,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             bw::bar_init(bar(&q_full[i]), 1);
             bw::bar_init(bar(&q_free[i]), 1);
             bw::bar_init(bar(&s_full[i]), 1);
+            bw::bar_init(bar(&p_half[i]), 4);
             bw::bar_init(bar(&p_full[i]), 4);
             bw::bar_init(bar(&y_full[i]), 1);
             bw::bar_init(bar(&met[i]), 4);
@@ -191,16 +192,23 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (!have(v)) break;
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (j >= q.blocks[x]) continue;
+                        const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
+                        auto half = [&](int i0) {
+#pragma unroll
+                            for (int i = i0; i < i0 + kTile / 32; ++i)
+                                bw::mma1_tmem(tmem + 2 * kTile + x * DP, tmem + x * kTile + i * 8, dv + i * 128, shape_y,
+                                              j > 0 || i > 0);
+                        };
+                        ok = bw::bar_wait(bar(&p_half[x]), blocks[x] & 1, &gave_up);
+                        if (!ok) break;
+                        bw::fence_after();
+                        // (set before the first half where it is set)
+                        const bool own = *const_cast<volatile uint32_t *>(&by_hand[x]) != blocks[x] + 1;
+                        if (own) half(0);
                         ok = bw::bar_wait(bar(&p_full[x]), blocks[x]++ & 1, &gave_up);
                         if (!ok) break;
                         bw::fence_after();
-                        if (*const_cast<volatile uint32_t *>(&by_hand[x]) != blocks[x]) {
-                            const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
-#pragma unroll
-                            for (int i = 0; i < kTile / 16; ++i)
-                                bw::mma1_tmem(tmem + 2 * kTile + x * DP, tmem + x * kTile + i * 8, dv + i * 128, shape_y,
-                                              j > 0 || i > 0);
-                        }
+                        if (own) half(kTile / 32);
                         if (j + 1 < q.blocks[x]) {
                             if (!have(k)) break;
                             scores(x, k);
@@ -243,6 +251,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 continue;
             }
             float m = -INFINITY, l = 0.0f;
+            auto hand_over = [&](uint64_t(&to)[2]) {  // P so far, to the products
+                bw::tmem_stored();
+                bw::fence_before();
+                __syncwarp();
+                if (lane == 0) bw::bar_arrive(bar(&to[x]));
+            };
             for (int j = 0; j < n; ++j) {
                 ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&s_full[x]), blocks++ & 1, &gave_up));
                 if (!ok) break;
@@ -262,10 +276,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                     for (int e = 0; e < kTile; ++e) s[e] = e <= r ? s[e] : -INFINITY;
                 }
-                float top[4] = {s[0], s[1], s[2], s[3]};
+                float top[4];
 #pragma unroll
-                for (int e = 4; e < kTile; ++e) top[e & 3] = fmaxf(top[e & 3], s[e]);
-                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                for (int e = 0; e < 4; ++e) top[e] = fmaxf(s[2 * e], s[2 * e + 1]);
+#pragma unroll
+                for (int e = 8; e < kTile; e += 2) top[e / 2 & 3] = max3(top[e / 2 & 3], s[e], s[e + 1]);
+                const float most = fmaxf(max3(top[0], top[1], top[2]), top[3]);
                 const float raised = fmaxf(m, most);
                 // (a row by its own scores alone: its bits do not depend on its neighbours)
                 const bool low = !((raised - m) * scale <= kSlack);
@@ -303,11 +319,13 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         p[e / 2] = pack2(t.x, t.y, T());
                     }
                     bw::tmem_store(at_s + e0 / 2, p);
+                    // the first half's products may start
+                    if (e0 == 32 && !diagonal) hand_over(p_half);
                 }
                 sum[0] = __fadd2_rn(sum[0], sum[1]);
                 l += sum[0].x + sum[0].y;
-                bw::tmem_stored();
                 if (diagonal) {
+                    bw::tmem_stored();
                     const uint32_t v = c + 2 * j + 1;
                     unsigned char *tile = dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes;
                     ok = bw::bar_wait(bar(&full[v % kStages]), (v / kStages) & 1, &gave_up);
@@ -317,10 +335,9 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&met[x]), finished & 1, &gave_up) && ok);
                     if (*const_cast<volatile uint32_t *>(&by_hand[x]) == blocks)
                         masked_product<T, DP>(at_y, [&](int g) { return at_s + g * 16; }, 4, tile, 0, 0, r + 1, j > 0);
+                    hand_over(p_half);
                 }
-                bw::fence_before();
-                __syncwarp();
-                if (lane == 0) bw::bar_arrive(bar(&p_full[x]));
+                hand_over(p_full);
             }
             c += 2 * max(q.blocks[0], q.blocks[1]);
             ok = ok && bw::bar_wait(bar(&y_full[x]), finished++ & 1, &gave_up);

@@ -21,6 +21,14 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
+// the largest of three, one instruction; a NaN counts as none
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+    return m;
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
 {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
