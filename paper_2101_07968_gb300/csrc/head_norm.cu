@@ -11,35 +11,19 @@
 //
 // Both directions are bound by memory: 2 (3) accesses of each element. A group of 8, 16 or 32 lanes
 // takes a head, eight elements a lane as two runs of four: the two halves of four pairs, so that
-// a pair is in one lane, and a run of the lanes is whole lines. A warp takes a token's heads in
-// turn, so that the angles and the norms' weights stay in registers.
+// a pair is in one lane, and a run of the lanes is whole lines. Blocks are dealt to queries and keys by
+// their shares, so that a thread holds one weight and its gradient; a warp takes a token's heads
+// in turn with the angles in registers. What it takes next comes by asynchronous copies, each lane
+// its own runs, several chunks ahead: loads to registers kept too few bytes on their way
+// (32,768 tokens x 40 heads x 128, gradient: 419 us at 25 % occupancy and 31 % of the issue slots).
 #include "layers.cuh"
 
 namespace dc {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kUnroll = 2;  // heads of a group that are on their way at once
-
-// Four neighbours as floats.
-template <typename T>
-__device__ __forceinline__ void load4(const T *p, float *v)
-{
-    const Vec<T, 4> e = *reinterpret_cast<const Vec<T, 4> *>(p);
-    const float2 a = pair_of(e.e), b = pair_of(e.e + 2);
-    v[0] = a.x;
-    v[1] = a.y;
-    v[2] = b.x;
-    v[3] = b.y;
-}
-template <typename T>
-__device__ __forceinline__ void store4(T *p, const float *v)
-{
-    Vec<T, 4> e;
-    put_pair(e.e, make_float2(v[0], v[1]));
-    put_pair(e.e + 2, make_float2(v[2], v[3]));
-    *reinterpret_cast<Vec<T, 4> *>(p) = e;
-}
+constexpr int kUnroll = 2;  // heads of a group in a chunk
+constexpr int kAhead = 4;   // chunks in a warp's ring
 
 __device__ __forceinline__ void angle(int64_t position, uint64_t turns, float &c, float &s)
 {
@@ -47,55 +31,79 @@ __device__ __forceinline__ void angle(int64_t position, uint64_t turns, float &c
     sincospif(float(int32_t(at >> 32)) * 0x1p-31f, &s, &c);
 }
 
-// A unit of work: heads [h0, h1) of a token, queries' heads first, then the keys'.
+// A unit of work: heads [h0, h1) of a token's queries or keys.
 struct Unit {
     int64_t token;
     int32_t h0, h1;
 };
-__device__ __forceinline__ Unit unit_at(const HeadNormArgs &a, int64_t u)
+__device__ __forceinline__ Unit unit_at(const HeadNormArgs &a, int which, int64_t u)
 {
-    const int heads = a.heads[0] + a.heads[1];
-    Unit q;
-    q.token = u / a.parts;
-    const int part = int(u - q.token * a.parts);
-    q.h0 = part * a.per_part;
-    q.h1 = min(heads, q.h0 + a.per_part);
+    // (tokens in parts are few)
+    Unit q = {u, 0, a.heads[which]};
+    if (a.parts[which] == 1) return q;
+    q.token = int(u) / a.parts[which];
+    const int part = int(u) % a.parts[which];
+    q.h0 = part * a.per_part[which];
+    q.h1 = min(a.heads[which], q.h0 + a.per_part[which]);
     return q;
 }
 
-// Sums of weights' gradients: lanes of the block that hold the same elements, then the block's row.
-// values [2][8] of each lane; partial [blocks][2][D].
-template <int LANES>
-__device__ __forceinline__ void add_up(const HeadNormArgs &a, float (&dw)[2][8], const int (&at)[2], bool mine)
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(void *to, const void *from)
 {
-    __shared__ float sums[2][kWarps][DC_HEAD_NORM_DIM_MAX];
+    const uint32_t at = uint32_t(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(at), "l"(from) : "memory");
+}
+
+// The angles of four pairs: cosines, sines and their negatives.
+struct Turn {
+    float2 c[2], s[2], n[2];
+};
+// Turns four pairs: halves of pairs in v[0..1] and v[2..3], or neighbours.
+__device__ __forceinline__ void turn(float2 (&v)[4], const Turn &t, bool interleaved)
+{
+    if (!interleaved) {
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
+        for (int k = 0; k < 2; ++k) {
+            const float2 e = v[k], f = v[k + 2];
+            v[k] = __ffma2_rn(e, t.c[k], __fmul2_rn(f, t.n[k]));
+            v[k + 2] = __ffma2_rn(e, t.s[k], __fmul2_rn(f, t.c[k]));
+        }
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int o = LANES; o < 32; o *= 2) dw[which][j] += __shfl_xor_sync(0xffffffffu, dw[which][j], o);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    if (lane < LANES && mine)
-#pragma unroll
-        for (int which = 0; which < 2; ++which)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sums[which][warp][at[j / 4] + j % 4] = dw[which][j];
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.D; i += kThreads) {
-        const int which = i / a.D, e = i - which * a.D;
-        float t = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) t += sums[which][w][e];
-        a.partial[int64_t(blockIdx.x) * 2 * a.D + i] = t;
+        for (int k = 0; k < 4; ++k) {
+            const float c = k & 1 ? t.c[k / 2].y : t.c[k / 2].x, s = k & 1 ? t.s[k / 2].y : t.s[k / 2].x;
+            const float n = k & 1 ? t.n[k / 2].y : t.n[k / 2].x;
+            v[k] = __ffma2_rn(make_float2(v[k].y, v[k].x), make_float2(n, s), __fmul2_rn(v[k], twice(c)));
+        }
     }
 }
 
-template <typename T, int LANES, bool GRAD>
-__global__ void __launch_bounds__(kThreads) head_norm_kernel(const __grid_constant__ HeadNormArgs a)
+template <typename T>
+__device__ __forceinline__ void unpack(const Vec<T, 4> &run, float2 *v)
 {
-    constexpr int kHeads = 32 / LANES;  // at a time, of a warp
-    const int lane = threadIdx.x % 32, l = lane % LANES, group = lane / LANES;
+    v[0] = pair_of(run.e);
+    v[1] = pair_of(run.e + 2);
+}
+
+// Blocks of an SM: what their rings leave room for (64 KB of 16-bit gradients' each).
+template <typename T, bool GRAD>
+constexpr int kResident = sizeof(T) == 4 ? (GRAD ? 1 : 3) : (GRAD ? 3 : 4);
+
+template <typename T, int LANES, bool GRAD>
+__global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel(const __grid_constant__ HeadNormArgs a)
+{
+    constexpr int kHeads = 32 / LANES, kChunk = kHeads * kUnroll;  // heads at a time, and of a chunk
+    constexpr int kRuns = kUnroll * 2 * (GRAD ? 2 : 1);
+    using Run = Vec<T, 4>;
+    extern __shared__ __align__(16) unsigned char dyn[];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % LANES, group = lane / LANES;
+    Run *const ring = reinterpret_cast<Run *>(dyn) + size_t(warp) * kAhead * kRuns * 32 + lane;
+    const int which = int(blockIdx.x) >= a.blocks[0];
+    const int block = int(blockIdx.x) - (which ? a.blocks[0] : 0);
     const bool mine = l * 8 < a.D, turned = l * 8 < a.rotary;
     // first elements of the lane's two runs
     int at[2] = {8 * l, 8 * l + 4};
@@ -103,119 +111,178 @@ __global__ void __launch_bounds__(kThreads) head_norm_kernel(const __grid_consta
         at[0] = 4 * l;
         at[1] = a.rotary / 2 + 4 * l;
     }
-    float w[2][8];
+    float2 w[4], dw[4];
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            w[which][j] = mine && a.w[which] ? to_float(static_cast<const T *>(a.w[which])[at[j / 4] + j % 4]) : 1.0f;
-    float dw[2][8] = {};
+    for (int k = 0; k < 4; ++k) {
+        w[k] = twice(1.0f);
+        if (mine && a.w[which]) {
+            const T *p = static_cast<const T *>(a.w[which]) + at[k / 2] + k % 2 * 2;
+            w[k] = make_float2(to_float(p[0]), to_float(p[1]));
+        }
+        dw[k] = twice(0.0f);
+    }
     const float inverse = 1.0f / float(a.D);
+    const T *const x0 = static_cast<const T *>(a.x[which]);
+    const int heads = a.heads[which];
+    const int64_t units = a.tokens * a.parts[which], step = int64_t(a.blocks[which]) * kWarps;
+    const int64_t first = int64_t(block) * kWarps + warp;
 
-    // One token after another (a block's warps take neighbours).
-    const int64_t units = a.tokens * a.parts;
-    for (int64_t u = int64_t(blockIdx.x) * kWarps + threadIdx.x / 32; u < units; u += int64_t(gridDim.x) * kWarps) {
-        const Unit q = unit_at(a, u);
-        float c[4], s[4];
-        {
-            const int64_t position = a.positions[q.token];
+    // chunks on their way: the next one's unit and how many of its heads are left, and the lane's runs there
+    int64_t next = first;
+    int left = 0, filled = 0;
+    const T *from = nullptr, *from_dy = nullptr;
+    const int64_t x_group = kHeads * a.head[which], apart = at[1] - at[0];
+    auto start = [&] {
+        if (next >= units) return;
+        const Unit q = unit_at(a, which, next);
+        left = q.h1 - q.h0 - group;
+        from = x0 + q.token * a.token[which] + (q.h0 + group) * a.head[which] + at[0];
+        if (GRAD) from_dy = static_cast<const T *>(a.dy[which]) + (q.token * heads + q.h0 + group) * a.D + at[0];
+    };
+    auto bring = [&] {
+        if (next < units) {
+            Run *const p = ring + filled * kRuns * 32;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                c[j] = 1.0f;
-                s[j] = 0.0f;
-                if (turned) angle(position, a.turns[4 * l + j], c[j], s[j]);
+            for (int i = 0; i < kUnroll; ++i) {
+                if (mine && left > i * kHeads) {
+                    copy_ahead<sizeof(Run)>(p + 2 * i * 32, from);
+                    copy_ahead<sizeof(Run)>(p + (2 * i + 1) * 32, from + apart);
+                    if (GRAD) {
+                        copy_ahead<sizeof(Run)>(p + (2 * (kUnroll + i)) * 32, from_dy);
+                        copy_ahead<sizeof(Run)>(p + (2 * (kUnroll + i) + 1) * 32, from_dy + apart);
+                    }
+                }
+                from += x_group;
+                if (GRAD) from_dy += kHeads * a.D;
+            }
+            filled = (filled + 1) % kAhead;
+            left -= kChunk;
+            if (left + group <= 0) {
+                next += step;
+                start();
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    start();
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const int first = which ? a.heads[0] : 0, end = min(q.h1, first + a.heads[which]);
-            const T *x = static_cast<const T *>(a.x[which]) + q.token * a.token[which];
-            const int64_t row = q.token * a.heads[which];
-            const T *dy = GRAD ? static_cast<const T *>(a.dy[which]) + row * a.D : nullptr;
-            T *y = static_cast<T *>(a.y[which]) + row * a.D;
-            for (int h0 = max(q.h0, first); h0 < end; h0 += kHeads * kUnroll) {
-                float v[kUnroll][8], d[GRAD ? kUnroll : 1][8];
+    for (int i = 0; i < kAhead - 1; ++i) bring();
+
+    int used = 0;
+    int64_t position = first < units ? a.positions[unit_at(a, which, first).token] : 0;
+    for (int64_t u = first; u < units; u += step) {
+        const Unit q = unit_at(a, which, u);
+        Turn angles;
 #pragma unroll
-                for (int i = 0; i < kUnroll; ++i) {
-                    const int h = h0 + i * kHeads + group - first;
-                    const bool there = mine && h + first < end;
+        for (int j = 0; j < 2; ++j) {
+            float2 c = twice(1.0f), s = twice(0.0f);
+            if (turned) {
+                angle(position, a.turns[4 * l + 2 * j], c.x, s.x);
+                angle(position, a.turns[4 * l + 2 * j + 1], c.y, s.y);
+            }
+            const float2 n = make_float2(-s.x, -s.y);
+            angles.c[j] = c;  // the gradient's turn back
+            angles.s[j] = GRAD ? n : s;
+            angles.n[j] = GRAD ? s : n;
+        }
+        if (u + step < units) position = a.positions[unit_at(a, which, u + step).token];
+        T *y = static_cast<T *>(a.y[which]) + (q.token * heads + q.h0 + group) * a.D + at[0];
+        for (int h0 = q.h0; h0 < q.h1; h0 += kChunk) {
+            bring();
+            asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+            const Run *const p = ring + used * kRuns * 32;
+            used = (used + 1) % kAhead;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-                    if (there) {
-                        load4(x + h * a.head[which] + at[0], v[i]);
-                        load4(x + h * a.head[which] + at[1], v[i] + 4);
-                    }
+            for (int i = 0; i < kUnroll; ++i) {
+                const bool there = mine && h0 + i * kHeads + group < q.h1;
+                float2 v[4], d[GRAD ? 4 : 1];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[k] = twice(0.0f);
+                    if (GRAD) d[k] = twice(0.0f);
+                }
+                if (there) {
+                    unpack(p[2 * i * 32], v);
+                    unpack(p[(2 * i + 1) * 32], v + 2);
                     if constexpr (GRAD) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) d[i][j] = 0.0f;
-                        if (there) {
-                            load4(dy + int64_t(h) * a.D + at[0], d[i]);
-                            load4(dy + int64_t(h) * a.D + at[1], d[i] + 4);
-                        }
+                        unpack(p[2 * (kUnroll + i) * 32], d);
+                        unpack(p[(2 * (kUnroll + i) + 1) * 32], d + 2);
                     }
                 }
+                float2 square = __fmul2_rn(v[0], v[0]), along = twice(0.0f);
 #pragma unroll
-                for (int i = 0; i < kUnroll; ++i) {
-                    const int h = h0 + i * kHeads + group - first;
-                    // a pair (e, f) of v[j], turned by (c, s): halves of pairs are four apart, or neighbours
-                    auto turn = [&](float(&t)[8], float sign) {
-                        if (!a.interleaved) {
+                for (int k = 1; k < 4; ++k) square = __ffma2_rn(v[k], v[k], square);
+                float2 g[GRAD ? 4 : 1];
+                if constexpr (GRAD) {
+                    if (turned) turn(d, angles, a.interleaved);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float e = t[j], f = t[j + 4];
-                                t[j] = e * c[j] - sign * f * s[j];
-                                t[j + 4] = f * c[j] + sign * e * s[j];
-                            }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float e = t[2 * j], f = t[2 * j + 1];
-                                t[2 * j] = e * c[j] - sign * f * s[j];
-                                t[2 * j + 1] = f * c[j] + sign * e * s[j];
-                            }
-                        }
-                    };
-                    float square = 0.0f, along = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) square += v[i][j] * v[i][j];
-                    if constexpr (GRAD) {
-                        if (turned) turn(d[i], -1.0f);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) along += d[i][j] * w[which][j] * v[i][j];
-                    }
-                    float rstd = 1.0f;
-                    if (a.norm) {
-#pragma unroll
-                        for (int o = LANES / 2; o > 0; o /= 2) {
-                            square += __shfl_xor_sync(0xffffffffu, square, o);
-                            if (GRAD) along += __shfl_xor_sync(0xffffffffu, along, o);
-                        }
-                        rstd = rsqrtf(square * inverse + a.eps);
-                    } else {
-                        along = 0.0f;
-                    }
-                    float out[8];
-                    if constexpr (GRAD) {
-                        const float back = along * inverse * rstd * rstd;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            dw[which][j] += d[i][j] * (v[i][j] * rstd);
-                            out[j] = rstd * (d[i][j] * w[which][j] - v[i][j] * back);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) out[j] = v[i][j] * rstd * w[which][j];
-                        if (turned) turn(out, 1.0f);
-                    }
-                    if (mine && h + first < end) {
-                        store4(y + int64_t(h) * a.D + at[0], out);
-                        store4(y + int64_t(h) * a.D + at[1], out + 4);
+                    for (int k = 0; k < 4; ++k) {
+                        g[k] = __fmul2_rn(d[k], w[k]);
+                        along = __ffma2_rn(g[k], v[k], along);
                     }
                 }
+                float rstd = 1.0f, sum = square.x + square.y, dot = along.x + along.y;
+                if (a.norm) {
+#pragma unroll
+                    for (int o = LANES / 2; o > 0; o /= 2) {
+                        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                        if (GRAD) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                    }
+                    rstd = rsqrtf(sum * inverse + a.eps);
+                } else {
+                    dot = 0.0f;
+                }
+                float2 out[4];
+                if constexpr (GRAD) {
+                    const float2 r = twice(rstd), back = twice(-dot * inverse * rstd * rstd);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 n = __fmul2_rn(v[k], r);
+                        dw[k] = __ffma2_rn(d[k], n, dw[k]);
+                        out[k] = __ffma2_rn(n, back, __fmul2_rn(g[k], r));
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) out[k] = __fmul2_rn(__fmul2_rn(v[k], twice(rstd)), w[k]);
+                    if (turned) turn(out, angles, a.interleaved);
+                }
+                if (there) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        Run e;
+                        put_pair(e.e, out[2 * k]);
+                        put_pair(e.e + 2, out[2 * k + 1]);
+                        *reinterpret_cast<Run *>(y + (k ? apart : 0)) = e;
+                    }
+                }
+                y += kHeads * a.D;
             }
         }
     }
-    if (GRAD && a.partial) add_up<LANES>(a, dw, at, mine);
+    if (GRAD && a.partial) {
+        // lanes of the block that hold the same elements, in a fixed order; then the block's row
+        __shared__ float sums[kWarps][DC_HEAD_NORM_DIM_MAX];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int o = LANES; o < 32; o *= 2) {
+                dw[k].x += __shfl_xor_sync(0xffffffffu, dw[k].x, o);
+                dw[k].y += __shfl_xor_sync(0xffffffffu, dw[k].y, o);
+            }
+        if (lane < LANES && mine)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sums[warp][at[k / 2] + k % 2 * 2] = dw[k].x;
+                sums[warp][at[k / 2] + k % 2 * 2 + 1] = dw[k].y;
+            }
+        __syncthreads();
+        for (int e = threadIdx.x; e < a.D; e += kThreads) {
+            float t = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kWarps; ++r) t += sums[r][e];
+            a.partial[int64_t(blockIdx.x) * a.D + e] = t;
+        }
+    }
 }
 
 // Sizes and strides of any kind: a warp per head, four pairs a lane, one element an access. Pairs
@@ -226,23 +293,22 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
     constexpr int kPairs = DC_HEAD_NORM_DIM_MAX / 2 / 32;
     const int lane = threadIdx.x % 32, half = a.rotary / 2;
     int e[kPairs][2];  // the pairs' elements; D and above: none
-    float w[2][kPairs][2], dw[2][kPairs][2] = {};
+    float w[kPairs][2], dw[kPairs][2] = {};
+    const int which = int(blockIdx.x) >= a.blocks[0], heads = a.heads[which];
+    const int block = int(blockIdx.x) - (which ? a.blocks[0] : 0);
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) {
         const int p = lane + 32 * j;
         e[j][0] = p >= half || a.interleaved ? 2 * p : p;
         e[j][1] = p >= half || a.interleaved ? 2 * p + 1 : p + half;
 #pragma unroll
-        for (int which = 0; which < 2; ++which)
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                w[which][j][k] =
-                    e[j][k] < a.D && a.w[which] ? to_float(static_cast<const T *>(a.w[which])[e[j][k]]) : 1.0f;
+        for (int k = 0; k < 2; ++k)
+            w[j][k] = e[j][k] < a.D && a.w[which] ? to_float(static_cast<const T *>(a.w[which])[e[j][k]]) : 1.0f;
     }
     const float inverse = 1.0f / float(a.D);
-    const int64_t units = a.tokens * a.parts;
-    for (int64_t u = int64_t(blockIdx.x) * kWarps + threadIdx.x / 32; u < units; u += int64_t(gridDim.x) * kWarps) {
-        const Unit q = unit_at(a, u);
+    const int64_t units = a.tokens * a.parts[which], step = int64_t(a.blocks[which]) * kWarps;
+    for (int64_t u = int64_t(block) * kWarps + threadIdx.x / 32; u < units; u += step) {
+        const Unit q = unit_at(a, which, u);
         float c[kPairs], s[kPairs];
         const int64_t position = a.positions[q.token];
 #pragma unroll
@@ -251,10 +317,9 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
             s[j] = 0.0f;
             if (lane + 32 * j < half) angle(position, a.turns[lane + 32 * j], c[j], s[j]);
         }
-        for (int at = q.h0; at < q.h1; ++at) {
-            const int which = at >= a.heads[0], h = at - (which ? a.heads[0] : 0);
+        for (int h = q.h0; h < q.h1; ++h) {
             const T *x = static_cast<const T *>(a.x[which]) + q.token * a.token[which] + h * a.head[which];
-            const int64_t row = (q.token * a.heads[which] + h) * a.D;
+            const int64_t row = (q.token * heads + h) * a.D;
             float v[kPairs][2], d[kPairs][2];
             float square = 0.0f, along = 0.0f;
 #pragma unroll
@@ -274,13 +339,12 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
                     t[j][1] = r * c[j] + sign * p * s[j];
                 }
             };
-            auto weight = [&](int j, int k) { return which ? w[1][j][k] : w[0][j][k]; };
             if (GRAD) {
                 turn(d, -1.0f);
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) along += d[j][k] * weight(j, k) * v[j][k];
+                    for (int k = 0; k < 2; ++k) along += d[j][k] * w[j][k] * v[j][k];
             }
             float rstd = 1.0f;
             if (a.norm) {
@@ -300,12 +364,10 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (GRAD) {
-                        const float t = d[j][k] * (v[j][k] * rstd);
-                        if (which) dw[1][j][k] += t;
-                        else dw[0][j][k] += t;
-                        out[j][k] = rstd * (d[j][k] * weight(j, k) - v[j][k] * back);
+                        dw[j][k] += d[j][k] * (v[j][k] * rstd);
+                        out[j][k] = rstd * (d[j][k] * w[j][k] - v[j][k] * back);
                     } else {
-                        out[j][k] = v[j][k] * rstd * weight(j, k);
+                        out[j][k] = v[j][k] * rstd * w[j][k];
                     }
                 }
             if (!GRAD) turn(out, 1.0f);
@@ -318,69 +380,101 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
         }
     }
     if (GRAD && a.partial) {
-        __shared__ float sums[2][kWarps][DC_HEAD_NORM_DIM_MAX];
+        __shared__ float sums[kWarps][DC_HEAD_NORM_DIM_MAX];
 #pragma unroll
-        for (int which = 0; which < 2; ++which)
+        for (int j = 0; j < kPairs; ++j)
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j)
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    if (e[j][k] < a.D) sums[which][threadIdx.x / 32][e[j][k]] = dw[which][j][k];
+            for (int k = 0; k < 2; ++k)
+                if (e[j][k] < a.D) sums[threadIdx.x / 32][e[j][k]] = dw[j][k];
         __syncthreads();
-        for (int i = threadIdx.x; i < 2 * a.D; i += kThreads) {
-            const int which = i / a.D, at = i - which * a.D;
+        for (int at = threadIdx.x; at < a.D; at += kThreads) {
             float t = 0.0f;
 #pragma unroll
-            for (int r = 0; r < kWarps; ++r) t += sums[which][r][at];
-            a.partial[int64_t(blockIdx.x) * 2 * a.D + i] = t;
+            for (int r = 0; r < kWarps; ++r) t += sums[r][at];
+            a.partial[int64_t(blockIdx.x) * a.D + at] = t;
         }
     }
 }
 
-// dw of both weights from the blocks' rows, in a fixed order: a warp per element.
-__global__ void __launch_bounds__(kThreads)
-weight_sums_kernel(const float *partial, int blocks, int D, float *dw_q, float *dw_k)
+// dw of both weights from the blocks' rows, in a fixed order: 32 elements a block, a warp every
+// 32nd row.
+__global__ void __launch_bounds__(1024)
+weight_sums_kernel(const float *partial, int q_blocks, int k_blocks, int D, float *dw_q, float *dw_k)
 {
-    const int i = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x % 32;
-    if (i >= 2 * D) return;
+    __shared__ float sums[32][33];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, e = blockIdx.x * 32 + lane;
+    float *const out = blockIdx.y ? dw_k : dw_q;
+    const int first = blockIdx.y ? q_blocks : 0, end = blockIdx.y ? q_blocks + k_blocks : q_blocks;
     float t = 0.0f;
-    for (int b = lane; b < blocks; b += 32) t += partial[int64_t(b) * 2 * D + i];
+    if (e < D)
+#pragma unroll 8
+        for (int b = first + warp; b < end; b += 32) t += partial[int64_t(b) * D + e];
+    sums[warp][lane] = t;
+    __syncthreads();
+    t = sums[lane][warp];
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) t += __shfl_xor_sync(0xffffffffu, t, o);
-    float *out = i < D ? dw_q : dw_k;
-    if (lane == 0 && out) out[i < D ? i : i - D] = t;
+    const int at = blockIdx.x * 32 + warp;
+    if (lane == 0 && at < D && out) out[at] = t;
 }
 
-constexpr int kMostBlocks = 8 * 160;  // rows that the weights' gradients may have
+constexpr int kMostBlocks = 4 * 160;  // rows that the weights' gradients may have
+
+template <typename T, int LANES, bool GRAD>
+cudaError_t launch_runs(const HeadNormArgs &a, cudaStream_t stream)
+{
+    constexpr int smem = kWarps * kAhead * kUnroll * 2 * (GRAD ? 2 : 1) * 32 * int(sizeof(Vec<T, 4>));
+    auto kernel = head_norm_kernel<T, LANES, GRAD>;
+    static DeviceCache cache;
+    int ready = 0;
+    const cudaError_t e = cache.get(ready, [&](int &v) {
+        v = 1;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    });
+    if (e != cudaSuccess) return e;
+    kernel<<<a.blocks[0] + a.blocks[1], kThreads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
 
 template <typename T, bool GRAD>
-cudaError_t launch(HeadNormArgs a, bool vector, cudaStream_t stream)
+cudaError_t launch(HeadNormArgs a, bool runs, cudaStream_t stream)
 {
     int sms = 0;
-    const cudaError_t e = sm_count(sms);
+    cudaError_t e = sm_count(sms);
     if (e != cudaSuccess) return e;
-    // Few tokens: heads are dealt to warps as finely as needed to fill the SMs
-    const int heads = a.heads[0] + a.heads[1], lanes = a.D <= 64 ? 8 : a.D <= 128 ? 16 : 32;
-    const int least = vector ? 32 / lanes * kUnroll : 1;
-    const int64_t wanted = int64_t(sms) * 4 * kWarps;
-    a.parts = 1;
-    while (a.tokens * a.parts < wanted && heads > a.parts * least) a.parts *= 2;
-    a.per_part = (heads + a.parts - 1) / a.parts;
-    const int64_t blocks = (a.tokens * a.parts + kWarps - 1) / kWarps;
-    int most = sms * 8 < kMostBlocks ? sms * 8 : kMostBlocks;
-    const int grid = int(blocks < most ? blocks : most);
-    if (!vector) {
-        head_norm_any_kernel<T, GRAD><<<grid, kThreads, 0, stream>>>(a);
-    } else {
-        switch (lanes) {
-            case 8: head_norm_kernel<T, 8, GRAD><<<grid, kThreads, 0, stream>>>(a); break;
-            case 16: head_norm_kernel<T, 16, GRAD><<<grid, kThreads, 0, stream>>>(a); break;
-            default: head_norm_kernel<T, 32, GRAD><<<grid, kThreads, 0, stream>>>(a);
-        }
+    // Few tokens: heads are dealt to warps as finely as needed to fill the SMs. Many: the blocks that
+    // fit at a time, by the shares of queries and keys.
+    const int lanes = a.D <= 64 ? 8 : a.D <= 128 ? 16 : 32, least = runs ? 32 / lanes * kUnroll : 1;
+    int most = sms * (runs ? kResident<T, GRAD> : 4);
+    if (most > kMostBlocks) most = kMostBlocks;
+    int64_t blocks[2];
+    for (int i = 0; i < 2; ++i) {
+        a.parts[i] = 1;
+        while (a.tokens * a.parts[i] < int64_t(sms) * kWarps && a.heads[i] > a.parts[i] * least) a.parts[i] *= 2;
+        a.per_part[i] = (a.heads[i] + a.parts[i] - 1) / a.parts[i];
+        blocks[i] = (a.tokens * a.parts[i] + kWarps - 1) / kWarps;
     }
-    if (GRAD && a.partial)
-        weight_sums_kernel<<<(2 * a.D + kWarps - 1) / kWarps, kThreads, 0, stream>>>(a.partial, grid, a.D, a.dw[0],
-                                                                                     a.dw[1]);
+    if (blocks[0] + blocks[1] > most) {
+        int64_t q = int64_t(most) * a.heads[0] / (a.heads[0] + a.heads[1]);
+        q = q < 1 ? 1 : q > most - 1 ? most - 1 : q;
+        if (blocks[0] < q) q = blocks[0];
+        const int64_t k = most - q;
+        blocks[0] = q;
+        if (blocks[1] > k) blocks[1] = k;
+    }
+    a.blocks[0] = int(blocks[0]);
+    a.blocks[1] = int(blocks[1]);
+    if (!runs) {
+        head_norm_any_kernel<T, GRAD><<<a.blocks[0] + a.blocks[1], kThreads, 0, stream>>>(a);
+        e = cudaGetLastError();
+    } else {
+        e = lanes == 8    ? launch_runs<T, 8, GRAD>(a, stream)
+            : lanes == 16 ? launch_runs<T, 16, GRAD>(a, stream)
+                          : launch_runs<T, 32, GRAD>(a, stream);
+    }
+    if (e != cudaSuccess || !GRAD || !a.partial) return e;
+    weight_sums_kernel<<<dim3((a.D + 31) / 32, 2), 1024, 0, stream>>>(a.partial, a.blocks[0], a.blocks[1], a.D, a.dw[0],
+                                                                      a.dw[1]);
     return cudaGetLastError();
 }
 
@@ -398,7 +492,7 @@ bool in_runs(int dtype, const HeadNormArgs &a, bool grad)
 
 }  // namespace
 
-size_t head_norm_workspace(int D) { return sizeof(float) * 2 * size_t(D) * kMostBlocks; }
+size_t head_norm_workspace(int D) { return sizeof(float) * size_t(D) * kMostBlocks; }
 
 cudaError_t launch_head_norm(int dtype, const HeadNormArgs &a, cudaStream_t stream)
 {

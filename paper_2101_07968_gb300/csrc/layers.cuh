@@ -175,7 +175,7 @@ struct HeadNormArgs {
     bool interleaved, norm;
     float eps;
     float *partial;           // gradient of the weights: the blocks' sums (nullable)
-    int32_t parts, per_part;  // of a token's heads, and the heads of one (set by the launcher)
+    int32_t parts[2], per_part[2], blocks[2];  // of a token's heads, the heads of one, the grid (set by the launcher)
     uint64_t turns[DC_HEAD_NORM_DIM_MAX / 2];  // of pair i per position, in 2^-64 of a turn
 };
 size_t head_norm_workspace(int D);
