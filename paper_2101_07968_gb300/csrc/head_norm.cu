@@ -16,6 +16,8 @@
 // in turn with the angles in registers. What it takes next comes by asynchronous copies, each lane
 // its own runs, several chunks ahead: loads to registers kept too few bytes on their way
 // (32,768 tokens x 40 heads x 128, gradient: 419 us at 25 % occupancy and 31 % of the issue slots).
+#include <type_traits>
+
 #include "layers.cuh"
 
 namespace dc {
@@ -23,7 +25,6 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 2;  // heads of a group in a chunk
-constexpr int kAhead = 4;   // chunks in a warp's ring
 
 __device__ __forceinline__ void angle(int64_t position, uint64_t turns, float &c, float &s)
 {
@@ -89,25 +90,30 @@ __device__ __forceinline__ void unpack(const Vec<T, 4> &run, float2 *v)
     v[1] = pair_of(run.e + 2);
 }
 
-// Blocks of an SM: what their rings leave room for (64 KB of 16-bit gradients' each).
+// Blocks of an SM: what registers (128 a thread for the gradient, or it spills) and rings leave room for.
 template <typename T, bool GRAD>
-constexpr int kResident = sizeof(T) == 4 ? (GRAD ? 1 : 3) : (GRAD ? 3 : 4);
+constexpr int kResident = GRAD ? 2 : 3;
+// chunks in a warp's ring
+template <typename T, bool GRAD>
+constexpr int kRing = GRAD && sizeof(T) == 4 ? 3 : 4;
 
-template <typename T, int LANES, bool GRAD>
+// PLAIN: every lane of a group has elements, all of them turn, and the halves of pairs are apart, which
+// most heads are: no branch between the heads of a chunk, so that their instructions mix.
+template <typename T, int LANES, bool GRAD, bool PLAIN>
 __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel(const __grid_constant__ HeadNormArgs a)
 {
     constexpr int kHeads = 32 / LANES, kChunk = kHeads * kUnroll;  // heads at a time, and of a chunk
-    constexpr int kRuns = kUnroll * 2 * (GRAD ? 2 : 1);
+    constexpr int kRuns = kUnroll * 2 * (GRAD ? 2 : 1), kAhead = kRing<T, GRAD>;
     using Run = Vec<T, 4>;
     extern __shared__ __align__(16) unsigned char dyn[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % LANES, group = lane / LANES;
     Run *const ring = reinterpret_cast<Run *>(dyn) + size_t(warp) * kAhead * kRuns * 32 + lane;
     const int which = int(blockIdx.x) >= a.blocks[0];
     const int block = int(blockIdx.x) - (which ? a.blocks[0] : 0);
-    const bool mine = l * 8 < a.D, turned = l * 8 < a.rotary;
+    const bool mine = PLAIN || l * 8 < a.D, turned = PLAIN || l * 8 < a.rotary, interleaved = !PLAIN && a.interleaved;
     // first elements of the lane's two runs
     int at[2] = {8 * l, 8 * l + 4};
-    if (turned && !a.interleaved) {
+    if (turned && !interleaved) {
         at[0] = 4 * l;
         at[1] = a.rotary / 2 + 4 * l;
     }
@@ -127,37 +133,41 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
     const int64_t units = a.tokens * a.parts[which], step = int64_t(a.blocks[which]) * kWarps;
     const int64_t first = int64_t(block) * kWarps + warp;
 
-    // chunks on their way: the next one's unit and how many of its heads are left, and the lane's runs there
+    // chunks on their way: the next one's unit, and the first of its heads
     int64_t next = first;
-    int left = 0, filled = 0;
-    const T *from = nullptr, *from_dy = nullptr;
-    const int64_t x_group = kHeads * a.head[which], apart = at[1] - at[0];
+    int to_h = 0, to_n = 0, filled = 0;
+    const T *from = nullptr, *from_dy = nullptr;  // the lane's runs in the unit's first head
+    const int64_t apart = at[1] - at[0], head = a.head[which];
     auto start = [&] {
         if (next >= units) return;
         const Unit q = unit_at(a, which, next);
-        left = q.h1 - q.h0 - group;
-        from = x0 + q.token * a.token[which] + (q.h0 + group) * a.head[which] + at[0];
-        if (GRAD) from_dy = static_cast<const T *>(a.dy[which]) + (q.token * heads + q.h0 + group) * a.D + at[0];
+        to_h = 0;
+        to_n = q.h1 - q.h0;
+        from = x0 + q.token * a.token[which] + q.h0 * head + at[0];
+        if (GRAD) from_dy = static_cast<const T *>(a.dy[which]) + (q.token * heads + q.h0) * a.D + at[0];
     };
     auto bring = [&] {
         if (next < units) {
             Run *const p = ring + filled * kRuns * 32;
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
-                if (mine && left > i * kHeads) {
-                    copy_ahead<sizeof(Run)>(p + 2 * i * 32, from);
-                    copy_ahead<sizeof(Run)>(p + (2 * i + 1) * 32, from + apart);
+                // past the last head: the first again, whose products are not used
+                int h = to_h + i * kHeads + group;
+                h = h < to_n ? h : 0;
+                if (mine) {
+                    const T *const p0 = from + h * head;
+                    copy_ahead<sizeof(Run)>(p + 2 * i * 32, p0);
+                    copy_ahead<sizeof(Run)>(p + (2 * i + 1) * 32, p0 + apart);
                     if (GRAD) {
-                        copy_ahead<sizeof(Run)>(p + (2 * (kUnroll + i)) * 32, from_dy);
-                        copy_ahead<sizeof(Run)>(p + (2 * (kUnroll + i) + 1) * 32, from_dy + apart);
+                        const T *const p1 = from_dy + h * a.D;
+                        copy_ahead<sizeof(Run)>(p + (2 * (kUnroll + i)) * 32, p1);
+                        copy_ahead<sizeof(Run)>(p + (2 * (kUnroll + i) + 1) * 32, p1 + apart);
                     }
                 }
-                from += x_group;
-                if (GRAD) from_dy += kHeads * a.D;
             }
             filled = (filled + 1) % kAhead;
-            left -= kChunk;
-            if (left + group <= 0) {
+            to_h += kChunk;
+            if (to_h >= to_n) {
                 next += step;
                 start();
             }
@@ -192,61 +202,62 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
             asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
             const Run *const p = ring + used * kRuns * 32;
             used = (used + 1) % kAhead;
+            float2 v[kUnroll][4], d[GRAD ? kUnroll : 1][4], g[GRAD ? kUnroll : 1][4];
+            float sum[kUnroll], dot[kUnroll];
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
-                const bool there = mine && h0 + i * kHeads + group < q.h1;
-                float2 v[4], d[GRAD ? 4 : 1];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    v[k] = twice(0.0f);
-                    if (GRAD) d[k] = twice(0.0f);
-                }
-                if (there) {
-                    unpack(p[2 * i * 32], v);
-                    unpack(p[(2 * i + 1) * 32], v + 2);
-                    if constexpr (GRAD) {
-                        unpack(p[2 * (kUnroll + i) * 32], d);
-                        unpack(p[(2 * (kUnroll + i) + 1) * 32], d + 2);
-                    }
-                }
-                float2 square = __fmul2_rn(v[0], v[0]), along = twice(0.0f);
-#pragma unroll
-                for (int k = 1; k < 4; ++k) square = __ffma2_rn(v[k], v[k], square);
-                float2 g[GRAD ? 4 : 1];
+                unpack(p[2 * i * 32], v[i]);
+                unpack(p[(2 * i + 1) * 32], v[i] + 2);
                 if constexpr (GRAD) {
-                    if (turned) turn(d, angles, a.interleaved);
+                    unpack(p[2 * (kUnroll + i) * 32], d[i]);
+                    unpack(p[(2 * (kUnroll + i) + 1) * 32], d[i] + 2);
+                }
+                if (!mine)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        g[k] = __fmul2_rn(d[k], w[k]);
-                        along = __ffma2_rn(g[k], v[k], along);
+                        v[i][k] = twice(0.0f);
+                        if (GRAD) d[i][k] = twice(0.0f);
                     }
-                }
-                float rstd = 1.0f, sum = square.x + square.y, dot = along.x + along.y;
-                if (a.norm) {
+                float2 square = __fmul2_rn(v[i][0], v[i][0]), along = twice(0.0f);
 #pragma unroll
-                    for (int o = LANES / 2; o > 0; o /= 2) {
-                        sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                        if (GRAD) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                for (int k = 1; k < 4; ++k) square = __ffma2_rn(v[i][k], v[i][k], square);
+                if constexpr (GRAD) {
+                    if (turned) turn(d[i], angles, interleaved);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        g[i][k] = __fmul2_rn(d[i][k], w[k]);
+                        along = __ffma2_rn(g[i][k], v[i][k], along);
                     }
-                    rstd = rsqrtf(sum * inverse + a.eps);
-                } else {
-                    dot = 0.0f;
                 }
+                sum[i] = square.x + square.y;
+                dot[i] = along.x + along.y;
+            }
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o /= 2)
+#pragma unroll
+                for (int i = 0; i < kUnroll; ++i) {
+                    sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+                    if (GRAD) dot[i] += __shfl_xor_sync(0xffffffffu, dot[i], o);
+                }
+#pragma unroll
+            for (int i = 0; i < kUnroll; ++i) {
+                const bool there = h0 + i * kHeads + group < q.h1;
+                const float rstd = a.norm ? rsqrtf(sum[i] * inverse + a.eps) : 1.0f;
                 float2 out[4];
                 if constexpr (GRAD) {
-                    const float2 r = twice(rstd), back = twice(-dot * inverse * rstd * rstd);
+                    const float2 r = twice(rstd), back = twice(a.norm ? -dot[i] * inverse * rstd * rstd : 0.0f);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float2 n = __fmul2_rn(v[k], r);
-                        dw[k] = __ffma2_rn(d[k], n, dw[k]);
-                        out[k] = __ffma2_rn(n, back, __fmul2_rn(g[k], r));
+                        const float2 n = __fmul2_rn(v[i][k], r);
+                        if (there) dw[k] = __ffma2_rn(d[i][k], n, dw[k]);
+                        out[k] = __ffma2_rn(n, back, __fmul2_rn(g[i][k], r));
                     }
                 } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) out[k] = __fmul2_rn(__fmul2_rn(v[k], twice(rstd)), w[k]);
-                    if (turned) turn(out, angles, a.interleaved);
+                    for (int k = 0; k < 4; ++k) out[k] = __fmul2_rn(__fmul2_rn(v[i][k], twice(rstd)), w[k]);
+                    if (turned) turn(out, angles, interleaved);
                 }
-                if (there) {
+                if (mine && there) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         Run e;
@@ -420,11 +431,11 @@ weight_sums_kernel(const float *partial, int q_blocks, int k_blocks, int D, floa
 
 constexpr int kMostBlocks = 4 * 160;  // rows that the weights' gradients may have
 
-template <typename T, int LANES, bool GRAD>
+template <typename T, int LANES, bool GRAD, bool PLAIN>
 cudaError_t launch_runs(const HeadNormArgs &a, cudaStream_t stream)
 {
-    constexpr int smem = kWarps * kAhead * kUnroll * 2 * (GRAD ? 2 : 1) * 32 * int(sizeof(Vec<T, 4>));
-    auto kernel = head_norm_kernel<T, LANES, GRAD>;
+    constexpr int smem = kWarps * kRing<T, GRAD> * kUnroll * 2 * (GRAD ? 2 : 1) * 32 * int(sizeof(Vec<T, 4>));
+    auto kernel = head_norm_kernel<T, LANES, GRAD, PLAIN>;
     static DeviceCache cache;
     int ready = 0;
     const cudaError_t e = cache.get(ready, [&](int &v) {
@@ -468,9 +479,13 @@ cudaError_t launch(HeadNormArgs a, bool runs, cudaStream_t stream)
         head_norm_any_kernel<T, GRAD><<<a.blocks[0] + a.blocks[1], kThreads, 0, stream>>>(a);
         e = cudaGetLastError();
     } else {
-        e = lanes == 8    ? launch_runs<T, 8, GRAD>(a, stream)
-            : lanes == 16 ? launch_runs<T, 16, GRAD>(a, stream)
-                          : launch_runs<T, 32, GRAD>(a, stream);
+        auto go = [&](auto plain) {
+            constexpr bool kPlain = decltype(plain)::value;
+            return lanes == 8    ? launch_runs<T, 8, GRAD, kPlain>(a, stream)
+                   : lanes == 16 ? launch_runs<T, 16, GRAD, kPlain>(a, stream)
+                                 : launch_runs<T, 32, GRAD, kPlain>(a, stream);
+        };
+        e = a.D == 8 * lanes && a.rotary == a.D && !a.interleaved ? go(std::true_type()) : go(std::false_type());
     }
     if (e != cudaSuccess || !GRAD || !a.partial) return e;
     weight_sums_kernel<<<dim3((a.D + 31) / 32, 2), 1024, 0, stream>>>(a.partial, a.blocks[0], a.blocks[1], a.D, a.dw[0],
