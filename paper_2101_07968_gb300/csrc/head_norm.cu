@@ -12,7 +12,7 @@
 // Both directions are bound by memory: 2 (3) accesses of each element. A group of 8, 16 or 32 lanes
 // takes a head, eight elements a lane as two runs of four: the two halves of four pairs, so that
 // a pair is in one lane, and a run of the lanes is whole lines. Blocks are dealt to queries and keys by
-// their shares, so that a thread holds one weight and its gradient; a warp takes a token's heads
+// their shares, so that a thread holds one weight and its gradient; a group takes a token's heads
 // in turn with the angles in registers. What it takes next comes by asynchronous copies, each lane
 // its own runs, several chunks ahead: loads to registers kept too few bytes on their way
 // (32,768 tokens x 40 heads x 128, gradient: 419 us at 25 % occupancy and 31 % of the issue slots).
@@ -24,7 +24,7 @@ namespace dc {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kUnroll = 2;  // heads of a group in a chunk
+constexpr int kUnroll = 2;  // heads in a chunk of a group
 
 __device__ __forceinline__ void angle(int64_t position, uint64_t turns, float &c, float &s)
 {
@@ -102,7 +102,7 @@ constexpr int kRing = GRAD && sizeof(T) == 4 ? 3 : 4;
 template <typename T, int LANES, bool GRAD, bool PLAIN>
 __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel(const __grid_constant__ HeadNormArgs a)
 {
-    constexpr int kHeads = 32 / LANES, kChunk = kHeads * kUnroll;  // heads at a time, and of a chunk
+    constexpr int kGroups = 32 / LANES;
     constexpr int kRuns = kUnroll * 2 * (GRAD ? 2 : 1), kAhead = kRing<T, GRAD>;
     using Run = Vec<T, 4>;
     extern __shared__ __align__(16) unsigned char dyn[];
@@ -130,8 +130,12 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
     const float inverse = 1.0f / float(a.D);
     const T *const x0 = static_cast<const T *>(a.x[which]);
     const int heads = a.heads[which];
-    const int64_t units = a.tokens * a.parts[which], step = int64_t(a.blocks[which]) * kWarps;
-    const int64_t first = int64_t(block) * kWarps + warp;
+    // a warp's groups take neighbouring units, and stay together: past the last unit, they do it again
+    // and write nothing
+    const int64_t units = a.tokens * a.parts[which], step = int64_t(a.blocks[which]) * kWarps * kGroups;
+    const int64_t first = (int64_t(block) * kWarps + warp) * kGroups;
+    const int per_unit = (a.per_part[which] + kUnroll - 1) / kUnroll * kUnroll;
+    auto unit = [&](int64_t u) { return unit_at(a, which, u + group < units ? u + group : units - 1); };
 
     // chunks on their way: the next one's unit, and the first of its heads
     int64_t next = first;
@@ -140,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
     const int64_t apart = at[1] - at[0], head = a.head[which];
     auto start = [&] {
         if (next >= units) return;
-        const Unit q = unit_at(a, which, next);
+        const Unit q = unit(next);
         to_h = 0;
         to_n = q.h1 - q.h0;
         from = x0 + q.token * a.token[which] + q.h0 * head + at[0];
@@ -152,8 +156,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
                 // past the last head: the first again, whose products are not used
-                int h = to_h + i * kHeads + group;
-                h = h < to_n ? h : 0;
+                const int h = to_h + i < to_n ? to_h + i : 0;
                 if (mine) {
                     const T *const p0 = from + h * head;
                     copy_ahead<sizeof(Run)>(p + 2 * i * 32, p0);
@@ -166,8 +169,8 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
                 }
             }
             filled = (filled + 1) % kAhead;
-            to_h += kChunk;
-            if (to_h >= to_n) {
+            to_h += kUnroll;
+            if (to_h >= per_unit) {
                 next += step;
                 start();
             }
@@ -179,9 +182,10 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
     for (int i = 0; i < kAhead - 1; ++i) bring();
 
     int used = 0;
-    int64_t position = first < units ? a.positions[unit_at(a, which, first).token] : 0;
+    int64_t position = first < units ? a.positions[unit(first).token] : 0;
     for (int64_t u = first; u < units; u += step) {
-        const Unit q = unit_at(a, which, u);
+        const Unit q = unit(u);
+        const int count = u + group < units ? q.h1 - q.h0 : 0;
         Turn angles;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -195,9 +199,9 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
             angles.s[j] = GRAD ? n : s;
             angles.n[j] = GRAD ? s : n;
         }
-        if (u + step < units) position = a.positions[unit_at(a, which, u + step).token];
-        T *y = static_cast<T *>(a.y[which]) + (q.token * heads + q.h0 + group) * a.D + at[0];
-        for (int h0 = q.h0; h0 < q.h1; h0 += kChunk) {
+        if (u + step < units) position = a.positions[unit(u + step).token];
+        T *y = static_cast<T *>(a.y[which]) + (q.token * heads + q.h0) * a.D + at[0];
+        for (int h0 = 0; h0 < per_unit; h0 += kUnroll) {
             bring();
             asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
             const Run *const p = ring + used * kRuns * 32;
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
                 }
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
-                const bool there = h0 + i * kHeads + group < q.h1;
+                const bool there = h0 + i < count;
                 const float rstd = a.norm ? rsqrtf(sum[i] * inverse + a.eps) : 1.0f;
                 float2 out[4];
                 if constexpr (GRAD) {
@@ -266,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
                         *reinterpret_cast<Run *>(y + (k ? apart : 0)) = e;
                     }
                 }
-                y += kHeads * a.D;
+                y += a.D;
             }
         }
     }
@@ -455,15 +459,16 @@ cudaError_t launch(HeadNormArgs a, bool runs, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     // Few tokens: heads are dealt to warps as finely as needed to fill the SMs. Many: the blocks that
     // fit at a time, by the shares of queries and keys.
-    const int lanes = a.D <= 64 ? 8 : a.D <= 128 ? 16 : 32, least = runs ? 32 / lanes * kUnroll : 1;
+    const int lanes = a.D <= 64 ? 8 : a.D <= 128 ? 16 : 32, least = runs ? kUnroll : 1;
+    const int units = kWarps * (runs ? 32 / lanes : 1);  // of a block at a time
     int most = sms * (runs ? kResident<T, GRAD> : 4);
     if (most > kMostBlocks) most = kMostBlocks;
     int64_t blocks[2];
     for (int i = 0; i < 2; ++i) {
         a.parts[i] = 1;
-        while (a.tokens * a.parts[i] < int64_t(sms) * kWarps && a.heads[i] > a.parts[i] * least) a.parts[i] *= 2;
+        while (a.tokens * a.parts[i] < int64_t(sms) * units && a.heads[i] > a.parts[i] * least) a.parts[i] *= 2;
         a.per_part[i] = (a.heads[i] + a.parts[i] - 1) / a.parts[i];
-        blocks[i] = (a.tokens * a.parts[i] + kWarps - 1) / kWarps;
+        blocks[i] = (a.tokens * a.parts[i] + units - 1) / units;
     }
     if (blocks[0] + blocks[1] > most) {
         int64_t q = int64_t(most) * a.heads[0] / (a.heads[0] + a.heads[1]);
