@@ -7,9 +7,12 @@
 // with P read from tensor memory and y held there. While one tile's warps are at their
 // exponentials the tensor cores work on the other tile.
 //
-//   warps 0-3, 4-7  a tile each: softmax, and the finished rows
-//   warp 8          copies (TMA)
-//   warp 9          products, by one thread
+//   warps 0-3, 4-7  a tile each: softmax
+//   warps 8-11      the finished rows of both tiles, while the next tiles' scores are made
+//   warp 12         copies (TMA)
+//   warp 13         products, by one thread
+//   warps 14, 15    look through the values on the diagonal
+// A launch has 128 registers a thread; the softmax's warps take more of them from the others.
 //
 // Rounding: P is rounded to the operands' type for the tensor cores, at most half a step of each
 // term, where y's own rounding is half a step of the sum; l adds the unrounded ones in floats.
@@ -19,7 +22,7 @@
 // A mask cuts only the block on the diagonal, the tile's last. Values there that are not finite
 // would reach rows that must not see them through 0 * inf. So rows after the sequence's end are overwritten
 // with zeros there, and the block's own are looked through: where one is not finite, that block's
-// y += P v is done by its own threads (masked_product).
+// y += P v is done by its tile's threads (masked_product).
 #include <cmath>
 
 #include "attention_mma.cuh"
@@ -29,9 +32,16 @@ namespace {
 
 using namespace am;
 
-constexpr int kThreads = 10 * 32;
+constexpr int kThreads = 16 * 32;
+constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;
+static_assert(2 * kSoftmaxRegs + 2 * kOtherRegs <= 4 * 128, "registers of the launch");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.0f;  // how far, in powers of two, the reference may be below the maximum
+
+__device__ __forceinline__ float positive_scale(const AttentionArgs &a)
+{
+    return (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * kLog2e;
+}
 
 struct Item {
     AttentionTile tile;
@@ -67,6 +77,13 @@ __device__ __forceinline__ Item item_at(const AttentionArgs &a, int64_t i)
     return q;
 }
 
+// Blocks of values on the diagonal, which are looked through: one for two heads, one for each of two tiles.
+template <bool PAIR>
+__device__ __forceinline__ uint32_t checks_of(const Item &q)
+{
+    return PAIR ? q.blocks[0] > 0 : (q.blocks[0] > 0) + (q.blocks[1] > 0);
+}
+
 template <typename T, int DP, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -75,13 +92,20 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     constexpr int kBoxes = DP / 64;
     constexpr uint32_t kBytes = kBoxes * kBox;  // of a tile in shared memory
     constexpr int kStages = DP == 64 ? 8 : 4;
+    constexpr int kChecks = 4;  // no more blocks of values are in the ring
     extern __shared__ unsigned char dyn[];
-    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2], met[2], last;
+    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2], y_free[2],
+        l_full[2],        look[kChecks], checked[kChecks], last;
     __shared__ uint32_t tmem_at, gave_up;
-    __shared__ uint32_t by_hand[2];  // a tile's block, counted from one, if its sums are done by hand
+    __shared__ uint32_t by_hand[kChecks];  // the check, counted from one, if its block's sums are done by hand
+
+    __shared__ float row_l[2][kTile], row_m[2][kTile];  // of finished tiles
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
+    auto is_by_hand = [&](uint32_t check) {
+        return *const_cast<volatile uint32_t *>(&by_hand[check % kChecks]) == check + 1;
+    };
     const uint32_t base = (bw::smem_addr(dyn) + 1023u) & ~1023u;
     const uint32_t ring = base + 2 * kBytes;
 
@@ -93,19 +117,24 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             bw::bar_init(bar(&p_half[i]), 4);
             bw::bar_init(bar(&p_full[i]), 4);
             bw::bar_init(bar(&y_full[i]), 1);
-            bw::bar_init(bar(&met[i]), 4);
-            by_hand[i] = 0;
+            bw::bar_init(bar(&y_free[i]), 4);
+            bw::bar_init(bar(&l_full[i]), 4);
         }
         for (int i = 0; i < kStages; ++i) {
             bw::bar_init(bar(&full[i]), 1);
             bw::bar_init(bar(&empty[i]), 1);
         }
+        for (int i = 0; i < kChecks; ++i) {
+            bw::bar_init(bar(&look[i]), 1);
+            bw::bar_init(bar(&checked[i]), 2);
+            by_hand[i] = 0;
+        }
         bw::bar_init(bar(&last), 1);
         gave_up = 0;
         bw::bar_init_fence();
     }
-    if (warp == 9) bw::tmem_alloc1(bw::smem_addr(&tmem_at), 512);
-    if (warp == 8 && lane == 0) {
+    if (warp == 13) bw::tmem_alloc1(bw::smem_addr(&tmem_at), 512);
+    if (warp == 12 && lane == 0) {
         bw::prefetch_map(&map_q);
         bw::prefetch_map(&map_k);
         bw::prefetch_map(&map_v);
@@ -116,13 +145,15 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const uint32_t tmem = tmem_at;  // scores of both tiles, then y of both
     const int64_t items = int64_t(a.plan->tiles) * (PAIR ? a.heads / 2 : a.heads);
 
-    if (warp == 8) {
+    if (warp >= 12) {
+        bw::fewer_registers<kOtherRegs>();
+        if (warp == 12) {
         if (bw::elect_one()) {  // copies
             int s = 0, done[2] = {0, 0};
             uint32_t phase = 1;
             bool ok = true;
             auto block = [&](const CUtensorMap &map, int head, int row) {
-                ok = ok && bw::bar_wait(bar(&empty[s]), phase, &gave_up);
+                ok = ok && bw::bar_wait_inline(bar(&empty[s]), phase, &gave_up);
                 if (!ok) return;
                 bw::bar_arrive_bytes(bar(&full[s]), kBytes);
                 for (int i = 0; i < kBoxes; ++i)
@@ -136,7 +167,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const Item q = item_at<PAIR>(a, i);
                 for (int x = 0; x < 2; ++x) {
                     if (q.blocks[x] == 0) continue;
-                    ok = ok && (done[x] == 0 || bw::bar_wait(bar(&q_free[x]), (done[x] - 1) & 1, &gave_up));
+                    ok = ok && (done[x] == 0 || bw::bar_wait_inline(bar(&q_free[x]), (done[x] - 1) & 1, &gave_up));
                     if (!ok) break;
                     ++done[x];
                     bw::bar_arrive_bytes(bar(&q_full[x]), kBytes);
@@ -151,17 +182,17 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
             }
         }
-    } else if (warp == 9) {
+        } else if (warp == 13) {
         if (bw::elect_one()) {  // products
             constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
             const uint32_t shape_s = bw::f16_shape(kBf, false, false, kTile, kTile);
             const uint32_t shape_y = bw::f16_shape(kBf, false, true, kTile, DP);
             uint32_t c = 0;  // blocks of the ring before this item
             int done[2] = {0, 0};
-            uint32_t blocks[2] = {0, 0};  // of either tile so far
+            uint32_t blocks[2] = {0, 0}, checks = 0;  // of either tile so far; of both
             bool ok = true;
             auto have = [&](uint32_t n) {
-                ok = ok && bw::bar_wait(bar(&full[n % kStages]), (n / kStages) & 1, &gave_up);
+                ok = ok && bw::bar_wait_inline(bar(&full[n % kStages]), (n / kStages) & 1, &gave_up);
                 return ok;
             };
             auto scores = [&](int x, uint32_t n) {
@@ -179,7 +210,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (n == 0) continue;
                 for (int x = 0; x < 2 && ok; ++x) {
                     if (q.blocks[x] == 0) continue;
-                    ok = bw::bar_wait(bar(&q_full[x]), done[x] & 1, &gave_up);
+                    ok = bw::bar_wait_inline(bar(&q_full[x]), done[x] & 1, &gave_up);
                     ++done[x];
                     if (!have(c)) break;
                     scores(x, c);
@@ -190,6 +221,9 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 for (int j = 0; j < n && ok; ++j) {
                     const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
                     if (!have(v)) break;
+                    // the diagonal's values are there: to be looked through
+                    for (int x = 0; x < (PAIR ? 1 : 2); ++x)
+                        if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&look[(checks + x) % kChecks]));
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (j >= q.blocks[x]) continue;
                         const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
@@ -199,13 +233,15 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                                 bw::mma1_tmem(tmem + 2 * kTile + x * DP, tmem + x * kTile + i * 8, dv + i * 128, shape_y,
                                               j > 0 || i > 0);
                         };
-                        ok = bw::bar_wait(bar(&p_half[x]), blocks[x] & 1, &gave_up);
+                        // the rows before these have left
+                        ok = j > 0 || done[x] < 2 || bw::bar_wait_inline(bar(&y_free[x]), done[x] & 1, &gave_up);
+                        ok = ok && bw::bar_wait_inline(bar(&p_half[x]), blocks[x] & 1, &gave_up);
                         if (!ok) break;
                         bw::fence_after();
-                        // (set before the first half where it is set)
-                        const bool own = *const_cast<volatile uint32_t *>(&by_hand[x]) != blocks[x] + 1;
+                        // (known before the first half is handed over)
+                        const bool own = j + 1 < q.blocks[x] || !is_by_hand(checks + (PAIR ? 0 : x));
                         if (own) half(0);
-                        ok = bw::bar_wait(bar(&p_full[x]), blocks[x]++ & 1, &gave_up);
+                        ok = bw::bar_wait_inline(bar(&p_full[x]), blocks[x]++ & 1, &gave_up);
                         if (!ok) break;
                         bw::fence_after();
                         if (own) half(kTile / 32);
@@ -222,34 +258,91 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (j + 1 < n) bw::commit1(bar(&empty[k % kStages]));
                 }
                 c += 2 * n;
+                checks += checks_of<PAIR>(q);
             }
             // arrivals land in this CTA's memory: it may not end before the last
             bw::commit1(bar(&last));
-            bw::bar_wait(bar(&last), 0, &gave_up);
+            bw::bar_wait_inline(bar(&last), 0, &gave_up);
         }
-    } else {  // softmax and the finished rows
-        const int x = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
-        const uint32_t at_s = lanes + x * kTile, at_y = lanes + 2 * kTile + x * DP;
+        } else {  // values on the diagonal
+        uint32_t c = 0, checks = 0;
+        bool ok = true;
+        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+            const Item q = item_at<PAIR>(a, i);
+            const uint32_t n = checks_of<PAIR>(q);
+            for (uint32_t x = 0; x < n; ++x, ++checks) {
+                const uint32_t v = c + 2 * q.blocks[x] - 1;
+                // (the ring's own barrier is waited for when it cannot be a round ahead or behind)
+                ok = bw::bar_wait_inline(bar(&look[checks % kChecks]), (checks / kChecks) & 1, &gave_up) &&
+                     bw::bar_wait_inline(bar(&full[v % kStages]), (v / kStages) & 1, &gave_up);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                unsigned char *tile = dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes;
+                for (int r = (warp - 14) * 32 + lane; r < kTile; r += 64)
+                    if (look_through<T, DP>(tile, r, q.rows[x]))
+                        *const_cast<volatile uint32_t *>(&by_hand[checks % kChecks]) = checks + 1;
+                __syncwarp();
+                if (lane == 0) bw::bar_arrive(bar(&checked[checks % kChecks]));
+            }
+            c += 2 * max(q.blocks[0], q.blocks[1]);
+        }
+        }
+    } else if (warp >= 8) {  // finished rows
+        bw::fewer_registers<kOtherRegs>();
+        const int w = warp & 3, r = w * 32 + lane;
+        const uint32_t at_y = tmem + (uint32_t(w * 32) << 16) + 2 * kTile;
         const bool wide = a.D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
+        const float scale = positive_scale(a);
+        uint32_t done[2] = {0, 0};
+        bool ok = true;
+        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+            const Item q = item_at<PAIR>(a, i);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                T *y = static_cast<T *>(a.y) + (int64_t(q.row0[x]) + r) * a.heads * a.D + int64_t(q.head[x]) * a.D;
+                float *lse = a.lse + q.head[x] * a.tokens + q.row0[x] + r;
+                if (q.blocks[x] == 0) {
+                    if (r < q.rows[x]) {  // of no sequence
+                        put_zeros(y, a.D, wide);
+                        *lse = 0.0f;
+                    }
+                    continue;
+                }
+                const uint32_t phase = done[x]++ & 1;
+                ok = ok && bw::bar_wait_inline(bar(&l_full[x]), phase, &gave_up) &&
+                     bw::bar_wait_inline(bar(&y_full[x]), phase, &gave_up);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                bw::fence_after();
+                const float l = row_l[x][r], m = row_m[x][r], by = 1.0f / l;
+#pragma unroll 1
+                for (int d = 0; d < DP; d += 32) {
+                    float v[32];
+                    __syncwarp();
+                    bw::tmem_load(at_y + x * DP + d, v);
+                    if (d + 32 == DP) {
+                        bw::fence_before();
+                        __syncwarp();
+                        if (lane == 0) bw::bar_arrive(bar(&y_free[x]));
+                    }
+                    if (r < q.rows[x]) put_row(y + d, v, by, a.D - d, wide);
+                }
+                if (r < q.rows[x]) *lse = (m * scale + log2f(l)) * kLn2;
+            }
+        }
+    } else {  // softmax
+        bw::more_registers<kSoftmaxRegs>();
+        const int x = warp >> 2, w = warp & 3, r = w * 32 + lane;
+        const uint32_t lanes = tmem + (uint32_t(w * 32) << 16);
+        const uint32_t at_s = lanes + x * kTile, at_y = lanes + 2 * kTile + x * DP;
         // scores are compared before they are scaled: by a positive factor, after the sign (or zero)
         const float sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
-        const float scale = (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * kLog2e;
-        uint32_t blocks = 0, finished = 0, c = 0;  // blocks and rounds of this tile; blocks of the ring
+        const float scale = positive_scale(a);
+        uint32_t blocks = 0, done = 0, c = 0, checks = 0;  // blocks and rounds of this tile; blocks of the ring; checks
         bool ok = true;
         for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
             const Item q = item_at<PAIR>(a, i);
             const int n = q.blocks[x];
-            T *y = static_cast<T *>(a.y) + (int64_t(q.row0[x]) + r) * a.heads * a.D + int64_t(q.head[x]) * a.D;
-            float *lse = a.lse + q.head[x] * a.tokens + q.row0[x] + r;
-            if (n == 0) {
-                if (r < q.rows[x]) {  // of no sequence
-                    put_zeros(y, a.D, wide);
-                    *lse = 0.0f;
-                }
-                c += 2 * max(q.blocks[0], q.blocks[1]);
-                continue;
-            }
             float m = -INFINITY, l = 0.0f;
             auto hand_over = [&](uint64_t(&to)[2]) {  // P so far, to the products
                 bw::tmem_stored();
@@ -258,7 +351,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (lane == 0) bw::bar_arrive(bar(&to[x]));
             };
             for (int j = 0; j < n; ++j) {
-                ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&s_full[x]), blocks++ & 1, &gave_up));
+                ok = __all_sync(0xffffffffu, bw::bar_wait_inline(bar(&s_full[x]), blocks++ & 1, &gave_up));
                 if (!ok) break;
                 bw::fence_after();
                 float s[kTile];
@@ -272,9 +365,14 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     for (int e = 0; e < kTile; ++e) s[e] *= sign;
                 }
                 const bool diagonal = j == n - 1;
-                if (diagonal) {
+                if (diagonal) {  // a warp's rows see all of the 32 keys before theirs, and none of those after
 #pragma unroll
-                    for (int e = 0; e < kTile; ++e) s[e] = e <= r ? s[e] : -INFINITY;
+                    for (int e0 = 0; e0 < kTile; e0 += 32) {
+                        if (e0 < w * 32) continue;
+                        const int last = e0 == w * 32 ? lane : -1;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s[e0 + e] = e <= last ? s[e0 + e] : -INFINITY;
+                    }
                 }
                 float top[4];
 #pragma unroll
@@ -326,33 +424,25 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 l += sum[0].x + sum[0].y;
                 if (diagonal) {
                     bw::tmem_stored();
-                    const uint32_t v = c + 2 * j + 1;
-                    unsigned char *tile = dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes;
-                    ok = bw::bar_wait(bar(&full[v % kStages]), (v / kStages) & 1, &gave_up);
-                    if (ok && look_through<T, DP>(tile, r, q.rows[x])) *const_cast<volatile uint32_t *>(&by_hand[x]) = blocks;
-                    __syncwarp();
-                    if (lane == 0) bw::bar_arrive(bar(&met[x]));
-                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&met[x]), finished & 1, &gave_up) && ok);
-                    if (*const_cast<volatile uint32_t *>(&by_hand[x]) == blocks)
-                        masked_product<T, DP>(at_y, [&](int g) { return at_s + g * 16; }, 4, tile, 0, 0, r + 1, j > 0);
+                    const uint32_t check = checks + (PAIR ? 0 : x), v = c + 2 * j + 1;
+                    ok = bw::bar_wait_inline(bar(&checked[check % kChecks]), (check / kChecks) & 1, &gave_up);
+                    // y, l and m of the rows before have been read
+                    ok = ok && (done == 0 || bw::bar_wait_inline(bar(&y_free[x]), (done - 1) & 1, &gave_up));
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    row_l[x][r] = l;
+                    row_m[x][r] = m;
+                    if (is_by_hand(check))
+                        masked_product<T, DP>(at_y, [&](int g) { return at_s + g * 16; }, 4,
+                                              dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes, 0, 0, r + 1, j > 0);
                     hand_over(p_half);
+                    if (lane == 0) bw::bar_arrive(bar(&l_full[x]));
                 }
                 hand_over(p_full);
             }
             c += 2 * max(q.blocks[0], q.blocks[1]);
-            ok = ok && bw::bar_wait(bar(&y_full[x]), finished++ & 1, &gave_up);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            bw::fence_after();
-            const float by = 1.0f / l;
-#pragma unroll 1
-            for (int d = 0; d < DP; d += 32) {
-                float v[32];
-                __syncwarp();
-                bw::tmem_load(at_y + d, v);
-                if (r < q.rows[x]) put_row(y + d, v, by, a.D - d, wide);
-            }
-            if (r < q.rows[x]) *lse = (m * scale + log2f(l)) * kLn2;
+            checks += checks_of<PAIR>(q);
+            done += n > 0;
         }
     }
     __syncwarp();
@@ -363,7 +453,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     }
     bw::fence_before();
     __syncthreads();
-    if (warp == 9) bw::tmem_free1(tmem, 512);
+    if (warp == 13) bw::tmem_free1(tmem, 512);
 }
 
 // ------------------------------------------------------------------------------ host

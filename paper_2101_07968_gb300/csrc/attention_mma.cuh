@@ -85,7 +85,7 @@ __device__ __forceinline__ bool look_through(unsigned char *tile, int r, int row
 // CUDA cores: where B holds infinities or NaN that some lanes must not see, zero weights
 // would not hide them. w: packed pairs in tensor memory, 16 columns for 32 c, at(c / 32); DP columns of acc.
 template <typename T, int DP, typename At>
-__device__ __noinline__ void masked_product(uint32_t acc, At at, int groups, const unsigned char *tile, int row0, int from,
+__device__ __forceinline__ void masked_product(uint32_t acc, At at, int groups, const unsigned char *tile, int row0, int from,
                                             int end, bool add)
 {
     for (int d0 = 0; d0 < DP; d0 += 16) {

@@ -41,6 +41,19 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Registers of this warpgroup's threads from here on, in multiples of eight; what all of them ask for has
+// to fit in what the CTA was launched with, and the kernel must be free of calls.
+template <int N>
+__device__ __forceinline__ void more_registers()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void fewer_registers()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // ------------------------------------------------------------------------ mbarriers
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
 {
@@ -120,6 +133,19 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     for (int i = 0; i < 16; ++i)
         if (bar_try(bar, parity)) return true;
     return bar_wait_long(bar, parity, gave_up, progress);
+}
+// The same without a call.
+__device__ __forceinline__ bool bar_wait_inline(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    if (bar_try(bar, parity)) return true;
+    const uint64_t start = now_ns();
+#pragma unroll 1
+    for (uint32_t i = 1; i < kWaitTries; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if ((i & 63u) == 0 && (*gave_up || now_ns() - start > kWaitNs)) break;
+    }
+    *gave_up = 1u;
+    return false;
 }
 
 // --------------------------------------------------------------------------- copies
