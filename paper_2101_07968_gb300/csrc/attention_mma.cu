@@ -5,7 +5,8 @@
 // For each tile and block: scores S = q k^T [row][key] into tensor memory; four warps, a thread
 // a row, take the row's maximum and write P = 2^(s - m) in 16 bits over the scores; y += P v,
 // with P read from tensor memory and y held there. While one tile's warps are at their
-// exponentials the tensor cores work on the other tile.
+// exponentials the tensor cores work on the other tile; what a tile waits for is its P v and next S, so
+// the first 64 keys' P is handed over as soon as it is made.
 //
 //   warps 0-3, 4-7  a tile each: softmax
 //   warps 8-11      the finished rows of both tiles, while the next tiles' scores are made
@@ -38,11 +39,6 @@ static_assert(2 * kSoftmaxRegs + 2 * kOtherRegs <= 4 * 128, "registers of the la
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.0f;  // how far, in powers of two, the reference may be below the maximum
 
-__device__ __forceinline__ float positive_scale(const AttentionArgs &a)
-{
-    return (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * kLog2e;
-}
-
 struct Item {
     AttentionTile tile;
     int32_t head[2], row0[2], rows[2], blocks[2], kv;
@@ -53,7 +49,7 @@ __device__ __forceinline__ Item item_at(const AttentionArgs &a, int64_t i)
 {
     const int per = PAIR ? a.heads / 2 : a.heads;
     Item q;
-    const int64_t t = i / per;
+    const int64_t t = i < (int64_t(1) << 31) ? int64_t(uint32_t(i) / uint32_t(per)) : i / per;
     q.tile = plan_tiles(a.plan)[t];
     const int h = int(i - t * per);
     const int before = (q.tile.row0 - max(q.tile.first, 0)) / kTile;
@@ -84,6 +80,14 @@ __device__ __forceinline__ uint32_t checks_of(const Item &q)
     return PAIR ? q.blocks[0] > 0 : (q.blocks[0] > 0) + (q.blocks[1] > 0);
 }
 
+// Tiles of queries in shared memory, taken in turn: the two at work, and what comes next (a tile's last scores
+// are made well before its last P v, and rows come from memory).
+template <int DP>
+constexpr int kTilesOfQ = DP == 64 ? 4 : 3;
+template <int DP>
+constexpr int kRing = DP == 64 ? 8 : 4;  // blocks of keys or values
+constexpr uint32_t kSharedBytes = 2560;  // barriers and rows' sums
+
 template <typename T, int DP, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -91,49 +95,55 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 {
     constexpr int kBoxes = DP / 64;
     constexpr uint32_t kBytes = kBoxes * kBox;  // of a tile in shared memory
-    constexpr int kStages = DP == 64 ? 8 : 4;
+    constexpr int kStages = kRing<DP>;
+    constexpr int kQ = kTilesOfQ<DP>;
     constexpr int kChecks = 4;  // no more blocks of values are in the ring
-    extern __shared__ unsigned char dyn[];
-    __shared__ alignas(8) uint64_t q_full[2], q_free[2], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2], y_free[2],
-        l_full[2],        look[kChecks], checked[kChecks], last;
-    __shared__ uint32_t tmem_at, gave_up;
-    __shared__ uint32_t by_hand[kChecks];  // the check, counted from one, if its block's sums are done by hand
-
-    __shared__ float row_l[2][kTile], row_m[2][kTile];  // of finished tiles
+    extern __shared__ __align__(1024) unsigned char dyn[];
+    struct Shared {
+        uint64_t q_full[kQ], q_free[kQ], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2],
+            y_free[2], l_full[2], look[kChecks], checked[kChecks], last;
+        uint32_t tmem_at, gave_up;
+        uint32_t by_hand[kChecks];  // the check, counted from one, if its block's sums are done by hand
+        float row_l[2][kTile], row_m[2][kTile];  // of finished tiles
+    };
+    static_assert(sizeof(Shared) <= kSharedBytes, "room behind the tiles");
+    Shared &h = *reinterpret_cast<Shared *>(dyn + (kQ + kStages) * kBytes);
+    uint32_t *const gave_up = &h.gave_up;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
     auto is_by_hand = [&](uint32_t check) {
-        return *const_cast<volatile uint32_t *>(&by_hand[check % kChecks]) == check + 1;
+        return *const_cast<volatile uint32_t *>(&h.by_hand[check % kChecks]) == check + 1;
     };
-    const uint32_t base = (bw::smem_addr(dyn) + 1023u) & ~1023u;
-    const uint32_t ring = base + 2 * kBytes;
+    const uint32_t base = bw::smem_addr(dyn), ring = base + kQ * kBytes;
 
     if (threadIdx.x == 0) {
+        for (int i = 0; i < kQ; ++i) {
+            bw::bar_init(bar(&h.q_full[i]), 1);
+            bw::bar_init(bar(&h.q_free[i]), 1);
+        }
         for (int i = 0; i < 2; ++i) {
-            bw::bar_init(bar(&q_full[i]), 1);
-            bw::bar_init(bar(&q_free[i]), 1);
-            bw::bar_init(bar(&s_full[i]), 1);
-            bw::bar_init(bar(&p_half[i]), 4);
-            bw::bar_init(bar(&p_full[i]), 4);
-            bw::bar_init(bar(&y_full[i]), 1);
-            bw::bar_init(bar(&y_free[i]), 4);
-            bw::bar_init(bar(&l_full[i]), 4);
+            bw::bar_init(bar(&h.s_full[i]), 1);
+            bw::bar_init(bar(&h.p_half[i]), 4);
+            bw::bar_init(bar(&h.p_full[i]), 4);
+            bw::bar_init(bar(&h.y_full[i]), 1);
+            bw::bar_init(bar(&h.y_free[i]), 4);
+            bw::bar_init(bar(&h.l_full[i]), 4);
         }
         for (int i = 0; i < kStages; ++i) {
-            bw::bar_init(bar(&full[i]), 1);
-            bw::bar_init(bar(&empty[i]), 1);
+            bw::bar_init(bar(&h.full[i]), 1);
+            bw::bar_init(bar(&h.empty[i]), 1);
         }
         for (int i = 0; i < kChecks; ++i) {
-            bw::bar_init(bar(&look[i]), 1);
-            bw::bar_init(bar(&checked[i]), 2);
-            by_hand[i] = 0;
+            bw::bar_init(bar(&h.look[i]), 1);
+            bw::bar_init(bar(&h.checked[i]), 2);
+            h.by_hand[i] = 0;
         }
-        bw::bar_init(bar(&last), 1);
-        gave_up = 0;
+        bw::bar_init(bar(&h.last), 1);
+        h.gave_up = 0;
         bw::bar_init_fence();
     }
-    if (warp == 13) bw::tmem_alloc1(bw::smem_addr(&tmem_at), 512);
+    if (warp == 13) bw::tmem_alloc1(bw::smem_addr(&h.tmem_at), 512);
     if (warp == 12 && lane == 0) {
         bw::prefetch_map(&map_q);
         bw::prefetch_map(&map_k);
@@ -142,22 +152,24 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     bw::fence_before();
     __syncthreads();
     bw::fence_after();
-    const uint32_t tmem = tmem_at;  // scores of both tiles, then y of both
-    const int64_t items = int64_t(a.plan->tiles) * (PAIR ? a.heads / 2 : a.heads);
+    const uint32_t tmem = h.tmem_at;  // scores of both tiles, then y of both
+    // the swizzled copies need tiles on 1,024-byte boundaries
+    const int64_t items = (base & 1023u) ? 0 : int64_t(a.plan->tiles) * (PAIR ? a.heads / 2 : a.heads);
+    if ((base & 1023u) && threadIdx.x == 0) h.gave_up = 1;
 
     if (warp >= 12) {
         bw::fewer_registers<kOtherRegs>();
         if (warp == 12) {
         if (bw::elect_one()) {  // copies
-            int s = 0, done[2] = {0, 0};
-            uint32_t phase = 1;
+            int s = 0;
+            uint32_t phase = 1, tiles = 0;  // of queries so far
             bool ok = true;
             auto block = [&](const CUtensorMap &map, int head, int row) {
-                ok = ok && bw::bar_wait_inline(bar(&empty[s]), phase, &gave_up);
+                ok = ok && bw::bar_wait_inline(bar(&h.empty[s]), phase, gave_up);
                 if (!ok) return;
-                bw::bar_arrive_bytes(bar(&full[s]), kBytes);
+                bw::bar_arrive_bytes(bar(&h.full[s]), kBytes);
                 for (int i = 0; i < kBoxes; ++i)
-                    bw::copy_3d1(ring + s * kBytes + i * kBox, &map, 64 * i, head, row, bar(&full[s]));
+                    bw::copy_3d1(ring + s * kBytes + i * kBox, &map, 64 * i, head, row, bar(&h.full[s]));
                 if (++s == kStages) {
                     s = 0;
                     phase ^= 1;
@@ -167,12 +179,13 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const Item q = item_at<PAIR>(a, i);
                 for (int x = 0; x < 2; ++x) {
                     if (q.blocks[x] == 0) continue;
-                    ok = ok && (done[x] == 0 || bw::bar_wait_inline(bar(&q_free[x]), (done[x] - 1) & 1, &gave_up));
+                    const uint32_t at = tiles % kQ;
+                    ok = ok && (tiles < kQ || bw::bar_wait_inline(bar(&h.q_free[at]), (tiles / kQ - 1) & 1, gave_up));
                     if (!ok) break;
-                    ++done[x];
-                    bw::bar_arrive_bytes(bar(&q_full[x]), kBytes);
+                    ++tiles;
+                    bw::bar_arrive_bytes(bar(&h.q_full[at]), kBytes);
                     for (int b = 0; b < kBoxes; ++b)
-                        bw::copy_3d1(base + x * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&q_full[x]));
+                        bw::copy_3d1(base + at * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&h.q_full[at]));
                     if (x == 0) block(map_k, q.kv, q.tile.first);
                 }
                 const int n = max(q.blocks[0], q.blocks[1]);
@@ -188,42 +201,48 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const uint32_t shape_s = bw::f16_shape(kBf, false, false, kTile, kTile);
             const uint32_t shape_y = bw::f16_shape(kBf, false, true, kTile, DP);
             uint32_t c = 0;  // blocks of the ring before this item
-            int done[2] = {0, 0};
-            uint32_t blocks[2] = {0, 0}, checks = 0;  // of either tile so far; of both
+            uint32_t tiles = 0, blocks[2] = {0, 0}, items_of[2] = {0, 0}, checks = 0;  // of either tile so far; of both
+            uint32_t at[2] = {0, 0};  // where the tiles' queries are
             bool ok = true;
             auto have = [&](uint32_t n) {
-                ok = ok && bw::bar_wait_inline(bar(&full[n % kStages]), (n / kStages) & 1, &gave_up);
+                ok = ok && bw::bar_wait_inline(bar(&h.full[n % kStages]), (n / kStages) & 1, gave_up);
                 return ok;
             };
             auto scores = [&](int x, uint32_t n) {
-                const uint64_t dq = bw::operand(base + x * kBytes, 16), dk = bw::operand(ring + n % kStages * kBytes, 16);
+                const uint64_t dq = bw::operand(base + at[x] * kBytes, 16), dk = bw::operand(ring + n % kStages * kBytes, 16);
                 bw::fence_after();
 #pragma unroll
                 for (int i = 0; i < DP / 16; ++i) {
-                    const uint64_t at = (i / 4) * (kBox >> 4) + (i % 4) * 2;
-                    bw::mma1(tmem + x * kTile, dq + at, dk + at, shape_s, i > 0);
+                    const uint64_t step = (i / 4) * (kBox >> 4) + (i % 4) * 2;
+                    bw::mma1(tmem + x * kTile, dq + step, dk + step, shape_s, i > 0);
                 }
             };
-            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-                const Item q = item_at<PAIR>(a, i);
+            // the next item is looked up while this one is at work
+            int64_t i = dealt(0, items);
+            Item next = {};
+            if (i >= 0) next = item_at<PAIR>(a, i);
+            for (int64_t round = 1; ok && i >= 0; ++round) {
+                const Item q = next;
                 const int n = max(q.blocks[0], q.blocks[1]);
-                if (n == 0) continue;
                 for (int x = 0; x < 2 && ok; ++x) {
                     if (q.blocks[x] == 0) continue;
-                    ok = bw::bar_wait_inline(bar(&q_full[x]), done[x] & 1, &gave_up);
-                    ++done[x];
+                    at[x] = tiles % kQ;
+                    ok = bw::bar_wait_inline(bar(&h.q_full[at[x]]), (tiles / kQ) & 1, gave_up);
+                    ++tiles;
                     if (!have(c)) break;
                     scores(x, c);
-                    bw::commit1(bar(&s_full[x]));
-                    if (q.blocks[x] == 1) bw::commit1(bar(&q_free[x]));
+                    bw::commit1(bar(&h.s_full[x]));
+                    if (q.blocks[x] == 1) bw::commit1(bar(&h.q_free[at[x]]));
                 }
-                bw::commit1(bar(&empty[c % kStages]));
+                if (n > 0) bw::commit1(bar(&h.empty[c % kStages]));
+                i = dealt(round, items);
+                if (i >= 0) next = item_at<PAIR>(a, i);
                 for (int j = 0; j < n && ok; ++j) {
                     const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
                     if (!have(v)) break;
                     // the diagonal's values are there: to be looked through
                     for (int x = 0; x < (PAIR ? 1 : 2); ++x)
-                        if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&look[(checks + x) % kChecks]));
+                        if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&h.look[(checks + x) % kChecks]));
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (j >= q.blocks[x]) continue;
                         const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
@@ -234,35 +253,35 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                                               j > 0 || i > 0);
                         };
                         // the rows before these have left
-                        ok = j > 0 || done[x] < 2 || bw::bar_wait_inline(bar(&y_free[x]), done[x] & 1, &gave_up);
-                        ok = ok && bw::bar_wait_inline(bar(&p_half[x]), blocks[x] & 1, &gave_up);
+                        ok = j > 0 || items_of[x]++ == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), items_of[x] & 1, gave_up);
+                        ok = ok && bw::bar_wait_inline(bar(&h.p_half[x]), blocks[x] & 1, gave_up);
                         if (!ok) break;
                         bw::fence_after();
                         // (known before the first half is handed over)
                         const bool own = j + 1 < q.blocks[x] || !is_by_hand(checks + (PAIR ? 0 : x));
                         if (own) half(0);
-                        ok = bw::bar_wait_inline(bar(&p_full[x]), blocks[x]++ & 1, &gave_up);
+                        ok = bw::bar_wait_inline(bar(&h.p_full[x]), blocks[x]++ & 1, gave_up);
                         if (!ok) break;
                         bw::fence_after();
                         if (own) half(kTile / 32);
                         if (j + 1 < q.blocks[x]) {
                             if (!have(k)) break;
                             scores(x, k);
-                            bw::commit1(bar(&s_full[x]));
-                            if (j + 2 == q.blocks[x]) bw::commit1(bar(&q_free[x]));
+                            bw::commit1(bar(&h.s_full[x]));
+                            if (j + 2 == q.blocks[x]) bw::commit1(bar(&h.q_free[at[x]]));
                         } else {
-                            bw::commit1(bar(&y_full[x]));
+                            bw::commit1(bar(&h.y_full[x]));
                         }
                     }
-                    bw::commit1(bar(&empty[v % kStages]));
-                    if (j + 1 < n) bw::commit1(bar(&empty[k % kStages]));
+                    bw::commit1(bar(&h.empty[v % kStages]));
+                    if (j + 1 < n) bw::commit1(bar(&h.empty[k % kStages]));
                 }
                 c += 2 * n;
                 checks += checks_of<PAIR>(q);
             }
             // arrivals land in this CTA's memory: it may not end before the last
-            bw::commit1(bar(&last));
-            bw::bar_wait_inline(bar(&last), 0, &gave_up);
+            bw::commit1(bar(&h.last));
+            bw::bar_wait_inline(bar(&h.last), 0, gave_up);
         }
         } else {  // values on the diagonal
         uint32_t c = 0, checks = 0;
@@ -273,16 +292,16 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             for (uint32_t x = 0; x < n; ++x, ++checks) {
                 const uint32_t v = c + 2 * q.blocks[x] - 1;
                 // (the ring's own barrier is waited for when it cannot be a round ahead or behind)
-                ok = bw::bar_wait_inline(bar(&look[checks % kChecks]), (checks / kChecks) & 1, &gave_up) &&
-                     bw::bar_wait_inline(bar(&full[v % kStages]), (v / kStages) & 1, &gave_up);
+                ok = bw::bar_wait_inline(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
+                     bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                unsigned char *tile = dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes;
+                unsigned char *tile = dyn + (kQ + v % kStages) * kBytes;
                 for (int r = (warp - 14) * 32 + lane; r < kTile; r += 64)
                     if (look_through<T, DP>(tile, r, q.rows[x]))
-                        *const_cast<volatile uint32_t *>(&by_hand[checks % kChecks]) = checks + 1;
+                        *const_cast<volatile uint32_t *>(&h.by_hand[checks % kChecks]) = checks + 1;
                 __syncwarp();
-                if (lane == 0) bw::bar_arrive(bar(&checked[checks % kChecks]));
+                if (lane == 0) bw::bar_arrive(bar(&h.checked[checks % kChecks]));
             }
             c += 2 * max(q.blocks[0], q.blocks[1]);
         }
@@ -292,7 +311,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int w = warp & 3, r = w * 32 + lane;
         const uint32_t at_y = tmem + (uint32_t(w * 32) << 16) + 2 * kTile;
         const bool wide = a.D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0;
-        const float scale = positive_scale(a);
+        const float scale = a.scale * kLog2e;
         uint32_t done[2] = {0, 0};
         bool ok = true;
         for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
@@ -309,12 +328,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     continue;
                 }
                 const uint32_t phase = done[x]++ & 1;
-                ok = ok && bw::bar_wait_inline(bar(&l_full[x]), phase, &gave_up) &&
-                     bw::bar_wait_inline(bar(&y_full[x]), phase, &gave_up);
+                ok = ok && bw::bar_wait_inline(bar(&h.l_full[x]), phase, gave_up) &&
+                     bw::bar_wait_inline(bar(&h.y_full[x]), phase, gave_up);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 bw::fence_after();
-                const float l = row_l[x][r], m = row_m[x][r], by = 1.0f / l;
+                const float l = h.row_l[x][r], m = h.row_m[x][r], by = 1.0f / l;
 #pragma unroll 1
                 for (int d = 0; d < DP; d += 32) {
                     float v[32];
@@ -323,7 +342,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (d + 32 == DP) {
                         bw::fence_before();
                         __syncwarp();
-                        if (lane == 0) bw::bar_arrive(bar(&y_free[x]));
+                        if (lane == 0) bw::bar_arrive(bar(&h.y_free[x]));
                     }
                     if (r < q.rows[x]) put_row(y + d, v, by, a.D - d, wide);
                 }
@@ -335,9 +354,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int x = warp >> 2, w = warp & 3, r = w * 32 + lane;
         const uint32_t lanes = tmem + (uint32_t(w * 32) << 16);
         const uint32_t at_s = lanes + x * kTile, at_y = lanes + 2 * kTile + x * DP;
-        // scores are compared before they are scaled: by a positive factor, after the sign (or zero)
-        const float sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
-        const float scale = positive_scale(a);
+        const float scale = a.scale * kLog2e;  // positive, so that unscaled scores can be compared
         uint32_t blocks = 0, done = 0, c = 0, checks = 0;  // blocks and rounds of this tile; blocks of the ring; checks
         bool ok = true;
         for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
@@ -351,7 +368,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (lane == 0) bw::bar_arrive(bar(&to[x]));
             };
             for (int j = 0; j < n; ++j) {
-                ok = __all_sync(0xffffffffu, bw::bar_wait_inline(bar(&s_full[x]), blocks++ & 1, &gave_up));
+                ok = __all_sync(0xffffffffu, bw::bar_wait_inline(bar(&h.s_full[x]), blocks++ & 1, gave_up));
                 if (!ok) break;
                 bw::fence_after();
                 float s[kTile];
@@ -359,10 +376,6 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     float(&lo)[64] = *reinterpret_cast<float(*)[64]>(s), (&hi)[64] = *reinterpret_cast<float(*)[64]>(s + 64);
                     bw::tmem_load(at_s, lo);
                     bw::tmem_load(at_s + 64, hi);
-                }
-                if (sign != 1.0f) {
-#pragma unroll
-                    for (int e = 0; e < kTile; ++e) s[e] *= sign;
                 }
                 const bool diagonal = j == n - 1;
                 if (diagonal) {  // a warp's rows see all of the 32 keys before theirs, and none of those after
@@ -418,27 +431,27 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     bw::tmem_store(at_s + e0 / 2, p);
                     // the first half's products may start
-                    if (e0 == 32 && !diagonal) hand_over(p_half);
+                    if (e0 == 32 && !diagonal) hand_over(h.p_half);
                 }
                 sum[0] = __fadd2_rn(sum[0], sum[1]);
                 l += sum[0].x + sum[0].y;
                 if (diagonal) {
                     bw::tmem_stored();
                     const uint32_t check = checks + (PAIR ? 0 : x), v = c + 2 * j + 1;
-                    ok = bw::bar_wait_inline(bar(&checked[check % kChecks]), (check / kChecks) & 1, &gave_up);
+                    ok = bw::bar_wait_inline(bar(&h.checked[check % kChecks]), (check / kChecks) & 1, gave_up);
                     // y, l and m of the rows before have been read
-                    ok = ok && (done == 0 || bw::bar_wait_inline(bar(&y_free[x]), (done - 1) & 1, &gave_up));
+                    ok = ok && (done == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), (done - 1) & 1, gave_up));
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    row_l[x][r] = l;
-                    row_m[x][r] = m;
+                    h.row_l[x][r] = l;
+                    h.row_m[x][r] = m;
                     if (is_by_hand(check))
                         masked_product<T, DP>(at_y, [&](int g) { return at_s + g * 16; }, 4,
-                                              dyn + (ring - bw::smem_addr(dyn)) + v % kStages * kBytes, 0, 0, r + 1, j > 0);
-                    hand_over(p_half);
-                    if (lane == 0) bw::bar_arrive(bar(&l_full[x]));
+                                              dyn + (kQ + v % kStages) * kBytes, 0, 0, r + 1, j > 0);
+                    hand_over(h.p_half);
+                    if (lane == 0) bw::bar_arrive(bar(&h.l_full[x]));
                 }
-                hand_over(p_full);
+                hand_over(h.p_full);
             }
             c += 2 * max(q.blocks[0], q.blocks[1]);
             checks += checks_of<PAIR>(q);
@@ -446,7 +459,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
     }
     __syncwarp();
-    if (*const_cast<volatile uint32_t *>(&gave_up)) {
+    if (*const_cast<volatile uint32_t *>(gave_up)) {
         // copies and products in flight still write this CTA's memory: let them end
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         if (threadIdx.x == 0 && a.status) *a.status = DC_ERR_INTERNAL;
@@ -484,7 +497,8 @@ cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t
         !am::heads_map(v, dtype, a.v, a.D, a.kv_heads, a.tokens, a.v_head, a.v_token))
         return cudaErrorInvalidValue;
     auto kernel = attention_mma_kernel<T, DP, PAIR>;
-    constexpr size_t smem = (2 + (DP == 64 ? 8 : 4)) * size_t(DP / 64) * kBox + 1024;
+    constexpr size_t smem = (kTilesOfQ<DP> + kRing<DP>) * size_t(DP / 64) * kBox + kSharedBytes;
+    static_assert(smem <= 232448, "shared memory of a CTA");
     static DeviceCache cache;
     int ready = 0, sms = 0;
     cudaError_t e = cache.get(ready, [&](int &n) {

@@ -181,7 +181,8 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArg
 }
 
 // The tensor cores' copies need heads that start on 16-byte boundaries: others are copied to rows of
-// whole 16 bytes first, eight elements a thread.
+// whole 16 bytes first, eight elements a thread. The forward kernel compares scores before it scales them, by a
+// positive factor: where the scale is negative (or zero), q is copied too, negated (or as zeros).
 struct Heads {
     const void *p;
     int64_t token, head;
@@ -192,19 +193,20 @@ bool aligned(const Heads &h, int64_t tokens)
 {
     return aligned16(h.p) && (tokens == 1 || h.token % 8 == 0) && (h.heads == 1 || h.head % 8 == 0);
 }
+template <typename T>
 __global__ void __launch_bounds__(256)
-align_heads_kernel(const uint16_t *x, uint16_t *to, int64_t units, int32_t heads, int32_t D, int32_t per, int64_t token,
-                   int64_t head)
+align_heads_kernel(const T *x, T *to, int64_t units, int32_t heads, int32_t D, int32_t per, int64_t token, int64_t head,
+                   float factor)
 {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (i >= units) return;
     const int64_t row = i / per, t = row / heads;
     const int d = int(i - row * per) * 8;
-    const uint16_t *p = x + t * token + (row - t * heads) * head + d;
-    Vec<uint16_t, 8> v;
+    const T *p = x + t * token + (row - t * heads) * head + d;
+    Vec<T, 8> v;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v.e[j] = d + j < D ? p[j] : uint16_t(0);
-    *reinterpret_cast<Vec<uint16_t, 8> *>(to + i * 8) = v;
+    for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(d + j < D ? to_float(p[j]) * factor : 0.0f);
+    *reinterpret_cast<Vec<T, 8> *>(to + i * 8) = v;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -239,7 +241,7 @@ Layout layout(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
     if (grad) at += round256(sizeof(float) * size_t(a.heads) * size_t(a.tokens));
     for (int i = 0; i < (grad ? 4 : 3) && dtype != DC_FP32; ++i) {
         const Heads h = operand(a, i);
-        l.copied[i] = !aligned(h, a.tokens);
+        l.copied[i] = !aligned(h, a.tokens) || (i == 0 && !grad && a.scale <= 0.0f);
         l.copy[i] = at;
         if (l.copied[i]) at += round256(size_t(a.tokens) * h.heads * padded(a.D) * 2);
     }
@@ -247,16 +249,22 @@ Layout layout(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
     return l;
 }
 
-cudaError_t align_operands(AttentionArgs &a, const Layout &l, unsigned char *ws, cudaStream_t stream)
+template <typename T>
+cudaError_t align_operands(AttentionArgs &a, const Layout &l, bool grad, unsigned char *ws, cudaStream_t stream)
 {
+    float factor = 1.0f;
+    if (!grad && a.scale <= 0.0f) {
+        factor = a.scale < 0.0f ? -1.0f : 0.0f;
+        a.scale = a.scale < 0.0f ? -a.scale : 1.0f;
+    }
     for (int i = 0; i < 4; ++i) {
         if (!l.copied[i]) continue;
         const Heads h = operand(a, i);
         const int64_t pad = padded(a.D), units = a.tokens * h.heads * (pad / 8), blocks = (units + 255) / 256;
         if (blocks > (int64_t(1) << 31) - 1) return cudaErrorInvalidValue;
-        uint16_t *to = reinterpret_cast<uint16_t *>(ws + l.copy[i]);
-        align_heads_kernel<<<unsigned(blocks), 256, 0, stream>>>(static_cast<const uint16_t *>(h.p), to, units, h.heads, a.D,
-                                                                 int(pad / 8), h.token, h.head);
+        T *to = reinterpret_cast<T *>(ws + l.copy[i]);
+        align_heads_kernel<T><<<unsigned(blocks), 256, 0, stream>>>(static_cast<const T *>(h.p), to, units, h.heads, a.D,
+                                                                    int(pad / 8), h.token, h.head, i == 0 ? factor : 1.0f);
         const void **p[4] = {&a.q, &a.k, &a.v, &a.dy};
         int64_t *token[4] = {&a.q_token, &a.k_token, &a.v_token, &a.dy_token};
         int64_t *head[4] = {&a.q_head, &a.k_head, &a.v_head, &a.dy_head};
@@ -268,15 +276,17 @@ cudaError_t align_operands(AttentionArgs &a, const Layout &l, unsigned char *ws,
 }
 
 template <typename T>
-cudaError_t gradient(int dtype, const AttentionArgs &a, int32_t sequences, AttentionPlan *plan, const Layout &l, int64_t most,
+cudaError_t gradient(int dtype, AttentionArgs a, int32_t sequences, unsigned char *ws, const Layout &l, int64_t most,
                      cudaStream_t stream)
 {
     int sms = 0;
-    const cudaError_t e = sm_count(sms);
+    cudaError_t e = sm_count(sms);
+    if (e == cudaSuccess) e = align_operands<T>(a, l, true, ws, stream);
     if (e != cudaSuccess) return e;
+    AttentionPlan *plan = reinterpret_cast<AttentionPlan *>(ws);
     const int64_t blocks = (a.tokens * a.heads + 15) / 16, limit = int64_t(sms) * 16;
     const unsigned grid = unsigned(blocks < limit ? blocks : limit);
-    const int32_t *start = reinterpret_cast<const int32_t *>(reinterpret_cast<unsigned char *>(plan) + l.start);
+    const int32_t *start = reinterpret_cast<const int32_t *>(ws + l.start);
     // operands of 16 bits are aligned by now; y is the caller's
     const int unit = 16 / int(sizeof(T));
     const bool wide = a.D % unit == 0 && aligned16(a.y) && aligned16(a.dy) && aligned16(a.v) && a.dy_token % unit == 0 &&
@@ -310,16 +320,15 @@ cudaError_t launch_attention(int dtype, AttentionArgs a, int32_t sequences, cons
     const int64_t most = attention_most_tiles(a.tokens, sequences, l.rows);
     if (!grad) {
         if (dtype == DC_FP32) return launch_attention_simt(a, most, stream);
-        const cudaError_t e = align_operands(a, l, ws, stream);
+        const cudaError_t e = dtype == DC_BF16 ? align_operands<__nv_bfloat16>(a, l, false, ws, stream)
+                                               : align_operands<__half>(a, l, false, ws, stream);
         return e == cudaSuccess ? launch_attention_mma(dtype, a, most, stream) : e;
     }
     a.delta = reinterpret_cast<float *>(ws + l.delta);
-    const cudaError_t e = align_operands(a, l, ws, stream);
-    if (e != cudaSuccess) return e;
     switch (dtype) {
-        case DC_BF16: return gradient<__nv_bfloat16>(dtype, a, sequences, plan, l, most, stream);
-        case DC_FP16: return gradient<__half>(dtype, a, sequences, plan, l, most, stream);
-        default: return gradient<float>(dtype, a, sequences, plan, l, most, stream);
+        case DC_BF16: return gradient<__nv_bfloat16>(dtype, a, sequences, ws, l, most, stream);
+        case DC_FP16: return gradient<__half>(dtype, a, sequences, ws, l, most, stream);
+        default: return gradient<float>(dtype, a, sequences, ws, l, most, stream);
     }
 }
 
