@@ -175,8 +175,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     phase ^= 1;
                 }
             };
-            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-                const Item q = item_at<PAIR>(a, i);
+            uint32_t checks = 0;
+            int64_t i = dealt(0, items);
+            Item next = {};
+            if (i >= 0) next = item_at<PAIR>(a, i);
+            for (int64_t round = 1; ok && i >= 0; ++round) {
+                const Item q = next;
                 for (int x = 0; x < 2; ++x) {
                     if (q.blocks[x] == 0) continue;
                     const uint32_t at = tiles % kQ;
@@ -188,11 +192,24 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         bw::copy_3d1(base + at * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&h.q_full[at]));
                     if (x == 0) block(map_k, q.kv, q.tile.first);
                 }
+                // the next item is looked up, and its queries come to the L2, while this one is at work
+                i = dealt(round, items);
+                if (i >= 0) {
+                    next = item_at<PAIR>(a, i);
+                    for (int x = 0; x < 2; ++x)
+                        for (int b = 0; b < kBoxes && next.blocks[x] > 0; ++b)
+                            bw::fetch_3d(&map_q, 64 * b, next.head[x], next.row0[x]);
+                }
                 const int n = max(q.blocks[0], q.blocks[1]);
                 for (int j = 0; j < n && ok; ++j) {
                     if (j > 0) block(map_k, q.kv, q.tile.first + j * kTile);
                     block(map_v, q.kv, q.tile.first + j * kTile);
+                    // values on the diagonal are to be looked through: their barrier's phase has begun, and does not
+                    // end twice before they are
+                    for (int x = 0; x < (PAIR ? 1 : 2) && ok; ++x)
+                        if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&h.look[(checks + x) % kChecks]));
                 }
+                checks += checks_of<PAIR>(q);
             }
         }
         } else if (warp == 13) {
@@ -240,9 +257,6 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 for (int j = 0; j < n && ok; ++j) {
                     const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
                     if (!have(v)) break;
-                    // the diagonal's values are there: to be looked through
-                    for (int x = 0; x < (PAIR ? 1 : 2); ++x)
-                        if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&h.look[(checks + x) % kChecks]));
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (j >= q.blocks[x]) continue;
                         const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
@@ -291,7 +305,6 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const uint32_t n = checks_of<PAIR>(q);
             for (uint32_t x = 0; x < n; ++x, ++checks) {
                 const uint32_t v = c + 2 * q.blocks[x] - 1;
-                // (the ring's own barrier is waited for when it cannot be a round ahead or behind)
                 ok = bw::bar_wait_inline(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
                      bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up);
                 ok = __all_sync(0xffffffffu, ok);

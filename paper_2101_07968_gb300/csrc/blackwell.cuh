@@ -176,6 +176,12 @@ __device__ __forceinline__ void copy_3d1(uint32_t dst, const void *map, int x, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+// A box brought to the L2 only.
+__device__ __forceinline__ void fetch_3d(const void *map, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
 // n bytes (a multiple of 16, both addresses on 16-byte boundaries)
 __device__ __forceinline__ void copy_bytes(uint32_t dst, const void *src, uint32_t n, uint32_t bar)
 {
