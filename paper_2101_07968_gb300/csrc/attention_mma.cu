@@ -12,7 +12,8 @@
 //   warps 8-11      the finished rows of both tiles, while the next tiles' scores are made
 //   warp 12         copies (TMA)
 //   warp 13         products, by one thread
-//   warps 14, 15    look through the values on the diagonal
+//   warp 14         looks through the values on the diagonal
+//   warp 15         looks up the items ahead of the others: the list is in memory, a thousand clocks away
 // A launch has 128 registers a thread; the softmax's warps take more of them from the others.
 //
 // Rounding: P is rounded to the operands' type for the tensor cores, at most half a step of each
@@ -39,40 +40,43 @@ static_assert(2 * kSoftmaxRegs + 2 * kOtherRegs <= 4 * 128, "registers of the la
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.0f;  // how far, in powers of two, the reference may be below the maximum
 
-struct Item {
-    AttentionTile tile;
-    int32_t head[2], row0[2], rows[2], blocks[2], kv;
+struct alignas(16) Item {
+    int32_t head[2], row0[2], rows[2], blocks[2];
+    int32_t kv, first;  // the key head; the sequence's first row
+    bool last;          // no item: the end
 };
+constexpr int kItems = 4, kItemUsers = 15;  // looked up ahead; warps that read each
 
 template <bool PAIR>
 __device__ __forceinline__ Item item_at(const AttentionArgs &a, int64_t i)
 {
     const int per = PAIR ? a.heads / 2 : a.heads;
     Item q;
-    const int64_t t = i < (int64_t(1) << 31) ? int64_t(uint32_t(i) / uint32_t(per)) : i / per;
-    q.tile = plan_tiles(a.plan)[t];
-    const int h = int(i - t * per);
-    const int before = (q.tile.row0 - max(q.tile.first, 0)) / kTile;
+    const int64_t at = i < (int64_t(1) << 31) ? int64_t(uint32_t(i) / uint32_t(per)) : i / per;
+    const AttentionTile t = plan_tiles(a.plan)[at];
+    const int h = int(i - at * per);
+    const int before = (t.row0 - max(t.first, 0)) / kTile;
     if (PAIR) {
         q.head[0] = 2 * h;
         q.head[1] = 2 * h + 1;
-        q.row0[0] = q.row0[1] = q.tile.row0;
-        q.rows[0] = q.rows[1] = q.tile.rows;
+        q.row0[0] = q.row0[1] = t.row0;
+        q.rows[0] = q.rows[1] = t.rows;
         q.blocks[0] = q.blocks[1] = before + 1;
     } else {
         q.head[0] = q.head[1] = h;
-        q.row0[0] = q.tile.row0;
-        q.row0[1] = q.tile.row0 + kTile;
-        q.rows[0] = min(kTile, q.tile.rows);
-        q.rows[1] = q.tile.rows - q.rows[0];
+        q.row0[0] = t.row0;
+        q.row0[1] = t.row0 + kTile;
+        q.rows[0] = min(kTile, t.rows);
+        q.rows[1] = t.rows - q.rows[0];
         q.blocks[0] = before + 1;
         q.blocks[1] = q.rows[1] > 0 ? before + 2 : 0;
     }
-    if (q.tile.first < 0) q.blocks[0] = q.blocks[1] = 0;
+    if (t.first < 0) q.blocks[0] = q.blocks[1] = 0;
     q.kv = q.head[0] / a.group;
+    q.first = t.first;
+    q.last = false;
     return q;
 }
-
 // Blocks of values on the diagonal, which are looked through: one for two heads, one for each of two tiles.
 template <bool PAIR>
 __device__ __forceinline__ uint32_t checks_of(const Item &q)
@@ -86,7 +90,7 @@ template <int DP>
 constexpr int kTilesOfQ = DP == 64 ? 4 : 3;
 template <int DP>
 constexpr int kRing = DP == 64 ? 8 : 4;  // blocks of keys or values
-constexpr uint32_t kSharedBytes = 2560;  // barriers and rows' sums
+constexpr uint32_t kSharedBytes = 2944;  // barriers and rows' sums
 
 template <typename T, int DP, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -101,10 +105,11 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     extern __shared__ __align__(1024) unsigned char dyn[];
     struct Shared {
         uint64_t q_full[kQ], q_free[kQ], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2],
-            y_free[2], l_full[2], look[kChecks], checked[kChecks], last;
+            y_free[2], l_full[2], look[kChecks], checked[kChecks], item_full[kItems], item_free[kItems], last;
         uint32_t tmem_at, gave_up;
         uint32_t by_hand[kChecks];  // the check, counted from one, if its block's sums are done by hand
         float row_l[2][kTile], row_m[2][kTile];  // of finished tiles
+        Item items[kItems];
     };
     static_assert(sizeof(Shared) <= kSharedBytes, "room behind the tiles");
     Shared &h = *reinterpret_cast<Shared *>(dyn + (kQ + kStages) * kBytes);
@@ -136,8 +141,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
         for (int i = 0; i < kChecks; ++i) {
             bw::bar_init(bar(&h.look[i]), 1);
-            bw::bar_init(bar(&h.checked[i]), 2);
+            bw::bar_init(bar(&h.checked[i]), 1);
             h.by_hand[i] = 0;
+        }
+        for (int i = 0; i < kItems; ++i) {
+            bw::bar_init(bar(&h.item_full[i]), 1);
+            bw::bar_init(bar(&h.item_free[i]), kItemUsers);
         }
         bw::bar_init(bar(&h.last), 1);
         h.gave_up = 0;
@@ -156,6 +165,21 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     // the swizzled copies need tiles on 1,024-byte boundaries
     const int64_t items = (base & 1023u) ? 0 : int64_t(a.plan->tiles) * (PAIR ? a.heads / 2 : a.heads);
     if ((base & 1023u) && threadIdx.x == 0) h.gave_up = 1;
+    // Item n of this CTA, by a thread or by a whole warp; false: there is none (or a wait was given up).
+    auto item_of_thread = [&](uint32_t n, Item &q) {
+        if (!bw::bar_wait_inline(bar(&h.item_full[n % kItems]), (n / kItems) & 1, gave_up)) return false;
+        q = h.items[n % kItems];
+        bw::bar_arrive(bar(&h.item_free[n % kItems]));
+        return !q.last;
+    };
+    auto item_of_warp = [&](uint32_t n, Item &q) {
+        const bool ok = bw::bar_wait_inline(bar(&h.item_full[n % kItems]), (n / kItems) & 1, gave_up);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        q = h.items[n % kItems];
+        __syncwarp();
+        if (lane == 0) bw::bar_arrive(bar(&h.item_free[n % kItems]));
+        return !q.last;
+    };
 
     if (warp >= 12) {
         bw::fewer_registers<kOtherRegs>();
@@ -176,11 +200,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
             };
             uint32_t checks = 0;
-            int64_t i = dealt(0, items);
-            Item next = {};
-            if (i >= 0) next = item_at<PAIR>(a, i);
-            for (int64_t round = 1; ok && i >= 0; ++round) {
-                const Item q = next;
+            Item q;
+            for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
                 for (int x = 0; x < 2; ++x) {
                     if (q.blocks[x] == 0) continue;
                     const uint32_t at = tiles % kQ;
@@ -190,20 +211,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     bw::bar_arrive_bytes(bar(&h.q_full[at]), kBytes);
                     for (int b = 0; b < kBoxes; ++b)
                         bw::copy_3d1(base + at * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&h.q_full[at]));
-                    if (x == 0) block(map_k, q.kv, q.tile.first);
-                }
-                // the next item is looked up, and its queries come to the L2, while this one is at work
-                i = dealt(round, items);
-                if (i >= 0) {
-                    next = item_at<PAIR>(a, i);
-                    for (int x = 0; x < 2; ++x)
-                        for (int b = 0; b < kBoxes && next.blocks[x] > 0; ++b)
-                            bw::fetch_3d(&map_q, 64 * b, next.head[x], next.row0[x]);
+                    if (x == 0) block(map_k, q.kv, q.first);
                 }
                 const int n = max(q.blocks[0], q.blocks[1]);
                 for (int j = 0; j < n && ok; ++j) {
-                    if (j > 0) block(map_k, q.kv, q.tile.first + j * kTile);
-                    block(map_v, q.kv, q.tile.first + j * kTile);
+                    if (j > 0) block(map_k, q.kv, q.first + j * kTile);
+                    block(map_v, q.kv, q.first + j * kTile);
                     // values on the diagonal are to be looked through: their barrier's phase has begun, and does not
                     // end twice before they are
                     for (int x = 0; x < (PAIR ? 1 : 2) && ok; ++x)
@@ -234,12 +247,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     bw::mma1(tmem + x * kTile, dq + step, dk + step, shape_s, i > 0);
                 }
             };
-            // the next item is looked up while this one is at work
-            int64_t i = dealt(0, items);
-            Item next = {};
-            if (i >= 0) next = item_at<PAIR>(a, i);
-            for (int64_t round = 1; ok && i >= 0; ++round) {
-                const Item q = next;
+            Item q;
+            for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
                 const int n = max(q.blocks[0], q.blocks[1]);
                 for (int x = 0; x < 2 && ok; ++x) {
                     if (q.blocks[x] == 0) continue;
@@ -252,8 +261,6 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (q.blocks[x] == 1) bw::commit1(bar(&h.q_free[at[x]]));
                 }
                 if (n > 0) bw::commit1(bar(&h.empty[c % kStages]));
-                i = dealt(round, items);
-                if (i >= 0) next = item_at<PAIR>(a, i);
                 for (int j = 0; j < n && ok; ++j) {
                     const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
                     if (!have(v)) break;
@@ -297,11 +304,11 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             bw::commit1(bar(&h.last));
             bw::bar_wait_inline(bar(&h.last), 0, gave_up);
         }
-        } else {  // values on the diagonal
+        } else if (warp == 14) {  // values on the diagonal
         uint32_t c = 0, checks = 0;
         bool ok = true;
-        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-            const Item q = item_at<PAIR>(a, i);
+        Item q;
+        for (uint32_t item = 0; ok && item_of_warp(item, q); ++item) {
             const uint32_t n = checks_of<PAIR>(q);
             for (uint32_t x = 0; x < n; ++x, ++checks) {
                 const uint32_t v = c + 2 * q.blocks[x] - 1;
@@ -310,13 +317,33 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 unsigned char *tile = dyn + (kQ + v % kStages) * kBytes;
-                for (int r = (warp - 14) * 32 + lane; r < kTile; r += 64)
+                for (int r = lane; r < kTile; r += 32)
                     if (look_through<T, DP>(tile, r, q.rows[x]))
                         *const_cast<volatile uint32_t *>(&h.by_hand[checks % kChecks]) = checks + 1;
                 __syncwarp();
                 if (lane == 0) bw::bar_arrive(bar(&h.checked[checks % kChecks]));
             }
             c += 2 * max(q.blocks[0], q.blocks[1]);
+        }
+        } else {
+        if (bw::elect_one()) {  // items
+            bool ok = true;
+            bool more = true;
+            for (int64_t round = 0; ok && more; ++round) {
+                const int64_t i = dealt(round, items);
+                const uint32_t at = uint32_t(round % kItems);
+                Item q = {};
+                q.last = true;
+                if (i >= 0) q = item_at<PAIR>(a, i);
+                more = !q.last;
+                ok = round < kItems || bw::bar_wait_inline(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up);
+                if (!ok) break;
+                h.items[at] = q;
+                bw::bar_arrive(bar(&h.item_full[at]));
+                // the queries come to the L2
+                for (int x = 0; x < 2; ++x)
+                    for (int b = 0; b < kBoxes && q.blocks[x] > 0; ++b) bw::fetch_3d(&map_q, 64 * b, q.head[x], q.row0[x]);
+            }
         }
         }
     } else if (warp >= 8) {  // finished rows
@@ -327,8 +354,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const float scale = a.scale * kLog2e;
         uint32_t done[2] = {0, 0};
         bool ok = true;
-        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-            const Item q = item_at<PAIR>(a, i);
+        Item q;
+        for (uint32_t item = 0; ok && item_of_warp(item, q); ++item) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 T *y = static_cast<T *>(a.y) + (int64_t(q.row0[x]) + r) * a.heads * a.D + int64_t(q.head[x]) * a.D;
@@ -370,8 +397,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const float scale = a.scale * kLog2e;  // positive, so that unscaled scores can be compared
         uint32_t blocks = 0, done = 0, c = 0, checks = 0;  // blocks and rounds of this tile; blocks of the ring; checks
         bool ok = true;
-        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-            const Item q = item_at<PAIR>(a, i);
+        Item q;
+        for (uint32_t item = 0; ok && item_of_warp(item, q); ++item) {
             const int n = q.blocks[x];
             float m = -INFINITY, l = 0.0f;
             auto hand_over = [&](uint64_t(&to)[2]) {  // P so far, to the products
