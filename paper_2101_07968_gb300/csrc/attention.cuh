@@ -35,6 +35,10 @@ struct AttentionArgs {
     int32_t heads, kv_heads, group, D;
     float scale;
     int32_t *status;
+    // gradient: a group's heads may be dealt to `split` blocks, whose sums of dk and dv, floats [2][split][tokens]
+    // [kv_heads][D], are then added up in order (1: none)
+    int32_t split;
+    float *partial;
 };
 
 // The most tiles of `rows` rows that a plan can have: a short one for each sequence, and the rows

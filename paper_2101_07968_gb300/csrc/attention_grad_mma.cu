@@ -5,7 +5,8 @@
 //            S^T = k q^T, dP^T = v dy^T, dv += P^T dy, dk += dS^T q
 //   rows:    a tile of 128 rows and a head, over the keys up to it: S = q k^T, dP = dy v^T, dq += dS k
 // Seven products a block instead of the five that one pass would need: dq of one pass would be summed
-// by many CTAs, in memory and in an order that depends on timing; so each sum has one owner.
+// by many CTAs, in memory and in an order that depends on timing; so each sum has one owner. Where tiles and
+// key heads are few, a group's heads are dealt to several CTAs, whose sums are joined afterwards.
 //
 // Both are one kernel: two stationary tiles, two rings of moving ones (X: q or k, Y: dy or v), scores
 // and dP in tensor memory [128][128], the sums [128][D] beside them, 512 columns in all.
@@ -51,13 +52,13 @@ struct Step {
 template <bool COLUMNS>
 struct Item {
     AttentionTile t;
-    int32_t outer, kv, per_head, steps;
+    int32_t outer, kv, part, head0, per_head, steps;
     __device__ __forceinline__ Step step(const AttentionArgs &a, int i) const
     {
         Step s;
         if (COLUMNS) {
             const int k = i / per_head, j = i - k * per_head;
-            s.head = outer * a.group + k;
+            s.head = head0 + k;
             s.c0 = t.row0 + j * kTile;
             s.count = min(kTile, t.end - s.c0);
             s.diagonal = j == 0;
@@ -73,12 +74,15 @@ struct Item {
 template <bool COLUMNS>
 __device__ __forceinline__ Item<COLUMNS> item_at(const AttentionArgs &a, int64_t i)
 {
-    const int outer = COLUMNS ? a.kv_heads : a.heads;
+    const int outer = COLUMNS ? a.kv_heads * a.split : a.heads;
     Item<COLUMNS> q;
-    const int64_t at = i / outer;
+    const int64_t at = i < (int64_t(1) << 31) ? int64_t(uint32_t(i) / uint32_t(outer)) : i / outer;
     q.t = plan_tiles(a.plan)[at];
-    q.outer = int(i - at * outer);
+    const int j = int(i - at * outer);
+    q.part = COLUMNS ? j / a.kv_heads : 0;
+    q.outer = j - q.part * a.kv_heads;
     q.kv = COLUMNS ? q.outer : q.outer / a.group;
+    q.head0 = COLUMNS ? q.kv * a.group + q.part * a.group / a.split : q.outer;
     if (q.t.first < 0) {
         q.per_head = q.steps = 0;
         return q;
@@ -88,7 +92,7 @@ __device__ __forceinline__ Item<COLUMNS> item_at(const AttentionArgs &a, int64_t
         q.t.row0 = q.t.first + (n - 1 - before) * kTile;
         q.t.rows = min(kTile, q.t.end - q.t.row0);
         q.per_head = before + 1;
-        q.steps = q.per_head * a.group;
+        q.steps = q.per_head * ((q.part + 1) * a.group / a.split - q.part * a.group / a.split);
     } else {
         q.per_head = q.steps = before + 1;
     }
@@ -172,7 +176,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     auto packed_at = [](int i) { return uint32_t(i / 4 * 64 + i % 4 * 8); };
     auto by_hand = [&](uint32_t n) { return *const_cast<volatile uint32_t *>(&b.by_hand[n & 1]) == n + 1; };
     // the swizzled copies need tiles on 1,024-byte boundaries
-    const int64_t items = (base & 1023u) ? 0 : int64_t(a.plan->tiles) * (COLUMNS ? a.kv_heads : a.heads);
+    const int64_t items = (base & 1023u) ? 0 : int64_t(a.plan->tiles) * (COLUMNS ? a.kv_heads * a.split : a.heads);
     if ((base & 1023u) && threadIdx.x == 0) b.gave_up = 1;
 
     if (warp == 8) {
@@ -330,8 +334,15 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
             const int64_t row = (int64_t(q.t.row0) + r) * (COLUMNS ? a.kv_heads : a.heads) * a.D + int64_t(q.outer) * a.D;
             T *const out = static_cast<T *>(!COLUMNS ? a.dq : side ? a.dk : a.dv) + row;
+            float *const part = !COLUMNS || a.split == 1 ? nullptr
+                                : a.partial + ((side ? 0 : a.split) + q.part) * a.tokens * a.kv_heads * a.D + row;
             if (q.steps == 0) {  // rows of no sequence
-                if (r < q.t.rows && (COLUMNS || side == 0)) put_zeros(out, a.D, wide);
+                if (r < q.t.rows && (COLUMNS || side == 0)) {
+                    if (part)
+                        for (int d = 0; d < a.D; ++d) part[d] = 0.0f;
+                    else
+                        put_zeros(out, a.D, wide);
+                }
                 continue;
             }
             float2 lse = {}, delta = {};
@@ -463,7 +474,12 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 float v[32];
                 __syncwarp();
                 bw::tmem_load(from + d, v);
-                if (r < q.t.rows) put_row(out + d0 + d, v, COLUMNS && side == 0 ? by1 : by0, a.D - d0 - d, wide);
+                const float by_sum = COLUMNS && side == 0 ? by1 : by0;
+                if (r >= q.t.rows) continue;
+                if (part)
+                    put_floats(part + d, v, by_sum, a.D - d);
+                else
+                    put_row(out + d0 + d, v, by_sum, a.D - d0 - d, wide);
             }
         }
     }
@@ -499,7 +515,7 @@ cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t
     });
     if (e == cudaSuccess) e = sm_count(sms);
     if (e != cudaSuccess) return e;
-    const int64_t items = most * (COLUMNS ? a.kv_heads : a.heads);
+    const int64_t items = most * (COLUMNS ? a.kv_heads * a.split : a.heads);
     kernel<<<unsigned(items < sms ? items : sms), kThreads, smem, stream>>>(q, k, v, dy, a);
     return cudaGetLastError();
 }

@@ -149,6 +149,19 @@ __device__ __forceinline__ void put_row(T *y, const float (&v)[32], float by, in
     }
 }
 
+__device__ __forceinline__ void put_floats(float *y, const float (&v)[32], float by, int D)
+{
+    if (D >= 32 && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4)
+            *reinterpret_cast<float4 *>(y + j) = make_float4(v[j] * by, v[j + 1] * by, v[j + 2] * by, v[j + 3] * by);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < D) y[j] = v[j] * by;
+    }
+}
+
 // Zeros in the lane's row.
 template <typename T>
 __device__ __forceinline__ void put_zeros(T *y, int D, bool wide)

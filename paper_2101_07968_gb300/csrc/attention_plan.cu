@@ -221,12 +221,37 @@ Heads operand(const AttentionArgs &a, int i)
     }
 }
 
+// dk and dv of a group's heads from `split` parts, in order.
+template <typename T>
+__global__ void __launch_bounds__(256) join_parts_kernel(const AttentionArgs a)
+{
+    const int64_t n = a.tokens * a.kv_heads * a.D, step = int64_t(gridDim.x) * 256;
+    T *const out = static_cast<T *>(blockIdx.y ? a.dv : a.dk);
+    const float *const parts = a.partial + blockIdx.y * a.split * n;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += step) {
+        float t = 0.0f;
+        for (int p = 0; p < a.split; ++p) t += parts[p * n + i];
+        out[i] = from_float<T>(t);
+    }
+}
+
+// How many parts a group's heads are dealt to: enough for two items an SM, if there are as many heads. One item
+// an SM or less is as long as its tile's: 2,000 floats in 3 sequences x 8 heads on 2 x 64, 799 us in one part.
+int32_t parts_of(const AttentionArgs &a, int32_t sequences, int rows, int sms)
+{
+    const int64_t items = (a.tokens / rows + (sequences < a.tokens ? sequences : a.tokens) + 1) * a.kv_heads;
+    const int64_t wanted = (2 * int64_t(sms) + items - 1) / items;
+    return int32_t(wanted < a.group ? wanted : a.group);
+}
+
 // Parts of the workspace; copy[i]: of operand i, where it needs one.
 struct Layout {
     int rows;  // of a tile
-    size_t first, start, delta, copy[4], total;
+    int32_t split;
+    size_t first, start, delta, partial, copy[4], total;
     bool copied[4];
 };
+constexpr int kMostSms = 160;  // (a workspace is asked for before the device is)
 Layout layout(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
 {
     Layout l = {};
@@ -239,6 +264,9 @@ Layout layout(int dtype, const AttentionArgs &a, int32_t sequences, bool grad)
     at += round256(sizeof(int32_t) * (size_t(sequences) + 3));
     l.delta = at;
     if (grad) at += round256(sizeof(float) * size_t(a.heads) * size_t(a.tokens));
+    l.split = grad ? parts_of(a, sequences, l.rows, kMostSms) : 1;
+    l.partial = at;
+    if (l.split > 1) at += round256(sizeof(float) * 2 * l.split * size_t(a.tokens) * a.kv_heads * a.D);
     for (int i = 0; i < (grad ? 4 : 3) && dtype != DC_FP32; ++i) {
         const Heads h = operand(a, i);
         l.copied[i] = !aligned(h, a.tokens) || (i == 0 && !grad && a.scale <= 0.0f);
@@ -296,8 +324,13 @@ cudaError_t gradient(int dtype, AttentionArgs a, int32_t sequences, unsigned cha
         attention_delta_kernel<T, true><<<grid, 256, 0, stream>>>(a, plan, start, sequences);
     else
         attention_delta_kernel<T, false><<<grid, 256, 0, stream>>>(a, plan, start, sequences);
-    if (sizeof(T) == 2) return launch_attention_grad_mma(dtype, a, most, stream);
-    return launch_attention_grad_simt(a, most, stream);
+    a.split = l.split;
+    a.partial = reinterpret_cast<float *>(ws + l.partial);
+    e = sizeof(T) == 2 ? launch_attention_grad_mma(dtype, a, most, stream) : launch_attention_grad_simt(a, most, stream);
+    if (e != cudaSuccess || a.split == 1) return e;
+    const int64_t join = (a.tokens * a.kv_heads * a.D + 255) / 256;
+    join_parts_kernel<T><<<dim3(unsigned(join < limit ? join : limit), 2), 256, 0, stream>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace

@@ -6,7 +6,8 @@
 //   rows     a tile of 64 rows and a head, over the keys up to it: dq = scale dS k
 //   columns  a tile of 64 keys and a key head, over its group's heads and the rows from it on:
 //            dv = P^T dy, dk = scale dS^T q
-// Each sum has one owner and one order: no atomics. What a mask leaves out is skipped, not
+// Each sum has one owner and one order: no atomics. Where tiles and key heads are few, a group's heads are
+// dealt to several blocks, whose sums are joined afterwards (attention_plan.cu). What a mask leaves out is skipped, not
 // multiplied by zero, so that whatever stands there is without effect.
 //
 // 256 threads, 4 x 4 scores a thread. Rows of operands lie in shared memory four floats apart from
@@ -191,14 +192,15 @@ __global__ void __launch_bounds__(kThreads) attention_grad_simt_kernel(const Att
     constexpr int kSize = kTile * kPitch<DP>;
     float *x0 = dyn, *x1 = x0 + kSize, *z0 = x1 + kSize, *z1 = z0 + kSize, *p = z1 + kSize;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const int outer = COLUMNS ? a.kv_heads : a.heads;
+    const int outer = COLUMNS ? a.kv_heads * a.split : a.heads;
     const int64_t items = int64_t(a.plan->tiles) * outer;
     const T *q = static_cast<const T *>(a.q), *k = static_cast<const T *>(a.k), *v = static_cast<const T *>(a.v);
     const T *dy = static_cast<const T *>(a.dy);
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         AttentionTile t = plan_tiles(a.plan)[item / outer];
-        const int o = int(item % outer), g = COLUMNS ? o : o / a.group;
-        const int64_t out = int64_t(outer) * a.D;
+        const int part = COLUMNS ? int(item % outer) / a.kv_heads : 0;
+        const int o = COLUMNS ? int(item % outer) % a.kv_heads : int(item % outer), g = COLUMNS ? o : o / a.group;
+        const int64_t out = int64_t(COLUMNS ? a.kv_heads : a.heads) * a.D;
         if (COLUMNS && t.first >= 0) {  // tile i from the end has the work of tile i from the start
             const int n = (t.end - t.first + kTile - 1) / kTile, i = n - 1 - (t.row0 - t.first) / kTile;
             t.row0 = t.first + i * kTile;
@@ -206,7 +208,15 @@ __global__ void __launch_bounds__(kThreads) attention_grad_simt_kernel(const Att
         }
         const int64_t at = t.row0 * out + int64_t(o) * a.D;
         T *const d0 = static_cast<T *>(COLUMNS ? a.dk : a.dq) + at, *const d1 = COLUMNS ? static_cast<T *>(a.dv) + at : nullptr;
+        const int64_t all = a.tokens * out;  // of a part
+        float *const p0 = COLUMNS && a.split > 1 ? a.partial + part * all + at : nullptr;
+        float *const p1 = p0 ? p0 + a.split * all : nullptr;
         if (t.first < 0) {
+            if (p0) {
+                put_zeros(p0, out, t.rows, a.D);
+                put_zeros(p1, out, t.rows, a.D);
+                continue;
+            }
             put_zeros(d0, out, t.rows, a.D);
             if (COLUMNS) put_zeros(d1, out, t.rows, a.D);
             continue;
@@ -220,7 +230,9 @@ __global__ void __launch_bounds__(kThreads) attention_grad_simt_kernel(const Att
             bring<T, DP>(x0, q + t.row0 * a.q_token + o * a.q_head, a.q_token, t.rows, a.D);
             bring<T, DP>(x1, dy + t.row0 * a.dy_token + o * a.dy_head, a.dy_token, t.rows, a.D);
         }
-        for (int h = COLUMNS ? g * a.group : o; h < (COLUMNS ? (g + 1) * a.group : o + 1); ++h) {
+        const int h0 = COLUMNS ? g * a.group + part * a.group / a.split : o;
+        const int h1 = COLUMNS ? g * a.group + (part + 1) * a.group / a.split : o + 1;
+        for (int h = h0; h < h1; ++h) {
             const int lo = COLUMNS ? t.row0 : t.first, hi = COLUMNS ? t.end : t.row0 + t.rows;
             for (int c0 = lo; c0 < hi; c0 += kTile) {
                 const int n = min(kTile, hi - c0);
@@ -267,6 +279,13 @@ __global__ void __launch_bounds__(kThreads) attention_grad_simt_kernel(const Att
             }
         }
         const float by0[4] = {a.scale, a.scale, a.scale, a.scale}, by1[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+        if constexpr (COLUMNS) {
+            if (p0) {
+                put<float, DP>(p0, out, t.rows, a.D, acc0, by0);
+                put<float, DP>(p1, out, t.rows, a.D, acc1, by1);
+                continue;
+            }
+        }
         put<T, DP>(d0, out, t.rows, a.D, acc0, by0);
         if constexpr (COLUMNS) put<T, DP>(d1, out, t.rows, a.D, acc1, by1);
     }
@@ -301,7 +320,7 @@ cudaError_t backward(const AttentionArgs &a, int64_t most, cudaStream_t stream)
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
     });
     if (e != cudaSuccess) return e;
-    const int64_t items = most * (COLUMNS ? a.kv_heads : a.heads), limit = int64_t(1) << 20;
+    const int64_t items = most * (COLUMNS ? a.kv_heads * a.split : a.heads), limit = int64_t(1) << 20;
     kernel<<<unsigned(items < limit ? items : limit), kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
