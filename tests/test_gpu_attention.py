@@ -92,6 +92,25 @@ def test_long(ly, dtype, H, G, D):
     check(both(ly, q, k, v, dy, offs(*o)), q, k, v, dy, o)
 
 
+@pytest.mark.parametrize("dtype,H,G,D", [(BF, 12, 4, 128), (HF, 9, 3, 64), (HF, 16, 8, 128), (BF, 8, 2, 64), (FL, 8, 2, 48),
+                                          (HF, 10, 2, 72)])
+def test_many_items(ly, dtype, H, G, D):
+    """Several times as many tiles as SMs: each block takes one after another, of long and short sequences."""
+    g = torch.Generator().manual_seed(8)
+    o = packed(*torch.randint(1, 600, (50,), generator=g).tolist(), 1300)
+    q, k, v, dy = operands(9, o[-1], H, G, D, dtype)
+    check(both(ly, q, k, v, dy, offs(*o)), q, k, v, dy, o)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H,G", [(7, 1), (16, 1), (5, 5), (64, 2)])
+def test_few_key_heads(ly, dtype, H, G):
+    """A group's heads dealt to several blocks, evenly and unevenly."""
+    o = packed(140, 300, 3)
+    q, k, v, dy = operands(H, o[-1] + 9, H, G, 64, dtype)
+    check(both(ly, q, k, v, dy, offs(*o)), q, k, v, dy, o)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_many_sequences(ly, dtype):
     """More sequences than a block of the plan takes at a time, empty ones among them."""
