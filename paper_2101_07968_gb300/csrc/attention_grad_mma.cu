@@ -167,6 +167,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         bw::prefetch_map(&map_v);
         bw::prefetch_map(&map_dy);
     }
+    pdl_wait();  // the list, the copies, delta (and for rows, the columns' pass) are there
     bw::fence_before();
     __syncthreads();
     bw::fence_after();
@@ -516,8 +517,7 @@ cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t
     if (e == cudaSuccess) e = sm_count(sms);
     if (e != cudaSuccess) return e;
     const int64_t items = most * (COLUMNS ? a.kv_heads * a.split : a.heads);
-    kernel<<<unsigned(items < sms ? items : sms), kThreads, smem, stream>>>(q, k, v, dy, a);
-    return cudaGetLastError();
+    return launch_early(kernel, items < sms ? items : sms, kThreads, smem, stream, q, k, v, dy, a);
 }
 
 }  // namespace

@@ -158,6 +158,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         bw::prefetch_map(&map_k);
         bw::prefetch_map(&map_v);
     }
+    pdl_wait();  // the list and the copies are there
     bw::fence_before();
     __syncthreads();
     bw::fence_after();
@@ -548,8 +549,7 @@ cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t
     if (e == cudaSuccess) e = sm_count(sms);
     if (e != cudaSuccess) return e;
     const int64_t items = most * (PAIR ? a.heads / 2 : a.heads);
-    kernel<<<unsigned(items < sms ? items : sms), kThreads, smem, stream>>>(q, k, v, a);
-    return cudaGetLastError();
+    return launch_early(kernel, items < sms ? items : sms, kThreads, smem, stream, q, k, v, a);
 }
 
 }  // namespace

@@ -131,33 +131,34 @@ __device__ __forceinline__ void masked_product(uint32_t acc, At at, int groups, 
     bw::tmem_stored();
 }
 
-// Thirty-two neighbours of a lane's row, times `by`, to memory; D: what is left of the row from here.
-template <typename T>
-__device__ __forceinline__ void put_row(T *y, const float (&v)[32], float by, int D, bool wide)
+// N neighbours of a lane's row, times `by`, to memory; D: what is left of the row from here.
+template <typename T, int N>
+__device__ __forceinline__ void put_row(T *y, const float (&v)[N], float by, int D, bool wide)
 {
     if (wide) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 8)
+        for (int j = 0; j < N; j += 8)
             if (j < D)
                 *reinterpret_cast<uint4 *>(y + j) =
                     make_uint4(pack2(v[j] * by, v[j + 1] * by, T()), pack2(v[j + 2] * by, v[j + 3] * by, T()),
                                pack2(v[j + 4] * by, v[j + 5] * by, T()), pack2(v[j + 6] * by, v[j + 7] * by, T()));
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < N; ++j)
             if (j < D) y[j] = from_float<T>(v[j] * by);
     }
 }
 
-__device__ __forceinline__ void put_floats(float *y, const float (&v)[32], float by, int D)
+template <int N>
+__device__ __forceinline__ void put_floats(float *y, const float (&v)[N], float by, int D)
 {
-    if (D >= 32 && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
+    if (D >= N && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 4)
+        for (int j = 0; j < N; j += 4)
             *reinterpret_cast<float4 *>(y + j) = make_float4(v[j] * by, v[j + 1] * by, v[j + 2] * by, v[j + 3] * by);
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < N; ++j)
             if (j < D) y[j] = v[j] * by;
     }
 }

@@ -45,6 +45,7 @@ attention_plan_kernel(const int64_t *offsets, int32_t sequences, int64_t tokens,
                       int32_t *first, int32_t *start)
 {
     __shared__ int warps[32], count[kBuckets], carry[2];
+    pdl_trigger();  // a kernel after this one gets ready while the list is made
     const int segments = sequences + 2;
     if (threadIdx.x < 2) carry[threadIdx.x] = 0;
     if (threadIdx.x < kBuckets) count[threadIdx.x] = 0;
@@ -139,29 +140,40 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArg
     };
     const int64_t rows = a.tokens * a.heads, step = int64_t(gridDim.x) * 16;
     const int l = threadIdx.x % 16;
+    auto row_token = [&](int64_t i) {
+        return rows < (int64_t(1) << 31) ? int64_t(uint32_t(i) / uint32_t(a.heads)) : i / a.heads;
+    };
     const int lo = start[1], hi = start[sequences + 1];  // the sequences' rows
     float top_dy = 0.0f, top_v = 0.0f;
-    for (int64_t i0 = int64_t(blockIdx.x) * 16; i0 < rows; i0 += step) {
-        const int64_t i = i0 + threadIdx.x / 16;
-        float s = 0.0f;
-        if (i < rows) {
-            const int64_t t = i / a.heads;
-            const T *y = static_cast<const T *>(a.y) + i * a.D;
-            const T *dy = static_cast<const T *>(a.dy) + t * a.dy_token + (i - t * a.heads) * a.dy_head;
-            const bool counts = t >= lo && t < hi;
-            for (int d = l * V; d < a.D; d += 16 * V) {
-                const Vec<T, V> p = bring(y + d, a.D - d), q = bring(dy + d, a.D - d);
+    constexpr int kAhead = 4;  // rows of a lane group on their way at once
+    for (int64_t i0 = int64_t(blockIdx.x) * 16 + threadIdx.x / 16; i0 < rows; i0 += kAhead * step) {
+        float s[kAhead] = {};
+        for (int d = l * V; d < a.D; d += 16 * V) {
+            Vec<T, V> p[kAhead], q[kAhead];
+            bool counts[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t i = min(i0 + k * step, rows - 1), t = row_token(i);
+                counts[k] = t >= lo && t < hi;
+                p[k] = bring(static_cast<const T *>(a.y) + i * a.D + d, a.D - d);
+                q[k] = bring(static_cast<const T *>(a.dy) + t * a.dy_token + (i - t * a.heads) * a.dy_head + d, a.D - d);
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float g = to_float(q.e[j]);
-                    s += to_float(p.e[j]) * g;
-                    if (kHalf && counts) top_dy = largest(top_dy, g);
+                    const float g = to_float(q[k].e[j]);
+                    s[k] += to_float(p[k].e[j]) * g;
+                    if (kHalf && counts[k]) top_dy = largest(top_dy, g);
                 }
-            }
         }
 #pragma unroll
-        for (int o = 8; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (l == 0 && i < rows) a.delta[i % a.heads * a.tokens + i / a.heads] = s;
+        for (int k = 0; k < kAhead; ++k) {
+#pragma unroll
+            for (int o = 8; o > 0; o /= 2) s[k] += __shfl_xor_sync(0xffffu << (threadIdx.x & 16), s[k], o);
+            const int64_t i = i0 + k * step, t = row_token(i);
+            if (l == 0 && i < rows) a.delta[(i - t * a.heads) * a.tokens + t] = s[k];
+        }
     }
     if constexpr (kHalf) {
         const int64_t first = int64_t(lo) * a.kv_heads, end = int64_t(hi) * a.kv_heads;
@@ -193,20 +205,31 @@ bool aligned(const Heads &h, int64_t tokens)
 {
     return aligned16(h.p) && (tokens == 1 || h.token % 8 == 0) && (h.heads == 1 || h.head % 8 == 0);
 }
+struct HeadsCopy {
+    const void *x;
+    void *to;
+    int64_t units, token, head;
+    int32_t heads, per;
+    float factor;
+};
+struct HeadsCopies {
+    HeadsCopy of[4];
+    int32_t D;
+};
 template <typename T>
-__global__ void __launch_bounds__(256)
-align_heads_kernel(const T *x, T *to, int64_t units, int32_t heads, int32_t D, int32_t per, int64_t token, int64_t head,
-                   float factor)
+__global__ void __launch_bounds__(256) align_heads_kernel(const HeadsCopies c)
 {
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= units) return;
-    const int64_t row = i / per, t = row / heads;
-    const int d = int(i - row * per) * 8;
-    const T *p = x + t * token + (row - t * heads) * head + d;
-    Vec<T, 8> v;
+    const HeadsCopy &m = c.of[blockIdx.y];
+    const int64_t step = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < m.units; i += step) {
+        const int64_t row = i / m.per, t = row / m.heads;
+        const int d = int(i - row * m.per) * 8;
+        const T *p = static_cast<const T *>(m.x) + t * m.token + (row - t * m.heads) * m.head + d;
+        Vec<T, 8> v;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(d + j < D ? to_float(p[j]) * factor : 0.0f);
-    *reinterpret_cast<Vec<T, 8> *>(to + i * 8) = v;
+        for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(d + j < c.D ? to_float(p[j]) * m.factor : 0.0f);
+        *reinterpret_cast<Vec<T, 8> *>(static_cast<T *>(m.to) + i * 8) = v;
+    }
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -285,14 +308,18 @@ cudaError_t align_operands(AttentionArgs &a, const Layout &l, bool grad, unsigne
         factor = a.scale < 0.0f ? -1.0f : 0.0f;
         a.scale = a.scale < 0.0f ? -a.scale : 1.0f;
     }
+    HeadsCopies c = {};
+    c.D = a.D;
+    int n = 0;
+    int64_t most = 0;
+    const int64_t pad = padded(a.D);
     for (int i = 0; i < 4; ++i) {
         if (!l.copied[i]) continue;
         const Heads h = operand(a, i);
-        const int64_t pad = padded(a.D), units = a.tokens * h.heads * (pad / 8), blocks = (units + 255) / 256;
-        if (blocks > (int64_t(1) << 31) - 1) return cudaErrorInvalidValue;
-        T *to = reinterpret_cast<T *>(ws + l.copy[i]);
-        align_heads_kernel<T><<<unsigned(blocks), 256, 0, stream>>>(static_cast<const T *>(h.p), to, units, h.heads, a.D,
-                                                                    int(pad / 8), h.token, h.head, i == 0 ? factor : 1.0f);
+        void *const to = ws + l.copy[i];
+        c.of[n] = {h.p, to, a.tokens * h.heads * (pad / 8), h.token, h.head, h.heads, int32_t(pad / 8), i == 0 ? factor : 1.0f};
+        if (c.of[n].units > most) most = c.of[n].units;
+        ++n;
         const void **p[4] = {&a.q, &a.k, &a.v, &a.dy};
         int64_t *token[4] = {&a.q_token, &a.k_token, &a.v_token, &a.dy_token};
         int64_t *head[4] = {&a.q_head, &a.k_head, &a.v_head, &a.dy_head};
@@ -300,7 +327,10 @@ cudaError_t align_operands(AttentionArgs &a, const Layout &l, bool grad, unsigne
         *token[i] = h.heads * pad;
         *head[i] = pad;
     }
-    return cudaSuccess;
+    if (n == 0) return cudaSuccess;
+    const int64_t blocks = (most + 255) / 256, limit = 8192;
+    align_heads_kernel<T><<<dim3(unsigned(blocks < limit ? blocks : limit), n), 256, 0, stream>>>(c);
+    return cudaGetLastError();
 }
 
 template <typename T>
