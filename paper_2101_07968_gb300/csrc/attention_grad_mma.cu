@@ -14,6 +14,7 @@
 //              they were made of (A operands may lie in tensor memory)
 //   warp 8     copies (TMA)       warp 9  products, by one thread
 //   warp 10    columns: lse and delta of each block's rows
+//   warp 11    looks through the blocks that a mask cuts
 // The products of one kind run while the warps make the other: S of the next block and dv beside dS,
 // dP of the next block and dk beside P.
 //
@@ -31,7 +32,8 @@ namespace {
 
 using namespace am;
 
-constexpr int kThreads = 11 * 32;
+constexpr int kThreads = 12 * 32;
+constexpr int kChecks = 4;  // no more blocks that a mask cuts are in a ring
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int DP, bool COLUMNS>
@@ -47,7 +49,7 @@ struct Shape {
 // A block of columns: its first row (key), how many there are of it, the head, and whether the mask cuts it.
 struct Step {
     int32_t head, c0, count;
-    bool diagonal;
+    bool diagonal, cut;
 };
 template <bool COLUMNS>
 struct Item {
@@ -62,11 +64,12 @@ struct Item {
             s.c0 = t.row0 + j * kTile;
             s.count = min(kTile, t.end - s.c0);
             s.diagonal = j == 0;
+            s.cut = s.diagonal || s.count < kTile;
         } else {
             s.head = outer;
             s.c0 = t.first + i * kTile;
             s.count = min(kTile, t.row0 + t.rows - s.c0);
-            s.diagonal = i == steps - 1;
+            s.diagonal = s.cut = i == steps - 1;
         }
         return s;
     }
@@ -122,9 +125,11 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     extern __shared__ __align__(1024) unsigned char dyn[];
     struct Bars {
         uint64_t still_full, still_free, x_full[G::kX], x_free[G::kX], y_full[G::kY], y_free[G::kY], l_full[G::kL],
-            l_free[G::kL], s_full, p_full, dp_full, ds_full, sums_full, met, last;
+            l_free[G::kL], s_full, p_full, dp_full, ds_full, sums_full, met, last,
+            look[kChecks], x_checked[kChecks], y_checked[kChecks];
         uint32_t tmem_at, gave_up;
-        uint32_t by_hand[2];  // block n, counted from one, if its sums are done by hand: in turn
+        // the check, counted from one, if the sums with its block of X (Y) are done by hand
+        uint32_t x_by_hand[kChecks], y_by_hand[kChecks];
     };
     static_assert(sizeof(Bars) <= G::kBars, "barriers' room");
     Bars &b = *reinterpret_cast<Bars *>(dyn + G::kTiles + G::kStats);
@@ -157,7 +162,13 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         bw::bar_init(bar(&b.sums_full), 1);
         bw::bar_init(bar(&b.met), 8);
         bw::bar_init(bar(&b.last), 1);
-        b.gave_up = b.by_hand[0] = b.by_hand[1] = 0;
+        for (int i = 0; i < kChecks; ++i) {
+            bw::bar_init(bar(&b.look[i]), 1);
+            bw::bar_init(bar(&b.x_checked[i]), 1);
+            bw::bar_init(bar(&b.y_checked[i]), 1);
+            b.x_by_hand[i] = b.y_by_hand[i] = 0;
+        }
+        b.gave_up = 0;
         bw::bar_init_fence();
     }
     if (warp == 9) bw::tmem_alloc1(bw::smem_addr(&b.tmem_at), 512);
@@ -175,7 +186,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     constexpr uint32_t kDp = kTile, kSum1 = 2 * kTile, kSum0 = kSum1 + (COLUMNS ? DP : 0);  // columns
     // A operand of step i of eight: pairs of 16 columns; the halves are 64 columns apart
     auto packed_at = [](int i) { return uint32_t(i / 4 * 64 + i % 4 * 8); };
-    auto by_hand = [&](uint32_t n) { return *const_cast<volatile uint32_t *>(&b.by_hand[n & 1]) == n + 1; };
+    auto by_hand = [&](const uint32_t(&of)[kChecks], uint32_t check) {
+        return *const_cast<const volatile uint32_t *>(&of[check % kChecks]) == check + 1;
+    };
     // the swizzled copies need tiles on 1,024-byte boundaries
     const int64_t items = (base & 1023u) ? 0 : int64_t(a.plan->tiles) * (COLUMNS ? a.kv_heads * a.split : a.heads);
     if ((base & 1023u) && threadIdx.x == 0) b.gave_up = 1;
@@ -188,8 +201,22 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             auto tile = [&](uint32_t to, const CUtensorMap &map, int head, int row, uint32_t full) {
                 for (int i = 0; i < kBoxes; ++i) bw::copy_3d1(to + i * kBox, &map, 64 * i, head, row, full);
             };
-            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-                const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
+            uint32_t checks = 0;
+            int64_t i = dealt(0, items);
+            Item<COLUMNS> next = {};
+            if (i >= 0) next = item_at<COLUMNS>(a, i);
+            for (int64_t round = 1; ok && i >= 0; ++round) {
+                const Item<COLUMNS> q = next;
+                // the next item is looked up, and its stationary tiles come to the L2, while this one is at work
+                i = dealt(round, items);
+                if (i >= 0) {
+                    next = item_at<COLUMNS>(a, i);
+                    const int head = COLUMNS ? next.kv : next.outer;
+                    for (int d = 0; d < kBoxes && next.steps > 0; ++d) {
+                        bw::fetch_3d(COLUMNS ? &map_k : &map_q, 64 * d, head, next.t.row0);
+                        bw::fetch_3d(COLUMNS ? &map_v : &map_dy, 64 * d, head, next.t.row0);
+                    }
+                }
                 if (q.steps == 0) continue;
                 ok = done == 0 || bw::bar_wait(bar(&b.still_free), (done - 1) & 1, gave_up);
                 if (!ok) break;
@@ -211,6 +238,8 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     bw::bar_arrive_bytes(bar(&b.y_full[y]), kBytes);
                     tile(ring_y + y * kBytes, COLUMNS ? map_dy : map_v, head, s.c0, bar(&b.y_full[y]));
                     ++ny;
+                    // to be looked through: the barriers' phases have begun, and do not end twice before that
+                    if (s.cut) bw::bar_arrive(bar(&b.look[checks++ % kChecks]));
                 }
             }
         }
@@ -239,9 +268,17 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 for (int i = 0; i < kTile / 16; ++i)
                     bw::mma1_tmem(tmem + d, tmem + packed + packed_at(i), db + i * 128, shape_d, add || i > 0);
             };
-            for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
-                const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
-                if (q.steps == 0) continue;
+            uint32_t checks = 0;
+            int64_t i = dealt(0, items);
+            Item<COLUMNS> next = {};
+            if (i >= 0) next = item_at<COLUMNS>(a, i);
+            for (int64_t round = 1; ok && i >= 0; ++round) {
+                const Item<COLUMNS> q = next;
+                i = dealt(round, items);
+                if (q.steps == 0) {
+                    if (i >= 0) next = item_at<COLUMNS>(a, i);
+                    continue;
+                }
                 ok = bw::bar_wait(bar(&b.still_full), done & 1, gave_up);
                 ++done;
                 auto first = [&](uint32_t m) {  // S of block m
@@ -258,19 +295,22 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 };
                 first(n);
                 second(n, q.steps == 1);
+                if (i >= 0) next = item_at<COLUMNS>(a, i);  // looked up while this one is at work
                 for (int j = 0; j < q.steps && ok; ++j, ++n) {
+                    const Step s = q.step(a, j);
                     ok = bw::bar_wait(bar(&b.p_full), n & 1, gave_up);
                     if (!ok) break;
                     bw::fence_after();
                     if (COLUMNS) {
-                        if (!by_hand(n)) sums(kSum1, 0, ring_y + n % G::kY * kBytes, j > 0);
+                        if (!s.diagonal || !by_hand(b.y_by_hand, checks)) sums(kSum1, 0, ring_y + n % G::kY * kBytes, j > 0);
                         bw::commit1(bar(&b.y_free[n % G::kY]));
                     }
                     if (j + 1 < q.steps) first(n + 1);
                     ok = ok && bw::bar_wait(bar(&b.ds_full), n & 1, gave_up);
                     if (!ok) break;
                     bw::fence_after();
-                    if (!by_hand(n)) sums(kSum0, kDp, ring_x + n % G::kX * kBytes, j > 0);
+                    if (!s.diagonal || !by_hand(b.x_by_hand, checks)) sums(kSum0, kDp, ring_x + n % G::kX * kBytes, j > 0);
+                    checks += s.cut;
                     bw::commit1(bar(&b.x_free[n % G::kX]));
                     if (j + 1 < q.steps) second(n + 1, j + 2 == q.steps);
                 }
@@ -311,6 +351,34 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 }
             }
         }
+    } else if (warp == 11) {  // blocks that a mask cuts
+        uint32_t n = 0, checks = 0;
+        bool ok = true;
+        for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
+            const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
+            for (int j = 0; j < q.steps; ++j, ++n) {
+                const Step s = q.step(a, j);
+                if (!s.cut) continue;
+                const uint32_t at = checks % kChecks;
+                ok = bw::bar_wait(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
+                // rows behind the mask: of Y where it is summed too, and of X
+                for (int of_x = COLUMNS ? 0 : 1; of_x < 2; ++of_x) {
+                    const uint32_t stage = of_x ? n % G::kX : n % G::kY, phase = of_x ? n / G::kX : n / G::kY;
+                    ok = __all_sync(0xffffffffu, ok && bw::bar_wait(bar(of_x ? &b.x_full[stage] : &b.y_full[stage]), phase & 1,
+                                                                     gave_up));
+                    if (!ok) break;
+                    unsigned char *const tile = dyn + (2 + (of_x ? 0 : G::kX) + stage) * kBytes;
+                    bool bad = false;
+                    for (int r = lane; r < kTile; r += 32) bad |= look_through<T, DP>(tile, r, s.count);
+                    if (bad && s.diagonal)
+                        *const_cast<volatile uint32_t *>(of_x ? &b.x_by_hand[at] : &b.y_by_hand[at]) = checks + 1;
+                    __syncwarp();
+                    if (lane == 0) bw::bar_arrive(bar(of_x ? &b.x_checked[at] : &b.y_checked[at]));
+                }
+                if (!ok) break;
+                ++checks;
+            }
+        }
     } else {  // P, dS and the finished sums
         const int side = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
@@ -321,7 +389,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         const bool wide = a.D % 8 == 0 && ((reinterpret_cast<uintptr_t>(COLUMNS ? a.dk : a.dq) |
                                             reinterpret_cast<uintptr_t>(COLUMNS ? a.dv : a.dq)) & 15) == 0;
         const float2 by = twice(scale), fs = twice(f);
-        uint32_t n = 0, finished = 0;
+        uint32_t n = 0, finished = 0, checks = 0;
         bool ok = true;
         uint32_t meetings = 0;
         auto meet = [&] {  // all eight warps
@@ -362,7 +430,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (!ok) break;
                 bw::fence_after();
                 // columns of this side that count: rows from the key on, or keys up to the row
-                const bool cut = s.diagonal || (COLUMNS && s.count < kTile);
+                const bool cut = s.cut;
                 const int from = (COLUMNS && s.diagonal ? r : 0) - side * 64;
                 const int end = (!COLUMNS && s.diagonal ? r + 1 : s.count) - side * 64;
                 float p[64];
@@ -396,23 +464,18 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (cut) make_p(std::true_type());
                 else make_p(std::false_type());
                 if (COLUMNS) bw::tmem_stored();
-                bool some = false;
-                unsigned char *const tile_x = dyn + (2 + n % G::kX) * kBytes, *const tile_y = dyn + (2 + G::kX + n % G::kY) * kBytes;
-                if (cut) {
-                    // rows behind the mask: of X, and of Y where it is summed too
-                    const bool x = COLUMNS ? side == 1 : side == 0, y = COLUMNS && side == 0;
-                    if (x) ok = bw::bar_wait(bar(&b.x_full[n % G::kX]), (n / G::kX) & 1, gave_up);
-                    if (y) ok = bw::bar_wait(bar(&b.y_full[n % G::kY]), (n / G::kY) & 1, gave_up);
-                    const bool bad = ok && (x || y) && look_through<T, DP>(x ? tile_x : tile_y, r, s.count);
-                    if (s.diagonal) {
-                        if (bad) *const_cast<volatile uint32_t *>(&b.by_hand[n & 1]) = n + 1;
+                const uint32_t at = checks % kChecks, check_phase = (checks / kChecks) & 1;
+                if (COLUMNS && cut) {  // Y has been looked through
+                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.y_checked[at]), check_phase, gave_up));
+                    if (!ok) break;
+                    if (s.diagonal && by_hand(b.y_by_hand, checks)) {
                         meet();
-                        some = by_hand(n);
+                        if (!ok) break;
+                        if (side == 0)
+                            masked_product<T, DP>(lanes + kSum1, [&](int g) { return lanes + packed_at(2 * g); }, 4,
+                                                  dyn + (2 + G::kX + n % G::kY) * kBytes, 0, r, s.count, j > 0);
                     }
                 }
-                if (COLUMNS && some && side == 0)
-                    masked_product<T, DP>(lanes + kSum1, [&](int g) { return lanes + packed_at(2 * g); }, 4, tile_y, 0,
-                                          r, s.count, j > 0);
                 bw::fence_before();
                 __syncwarp();
                 if (lane == 0) bw::bar_arrive(bar(&b.p_full));
@@ -449,11 +512,18 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (cut) make_ds(std::true_type());
                 else make_ds(std::false_type());
                 bw::tmem_stored();
-                if (some) {
-                    meet();
-                    if (side == (COLUMNS ? 1 : 0))
-                        masked_product<T, DP>(lanes + kSum0, [&](int g) { return lanes + kDp + packed_at(2 * g); }, 4, tile_x,
-                                              0, COLUMNS ? r : 0, COLUMNS ? s.count : r + 1, j > 0);
+                if (cut) {  // X too
+                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.x_checked[at]), check_phase, gave_up));
+                    if (!ok) break;
+                    if (s.diagonal && by_hand(b.x_by_hand, checks)) {
+                        meet();
+                        if (!ok) break;
+                        if (side == (COLUMNS ? 1 : 0))
+                            masked_product<T, DP>(lanes + kSum0, [&](int g) { return lanes + kDp + packed_at(2 * g); }, 4,
+                                                  dyn + (2 + n % G::kX) * kBytes, 0, COLUMNS ? r : 0, COLUMNS ? s.count : r + 1,
+                                                  j > 0);
+                    }
+                    ++checks;
                 }
                 bw::fence_before();
                 __syncwarp();

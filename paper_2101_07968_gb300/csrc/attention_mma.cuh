@@ -42,18 +42,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
 __device__ __forceinline__ float2 unpack2(uint32_t v, __nv_bfloat16) { return pair_of(reinterpret_cast<const __nv_bfloat16 *>(&v)); }
 __device__ __forceinline__ float2 unpack2(uint32_t v, __half) { return pair_of(reinterpret_cast<const __half *>(&v)); }
 
-// Whether any of eight elements is an infinity or NaN: an exponent of all ones.
+// Bits 15 and 31 say whether any of eight elements is an infinity or NaN: an exponent of all ones carries over.
 template <typename T>
-__device__ __forceinline__ bool any_not_finite(uint4 v)
+__device__ __forceinline__ uint32_t not_finite(uint4 v)
 {
     constexpr uint32_t e = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-        bad |= __vcmpeq2(w & e, e) != 0;
-    }
-    return bad;
+    constexpr uint32_t one = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+    return ((v.x & e) + one) | ((v.y & e) + one) | ((v.z & e) + one) | ((v.w & e) + one);
 }
 
 // Sixteen bytes of a tile's row as the copies lay them: boxes of 64 elements, 128 bytes a row, the
@@ -68,17 +63,17 @@ __device__ __forceinline__ uint4 tile_unit(const unsigned char *tile, int row, i
 template <typename T, int DP>
 __device__ __forceinline__ bool look_through(unsigned char *tile, int r, int rows)
 {
-    bool bad = false;
+    uint32_t bad = 0;
     if (r < rows) {
 #pragma unroll
-        for (int u = 0; u < DP / 8; ++u) bad |= any_not_finite<T>(tile_unit(tile, r, u));
+        for (int u = 0; u < DP / 8; ++u) bad |= not_finite<T>(tile_unit(tile, r, u));
     } else {
 #pragma unroll
         for (int u = 0; u < DP / 8; ++u)
             *reinterpret_cast<uint4 *>(tile + (u >> 3) * kBox + r * 128 + ((u & 7) << 4)) = make_uint4(0, 0, 0, 0);
         bw::fence_async();
     }
-    return bad;
+    return (bad & 0x80008000u) != 0;
 }
 
 // acc[lane][..] (+)= the sum of w[lane][c] B[c][..] over columns c of the lane's own range [from, end), on the

@@ -258,11 +258,14 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttentionArgs a)
     }
 }
 
-// How many parts a group's heads are dealt to: enough for two items an SM, if there are as many heads. One item
-// an SM or less is as long as its tile's: 2,000 floats in 3 sequences x 8 heads on 2 x 64, 799 us in one part.
+// How many parts a group's heads are dealt to. With an item an SM or more, one: the parts' sums cost a pass over
+// memory (8,192 tokens x 8 heads on 4 x 128, 256 items: 335 us in one part, 373 in two). With fewer, enough for two
+// items an SM, if there are as many heads: a pass lasts as long as its longest item (2,000 floats in 3 sequences x 8
+// heads on 2 x 64, 70 items: 1,123 us in one part, 592 in four).
 int32_t parts_of(const AttentionArgs &a, int32_t sequences, int rows, int sms)
 {
     const int64_t items = (a.tokens / rows + (sequences < a.tokens ? sequences : a.tokens) + 1) * a.kv_heads;
+    if (items >= sms) return 1;
     const int64_t wanted = (2 * int64_t(sms) + items - 1) / items;
     return int32_t(wanted < a.group ? wanted : a.group);
 }
