@@ -3,9 +3,13 @@
 //   P = 2^(scale' S - lse'), dS = P (dy v^T - delta), delta = dy . y
 //   columns: a tile of 128 keys and a key head, over its group's heads and the rows from it on:
 //            S^T = k q^T, dP^T = v dy^T, dv += P^T dy, dk += dS^T q
-//   rows:    a tile of 128 rows and a head, over the keys up to it: S = q k^T, dP = dy v^T, dq += dS k
+//   rows:    a tile of 128 rows and a head, over the keys up to it: S = q k^T, dP = dy v^T, dq += dS k,
+//            b += P k
 // Seven products a block instead of the five that one pass would need: dq of one pass would be summed
-// by many CTAs, in memory and in an order that depends on timing; so each sum has one owner. Where tiles and
+// by many CTAs, in memory and in an order that depends on timing; so each sum has one owner.
+// The eighth, b, takes back what y's rounding does to delta: as a row of P sums to one, a row of dS sums to zero, and
+// what it sums to instead, E, is what delta lacks. So the rows' pass comes first, gives dq - E b, and leaves
+// delta + E for the columns' (in rows of 16 keys bfloat16's dq is 4.0e-3 off without, 2.3 with; 1.6 is its own rounding). Where tiles and
 // key heads are few, a group's heads are dealt to several CTAs, whose sums are joined afterwards.
 //
 // Both are one kernel: two stationary tiles, two rings of moving ones (X: q or k, Y: dy or v), scores
@@ -41,7 +45,7 @@ struct Shape {
     static constexpr uint32_t kBytes = DP / 64 * kBox;
     static constexpr int kX = DP == 64 ? 4 : 3, kY = DP == 64 ? 4 : 2, kL = 2;
     static constexpr uint32_t kTiles = (2 + kX + kY) * kBytes;
-    static constexpr uint32_t kStats = COLUMNS ? kL * 2 * kTile * sizeof(float) : 0;
+    static constexpr uint32_t kStats = (COLUMNS ? kL * 2 : 2) * kTile * sizeof(float);
     static constexpr uint32_t kBars = 512;
     static constexpr uint32_t kSmem = kTiles + kStats + kBars;
 };
@@ -133,7 +137,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     };
     static_assert(sizeof(Bars) <= G::kBars, "barriers' room");
     Bars &b = *reinterpret_cast<Bars *>(dyn + G::kTiles + G::kStats);
-    float *const stats = reinterpret_cast<float *>(dyn + G::kTiles);  // [kL][lse, delta][128]
+    float *const stats = reinterpret_cast<float *>(dyn + G::kTiles);  // columns: [kL][lse, delta][128]; rows: [2][128], E
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto bar = [](uint64_t *p) { return bw::smem_addr(p); };
@@ -178,12 +182,12 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         bw::prefetch_map(&map_v);
         bw::prefetch_map(&map_dy);
     }
-    pdl_wait();  // the list, the copies, delta (and for rows, the columns' pass) are there
+    pdl_wait();  // the list, the copies and delta are there (for columns, from the rows' pass)
     bw::fence_before();
     __syncthreads();
     bw::fence_after();
     const uint32_t tmem = b.tmem_at;
-    constexpr uint32_t kDp = kTile, kSum1 = 2 * kTile, kSum0 = kSum1 + (COLUMNS ? DP : 0);  // columns
+    constexpr uint32_t kDp = kTile, kSum1 = 2 * kTile, kSum0 = kSum1 + DP;  // columns: dv or b, and dk or dq
     // A operand of step i of eight: pairs of 16 columns; the halves are 64 columns apart
     auto packed_at = [](int i) { return uint32_t(i / 4 * 64 + i % 4 * 8); };
     auto by_hand = [&](const uint32_t(&of)[kChecks], uint32_t check) {
@@ -301,10 +305,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     ok = bw::bar_wait(bar(&b.p_full), n & 1, gave_up);
                     if (!ok) break;
                     bw::fence_after();
-                    if (COLUMNS) {
-                        if (!s.diagonal || !by_hand(b.y_by_hand, checks)) sums(kSum1, 0, ring_y + n % G::kY * kBytes, j > 0);
-                        bw::commit1(bar(&b.y_free[n % G::kY]));
-                    }
+                    if (!s.diagonal || !by_hand(COLUMNS ? b.y_by_hand : b.x_by_hand, checks))
+                        sums(kSum1, 0, COLUMNS ? ring_y + n % G::kY * kBytes : ring_x + n % G::kX * kBytes, j > 0);
+                    if (COLUMNS) bw::commit1(bar(&b.y_free[n % G::kY]));
                     if (j + 1 < q.steps) first(n + 1);
                     ok = ok && bw::bar_wait(bar(&b.ds_full), n & 1, gave_up);
                     if (!ok) break;
@@ -414,7 +417,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 }
                 continue;
             }
-            float2 lse = {}, delta = {};
+            float2 lse = {}, delta = {}, excess = {};  // excess: rows, what dS sums to
             if (!COLUMNS) {
                 const int64_t at = q.outer * a.tokens + q.t.row0 + r;
                 const bool there = r < q.t.rows;
@@ -452,28 +455,31 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                             if constexpr (decltype(masked)::value)
 #pragma unroll
                                 for (int k = e; k < e + 4; ++k) p[k] = k >= from && k < end ? p[k] : 0.0f;
-                            if (COLUMNS) {
-                                out16[(e - e0) / 2] = pack2(p[e], p[e + 1], T());
-                                out16[(e - e0) / 2 + 1] = pack2(p[e + 2], p[e + 3], T());
-                            }
+                            out16[(e - e0) / 2] = pack2(p[e], p[e + 1], T());
+                            out16[(e - e0) / 2 + 1] = pack2(p[e + 2], p[e + 3], T());
                         }
-                        if (COLUMNS) bw::tmem_store(at_s + e0 / 2, out16);
+                        bw::tmem_store(at_s + e0 / 2, out16);
                     }
                 };
                 // most blocks are whole: the mask's selections would double the work of a block
                 if (cut) make_p(std::true_type());
                 else make_p(std::false_type());
-                if (COLUMNS) bw::tmem_stored();
+                bw::tmem_stored();
                 const uint32_t at = checks % kChecks, check_phase = (checks / kChecks) & 1;
-                if (COLUMNS && cut) {  // Y has been looked through
-                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.y_checked[at]), check_phase, gave_up));
+                // what P is multiplied with (Y, or X) has been looked through
+                bool hand = false;
+                if (cut) {
+                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(COLUMNS ? &b.y_checked[at] : &b.x_checked[at]), check_phase,
+                                                              gave_up));
                     if (!ok) break;
-                    if (s.diagonal && by_hand(b.y_by_hand, checks)) {
+                    hand = s.diagonal && by_hand(COLUMNS ? b.y_by_hand : b.x_by_hand, checks);
+                    if (hand) {
                         meet();
                         if (!ok) break;
                         if (side == 0)
                             masked_product<T, DP>(lanes + kSum1, [&](int g) { return lanes + packed_at(2 * g); }, 4,
-                                                  dyn + (2 + G::kX + n % G::kY) * kBytes, 0, r, s.count, j > 0);
+                                                  dyn + (COLUMNS ? 2 + G::kX + n % G::kY : 2 + n % G::kX) * kBytes, 0,
+                                                  COLUMNS ? r : 0, COLUMNS ? s.count : r + 1, j > 0);
                     }
                 }
                 bw::fence_before();
@@ -503,6 +509,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                                 u.x = k + 2 >= from && k + 2 < end ? u.x : 0.0f;
                                 u.y = k + 3 >= from && k + 3 < end ? u.y : 0.0f;
                             }
+                            if (!COLUMNS) excess = __fadd2_rn(excess, __fadd2_rn(t, u));
                             out16[e / 2] = pack2(t.x, t.y, T());
                             out16[e / 2 + 1] = pack2(u.x, u.y, T());
                         }
@@ -512,10 +519,13 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 if (cut) make_ds(std::true_type());
                 else make_ds(std::false_type());
                 bw::tmem_stored();
-                if (cut) {  // X too
-                    ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.x_checked[at]), check_phase, gave_up));
-                    if (!ok) break;
-                    if (s.diagonal && by_hand(b.x_by_hand, checks)) {
+                if (cut) {
+                    if (COLUMNS) {  // X too
+                        ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.x_checked[at]), check_phase, gave_up));
+                        if (!ok) break;
+                        hand = s.diagonal && by_hand(b.x_by_hand, checks);
+                    }
+                    if (hand) {
                         meet();
                         if (!ok) break;
                         if (side == (COLUMNS ? 1 : 0))
@@ -537,15 +547,30 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             if (!ok) break;
             ++finished;
             bw::fence_after();
+            float lacks = 0.0f;
+            if (!COLUMNS) {
+                stats[side * kTile + r] = excess.x + excess.y;
+                meet();
+                if (!ok) break;
+                lacks = stats[r] + stats[kTile + r];
+                if (side == 0 && r < q.t.rows) a.delta[q.outer * a.tokens + q.t.row0 + r] += lacks / f;
+                meet();  // both have read them
+                if (!ok) break;
+            }
             constexpr int kCols = COLUMNS ? DP : DP / 2;  // of a thread
             const int d0 = COLUMNS ? 0 : side * kCols;
             const uint32_t from = lanes + (COLUMNS && side == 0 ? kSum1 : kSum0) + d0;
+            const float by_sum = COLUMNS && side == 0 ? by1 : by0;
 #pragma unroll 1
-            for (int d = 0; d < kCols; d += 32) {
-                float v[32];
+            for (int d = 0; d < kCols; d += 16) {
+                float v[16], b_row[16];
                 __syncwarp();
                 bw::tmem_load(from + d, v);
-                const float by_sum = COLUMNS && side == 0 ? by1 : by0;
+                if (!COLUMNS) {
+                    bw::tmem_load(lanes + kSum1 + d0 + d, b_row);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] -= lacks * b_row[e];
+                }
                 if (r >= q.t.rows) continue;
                 if (part)
                     put_floats(part + d, v, by_sum, a.D - d);
@@ -596,9 +621,9 @@ cudaError_t launch_attention_grad_mma(int dtype, const AttentionArgs &a, int64_t
 {
     auto go = [&](auto t) {
         using T = decltype(t);
-        cudaError_t e = a.D <= 64 ? launch<T, 64, true>(dtype, a, most, stream) : launch<T, 128, true>(dtype, a, most, stream);
+        cudaError_t e = a.D <= 64 ? launch<T, 64, false>(dtype, a, most, stream) : launch<T, 128, false>(dtype, a, most, stream);
         if (e == cudaSuccess)
-            e = a.D <= 64 ? launch<T, 64, false>(dtype, a, most, stream) : launch<T, 128, false>(dtype, a, most, stream);
+            e = a.D <= 64 ? launch<T, 64, true>(dtype, a, most, stream) : launch<T, 128, true>(dtype, a, most, stream);
         return e;
     };
     return dtype == DC_BF16 ? go(__nv_bfloat16()) : go(__half());

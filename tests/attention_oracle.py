@@ -6,7 +6,9 @@ Attention, 16-bit types: scores are sums of D products in 32 bits, off by dS = (
 |q| . |k|, and so is their exponential, relatively, with 8 EPS for the exponential itself. P = e^(S -
 lse) and dS are rounded to T before the products with v, dy, k and q (u each; half as low as 2^-25
 in its own scale), and those sums of n terms lose at most (n + 16) EPS of their terms' magnitudes.
-Floats round neither (u = 2^-24). The gradient takes y as rounded to T: dy . y is off by u |dy| . |y|.
+Floats round neither (u = 2^-24). The gradient takes y as rounded to T, so that dy . y is off by w = |dy| . |y's
+error|. Floats feel that as it is; for 16-bit types it is taken back by what a row of dS sums to, so that w is felt
+through the rounding of P alone (3 u w), and the row's own errors once more.
 """
 import math
 
@@ -124,8 +126,14 @@ def attention(q, k, v, offsets, scale, dy=None, y_used=None, dtype=torch.float32
             dp = d @ V.t()
             delta = (d * Y).sum(-1, keepdim=True)
             ds = p * (dp - delta)
-            wrong = (D + 4) * EPS * (d.abs() @ V.abs().t()) + (d.abs() * (used - Y).abs()).sum(-1, keepdim=True) \
+            rounded = (d.abs() * (used - Y).abs()).sum(-1, keepdim=True)
+            wrong = (D + 4) * EPS * (d.abs() @ V.abs().t()) \
                 + (D + 4) * EPS * (d.abs() * Y.abs()).sum(-1, keepdim=True) + EPS * (dp.abs() + delta.abs())
+            if dtype is torch.float32:
+                wrong = wrong + rounded
+            else:
+                row = ((ds.abs() + p * rounded) * (e + sum_eps) + p * wrong).sum(-1, keepdim=True)
+                wrong = wrong + (3 * u + tiny) * rounded + row
             ds_off = ds.abs() * (e + u) + p * wrong * (1 + e) + (tiny * big * 2.0 ** -13 * (~later).double() if half else 0.0)
             val["dv"][a:b, g] += p.t() @ d
             val["dq"][a:b, h] = scale * ds @ K

@@ -281,6 +281,19 @@ def test_small_gradients_of_halves(ly):
         assert float(((g - value).abs() - (lo.UNIT[HF] * (value.abs() + bound) + bound))[ok].max()) <= 0, n
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_gradient_does_not_feel_how_y_was_rounded(ly, dtype):
+    """Short rows, whose y is large: y off by four roundings gives the gradients of the exact one."""
+    o = packed(*[7] * 30, 60)
+    q, k, v, dy = operands(93, o[-1], 4, 2, 64, dtype)
+    y, lse = ly.attention(q, k, v, offs(*o))
+    worse = (y.float() * (1 + 4 * lo.UNIT[dtype])).to(dtype)
+    got = dict(zip(("dq", "dk", "dv"), ly.attention_grad(dy, q, k, v, worse, lse, offs(*o))))
+    want = ao.attention(q.double(), k.double(), v.double(), o, 64 ** -0.5, dy.double(), worse.double(), dtype)
+    for n in got:
+        lo.assert_within(got[n], *want[n], n)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_against_differences(ly, dtype):
     """The definition's own gradients (which the kernels are tested against) against differences."""
