@@ -457,10 +457,13 @@ dc_status dc_block_norm_grad(const dc_block_norm_cfg *cfg, const void *dy, const
  * Outputs may be their own inputs (q_out = q of contiguous q; dq = dq_out).
  * Errors: DC_ERR_NULL, DC_ERR_BAD_LAYER (dtype; tokens outside [0, 2^31 - 1]; heads or kv_heads
  * outside [1, DC_HEADS_MAX]; D outside [1, DC_HEAD_NORM_DIM_MAX]; rotary odd, negative or above D;
- * base <= 0 or not finite; eps < 0; heads that overlap), DC_ERR_WORKSPACE, DC_ERR_CUDA.
+ * base outside [DC_ROTARY_BASE_MIN, DC_ROTARY_BASE_MAX]; eps < 0 or not finite; heads that overlap),
+ * DC_ERR_WORKSPACE, DC_ERR_CUDA.
  * ---------------------------------------------------------------------- */
 #define DC_HEADS_MAX 1024
 #define DC_HEAD_NORM_DIM_MAX 256
+#define DC_ROTARY_BASE_MIN 1e-3
+#define DC_ROTARY_BASE_MAX 1e30
 typedef struct dc_head_norm_cfg {
     int32_t dtype, heads, kv_heads, D, rotary, interleaved, norm;
     int64_t tokens;
@@ -488,7 +491,11 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
  * (of y; contiguous), the call's inputs, y and lse, and writes dq, dk, dv (contiguous):
  *   P = e^(S - lse),  dS_ij = P_ij (dy_i . v_j - dy_i . y_i),
  *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dy_i
- * with the sums of dk and dv over every head that reads the key head. What stands in rows of
+ * with the sums of dk and dv over every head that reads the key head. 16-bit types run on the tensor
+ * cores: P and dS are rounded to the type for their products (each at most half a step of a term; halves
+ * in a power of two of their own, so that small gradients keep their digits), everything else is in floats,
+ * and what y's own rounding does to dy_i . y_i is taken back, since a row of dS sums to zero. Floats run on
+ * the CUDA cores. What stands in rows of
  * other sequences, or of keys after a row, has no effect on it, infinities and NaN included.
  * Rows of no sequence (before offsets[0] or from offsets[sequences] on) get zeros in y, lse,
  * dq, dk and dv. An offset outside [0, tokens], or below an earlier one, counts as the nearest
@@ -496,13 +503,14 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
  * workspace: dc_attention_workspace_bytes(shape, grad, q, k, v, dy) bytes, 256-byte aligned, used
  * during the call's kernels only (grad 0 or 1; the addresses decide whether copies are
  * needed; dy of no account for grad 0). status (device, nullable): as for the expert products.
- * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; tokens outside [0, 2^31 - 1]; sequences outside
+ * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; tokens outside [0, DC_ATTENTION_TOKENS_MAX]; sequences outside
  * [0, DC_SEQUENCES_MAX]; heads or kv_heads outside [1, DC_HEADS_MAX]; heads not a multiple of
- * kv_heads; D outside [1, DC_ATTENTION_DIM_MAX]; a scale that is not finite; heads that
+ * kv_heads; D outside [1, DC_ATTENTION_DIM_MAX]; a scale that is not finite (twice it, as a float); heads that
  * overlap, or strides above 2^37); DC_ERR_WORKSPACE; DC_ERR_CUDA.
  * ---------------------------------------------------------------------- */
 #define DC_ATTENTION_DIM_MAX 128
 #define DC_SEQUENCES_MAX 1048576
+#define DC_ATTENTION_TOKENS_MAX 2147482624 /* 2^31 - 1024 */
 typedef struct dc_attention_shape {
     int32_t dtype, heads, kv_heads, D, sequences;
     int64_t tokens;

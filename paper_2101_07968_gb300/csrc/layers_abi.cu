@@ -139,7 +139,8 @@ dc_status check_head_norm(const dc_head_norm_cfg *c)
     if (!c) return DC_ERR_NULL;
     const bool ok = dtype_ok(c->dtype) && rows_ok(c->tokens) && count_ok(c->heads) && count_ok(c->kv_heads) &&
                     c->D >= 1 && c->D <= DC_HEAD_NORM_DIM_MAX && c->rotary >= 0 && c->rotary <= c->D &&
-                    c->rotary % 2 == 0 && c->base > 0.0 && std::isfinite(c->base) && c->eps >= 0.0 &&
+                    c->rotary % 2 == 0 && c->base >= DC_ROTARY_BASE_MIN && c->base <= DC_ROTARY_BASE_MAX &&
+                    c->eps >= 0.0 && std::isfinite(float(c->eps)) &&
                     heads_ok(c->q_token, c->q_head, c->heads, c->D, c->tokens) &&
                     heads_ok(c->k_token, c->k_head, c->kv_heads, c->D, c->tokens);
     return ok ? DC_OK : DC_ERR_BAD_LAYER;
@@ -170,10 +171,11 @@ HeadNormArgs head_norm_args(const dc_head_norm_cfg *c)
 dc_status check_attention(const dc_attention_shape *s)
 {
     if (!s) return DC_ERR_NULL;
-    const bool ok = dtype_ok(s->dtype) && rows_ok(s->tokens) && s->sequences >= 0 &&
+    // tiles' ends and scaled scores stay in range
+    const bool ok = dtype_ok(s->dtype) && s->tokens >= 0 && s->tokens <= DC_ATTENTION_TOKENS_MAX && s->sequences >= 0 &&
                     s->sequences <= DC_SEQUENCES_MAX && count_ok(s->heads) && count_ok(s->kv_heads) &&
                     s->heads % s->kv_heads == 0 && s->D >= 1 && s->D <= DC_ATTENTION_DIM_MAX &&
-                    std::isfinite(s->scale) && heads_ok(s->q_token, s->q_head, s->heads, s->D, s->tokens) &&
+                    std::isfinite(2.0f * float(s->scale)) && heads_ok(s->q_token, s->q_head, s->heads, s->D, s->tokens) &&
                     heads_ok(s->k_token, s->k_head, s->kv_heads, s->D, s->tokens) &&
                     heads_ok(s->v_token, s->v_head, s->kv_heads, s->D, s->tokens);
     return ok ? DC_OK : DC_ERR_BAD_LAYER;

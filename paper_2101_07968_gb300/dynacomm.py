@@ -33,6 +33,7 @@ DC_BF16, DC_FP16, DC_FP32 = 0, 1, 2
 DC_ACT_SILU, DC_ACT_GELU = 0, 1
 DC_NORM_RMS, DC_NORM_LAYER = 0, 1
 DC_HEADS_MAX, DC_HEAD_NORM_DIM_MAX, DC_ATTENTION_DIM_MAX, DC_SEQUENCES_MAX = 1024, 256, 128, 1048576
+DC_ATTENTION_TOKENS_MAX, DC_ROTARY_BASE_MIN, DC_ROTARY_BASE_MAX = 2147482624, 1e-3, 1e30
 DC_EXPERTS_MAX, DC_LAYER_DIM_MAX, DC_NORM_DIM_MAX, DC_FEW_ROWS = 1024, 1048576, 16384, 4
 
 

@@ -40,7 +40,8 @@ def test_head_norm_checks(lib):
         null.get("dk", FAKE), dwq, None, ws, n, None)
     for bad in STRIDES + [dict(dtype=3), dict(heads=0), dict(kv_heads=0), dict(heads=1025, q_token=1025 * 64), dict(D=0),
                           dict(D=257, q_head=257, k_head=257, q_token=2000, k_token=1000), dict(rotary=63), dict(rotary=-2),
-                          dict(rotary=66), dict(tokens=-1), dict(tokens=2**31), dict(base=0.0), dict(base=-1.0),
+                          dict(rotary=66), dict(tokens=-1), dict(tokens=2**31), dict(base=0.0), dict(base=-1.0), dict(base=9e-4),
+                          dict(base=1.1e30), dict(eps=1e39),
                           dict(base=float("inf")), dict(base=float("nan")), dict(eps=-1e-9), dict(eps=float("nan"))]:
         assert fwd(norm_cfg(**bad)) == dc.DC_ERR_BAD_LAYER, bad
         assert bwd(norm_cfg(**bad)) == dc.DC_ERR_BAD_LAYER, bad
@@ -66,7 +67,7 @@ def test_attention_checks(lib):
                                                                      None)
     for bad in STRIDES + [dict(dtype=3), dict(dtype=-1), dict(heads=3), dict(heads=0), dict(kv_heads=0), dict(kv_heads=8), dict(D=0),
                           dict(D=129, q_head=129, k_head=129, v_head=129, q_token=999, k_token=999, v_token=999),
-                          dict(sequences=-1), dict(sequences=2**20 + 1), dict(tokens=-1), dict(tokens=2**31),
+                          dict(sequences=-1), dict(sequences=2**20 + 1), dict(tokens=-1), dict(tokens=2**31 - 1023), dict(scale=3e38),
                           dict(scale=float("nan")), dict(scale=float("inf")), dict(v_head=63), dict(v_token=127)]:
         assert fwd(shape(**bad)) == dc.DC_ERR_BAD_LAYER, bad
         assert bwd(shape(**bad)) == dc.DC_ERR_BAD_LAYER, bad

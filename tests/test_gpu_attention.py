@@ -156,6 +156,13 @@ def test_strides(ly, dtype):
         a = both(ly, q, k, v, dy, o)
         b = both(ly, q.contiguous(), k.contiguous(), v.contiguous(), dy, o)
         assert all(torch.equal(a[n], b[n]) for n in a)
+    # heads of 75 elements 80 apart: aligned as they are; the same bits as of copies
+    wide = normal(6, T, H + 2 * G, 80, dtype=dtype)[..., :75]
+    q, k, v, d75 = wide[:, :H], wide[:, H:H + G], wide[:, H + G:], normal(7, T, H, 75, dtype=dtype)
+    a = both(ly, q, k, v, d75, o)
+    b = both(ly, q.contiguous(), k.contiguous(), v.contiguous(), d75, o)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    q, k, v = across[:, :H], across[:, H:H + G], across[:, H + G:]
     # a gradient that is contiguous but starts off 16-byte boundaries
     shifted = torch.empty(dy.numel() + 1, dtype=dtype, device="cuda")[1:].view(dy.shape).copy_(dy)
     assert all(torch.equal(x, y) for x, y in zip(both(ly, q, k, v, shifted, o).values(), both(ly, q, k, v, dy, o).values()))

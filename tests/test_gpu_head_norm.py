@@ -191,6 +191,29 @@ def test_far_addresses(ly):
     assert torch.equal(a["dq"][last], b["dq"]) and torch.equal(a["dk"][last], b["dk"])
 
 
+@pytest.mark.parametrize("D,H,G", [(64, 5, 2), (128, 3, 1), (50, 4, 3)])
+def test_in_place(ly, D, H, G):
+    """The C functions may write over their inputs."""
+    import ctypes
+
+    from paper_2101_07968_gb300 import dynacomm as dc
+    T = 700
+    q, k, wq, wk, dq, dk = operands(29, T, H, G, D, BF)
+    pos = torch.arange(T, device="cuda")
+    want = ly.head_norm_rotary(q, k, pos, wq, wk)
+    grad = ly.head_norm_rotary_grad(dq, dk, q, k, pos, wq, wk)
+    cfg = ctypes.byref(dc.dc_head_norm_cfg(dc.DC_BF16, H, G, D, D, 0, 1, T, H * D, D, G * D, D, 1e4, 1e-6))
+    s, p = torch.cuda.current_stream().cuda_stream, lambda t: t.data_ptr()
+    need = dc.lib().dc_head_norm_rotary_grad_workspace_bytes(cfg)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    dw = torch.empty(2, D, device="cuda")
+    assert dc.lib().dc_head_norm_rotary_grad(cfg, p(dq), p(dk), p(q), p(k), p(pos), p(wq), p(wk), p(dq), p(dk), p(dw[0]),
+                                             p(dw[1]), p(ws), need, s) == 0
+    assert torch.equal(dq, grad["dq"]) and torch.equal(dk, grad["dk"]) and torch.equal(dw[0], grad["dw_q"])
+    assert dc.lib().dc_head_norm_rotary(cfg, p(q), p(k), p(pos), p(wq), p(wk), p(q), p(k), s) == 0
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
 def test_against_differences(ly):
     q, k, wq, wk, dq, dk = (lo.d64(t) for t in operands(23, 3, 2, 1, 10, FL))
     pos = torch.tensor([0, 4, 9])
