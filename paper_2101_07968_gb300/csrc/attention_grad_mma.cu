@@ -55,26 +55,29 @@ struct Step {
     int32_t head, c0, count;
     bool diagonal, cut;
 };
+// Where an item's work is: the head of the group, and its block.
+struct Walk {
+    int32_t head = 0, block = 0;
+    __device__ __forceinline__ void next(int per_head)
+    {
+        if (++block == per_head) {
+            block = 0;
+            ++head;
+        }
+    }
+};
 template <bool COLUMNS>
 struct Item {
     AttentionTile t;
     int32_t outer, kv, part, head0, per_head, steps;
-    __device__ __forceinline__ Step step(const AttentionArgs &a, int i) const
+    __device__ __forceinline__ Step step(const Walk &w) const
     {
         Step s;
-        if (COLUMNS) {
-            const int k = i / per_head, j = i - k * per_head;
-            s.head = head0 + k;
-            s.c0 = t.row0 + j * kTile;
-            s.count = min(kTile, t.end - s.c0);
-            s.diagonal = j == 0;
-            s.cut = s.diagonal || s.count < kTile;
-        } else {
-            s.head = outer;
-            s.c0 = t.first + i * kTile;
-            s.count = min(kTile, t.row0 + t.rows - s.c0);
-            s.diagonal = s.cut = i == steps - 1;
-        }
+        s.head = head0 + w.head;
+        s.c0 = (COLUMNS ? t.row0 : t.first) + w.block * kTile;
+        s.count = min(kTile, (COLUMNS ? t.end : t.row0 + t.rows) - s.c0);
+        s.diagonal = w.block == (COLUMNS ? 0 : per_head - 1);
+        s.cut = s.diagonal || (COLUMNS && s.count < kTile);
         return s;
     }
 };
@@ -228,8 +231,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 bw::bar_arrive_bytes(bar(&b.still_full), 2 * kBytes);
                 tile(base, COLUMNS ? map_k : map_q, COLUMNS ? q.kv : q.outer, q.t.row0, bar(&b.still_full));
                 tile(base + kBytes, COLUMNS ? map_v : map_dy, COLUMNS ? q.kv : q.outer, q.t.row0, bar(&b.still_full));
-                for (int j = 0; j < q.steps; ++j) {
-                    const Step s = q.step(a, j);
+                Walk w;
+                for (int j = 0; j < q.steps; ++j, w.next(q.per_head)) {
+                    const Step s = q.step(w);
                     const int head = COLUMNS ? s.head : q.kv;
                     const uint32_t x = nx % G::kX, y = ny % G::kY;
                     ok = nx < G::kX || bw::bar_wait(bar(&b.x_free[x]), (nx / G::kX - 1) & 1, gave_up);
@@ -300,8 +304,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 first(n);
                 second(n, q.steps == 1);
                 if (i >= 0) next = item_at<COLUMNS>(a, i);  // looked up while this one is at work
-                for (int j = 0; j < q.steps && ok; ++j, ++n) {
-                    const Step s = q.step(a, j);
+                Walk w;
+                for (int j = 0; j < q.steps && ok; ++j, ++n, w.next(q.per_head)) {
+                    const Step s = q.step(w);
                     ok = bw::bar_wait(bar(&b.p_full), n & 1, gave_up);
                     if (!ok) break;
                     bw::fence_after();
@@ -330,8 +335,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             bool ok = true;
             for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
                 const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
-                for (int j = 0; j < q.steps; ++j, ++n) {
-                    const Step s = q.step(a, j);
+                Walk w;
+                for (int j = 0; j < q.steps; ++j, ++n, w.next(q.per_head)) {
+                    const Step s = q.step(w);
                     const int64_t at = s.head * a.tokens + s.c0;
                     float l[4], d[4];
 #pragma unroll
@@ -359,8 +365,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         bool ok = true;
         for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
             const Item<COLUMNS> q = item_at<COLUMNS>(a, i);
-            for (int j = 0; j < q.steps; ++j, ++n) {
-                const Step s = q.step(a, j);
+            Walk w;
+            for (int j = 0; j < q.steps; ++j, ++n, w.next(q.per_head)) {
+                const Step s = q.step(w);
                 if (!s.cut) continue;
                 const uint32_t at = checks % kChecks;
                 ok = bw::bar_wait(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
@@ -424,8 +431,9 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 lse = twice(there ? -a.lse[at] * kLog2e : 0.0f);
                 delta = twice(there ? -a.delta[at] * f : 0.0f);
             }
-            for (int j = 0; j < q.steps; ++j, ++n) {
-                const Step s = q.step(a, j);
+            Walk w;
+            for (int j = 0; j < q.steps; ++j, ++n, w.next(q.per_head)) {
+                const Step s = q.step(w);
                 const float *const l = stats + n % G::kL * 2 * kTile + side * 64;
                 ok = bw::bar_wait(bar(&b.s_full), n & 1, gave_up);
                 if (COLUMNS) ok = ok && bw::bar_wait(bar(&b.l_full[n % G::kL]), (n / G::kL) & 1, gave_up);
