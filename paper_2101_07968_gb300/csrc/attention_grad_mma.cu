@@ -370,7 +370,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 const Step s = q.step(w);
                 if (!s.cut) continue;
                 const uint32_t at = checks % kChecks;
-                ok = bw::bar_wait(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
+                ok = bw::bar_wait_idle(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
                 // rows behind the mask: of Y where it is summed too, and of X
                 for (int of_x = COLUMNS ? 0 : 1; of_x < 2; ++of_x) {
                     const uint32_t stage = of_x ? n % G::kX : n % G::kY, phase = of_x ? n / G::kX : n / G::kY;

@@ -313,7 +313,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const uint32_t n = checks_of<PAIR>(q);
             for (uint32_t x = 0; x < n; ++x, ++checks) {
                 const uint32_t v = c + 2 * q.blocks[x] - 1;
-                ok = bw::bar_wait_inline(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
+                ok = bw::bar_wait_idle(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
                      bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
@@ -337,7 +337,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 q.last = true;
                 if (i >= 0) q = item_at<PAIR>(a, i);
                 more = !q.last;
-                ok = round < kItems || bw::bar_wait_inline(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up);
+                ok = round < kItems || bw::bar_wait_idle(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up);
                 if (!ok) break;
                 h.items[at] = q;
                 bw::bar_arrive(bar(&h.item_full[at]));

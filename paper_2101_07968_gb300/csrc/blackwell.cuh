@@ -134,6 +134,19 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         if (bar_try(bar, parity)) return true;
     return bar_wait_long(bar, parity, gave_up, progress);
 }
+// The same for a thread whose work is seldom and early: it sleeps between tries and leaves its issue slots to others.
+__device__ __forceinline__ bool bar_wait_idle(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    const uint64_t start = now_ns();
+#pragma unroll 1
+    for (uint32_t i = 0; i < kWaitTries; ++i) {
+        if (bar_try(bar, parity)) return true;
+        __nanosleep(100);
+        if ((i & 63u) == 63u && (*gave_up || now_ns() - start > kWaitNs)) break;
+    }
+    *gave_up = 1u;
+    return false;
+}
 // The same without a call.
 __device__ __forceinline__ bool bar_wait_inline(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
 {
