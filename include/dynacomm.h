@@ -494,8 +494,9 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
  * with the sums of dk and dv over every head that reads the key head. 16-bit types run on the tensor
  * cores: P and dS are rounded to the type for their products (each at most half a step of a term; halves
  * in a power of two of their own, so that small gradients keep their digits), everything else is in floats,
- * and what y's own rounding does to dy_i . y_i is taken back, since a row of dS sums to zero. Floats run on
- * the CUDA cores. What stands in rows of
+ * and what y's own rounding does to dy_i . y_i is taken back, since a row of dS sums to zero. Sums on the
+ * tensor cores are cut off toward zero where floats would round: by some 2^-24 of their terms' magnitudes for
+ * every 16 terms (6e-5 for 16,384 terms of one sign). Floats run on the CUDA cores. What stands in rows of
  * other sequences, or of keys after a row, has no effect on it, infinities and NaN included.
  * Rows of no sequence (before offsets[0] or from offsets[sequences] on) get zeros in y, lse,
  * dq, dk and dv. An offset outside [0, tokens], or below an earlier one, counts as the nearest
