@@ -374,7 +374,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 const Step s = q.step(w);
                 if (!s.cut) continue;
                 const uint32_t at = checks % kChecks;
-                ok = bw::bar_wait_idle(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
+                ok = bw::bar_wait(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
                 // rows behind the mask: of Y where it is summed too, and of X
                 for (int of_x = COLUMNS ? 0 : 1; of_x < 2; ++of_x) {
                     const uint32_t stage = of_x ? n % G::kX : n % G::kY, phase = of_x ? n / G::kX : n / G::kY;
@@ -561,27 +561,26 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             bw::fence_after();
             float lacks = 0.0f;
             if (!COLUMNS) {
+                // (read long before they are written again: an item's sums wait for every warp)
                 stats[side * kTile + r] = excess.x + excess.y;
                 meet();
                 if (!ok) break;
                 lacks = stats[r] + stats[kTile + r];
                 if (side == 0 && r < q.t.rows) a.delta[q.outer * a.tokens + q.t.row0 + r] += lacks / f;
-                meet();  // both have read them
-                if (!ok) break;
             }
             constexpr int kCols = COLUMNS ? DP : DP / 2;  // of a thread
             const int d0 = COLUMNS ? 0 : side * kCols;
             const uint32_t from = lanes + (COLUMNS && side == 0 ? kSum1 : kSum0) + d0;
             const float by_sum = COLUMNS && side == 0 ? by1 : by0;
 #pragma unroll 1
-            for (int d = 0; d < kCols; d += 16) {
-                float v[16], b_row[16];
+            for (int d = 0; d < kCols; d += 32) {
+                float v[32], b_row[32];
                 __syncwarp();
                 bw::tmem_load(from + d, v);
                 if (!COLUMNS) {
                     bw::tmem_load(lanes + kSum1 + d0 + d, b_row);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] -= lacks * b_row[e];
+                    for (int e = 0; e < 32; ++e) v[e] -= lacks * b_row[e];
                 }
                 if (r >= q.t.rows) continue;
                 if (part)
