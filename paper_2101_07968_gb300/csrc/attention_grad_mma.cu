@@ -7,10 +7,11 @@
 //            b += P k
 // Seven products a block instead of the five that one pass would need: dq of one pass would be summed
 // by many CTAs, in memory and in an order that depends on timing; so each sum has one owner.
-// The eighth, b, takes back what y's rounding does to delta: as a row of P sums to one, a row of dS sums to zero, and
-// what it sums to instead, E, is what delta lacks. So the rows' pass comes first, gives dq - E b, and leaves
-// delta + E for the columns' (in rows of 16 keys bfloat16's dq is 4.0e-3 off without, 2.3 with; 1.6 is its own rounding). Where tiles and
-// key heads are few, a group's heads are dealt to several CTAs, whose sums are joined afterwards.
+// The eighth, b, takes back what y's rounding does to delta: as a row of P sums to one, a row of dS sums to zero,
+// and what it sums to instead, E, is what delta lacks. So the rows' pass comes first, gives dq - E b, and leaves
+// delta + E for the columns' (in rows of 16 keys bfloat16's dq is 4.0e-3 off without, 2.3 with; 1.6 is its own
+// rounding). Where tiles and key heads are few, a group's heads are dealt to several CTAs, whose sums are joined
+// afterwards.
 //
 // Both are one kernel: two stationary tiles, two rings of moving ones (X: q or k, Y: dy or v), scores
 // and dP in tensor memory [128][128], the sums [128][D] beside them, 512 columns in all.
@@ -22,9 +23,9 @@
 // The products of one kind run while the warps make the other: S of the next block and dv beside dS,
 // dP of the next block and dk beside P.
 //
-// Measured (one GB300): 32,768 tokens in 14 sequences x 32 heads on 8 x 128, rows 1,125 us, columns 1,362 us; one prompt of
-// 16,384 x 16 x 128 2.5 ms, 1,750 TFLOP/s of the eight products. Tensor cores busy 75-81 % of the time; heads of 64 are bound
-// by the warps: a step of 128 x 128 takes them 1,900 clocks (rows) and 2,500 (columns), the products 1,024.
+// Measured (one GB300): 32,768 tokens in 14 sequences x 32 heads on 8 x 128, rows 1,091 us, columns 1,380 us; one
+// prompt of 16,384 x 16 x 128 2.45 ms, 1,795 TFLOP/s of the eight products. Tensor cores busy 75-81 % of the time; heads
+// of 64 are bound by the warps: a step of 128 x 128 takes them 1,900 clocks (rows) and 2,500 (columns), the products 1,024.
 //
 // Rounding: P and dS are rounded to the operands' type for the tensor cores, half a step of each
 // term. Halves have few exponents: P, at most 1, is held 2^8 times larger, and dS in a power of two
@@ -602,15 +603,13 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 }
 
 // ------------------------------------------------------------------------------ host
-template <typename T, int DP, bool COLUMNS>
-cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
-{
+struct Maps {
     CUtensorMap q, k, v, dy;
-    if (!heads_map(q, dtype, a.q, a.D, a.heads, a.tokens, a.q_head, a.q_token) ||
-        !heads_map(k, dtype, a.k, a.D, a.kv_heads, a.tokens, a.k_head, a.k_token) ||
-        !heads_map(v, dtype, a.v, a.D, a.kv_heads, a.tokens, a.v_head, a.v_token) ||
-        !heads_map(dy, dtype, a.dy, a.D, a.heads, a.tokens, a.dy_head, a.dy_token))
-        return cudaErrorInvalidValue;
+};
+
+template <typename T, int DP, bool COLUMNS>
+cudaError_t launch(const Maps &m, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
     auto kernel = attention_grad_mma_kernel<T, DP, COLUMNS>;
     constexpr int smem = int(Shape<DP, COLUMNS>::kSmem);
     static_assert(smem <= 232448, "shared memory of a CTA");
@@ -623,21 +622,30 @@ cudaError_t launch(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t
     if (e == cudaSuccess) e = sm_count(sms);
     if (e != cudaSuccess) return e;
     const int64_t items = most * (COLUMNS ? a.kv_heads * a.split : a.heads);
-    return launch_early(kernel, items < sms ? items : sms, kThreads, smem, stream, q, k, v, dy, a);
+    return launch_early(kernel, items < sms ? items : sms, kThreads, smem, stream, m.q, m.k, m.v, m.dy, a);
+}
+
+// The rows' pass first: it completes delta.
+template <typename T, int DP>
+cudaError_t both(const Maps &m, const AttentionArgs &a, int64_t most, cudaStream_t stream)
+{
+    const cudaError_t e = launch<T, DP, false>(m, a, most, stream);
+    return e == cudaSuccess ? launch<T, DP, true>(m, a, most, stream) : e;
 }
 
 }  // namespace
 
 cudaError_t launch_attention_grad_mma(int dtype, const AttentionArgs &a, int64_t most, cudaStream_t stream)
 {
-    auto go = [&](auto t) {
-        using T = decltype(t);
-        cudaError_t e = a.D <= 64 ? launch<T, 64, false>(dtype, a, most, stream) : launch<T, 128, false>(dtype, a, most, stream);
-        if (e == cudaSuccess)
-            e = a.D <= 64 ? launch<T, 64, true>(dtype, a, most, stream) : launch<T, 128, true>(dtype, a, most, stream);
-        return e;
-    };
-    return dtype == DC_BF16 ? go(__nv_bfloat16()) : go(__half());
+    Maps m;
+    if (!heads_map(m.q, dtype, a.q, a.D, a.heads, a.tokens, a.q_head, a.q_token) ||
+        !heads_map(m.k, dtype, a.k, a.D, a.kv_heads, a.tokens, a.k_head, a.k_token) ||
+        !heads_map(m.v, dtype, a.v, a.D, a.kv_heads, a.tokens, a.v_head, a.v_token) ||
+        !heads_map(m.dy, dtype, a.dy, a.D, a.heads, a.tokens, a.dy_head, a.dy_token))
+        return cudaErrorInvalidValue;
+    if (dtype == DC_BF16)
+        return a.D <= 64 ? both<__nv_bfloat16, 64>(m, a, most, stream) : both<__nv_bfloat16, 128>(m, a, most, stream);
+    return a.D <= 64 ? both<__half, 64>(m, a, most, stream) : both<__half, 128>(m, a, most, stream);
 }
 
 }  // namespace dc

@@ -190,167 +190,167 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (warp >= 12) {
         bw::fewer_registers<kOtherRegs>();
         if (warp == 12) {
-        if (bw::elect_one()) {  // copies
-            int s = 0;
-            uint32_t phase = 1, tiles = 0;  // of queries so far
-            bool ok = true;
-            auto block = [&](const CUtensorMap &map, int head, int row) {
-                ok = ok && bw::bar_wait_inline(bar(&h.empty[s]), phase, gave_up);
-                if (!ok) return;
-                bw::bar_arrive_bytes(bar(&h.full[s]), kBytes);
-                for (int i = 0; i < kBoxes; ++i)
-                    bw::copy_3d1(ring + s * kBytes + i * kBox, &map, 64 * i, head, row, bar(&h.full[s]));
-                if (++s == kStages) {
-                    s = 0;
-                    phase ^= 1;
-                }
-            };
-            uint32_t checks = 0;
-            Item q;
-            for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
-                for (int x = 0; x < 2; ++x) {
-                    if (q.blocks[x] == 0) continue;
-                    const uint32_t at = tiles % kQ;
-                    ok = ok && (tiles < kQ || bw::bar_wait_inline(bar(&h.q_free[at]), (tiles / kQ - 1) & 1, gave_up));
-                    if (!ok) break;
-                    ++tiles;
-                    bw::bar_arrive_bytes(bar(&h.q_full[at]), kBytes);
-                    for (int b = 0; b < kBoxes; ++b)
-                        bw::copy_3d1(base + at * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&h.q_full[at]));
-                    if (x == 0) block(map_k, q.kv, q.first);
-                }
-                const int n = max(q.blocks[0], q.blocks[1]);
-                for (int j = 0; j < n && ok; ++j) {
-                    if (j > 0) block(map_k, q.kv, q.first + j * kTile);
-                    block(map_v, q.kv, q.first + j * kTile);
-                    // values on the diagonal are to be looked through: their barrier's phase has begun, and does not
-                    // end twice before they are
-                    for (int x = 0; x < (PAIR ? 1 : 2) && ok; ++x)
-                        if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&h.look[(checks + x) % kChecks]));
-                }
-                checks += checks_of<PAIR>(q);
-            }
-        }
-        } else if (warp == 13) {
-        if (bw::elect_one()) {  // products
-            constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
-            const uint32_t shape_s = bw::f16_shape(kBf, false, false, kTile, kTile);
-            const uint32_t shape_y = bw::f16_shape(kBf, false, true, kTile, DP);
-            uint32_t c = 0;  // blocks of the ring before this item
-            uint32_t tiles = 0, blocks[2] = {0, 0}, items_of[2] = {0, 0}, checks = 0;  // of either tile so far; of both
-            uint32_t at[2] = {0, 0};  // where the tiles' queries are
-            bool ok = true;
-            auto have = [&](uint32_t n) {
-                ok = ok && bw::bar_wait_inline(bar(&h.full[n % kStages]), (n / kStages) & 1, gave_up);
-                return ok;
-            };
-            auto scores = [&](int x, uint32_t n) {
-                const uint64_t dq = bw::operand(base + at[x] * kBytes, 16), dk = bw::operand(ring + n % kStages * kBytes, 16);
-                bw::fence_after();
-#pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    const uint64_t step = (i / 4) * (kBox >> 4) + (i % 4) * 2;
-                    bw::mma1(tmem + x * kTile, dq + step, dk + step, shape_s, i > 0);
-                }
-            };
-            Item q;
-            for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
-                const int n = max(q.blocks[0], q.blocks[1]);
-                for (int x = 0; x < 2 && ok; ++x) {
-                    if (q.blocks[x] == 0) continue;
-                    at[x] = tiles % kQ;
-                    ok = bw::bar_wait_inline(bar(&h.q_full[at[x]]), (tiles / kQ) & 1, gave_up);
-                    ++tiles;
-                    if (!have(c)) break;
-                    scores(x, c);
-                    bw::commit1(bar(&h.s_full[x]));
-                    if (q.blocks[x] == 1) bw::commit1(bar(&h.q_free[at[x]]));
-                }
-                if (n > 0) bw::commit1(bar(&h.empty[c % kStages]));
-                for (int j = 0; j < n && ok; ++j) {
-                    const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
-                    if (!have(v)) break;
-                    for (int x = 0; x < 2 && ok; ++x) {
-                        if (j >= q.blocks[x]) continue;
-                        const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
-                        auto half = [&](int i0) {
-#pragma unroll
-                            for (int i = i0; i < i0 + kTile / 32; ++i)
-                                bw::mma1_tmem(tmem + 2 * kTile + x * DP, tmem + x * kTile + i * 8, dv + i * 128, shape_y,
-                                              j > 0 || i > 0);
-                        };
-                        // the rows before these have left
-                        ok = j > 0 || items_of[x]++ == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), items_of[x] & 1, gave_up);
-                        ok = ok && bw::bar_wait_inline(bar(&h.p_half[x]), blocks[x] & 1, gave_up);
-                        if (!ok) break;
-                        bw::fence_after();
-                        // (known before the first half is handed over)
-                        const bool own = j + 1 < q.blocks[x] || !is_by_hand(checks + (PAIR ? 0 : x));
-                        if (own) half(0);
-                        ok = bw::bar_wait_inline(bar(&h.p_full[x]), blocks[x]++ & 1, gave_up);
-                        if (!ok) break;
-                        bw::fence_after();
-                        if (own) half(kTile / 32);
-                        if (j + 1 < q.blocks[x]) {
-                            if (!have(k)) break;
-                            scores(x, k);
-                            bw::commit1(bar(&h.s_full[x]));
-                            if (j + 2 == q.blocks[x]) bw::commit1(bar(&h.q_free[at[x]]));
-                        } else {
-                            bw::commit1(bar(&h.y_full[x]));
-                        }
+            if (bw::elect_one()) {  // copies
+                int s = 0;
+                uint32_t phase = 1, tiles = 0;  // of queries so far
+                bool ok = true;
+                auto block = [&](const CUtensorMap &map, int head, int row) {
+                    ok = ok && bw::bar_wait_inline(bar(&h.empty[s]), phase, gave_up);
+                    if (!ok) return;
+                    bw::bar_arrive_bytes(bar(&h.full[s]), kBytes);
+                    for (int i = 0; i < kBoxes; ++i)
+                        bw::copy_3d1(ring + s * kBytes + i * kBox, &map, 64 * i, head, row, bar(&h.full[s]));
+                    if (++s == kStages) {
+                        s = 0;
+                        phase ^= 1;
                     }
-                    bw::commit1(bar(&h.empty[v % kStages]));
-                    if (j + 1 < n) bw::commit1(bar(&h.empty[k % kStages]));
+                };
+                uint32_t checks = 0;
+                Item q;
+                for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
+                    for (int x = 0; x < 2; ++x) {
+                        if (q.blocks[x] == 0) continue;
+                        const uint32_t at = tiles % kQ;
+                        ok = ok && (tiles < kQ || bw::bar_wait_inline(bar(&h.q_free[at]), (tiles / kQ - 1) & 1, gave_up));
+                        if (!ok) break;
+                        ++tiles;
+                        bw::bar_arrive_bytes(bar(&h.q_full[at]), kBytes);
+                        for (int b = 0; b < kBoxes; ++b)
+                            bw::copy_3d1(base + at * kBytes + b * kBox, &map_q, 64 * b, q.head[x], q.row0[x], bar(&h.q_full[at]));
+                        if (x == 0) block(map_k, q.kv, q.first);
+                    }
+                    const int n = max(q.blocks[0], q.blocks[1]);
+                    for (int j = 0; j < n && ok; ++j) {
+                        if (j > 0) block(map_k, q.kv, q.first + j * kTile);
+                        block(map_v, q.kv, q.first + j * kTile);
+                        // values on the diagonal are to be looked through: their barrier's phase has begun, and does not
+                        // end twice before they are
+                        for (int x = 0; x < (PAIR ? 1 : 2) && ok; ++x)
+                            if (j + 1 == q.blocks[x]) bw::bar_arrive(bar(&h.look[(checks + x) % kChecks]));
+                    }
+                    checks += checks_of<PAIR>(q);
                 }
-                c += 2 * n;
-                checks += checks_of<PAIR>(q);
             }
-            // arrivals land in this CTA's memory: it may not end before the last
-            bw::commit1(bar(&h.last));
-            bw::bar_wait_inline(bar(&h.last), 0, gave_up);
-        }
+        } else if (warp == 13) {
+            if (bw::elect_one()) {  // products
+                constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
+                const uint32_t shape_s = bw::f16_shape(kBf, false, false, kTile, kTile);
+                const uint32_t shape_y = bw::f16_shape(kBf, false, true, kTile, DP);
+                uint32_t c = 0;  // blocks of the ring before this item
+                uint32_t tiles = 0, blocks[2] = {0, 0}, items_of[2] = {0, 0}, checks = 0;  // of either tile so far; of both
+                uint32_t at[2] = {0, 0};  // where the tiles' queries are
+                bool ok = true;
+                auto have = [&](uint32_t n) {
+                    ok = ok && bw::bar_wait_inline(bar(&h.full[n % kStages]), (n / kStages) & 1, gave_up);
+                    return ok;
+                };
+                auto scores = [&](int x, uint32_t n) {
+                    const uint64_t dq = bw::operand(base + at[x] * kBytes, 16), dk = bw::operand(ring + n % kStages * kBytes, 16);
+                    bw::fence_after();
+#pragma unroll
+                    for (int i = 0; i < DP / 16; ++i) {
+                        const uint64_t step = (i / 4) * (kBox >> 4) + (i % 4) * 2;
+                        bw::mma1(tmem + x * kTile, dq + step, dk + step, shape_s, i > 0);
+                    }
+                };
+                Item q;
+                for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
+                    const int n = max(q.blocks[0], q.blocks[1]);
+                    for (int x = 0; x < 2 && ok; ++x) {
+                        if (q.blocks[x] == 0) continue;
+                        at[x] = tiles % kQ;
+                        ok = bw::bar_wait_inline(bar(&h.q_full[at[x]]), (tiles / kQ) & 1, gave_up);
+                        ++tiles;
+                        if (!have(c)) break;
+                        scores(x, c);
+                        bw::commit1(bar(&h.s_full[x]));
+                        if (q.blocks[x] == 1) bw::commit1(bar(&h.q_free[at[x]]));
+                    }
+                    if (n > 0) bw::commit1(bar(&h.empty[c % kStages]));
+                    for (int j = 0; j < n && ok; ++j) {
+                        const uint32_t k = c + 2 * j + 2, v = c + 2 * j + 1;
+                        if (!have(v)) break;
+                        for (int x = 0; x < 2 && ok; ++x) {
+                            if (j >= q.blocks[x]) continue;
+                            const uint64_t dv = bw::operand(ring + v % kStages * kBytes, kBox);
+                            auto half = [&](int i0) {
+#pragma unroll
+                                for (int i = i0; i < i0 + kTile / 32; ++i)
+                                    bw::mma1_tmem(tmem + 2 * kTile + x * DP, tmem + x * kTile + i * 8, dv + i * 128, shape_y,
+                                                  j > 0 || i > 0);
+                            };
+                            // the rows before these have left
+                            ok = j > 0 || items_of[x]++ == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), items_of[x] & 1, gave_up);
+                            ok = ok && bw::bar_wait_inline(bar(&h.p_half[x]), blocks[x] & 1, gave_up);
+                            if (!ok) break;
+                            bw::fence_after();
+                            // (known before the first half is handed over)
+                            const bool own = j + 1 < q.blocks[x] || !is_by_hand(checks + (PAIR ? 0 : x));
+                            if (own) half(0);
+                            ok = bw::bar_wait_inline(bar(&h.p_full[x]), blocks[x]++ & 1, gave_up);
+                            if (!ok) break;
+                            bw::fence_after();
+                            if (own) half(kTile / 32);
+                            if (j + 1 < q.blocks[x]) {
+                                if (!have(k)) break;
+                                scores(x, k);
+                                bw::commit1(bar(&h.s_full[x]));
+                                if (j + 2 == q.blocks[x]) bw::commit1(bar(&h.q_free[at[x]]));
+                            } else {
+                                bw::commit1(bar(&h.y_full[x]));
+                            }
+                        }
+                        bw::commit1(bar(&h.empty[v % kStages]));
+                        if (j + 1 < n) bw::commit1(bar(&h.empty[k % kStages]));
+                    }
+                    c += 2 * n;
+                    checks += checks_of<PAIR>(q);
+                }
+                // arrivals land in this CTA's memory: it may not end before the last
+                bw::commit1(bar(&h.last));
+                bw::bar_wait_inline(bar(&h.last), 0, gave_up);
+            }
         } else if (warp == 14) {  // values on the diagonal
-        uint32_t c = 0, checks = 0;
-        bool ok = true;
-        Item q;
-        for (uint32_t item = 0; ok && item_of_warp(item, q); ++item) {
-            const uint32_t n = checks_of<PAIR>(q);
-            for (uint32_t x = 0; x < n; ++x, ++checks) {
-                const uint32_t v = c + 2 * q.blocks[x] - 1;
-                ok = bw::bar_wait_idle(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
-                     bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                unsigned char *tile = dyn + (kQ + v % kStages) * kBytes;
-                for (int r = lane; r < kTile; r += 32)
-                    if (look_through<T, DP>(tile, r, q.rows[x]))
-                        *const_cast<volatile uint32_t *>(&h.by_hand[checks % kChecks]) = checks + 1;
-                __syncwarp();
-                if (lane == 0) bw::bar_arrive(bar(&h.checked[checks % kChecks]));
-            }
-            c += 2 * max(q.blocks[0], q.blocks[1]);
-        }
-        } else {
-        if (bw::elect_one()) {  // items
+            uint32_t c = 0, checks = 0;
             bool ok = true;
-            bool more = true;
-            for (int64_t round = 0; ok && more; ++round) {
-                const int64_t i = dealt(round, items);
-                const uint32_t at = uint32_t(round % kItems);
-                Item q = {};
-                q.last = true;
-                if (i >= 0) q = item_at<PAIR>(a, i);
-                more = !q.last;
-                ok = round < kItems || bw::bar_wait_idle(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up);
-                if (!ok) break;
-                h.items[at] = q;
-                bw::bar_arrive(bar(&h.item_full[at]));
-                // the queries come to the L2
-                for (int x = 0; x < 2; ++x)
-                    for (int b = 0; b < kBoxes && q.blocks[x] > 0; ++b) bw::fetch_3d(&map_q, 64 * b, q.head[x], q.row0[x]);
+            Item q;
+            for (uint32_t item = 0; ok && item_of_warp(item, q); ++item) {
+                const uint32_t n = checks_of<PAIR>(q);
+                for (uint32_t x = 0; x < n; ++x, ++checks) {
+                    const uint32_t v = c + 2 * q.blocks[x] - 1;
+                    ok = bw::bar_wait_idle(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
+                         bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    unsigned char *tile = dyn + (kQ + v % kStages) * kBytes;
+                    for (int r = lane; r < kTile; r += 32)
+                        if (look_through<T, DP>(tile, r, q.rows[x]))
+                            *const_cast<volatile uint32_t *>(&h.by_hand[checks % kChecks]) = checks + 1;
+                    __syncwarp();
+                    if (lane == 0) bw::bar_arrive(bar(&h.checked[checks % kChecks]));
+                }
+                c += 2 * max(q.blocks[0], q.blocks[1]);
             }
-        }
+        } else {
+            if (bw::elect_one()) {  // items
+                bool ok = true;
+                bool more = true;
+                for (int64_t round = 0; ok && more; ++round) {
+                    const int64_t i = dealt(round, items);
+                    const uint32_t at = uint32_t(round % kItems);
+                    Item q = {};
+                    q.last = true;
+                    if (i >= 0) q = item_at<PAIR>(a, i);
+                    more = !q.last;
+                    ok = round < kItems || bw::bar_wait_idle(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up);
+                    if (!ok) break;
+                    h.items[at] = q;
+                    bw::bar_arrive(bar(&h.item_full[at]));
+                    // the queries come to the L2
+                    for (int x = 0; x < 2; ++x)
+                        for (int b = 0; b < kBoxes && q.blocks[x] > 0; ++b) bw::fetch_3d(&map_q, 64 * b, q.head[x], q.row0[x]);
+                }
+            }
         }
     } else if (warp >= 8) {  // finished rows
         bw::fewer_registers<kOtherRegs>();
