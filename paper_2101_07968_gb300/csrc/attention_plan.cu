@@ -118,8 +118,9 @@ attention_plan_kernel(const int64_t *offsets, int32_t sequences, int64_t tokens,
 }
 
 // delta[h][t] = sum over d of dy y: sixteen lanes a row of a head, sixteen bytes a lane at a time (32,768 tokens x 32
-// heads x 128: 104 us, 5.2 TB/s; two or four rows on their way at once, or neighbouring tokens a block: no less). Halves: also the largest finite |dy| and |v| of the sequences' rows, from
-// which the power of two follows that dS is held in; a maximum does not depend on the order.
+// heads x 128: 104 us, 5.2 TB/s; two or four rows on their way at once, or neighbouring tokens a block: no less). Halves:
+// also the largest finite |dy| and |v| of the sequences' rows, from which the power of two follows that dS is held in; a
+// maximum does not depend on the order.
 __device__ __forceinline__ float largest(float top, float x)
 {
     x = fabsf(x);
