@@ -568,6 +568,15 @@ dc_status dc_roof_int_probe(int32_t variant, int32_t blocks, int32_t threads, in
  * ---------------------------------------------------------------------- */
 dc_status dc_wait_probe(int32_t *status, cudaStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * dc_head_parts_probe -- test support, on the host alone: how the head norms deal a token's heads
+ * to groups of lanes where tokens are few. Part i of `parts` has the heads from i * per_part on, per_part
+ * of them or, the last part, what is left; `wanted` units of work fill the GPU, and a part
+ * other than the last has `least` heads or more where there are as many.
+ * ---------------------------------------------------------------------- */
+void dc_head_parts_probe(int64_t tokens, int32_t heads, int64_t wanted, int32_t least, int32_t *parts,
+                         int32_t *per_part);
+
 #ifdef __cplusplus
 }
 #endif

@@ -466,9 +466,9 @@ cudaError_t launch(HeadNormArgs a, bool runs, cudaStream_t stream)
     if (most > kMostBlocks) most = kMostBlocks;
     int64_t blocks[2];
     for (int i = 0; i < 2; ++i) {
-        a.parts[i] = 1;
-        while (a.tokens * a.parts[i] < int64_t(sms) * units && a.heads[i] > a.parts[i] * least) a.parts[i] *= 2;
-        a.per_part[i] = (a.heads[i] + a.parts[i] - 1) / a.parts[i];
+        const HeadParts p = head_parts(a.tokens, a.heads[i], int64_t(sms) * units, least);
+        a.parts[i] = p.parts;
+        a.per_part[i] = p.per_part;
         blocks[i] = (a.tokens * a.parts[i] + units - 1) / units;
     }
     if (blocks[0] + blocks[1] > most) {

@@ -178,6 +178,19 @@ struct HeadNormArgs {
     int32_t parts[2], per_part[2], blocks[2];  // of a token's heads, the heads of one, the grid (set by the launcher)
     uint64_t turns[DC_HEAD_NORM_DIM_MAX / 2];  // of pair i per position, in 2^-64 of a turn
 };
+// Few tokens: a token's heads are dealt to `parts` groups, `per_part` each (the last part's fewer, but one at least:
+// copies start at a part's first head), as finely as tokens * parts >= wanted needs, but not finer than `least` heads
+// a part.
+struct HeadParts {
+    int32_t parts, per_part;
+};
+inline HeadParts head_parts(int64_t tokens, int32_t heads, int64_t wanted, int32_t least)
+{
+    int32_t parts = 1;
+    while (tokens * parts < wanted && heads > parts * least) parts *= 2;
+    const int32_t per = (heads + parts - 1) / parts;
+    return {(heads + per - 1) / per, per};  // rounded up, the last parts would begin past the last head
+}
 size_t head_norm_workspace(int D);
 cudaError_t launch_head_norm(int dtype, const HeadNormArgs &a, cudaStream_t stream);
 cudaError_t launch_head_norm_grad(int dtype, const HeadNormArgs &a, cudaStream_t stream);

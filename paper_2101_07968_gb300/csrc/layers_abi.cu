@@ -428,6 +428,14 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
     return dc::result(dc::launch_head_norm_grad(cfg->dtype, a, stream));
 }
 
+void dc_head_parts_probe(int64_t tokens, int32_t heads, int64_t wanted, int32_t least, int32_t *parts,
+                         int32_t *per_part)
+{
+    const dc::HeadParts p = dc::head_parts(tokens, heads, wanted, least);
+    *parts = p.parts;
+    *per_part = p.per_part;
+}
+
 size_t dc_attention_workspace_bytes(const dc_attention_shape *s, int32_t grad, const void *q,
                                     const void *k, const void *v, const void *dy)
 {

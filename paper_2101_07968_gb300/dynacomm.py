@@ -134,6 +134,7 @@ _SIGNATURES = {
     "dc_attention": (_I32, [_ATTENTION] + [_VP] * 8 + [_SZ, _VP]),
     "dc_attention_grad": (_I32, [_ATTENTION] + [_VP] * 12 + [_SZ, _VP]),
     "dc_wait_probe": (_I32, [_VP, _VP]),
+    "dc_head_parts_probe": (None, [_I64, _I32, _I64, _I32, _VP, _VP]),
 }
 
 
