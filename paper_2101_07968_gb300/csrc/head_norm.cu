@@ -350,6 +350,8 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
             auto turn = [&](float(&t)[kPairs][2], float sign) {
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j) {
+                    // (a turn by nothing is none: zero times an infinity would reach the neighbour)
+                    if (lane + 32 * j >= half) continue;
                     const float p = t[j][0], r = t[j][1];
                     t[j][0] = p * c[j] - sign * r * s[j];
                     t[j][1] = r * c[j] + sign * p * s[j];
