@@ -250,12 +250,14 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
                 const float rstd = a.norm ? rsqrtf(sum[i] * inverse + a.eps) : 1.0f;
                 float2 out[4];
                 if constexpr (GRAD) {
-                    const float2 r = twice(rstd), back = twice(a.norm ? -dot[i] * inverse * rstd * rstd : 0.0f);
+                    const float2 r = twice(rstd), back = twice(-dot[i] * inverse * rstd * rstd);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float2 n = __fmul2_rn(v[i][k], r);
                         if (there) dw[k] = __ffma2_rn(d[i][k], n, dw[k]);
-                        out[k] = __ffma2_rn(n, back, __fmul2_rn(g[i][k], r));
+                        // (without a norm x is not read: zero times an infinity would be)
+                        out[k] = __fmul2_rn(g[i][k], r);
+                        if (a.norm) out[k] = __ffma2_rn(n, back, out[k]);
                     }
                 } else {
 #pragma unroll
@@ -372,8 +374,6 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
                     if (GRAD) along += __shfl_xor_sync(0xffffffffu, along, o);
                 }
                 rstd = rsqrtf(square * inverse + a.eps);
-            } else {
-                along = 0.0f;
             }
             float out[kPairs][2];
             const float back = along * inverse * rstd * rstd;
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
                 for (int k = 0; k < 2; ++k) {
                     if (GRAD) {
                         dw[j][k] += d[j][k] * (v[j][k] * rstd);
-                        out[j][k] = rstd * (d[j][k] * w[j][k] - v[j][k] * back);
+                        out[j][k] = a.norm ? rstd * (d[j][k] * w[j][k] - v[j][k] * back) : d[j][k] * w[j][k];
                     } else {
                         out[j][k] = v[j][k] * rstd * w[j][k];
                     }

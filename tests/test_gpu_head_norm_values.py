@@ -66,3 +66,20 @@ def test_elements_that_turn(ly, dtype, D, rotary):  # noqa: F811
         other = torch.ones_like(q, dtype=torch.bool)
         other[1, 0, 2] = other[1, 0, 3 if interleaved else 2 + rotary // 2] = False
         assert torch.equal(bits(got)[other], bits(want)[other])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,rotary", [(64, 64), (64, 32), (128, 128), (65, 20), (50, 50)])
+@pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
+def test_gradient_without_a_norm_does_not_read_its_input(ly, dtype, D, rotary, what):  # noqa: F811
+    """Without a norm, dq and dk are the weights times what comes back, whatever stands in q and k; of the
+    weights' gradients only that element's feels it."""
+    q, k, wq, wk, dq, dk = operands(D, 6, 3, 2, D, dtype)
+    pos = torch.arange(6, device="cuda")
+    want = ly.head_norm_rotary_grad(dq, dk, q, k, pos, wq, wk, rotary=rotary, norm=False)
+    q[3, 2, 5] = what
+    got = ly.head_norm_rotary_grad(dq, dk, q, k, pos, wq, wk, rotary=rotary, norm=False)
+    assert torch.equal(got["dq"], want["dq"]) and torch.equal(got["dk"], want["dk"])
+    others = torch.arange(D, device="cuda") != 5
+    assert torch.equal(got["dw_q"][others], want["dw_q"][others]) and not torch.isfinite(got["dw_q"][5])
+    assert torch.equal(got["dw_k"], want["dw_k"])
