@@ -28,7 +28,7 @@
 // of 64 are bound by the warps: a step of 128 x 128 takes them 1,900 clocks (rows) and 2,500 (columns), the products 1,024.
 //
 // Rounding: P and dS are rounded to the operands' type for the tensor cores, half a step of each
-// term. Halves have few exponents: P, at most 1, is held 2^8 times larger, and dS in a power of two
+// term. Halves have few exponents: P, at most 1, is held 2^14 times larger, and dS in a power of two
 // that no |dP - delta| <= 2 D max|dy| max|v| can overflow, known from a pass over dy and v; both are undone
 // in floats at the end. What a mask hides is zero by selection, and operands' rows behind it are
 // looked through as in the forward pass.
@@ -133,7 +133,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     constexpr int kBoxes = DP / 64;
     constexpr uint32_t kBytes = G::kBytes;
     constexpr bool kHalf = std::is_same<T, __half>::value;
-    constexpr int kPPower = kHalf && COLUMNS ? 8 : 0;  // P is held 2^kPPower times larger
+    constexpr int kPPower = kHalf ? 14 : 0;  // P is held 2^kPPower times larger
     extern __shared__ __align__(1024) unsigned char dyn[];
     struct Bars {
         uint64_t still_full, still_free, x_full[G::kX], x_free[G::kX], y_full[G::kY], y_free[G::kY], l_full[G::kL],
@@ -433,7 +433,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             if (!COLUMNS) {
                 const int64_t at = q.outer * a.tokens + q.t.row0 + r;
                 const bool there = r < q.t.rows;
-                lse = twice(there ? -a.lse[at] * kLog2e : 0.0f);
+                lse = twice((there ? -a.lse[at] * kLog2e : 0.0f) + float(kPPower));
                 delta = twice(there ? -a.delta[at] * f : 0.0f);
             }
             Walk w;
@@ -567,7 +567,8 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 meet();
                 if (!ok) break;
                 lacks = stats[r] + stats[kTile + r];
-                if (side == 0 && r < q.t.rows) a.delta[q.outer * a.tokens + q.t.row0 + r] += lacks / f;
+                if (side == 0 && r < q.t.rows) a.delta[q.outer * a.tokens + q.t.row0 + r] += lacks * ldexpf(1.0f, -power);
+                lacks *= by1;  // b is P's
             }
             constexpr int kCols = COLUMNS ? DP : DP / 2;  // of a thread
             const int d0 = COLUMNS ? 0 : side * kCols;

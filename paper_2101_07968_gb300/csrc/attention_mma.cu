@@ -24,7 +24,9 @@
 // Rounding: P is rounded to the operands' type for the tensor cores, at most half a step of each
 // term, where y's own rounding is half a step of the sum; l adds the unrounded ones in floats.
 // The reference m is not raised with every larger maximum but once it is 2^8 too low: P up to 256
-// is as good in 16 bits with a floating point, and y in tensor memory is seldom rescaled.
+// is as good in 16 bits with a floating point, and y in tensor memory is seldom rescaled. Halves have few
+// exponents: P and l are held 2^7 times larger, up to 2^15, so that steps below their normal range are 2^-31 of the
+// reference and what a term loses there is 2^-32 of it (without, 16,384 keys behind one that is ahead by 17 were 44 % off).
 //
 // A mask cuts only the block on the diagonal, the tile's last. Values there that are not finite
 // would reach rows that must not see them through 0 * inf. So rows after the sequence's end are overwritten
@@ -44,6 +46,8 @@ constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;
 static_assert(2 * kSoftmaxRegs + 2 * kOtherRegs <= 4 * 128, "registers of the launch");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.0f;  // how far, in powers of two, the reference may be below the maximum
+template <typename T>
+constexpr float kPPower = std::is_same<T, __half>::value ? 7.0f : 0.0f;  // P is held 2^kPPower times larger, and l
 
 struct alignas(16) Item {
     int32_t head[2], row0[2], rows[2], blocks[2];
@@ -392,7 +396,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     if (r < q.rows[x]) put_row(y + d, v, by, a.D - d, wide);
                 }
-                if (r < q.rows[x]) *lse = (m * scale + log2f(l)) * kLn2;
+                if (r < q.rows[x]) *lse = (m * scale + (log2f(l) - kPPower<T>)) * kLn2;
             }
         }
     } else {  // softmax
@@ -462,7 +466,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                 }
                 // nothing but -inf so far: any finite reference will do
-                const float2 minus = twice(m == -INFINITY ? 0.0f : -m * scale), by = twice(scale);
+                const float2 minus = twice(kPPower<T> + (m == -INFINITY ? 0.0f : -m * scale)), by = twice(scale);
                 float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
                 for (int e0 = 0; e0 < kTile; e0 += 32) {
