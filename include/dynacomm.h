@@ -493,8 +493,9 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
  *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dy_i
  * with the sums of dk and dv over every head that reads the key head. 16-bit types run on the tensor
  * cores: P and dS are rounded to the type for their products (each at most half a step of a term; halves
- * in a power of two of their own, so that small gradients keep their digits and a term of P loses no more than 2^-32 of
- * its row's largest forward, 2^-39 backward), everything else is in floats,
+ * in powers of two: dS one of each row's for dq and of each key's for dk, from what that row or key sees, so that small
+ * gradients keep their digits beside large ones; a term of P loses no more than 2^-32 of its row's largest forward,
+ * 2^-39 backward), everything else is in floats,
  * and what y's own rounding does to dy_i . y_i is taken back, since a row of dS sums to zero. Sums on the
  * tensor cores are cut off toward zero where floats would round: by some 2^-24 of their terms' magnitudes for
  * every 16 terms (6e-5 for 16,384 terms of one sign). Floats run on the CUDA cores. What stands in rows of

@@ -16,8 +16,7 @@ struct AttentionTile {
 // The plan's head in the workspace, then its tiles.
 struct AttentionPlan {
     int32_t tiles;
-    uint32_t top_v, top_do;  // largest finite magnitudes (float bits): the scale of halves' gradients
-    int32_t pad[13];
+    int32_t pad[15];
 };
 __host__ __device__ inline const AttentionTile *plan_tiles(const AttentionPlan *p)
 {
@@ -30,6 +29,9 @@ struct AttentionArgs {
     void *y, *dq, *dk, *dv;          // contiguous
     float *lse;                      // [heads][tokens]
     float *delta;                    // [heads][tokens]: sum of dy y
+    // gradient of halves, the powers of two that dS is held in: [heads][tokens] of a row's dq, [kv_heads][tokens] of a
+    // key's dk
+    const int8_t *row_power, *key_power;
     const AttentionPlan *plan;
     int64_t tokens;
     int32_t heads, kv_heads, group, D;

@@ -28,9 +28,9 @@
 // of 64 are bound by the warps: a step of 128 x 128 takes them 1,900 clocks (rows) and 2,500 (columns), the products 1,024.
 //
 // Rounding: P and dS are rounded to the operands' type for the tensor cores, half a step of each
-// term. Halves have few exponents: P, at most 1, is held 2^14 times larger, and dS in a power of two
-// that no |dP - delta| <= 2 D max|dy| max|v| can overflow, known from a pass over dy and v; both are undone
-// in floats at the end. What a mask hides is zero by selection, and operands' rows behind it are
+// term. Halves have few exponents: P, at most 1, is held 2^14 times larger, and dS in a power of
+// two of the lane's own, row or key, that nothing which it may see can overflow (attention_plan.cu); both are
+// undone in floats at the end. What a mask hides is zero by selection, and operands' rows behind it are
 // looked through as in the forward pass.
 #include <cmath>
 
@@ -112,15 +112,6 @@ __device__ __forceinline__ Item<COLUMNS> item_at(const AttentionArgs &a, int64_t
         q.per_head = q.steps = before + 1;
     }
     return q;
-}
-
-// The power of two that dS of halves is held in.
-template <typename T>
-__device__ __forceinline__ int half_power(const AttentionArgs &a)
-{
-    if constexpr (!std::is_same<T, __half>::value) return 0;
-    const float top = 2.0f * float(a.D) * __uint_as_float(a.plan->top_do) * __uint_as_float(a.plan->top_v);
-    return top > 0.0f ? min(max(15 - (ilogbf(top) + 1), -96), 96) : 0;
 }
 
 template <typename T, int DP, bool COLUMNS>
@@ -335,7 +326,6 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         }
     } else if (warp == 10) {
         if (COLUMNS) {  // lse and delta, as the warps use them
-            const float f = ldexpf(1.0f, half_power<T>(a) - kPPower);
             uint32_t n = 0;
             bool ok = true;
             for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
@@ -358,7 +348,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         to[lane + 32 * k] = -l[k] * kLog2e + float(kPPower);
-                        to[kTile + lane + 32 * k] = -d[k] * f;
+                        to[kTile + lane + 32 * k] = -d[k];
                     }
                     __syncwarp();
                     if (lane == 0) bw::bar_arrive(bar(&b.l_full[n % G::kL]));
@@ -398,12 +388,10 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         const int side = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
         const uint32_t at_s = lanes + side * 64, at_dp = at_s + kDp;
-        const int power = half_power<T>(a);
-        const float f = ldexpf(1.0f, power - kPPower), scale = a.scale * kLog2e;
-        const float by0 = a.scale * ldexpf(1.0f, -power), by1 = ldexpf(1.0f, -kPPower);
+        const float scale = a.scale * kLog2e, by1 = ldexpf(1.0f, -kPPower);
         const bool wide = a.D % 8 == 0 && ((reinterpret_cast<uintptr_t>(COLUMNS ? a.dk : a.dq) |
                                             reinterpret_cast<uintptr_t>(COLUMNS ? a.dv : a.dq)) & 15) == 0;
-        const float2 by = twice(scale), fs = twice(f);
+        const float2 by = twice(scale);
         uint32_t n = 0, finished = 0, checks = 0;
         bool ok = true;
         uint32_t meetings = 0;
@@ -430,11 +418,13 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 continue;
             }
             float2 lse = {}, delta = {}, excess = {};  // excess: rows, what dS sums to
+            const int64_t own = q.outer * a.tokens + q.t.row0 + r;  // the lane's row or key
+            const bool there = r < q.t.rows;
+            const int power = kHalf && there ? (COLUMNS ? a.key_power : a.row_power)[own] : 0;
+            const float2 fs = twice(ldexpf(1.0f, power - kPPower));
             if (!COLUMNS) {
-                const int64_t at = q.outer * a.tokens + q.t.row0 + r;
-                const bool there = r < q.t.rows;
-                lse = twice((there ? -a.lse[at] * kLog2e : 0.0f) + float(kPPower));
-                delta = twice(there ? -a.delta[at] * f : 0.0f);
+                lse = twice((there ? -a.lse[own] * kLog2e : 0.0f) + float(kPPower));
+                delta = twice(there ? -a.delta[own] * fs.x : 0.0f);
             }
             Walk w;
             for (int j = 0; j < q.steps; ++j, ++n, w.next(q.per_head)) {
@@ -511,8 +501,18 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         for (int e = 0; e < 32; e += 4) {
                             const float4 minus = COLUMNS ? *reinterpret_cast<const float4 *>(l + kTile + e0 + e)
                                                          : make_float4(delta.x, delta.x, delta.x, delta.x);
-                            float2 t = __ffma2_rn(make_float2(d[e], d[e + 1]), fs, make_float2(minus.x, minus.y));
-                            float2 u = __ffma2_rn(make_float2(d[e + 2], d[e + 3]), fs, make_float2(minus.z, minus.w));
+                            float2 t = make_float2(d[e], d[e + 1]), u = make_float2(d[e + 2], d[e + 3]);
+                            if constexpr (kHalf && !COLUMNS) {  // delta is in the row's scale
+                                t = __ffma2_rn(t, fs, make_float2(minus.x, minus.y));
+                                u = __ffma2_rn(u, fs, make_float2(minus.z, minus.w));
+                            } else {
+                                t = __fadd2_rn(t, make_float2(minus.x, minus.y));
+                                u = __fadd2_rn(u, make_float2(minus.z, minus.w));
+                            }
+                            if constexpr (kHalf && COLUMNS) {  // a lane is a key: one product more, 609 -> 652 us of
+                                t = __fmul2_rn(t, fs);         // columns (16,384 tokens in 2 sequences x 16 x 64)
+                                u = __fmul2_rn(u, fs);
+                            }
                             t = __fmul2_rn(t, make_float2(p[e0 + e], p[e0 + e + 1]));
                             u = __fmul2_rn(u, make_float2(p[e0 + e + 2], p[e0 + e + 3]));
                             if constexpr (decltype(masked)::value) {
@@ -567,13 +567,13 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 meet();
                 if (!ok) break;
                 lacks = stats[r] + stats[kTile + r];
-                if (side == 0 && r < q.t.rows) a.delta[q.outer * a.tokens + q.t.row0 + r] += lacks * ldexpf(1.0f, -power);
+                if (side == 0 && r < q.t.rows) a.delta[own] += lacks * ldexpf(1.0f, -power);
                 lacks *= by1;  // b is P's
             }
             constexpr int kCols = COLUMNS ? DP : DP / 2;  // of a thread
             const int d0 = COLUMNS ? 0 : side * kCols;
             const uint32_t from = lanes + (COLUMNS && side == 0 ? kSum1 : kSum0) + d0;
-            const float by_sum = COLUMNS && side == 0 ? by1 : by0;
+            const float by_sum = COLUMNS && side == 0 ? by1 : a.scale * ldexpf(1.0f, -power);
 #pragma unroll 1
             for (int d = 0; d < kCols; d += 32) {
                 float v[32], b_row[32];

@@ -1,14 +1,18 @@
-"""Attention of halves on the GPU, whose exponents are few: flat tails of long rows, keys of little weight.
+"""Attention of halves on the GPU, whose exponents are few: flat tails of long rows, and gradients beside others that
+are larger by orders of magnitude, in other sequences, heads, later keys and earlier rows.
 
 Bounds. P is held 2^7 times larger forward (2^14 in the gradient): what lies below 2^-14 of that is rounded in steps
-of 2^-24 of it, so a term is off by 2^-32 (2^-39) of the row's largest at most, besides half's rounding u = 2^-11."""
+of 2^-24 of it, so a term is off by 2^-32 (2^-39) of the row's largest at most, besides half's rounding u = 2^-11.
+dS is held in a power of two that follows from what an output may see and nothing else: whatever it may not see leaves
+its bits as they are."""
 import math
 
 import pytest
 import torch
 
+import attention_oracle as ao
 import layer_oracle as lo
-from test_gpu_attention import BF, HF, ly, offs  # noqa: F401
+from test_gpu_attention import BF, HF, both, ly, normal, offs, operands, packed  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 U = lo.UNIT[HF]
@@ -60,3 +64,102 @@ def test_values_of_faint_keys(ly):  # noqa: F811
     dv = ly.attention_grad(dy, q, k, v, y, lse, offs(0, n))[2]
     want = (1000.0 * p.sum()).expand(D)
     lo.assert_within(dv[0, 0], want, want * (U + n * 2.0 ** -22) + 1000.0 * n * 2.0 ** -39, "dv")
+
+
+def gradients(ly, q, k, v, dy, o):  # noqa: F811
+    y, lse = ly.attention(q, k, v, offs(*o))
+    return y, dict(zip(("dq", "dk", "dv"), ly.attention_grad(dy, q, k, v, y, lse, offs(*o))))
+
+
+def small(D=64, H=4, G=2):
+    o = packed(300, 500, 224)
+    q, k, v, dy = operands(17, o[-1], H, G, D, HF)
+    return o, q, k, v, dy * 1e-3
+
+
+@pytest.mark.parametrize("D", [64, 128, 75])
+@pytest.mark.parametrize("big_dy,big_v", [(100.0, 20.0), (1000.0, 60.0), (60000.0, 1.0), (60000.0, 60000.0)])
+def test_large_values_of_another_sequence(ly, D, big_dy, big_v):  # noqa: F811
+    """Finite ones, of the magnitudes that halves hold: no bit of the others' gradients changes, and each
+    sequence's are within the bounds of a call of its own."""
+    o, q, k, v, dy = small(D)
+    _, want = gradients(ly, q, k, v, dy, o)
+    for a, b in ((300, 800), (800, 1024)):
+        v2, dy2 = v.clone(), dy.clone()
+        v2[a:b] = (normal(3, b - a, v.shape[1], D) * big_v).clamp(-6e4, 6e4).half()
+        dy2[a:b] = (normal(4, b - a, q.shape[1], D) * big_dy).clamp(-6e4, 6e4).half()
+        y, got = gradients(ly, q, k, v2, dy2, o)
+        for s, e in zip(o[:-1], o[1:]):
+            if s == a:
+                continue
+            for n in got:
+                assert torch.equal(got[n][s:e], want[n][s:e]), (n, s)
+            own = ao.attention(*(t[s:e].double() for t in (q, k, v)), [0, e - s], D ** -0.5, dy[s:e].double(),
+                               y[s:e].double(), HF)
+            for n in got:
+                lo.assert_within(got[n][s:e], *own[n], n)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("big", [100.0, 6e4])
+def test_large_values_of_another_head(ly, D, big):  # noqa: F811
+    """Key head 1 and the query heads that read it: those of key head 0 keep their bits."""
+    o, q, k, v, dy = small(D)
+    _, want = gradients(ly, q, k, v, dy, o)
+    v[:, 1] = big
+    dy[:, 2:] = big
+    _, got = gradients(ly, q, k, v, dy, o)
+    assert torch.equal(got["dq"][:, :2], want["dq"][:, :2])
+    assert torch.equal(got["dk"][:, 0], want["dk"][:, 0]) and torch.equal(got["dv"][:, 0], want["dv"][:, 0])
+    # a query head alone: the other's dq, which shares its keys
+    dy2 = dy.clone()
+    dy2[:, 0] = big
+    _, one = gradients(ly, q, k, v, dy2, o)
+    assert torch.equal(one["dq"][:, 1], want["dq"][:, 1])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [1, 127, 128, 200, 499])
+@pytest.mark.parametrize("big", [100.0, 6e4])
+def test_large_values_behind_the_mask(ly, D, at, big):  # noqa: F811
+    """Of a later key: earlier rows' dq; of an earlier row: later keys' dk and dv."""
+    o = [0, 500]
+    q, k, v, dy = operands(19, 500, 4, 2, D, HF)
+    dy = dy * 1e-3
+    _, want = gradients(ly, q, k, v, dy, o)
+    v2 = v.clone()
+    v2[at] = big
+    _, got = gradients(ly, q, k, v2, dy, o)
+    assert torch.equal(got["dq"][:at], want["dq"][:at])
+    dy2 = dy.clone()
+    dy2[at] = big
+    _, got = gradients(ly, q, k, v, dy2, o)
+    assert torch.equal(got["dk"][at + 1:], want["dk"][at + 1:]) and torch.equal(got["dv"][at + 1:], want["dv"][at + 1:])
+    # rows apart from it: dq is a row's own
+    other = torch.arange(500, device="cuda") != at
+    assert torch.equal(got["dq"][other], want["dq"][other])
+
+
+@pytest.mark.parametrize("power", [-22, -12, 0, 10])
+@pytest.mark.parametrize("D", [64, 128])
+def test_gradients_of_any_size(ly, D, power):  # noqa: F811
+    """Every row, head and sequence in a magnitude of its own."""
+    o = packed(200, 1, 431)
+    q, k, v, dy = operands(23, o[-1], 4, 2, D, HF, scale=0.8)
+    dy = (dy.float() * torch.exp2(torch.randint(-2, 3, (o[-1], 4, 1), device="cuda") + float(power))).half()
+    y, got = gradients(ly, q, k, v, dy, o)
+    want = ao.attention(*(t.double() for t in (q, k, v)), o, D ** -0.5, dy.double(), y.double(), HF)
+    for n in got:
+        lo.assert_within(got[n], *want[n], n)
+
+
+@pytest.mark.parametrize("zero", ["dy", "v", "both"])
+def test_gradients_of_zeros(ly, zero):  # noqa: F811
+    o, q, k, v, dy = small()
+    if zero != "v":
+        dy.zero_()
+    if zero != "dy":
+        v.zero_()
+    y, got = gradients(ly, q, k, v, dy, o)
+    assert not got["dq"].any() and not got["dk"].any()
+    assert zero == "v" or not got["dv"].any()
