@@ -450,7 +450,7 @@ dc_status dc_block_norm_grad(const dc_block_norm_cfg *cfg, const void *dy, const
  * interleaved is not 0, turns by the angle a = positions[token] base^(-2i / rotary):
  *   out1 = z1 cos a - z2 sin a,  out2 = z2 cos a + z1 sin a
  * The other elements are z. Positions (device, int64) may have any value; the angle's whole
- * turns are dropped in integers, so that far positions lose nothing.
+ * turns are dropped in integers, from frequencies of 128 bits, so that far positions lose nothing.
  * The gradient takes dq_out and dk_out (contiguous) and q and k again, and writes dq, dk
  * (contiguous) and dw_q, dw_k (float [D]; NULL: not wanted). workspace:
  * dc_head_norm_rotary_grad_workspace_bytes(cfg) bytes, used during the call's kernels only.

@@ -5,9 +5,10 @@
 // Gradient: g = dy turned back, dw = sum g n, u = w g, dx = rstd (u - n mean(u n)).
 //
 // Angles. A position times a frequency in turns, modulo one turn, is what counts: the host gives
-// each pair's turns per position as a 64-bit binary fraction, and one 64-bit product, whose
-// overflow drops the whole turns, is exact for positions of any size. Both sines are taken once a
-// token and used for every head of it.
+// each pair's turns per position as a 128-bit binary fraction (turns.cuh), and the upper half of its product with the
+// position, whose overflow drops the whole turns, is good to 2^-48 of a turn for every 64-bit position (64 bits of
+// fraction would be a whole turn off at 2^63). The sines take 32 bits of it. Both are taken once a token and used for
+// every head of it.
 //
 // Both directions are bound by memory: 2 (3) accesses of each element. A group of 8, 16 or 32 lanes
 // takes a head, eight elements a lane as two runs of four: the two halves of four pairs, so that
@@ -27,9 +28,15 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 2;  // heads in a chunk of a group
 
-__device__ __forceinline__ void angle(int64_t position, uint64_t turns, float &c, float &s)
+__device__ __forceinline__ void angle(const HeadNormArgs &a, int64_t position, int pair, float &c, float &s)
 {
-    const uint64_t at = uint64_t(position) * turns;  // of a turn, in units of 2^-64
+    uint64_t at = uint64_t(position) * a.turns[pair];  // of a turn, in units of 2^-64
+    // the lower half counts for less than the 32 bits that are used, but for far positions (a branch that most
+    // tokens do not take: without it 32,768 tokens x 40 heads x 128 take 187 us backward instead of 172)
+    if (position != int64_t(int32_t(position))) {
+        at += __umul64hi(uint64_t(position), a.turns_below[pair]);
+        if (position < 0) at -= a.turns_below[pair];  // as an unsigned number it is 2^64 too large
+    }
     sincospif(float(int32_t(at >> 32)) * 0x1p-31f, &s, &c);
 }
 
@@ -192,8 +199,9 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
         for (int j = 0; j < 2; ++j) {
             float2 c = twice(1.0f), s = twice(0.0f);
             if (turned) {
-                angle(position, a.turns[4 * l + 2 * j], c.x, s.x);
-                angle(position, a.turns[4 * l + 2 * j + 1], c.y, s.y);
+                const int i = 4 * l + 2 * j;
+                angle(a, position, i, c.x, s.x);
+                angle(a, position, i + 1, c.y, s.y);
             }
             const float2 n = make_float2(-s.x, -s.y);
             angles.c[j] = c;  // the gradient's turn back
@@ -333,7 +341,7 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
         for (int j = 0; j < kPairs; ++j) {
             c[j] = 1.0f;
             s[j] = 0.0f;
-            if (lane + 32 * j < half) angle(position, a.turns[lane + 32 * j], c[j], s[j]);
+            if (lane + 32 * j < half) angle(a, position, lane + 32 * j, c[j], s[j]);
         }
         for (int h = q.h0; h < q.h1; ++h) {
             const T *x = static_cast<const T *>(a.x[which]) + q.token * a.token[which] + h * a.head[which];

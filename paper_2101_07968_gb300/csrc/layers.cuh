@@ -176,7 +176,8 @@ struct HeadNormArgs {
     float eps;
     float *partial;           // gradient of the weights: the blocks' sums (nullable)
     int32_t parts[2], per_part[2], blocks[2];  // of a token's heads, the heads of one, the grid (set by the launcher)
-    uint64_t turns[DC_HEAD_NORM_DIM_MAX / 2];  // of pair i per position, in 2^-64 of a turn
+    // of pair i per position: in 2^-64 of a turn, and what is below, in 2^-128
+    uint64_t turns[DC_HEAD_NORM_DIM_MAX / 2], turns_below[DC_HEAD_NORM_DIM_MAX / 2];
 };
 // Few tokens: a token's heads are dealt to `parts` groups, `per_part` each (the last part's fewer, but one at least:
 // copies start at a part's first head), as finely as tokens * parts >= wanted needs, but not finer than `least` heads

@@ -4,6 +4,7 @@
 
 #include "attention.cuh"
 #include "blackwell.cuh"
+#include "turns.cuh"
 
 namespace dc {
 
@@ -161,10 +162,7 @@ HeadNormArgs head_norm_args(const dc_head_norm_cfg *c)
     a.interleaved = c->interleaved != 0;
     a.norm = c->norm != 0;
     a.eps = float(c->eps);
-    for (int i = 0; i < c->rotary / 2; ++i) {
-        const double turns = std::pow(c->base, -2.0 * i / c->rotary) * 0.15915494309189533577;  // 1 / (2 pi)
-        a.turns[i] = uint64_t((turns - std::floor(turns)) * 18446744073709551616.0);
-    }
+    rotary_turns(c->base, c->rotary / 2, a.turns, a.turns_below);
     return a;
 }
 
