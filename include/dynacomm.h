@@ -564,7 +564,7 @@ dc_status dc_roof_int_probe(int32_t variant, int32_t blocks, int32_t threads, in
                             uint32_t *sink, cudaStream_t stream);
 
 /* ------------------------------------------------------------------------
- * dc_wait_probe -- test support: one small block in which two threads wait, as the layer
+ * dc_wait_probe -- test support: one small block in which four threads wait, as the layer
  * operators' kernels do, for copies that nothing has started. The waits run out within some
  * two seconds, and the kernel ends and sets status (device) to DC_ERR_INTERNAL as theirs do.
  * ---------------------------------------------------------------------- */

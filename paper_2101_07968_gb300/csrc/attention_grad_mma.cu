@@ -131,6 +131,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             l_free[G::kL], s_full, p_full, dp_full, ds_full, sums_full, met, last,
             look[kChecks], x_checked[kChecks], y_checked[kChecks];
         uint32_t tmem_at, gave_up;
+        uint32_t progress;  // blocks done: an item takes as long as its rows are many, and so do some waits
         // the check, counted from one, if the sums with its block of X (Y) are done by hand
         uint32_t x_by_hand[kChecks], y_by_hand[kChecks];
     };
@@ -142,6 +143,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     auto bar = [](uint64_t *p) { return bw::smem_addr(p); };
     const uint32_t base = bw::smem_addr(dyn), ring_x = base + 2 * kBytes, ring_y = ring_x + G::kX * kBytes;
     uint32_t *const gave_up = &b.gave_up;
+    volatile uint32_t *const progress = &b.progress;
 
     if (threadIdx.x == 0) {
         bw::bar_init(bar(&b.still_full), 1);
@@ -171,7 +173,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             bw::bar_init(bar(&b.y_checked[i]), 1);
             b.x_by_hand[i] = b.y_by_hand[i] = 0;
         }
-        b.gave_up = 0;
+        b.gave_up = b.progress = 0;
         bw::bar_init_fence();
     }
     if (warp == 9) bw::tmem_alloc1(bw::smem_addr(&b.tmem_at), 512);
@@ -221,7 +223,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     }
                 }
                 if (q.steps == 0) continue;
-                ok = done == 0 || bw::bar_wait(bar(&b.still_free), (done - 1) & 1, gave_up);
+                ok = done == 0 || bw::bar_wait(bar(&b.still_free), (done - 1) & 1, gave_up, progress);
                 if (!ok) break;
                 ++done;
                 bw::bar_arrive_bytes(bar(&b.still_full), 2 * kBytes);
@@ -232,12 +234,12 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     const Step s = q.step(w);
                     const int head = COLUMNS ? s.head : q.kv;
                     const uint32_t x = nx % G::kX, y = ny % G::kY;
-                    ok = nx < G::kX || bw::bar_wait(bar(&b.x_free[x]), (nx / G::kX - 1) & 1, gave_up);
+                    ok = nx < G::kX || bw::bar_wait(bar(&b.x_free[x]), (nx / G::kX - 1) & 1, gave_up, progress);
                     if (!ok) break;
                     bw::bar_arrive_bytes(bar(&b.x_full[x]), kBytes);
                     tile(ring_x + x * kBytes, COLUMNS ? map_q : map_k, head, s.c0, bar(&b.x_full[x]));
                     ++nx;
-                    ok = ny < G::kY || bw::bar_wait(bar(&b.y_free[y]), (ny / G::kY - 1) & 1, gave_up);
+                    ok = ny < G::kY || bw::bar_wait(bar(&b.y_free[y]), (ny / G::kY - 1) & 1, gave_up, progress);
                     if (!ok) break;
                     bw::bar_arrive_bytes(bar(&b.y_full[y]), kBytes);
                     tile(ring_y + y * kBytes, COLUMNS ? map_dy : map_v, head, s.c0, bar(&b.y_full[y]));
@@ -255,8 +257,12 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             int done = 0;
             uint32_t n = 0;  // blocks so far
             bool ok = true;
-            auto x_there = [&](uint32_t m) { return ok = ok && bw::bar_wait(bar(&b.x_full[m % G::kX]), (m / G::kX) & 1, gave_up); };
-            auto y_there = [&](uint32_t m) { return ok = ok && bw::bar_wait(bar(&b.y_full[m % G::kY]), (m / G::kY) & 1, gave_up); };
+            auto x_there = [&](uint32_t m) {
+                return ok = ok && bw::bar_wait(bar(&b.x_full[m % G::kX]), (m / G::kX) & 1, gave_up, progress);
+            };
+            auto y_there = [&](uint32_t m) {
+                return ok = ok && bw::bar_wait(bar(&b.y_full[m % G::kY]), (m / G::kY) & 1, gave_up, progress);
+            };
             auto scores = [&](uint32_t d, uint32_t still, uint32_t moving) {
                 const uint64_t da = bw::operand(still, 16), db = bw::operand(moving, 16);
                 bw::fence_after();
@@ -283,7 +289,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     if (i >= 0) next = item_at<COLUMNS>(a, i);
                     continue;
                 }
-                ok = bw::bar_wait(bar(&b.still_full), done & 1, gave_up);
+                ok = bw::bar_wait(bar(&b.still_full), done & 1, gave_up, progress);
                 ++done;
                 auto first = [&](uint32_t m) {  // S of block m
                     if (!x_there(m)) return;
@@ -303,18 +309,19 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 Walk w;
                 for (int j = 0; j < q.steps && ok; ++j, ++n, w.next(q.per_head)) {
                     const Step s = q.step(w);
-                    ok = bw::bar_wait(bar(&b.p_full), n & 1, gave_up);
+                    ok = bw::bar_wait(bar(&b.p_full), n & 1, gave_up, progress);
                     if (!ok) break;
                     bw::fence_after();
                     if (!s.diagonal || !by_hand(COLUMNS ? b.y_by_hand : b.x_by_hand, checks))
                         sums(kSum1, 0, COLUMNS ? ring_y + n % G::kY * kBytes : ring_x + n % G::kX * kBytes, j > 0);
                     if (COLUMNS) bw::commit1(bar(&b.y_free[n % G::kY]));
                     if (j + 1 < q.steps) first(n + 1);
-                    ok = ok && bw::bar_wait(bar(&b.ds_full), n & 1, gave_up);
+                    ok = ok && bw::bar_wait(bar(&b.ds_full), n & 1, gave_up, progress);
                     if (!ok) break;
                     bw::fence_after();
                     if (!s.diagonal || !by_hand(b.x_by_hand, checks)) sums(kSum0, kDp, ring_x + n % G::kX * kBytes, j > 0);
                     checks += s.cut;
+                    *progress = n + 1;
                     bw::commit1(bar(&b.x_free[n % G::kX]));
                     if (j + 1 < q.steps) second(n + 1, j + 2 == q.steps);
                 }
@@ -322,7 +329,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             }
             // arrivals land in this CTA's memory: it may not end before the last
             bw::commit1(bar(&b.last));
-            bw::bar_wait(bar(&b.last), 0, gave_up);
+            bw::bar_wait(bar(&b.last), 0, gave_up, progress);
         }
     } else if (warp == 10) {
         if (COLUMNS) {  // lse and delta, as the warps use them
@@ -341,7 +348,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         l[k] = c < s.count ? a.lse[at + c] : 0.0f;
                         d[k] = c < s.count ? a.delta[at + c] : 0.0f;
                     }
-                    ok = n < G::kL || bw::bar_wait(bar(&b.l_free[n % G::kL]), (n / G::kL - 1) & 1, gave_up);
+                    ok = n < G::kL || bw::bar_wait(bar(&b.l_free[n % G::kL]), (n / G::kL - 1) & 1, gave_up, progress);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     float *to = stats + n % G::kL * 2 * kTile;
@@ -365,12 +372,12 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 const Step s = q.step(w);
                 if (!s.cut) continue;
                 const uint32_t at = checks % kChecks;
-                ok = bw::bar_wait(bar(&b.look[at]), (checks / kChecks) & 1, gave_up);
+                ok = bw::bar_wait(bar(&b.look[at]), (checks / kChecks) & 1, gave_up, progress);
                 // rows behind the mask: of Y where it is summed too, and of X
                 for (int of_x = COLUMNS ? 0 : 1; of_x < 2; ++of_x) {
                     const uint32_t stage = of_x ? n % G::kX : n % G::kY, phase = of_x ? n / G::kX : n / G::kY;
                     ok = __all_sync(0xffffffffu, ok && bw::bar_wait(bar(of_x ? &b.x_full[stage] : &b.y_full[stage]), phase & 1,
-                                                                     gave_up));
+                                                                     gave_up, progress));
                     if (!ok) break;
                     unsigned char *const tile = dyn + (2 + (of_x ? 0 : G::kX) + stage) * kBytes;
                     bool bad = false;
@@ -399,7 +406,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             bw::fence_before();
             __syncwarp();
             if (lane == 0) bw::bar_arrive(bar(&b.met));
-            ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.met), meetings++ & 1, gave_up) && ok);
+            ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.met), meetings++ & 1, gave_up, progress) && ok);
             bw::fence_after();
         };
         for (int64_t round = 0, i; ok && (i = dealt(round, items)) >= 0; ++round) {
@@ -430,8 +437,8 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             for (int j = 0; j < q.steps; ++j, ++n, w.next(q.per_head)) {
                 const Step s = q.step(w);
                 const float *const l = stats + n % G::kL * 2 * kTile + side * 64;
-                ok = bw::bar_wait(bar(&b.s_full), n & 1, gave_up);
-                if (COLUMNS) ok = ok && bw::bar_wait(bar(&b.l_full[n % G::kL]), (n / G::kL) & 1, gave_up);
+                ok = bw::bar_wait(bar(&b.s_full), n & 1, gave_up, progress);
+                if (COLUMNS) ok = ok && bw::bar_wait(bar(&b.l_full[n % G::kL]), (n / G::kL) & 1, gave_up, progress);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 bw::fence_after();
@@ -473,7 +480,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 bool hand = false;
                 if (cut) {
                     ok = __all_sync(0xffffffffu, bw::bar_wait(bar(COLUMNS ? &b.y_checked[at] : &b.x_checked[at]), check_phase,
-                                                              gave_up));
+                                                              gave_up, progress));
                     if (!ok) break;
                     hand = s.diagonal && by_hand(COLUMNS ? b.y_by_hand : b.x_by_hand, checks);
                     if (hand) {
@@ -488,7 +495,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 bw::fence_before();
                 __syncwarp();
                 if (lane == 0) bw::bar_arrive(bar(&b.p_full));
-                ok = __all_sync(0xffffffffu, ok && bw::bar_wait(bar(&b.dp_full), n & 1, gave_up));
+                ok = __all_sync(0xffffffffu, ok && bw::bar_wait(bar(&b.dp_full), n & 1, gave_up, progress));
                 if (!ok) break;
                 bw::fence_after();
                 auto make_ds = [&](auto masked) {
@@ -534,7 +541,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 bw::tmem_stored();
                 if (cut) {
                     if (COLUMNS) {  // X too
-                        ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.x_checked[at]), check_phase, gave_up));
+                        ok = __all_sync(0xffffffffu, bw::bar_wait(bar(&b.x_checked[at]), check_phase, gave_up, progress));
                         if (!ok) break;
                         hand = s.diagonal && by_hand(b.x_by_hand, checks);
                     }
@@ -555,7 +562,7 @@ attention_grad_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                     bw::bar_arrive(bar(&b.ds_full));
                 }
             }
-            ok = ok && bw::bar_wait(bar(&b.sums_full), finished & 1, gave_up);
+            ok = ok && bw::bar_wait(bar(&b.sums_full), finished & 1, gave_up, progress);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             ++finished;

@@ -115,6 +115,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     struct Shared {
         uint64_t q_full[kQ], q_free[kQ], full[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], y_full[2],
             y_free[2], l_full[2], look[kChecks], checked[kChecks], item_full[kItems], item_free[kItems], last;
+        uint64_t until;  // when waits end, set anew with every copy: an item takes as long as its keys are many
         uint32_t tmem_at, gave_up;
         uint32_t by_hand[kChecks];  // the check, counted from one, if its block's sums are done by hand
         float row_l[2][kTile], row_m[2][kTile];  // of finished tiles
@@ -123,6 +124,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     static_assert(sizeof(Shared) <= kSharedBytes, "room behind the tiles");
     Shared &h = *reinterpret_cast<Shared *>(dyn + (kQ + kStages) * kBytes);
     uint32_t *const gave_up = &h.gave_up;
+    volatile uint64_t *const until = &h.until;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto bar = [](uint64_t *b) { return bw::smem_addr(b); };
@@ -168,6 +170,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         bw::prefetch_map(&map_v);
     }
     pdl_wait();  // the list and the copies are there
+    if (threadIdx.x == 0) bw::wait_on(until);
     bw::fence_before();
     __syncthreads();
     bw::fence_after();
@@ -177,13 +180,13 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if ((base & 1023u) && threadIdx.x == 0) h.gave_up = 1;
     // Item n of this CTA, by a thread or by a whole warp; false: there is none (or a wait was given up).
     auto item_of_thread = [&](uint32_t n, Item &q) {
-        if (!bw::bar_wait_inline(bar(&h.item_full[n % kItems]), (n / kItems) & 1, gave_up)) return false;
+        if (!bw::bar_wait_inline(bar(&h.item_full[n % kItems]), (n / kItems) & 1, gave_up, until)) return false;
         q = h.items[n % kItems];
         bw::bar_arrive(bar(&h.item_free[n % kItems]));
         return !q.last;
     };
     auto item_of_warp = [&](uint32_t n, Item &q) {
-        const bool ok = bw::bar_wait_inline(bar(&h.item_full[n % kItems]), (n / kItems) & 1, gave_up);
+        const bool ok = bw::bar_wait_inline(bar(&h.item_full[n % kItems]), (n / kItems) & 1, gave_up, until);
         if (!__all_sync(0xffffffffu, ok)) return false;
         q = h.items[n % kItems];
         __syncwarp();
@@ -199,8 +202,9 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 uint32_t phase = 1, tiles = 0;  // of queries so far
                 bool ok = true;
                 auto block = [&](const CUtensorMap &map, int head, int row) {
-                    ok = ok && bw::bar_wait_inline(bar(&h.empty[s]), phase, gave_up);
+                    ok = ok && bw::bar_wait_inline(bar(&h.empty[s]), phase, gave_up, until);
                     if (!ok) return;
+                    bw::wait_on(until);
                     bw::bar_arrive_bytes(bar(&h.full[s]), kBytes);
                     for (int i = 0; i < kBoxes; ++i)
                         bw::copy_3d1(ring + s * kBytes + i * kBox, &map, 64 * i, head, row, bar(&h.full[s]));
@@ -212,10 +216,12 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 uint32_t checks = 0;
                 Item q;
                 for (uint32_t item = 0; ok && item_of_thread(item, q); ++item) {
+                    bw::wait_on(until);
                     for (int x = 0; x < 2; ++x) {
                         if (q.blocks[x] == 0) continue;
                         const uint32_t at = tiles % kQ;
-                        ok = ok && (tiles < kQ || bw::bar_wait_inline(bar(&h.q_free[at]), (tiles / kQ - 1) & 1, gave_up));
+                        ok = ok && (tiles < kQ ||
+                                    bw::bar_wait_inline(bar(&h.q_free[at]), (tiles / kQ - 1) & 1, gave_up, until));
                         if (!ok) break;
                         ++tiles;
                         bw::bar_arrive_bytes(bar(&h.q_full[at]), kBytes);
@@ -245,7 +251,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 uint32_t at[2] = {0, 0};  // where the tiles' queries are
                 bool ok = true;
                 auto have = [&](uint32_t n) {
-                    ok = ok && bw::bar_wait_inline(bar(&h.full[n % kStages]), (n / kStages) & 1, gave_up);
+                    ok = ok && bw::bar_wait_inline(bar(&h.full[n % kStages]), (n / kStages) & 1, gave_up, until);
                     return ok;
                 };
                 auto scores = [&](int x, uint32_t n) {
@@ -263,7 +269,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (q.blocks[x] == 0) continue;
                         at[x] = tiles % kQ;
-                        ok = bw::bar_wait_inline(bar(&h.q_full[at[x]]), (tiles / kQ) & 1, gave_up);
+                        ok = bw::bar_wait_inline(bar(&h.q_full[at[x]]), (tiles / kQ) & 1, gave_up, until);
                         ++tiles;
                         if (!have(c)) break;
                         scores(x, c);
@@ -284,14 +290,15 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                                                   j > 0 || i > 0);
                             };
                             // the rows before these have left
-                            ok = j > 0 || items_of[x]++ == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), items_of[x] & 1, gave_up);
-                            ok = ok && bw::bar_wait_inline(bar(&h.p_half[x]), blocks[x] & 1, gave_up);
+                            ok = j > 0 || items_of[x]++ == 0 ||
+                                 bw::bar_wait_inline(bar(&h.y_free[x]), items_of[x] & 1, gave_up, until);
+                            ok = ok && bw::bar_wait_inline(bar(&h.p_half[x]), blocks[x] & 1, gave_up, until);
                             if (!ok) break;
                             bw::fence_after();
                             // (known before the first half is handed over)
                             const bool own = j + 1 < q.blocks[x] || !is_by_hand(checks + (PAIR ? 0 : x));
                             if (own) half(0);
-                            ok = bw::bar_wait_inline(bar(&h.p_full[x]), blocks[x]++ & 1, gave_up);
+                            ok = bw::bar_wait_inline(bar(&h.p_full[x]), blocks[x]++ & 1, gave_up, until);
                             if (!ok) break;
                             bw::fence_after();
                             if (own) half(kTile / 32);
@@ -312,7 +319,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
                 // arrivals land in this CTA's memory: it may not end before the last
                 bw::commit1(bar(&h.last));
-                bw::bar_wait_inline(bar(&h.last), 0, gave_up);
+                bw::bar_wait_inline(bar(&h.last), 0, gave_up, until);
             }
         } else if (warp == 14) {  // values on the diagonal
             uint32_t c = 0, checks = 0;
@@ -322,8 +329,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const uint32_t n = checks_of<PAIR>(q);
                 for (uint32_t x = 0; x < n; ++x, ++checks) {
                     const uint32_t v = c + 2 * q.blocks[x] - 1;
-                    ok = bw::bar_wait_idle(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up) &&
-                         bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up);
+                    ok = bw::bar_wait_idle(bar(&h.look[checks % kChecks]), (checks / kChecks) & 1, gave_up, until) &&
+                         bw::bar_wait_inline(bar(&h.full[v % kStages]), (v / kStages) & 1, gave_up, until);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     unsigned char *tile = dyn + (kQ + v % kStages) * kBytes;
@@ -346,7 +353,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     q.last = true;
                     if (i >= 0) q = item_at<PAIR>(a, i);
                     more = !q.last;
-                    ok = round < kItems || bw::bar_wait_idle(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up);
+                    ok = round < kItems || bw::bar_wait_idle(bar(&h.item_free[at]), uint32_t(round / kItems - 1) & 1, gave_up,
+                                                             until);
                     if (!ok) break;
                     h.items[at] = q;
                     bw::bar_arrive(bar(&h.item_full[at]));
@@ -378,8 +386,8 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     continue;
                 }
                 const uint32_t phase = done[x]++ & 1;
-                ok = ok && bw::bar_wait_inline(bar(&h.l_full[x]), phase, gave_up) &&
-                     bw::bar_wait_inline(bar(&h.y_full[x]), phase, gave_up);
+                ok = ok && bw::bar_wait_inline(bar(&h.l_full[x]), phase, gave_up, until) &&
+                     bw::bar_wait_inline(bar(&h.y_full[x]), phase, gave_up, until);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 bw::fence_after();
@@ -418,7 +426,7 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (lane == 0) bw::bar_arrive(bar(&to[x]));
             };
             for (int j = 0; j < n; ++j) {
-                ok = __all_sync(0xffffffffu, bw::bar_wait_inline(bar(&h.s_full[x]), blocks++ & 1, gave_up));
+                ok = __all_sync(0xffffffffu, bw::bar_wait_inline(bar(&h.s_full[x]), blocks++ & 1, gave_up, until));
                 if (!ok) break;
                 bw::fence_after();
                 float s[kTile];
@@ -488,9 +496,9 @@ attention_mma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (diagonal) {
                     bw::tmem_stored();
                     const uint32_t check = checks + (PAIR ? 0 : x), v = c + 2 * j + 1;
-                    ok = bw::bar_wait_inline(bar(&h.checked[check % kChecks]), (check / kChecks) & 1, gave_up);
+                    ok = bw::bar_wait_inline(bar(&h.checked[check % kChecks]), (check / kChecks) & 1, gave_up, until);
                     // y, l and m of the rows before have been read
-                    ok = ok && (done == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), (done - 1) & 1, gave_up));
+                    ok = ok && (done == 0 || bw::bar_wait_inline(bar(&h.y_free[x]), (done - 1) & 1, gave_up, until));
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     h.row_l[x][r] = l;

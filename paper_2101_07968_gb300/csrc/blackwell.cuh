@@ -134,28 +134,30 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         if (bar_try(bar, parity)) return true;
     return bar_wait_long(bar, parity, gave_up, progress);
 }
-// The same for a thread whose work is seldom and early: it sleeps between tries and leaves its issue slots to others.
-__device__ __forceinline__ bool bar_wait_idle(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+// A wait that ends once the time is past `until`, a word of the CTA's that a thread sets anew (wait_on) as its work goes
+// on: what one waits for may take any number of blocks. Without a call.
+__device__ __forceinline__ void wait_on(volatile uint64_t *until) { *until = now_ns() + kWaitNs; }
+__device__ __forceinline__ bool bar_wait_inline(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up,
+                                                volatile uint64_t *until)
 {
-    const uint64_t start = now_ns();
+    if (bar_try(bar, parity)) return true;
 #pragma unroll 1
-    for (uint32_t i = 0; i < kWaitTries; ++i) {
+    for (uint32_t i = 1;; ++i) {
         if (bar_try(bar, parity)) return true;
-        __nanosleep(100);
-        if ((i & 63u) == 63u && (*gave_up || now_ns() - start > kWaitNs)) break;
+        if ((i & 63u) == 0 && (*gave_up || now_ns() > *until)) break;
     }
     *gave_up = 1u;
     return false;
 }
-// The same without a call.
-__device__ __forceinline__ bool bar_wait_inline(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+// The same for a thread whose work is seldom and early: it sleeps between tries and leaves its issue slots to others.
+__device__ __forceinline__ bool bar_wait_idle(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up,
+                                              volatile uint64_t *until)
 {
-    if (bar_try(bar, parity)) return true;
-    const uint64_t start = now_ns();
 #pragma unroll 1
-    for (uint32_t i = 1; i < kWaitTries; ++i) {
+    for (uint32_t i = 1;; ++i) {
         if (bar_try(bar, parity)) return true;
-        if ((i & 63u) == 0 && (*gave_up || now_ns() - start > kWaitNs)) break;
+        __nanosleep(100);
+        if ((i & 63u) == 0 && (*gave_up || now_ns() > *until)) break;
     }
     *gave_up = 1u;
     return false;

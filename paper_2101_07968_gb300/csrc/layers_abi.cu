@@ -203,19 +203,26 @@ AttentionArgs attention_args(const dc_attention_shape *s, const void *q, const v
     return a;
 }
 
-// Both warps' waits end: the first to run out makes the other give up.
+// Every warp's wait ends, each kind of them: the first to run out makes the others give up.
 __global__ void wait_probe_kernel(int32_t *status)
 {
-    __shared__ alignas(8) uint64_t bars[2];
+    __shared__ alignas(8) uint64_t bars[4], until;
     __shared__ uint32_t gave_up;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) bw::bar_init(bw::smem_addr(&bars[i]), 1);
+        for (int i = 0; i < 4; ++i) bw::bar_init(bw::smem_addr(&bars[i]), 1);
         gave_up = 0;
+        bw::wait_on(&until);
         bw::bar_init_fence();
     }
     __syncthreads();
     bool arrived = false;
-    if (threadIdx.x % 32 == 0) arrived = bw::bar_wait(bw::smem_addr(&bars[threadIdx.x / 32]), 0, &gave_up);
+    const int warp = threadIdx.x / 32;
+    if (threadIdx.x % 32 == 0) {
+        const uint32_t bar = bw::smem_addr(&bars[warp]);
+        arrived = warp == 3   ? bw::bar_wait_idle(bar, 0, &gave_up, &until)
+                  : warp == 2 ? bw::bar_wait_inline(bar, 0, &gave_up, &until)
+                              : bw::bar_wait(bar, 0, &gave_up);
+    }
     const bool any = __syncthreads_or(arrived);
     if (threadIdx.x == 0 && gave_up && !any) *status = DC_ERR_INTERNAL;
 }
@@ -485,7 +492,7 @@ dc_status dc_wait_probe(int32_t *status, cudaStream_t stream)
 {
     const dc::NvtxRange nvtx("dc_wait_probe");
     if (!status) return DC_ERR_NULL;
-    dc::wait_probe_kernel<<<1, 64, 0, stream>>>(status);
+    dc::wait_probe_kernel<<<1, 128, 0, stream>>>(status);
     return dc::result(cudaGetLastError());
 }
 
