@@ -508,8 +508,8 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
  * needed; dy of no account for grad 0). status (device, nullable): as for the expert products.
  * Errors: DC_ERR_NULL; DC_ERR_BAD_LAYER (dtype; tokens outside [0, DC_ATTENTION_TOKENS_MAX]; sequences outside
  * [0, DC_SEQUENCES_MAX]; heads or kv_heads outside [1, DC_HEADS_MAX]; heads not a multiple of
- * kv_heads; D outside [1, DC_ATTENTION_DIM_MAX]; a scale that is not finite (twice it, as a float); heads that
- * overlap, or strides above 2^37); DC_ERR_WORKSPACE; DC_ERR_CUDA.
+ * kv_heads; (tokens / 64 + 1) heads / kv_heads above 2^31 - 1; D outside [1, DC_ATTENTION_DIM_MAX]; a scale that is
+ * not finite (twice it, as a float); heads that overlap, or strides above 2^37); DC_ERR_WORKSPACE; DC_ERR_CUDA.
  * ---------------------------------------------------------------------- */
 #define DC_ATTENTION_DIM_MAX 128
 #define DC_SEQUENCES_MAX 1048576

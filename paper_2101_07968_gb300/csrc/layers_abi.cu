@@ -169,10 +169,11 @@ HeadNormArgs head_norm_args(const dc_head_norm_cfg *c)
 dc_status check_attention(const dc_attention_shape *s)
 {
     if (!s) return DC_ERR_NULL;
-    // tiles' ends and scaled scores stay in range
+    // tiles' ends, scaled scores and an item's steps (a group's heads, each over a sequence) stay in range
     const bool ok = dtype_ok(s->dtype) && s->tokens >= 0 && s->tokens <= DC_ATTENTION_TOKENS_MAX && s->sequences >= 0 &&
                     s->sequences <= DC_SEQUENCES_MAX && count_ok(s->heads) && count_ok(s->kv_heads) &&
-                    s->heads % s->kv_heads == 0 && s->D >= 1 && s->D <= DC_ATTENTION_DIM_MAX &&
+                    s->heads % s->kv_heads == 0 &&
+                    (s->tokens / kSimtRows + 1) * (s->heads / s->kv_heads) <= INT32_MAX && s->D >= 1 && s->D <= DC_ATTENTION_DIM_MAX &&
                     std::isfinite(2.0f * float(s->scale)) && heads_ok(s->q_token, s->q_head, s->heads, s->D, s->tokens) &&
                     heads_ok(s->k_token, s->k_head, s->kv_heads, s->D, s->tokens) &&
                     heads_ok(s->v_token, s->v_head, s->kv_heads, s->D, s->tokens);
