@@ -7,8 +7,8 @@
 
 namespace dc {
 
-// `rows` rows from row0 on, tile `at` of `of` of a sequence that starts at row `first` and ends
-// before `end`. first < 0: rows of no sequence, whose outputs are zeros.
+// `rows` rows from row0 on, of a sequence that starts at row `first` and ends before `end`. first < 0: rows of no
+// sequence, whose outputs are zeros.
 struct AttentionTile {
     int32_t row0, rows, first, end;
 };
