@@ -28,14 +28,18 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 2;  // heads in a chunk of a group
 
-__device__ __forceinline__ void angle(const HeadNormArgs &a, int64_t position, int pair, float &c, float &s)
+template <int N>
+__device__ __forceinline__ void angle(const Turns<N> &turns, int64_t position, int pair, float &c, float &s)
 {
-    uint64_t at = uint64_t(position) * a.turns[pair];  // of a turn, in units of 2^-64
+    uint64_t at = uint64_t(position) * turns.upper[pair];  // of a turn, in units of 2^-64
     // the lower half counts for less than the 32 bits that are used, but for far positions (a branch that most
     // tokens do not take: without it 32,768 tokens x 40 heads x 128 take 187 us backward instead of 172)
     if (position != int64_t(int32_t(position))) {
-        at += __umul64hi(uint64_t(position), a.turns_below[pair]);
-        if (position < 0) at -= a.turns_below[pair];  // as an unsigned number it is 2^64 too large
+        int p;  // (the lower half is not to be read ahead of the branch)
+        asm volatile("mov.u32 %0, %1;" : "=r"(p) : "r"(pair));
+        const uint64_t below = turns.below[p];
+        at += __umul64hi(uint64_t(position), below);
+        if (position < 0) at -= below;  // as an unsigned number it is 2^64 too large
     }
     sincospif(float(int32_t(at >> 32)) * 0x1p-31f, &s, &c);
 }
@@ -108,7 +112,7 @@ constexpr int kRing = GRAD && sizeof(T) == 4 ? 3 : 4;
 // PLAIN: every lane of a group has elements, all of them turn, and the halves of pairs are apart, which
 // most heads are: no branch between the heads of a chunk, so that their instructions mix.
 template <typename T, int LANES, bool GRAD, bool PLAIN>
-__global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel(const __grid_constant__ HeadNormArgs a)
+__global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Turns<LANES * 4> turns)
 {
     constexpr int kGroups = 32 / LANES;
     constexpr int kRuns = kUnroll * 2 * (GRAD ? 2 : 1), kAhead = kRing<T, GRAD>;
@@ -200,8 +204,8 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
             float2 c = twice(1.0f), s = twice(0.0f);
             if (turned) {
                 const int i = 4 * l + 2 * j;
-                angle(a, position, i, c.x, s.x);
-                angle(a, position, i + 1, c.y, s.y);
+                angle(turns, position, i, c.x, s.x);
+                angle(turns, position, i + 1, c.y, s.y);
             }
             const float2 n = make_float2(-s.x, -s.y);
             angles.c[j] = c;  // the gradient's turn back
@@ -313,8 +317,9 @@ __global__ void __launch_bounds__(kThreads, kResident<T, GRAD>) head_norm_kernel
 
 // Sizes and strides of any kind: a warp per head, four pairs a lane, one element an access. Pairs
 // from rotary / 2 on are neighbours that do not turn; the last may be a single element.
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_constant__ HeadNormArgs a)
+template <typename T, bool GRAD, int N>
+__global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_constant__ HeadNormArgs a,
+                                                                 const __grid_constant__ Turns<N> turns)
 {
     constexpr int kPairs = DC_HEAD_NORM_DIM_MAX / 2 / 32;
     const int lane = threadIdx.x % 32, half = a.rotary / 2;
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(kThreads) head_norm_any_kernel(const __grid_co
         for (int j = 0; j < kPairs; ++j) {
             c[j] = 1.0f;
             s[j] = 0.0f;
-            if (lane + 32 * j < half) angle(a, position, lane + 32 * j, c[j], s[j]);
+            if (lane + 32 * j < half) angle(turns, position, lane + 32 * j, c[j], s[j]);
         }
         for (int h = q.h0; h < q.h1; ++h) {
             const T *x = static_cast<const T *>(a.x[which]) + q.token * a.token[which] + h * a.head[which];
@@ -447,7 +452,7 @@ weight_sums_kernel(const float *partial, int q_blocks, int k_blocks, int D, floa
 constexpr int kMostBlocks = 4 * 160;  // rows that the weights' gradients may have
 
 template <typename T, int LANES, bool GRAD, bool PLAIN>
-cudaError_t launch_runs(const HeadNormArgs &a, cudaStream_t stream)
+cudaError_t launch_runs(const HeadNormArgs &a, const AllTurns &turns, cudaStream_t stream)
 {
     constexpr int smem = kWarps * kRing<T, GRAD> * kUnroll * 2 * (GRAD ? 2 : 1) * 32 * int(sizeof(Vec<T, 4>));
     auto kernel = head_norm_kernel<T, LANES, GRAD, PLAIN>;
@@ -458,12 +463,12 @@ cudaError_t launch_runs(const HeadNormArgs &a, cudaStream_t stream)
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     });
     if (e != cudaSuccess) return e;
-    kernel<<<a.blocks[0] + a.blocks[1], kThreads, smem, stream>>>(a);
+    kernel<<<a.blocks[0] + a.blocks[1], kThreads, smem, stream>>>(a, first_turns<LANES * 4>(turns));
     return cudaGetLastError();
 }
 
 template <typename T, bool GRAD>
-cudaError_t launch(HeadNormArgs a, bool runs, cudaStream_t stream)
+cudaError_t launch(HeadNormArgs a, const AllTurns &turns, bool runs, cudaStream_t stream)
 {
     int sms = 0;
     cudaError_t e = sm_count(sms);
@@ -492,14 +497,18 @@ cudaError_t launch(HeadNormArgs a, bool runs, cudaStream_t stream)
     a.blocks[0] = int(blocks[0]);
     a.blocks[1] = int(blocks[1]);
     if (!runs) {
-        head_norm_any_kernel<T, GRAD><<<a.blocks[0] + a.blocks[1], kThreads, 0, stream>>>(a);
+        const int grid = a.blocks[0] + a.blocks[1];
+        if (a.rotary <= 128)
+            head_norm_any_kernel<T, GRAD, 64><<<grid, kThreads, 0, stream>>>(a, first_turns<64>(turns));
+        else
+            head_norm_any_kernel<T, GRAD, 128><<<grid, kThreads, 0, stream>>>(a, turns);
         e = cudaGetLastError();
     } else {
         auto go = [&](auto plain) {
             constexpr bool kPlain = decltype(plain)::value;
-            return lanes == 8    ? launch_runs<T, 8, GRAD, kPlain>(a, stream)
-                   : lanes == 16 ? launch_runs<T, 16, GRAD, kPlain>(a, stream)
-                                 : launch_runs<T, 32, GRAD, kPlain>(a, stream);
+            return lanes == 8    ? launch_runs<T, 8, GRAD, kPlain>(a, turns, stream)
+                   : lanes == 16 ? launch_runs<T, 16, GRAD, kPlain>(a, turns, stream)
+                                 : launch_runs<T, 32, GRAD, kPlain>(a, turns, stream);
         };
         e = a.D == 8 * lanes && a.rotary == a.D && !a.interleaved ? go(std::true_type()) : go(std::false_type());
     }
@@ -525,14 +534,14 @@ bool in_runs(int dtype, const HeadNormArgs &a, bool grad)
 
 size_t head_norm_workspace(int D) { return sizeof(float) * size_t(D) * kMostBlocks; }
 
-cudaError_t launch_head_norm(int dtype, const HeadNormArgs &a, cudaStream_t stream)
+cudaError_t launch_head_norm(int dtype, const HeadNormArgs &a, const AllTurns &turns, cudaStream_t stream)
 {
-    DC_DTYPE_SWITCH(dtype, T, return (launch<T, false>(a, in_runs(dtype, a, false), stream));)
+    DC_DTYPE_SWITCH(dtype, T, return (launch<T, false>(a, turns, in_runs(dtype, a, false), stream));)
 }
 
-cudaError_t launch_head_norm_grad(int dtype, const HeadNormArgs &a, cudaStream_t stream)
+cudaError_t launch_head_norm_grad(int dtype, const HeadNormArgs &a, const AllTurns &turns, cudaStream_t stream)
 {
-    DC_DTYPE_SWITCH(dtype, T, return (launch<T, true>(a, in_runs(dtype, a, true), stream));)
+    DC_DTYPE_SWITCH(dtype, T, return (launch<T, true>(a, turns, in_runs(dtype, a, true), stream));)
 }
 
 }  // namespace dc

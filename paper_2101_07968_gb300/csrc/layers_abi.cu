@@ -162,8 +162,14 @@ HeadNormArgs head_norm_args(const dc_head_norm_cfg *c)
     a.interleaved = c->interleaved != 0;
     a.norm = c->norm != 0;
     a.eps = float(c->eps);
-    rotary_turns(c->base, c->rotary / 2, a.turns, a.turns_below);
     return a;
+}
+
+AllTurns turns_of(const dc_head_norm_cfg *c)
+{
+    AllTurns t = {};
+    rotary_turns(c->base, c->rotary / 2, t.upper, t.below);
+    return t;
 }
 
 dc_status check_attention(const dc_attention_shape *s)
@@ -391,7 +397,7 @@ dc_status dc_head_norm_rotary(const dc_head_norm_cfg *cfg, const void *q, const 
     a.y[0] = q_out;
     a.y[1] = k_out;
     a.positions = positions;
-    return dc::result(dc::launch_head_norm(cfg->dtype, a, stream));
+    return dc::result(dc::launch_head_norm(cfg->dtype, a, dc::turns_of(cfg), stream));
 }
 
 size_t dc_head_norm_rotary_grad_workspace_bytes(const dc_head_norm_cfg *cfg)
@@ -431,7 +437,7 @@ dc_status dc_head_norm_rotary_grad(const dc_head_norm_cfg *cfg, const void *dq_o
     a.dw[1] = dw_k;
     a.positions = positions;
     a.partial = sums ? static_cast<float *>(workspace) : nullptr;
-    return dc::result(dc::launch_head_norm_grad(cfg->dtype, a, stream));
+    return dc::result(dc::launch_head_norm_grad(cfg->dtype, a, dc::turns_of(cfg), stream));
 }
 
 void dc_head_parts_probe(int64_t tokens, int32_t heads, int64_t wanted, int32_t least, int32_t *parts,
