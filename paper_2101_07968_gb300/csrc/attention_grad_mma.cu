@@ -23,9 +23,10 @@
 // The products of one kind run while the warps make the other: S of the next block and dv beside dS,
 // dP of the next block and dk beside P.
 //
-// Measured (one GB300): 32,768 tokens in 14 sequences x 32 heads on 8 x 128, rows 1,091 us, columns 1,380 us; one
-// prompt of 16,384 x 16 x 128 2.45 ms, 1,795 TFLOP/s of the eight products. Tensor cores busy 75-81 % of the time; heads
-// of 64 are bound by the warps: a step of 128 x 128 takes them 1,900 clocks (rows) and 2,500 (columns), the products 1,024.
+// Measured (one GB300): 32,768 tokens in 14 sequences x 32 heads on 8 x 128, rows 1,119 us, columns 1,380 us; one
+// prompt of 16,384 x 16 x 128 2.51 ms, 1,752 TFLOP/s of the eight products. Tensor cores busy 75-81 % of the time; heads
+// of 64 are bound by the warps: a step of 128 x 128 takes them 1,900 clocks (rows) and 2,500 (columns; halves 2,700), the
+// products 1,024.
 //
 // Rounding: P and dS are rounded to the operands' type for the tensor cores, half a step of each
 // term. Halves have few exponents: P, at most 1, is held 2^14 times larger, and dS in a power of

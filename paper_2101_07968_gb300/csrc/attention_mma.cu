@@ -16,8 +16,8 @@
 //   warp 15         looks up the items ahead of the others: the list is in memory, a thousand clocks away
 // A launch has 128 registers a thread; the softmax's warps take more of them from the others.
 //
-// Measured (one GB300): one prompt of 16,384 tokens x 16 heads x 128 684 us, 1,608 TFLOP/s (library products of one
-// matrix 1,859); x 64 565 us; 8 sequences of 2,048 x 32 heads on 8 x 128 277 us. Tensor cores busy 68 % of the time; a tile's
+// Measured (one GB300): one prompt of 16,384 tokens x 16 heads x 128 688 us, 1,598 TFLOP/s (library products of one
+// matrix 1,859); x 64 572 us; 8 sequences of 2,048 x 32 heads on 8 x 128 265 us. Tensor cores busy 69 % of the time; a tile's
 // block takes its softmax's 1,650 clocks and 1,390 until the next scores are there, of which the products are 1,024.
 // Bound by that chain, and by shared memory: a product of scores reads two operands of 4 KB in its 64 clocks.
 //

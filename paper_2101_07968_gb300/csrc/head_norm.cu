@@ -16,8 +16,8 @@
 // their shares, so that a thread holds one weight and its gradient; a group takes a token's heads
 // in turn with the angles in registers. What it takes next comes by asynchronous copies, each lane
 // its own runs, several chunks ahead: loads to registers kept too few bytes on their way
-// (32,768 tokens x 40 heads x 128, gradient: 419 us at 25 % occupancy and 31 % of the issue slots). Now 170 us, 5.9 TB/s,
-// and 120 us forward, 5.5 TB/s.
+// (32,768 tokens x 40 heads x 128, gradient: 419 us at 25 % occupancy and 31 % of the issue slots). Now 172 us, 5.8 TB/s,
+// and 121 us forward, 5.5 TB/s; floats 319 us, 6.3 TB/s, and 219 us, 6.1 TB/s.
 #include <type_traits>
 
 #include "layers.cuh"
