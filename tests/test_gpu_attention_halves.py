@@ -163,3 +163,58 @@ def test_gradients_of_zeros(ly, zero):  # noqa: F811
     y, got = gradients(ly, q, k, v, dy, o)
     assert not got["dq"].any() and not got["dk"].any()
     assert zero == "v" or not got["dv"].any()
+
+
+def test_captured(ly):  # noqa: F811
+    """The gradient's powers of two follow the values of a replay, and the lengths."""
+    o, q, k, v, dy = small()
+    o = offs(*o)
+    y, lse = ly.attention(q, k, v, o)
+    ly.attention_grad(dy, q, k, v, y, lse, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, lse = ly.attention(q, k, v, o)
+        out = ly.attention_grad(dy, q, k, v, y, lse, o)
+    for lengths, by in ((None, 1.0), ((500, 300, 200), 3e4), ((1, 2, 1000), 1e-7)):
+        if lengths:
+            o.copy_(offs(*packed(*lengths)))
+        dy.copy_((dy.float() * by).clamp(-6e4, 6e4))
+        graph.replay()
+        want_y, want_lse = ly.attention(q, k, v, o)
+        want = ly.attention_grad(dy, q, k, v, want_y, want_lse, o)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want_y) and all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("H,G", [(16, 1), (7, 1)])
+def test_large_values_of_another_sequence_in_parts(ly, H, G):  # noqa: F811
+    """The same where a group's heads are dealt to several blocks."""
+    o, D = packed(200, 130), 64
+    q, k, v, dy = operands(29, o[-1], H, G, D, HF)
+    dy = dy * 1e-3
+    _, want = gradients(ly, q, k, v, dy, o)
+    v[200:], dy[200:] = 6e4, 6e4
+    _, got = gradients(ly, q, k, v, dy, o)
+    assert all(torch.equal(got[n][:200], want[n][:200]) for n in got)
+
+
+def test_two_streams_at_once(ly):  # noqa: F811
+    """Two gradients on two streams, their kernels mixed."""
+    o, q, k, v, dy = small(128)
+    y, want = gradients(ly, q, k, v, dy, o)
+    lse = ly.attention(q, k, v, offs(*o))[1]
+    other = (dy.float() * 1e4).half()
+    want2 = ly.attention_grad(other, q, k, v, y, lse, offs(*o))
+    at = offs(*o)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(10):
+        for i, d in enumerate((dy, other)):
+            got[i].append(ly.attention_grad(d, q, k, v, y, lse, at, stream=streams[i]))
+    torch.cuda.synchronize()
+    for r in got[0]:
+        assert all(torch.equal(a, want[n]) for a, n in zip(r, ("dq", "dk", "dv")))
+    for r in got[1]:
+        assert all(torch.equal(a, b) for a, b in zip(r, want2))
